@@ -165,7 +165,7 @@ XSM_API xsm_status xsm_generate_host(xsm_ctx *ctx, int batch, const void *h_cond
 /* Ends the context (waits for its stream); weights and workspace go back to the caller. */
 XSM_API xsm_status xsm_destroy(xsm_ctx *ctx);
 
-/* Text of the last error of this context (or of the last failed xsm_create when ctx is NULL). */
+/* Text of the last error of this context (or, when ctx is NULL, of the last failed call of this thread that had no context). */
 XSM_API const char *xsm_last_error(const xsm_ctx *ctx);
 
 /* Number of kernels this context has launched so far. */
@@ -228,6 +228,103 @@ XSM_API int xsm_debug_plan(const xsm_model_config *cfg, int batch, int prompt_po
 
 /* Launches the stages of a step one after the other, without overlap, instead of as a recorded graph (1) or back (0). */
 XSM_API xsm_status xsm_debug_set_phase_launch(xsm_ctx *ctx, int on);
+
+/* ---- operators on a caller's own paged cache and on a caller's own logits ----
+ *
+ * What a decoder with another block than this library's needs next to it: keys and values appended to pages with the
+ * rotation of the positions, attention of the newest tokens over the pages, log probabilities of given tokens with
+ * their gradient.  No xsm_ctx is involved; the library allocates no device memory and keeps none of the arrays of a call.  Every call
+ * is enqueued on the CUDA stream that is handed to it (cudaStream_t as void*, NULL: the default stream) of the current device, waits for
+ * nothing and may be captured.  Errors are found on the host before the launch; their text is xsm_last_error(NULL) of the same thread.
+ * What only the device knows (page numbers, lengths, tokens) is bounded there: see each call.  Element types: */
+typedef enum { XSM_F32 = 0, XSM_BF16 = 1, XSM_F16 = 2 } xsm_dtype;
+
+/* Pools of keys and of values, DEVICE [n_pages][n_kv_heads][page_size][d_head] with strides in elements (the elements of a row are
+ * neighbours; [n_pages][page_size][n_kv_heads][d_head] is the same with other strides).  Position p of a sequence is row p mod page_size
+ * of page block_table[sequence][p / page_size].  d_head 32, 64, 96, 128 or 256, page_size a multiple of 16, pools 16-byte aligned, strides
+ * multiples of 16 bytes. */
+typedef struct {
+    int64_t page_stride, head_stride, row_stride;
+    int32_t n_pages, n_kv_heads, page_size, d_head, dtype;
+} xsm_kv_config;
+
+typedef struct xsm_kv xsm_kv;      /* HOST description of two pools; borrows them until xsm_kv_destroy */
+XSM_API xsm_status xsm_kv_create(const xsm_kv_config *cfg, void *d_k, void *d_v, xsm_kv **out);
+XSM_API xsm_status xsm_kv_destroy(xsm_kv *kv);
+
+/* Appends m new tokens to each of `batch` sequences: token j of sequence b goes to position starts[b] + j, if j < counts[b].  Keys, and
+ * queries where there are any, are rotated by their position before: pair i of the first rope_dims elements of a head, (i, i + rope_dims/2)
+ * or with `interleaved` (2i, 2i + 1), by the angle whose cosine and sine are rope[position][i]; the other elements pass.  Values
+ * pass.  Arithmetic in fp32, rounded once to the pool's type (fp16: beyond +-65504 stored as +-65504) and to in_dtype for q_out.
+ * A token without a place (a position below 0 or beyond the table's or, where there is one, the rope's last; a page number outside the pool) is not
+ * written; the row of q_out of a token that is not to be appended (j >= counts[b]), or whose position the rope does not have, is zero.
+ * q, k, v, q_out: DEVICE, strides in elements of sequence, token, head; neighbouring elements of a head.  q_out may be q. */
+typedef struct {
+    const void *q, *k, *v;                /* in_dtype [batch][m][n_heads or n_kv_heads][d_head]; q may be NULL */
+    void *q_out;                          /* in_dtype [batch][m][n_heads][d_head] */
+    const int32_t *block_table;           /* DEVICE [batch][max_pages] */
+    const int32_t *starts, *counts;       /* DEVICE [batch]; counts may be NULL: m each */
+    const float *rope;                    /* DEVICE [rope_positions][rope_dims/2][2] cosine, sine; NULL: no rotation */
+    int64_t q_stride[3], k_stride[3], v_stride[3], q_out_stride[3], table_stride;
+    int32_t batch, m, n_heads, in_dtype, max_pages, rope_positions, rope_dims, interleaved;
+} xsm_kv_append_args;
+XSM_API xsm_status xsm_kv_append(const xsm_kv *kv, const xsm_kv_append_args *a, void *cuda_stream);
+
+/* Attention of the m newest tokens of each sequence (1 to 16) over its pages.  Query j of sequence b, of n_b = counts[b] (NULL: m), sees the
+ * positions t < lengths[b] and, with `causal`, t <= p = lengths[b] - n_b + j, with `window` > 0 also t > p - window.  For every query head,
+ * which reads key head (head / (n_heads / n_kv_heads)):  out = sum_t softmax_t(scale q.k_t) v_t,  lse = log sum_t exp(scale q.k_t).
+ * Where nothing is visible, and for j >= n_b, out is zero and lse -infinity.  What unseen positions hold does not matter, infinities and
+ * NaN included.  Lengths beyond the table's end there; pages whose number lies outside the pool are not seen.
+ * Sums and softmax in fp32.  q_dtype is the pool's type, or, over an fp16 pool, any.
+ * workspace: DEVICE, xsm_kv_attend_workspace bytes, 16-byte aligned, zeroed by the caller before its first use; calls that share
+ * one follow each other on one stream. */
+typedef struct {
+    const void *q;                        /* q_dtype [batch][m][n_heads][d_head], strides as above, 16-byte aligned */
+    void *out;                            /* likewise */
+    float *lse;                           /* [batch][m][n_heads], may be NULL */
+    const int32_t *block_table;           /* DEVICE [batch][max_pages] */
+    const int32_t *lengths, *counts;      /* DEVICE [batch]: positions in the cache, the new ones included */
+    void *workspace;
+    int64_t q_stride[3], out_stride[3], table_stride, workspace_bytes;
+    int32_t batch, m, n_heads, q_dtype, max_pages, causal, window;
+    float scale;
+} xsm_kv_attend_args;
+XSM_API size_t xsm_kv_attend_workspace(const xsm_kv *kv, int batch, int m, int n_heads);
+XSM_API xsm_status xsm_kv_attend(const xsm_kv *kv, const xsm_kv_attend_args *a, void *cuda_stream);
+
+/* Log probabilities under softmax(logits / temperature), of `rows` rows of `vocab` logits:
+ *   lse = log sum_j exp(z_j),  logprob = z_token - lse,  entropy = -sum_j p_j log p_j,  z = logits / temperature, p = exp(z - lse),
+ * and the `top` (0 to 32) largest logits, equal ones by the lower index first: top_ids, top_logprobs = z - lse.
+ * A token outside [0, vocab) is no token: its logprob is 0.  Logits of -infinity have no part (p log p = 0); a row that has
+ * nothing else has lse and logprobs of -infinity and entropy 0.  A row with NaN or +infinity has NaN results; NaN ranks below everything. */
+typedef struct {
+    const void *logits;                   /* DEVICE dtype [rows][vocab], row stride in elements */
+    const void *tokens;                   /* DEVICE int32 or int64 [rows], stride in elements */
+    float *logprob, *entropy, *lse;       /* DEVICE [rows] */
+    int32_t *top_ids;                     /* DEVICE [rows][top] */
+    float *top_logprobs;                  /* DEVICE [rows][top] */
+    int64_t row_stride, token_stride;
+    int32_t rows, vocab, dtype, token_bytes, top;
+    float temperature;
+} xsm_logprob_args;
+XSM_API xsm_status xsm_token_logprobs(const xsm_logprob_args *a, void *cuda_stream);
+
+/* The gradient of sum_rows (g logprob + g_entropy entropy + g_lse lse + sum_i g_top_i top_logprob_i) by the logits, in their type:
+ *   d_j = ([j = token] g + sum_i [j = top_ids_i] g_top_i - p_j (g + sum_i g_top_i - g_lse) - g_entropy p_j (log p_j + entropy)) / temperature,
+ * from lse, entropy and top_ids of the call above.  g counts only where there is a token.  Rows with an lse of -infinity have gradient 0.
+ * d_logits may be logits. */
+typedef struct {
+    const void *logits, *tokens;          /* as above */
+    const float *lse, *entropy;           /* DEVICE [rows]; entropy may be NULL without g_entropy */
+    const int32_t *top_ids;               /* DEVICE [rows][top]; NULL with top 0 */
+    const float *g_logprob, *g_entropy, *g_lse;      /* DEVICE [rows], strides in elements; each may be NULL */
+    const float *g_top;                   /* DEVICE [rows][top], may be NULL */
+    void *d_logits;                       /* DEVICE dtype [rows][vocab] */
+    int64_t row_stride, token_stride, g_logprob_stride, g_entropy_stride, g_lse_stride, d_row_stride;
+    int32_t rows, vocab, dtype, token_bytes, top;
+    float temperature;
+} xsm_logprob_grad_args;
+XSM_API xsm_status xsm_token_logprobs_grad(const xsm_logprob_grad_args *a, void *cuda_stream);
 
 #ifdef __cplusplus
 }

@@ -23,7 +23,8 @@ EXPORTS = [
     "xsm_generate_host", "xsm_destroy", "xsm_last_error", "xsm_kernel_launches", "xsm_debug_get_logits",
     "xsm_debug_get_kv", "xsm_debug_set_drafts", "xsm_debug_get_state", "xsm_debug_set_phase_launch",
     "xsm_debug_trace_step", "xsm_spec_step_static", "xsm_debug_set_wait_limits", "xsm_debug_launch_stage",
-    "xsm_debug_set_script", "xsm_debug_plan",
+    "xsm_debug_set_script", "xsm_debug_plan", "xsm_kv_create", "xsm_kv_destroy", "xsm_kv_append", "xsm_kv_attend_workspace",
+    "xsm_kv_attend", "xsm_token_logprobs", "xsm_token_logprobs_grad",
 ]
 
 
@@ -43,6 +44,11 @@ class ModelConfig(C.Structure):
 class DecodeConfig(C.Structure):
     _fields_ = [("verify_mode", C.c_int), ("k_accept", C.c_int), ("delta", C.c_float), ("sample_mode", C.c_int),
                 ("k_sample", C.c_int), ("temperature", C.c_float), ("seed", C.c_uint64)]
+
+
+class KvConfig(C.Structure):
+    _fields_ = [(n, C.c_int64) for n in ("page_stride", "head_stride", "row_stride")] + [
+        (n, C.c_int32) for n in ("n_pages", "n_kv_heads", "page_size", "d_head", "dtype")]
 
 
 class Stats(C.Structure):
@@ -90,6 +96,14 @@ def load(path: str | None = None):
     L.xsm_debug_plan.argtypes = [C.POINTER(ModelConfig), C.c_int, C.c_int, C.c_int, vp, vp, C.c_int]
     L.xsm_debug_launch_stage.argtypes = [vp, C.c_int]
     L.xsm_debug_trace_step.argtypes = [vp, vp, C.c_size_t, C.POINTER(C.c_int), C.POINTER(C.c_int)]
+    L.xsm_kv_create.argtypes = [C.POINTER(KvConfig), vp, vp, C.POINTER(vp)]
+    L.xsm_kv_destroy.argtypes = [vp]
+    L.xsm_kv_append.argtypes = [vp, vp, vp]
+    L.xsm_kv_attend.argtypes = [vp, vp, vp]
+    L.xsm_kv_attend_workspace.restype = C.c_size_t
+    L.xsm_kv_attend_workspace.argtypes = [vp, C.c_int, C.c_int, C.c_int]
+    L.xsm_token_logprobs.argtypes = [vp, vp]
+    L.xsm_token_logprobs_grad.argtypes = [vp, vp]
     if path is None:
         _lib = L
     return L

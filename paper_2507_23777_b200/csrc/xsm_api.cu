@@ -1,6 +1,7 @@
 // Host side of the C ABI declared in include/xsm.h: argument checks, workspace layout, requests.  No device memory is allocated here; everything lives in the caller's workspace.
 #include "../../include/xsm.h"
 #include "xsm_host.h"
+#include "xsm_ops.h"
 
 #include <limits.h>
 #include <math.h>
@@ -284,6 +285,14 @@ xsm_status copy_step(xsm_ctx *ctx, int32_t *d_new_tokens, int32_t *d_n_new) {
 }
 
 }  // namespace
+
+xsm_status xsm::op_failed(xsm_status st, const char *msg) noexcept {
+    try {
+        g_create_error = msg;
+    } catch (...) {            // no memory for the text: the status stands alone
+    }
+    return st;
+}
 
 extern "C" {
 

@@ -1,0 +1,172 @@
+// Pools of keys and values of a caller (xsm_kv), and new tokens appended to them: keys and queries rotated by their position on
+// the way.
+#include "xsm_ops.h"
+
+#include <new>
+
+namespace xsm {
+
+struct AppendArgs {
+    const void *q, *k, *v;
+    void *q_out;
+    const int *starts, *counts;
+    const float2 *rope;
+    long long qs[3], ks[3], vs[3], os[3];       // strides of sequence, token, head
+    int m, heads, d, rope_n, rot, interleaved;
+};
+
+template <typename T, int N> struct __align__(sizeof(T) * N > 16 ? 16 : sizeof(T) * N) Vec { T e[N]; };
+
+template <typename T, int N> __device__ __forceinline__ void load_f(const T *p, float (&x)[N]) {
+    const Vec<T, N> v = *reinterpret_cast<const Vec<T, N> *>(p);
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] = to_f(v.e[i]);
+}
+template <bool kPool, typename T, int N> __device__ __forceinline__ void store_f(T *p, const float (&x)[N]) {
+    Vec<T, N> v;
+#pragma unroll
+    for (int i = 0; i < N; ++i) v.e[i] = kPool ? to_stored<T>(x[i]) : rounded<T>(x[i]);
+    *reinterpret_cast<Vec<T, N> *>(p) = v;
+}
+
+// A block for every token; a thread takes N pairs of elements of a head at a time (N = 8: whole 16-byte pieces; N = 1 where the rotated
+// part or the alignment does not allow that).  Items of a token: heads of q, of k, of v, d / 2N items each, the rotated ones first.
+template <typename TI, typename TC, int N>
+__global__ void __launch_bounds__(256) append_kernel(const __grid_constant__ AppendArgs A, const __grid_constant__ Pages P) {
+    const int b = blockIdx.x / A.m, j = blockIdx.x - b * A.m;
+    const int per_head = A.d / (2 * N), rotated = A.rot / (2 * N), n = (A.heads + 2 * P.kv_heads) * per_head;
+    const bool real = A.counts == nullptr || j < A.counts[b];
+    const long long pos = (long long)A.starts[b] + j;
+    const bool has_angle = A.rope == nullptr || (pos >= 0 && pos < A.rope_n);
+    long long place = -1;                        // of the row in head 0, in elements
+    if (real && has_angle && pos >= 0 && pos / P.size < P.max_pages) {
+        const int page = P.table[b * P.table_ld + pos / P.size];
+        if (page >= 0 && page < P.n_pages) place = page * P.page + (pos % P.size) * P.row;
+    }
+    for (int it = threadIdx.x; it < n; it += blockDim.x) {
+        const int slot = it / per_head, c = it - slot * per_head;
+        const bool is_q = slot < A.heads, is_v = slot >= A.heads + P.kv_heads;
+        const int head = is_q ? slot : is_v ? slot - A.heads - P.kv_heads : slot - A.heads;
+        const bool turn = !is_v && c < rotated;
+        // the two runs of N elements that this thread takes
+        const int e0 = turn && !A.interleaved ? c * N : c * 2 * N, e1 = turn && !A.interleaved ? e0 + A.rot / 2 : e0 + N;
+        if (!is_q && place < 0) continue;
+        const long long *s = is_q ? A.qs : is_v ? A.vs : A.ks;
+        const TI *src = reinterpret_cast<const TI *>(is_q ? A.q : is_v ? A.v : A.k) + b * s[0] + j * s[1] + head * s[2];
+        float x[N], y[N];
+        load_f<TI, N>(src + e0, x);
+        load_f<TI, N>(src + e1, y);
+        if (turn && real && has_angle) {
+            const float2 *cs = A.rope + pos * (A.rot / 2) + c * N;
+            if (A.interleaved) {
+#pragma unroll
+                for (int i = 0; i < N; i += 2) {
+                    if (N == 1) {
+                        const float2 t = cs[0];
+                        const float u = x[0] * t.x - y[0] * t.y, w = x[0] * t.y + y[0] * t.x;
+                        x[0] = u; y[0] = w;
+                    } else {
+                        const float2 t = cs[i / 2], r = cs[N / 2 + i / 2];
+                        float u = x[i] * t.x - x[(i + 1) % N] * t.y, w = x[i] * t.y + x[(i + 1) % N] * t.x;
+                        x[i] = u; x[(i + 1) % N] = w;
+                        u = y[i] * r.x - y[(i + 1) % N] * r.y; w = y[i] * r.y + y[(i + 1) % N] * r.x;
+                        y[i] = u; y[(i + 1) % N] = w;
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    const float2 t = cs[i];
+                    const float u = x[i] * t.x - y[i] * t.y, w = x[i] * t.y + y[i] * t.x;
+                    x[i] = u; y[i] = w;
+                }
+            }
+        }
+        if (is_q) {
+            if (!real || !has_angle) {
+#pragma unroll
+                for (int i = 0; i < N; ++i) x[i] = y[i] = 0.f;
+            }
+            TI *dst = reinterpret_cast<TI *>(A.q_out) + b * A.os[0] + j * A.os[1] + head * A.os[2];
+            store_f<false>(dst + e0, x);
+            store_f<false>(dst + e1, y);
+        } else {
+            TC *dst = reinterpret_cast<TC *>(is_v ? P.v : P.k) + place + head * P.head;
+            store_f<true>(dst + e0, x);
+            store_f<true>(dst + e1, y);
+        }
+    }
+}
+
+static bool aligned(const void *p, const int64_t (&s)[3], int es) {
+    return ((uintptr_t)p | (uintptr_t)(s[0] * es) | (uintptr_t)(s[1] * es) | (uintptr_t)(s[2] * es)) % 16 == 0;
+}
+
+}  // namespace xsm
+
+using namespace xsm;
+
+xsm_status xsm_kv_create(const xsm_kv_config *cfg, void *d_k, void *d_v, xsm_kv **out) {
+    if (!cfg || !d_k || !d_v || !out) return op_failed(XSM_ERR_INVALID_ARG, "null argument");
+    const xsm_kv_config &c = *cfg;
+    if (!is_dtype(c.dtype)) return op_failed(XSM_ERR_INVALID_ARG, "dtype must be 0 (fp32), 1 (bf16) or 2 (fp16)");
+    if (c.d_head != 32 && c.d_head != 64 && c.d_head != 96 && c.d_head != 128 && c.d_head != 256)
+        return op_failed(XSM_ERR_INVALID_ARG, "d_head must be 32, 64, 96, 128 or 256");
+    if (c.page_size < 16 || c.page_size % 16) return op_failed(XSM_ERR_INVALID_ARG, "page_size must be a positive multiple of 16");
+    if (c.n_pages < 1 || c.n_kv_heads < 1 || c.n_kv_heads > 1024) return op_failed(XSM_ERR_INVALID_ARG, "n_pages must be positive and n_kv_heads in [1, 1024]");
+    const int per16 = 16 / element_size(c.dtype);
+    if (c.row_stride < c.d_head || c.head_stride < c.d_head || c.page_stride < c.d_head || c.row_stride % per16 || c.head_stride % per16 || c.page_stride % per16)
+        return op_failed(XSM_ERR_INVALID_ARG, "strides of the pools must be multiples of 16 bytes and no shorter than a row");
+    if (((uintptr_t)d_k | (uintptr_t)d_v) % 16) return op_failed(XSM_ERR_INVALID_ARG, "the pools must be 16-byte aligned");
+    xsm_kv *kv = new (std::nothrow) xsm_kv;
+    if (!kv) return op_failed(XSM_ERR_CAPACITY, "out of host memory");
+    kv->cfg = c;
+    kv->k = d_k;
+    kv->v = d_v;
+    *out = kv;
+    return XSM_OK;
+}
+
+xsm_status xsm_kv_destroy(xsm_kv *kv) {
+    if (!kv) return op_failed(XSM_ERR_INVALID_ARG, "null argument");
+    delete kv;
+    return XSM_OK;
+}
+
+xsm_status xsm_kv_append(const xsm_kv *kv, const xsm_kv_append_args *a, void *cuda_stream) {
+    if (!kv || !a) return op_failed(XSM_ERR_INVALID_ARG, "null argument");
+    if (a->batch < 0 || a->m < 0 || a->n_heads < 0 || a->max_pages < 0) return op_failed(XSM_ERR_INVALID_ARG, "batch, m, n_heads and max_pages must not be negative");
+    if (a->n_heads > 4096) return op_failed(XSM_ERR_INVALID_ARG, "n_heads must not exceed 4096");
+    if (!is_dtype(a->in_dtype)) return op_failed(XSM_ERR_INVALID_ARG, "in_dtype must be 0 (fp32), 1 (bf16) or 2 (fp16)");
+    if (a->rope && (a->rope_dims < 2 || a->rope_dims % 2 || a->rope_dims > kv->cfg.d_head || a->rope_positions < 1))
+        return op_failed(XSM_ERR_INVALID_ARG, "rope_dims must be even and in [2, d_head], rope_positions positive");
+    const long long tokens = (long long)a->batch * a->m;
+    if (tokens == 0) return XSM_OK;
+    if (tokens > 0x7fffffff) return op_failed(XSM_ERR_INVALID_ARG, "more than 2^31 - 1 tokens");
+    if (!a->k || !a->v || !a->block_table || !a->starts) return op_failed(XSM_ERR_INVALID_ARG, "null argument");
+    if (a->n_heads && (!a->q || !a->q_out)) return op_failed(XSM_ERR_INVALID_ARG, "n_heads without q or q_out");
+    AppendArgs A;
+    A.q = a->q; A.k = a->k; A.v = a->v; A.q_out = a->q_out;
+    A.starts = a->starts; A.counts = a->counts;
+    A.rope = reinterpret_cast<const float2 *>(a->rope);
+    for (int i = 0; i < 3; ++i) { A.qs[i] = a->q_stride[i]; A.ks[i] = a->k_stride[i]; A.vs[i] = a->v_stride[i]; A.os[i] = a->q_out_stride[i]; }
+    A.m = a->m; A.heads = a->n_heads; A.d = kv->cfg.d_head; A.rope_n = a->rope_positions;
+    A.rot = a->rope ? a->rope_dims : 0;
+    A.interleaved = a->interleaved != 0;
+    const Pages P = pages_of(*kv, a->block_table, a->table_stride, a->max_pages);
+    const int es = element_size(a->in_dtype);
+    if (((uintptr_t)a->rope) % 8) return op_failed(XSM_ERR_INVALID_ARG, "rope must be 8-byte aligned");
+    const bool wide = A.rot % 16 == 0 && aligned(a->k, a->k_stride, es) && aligned(a->v, a->v_stride, es) &&
+                      (a->n_heads == 0 || (aligned(a->q, a->q_stride, es) && aligned(a->q_out, a->q_out_stride, es)));
+    const int items = (A.heads + 2 * P.kv_heads) * (A.d / (wide ? 16 : 2));
+    const int threads = items >= 256 ? 256 : (items + 31) / 32 * 32;
+    with_dtype(a->in_dtype, [&](auto in) {
+        with_dtype(kv->cfg.dtype, [&](auto stored) {
+            using TI = decltype(in);
+            using TC = decltype(stored);
+            if (wide) append_kernel<TI, TC, 8><<<(unsigned)tokens, threads, 0, (cudaStream_t)cuda_stream>>>(A, P);
+            else append_kernel<TI, TC, 1><<<(unsigned)tokens, threads, 0, (cudaStream_t)cuda_stream>>>(A, P);
+        });
+    });
+    return launched(cudaGetLastError());
+}
