@@ -2,6 +2,8 @@
 // the way.
 #include "xsm_ops.h"
 
+#include <cuda.h>
+
 #include <new>
 
 namespace xsm {
@@ -98,6 +100,22 @@ __global__ void __launch_bounds__(256) append_kernel(const __grid_constant__ App
     }
 }
 
+typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
+                                  const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                  CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+// tensor map of a pool: elements, rows of a page, heads, pages
+static bool pool_map(EncodeTiledFn encode, TensorMap *out, const xsm_kv_config &c, void *pool, int box_rows) {
+    const int es = element_size(c.dtype), box_w = es == 4 ? 32 : c.d_head % 64 == 0 ? 64 : 32;
+    cuuint64_t dims[4] = {(cuuint64_t)c.d_head, (cuuint64_t)c.page_size, (cuuint64_t)c.n_kv_heads, (cuuint64_t)c.n_pages};
+    cuuint64_t strides[3] = {(cuuint64_t)c.row_stride * es, (cuuint64_t)c.head_stride * es, (cuuint64_t)c.page_stride * es};
+    cuuint32_t box[4] = {(cuuint32_t)box_w, (cuuint32_t)box_rows, 1, 1}, estr[4] = {1, 1, 1, 1};
+    return encode(reinterpret_cast<CUtensorMap *>(out),
+                  c.dtype == XSM_F32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : c.dtype == XSM_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16,
+                  4, pool, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, box_w * es == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
+                  CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 static bool aligned(const void *p, const int64_t (&s)[3], int es) {
     return ((uintptr_t)p | (uintptr_t)(s[0] * es) | (uintptr_t)(s[1] * es) | (uintptr_t)(s[2] * es)) % 16 == 0;
 }
@@ -123,6 +141,22 @@ xsm_status xsm_kv_create(const xsm_kv_config *cfg, void *d_k, void *d_v, xsm_kv 
     kv->cfg = c;
     kv->k = d_k;
     kv->v = d_v;
+    kv->box_rows = c.page_size % 32 ? 16 : 32;
+    int dev = 0;
+    void *encode = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&kv->sms, cudaDevAttrMultiProcessorCount, dev);
+    if (e == cudaSuccess) e = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &encode, cudaEnableDefault, &q);
+    if (e != cudaSuccess) {
+        delete kv;
+        return launched(e);
+    }
+    if (q != cudaDriverEntryPointSuccess || !pool_map((EncodeTiledFn)encode, &kv->k_map, c, d_k, kv->box_rows) ||
+        !pool_map((EncodeTiledFn)encode, &kv->v_map, c, d_v, kv->box_rows)) {
+        delete kv;
+        return op_failed(XSM_ERR_CUDA, "the tensor maps of the pools could not be made");
+    }
     *out = kv;
     return XSM_OK;
 }

@@ -1,67 +1,710 @@
 // Attention of the newest tokens of each sequence over a caller's paged pools (xsm_kv).
+//
+// A unit is a sequence, a key head and up to 64 of the query rows (tokens x heads of the group) that read it.  What a unit has to do is
+// counted in granules of 256 positions, and all granules of the call, in one row, are cut into equal runs, one for every CTA of a grid
+// that fills the chip once: lengths are known on the device alone, and neither short nor long sequences leave SMs without work.
+// A unit that a cut goes through leaves partial results (maximum, sum, unnormalised output) in the workspace; the CTA that is the last
+// to arrive at the unit's counter adds them up in the order of the positions, so results do not depend on which one that is.
+//
+// In a CTA a producer warp streams stages of 32 positions (boxes of the keys' and values' tensor maps; page numbers looked up 32
+// stages at a time) through a ring in shared memory.  Eight warps attend: row tiles of sixteen rows (one, two or four of them) times as many
+// groups as that leaves, which take the stages in turn.  A warp keeps its rows' output and running maximum in registers:
+// S = Q K^T, online softmax, O += P V with mma.sync; 16-bit weights enter as the sum of a rounded part and its remainder where
+// the output is to be as exact as the type allows, fp32 operands as parts of eleven bits whose three large products are added up.
 #include "xsm_ops.h"
 
 #include <limits.h>
 #include <math.h>
+#include <string.h>
+
+#include <type_traits>
 
 namespace xsm {
+
+constexpr int kStage = 32;            // positions of a stage
+constexpr int kGranule = 8;           // stages that are never cut apart
+constexpr int kAttendWarps = 8;
+constexpr int kRing = 16;             // most stages in shared memory
+// Workspace: status word and counters, which every call leaves at zero, in a place that does not depend on the call; then the partial results.
+constexpr int kHeadBytes = 4096, kMaxGrid = kHeadBytes / 4 - 4;
 
 struct AttendArgs {
     const void *q;
     void *out;
     float *lse;
-    const int *lengths, *counts;
-    long long qs[3], os[3];
-    int m, heads, group, causal, window;
-    float scale;
+    const int *lengths, *counts, *table;
+    int *counters, *status;           // a counter for every CTA, used for the unit that the next CTA shares with it; status word of the waits
+    float *partial;                   // two places for every CTA
+    long long qs[3], os[3], table_ld;
+    int batch, m, heads, group, kv_heads;
+    int rt, row_groups, n_rows;       // row tiles of a unit, units that share a key head, query rows of a key head
+    int causal, window, page, max_pages, n_pages, box_rows;
+    int ring, turns;                  // stages in shared memory, groups of warps that take them in turn: every place of the ring is one group's
+    float c;                          // scale * log2(e)
 };
 
-// One block for every query row of every head: its four warps take keys in turn, a lane holds every 32nd element of the row; the online
-// softmax of a warp is joined with the others' at the end.
-template <typename TQ, typename TC, int DH>
-__global__ void __launch_bounds__(128) attend_kernel(const __grid_constant__ AttendArgs A, const __grid_constant__ Pages P) {
-    constexpr int E = DH / 32;
-    __shared__ float s_o[4][DH], s_m[4], s_l[4];
-    const int h = blockIdx.x % A.heads, j = (blockIdx.x / A.heads) % A.m, b = blockIdx.x / (A.heads * A.m);
+template <typename T, int DH> struct Shape {
+    static constexpr int es = sizeof(T), box_w = es == 4 ? 32 : DH % 64 == 0 ? 64 : 32;      // elements of a box's row
+    static constexpr int rb = box_w * es, boxes = DH / box_w, box_bytes = kStage * rb;
+    static constexpr int half = boxes * box_bytes, stage = 2 * half;                          // keys, then values
+    static constexpr int steps = DH * es / 32;                                                // products over 32 bytes of a row
+    static constexpr int ld = DH + 4;                                                         // rows of parked outputs
+    // shared-memory address of 16-byte chunk ch of row r
+    static __device__ __forceinline__ uint32_t at(uint32_t base, int r, int ch) {
+        constexpr int per = rb / 16;
+        const int x = ch % per, s = rb == 128 ? r & 7 : (r >> 1) & 3;
+        return base + (ch / per) * box_bytes + r * rb + ((x ^ s) << 4);
+    }
+};
+__host__ __device__ constexpr int parked_bytes(int dh) { return 4 * 16 * (dh + 4) * 4 + 4 * 16 * 2 * 4; }
+// query operands of a row tile, in the order in which the lanes take them
+__host__ __device__ constexpr int query_bytes(int dh, int es, bool split) { return dh * es / 32 * 512 * (split ? 2 : 1); }
+
+// What a sequence has to do.  Row j of its nq queries sees [begin_j, end_j): end_j = end - nq + 1 + j (all: end), begin_j = end_j - window.
+struct Span {
+    int base, end, first_end, first_begin, last_begin, nq, stages;
+};
+__device__ __forceinline__ Span span_of(const AttendArgs &A, int b) {
+    Span s;
+    const long long room = (long long)A.max_pages * A.page;
+    int len = A.lengths[b];
+    len = len > room ? (int)room : len < 0 ? 0 : len;
+    len = min(len, INT_MAX - 2 * kStage);
+    s.nq = A.counts ? max(0, min(A.counts[b], A.m)) : A.m;
+    s.end = s.nq == 0 ? 0 : len;
+    s.first_end = A.causal ? s.end - s.nq + 1 : s.end;
+    s.first_begin = A.window > 0 ? max(0, s.first_end - A.window) : 0;
+    s.last_begin = A.window > 0 ? max(0, s.end - A.window) : 0;
+    s.base = s.first_begin / A.box_rows * A.box_rows;
+    s.stages = max(1, (s.end - s.base + kStage - 1) / kStage);
+    return s;
+}
+__device__ __forceinline__ int granules(const Span &s) { return (s.stages + kGranule - 1) / kGranule; }
+
+// The run of granules of this CTA, and where it starts.  Every warp works it out for itself.
+struct Run {
+    long long at, end, total, before;       // granules; before: those of the sequences before b
+    int b, ctas;                             // CTAs that have work
+};
+__device__ __forceinline__ long long warp_sum_ll(long long v) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
+}
+__device__ __forceinline__ Run run_of(const AttendArgs &A, int units) {
+    const int lane = threadIdx.x & 31;
+    long long sum = 0;
+    int first = 0;                           // of the first 32 sequences, which most calls end with
+    for (int b = lane; b < A.batch; b += 32) {
+        const int g = granules(span_of(A, b));
+        if (b == lane) first = g;
+        sum += g;
+    }
+    Run r;
+    r.total = warp_sum_ll(sum) * units;
+    r.ctas = (int)min((long long)gridDim.x, r.total);        // every one of them has a granule at least
+    if ((int)blockIdx.x >= r.ctas) {
+        r.at = r.end = r.before = 0; r.b = 0;
+        return r;
+    }
+    r.at = r.total * blockIdx.x / r.ctas;
+    r.end = r.total * (blockIdx.x + 1) / r.ctas;
+    long long before = 0;
+    for (int b0 = 0;; b0 += 32) {
+        const int b = b0 + lane, mine = b >= A.batch ? 0 : b0 == 0 ? first : granules(span_of(A, b));
+        long long up = mine;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const long long v = __shfl_up_sync(0xffffffffu, up, o);
+            if (lane >= o) up += v;
+        }
+        const unsigned past = __ballot_sync(0xffffffffu, b < A.batch && (before + up) * units > r.at);
+        if (past) {
+            const int l = __ffs(past) - 1;
+            r.b = b0 + l;
+            r.before = (before + __shfl_sync(0xffffffffu, up - mine, l)) * units;
+            return r;
+        }
+        before += __shfl_sync(0xffffffffu, up, 31);
+        if (b0 + 32 >= A.batch) break;
+    }
+    r.at = r.end = r.before = 0; r.b = 0;          // (not reached: the granules of all sequences are `total`)
+    return r;
+}
+
+// The part of a unit that a CTA does.
+struct Segment {
+    int unit, stage0, stage1;                // of the sequence; stages
+    long long first, last;                   // the whole unit's granules
+    bool whole;
+};
+
+template <typename F> __device__ __forceinline__ void walk(const AttendArgs &A, int units, F &&f) {
+    Run r = run_of(A, units);
+    while (r.at < r.end) {
+        const Span sp = span_of(A, r.b);
+        const int per = granules(sp);
+        const long long behind = r.before + (long long)per * units;
+        while (r.at < r.end && r.at < behind) {
+            Segment s;
+            const long long rel = r.at - r.before;
+            s.unit = (int)(rel / per);
+            const int g0 = (int)(rel - (long long)s.unit * per);
+            const int g1 = (int)min((long long)per, g0 + (r.end - r.at));
+            s.stage0 = g0 * kGranule;
+            s.stage1 = min(sp.stages, g1 * kGranule);
+            s.first = r.before + (long long)s.unit * per;
+            s.last = s.first + per;
+            s.whole = g0 == 0 && g1 == per;
+            f(r.b, sp, s, r);
+            r.at += g1 - g0;
+        }
+        r.before = behind;
+        ++r.b;
+    }
+}
+
+__device__ __forceinline__ void tma_box4(uint32_t dst, const void *tmap, int x, int row, int head, int page, uint32_t bar) {
+    asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
+                 :: "r"(dst), "l"(tmap), "r"(x), "r"(row), "r"(head), "r"(page), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void mma1688_tf32(float (&c)[4], unsigned a0, unsigned a1, unsigned a2, unsigned a3, unsigned b0, unsigned b1) {
+    asm volatile("mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void mma16(float (&c)[4], const uint4 &a, unsigned b0, unsigned b1, __half) { mma16816_f16(c, a.x, a.y, a.z, a.w, b0, b1); }
+__device__ __forceinline__ void mma16(float (&c)[4], const uint4 &a, unsigned b0, unsigned b1, bf16) { mma16816_bf16(c, a.x, a.y, a.z, a.w, b0, b1); }
+
+// x = part + rest: part has the leading eleven bits (a tf32 operand), the rest keeps what a tf32 operand can of the others
+__device__ __forceinline__ unsigned tf32_part(float x) { return __float_as_uint(x) & 0xffffe000u; }
+__device__ __forceinline__ unsigned tf32_rest(float x) { return __float_as_uint(x - __uint_as_float(tf32_part(x))); }
+// (infinities and NaN: the difference of two infinities would be NaN where the product alone is right)
+__device__ __forceinline__ unsigned tf32_rest_of(float x, unsigned part) { return (part & 0x7f800000u) == 0x7f800000u ? 0u : __float_as_uint(x - __uint_as_float(part)); }
+
+// two values as 16-bit operands, first in the low half, and what the rounding took off
+template <typename T> __device__ __forceinline__ unsigned pack2(float a, float b);
+template <> __device__ __forceinline__ unsigned pack2<__half>(float a, float b) {
+    const __half2 h = __floats2half2_rn(a, b);
+    return *reinterpret_cast<const unsigned *>(&h);
+}
+template <> __device__ __forceinline__ unsigned pack2<bf16>(float a, float b) {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const unsigned *>(&h);
+}
+template <typename T> __device__ __forceinline__ unsigned rest2(float a, float b, unsigned p);
+template <> __device__ __forceinline__ unsigned rest2<__half>(float a, float b, unsigned p) {
+    const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&p));
+    return pack2<__half>(a - f.x, b - f.y);
+}
+template <> __device__ __forceinline__ unsigned rest2<bf16>(float a, float b, unsigned p) {
+    return pack2<bf16>(a - __uint_as_float(p << 16), b - __uint_as_float(p & 0xffff0000u));
+}
+// whether one of two 16-bit values (an fp32 value) is infinite or NaN
+template <typename T> __device__ __forceinline__ bool not_finite(unsigned v) {
+    if (std::is_same<T, float>::value) return (v & 0x7f800000u) == 0x7f800000u;
+    const unsigned e = std::is_same<T, bf16>::value ? 0x7f80u : 0x7c00u;
+    return (v & e) == e || (v & (e << 16)) == (e << 16);
+}
+__device__ __forceinline__ unsigned lds32(uint32_t a) {
+    unsigned v;
+    asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v) : "r"(a));
+    return v;
+}
+__device__ __forceinline__ uint4 lds128(uint32_t a) {
+    uint4 v;
+    asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a));
+    return v;
+}
+
+// A warp's sixteen rows: lane 4g + t has rows g and g + 8, columns 8j + 2t and + 1.
+template <int DH> struct RowState {
+    float o[DH / 8][4], m[2], l[2];           // l: this lane's keys only
+};
+
+// bits of the positions base..base+31 inside [begin, end)
+__device__ __forceinline__ unsigned inside(int base, int begin, int end) {
+    const int lo = max(0, begin - base), hi = min(kStage, end - base);
+    if (lo >= hi) return 0u;
+    return (hi == 32 ? ~0u : (1u << hi) - 1u) & ~((1u << lo) - 1u);
+}
+
+// O += P V over the 32 positions of a stage.  kept: positions that take part; the others' values may be anything (kMask: they are
+// read as zeros, so that zero weights do not meet infinities).  kSome: only rows of which `mine` is set get anything.
+template <typename T, int DH, bool kSplit, bool kMask, bool kSome>
+__device__ __forceinline__ void add_values(const float (&p)[4][4], uint32_t v_base, unsigned kept, const bool (&mine)[2], RowState<DH> &st) {
+    using S = Shape<T, DH>;
+    const int lane = threadIdx.x & 31, t = lane & 3, g = lane >> 2;
+    if constexpr (std::is_same<T, float>::value) {
+#pragma unroll
+        for (int nt = 0; nt < 4; ++nt) {
+            const unsigned a0 = tf32_part(p[nt][0]), a1 = tf32_part(p[nt][2]), a2 = tf32_part(p[nt][1]), a3 = tf32_part(p[nt][3]);
+            const unsigned r0 = tf32_rest(p[nt][0]), r1 = tf32_rest(p[nt][2]), r2 = tf32_rest(p[nt][1]), r3 = tf32_rest(p[nt][3]);
+            const int k0 = nt * 8 + 2 * t;
+#pragma unroll
+            for (int j = 0; j < DH / 8; ++j) {
+                unsigned x = lds32(S::at(v_base, k0, 2 * j + (g >> 2)) + (g & 3) * 4), y = lds32(S::at(v_base, k0 + 1, 2 * j + (g >> 2)) + (g & 3) * 4);
+                if (kMask) { x = (kept >> k0) & 1u ? x : 0u; y = (kept >> (k0 + 1)) & 1u ? y : 0u; }
+                const unsigned xh = x & 0xffffe000u, yh = y & 0xffffe000u;
+                const unsigned xl = tf32_rest_of(__uint_as_float(x), xh), yl = tf32_rest_of(__uint_as_float(y), yh);
+                float add[4] = {0.f, 0.f, 0.f, 0.f};
+                float (&o)[4] = kSome ? add : st.o[j];
+                mma1688_tf32(o, r0, r1, r2, r3, xh, yh);
+                mma1688_tf32(o, a0, a1, a2, a3, xl, yl);
+                mma1688_tf32(o, a0, a1, a2, a3, xh, yh);
+                if (kSome) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) if (mine[i >> 1]) st.o[j][i] += add[i];
+                }
+            }
+        }
+    } else {
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk) {
+            const float (&u)[4] = p[2 * kk], (&w)[4] = p[2 * kk + 1];
+            const uint4 a = make_uint4(pack2<T>(u[0], u[1]), pack2<T>(u[2], u[3]), pack2<T>(w[0], w[1]), pack2<T>(w[2], w[3]));
+            uint4 r;
+            if (kSplit) r = make_uint4(rest2<T>(u[0], u[1], a.x), rest2<T>(u[2], u[3], a.y), rest2<T>(w[0], w[1], a.z), rest2<T>(w[2], w[3], a.w));
+            const int row = kk * 16 + (lane & 7) + (((lane >> 3) & 1) << 3);
+            unsigned m0 = ~0u, m1 = ~0u;
+            if (kMask) {
+                const unsigned b0 = kept >> (kk * 16 + 2 * t), b1 = kept >> (kk * 16 + 2 * t + 8);
+                m0 = (b0 & 1u ? 0xffffu : 0u) | (b0 & 2u ? 0xffff0000u : 0u);
+                m1 = (b1 & 1u ? 0xffffu : 0u) | (b1 & 2u ? 0xffff0000u : 0u);
+            }
+#pragma unroll
+            for (int j = 0; j < DH / 8; j += 2) {
+                unsigned v[4];
+                ldmatrix_x4_trans(v, S::at(v_base, row, j + (lane >> 4)));
+                if (kMask) { v[0] &= m0; v[1] &= m1; v[2] &= m0; v[3] &= m1; }
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    float add[4] = {0.f, 0.f, 0.f, 0.f};
+                    float (&o)[4] = kSome ? add : st.o[j + h];
+                    if (kSplit) mma16(o, r, v[2 * h], v[2 * h + 1], T());
+                    mma16(o, a, v[2 * h], v[2 * h + 1], T());
+                    if (kSome) {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) if (mine[i >> 1]) st.o[j + h][i] += add[i];
+                    }
+                }
+            }
+        }
+    }
+}
+
+// whether a position of `some` holds a value that is not finite
+template <typename T, int DH> __device__ __forceinline__ bool odd_values(uint32_t v_base, unsigned some) {
+    using S = Shape<T, DH>;
+    const int lane = threadIdx.x & 31;
+    bool odd = false;
+    for (int r = 0; r < kStage; ++r) {
+        if (!((some >> r) & 1u)) continue;
+        for (int w = lane; w < DH * S::es / 4; w += 32) odd |= not_finite<T>(lds32(S::at(v_base, r, w >> 2) + (w & 3) * 4));
+    }
+    return __any_sync(0xffffffffu, odd);
+}
+
+// What masks a stage for a warp: positions that its two rows see, that any row of the sequence sees, that all of them do.
+struct StageMask {
+    unsigned row[2], any, all, valid;
+};
+
+// One stage for the sixteen rows of a warp.
+template <typename T, int DH, bool kSplitQ, bool kSplitP, bool kMask>
+__device__ __forceinline__ void attend_stage(uint32_t q_base, uint32_t stage, float c, const StageMask &mask, const AttendArgs &A, const Span &sp, int base,
+                                             const int (&token)[2], RowState<DH> &st) {
+    using S = Shape<T, DH>;
+    const int lane = threadIdx.x & 31, t = lane & 3;
+    float s[4][4];
+#pragma unroll
+    for (int nt = 0; nt < 4; ++nt) s[nt][0] = s[nt][1] = s[nt][2] = s[nt][3] = 0.f;
+    const int row = (lane & 7) + ((lane >> 4) << 3);
+#pragma unroll
+    for (int ks = 0; ks < S::steps; ++ks) {
+        const uint4 a = lds128(q_base + ks * 512 + lane * 16);
+        uint4 al;
+        if (kSplitQ || S::es == 4) al = lds128(q_base + (S::steps + ks) * 512 + lane * 16);
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt) {
+            unsigned k[4];
+            ldmatrix_x4(k, S::at(stage, kt * 16 + row, 2 * ks + ((lane >> 3) & 1)));
+            if constexpr (S::es == 4) {
+                unsigned h[4], l[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) { h[i] = k[i] & 0xffffe000u; l[i] = tf32_rest_of(__uint_as_float(k[i]), h[i]); }
+#pragma unroll
+                for (int n = 0; n < 2; ++n) {
+                    mma1688_tf32(s[2 * kt + n], al.x, al.y, al.z, al.w, h[2 * n], h[2 * n + 1]);
+                    mma1688_tf32(s[2 * kt + n], a.x, a.y, a.z, a.w, l[2 * n], l[2 * n + 1]);
+                    mma1688_tf32(s[2 * kt + n], a.x, a.y, a.z, a.w, h[2 * n], h[2 * n + 1]);
+                }
+            } else {
+#pragma unroll
+                for (int n = 0; n < 2; ++n) {
+                    if (kSplitQ) mma16(s[2 * kt + n], al, k[2 * n], k[2 * n + 1], T());
+                    mma16(s[2 * kt + n], a, k[2 * n], k[2 * n + 1], T());
+                }
+            }
+        }
+    }
+    float top[2] = {st.m[0], st.m[1]};
+#pragma unroll
+    for (int nt = 0; nt < 4; ++nt)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            s[nt][i] *= c;
+            if (kMask && !((mask.row[i >> 1] >> (nt * 8 + 2 * t + (i & 1))) & 1u)) s[nt][i] = -INFINITY;
+            top[i >> 1] = fmaxf(top[i >> 1], s[nt][i]);
+        }
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+        top[r] = fmaxf(top[r], __shfl_xor_sync(0xffffffffu, top[r], 1));
+        top[r] = fmaxf(top[r], __shfl_xor_sync(0xffffffffu, top[r], 2));
+    }
+    // nothing seen so far: any finite reference will do, the weights are zero
+    const float ref0 = kMask && top[0] == -INFINITY ? 0.f : top[0], ref1 = kMask && top[1] == -INFINITY ? 0.f : top[1];
+    if (__any_sync(0xffffffffu, top[0] != st.m[0] || top[1] != st.m[1])) {
+        const float f0 = ex2(st.m[0] - ref0), f1 = ex2(st.m[1] - ref1);
+        st.l[0] *= f0; st.l[1] *= f1;
+#pragma unroll
+        for (int j = 0; j < DH / 8; ++j) { st.o[j][0] *= f0; st.o[j][1] *= f0; st.o[j][2] *= f1; st.o[j][3] *= f1; }
+        st.m[0] = top[0]; st.m[1] = top[1];
+    }
+#pragma unroll
+    for (int nt = 0; nt < 4; ++nt) {
+        s[nt][0] = ex2(s[nt][0] - ref0); s[nt][1] = ex2(s[nt][1] - ref0);
+        s[nt][2] = ex2(s[nt][2] - ref1); s[nt][3] = ex2(s[nt][3] - ref1);
+        st.l[0] += s[nt][0] + s[nt][1];
+        st.l[1] += s[nt][2] + s[nt][3];
+    }
+    const uint32_t v_base = stage + S::half;
+    const bool all[2] = {true, true};
+    if (!kMask) {
+        add_values<T, DH, kSplitP, false, false>(s, v_base, ~0u, all, st);
+    } else {
+        const unsigned some = mask.any & ~mask.all;       // positions that some rows see and others do not
+        if (some == 0u || !odd_values<T, DH>(v_base, some)) {
+            add_values<T, DH, kSplitP, true, false>(s, v_base, mask.any, all, st);
+        } else {                                          // one of them holds an infinity or NaN: the rows of one token after the other
+            for (int j = 0; j < sp.nq; ++j) {
+                const int end = A.causal ? sp.first_end + j : sp.end, begin = A.window > 0 ? max(0, end - A.window) : 0;
+                const bool mine[2] = {token[0] == j, token[1] == j};
+                add_values<T, DH, kSplitP, true, true>(s, v_base, inside(base, begin, end) & mask.valid, mine, st);
+            }
+        }
+    }
+}
+
+// the eight attending warps
+__device__ __forceinline__ void bar_attend() { bar_sync<kAttendWarps * 32>(1); }
+
+template <typename TQ> __device__ __forceinline__ void store4(TQ *p, float4 v) {
+    if constexpr (sizeof(TQ) == 4) *reinterpret_cast<float4 *>(p) = v;
+    else *reinterpret_cast<uint2 *>(p) = make_uint2(pack2<TQ>(v.x, v.y), pack2<TQ>(v.z, v.w));
+}
+
+// output of one row's four elements and its lse, from the joined state
+template <typename TQ> __device__ __forceinline__ void finish(const AttendArgs &A, const Span &sp, int b, int unit, int row, int d, float4 o, float m, float l) {
+    const int kvh = unit / A.row_groups, r = (unit % A.row_groups) * A.rt * 16 + row, j = r / A.group, h = kvh * A.group + (r - j * A.group);
+    const bool none = j >= sp.nq || l == 0.f;
+    const float f = none ? 0.f : 1.f / l;
+    TQ *p = reinterpret_cast<TQ *>(A.out) + b * A.os[0] + j * A.os[1] + h * A.os[2] + d;
+    store4<TQ>(p, none ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(o.x * f, o.y * f, o.z * f, o.w * f));
+    if (d == 0 && A.lse) A.lse[((long long)b * A.m + j) * A.heads + h] = none ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
+}
+
+template <typename T, typename TQ, int DH>
+__global__ void __launch_bounds__((kAttendWarps + 1) * 32, 1)
+attend_kernel(const __grid_constant__ TensorMap k_map, const __grid_constant__ TensorMap v_map, const __grid_constant__ AttendArgs A) {
+    using S = Shape<T, DH>;
+    // queries with more bits than the pools' type enter as two parts; so do the weights, unless the output has fewer bits than they
+    constexpr bool kSplitQ = S::es == 2 && sizeof(TQ) == 4, kSplitP = !(std::is_same<T, __half>::value && std::is_same<TQ, bf16>::value);
+    extern __shared__ __align__(1024) unsigned char smem[];
+    __shared__ __align__(8) unsigned long long s_full[kRing], s_empty[kRing];
+    __shared__ int2 s_info[kRing];            // first position of a stage, which halves exist
+    __shared__ int s_last;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int n_q = A.counts ? min(A.counts[b], A.m) : A.m;
-    const long long n = min((long long)A.lengths[b], (long long)P.max_pages * P.size);
-    long long end = j < n_q ? n : 0, begin = 0;
-    if (A.causal) end = min(end, n - n_q + j + 1);
-    if (A.causal && A.window > 0) begin = max(0LL, end - A.window);
-    float q[E], o[E], mx = -INFINITY, l = 0.f;
-    const TQ *qp = reinterpret_cast<const TQ *>(A.q) + b * A.qs[0] + j * A.qs[1] + h * A.qs[2];
-#pragma unroll
-    for (int e = 0; e < E; ++e) { q[e] = to_f(qp[lane + 32 * e]) * A.scale; o[e] = 0.f; }
-    for (long long t = begin + warp; t < end; t += 4) {
-        const int page = P.table[b * P.table_ld + t / P.size];
-        if (page < 0 || page >= P.n_pages) continue;
-        const long long at = page * P.page + (h / A.group) * P.head + (t % P.size) * P.row;
-        const TC *kp = reinterpret_cast<const TC *>(P.k) + at, *vp = reinterpret_cast<const TC *>(P.v) + at;
-        float s = 0.f;
-#pragma unroll
-        for (int e = 0; e < E; ++e) s += q[e] * to_f(kp[lane + 32 * e]);
-        s = warp_sum(s);
-        const float top = fmaxf(mx, s), f = mx == top ? 1.f : expf(mx - top), p = expf(s - top);
-        l = l * f + p;
-#pragma unroll
-        for (int e = 0; e < E; ++e) o[e] = o[e] * f + p * to_f(vp[lane + 32 * e]);
-        mx = top;
+    const uint32_t ring = smem_u32(smem), full = smem_u32(s_full), empty = smem_u32(s_empty);
+    float *parked = reinterpret_cast<float *>(smem + A.ring * S::stage), *parked_ml = parked + 4 * 16 * S::ld;
+    unsigned char *queries = smem + A.ring * S::stage + parked_bytes(DH);
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < A.ring; ++i) { mbar_init(full + 8 * i, 1); mbar_init(empty + 8 * i, A.rt); }
+        mbar_init_fence();
     }
-#pragma unroll
-    for (int e = 0; e < E; ++e) s_o[warp][lane + 32 * e] = o[e];
-    if (lane == 0) { s_m[warp] = mx; s_l[warp] = l; }
     __syncthreads();
-    const float top = fmaxf(fmaxf(s_m[0], s_m[1]), fmaxf(s_m[2], s_m[3]));
-    float total = 0.f, f[4];
-    for (int w = 0; w < 4; ++w) { f[w] = s_l[w] == 0.f ? 0.f : expf(s_m[w] - top); total += s_l[w] * f[w]; }
-    TQ *op = reinterpret_cast<TQ *>(A.out) + b * A.os[0] + j * A.os[1] + h * A.os[2];
-    for (int e = threadIdx.x; e < DH; e += 128) {
-        float v = 0.f;
-        for (int w = 0; w < 4; ++w) v += f[w] == 0.f ? 0.f : s_o[w][e] * f[w];
-        op[e] = rounded<TQ>(total == 0.f ? 0.f : v / total);
+    const int units = A.kv_heads * A.row_groups;
+
+    if (warp == kAttendWarps) {
+        int it = 0;
+        walk(A, units, [&](int b, const Span &sp, const Segment &seg, const Run &) {
+            const int kvh = seg.unit / A.row_groups, halves = A.box_rows == kStage ? 1 : 2;
+            for (int s0 = seg.stage0; s0 < seg.stage1; s0 += 32) {
+                // page and first row in it of both halves of the stage s0 + lane
+                int page[2] = {-1, -1}, row[2] = {0, 0};
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int pos = sp.base + (s0 + lane) * kStage + h * 16;
+                    if (h < halves && s0 + lane < seg.stage1 && pos < sp.end) {
+                        const int slot = pos / A.page;
+                        page[h] = A.table[b * A.table_ld + slot];
+                        row[h] = pos - slot * A.page;
+                    }
+                    if (page[h] < 0 || page[h] >= A.n_pages) page[h] = -1;        // outside the pool: zeros are read, nobody sees them
+                }
+                const int n = min(32, seg.stage1 - s0);
+                for (int i = 0; i < n; ++i, ++it) {
+                    int pg[2], rw[2];
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) { pg[h] = __shfl_sync(0xffffffffu, page[h], i); rw[h] = __shfl_sync(0xffffffffu, row[h], i); }
+                    const int slot = it % A.ring;
+                    if (lane == 0) {
+                        if (it >= A.ring) mbar_wait(empty + 8 * slot, (it / A.ring - 1) & 1, kMbarSpinLimit, A.status);
+                        s_info[slot] = make_int2(sp.base + (s0 + i) * kStage,
+                                                 halves == 1 ? (pg[0] >= 0 ? 3 : 0) : (pg[0] >= 0 ? 1 : 0) | (pg[1] >= 0 ? 2 : 0));
+                        mbar_arrive_expect_tx(full + 8 * slot, S::stage);
+                        const uint32_t dst = ring + slot * S::stage;
+#pragma unroll
+                        for (int x = 0; x < S::boxes; ++x) {
+                            tma_box4(dst + x * S::box_bytes, &k_map, x * S::box_w, rw[0], kvh, pg[0], full + 8 * slot);
+                            if (halves == 2) tma_box4(dst + x * S::box_bytes + 16 * S::rb, &k_map, x * S::box_w, rw[1], kvh, pg[1], full + 8 * slot);
+                        }
+#pragma unroll
+                        for (int x = 0; x < S::boxes; ++x) {
+                            tma_box4(dst + S::half + x * S::box_bytes, &v_map, x * S::box_w, rw[0], kvh, pg[0], full + 8 * slot);
+                            if (halves == 2) tma_box4(dst + S::half + x * S::box_bytes + 16 * S::rb, &v_map, x * S::box_w, rw[1], kvh, pg[1], full + 8 * slot);
+                        }
+                    }
+                }
+            }
+        });
+        // every copy lands before the CTA ends, also where an attending warp has given up
+        if (lane == 0)
+            for (int i = max(0, it - A.ring); i < it; ++i) mbar_wait(full + 8 * (i % A.ring), (i / A.ring) & 1, kMbarSpinLimit, A.status);
+        return;
     }
-    if (A.lse && threadIdx.x == 0) A.lse[((long long)b * A.m + j) * A.heads + h] = total == 0.f ? -INFINITY : top + logf(total);
+
+    const int tile = warp % A.rt, turns = A.turns, turn = warp / A.rt;      // row tile; groups that take stages, which of them (behind the last: none)
+    const int g = lane >> 2, t = lane & 3, tid = threadIdx.x;
+    const int slot_floats = A.rt * 16 * (DH + 2);
+    int it0 = 0;
+    walk(A, units, [&](int b, const Span &sp, const Segment &seg, const Run &run) {
+        const int kvh = seg.unit / A.row_groups, row0 = (seg.unit % A.row_groups) * A.rt * 16, rows = min(A.rt * 16, A.n_rows - row0);
+        // queries: a thread takes 32 bits (two elements, or one of fp32) at a time and puts them where the lanes of the products look for them
+        constexpr int per = S::es == 4 ? 1 : 2;
+        for (int i = tid; i < A.rt * 16 * (DH / per); i += kAttendWarps * 32) {
+            const int r = i / (DH / per), e = (i - r * (DH / per)) * per;
+            float x[per];
+            if (r < rows) {
+                const int j = (row0 + r) / A.group, h = kvh * A.group + (row0 + r - j * A.group);
+                const TQ *p = reinterpret_cast<const TQ *>(A.q) + b * A.qs[0] + j * A.qs[1] + h * A.qs[2] + e;
+#pragma unroll
+                for (int k = 0; k < per; ++k) x[k] = to_f(p[k]);
+            } else {
+#pragma unroll
+                for (int k = 0; k < per; ++k) x[k] = 0.f;
+            }
+            // 32 bytes of a row a step; lane 4 (row mod 8) + (word mod 4), register (row / 8) + 2 (word / 4)
+            const int word = e / per, ks = word / 8, w = word % 8, in = r & 15;
+            unsigned *dst = reinterpret_cast<unsigned *>(queries + (r >> 4) * query_bytes(DH, S::es, kSplitQ || S::es == 4) + ks * 512 + ((in & 7) * 4 + (w & 3)) * 16) +
+                            (in >> 3) + 2 * (w >> 2);
+            if constexpr (S::es == 4) {
+                const unsigned hi = tf32_part(x[0]);
+                dst[0] = hi;
+                dst[S::steps * 128] = tf32_rest_of(x[0], hi);
+            } else {
+                const unsigned hi = pack2<T>(x[0], x[per - 1]);
+                dst[0] = hi;
+                if (kSplitQ) dst[S::steps * 128] = rest2<T>(x[0], x[per - 1], hi);
+            }
+        }
+        bar_attend();
+
+        RowState<DH> st;
+#pragma unroll
+        for (int j = 0; j < DH / 8; ++j) st.o[j][0] = st.o[j][1] = st.o[j][2] = st.o[j][3] = 0.f;
+        st.m[0] = st.m[1] = -INFINITY;
+        st.l[0] = st.l[1] = 0.f;
+        const uint32_t q_base = smem_u32(queries) + tile * query_bytes(DH, S::es, kSplitQ || S::es == 4);
+        int token[2], begin[2], end[2];
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+            const int row = row0 + tile * 16 + g + 8 * r;
+            token[r] = row / A.group;
+            end[r] = token[r] >= sp.nq ? 0 : A.causal ? sp.first_end + token[r] : sp.end;
+            begin[r] = A.window > 0 ? max(0, end[r] - A.window) : 0;
+        }
+        const int n = seg.stage1 - seg.stage0;
+        for (int i = turn < turns ? (turn - it0 % turns + turns) % turns : n; i < n; i += turns) {
+            const int it = it0 + i, slot = it % A.ring;
+            mbar_wait(full + 8 * slot, (it / A.ring) & 1, kMbarSpinLimit, A.status);
+            const int2 info = s_info[slot];
+            const uint32_t stage = ring + slot * S::stage;
+            StageMask mask;
+            if (info.y == 3 && info.x >= sp.last_begin && info.x + kStage <= sp.first_end) {
+                attend_stage<T, DH, kSplitQ, kSplitP, false>(q_base, stage, A.c, mask, A, sp, info.x, token, st);
+            } else {
+                mask.valid = (info.y & 1 ? 0xffffu : 0u) | (info.y & 2 ? 0xffff0000u : 0u);
+                mask.row[0] = inside(info.x, begin[0], end[0]) & mask.valid;
+                mask.row[1] = inside(info.x, begin[1], end[1]) & mask.valid;
+                mask.any = inside(info.x, sp.first_begin, sp.end) & mask.valid;
+                mask.all = inside(info.x, sp.last_begin, sp.first_end);
+                attend_stage<T, DH, kSplitQ, kSplitP, true>(q_base, stage, A.c, mask, A, sp, info.x, token, st);
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(empty + 8 * slot);
+        }
+        it0 += n;
+
+        // the states of the warps: 4..7 hand theirs to 0..3, which park the joined ones
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+            st.l[r] += __shfl_xor_sync(0xffffffffu, st.l[r], 1);
+            st.l[r] += __shfl_xor_sync(0xffffffffu, st.l[r], 2);
+        }
+        float *mine = parked + (warp & 3) * 16 * S::ld, *mine_ml = parked_ml + (warp & 3) * 32;
+        auto park = [&] {
+#pragma unroll
+            for (int j = 0; j < DH / 8; ++j) {
+                *reinterpret_cast<float2 *>(mine + g * S::ld + 8 * j + 2 * t) = make_float2(st.o[j][0], st.o[j][1]);
+                *reinterpret_cast<float2 *>(mine + (g + 8) * S::ld + 8 * j + 2 * t) = make_float2(st.o[j][2], st.o[j][3]);
+            }
+            if (t == 0) {
+                mine_ml[2 * g] = st.m[0]; mine_ml[2 * g + 1] = st.l[0];
+                mine_ml[2 * g + 16] = st.m[1]; mine_ml[2 * g + 17] = st.l[1];
+            }
+        };
+        if (warp >= 4) park();
+        bar_attend();
+        if (warp < 4) {
+            float f[2], h[2];
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+                const float m = mine_ml[2 * g + 16 * r], l = mine_ml[2 * g + 16 * r + 1], top = fmaxf(m, st.m[r]), ref = top == -INFINITY ? 0.f : top;
+                f[r] = ex2(st.m[r] - ref); h[r] = ex2(m - ref);
+                st.l[r] = st.l[r] * f[r] + l * h[r];
+                st.m[r] = top;
+            }
+#pragma unroll
+            for (int j = 0; j < DH / 8; ++j) {
+                const float2 x = *reinterpret_cast<float2 *>(mine + g * S::ld + 8 * j + 2 * t), y = *reinterpret_cast<float2 *>(mine + (g + 8) * S::ld + 8 * j + 2 * t);
+                st.o[j][0] = st.o[j][0] * f[0] + x.x * h[0]; st.o[j][1] = st.o[j][1] * f[0] + x.y * h[0];
+                st.o[j][2] = st.o[j][2] * f[1] + y.x * h[1]; st.o[j][3] = st.o[j][3] * f[1] + y.y * h[1];
+            }
+            __syncwarp();
+            park();
+        }
+        bar_attend();
+        const int items = rows * (DH / 4), tiles = A.rt;
+        float *slot = A.partial;
+        if (!seg.whole) {
+            const long long start = run.total * blockIdx.x / run.ctas;
+            slot += (2 * (long long)blockIdx.x + (start < seg.first ? 1 : 0)) * slot_floats;
+        }
+        for (int i = tid; i < items; i += kAttendWarps * 32) {
+            const int r = i / (DH / 4), d = (i - r * (DH / 4)) * 4;
+            float m = -INFINITY, l = 0.f;
+            float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+            for (int w = r >> 4; w < 4; w += tiles) m = fmaxf(m, parked_ml[w * 32 + 2 * (r & 15)]);
+            const float ref = m == -INFINITY ? 0.f : m;
+            for (int w = r >> 4; w < 4; w += tiles) {
+                const float f = ex2(parked_ml[w * 32 + 2 * (r & 15)] - ref);
+                const float4 x = *reinterpret_cast<const float4 *>(parked + w * 16 * S::ld + (r & 15) * S::ld + d);
+                l += parked_ml[w * 32 + 2 * (r & 15) + 1] * f;
+                o.x += x.x * f; o.y += x.y * f; o.z += x.z * f; o.w += x.w * f;
+            }
+            if (seg.whole) {
+                finish<TQ>(A, sp, b, seg.unit, r, d, o, m, l);
+            } else {
+                __stcg(reinterpret_cast<float4 *>(slot + r * DH + d), o);
+                if (d == 0) __stcg(reinterpret_cast<float2 *>(slot + A.rt * 16 * DH + 2 * r), make_float2(m, l));
+            }
+        }
+        if (!seg.whole) {
+            // CTAs whose runs meet this unit: the one with its first granule to the one with its last
+            const int c0 = (int)(((seg.first + 1) * run.ctas - 1) / run.total), c1 = (int)((seg.last * run.ctas - 1) / run.total);
+            bar_attend();
+            if (tid == 0) {
+                int *counter = A.counters + c0;      // c0 is the first at no other unit that is cut
+                __threadfence();
+                const int last = atomicAdd(counter, 1) == c1 - c0;
+                if (last) *counter = 0;            // as the next call wants it
+                __threadfence();
+                s_last = last;
+            }
+            bar_attend();
+            if (s_last) {
+                const bool second = run.total * c0 / run.ctas < seg.first;
+                for (int i = tid; i < items; i += kAttendWarps * 32) {
+                    const int r = i / (DH / 4), d = (i - r * (DH / 4)) * 4;
+                    float m = -INFINITY, l = 0.f;
+                    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+                    auto place = [&](int c) { return A.partial + (2 * (long long)c + (c == c0 && second ? 1 : 0)) * slot_floats; };
+#pragma unroll 4
+                    for (int c = c0; c <= c1; ++c) m = fmaxf(m, __ldcg(place(c) + A.rt * 16 * DH + 2 * r));
+                    const float ref = m == -INFINITY ? 0.f : m;
+#pragma unroll 4
+                    for (int c = c0; c <= c1; ++c) {
+                        const float2 ml = __ldcg(reinterpret_cast<const float2 *>(place(c) + A.rt * 16 * DH + 2 * r));
+                        const float4 x = __ldcg(reinterpret_cast<const float4 *>(place(c) + r * DH + d));
+                        const float f = ex2(ml.x - ref);
+                        l += ml.y * f;
+                        o.x += x.x * f; o.y += x.y * f; o.z += x.z * f; o.w += x.w * f;
+                    }
+                    finish<TQ>(A, sp, b, seg.unit, r, d, o, m, l);
+                }
+            }
+        }
+        bar_attend();                            // parked states and queries are free again
+    });
+}
+
+// --------------------------------------------------------------------------------------------- host
+
+struct AttendPlan {
+    int rt, row_groups, ring, turns, smem, grid;
+    long long units;
+    size_t workspace;
+};
+
+static AttendPlan plan_attend(const xsm_kv &kv, int batch, int m, int n_heads, bool split_q) {
+    const xsm_kv_config &c = kv.cfg;
+    const int es = element_size(c.dtype), rows = m * (n_heads / c.n_kv_heads), tiles = (rows + 15) / 16;
+    AttendPlan p;
+    const int q = query_bytes(c.d_head, es, split_q || es == 4), stage = 2 * kStage * c.d_head * es;
+    p.rt = tiles >= 3 ? 4 : tiles;
+    // Shared memory: the ring gets what the parked states and the queries leave.  Queries of wide fp32 heads would leave less than two stages.
+    auto left = [&](int rt) { return kCtaSmem - 1024 - parked_bytes(c.d_head) - rt * q; };
+    while (p.rt > 1 && left(p.rt) < 2 * stage) p.rt /= 2;
+    p.ring = left(p.rt) / stage < kRing ? left(p.rt) / stage : kRing;
+    // Whoever waits for a stage must have seen the one before it in the same place (a barrier tells one phase from the next, not from the
+    // one after): groups of warps and places of the ring go together.
+    p.turns = kAttendWarps / p.rt;
+    while (p.turns > p.ring) p.turns /= 2;
+    p.ring -= p.ring % p.turns;
+    p.row_groups = (tiles + p.rt - 1) / p.rt;
+    p.smem = p.ring * stage + parked_bytes(c.d_head) + p.rt * q;
+    p.units = (long long)batch * c.n_kv_heads * p.row_groups;
+    p.grid = kv.sms < kMaxGrid ? kv.sms : kMaxGrid;
+    p.workspace = kHeadBytes + 2 * (size_t)p.grid * p.rt * 16 * (c.d_head + 2) * 4;
+    return p;
+}
+
+template <typename T, typename TQ, int DH>
+static cudaError_t launch_attend(const xsm_kv &kv, const AttendArgs &A, const AttendPlan &p, cudaStream_t st) {
+    const void *fn = (const void *)attend_kernel<T, TQ, DH>;
+    const cudaError_t e = open_kernel(fn, p.smem, false);
+    if (e != cudaSuccess) return e;
+    attend_kernel<T, TQ, DH><<<p.grid, (kAttendWarps + 1) * 32, p.smem, st>>>(kv.k_map, kv.v_map, A);
+    return cudaGetLastError();
+}
+template <typename T, typename TQ> static cudaError_t launch_width(const xsm_kv &kv, const AttendArgs &A, const AttendPlan &p, cudaStream_t st) {
+    switch (kv.cfg.d_head) {
+        case 32: return launch_attend<T, TQ, 32>(kv, A, p, st);
+        case 64: return launch_attend<T, TQ, 64>(kv, A, p, st);
+        case 96: return launch_attend<T, TQ, 96>(kv, A, p, st);
+        case 128: return launch_attend<T, TQ, 128>(kv, A, p, st);
+        default: return launch_attend<T, TQ, 256>(kv, A, p, st);
+    }
 }
 
 }  // namespace xsm
@@ -69,8 +712,9 @@ __global__ void __launch_bounds__(128) attend_kernel(const __grid_constant__ Att
 using namespace xsm;
 
 size_t xsm_kv_attend_workspace(const xsm_kv *kv, int batch, int m, int n_heads) {
-    if (!kv || batch < 1 || m < 1 || m > XSM_MAX_DRAFT || n_heads < 1) return 0;
-    return 16;
+    if (!kv || batch < 1 || m < 1 || m > XSM_MAX_DRAFT || n_heads < 1 || n_heads > 4096 || n_heads % kv->cfg.n_kv_heads) return 0;
+    const size_t a = plan_attend(*kv, batch, m, n_heads, false).workspace, b = plan_attend(*kv, batch, m, n_heads, true).workspace;
+    return a > b ? a : b;
 }
 
 xsm_status xsm_kv_attend(const xsm_kv *kv, const xsm_kv_attend_args *a, void *cuda_stream) {
@@ -85,29 +729,27 @@ xsm_status xsm_kv_attend(const xsm_kv *kv, const xsm_kv_attend_args *a, void *cu
     if (!(fabsf(a->scale) < INFINITY)) return op_failed(XSM_ERR_INVALID_ARG, "scale must be finite");
     if (a->batch == 0) return XSM_OK;
     if (!a->q || !a->out || !a->block_table || !a->lengths || !a->workspace) return op_failed(XSM_ERR_INVALID_ARG, "null argument");
-    if (a->workspace_bytes < (int64_t)xsm_kv_attend_workspace(kv, a->batch, a->m, a->n_heads)) return op_failed(XSM_ERR_CAPACITY, "the workspace is too small");
+    const AttendPlan p = plan_attend(*kv, a->batch, a->m, a->n_heads, a->q_dtype == XSM_F32 && c.dtype != XSM_F32);
+    if (p.units > INT_MAX / 4) return op_failed(XSM_ERR_INVALID_ARG, "batch * heads is too large");
+    if (a->workspace_bytes < (int64_t)p.workspace) return op_failed(XSM_ERR_CAPACITY, "the workspace is too small");
     const int per16 = 16 / element_size(a->q_dtype);
     for (int i = 0; i < 3; ++i)
         if (a->q_stride[i] % per16 || a->out_stride[i] % per16) return op_failed(XSM_ERR_INVALID_ARG, "strides of q and out must be multiples of 16 bytes");
     if (((uintptr_t)a->q | (uintptr_t)a->out | (uintptr_t)a->workspace) % 16) return op_failed(XSM_ERR_INVALID_ARG, "q, out and workspace must be 16-byte aligned");
-    const long long rows = (long long)a->batch * a->m * a->n_heads;
-    if (rows > INT_MAX) return op_failed(XSM_ERR_INVALID_ARG, "more than 2^31 - 1 rows");
     AttendArgs A;
-    A.q = a->q; A.out = a->out; A.lse = a->lse; A.lengths = a->lengths; A.counts = a->counts;
+    A.q = a->q; A.out = a->out; A.lse = a->lse; A.lengths = a->lengths; A.counts = a->counts; A.table = a->block_table; A.table_ld = a->table_stride;
+    A.status = (int *)a->workspace;
+    A.counters = A.status + 4;
+    A.partial = reinterpret_cast<float *>((char *)a->workspace + kHeadBytes);
     for (int i = 0; i < 3; ++i) { A.qs[i] = a->q_stride[i]; A.os[i] = a->out_stride[i]; }
-    A.m = a->m; A.heads = a->n_heads; A.group = a->n_heads / c.n_kv_heads; A.causal = a->causal != 0; A.window = a->window; A.scale = a->scale;
-    const Pages P = pages_of(*kv, a->block_table, a->table_stride, a->max_pages);
-    with_dtype(a->q_dtype, [&](auto q) {
-        with_dtype(c.dtype, [&](auto s) {
-            using TQ = decltype(q);
-            using TC = decltype(s);
-            const cudaStream_t st = (cudaStream_t)cuda_stream;
-            if (c.d_head == 32) attend_kernel<TQ, TC, 32><<<(unsigned)rows, 128, 0, st>>>(A, P);
-            else if (c.d_head == 64) attend_kernel<TQ, TC, 64><<<(unsigned)rows, 128, 0, st>>>(A, P);
-            else if (c.d_head == 96) attend_kernel<TQ, TC, 96><<<(unsigned)rows, 128, 0, st>>>(A, P);
-            else if (c.d_head == 128) attend_kernel<TQ, TC, 128><<<(unsigned)rows, 128, 0, st>>>(A, P);
-            else attend_kernel<TQ, TC, 256><<<(unsigned)rows, 128, 0, st>>>(A, P);
-        });
-    });
-    return launched(cudaGetLastError());
+    A.batch = a->batch; A.m = a->m; A.heads = a->n_heads; A.group = a->n_heads / c.n_kv_heads; A.kv_heads = c.n_kv_heads;
+    A.rt = p.rt; A.row_groups = p.row_groups; A.n_rows = A.m * A.group; A.ring = p.ring; A.turns = p.turns;
+    A.causal = a->causal != 0; A.window = a->window; A.page = c.page_size; A.max_pages = a->max_pages; A.n_pages = c.n_pages; A.box_rows = kv->box_rows;
+    A.c = (float)((double)a->scale * 1.4426950408889634);
+    const cudaStream_t st = (cudaStream_t)cuda_stream;
+    if (c.dtype == XSM_F32) return launched(launch_width<float, float>(*kv, A, p, st));
+    if (c.dtype == XSM_BF16) return launched(launch_width<bf16, bf16>(*kv, A, p, st));
+    if (a->q_dtype == XSM_F32) return launched(launch_width<__half, float>(*kv, A, p, st));
+    if (a->q_dtype == XSM_BF16) return launched(launch_width<__half, bf16>(*kv, A, p, st));
+    return launched(launch_width<__half, __half>(*kv, A, p, st));
 }

@@ -1,7 +1,6 @@
 // Shared by the operators on a caller's own paged cache and logits (xsm_append.cu, xsm_attend.cu, xsm_logprob.cu).
 #pragma once
-#include "../../include/xsm.h"
-#include "xsm_common.cuh"
+#include "xsm_host.h"
 
 #include <stddef.h>
 #include <stdint.h>
@@ -9,6 +8,9 @@
 struct xsm_kv {
     xsm_kv_config cfg;
     void *k, *v;
+    // boxes of 16 or 32 positions of a head, as many elements wide as fill 128 (d_head 32 and 96 of 16 bits: 64) bytes, swizzled
+    xsm::TensorMap k_map, v_map;
+    int box_rows, sms;
 };
 
 namespace xsm {
