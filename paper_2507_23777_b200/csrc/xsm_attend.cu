@@ -1,7 +1,7 @@
 // Attention of the newest tokens of each sequence over a caller's paged pools (xsm_kv).
 //
 // A unit is a sequence, a key head and up to 64 of the query rows (tokens x heads of the group) that read it.  What a unit has to do is
-// counted in granules of 256 positions, and all granules of the call, in one row, are cut into equal runs, one for every CTA of a grid
+// counted in granules of 128 positions, and all granules of the call, in one row, are cut into equal runs, one for every CTA of a grid
 // that fills the chip once: lengths are known on the device alone, and neither short nor long sequences leave SMs without work.
 // A unit that a cut goes through leaves partial results (maximum, sum, unnormalised output) in the workspace; the CTA that is the last
 // to arrive at the unit's counter adds them up in the order of the positions, so results do not depend on which one that is.
@@ -22,8 +22,8 @@
 namespace xsm {
 
 constexpr int kStage = 32;            // positions of a stage
-constexpr int kGranule = 8;           // stages that are never cut apart
-constexpr int kAttendWarps = 8;
+constexpr int kGranule = 4;           // stages that are never cut apart
+constexpr int kAttendWarps = 8, kProducers = 4;
 constexpr int kRing = 16;             // most stages in shared memory
 // Workspace: status word and counters, which every call leaves at zero, in a place that does not depend on the call; then the partial results.
 constexpr int kHeadBytes = 4096, kMaxGrid = kHeadBytes / 4 - 4;
@@ -39,7 +39,8 @@ struct AttendArgs {
     int batch, m, heads, group, kv_heads;
     int rt, row_groups, n_rows;       // row tiles of a unit, units that share a key head, query rows of a key head
     int causal, window, page, max_pages, n_pages, box_rows;
-    int ring, turns;                  // stages in shared memory, groups of warps that take them in turn: every place of the ring is one group's
+    int parked;                       // warps that park their state at the end of a unit
+    int ring, turns, producers;       // stages in shared memory; groups of warps that take them in turn, warps that fetch them: every place is one of each's
     float c;                          // scale * log2(e)
 };
 
@@ -56,9 +57,12 @@ template <typename T, int DH> struct Shape {
         return base + (ch / per) * box_bytes + r * rb + ((x ^ s) << 4);
     }
 };
-__host__ __device__ constexpr int parked_bytes(int dh) { return 4 * 16 * (dh + 4) * 4 + 4 * 16 * 2 * 4; }
+__host__ __device__ constexpr int parked_bytes(int dh, int warps) { return warps * 16 * ((dh + 4) + 2) * 4; }
 // query operands of a row tile, in the order in which the lanes take them
 __host__ __device__ constexpr int query_bytes(int dh, int es, bool split) { return dh * es / 32 * 512 * (split ? 2 : 1); }
+
+// query rows as they are in memory, on their way to that
+__host__ __device__ constexpr int raw_bytes(int dh, int es) { return 16 * (dh * es + 16); }
 
 // What a sequence has to do.  Row j of its nq queries sees [begin_j, end_j): end_j = end - nq + 1 + j (all: end), begin_j = end_j - window.
 struct Span {
@@ -81,41 +85,46 @@ __device__ __forceinline__ Span span_of(const AttendArgs &A, int b) {
 }
 __device__ __forceinline__ int granules(const Span &s) { return (s.stages + kGranule - 1) / kGranule; }
 
-// The run of granules of this CTA, and where it starts.  Every warp works it out for itself.
+// The run of granules of this CTA, and where it starts.  Every warp works it out for itself.  (The host has made sure that the granules
+// of all units fit 31 bits.)
 struct Run {
-    long long at, end, total, before;       // granules; before: those of the sequences before b
-    int b, ctas;                             // CTAs that have work
+    int at, end, before;                     // granules; before: those of the sequences before b
+    int b;
+    int ctas, quot, rem;                     // CTAs that have work: the first `rem` have quot + 1 granules, the others quot
+    __device__ __forceinline__ int start(int cta) const { return cta * quot + min(cta, rem); }
+    __device__ __forceinline__ int owner(int granule) const {
+        const int more = rem * (quot + 1);
+        return granule < more ? granule / (quot + 1) : rem + (granule - more) / quot;
+    }
 };
-__device__ __forceinline__ long long warp_sum_ll(long long v) {
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-    return v;
-}
 __device__ __forceinline__ Run run_of(const AttendArgs &A, int units) {
     const int lane = threadIdx.x & 31;
-    long long sum = 0;
-    int first = 0;                           // of the first 32 sequences, which most calls end with
+    int sum = 0, first = 0;                  // first: of the first 32 sequences, which most calls end with
     for (int b = lane; b < A.batch; b += 32) {
         const int g = granules(span_of(A, b));
         if (b == lane) first = g;
         sum += g;
     }
     Run r;
-    r.total = warp_sum_ll(sum) * units;
-    r.ctas = (int)min((long long)gridDim.x, r.total);        // every one of them has a granule at least
+    const int total = (int)__reduce_add_sync(0xffffffffu, (unsigned)sum) * units;
+    r.ctas = min((int)gridDim.x, total);     // every one of them has a granule at least
+    r.quot = total / r.ctas;
+    r.rem = total - r.quot * r.ctas;
+    r.at = r.start(blockIdx.x);
+    r.end = r.start(blockIdx.x + 1);
+    r.b = 0;
+    r.before = 0;
     if ((int)blockIdx.x >= r.ctas) {
-        r.at = r.end = r.before = 0; r.b = 0;
+        r.end = r.at;
         return r;
     }
-    r.at = r.total * blockIdx.x / r.ctas;
-    r.end = r.total * (blockIdx.x + 1) / r.ctas;
-    long long before = 0;
-    for (int b0 = 0;; b0 += 32) {
+    int before = 0;
+    for (int b0 = 0; b0 < A.batch; b0 += 32) {
         const int b = b0 + lane, mine = b >= A.batch ? 0 : b0 == 0 ? first : granules(span_of(A, b));
-        long long up = mine;
+        int up = mine;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
-            const long long v = __shfl_up_sync(0xffffffffu, up, o);
+            const int v = __shfl_up_sync(0xffffffffu, up, o);
             if (lane >= o) up += v;
         }
         const unsigned past = __ballot_sync(0xffffffffu, b < A.batch && (before + up) * units > r.at);
@@ -123,39 +132,36 @@ __device__ __forceinline__ Run run_of(const AttendArgs &A, int units) {
             const int l = __ffs(past) - 1;
             r.b = b0 + l;
             r.before = (before + __shfl_sync(0xffffffffu, up - mine, l)) * units;
-            return r;
+            break;
         }
         before += __shfl_sync(0xffffffffu, up, 31);
-        if (b0 + 32 >= A.batch) break;
     }
-    r.at = r.end = r.before = 0; r.b = 0;          // (not reached: the granules of all sequences are `total`)
     return r;
 }
 
 // The part of a unit that a CTA does.
 struct Segment {
     int unit, stage0, stage1;                // of the sequence; stages
-    long long first, last;                   // the whole unit's granules
-    bool whole;
+    int first, last;                         // the whole unit's granules
+    bool whole, more;                        // the CTA does all of the unit; has another one behind it (the next of the sequence, or the next sequence's first)
 };
 
 template <typename F> __device__ __forceinline__ void walk(const AttendArgs &A, int units, F &&f) {
     Run r = run_of(A, units);
     while (r.at < r.end) {
         const Span sp = span_of(A, r.b);
-        const int per = granules(sp);
-        const long long behind = r.before + (long long)per * units;
+        const int per = granules(sp), behind = r.before + per * units;
         while (r.at < r.end && r.at < behind) {
             Segment s;
-            const long long rel = r.at - r.before;
-            s.unit = (int)(rel / per);
-            const int g0 = (int)(rel - (long long)s.unit * per);
-            const int g1 = (int)min((long long)per, g0 + (r.end - r.at));
+            const int rel = r.at - r.before;
+            s.unit = rel / per;
+            const int g0 = rel - s.unit * per, g1 = min(per, g0 + (r.end - r.at));
             s.stage0 = g0 * kGranule;
             s.stage1 = min(sp.stages, g1 * kGranule);
-            s.first = r.before + (long long)s.unit * per;
+            s.first = r.before + s.unit * per;
             s.last = s.first + per;
             s.whole = g0 == 0 && g1 == per;
+            s.more = r.at + g1 - g0 < r.end;
             f(r.b, sp, s, r);
             r.at += g1 - g0;
         }
@@ -414,7 +420,7 @@ template <typename TQ> __device__ __forceinline__ void finish(const AttendArgs &
 }
 
 template <typename T, typename TQ, int DH>
-__global__ void __launch_bounds__((kAttendWarps + 1) * 32, 1)
+__global__ void __launch_bounds__((kAttendWarps + kProducers) * 32, 1)
 attend_kernel(const __grid_constant__ TensorMap k_map, const __grid_constant__ TensorMap v_map, const __grid_constant__ AttendArgs A) {
     using S = Shape<T, DH>;
     // queries with more bits than the pools' type enter as two parts; so do the weights, unless the output has fewer bits than they
@@ -422,11 +428,12 @@ attend_kernel(const __grid_constant__ TensorMap k_map, const __grid_constant__ T
     extern __shared__ __align__(1024) unsigned char smem[];
     __shared__ __align__(8) unsigned long long s_full[kRing], s_empty[kRing];
     __shared__ int2 s_info[kRing];            // first position of a stage, which halves exist
-    __shared__ int s_last;
+    struct Left { int b, unit, nq, c0, c1; bool second, last; };
+    __shared__ Left s_left[2];                // units that other CTAs share: at most the run's first and its last
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t ring = smem_u32(smem), full = smem_u32(s_full), empty = smem_u32(s_empty);
-    float *parked = reinterpret_cast<float *>(smem + A.ring * S::stage), *parked_ml = parked + 4 * 16 * S::ld;
-    unsigned char *queries = smem + A.ring * S::stage + parked_bytes(DH);
+    float *parked = reinterpret_cast<float *>(smem + A.ring * S::stage), *parked_ml = parked + A.parked * 16 * S::ld;
+    unsigned char *queries = smem + A.ring * S::stage + parked_bytes(DH, A.parked);
     if (threadIdx.x == 0) {
         for (int i = 0; i < A.ring; ++i) { mbar_init(full + 8 * i, 1); mbar_init(empty + 8 * i, A.rt); }
         mbar_init_fence();
@@ -434,51 +441,60 @@ attend_kernel(const __grid_constant__ TensorMap k_map, const __grid_constant__ T
     __syncthreads();
     const int units = A.kv_heads * A.row_groups;
 
-    if (warp == kAttendWarps) {
-        int it = 0;
+    if (warp >= kAttendWarps) {
+        // producer p of n takes stages p, p + n, ... of the CTA; slot and phase are those of its next one
+        const int p = warp - kAttendWarps;
+        if (p >= A.producers) return;
+        int it = 0, slot = 0, phase = 1, next = p;                    // it: stages of the segments before
+        auto advance = [&](int by) {
+            slot += by;
+            while (slot >= A.ring) { slot -= A.ring; phase ^= 1; }
+        };
+        advance(p);
         walk(A, units, [&](int b, const Span &sp, const Segment &seg, const Run &) {
-            const int kvh = seg.unit / A.row_groups, halves = A.box_rows == kStage ? 1 : 2;
-            for (int s0 = seg.stage0; s0 < seg.stage1; s0 += 32) {
-                // page and first row in it of both halves of the stage s0 + lane
+            const int kvh = seg.unit / A.row_groups, halves = A.box_rows == kStage ? 1 : 2, n = seg.stage1 - seg.stage0;
+            while (next < it + n) {
+                // page and first row in it of both halves of the stage that is this lane's of the next 32
                 int page[2] = {-1, -1}, row[2] = {0, 0};
+                const int mine = next - it + lane * A.producers, first = sp.base + (seg.stage0 + mine) * kStage;
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    const int pos = sp.base + (s0 + lane) * kStage + h * 16;
-                    if (h < halves && s0 + lane < seg.stage1 && pos < sp.end) {
-                        const int slot = pos / A.page;
-                        page[h] = A.table[b * A.table_ld + slot];
-                        row[h] = pos - slot * A.page;
+                    const int pos = first + h * 16;
+                    if (h < halves && mine < n && pos < sp.end) {
+                        const int at = pos / A.page;
+                        page[h] = A.table[b * A.table_ld + at];
+                        row[h] = pos - at * A.page;
                     }
                     if (page[h] < 0 || page[h] >= A.n_pages) page[h] = -1;        // outside the pool: zeros are read, nobody sees them
                 }
-                const int n = min(32, seg.stage1 - s0);
-                for (int i = 0; i < n; ++i, ++it) {
+                for (int i = 0; i < 32 && next < it + n; ++i, next += A.producers) {
                     int pg[2], rw[2];
 #pragma unroll
                     for (int h = 0; h < 2; ++h) { pg[h] = __shfl_sync(0xffffffffu, page[h], i); rw[h] = __shfl_sync(0xffffffffu, row[h], i); }
-                    const int slot = it % A.ring;
+                    const int pos = __shfl_sync(0xffffffffu, first, i);
                     if (lane == 0) {
-                        if (it >= A.ring) mbar_wait(empty + 8 * slot, (it / A.ring - 1) & 1, kMbarSpinLimit, A.status);
-                        s_info[slot] = make_int2(sp.base + (s0 + i) * kStage,
-                                                 halves == 1 ? (pg[0] >= 0 ? 3 : 0) : (pg[0] >= 0 ? 1 : 0) | (pg[1] >= 0 ? 2 : 0));
-                        mbar_arrive_expect_tx(full + 8 * slot, S::stage);
-                        const uint32_t dst = ring + slot * S::stage;
+                        const uint32_t bar = full + 8 * slot, dst = ring + slot * S::stage;
+                        if (next >= A.ring) mbar_wait(empty + 8 * slot, phase, kMbarSpinLimit, A.status);
+                        s_info[slot] = make_int2(pos, halves == 1 ? (pg[0] >= 0 ? 3 : 0) : (pg[0] >= 0 ? 1 : 0) | (pg[1] >= 0 ? 2 : 0));
+                        mbar_arrive_expect_tx(bar, S::stage);
 #pragma unroll
                         for (int x = 0; x < S::boxes; ++x) {
-                            tma_box4(dst + x * S::box_bytes, &k_map, x * S::box_w, rw[0], kvh, pg[0], full + 8 * slot);
-                            if (halves == 2) tma_box4(dst + x * S::box_bytes + 16 * S::rb, &k_map, x * S::box_w, rw[1], kvh, pg[1], full + 8 * slot);
+                            tma_box4(dst + x * S::box_bytes, &k_map, x * S::box_w, rw[0], kvh, pg[0], bar);
+                            if (halves == 2) tma_box4(dst + x * S::box_bytes + 16 * S::rb, &k_map, x * S::box_w, rw[1], kvh, pg[1], bar);
                         }
 #pragma unroll
                         for (int x = 0; x < S::boxes; ++x) {
-                            tma_box4(dst + S::half + x * S::box_bytes, &v_map, x * S::box_w, rw[0], kvh, pg[0], full + 8 * slot);
-                            if (halves == 2) tma_box4(dst + S::half + x * S::box_bytes + 16 * S::rb, &v_map, x * S::box_w, rw[1], kvh, pg[1], full + 8 * slot);
+                            tma_box4(dst + S::half + x * S::box_bytes, &v_map, x * S::box_w, rw[0], kvh, pg[0], bar);
+                            if (halves == 2) tma_box4(dst + S::half + x * S::box_bytes + 16 * S::rb, &v_map, x * S::box_w, rw[1], kvh, pg[1], bar);
                         }
                     }
+                    advance(A.producers);
                 }
             }
+            it += n;
         });
         // every copy lands before the CTA ends, also where an attending warp has given up
-        if (lane == 0)
+        if (warp == kAttendWarps && lane == 0)
             for (int i = max(0, it - A.ring); i < it; ++i) mbar_wait(full + 8 * (i % A.ring), (i / A.ring) & 1, kMbarSpinLimit, A.status);
         return;
     }
@@ -486,23 +502,34 @@ attend_kernel(const __grid_constant__ TensorMap k_map, const __grid_constant__ T
     const int tile = warp % A.rt, turns = A.turns, turn = warp / A.rt;      // row tile; groups that take stages, which of them (behind the last: none)
     const int g = lane >> 2, t = lane & 3, tid = threadIdx.x;
     const int slot_floats = A.rt * 16 * (DH + 2);
-    int it0 = 0;
+    unsigned char *raw = queries + A.rt * query_bytes(DH, S::es, kSplitQ || S::es == 4);
+    constexpr int raw_ld = DH * (int)sizeof(TQ) + 16;
+    // requests the query rows of a unit
+    auto fetch_rows = [&](int b, int unit) {
+        constexpr int chunks = DH * (int)sizeof(TQ) / 16;
+        const int kvh = unit / A.row_groups, row0 = (unit % A.row_groups) * A.rt * 16, rows = min(A.rt * 16, A.n_rows - row0);
+        for (int i = tid; i < rows * chunks; i += kAttendWarps * 32) {
+            const int r = i / chunks, c = i - r * chunks, j = (row0 + r) / A.group, h = kvh * A.group + (row0 + r - j * A.group);
+            const TQ *p = reinterpret_cast<const TQ *>(A.q) + b * A.qs[0] + j * A.qs[1] + h * A.qs[2];
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"(smem_u32(raw) + r * raw_ld + c * 16), "l"(reinterpret_cast<const char *>(p) + c * 16) : "memory");
+        }
+    };
+    bool opening = true;
+    int pending = 0;
+    int it0 = 0, next = turn < turns ? turn : INT_MAX, slot = turn, phase = 0;      // stages of the segments before; this warp's next one
     walk(A, units, [&](int b, const Span &sp, const Segment &seg, const Run &run) {
         const int kvh = seg.unit / A.row_groups, row0 = (seg.unit % A.row_groups) * A.rt * 16, rows = min(A.rt * 16, A.n_rows - row0);
-        // queries: a thread takes 32 bits (two elements, or one of fp32) at a time and puts them where the lanes of the products look for them
+        if (opening) fetch_rows(b, seg.unit);
+        opening = false;
+        asm volatile("cp.async.wait_all;" ::: "memory");
+        bar_attend();                            // the rows are here; what the segment before parked has been read
+        // a thread takes 32 bits (two elements, or one of fp32) at a time and puts them where the lanes of the products look for them
         constexpr int per = S::es == 4 ? 1 : 2;
         for (int i = tid; i < A.rt * 16 * (DH / per); i += kAttendWarps * 32) {
             const int r = i / (DH / per), e = (i - r * (DH / per)) * per;
             float x[per];
-            if (r < rows) {
-                const int j = (row0 + r) / A.group, h = kvh * A.group + (row0 + r - j * A.group);
-                const TQ *p = reinterpret_cast<const TQ *>(A.q) + b * A.qs[0] + j * A.qs[1] + h * A.qs[2] + e;
 #pragma unroll
-                for (int k = 0; k < per; ++k) x[k] = to_f(p[k]);
-            } else {
-#pragma unroll
-                for (int k = 0; k < per; ++k) x[k] = 0.f;
-            }
+            for (int k = 0; k < per; ++k) x[k] = r < rows ? to_f(reinterpret_cast<const TQ *>(raw + r * raw_ld)[e + k]) : 0.f;
             // 32 bytes of a row a step; lane 4 (row mod 8) + (word mod 4), register (row / 8) + 2 (word / 4)
             const int word = e / per, ks = word / 8, w = word % 8, in = r & 15;
             unsigned *dst = reinterpret_cast<unsigned *>(queries + (r >> 4) * query_bytes(DH, S::es, kSplitQ || S::es == 4) + ks * 512 + ((in & 7) * 4 + (w & 3)) * 16) +
@@ -518,6 +545,10 @@ attend_kernel(const __grid_constant__ TensorMap k_map, const __grid_constant__ T
             }
         }
         bar_attend();
+        if (seg.more) {
+            const bool same = seg.unit + 1 < units;
+            fetch_rows(same ? b : b + 1, same ? seg.unit + 1 : 0);
+        }
 
         RowState<DH> st;
 #pragma unroll
@@ -534,9 +565,8 @@ attend_kernel(const __grid_constant__ TensorMap k_map, const __grid_constant__ T
             begin[r] = A.window > 0 ? max(0, end[r] - A.window) : 0;
         }
         const int n = seg.stage1 - seg.stage0;
-        for (int i = turn < turns ? (turn - it0 % turns + turns) % turns : n; i < n; i += turns) {
-            const int it = it0 + i, slot = it % A.ring;
-            mbar_wait(full + 8 * slot, (it / A.ring) & 1, kMbarSpinLimit, A.status);
+        for (; next < it0 + n; next += turns) {
+            mbar_wait(full + 8 * slot, phase, kMbarSpinLimit, A.status);
             const int2 info = s_info[slot];
             const uint32_t stage = ring + slot * S::stage;
             StageMask mask;
@@ -552,10 +582,12 @@ attend_kernel(const __grid_constant__ TensorMap k_map, const __grid_constant__ T
             }
             __syncwarp();
             if (lane == 0) mbar_arrive(empty + 8 * slot);
+            slot += turns;
+            if (slot >= A.ring) { slot -= A.ring; phase ^= 1; }
         }
         it0 += n;
 
-        // the states of the warps: 4..7 hand theirs to 0..3, which park the joined ones
+        // the states of the warps: of eight, 4..7 hand theirs to 0..3, which park the joined ones
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
             st.l[r] += __shfl_xor_sync(0xffffffffu, st.l[r], 1);
@@ -573,9 +605,12 @@ attend_kernel(const __grid_constant__ TensorMap k_map, const __grid_constant__ T
                 mine_ml[2 * g + 16] = st.m[1]; mine_ml[2 * g + 17] = st.l[1];
             }
         };
-        if (warp >= 4) park();
-        bar_attend();
-        if (warp < 4) {
+        const bool eight = turns * A.rt == kAttendWarps;
+        if (eight) {
+            if (warp >= 4) park();
+            bar_attend();
+        }
+        if (eight && warp < 4) {
             float f[2], h[2];
 #pragma unroll
             for (int r = 0; r < 2; ++r) {
@@ -591,22 +626,21 @@ attend_kernel(const __grid_constant__ TensorMap k_map, const __grid_constant__ T
                 st.o[j][2] = st.o[j][2] * f[1] + y.x * h[1]; st.o[j][3] = st.o[j][3] * f[1] + y.y * h[1];
             }
             __syncwarp();
-            park();
         }
+        if (warp < A.parked) park();
         bar_attend();
         const int items = rows * (DH / 4), tiles = A.rt;
-        float *slot = A.partial;
+        float *place = A.partial;
         if (!seg.whole) {
-            const long long start = run.total * blockIdx.x / run.ctas;
-            slot += (2 * (long long)blockIdx.x + (start < seg.first ? 1 : 0)) * slot_floats;
+            place += (2 * (long long)blockIdx.x + (run.start(blockIdx.x) < seg.first ? 1 : 0)) * slot_floats;
         }
         for (int i = tid; i < items; i += kAttendWarps * 32) {
             const int r = i / (DH / 4), d = (i - r * (DH / 4)) * 4;
             float m = -INFINITY, l = 0.f;
             float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-            for (int w = r >> 4; w < 4; w += tiles) m = fmaxf(m, parked_ml[w * 32 + 2 * (r & 15)]);
+            for (int w = r >> 4; w < A.parked; w += tiles) m = fmaxf(m, parked_ml[w * 32 + 2 * (r & 15)]);
             const float ref = m == -INFINITY ? 0.f : m;
-            for (int w = r >> 4; w < 4; w += tiles) {
+            for (int w = r >> 4; w < A.parked; w += tiles) {
                 const float f = ex2(parked_ml[w * 32 + 2 * (r & 15)] - ref);
                 const float4 x = *reinterpret_cast<const float4 *>(parked + w * 16 * S::ld + (r & 15) * S::ld + d);
                 l += parked_ml[w * 32 + 2 * (r & 15) + 1] * f;
@@ -615,74 +649,103 @@ attend_kernel(const __grid_constant__ TensorMap k_map, const __grid_constant__ T
             if (seg.whole) {
                 finish<TQ>(A, sp, b, seg.unit, r, d, o, m, l);
             } else {
-                __stcg(reinterpret_cast<float4 *>(slot + r * DH + d), o);
-                if (d == 0) __stcg(reinterpret_cast<float2 *>(slot + A.rt * 16 * DH + 2 * r), make_float2(m, l));
+                __stcg(reinterpret_cast<float4 *>(place + r * DH + d), o);
+                if (d == 0) __stcg(reinterpret_cast<float2 *>(place + A.rt * 16 * DH + 2 * r), make_float2(m, l));
             }
         }
         if (!seg.whole) {
-            // CTAs whose runs meet this unit: the one with its first granule to the one with its last
-            const int c0 = (int)(((seg.first + 1) * run.ctas - 1) / run.total), c1 = (int)((seg.last * run.ctas - 1) / run.total);
-            bar_attend();
+            // CTAs whose runs meet this unit: the one with its first granule to the one with its last.  Whether this CTA is the last of them to
+            // be there is asked at its end, when all its runs' writes are done.
             if (tid == 0) {
-                int *counter = A.counters + c0;      // c0 is the first at no other unit that is cut
-                __threadfence();
-                const int last = atomicAdd(counter, 1) == c1 - c0;
-                if (last) *counter = 0;            // as the next call wants it
-                __threadfence();
-                s_last = last;
+                const int c0 = run.owner(seg.first), c1 = run.owner(seg.last - 1);
+                s_left[pending] = Left{b, seg.unit, sp.nq, c0, c1, run.start(c0) < seg.first, false};
             }
-            bar_attend();
-            if (s_last) {
-                const bool second = run.total * c0 / run.ctas < seg.first;
-                for (int i = tid; i < items; i += kAttendWarps * 32) {
-                    const int r = i / (DH / 4), d = (i - r * (DH / 4)) * 4;
-                    float m = -INFINITY, l = 0.f;
-                    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-                    auto place = [&](int c) { return A.partial + (2 * (long long)c + (c == c0 && second ? 1 : 0)) * slot_floats; };
-#pragma unroll 4
-                    for (int c = c0; c <= c1; ++c) m = fmaxf(m, __ldcg(place(c) + A.rt * 16 * DH + 2 * r));
-                    const float ref = m == -INFINITY ? 0.f : m;
-#pragma unroll 4
-                    for (int c = c0; c <= c1; ++c) {
-                        const float2 ml = __ldcg(reinterpret_cast<const float2 *>(place(c) + A.rt * 16 * DH + 2 * r));
-                        const float4 x = __ldcg(reinterpret_cast<const float4 *>(place(c) + r * DH + d));
-                        const float f = ex2(ml.x - ref);
-                        l += ml.y * f;
-                        o.x += x.x * f; o.y += x.y * f; o.z += x.z * f; o.w += x.w * f;
+            ++pending;
+        }
+    });
+    if (pending == 0) return;
+    bar_attend();
+    if (tid < pending) {
+        // c0 is the first at no other unit that is cut: its counter is this unit's
+        int *counter = A.counters + s_left[tid].c0, before;
+        asm volatile("atom.add.acq_rel.gpu.global.s32 %0, [%1], 1;" : "=r"(before) : "l"(counter) : "memory");
+        const bool last = before == s_left[tid].c1 - s_left[tid].c0;
+        if (last) *counter = 0;                  // as the next call wants it
+        s_left[tid].last = last;
+    }
+    bar_attend();
+    for (int u = 0; u < pending; ++u) {
+        const Left left = s_left[u];
+        if (!left.last) continue;
+        Span sp;
+        sp.nq = left.nq;
+        const int rows = min(A.rt * 16, A.n_rows - (left.unit % A.row_groups) * A.rt * 16);
+        auto place = [&](int c) { return A.partial + (2 * (long long)c + (c == left.c0 && left.second ? 1 : 0)) * slot_floats; };
+        for (int i = tid; i < rows * (DH / 4); i += kAttendWarps * 32) {
+            const int r = i / (DH / 4), d = (i - r * (DH / 4)) * 4;
+            float m = -INFINITY, l = 0.f;
+            float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+            for (int c = left.c0; c <= left.c1; c += 8) {           // eight of them on their way at a time
+                float2 ml[8];
+                float4 x[8];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    ml[k] = make_float2(-INFINITY, 0.f);
+                    x[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+                    if (c + k <= left.c1) {
+                        ml[k] = __ldcg(reinterpret_cast<const float2 *>(place(c + k) + A.rt * 16 * DH + 2 * r));
+                        x[k] = __ldcg(reinterpret_cast<const float4 *>(place(c + k) + r * DH + d));
                     }
-                    finish<TQ>(A, sp, b, seg.unit, r, d, o, m, l);
+                }
+                float top = m;
+#pragma unroll
+                for (int k = 0; k < 8; ++k) top = fmaxf(top, ml[k].x);
+                const float ref = top == -INFINITY ? 0.f : top, f0 = ex2(m - ref);
+                l *= f0; o.x *= f0; o.y *= f0; o.z *= f0; o.w *= f0;
+                m = top;
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    const float f = ex2(ml[k].x - ref);
+                    l += ml[k].y * f;
+                    o.x += x[k].x * f; o.y += x[k].y * f; o.z += x[k].z * f; o.w += x[k].w * f;
                 }
             }
+            finish<TQ>(A, sp, left.b, left.unit, r, d, o, m, l);
         }
-        bar_attend();                            // parked states and queries are free again
-    });
+    }
 }
 
 // --------------------------------------------------------------------------------------------- host
 
 struct AttendPlan {
-    int rt, row_groups, ring, turns, smem, grid;
+    int rt, row_groups, ring, turns, producers, parked, smem, grid;
     long long units;
     size_t workspace;
 };
 
-static AttendPlan plan_attend(const xsm_kv &kv, int batch, int m, int n_heads, bool split_q) {
+static AttendPlan plan_attend(const xsm_kv &kv, int batch, int m, int n_heads, int q_dtype) {
     const xsm_kv_config &c = kv.cfg;
     const int es = element_size(c.dtype), rows = m * (n_heads / c.n_kv_heads), tiles = (rows + 15) / 16;
     AttendPlan p;
-    const int q = query_bytes(c.d_head, es, split_q || es == 4), stage = 2 * kStage * c.d_head * es;
+    const int q = query_bytes(c.d_head, es, es == 4 || q_dtype == XSM_F32) + raw_bytes(c.d_head, element_size(q_dtype)), stage = 2 * kStage * c.d_head * es;
     p.rt = tiles >= 3 ? 4 : tiles;
-    // Shared memory: the ring gets what the parked states and the queries leave.  Queries of wide fp32 heads would leave less than two stages.
-    auto left = [&](int rt) { return kCtaSmem - 1024 - parked_bytes(c.d_head) - rt * q; };
-    while (p.rt > 1 && left(p.rt) < 2 * stage) p.rt /= 2;
-    p.ring = left(p.rt) / stage < kRing ? left(p.rt) / stage : kRing;
+    // Shared memory: the ring gets what the parked states and the queries leave.  A group of warps that takes stages wants two places, one to
+    // work on and one that fills; so few groups that wide rows leave no room, then fewer row tiles.
+    auto left = [&](int rt, int turns) { return kCtaSmem - 1024 - parked_bytes(c.d_head, rt * turns < 4 ? rt * turns : 4) - rt * q; };
+    for (;; p.rt /= 2) {
+        p.turns = kAttendWarps / p.rt;
+        while (p.turns > 1 && left(p.rt, p.turns) / stage < 2 * p.turns) p.turns /= 2;
+        if (p.rt == 1 || left(p.rt, p.turns) / stage >= 2) break;
+    }
+    p.parked = p.rt * p.turns < 4 ? p.rt * p.turns : 4;
+    p.ring = left(p.rt, p.turns) / stage < kRing ? left(p.rt, p.turns) / stage : kRing;
     // Whoever waits for a stage must have seen the one before it in the same place (a barrier tells one phase from the next, not from the
-    // one after): groups of warps and places of the ring go together.
-    p.turns = kAttendWarps / p.rt;
-    while (p.turns > p.ring) p.turns /= 2;
-    p.ring -= p.ring % p.turns;
+    // one after): groups of warps, and producers, have places of the ring of their own.  (All are powers of two, none larger than the ring.)
+    p.producers = kProducers;
+    while (p.producers > p.ring) p.producers /= 2;
+    p.ring -= p.ring % (p.turns > p.producers ? p.turns : p.producers);
     p.row_groups = (tiles + p.rt - 1) / p.rt;
-    p.smem = p.ring * stage + parked_bytes(c.d_head) + p.rt * q;
+    p.smem = p.ring * stage + parked_bytes(c.d_head, p.parked) + p.rt * q;
     p.units = (long long)batch * c.n_kv_heads * p.row_groups;
     p.grid = kv.sms < kMaxGrid ? kv.sms : kMaxGrid;
     p.workspace = kHeadBytes + 2 * (size_t)p.grid * p.rt * 16 * (c.d_head + 2) * 4;
@@ -694,7 +757,7 @@ static cudaError_t launch_attend(const xsm_kv &kv, const AttendArgs &A, const At
     const void *fn = (const void *)attend_kernel<T, TQ, DH>;
     const cudaError_t e = open_kernel(fn, p.smem, false);
     if (e != cudaSuccess) return e;
-    attend_kernel<T, TQ, DH><<<p.grid, (kAttendWarps + 1) * 32, p.smem, st>>>(kv.k_map, kv.v_map, A);
+    attend_kernel<T, TQ, DH><<<p.grid, (kAttendWarps + kProducers) * 32, p.smem, st>>>(kv.k_map, kv.v_map, A);
     return cudaGetLastError();
 }
 template <typename T, typename TQ> static cudaError_t launch_width(const xsm_kv &kv, const AttendArgs &A, const AttendPlan &p, cudaStream_t st) {
@@ -713,7 +776,7 @@ using namespace xsm;
 
 size_t xsm_kv_attend_workspace(const xsm_kv *kv, int batch, int m, int n_heads) {
     if (!kv || batch < 1 || m < 1 || m > XSM_MAX_DRAFT || n_heads < 1 || n_heads > 4096 || n_heads % kv->cfg.n_kv_heads) return 0;
-    const size_t a = plan_attend(*kv, batch, m, n_heads, false).workspace, b = plan_attend(*kv, batch, m, n_heads, true).workspace;
+    const size_t a = plan_attend(*kv, batch, m, n_heads, kv->cfg.dtype).workspace, b = plan_attend(*kv, batch, m, n_heads, XSM_F32).workspace;
     return a > b ? a : b;
 }
 
@@ -729,8 +792,8 @@ xsm_status xsm_kv_attend(const xsm_kv *kv, const xsm_kv_attend_args *a, void *cu
     if (!(fabsf(a->scale) < INFINITY)) return op_failed(XSM_ERR_INVALID_ARG, "scale must be finite");
     if (a->batch == 0) return XSM_OK;
     if (!a->q || !a->out || !a->block_table || !a->lengths || !a->workspace) return op_failed(XSM_ERR_INVALID_ARG, "null argument");
-    const AttendPlan p = plan_attend(*kv, a->batch, a->m, a->n_heads, a->q_dtype == XSM_F32 && c.dtype != XSM_F32);
-    if (p.units > INT_MAX / 4) return op_failed(XSM_ERR_INVALID_ARG, "batch * heads is too large");
+    const AttendPlan p = plan_attend(*kv, a->batch, a->m, a->n_heads, a->q_dtype);
+    if ((double)p.units * ((double)a->max_pages * c.page_size / (kStage * kGranule) + 2) > INT_MAX / 2) return op_failed(XSM_ERR_INVALID_ARG, "batch * heads * positions is too large");
     if (a->workspace_bytes < (int64_t)p.workspace) return op_failed(XSM_ERR_CAPACITY, "the workspace is too small");
     const int per16 = 16 / element_size(a->q_dtype);
     for (int i = 0; i < 3; ++i)
@@ -743,7 +806,7 @@ xsm_status xsm_kv_attend(const xsm_kv *kv, const xsm_kv_attend_args *a, void *cu
     A.partial = reinterpret_cast<float *>((char *)a->workspace + kHeadBytes);
     for (int i = 0; i < 3; ++i) { A.qs[i] = a->q_stride[i]; A.os[i] = a->out_stride[i]; }
     A.batch = a->batch; A.m = a->m; A.heads = a->n_heads; A.group = a->n_heads / c.n_kv_heads; A.kv_heads = c.n_kv_heads;
-    A.rt = p.rt; A.row_groups = p.row_groups; A.n_rows = A.m * A.group; A.ring = p.ring; A.turns = p.turns;
+    A.rt = p.rt; A.row_groups = p.row_groups; A.n_rows = A.m * A.group; A.ring = p.ring; A.turns = p.turns; A.producers = p.producers; A.parked = p.parked;
     A.causal = a->causal != 0; A.window = a->window; A.page = c.page_size; A.max_pages = a->max_pages; A.n_pages = c.n_pages; A.box_rows = kv->box_rows;
     A.c = (float)((double)a->scale * 1.4426950408889634);
     const cudaStream_t st = (cudaStream_t)cuda_stream;
