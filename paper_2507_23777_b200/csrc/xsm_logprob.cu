@@ -1,7 +1,7 @@
 // Log probabilities of given tokens with entropy and top alternatives, and their gradient by the logits.
 //
-// Forward: one pass over a row with a running maximum m, s = sum exp((z - m)/T) and t = sum exp((z - m)/T) (z - m); then
-// lse = m/T + log s, logprob = (z_token - m)/T - log s, entropy = log s - t/(s T).  A block of 256 threads takes a row; where
+// Forward: one pass over a row with a running maximum m, s = sum exp((z - m)/T) and t = sum exp((z - m)/T) (z - m)/T; then
+// lse = m/T + log s, logprob = (z_token - m)/T - log s, entropy = log s - t/s.  A block of 128 threads takes a row; where
 // there are fewer rows than keep the chip busy a cluster of blocks takes a part of the row each and joins through shared memory.
 // Alternatives: the largest logits of every thread bound the k-th largest of the row from below; what reaches the bound, usually little more
 // than k logits, is collected in a second look at the row (out of registers, or the caches) and sorted by counting.
@@ -15,7 +15,7 @@
 namespace xsm {
 
 constexpr int kMaxTop = 32;
-constexpr int kRowThreads = 256, kRowWarps = kRowThreads / 32;
+constexpr int kRowThreads = 128, kRowWarps = kRowThreads / 32;
 constexpr int kAhead = 4;                 // 16-byte pieces that a thread has under way
 constexpr int kCandidates = 512;
 
@@ -25,7 +25,8 @@ struct LogprobArgs {
     int *top_ids;
     float *top_logprobs;
     long long row_ld, token_ld;
-    int vocab, token_bytes, top, cuts;    // cuts: blocks of a cluster, each with a part of the row
+    int vocab, token_bytes, top;
+    int cuts, cut_shift;                  // blocks of a cluster, each with a part of the row: 2^cut_shift
     float inv_t;
 };
 
@@ -59,20 +60,60 @@ template <typename T> struct Pieces {
         return i < head ? i : i >= 32 && i < 32 + tail ? head + pieces * n + i - 32 : -1;
     }
 };
-template <typename T> __device__ __forceinline__ void widen(const uint4 &v, float (&x)[Pieces<T>::n]) {
+// two fp32 numbers that are worked on together
+typedef unsigned long long Two;
+__device__ __forceinline__ Two two(float a, float b) {
+    Two r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ float2 apart(Two v) {
+    float2 r;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+    return r;
+}
+__device__ __forceinline__ Two fma2(Two a, Two b, Two c) {
+    Two r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ Two add2(Two a, Two b) {
+    Two r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ Two mul2(Two a, Two b) {
+    Two r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+// elements 2i and 2i + 1 of a piece
+template <typename T> __device__ __forceinline__ float2 pair(const uint4 &v, int i) {
     const unsigned w[4] = {v.x, v.y, v.z, v.w};
+    if constexpr (sizeof(T) == 4) return make_float2(__uint_as_float(w[2 * i]), __uint_as_float(w[2 * i + 1]));
+    else if constexpr (std::is_same<T, bf16>::value) return make_float2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u));
+    else return __half22float2(*reinterpret_cast<const __half2 *>(&w[i]));
+}
+template <typename T> __device__ __forceinline__ void widen(const uint4 &v, float (&x)[Pieces<T>::n]) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        if constexpr (sizeof(T) == 4) {
-            x[i] = __uint_as_float(w[i]);
-        } else if constexpr (std::is_same<T, bf16>::value) {
-            x[2 * i] = __uint_as_float(w[i] << 16);
-            x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-        } else {
-            const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&w[i]));
-            x[2 * i] = f.x;
-            x[2 * i + 1] = f.y;
-        }
+    for (int i = 0; i < Pieces<T>::n / 2; ++i) {
+        const float2 f = pair<T>(v, i);
+        x[2 * i] = f.x;
+        x[2 * i + 1] = f.y;
+    }
+}
+// largest element of a piece (NaN aside)
+template <typename T> __device__ __forceinline__ float largest(const uint4 &v) {
+    if constexpr (sizeof(T) == 4) {
+        return fmaxf(fmaxf(__uint_as_float(v.x), __uint_as_float(v.y)), fmaxf(__uint_as_float(v.z), __uint_as_float(v.w)));
+    } else if constexpr (std::is_same<T, bf16>::value) {
+        const __nv_bfloat162 *h = reinterpret_cast<const __nv_bfloat162 *>(&v);
+        const __nv_bfloat162 m = __hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3]));
+        return fmaxf(__low2float(m), __high2float(m));
+    } else {
+        const __half2 *h = reinterpret_cast<const __half2 *>(&v);
+        const __half2 m = __hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3]));
+        return fmaxf(__low2float(m), __high2float(m));
     }
 }
 template <typename T> __device__ __forceinline__ uint4 nothing() {      // -infinity everywhere
@@ -80,31 +121,33 @@ template <typename T> __device__ __forceinline__ uint4 nothing() {      // -infi
     return make_uint4(w, w, w, w);
 }
 
-// Running maximum and sums of a part of a row.
+// Running maximum m and sums of a part of a row: s = sum 2^x, t = sum 2^x x, x = (z - m) c with c = log2(e) / T.
 struct Part {
     float m, s, t;
     // the same sums against a maximum that is no smaller
     __device__ __forceinline__ void rebase(float top, float c) {
-        const float d = fmaxf(m - top, -1e30f), f = m == -INFINITY ? 0.f : ex2(d * c);      // (nothing yet: s = t = 0, but -infinity times 0 is none)
+        const float d = fmaxf((m - top) * c, -1e30f), f = m == -INFINITY ? 0.f : ex2(d);      // (nothing yet: s = t = 0, but -infinity times 0 is none)
         t = f * (t + s * d);
         s *= f;
         m = top;
     }
-    __device__ __forceinline__ void join(Part o, float c) {
-        const float top = fmaxf(m, o.m);
+    // over the first `lanes` lanes of a warp, in every one of them
+    __device__ __forceinline__ void join(int lanes, float c) {
+        float top = m;
+        for (int o = lanes / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
         if (m != top) rebase(top, c);
-        if (o.m != top) o.rebase(top, c);
-        s += o.s;
-        t += o.t;
+        for (int o = lanes / 2; o > 0; o >>= 1) {
+            s += __shfl_xor_sync(0xffffffffu, s, o);
+            t += __shfl_xor_sync(0xffffffffu, t, o);
+        }
     }
 };
-template <int N> __device__ __forceinline__ void take(Part &a, const float (&x)[N], float ref, float c, float &s, float &t) {
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-        const float d = x[i] - ref, e = ex2(d * c);
-        s += e;
-        t = fmaf(e, fmaxf(d, -1e30f), t);
-    }
+// Two more elements.  (The difference first: that of the maximum to itself is zero, and nothing overflows.)
+__device__ __forceinline__ void take(float2 z, Two minus_m, Two c, Two &s, Two &t) {
+    const float2 x = apart(mul2(add2(two(z.x, z.y), minus_m), c));
+    const Two e = two(ex2(x.x), ex2(x.y));
+    s = add2(s, e);
+    t = fma2(e, two(fmaxf(x.x, -1e30f), fmaxf(x.y, -1e30f)), t);
 }
 
 struct RowShared {
@@ -112,9 +155,22 @@ struct RowShared {
     unsigned bound[kRowWarps];
     int found;
     unsigned long long key[kRowWarps];
-    unsigned long long candidate[kCandidates];
+    __align__(16) unsigned long long candidate[kCandidates + 8];
     unsigned long long best[kMaxTop];
 };
+
+// how many of n keys are larger than this one (what lies behind them up to a multiple of eight is zero)
+__device__ __forceinline__ int larger(const unsigned long long *keys, int n, unsigned long long key) {
+    int count = 0;
+    for (int k = 0; k < n; k += 8) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const ulonglong2 v = *reinterpret_cast<const ulonglong2 *>(keys + k + 2 * q);
+            count += (v.x > key) + (v.y > key);
+        }
+    }
+    return count;
+}
 
 // The `top` largest of a run one after the other, each the largest below the one before: for rows whose bound collects too many (all
 // alike, or -infinity) or too few (NaN).
@@ -141,14 +197,14 @@ template <typename T> __device__ __noinline__ void best_one_by_one(const T *z, i
     __syncthreads();
 }
 
-template <typename T, bool kTop> __global__ void __launch_bounds__(kRowThreads, 4) logprob_kernel(const __grid_constant__ LogprobArgs A) {
+template <typename T, bool kTop> __global__ void __launch_bounds__(kRowThreads, kTop ? 8 : 12) logprob_kernel(const __grid_constant__ LogprobArgs A) {
     constexpr int N = Pieces<T>::n;
     __shared__ RowShared sh;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int cut = A.cuts > 1 ? (int)cluster_rank() : 0;
-    const long long row = blockIdx.x / A.cuts;
+    const int cut = blockIdx.x & (A.cuts - 1);          // (clusters start at multiples of their size: this is the rank)
+    const long long row = blockIdx.x >> A.cut_shift;
     const T *z = reinterpret_cast<const T *>(A.logits) + row * A.row_ld;
-    const int i0 = (int)((long long)A.vocab * cut / A.cuts), count = (int)((long long)A.vocab * (cut + 1) / A.cuts) - i0;
+    const int i0 = (int)(((long long)A.vocab * cut) >> A.cut_shift), count = (int)(((long long)A.vocab * (cut + 1)) >> A.cut_shift) - i0;
     const Pieces<T> in(z + i0, count);
     const float c = A.inv_t * kLog2e;
     if (kTop && tid == 0) sh.found = 0;
@@ -170,38 +226,26 @@ template <typename T, bool kTop> __global__ void __launch_bounds__(kRowThreads, 
             const int i = at + u * kRowThreads + tid;
             v[u] = i < in.pieces ? in.piece(i) : nothing<T>();
         }
-        float top = at == 0 ? fmaxf(a.m, single) : a.m;
+        float top = at == 0 ? single : a.m;
+        if (!(top == top)) top = a.m;
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u) {
-            float x[N];
-            widen<T>(v[u], x);
-#pragma unroll
-            for (int i = 0; i < N; ++i) top = fmaxf(top, x[i]);
-        }
+        for (int u = 0; u < kAhead; ++u) top = fmaxf(top, largest<T>(v[u]));
         if (top > a.m) a.rebase(top, c);
         const float ref = a.m == -INFINITY ? 0.f : a.m;
-        float s = 0.f, t = 0.f;
+        const Two cc = two(c, c), minus = two(-ref, -ref);
+        Two s = two(0.f, 0.f), t = s;
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u) {
-            float x[N];
-            widen<T>(v[u], x);
-            take(a, x, ref, c, s, t);
-        }
-        if (at == 0) {
-            const float x[1] = {single};
-            take(a, x, ref, c, s, t);
-        }
-        a.s += s;
-        a.t += t;
+        for (int u = 0; u < kAhead; ++u)
+#pragma unroll
+            for (int i = 0; i < N / 2; ++i) take(pair<T>(v[u], i), minus, cc, s, t);
+        if (at == 0) take(make_float2(single, -INFINITY), minus, cc, s, t);
+        const float2 s2 = apart(s), t2 = apart(t);
+        a.s += s2.x + s2.y;
+        a.t += t2.x + t2.y;
     }
     const unsigned mine = kTop ? order_of(a.m) : 0u;
     const int full_warps = min(kRowWarps, max(1, in.pieces / 32));
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-        Part b;
-        b.m = __shfl_xor_sync(0xffffffffu, a.m, o); b.s = __shfl_xor_sync(0xffffffffu, a.s, o); b.t = __shfl_xor_sync(0xffffffffu, a.t, o);
-        a.join(b, c);
-    }
+    a.join(32, c);
     if (kTop) {
         // the j-th largest of the maxima of a warp's threads, as many as make `top` over the warps that are full of pieces: at least `top` logits
         // reach the least of these warps' bounds
@@ -216,9 +260,10 @@ template <typename T, bool kTop> __global__ void __launch_bounds__(kRowThreads, 
     }
     if (lane == 0) sh.part[warp] = a;
     __syncthreads();
-    if (tid == 0) {
-        for (int w = 1; w < kRowWarps; ++w) a.join(sh.part[w], c);
-        if (A.cuts > 1) sh.joined = a;
+    if (warp == 0) {
+        a = lane < kRowWarps ? sh.part[lane] : Part{-INFINITY, 0.f, 0.f};
+        a.join(kRowWarps, c);
+        if (A.cuts > 1 && lane == 0) sh.joined = a;
     }
     if (kTop) {
         unsigned bound = sh.bound[0];
@@ -247,6 +292,7 @@ template <typename T, bool kTop> __global__ void __launch_bounds__(kRowThreads, 
                 for (int u = 0; u < kAhead; ++u) {
                     const int i = at + u * kRowThreads + tid;
                     if (i >= in.pieces) continue;
+                    if (!(largest<T>(v[u]) >= least)) continue;
                     float x[N];
                     widen<T>(v[u], x);
 #pragma unroll
@@ -255,14 +301,17 @@ template <typename T, bool kTop> __global__ void __launch_bounds__(kRowThreads, 
             }
             __syncthreads();
             found = sh.found;
+            if (found <= kCandidates) {
+                if (tid < 8) sh.candidate[found + tid] = 0;
+                __syncthreads();
+            }
         }
         if (found < want || found > kCandidates) {
             best_one_by_one(z + i0, count, i0, want, sh);
         } else {
             for (int i = tid; i < found; i += kRowThreads) {
                 const unsigned long long key = sh.candidate[i];
-                int before = 0;
-                for (int k = 0; k < found; ++k) before += sh.candidate[k] > key;
+                const int before = larger(sh.candidate, found, key);
                 if (before < want) sh.best[before] = key;
             }
         }
@@ -274,29 +323,28 @@ template <typename T, bool kTop> __global__ void __launch_bounds__(kRowThreads, 
         cluster_arrive();
         cluster_wait();
         if (cut == 0) {
-            const uint32_t theirs = smem_u32(&sh.joined);
-            if (tid == 0) {
-                for (int r = 1; r < A.cuts; ++r) {
-                    const uint32_t at = map_rank(theirs, r);
-                    Part b{ld_cluster_f32(at), ld_cluster_f32(at + 4), ld_cluster_f32(at + 8)};
-                    a.join(b, c);
+            if (warp == 0) {
+                a = Part{-INFINITY, 0.f, 0.f};
+                if (lane < A.cuts) {
+                    const uint32_t at = map_rank(smem_u32(&sh.joined), lane);
+                    a = Part{ld_cluster_f32(at), ld_cluster_f32(at + 4), ld_cluster_f32(at + 8)};
                 }
+                a.join(8, c);
             }
             if (kTop) {
                 // the parts' best, in order, side by side; the first of them all
                 const int n = A.cuts * A.top;
-                unsigned long long key = 0;
-                if (tid < n) {
-                    const uint32_t at = map_rank(smem_u32(&sh.best[tid % A.top]), tid / A.top);
+                for (int i = tid; i < n; i += kRowThreads) {
+                    const uint32_t at = map_rank(smem_u32(&sh.best[i % A.top]), i / A.top);
                     const unsigned lo = __float_as_uint(ld_cluster_f32(at)), hi = __float_as_uint(ld_cluster_f32(at + 4));
-                    key = ((unsigned long long)hi << 32) | lo;
-                    sh.candidate[tid] = key;
+                    sh.candidate[i] = ((unsigned long long)hi << 32) | lo;
                 }
+                if (tid < 8) sh.candidate[n + tid] = 0;
                 __syncthreads();
-                if (tid < n) {
-                    int before = 0;
-                    for (int k = 0; k < n; ++k) before += sh.candidate[k] > key || (sh.candidate[k] == key && k < tid);
-                    if (before < A.top) sh.best[before] = key;
+                for (int i = tid; i < n; i += kRowThreads) {
+                    const unsigned long long key = sh.candidate[i];
+                    const int before = larger(sh.candidate, n, key);
+                    if (key != 0 && before < A.top) sh.best[before] = key;
                 }
                 __syncthreads();
             }
@@ -310,7 +358,7 @@ template <typename T, bool kTop> __global__ void __launch_bounds__(kRowThreads, 
         const float log_s = logf(a.s), ref = a.m == -INFINITY ? 0.f : a.m;
         const bool none = a.s == 0.f;                                     // nothing but -infinity
         A.logprob[row] = token < 0 ? 0.f : none ? -INFINITY : (given - ref) * A.inv_t - log_s;
-        A.entropy[row] = none ? 0.f : log_s - a.t / a.s * A.inv_t;
+        A.entropy[row] = none ? 0.f : log_s - a.t / a.s * 0.69314718055994531f;
         A.lse[row] = none ? -INFINITY : ref * A.inv_t + log_s;
         if (kTop) sh.part[0] = Part{ref, log_s, none ? 1.f : 0.f};
     }
@@ -331,17 +379,18 @@ struct GradArgs {
     const float *g_logprob, *g_entropy, *g_lse, *g_top;
     void *d_logits;
     long long row_ld, token_ld, gl_ld, ge_ld, gs_ld, d_ld;
-    int vocab, token_bytes, top, chunks;   // chunks: blocks of a row
+    int vocab, token_bytes, top, per_block;      // pieces of a row that a block takes
     float inv_t;
 };
 
-// The numbers of a row that its elements' gradients are made of, divided by T where they enter linearly.
+// The numbers of a row that its elements' gradients are made of: with x = log2 p = z c - lse', the gradient is -p (total' + ge' x), where
+// total' has the entropy's share and everything the factor 1/T.  A row with nothing left: lse' infinite, so p = 0, and the rest zero.
 struct RowGrad {
-    float lse, entropy, total, ge, inv_t;
-    bool none;
+    float c, lse, total, ge, g;
+    int token;
     __device__ __forceinline__ float of(float z) const {
-        const float logp = fmaf(z, inv_t, -lse), p = ex2(logp * kLog2e);
-        return -p * fmaf(ge, fmaxf(logp, -1e3f) + entropy, total);        // (p is zero below -104: the bound only keeps 0 * -infinity out)
+        const float x = fmaf(z, c, -lse);
+        return -ex2(x) * fmaf(ge, fmaxf(x, -1e3f), total);                // (p is zero below -150: the bound only keeps 0 * -infinity out)
     }
 };
 
@@ -361,109 +410,118 @@ template <typename T> __device__ __forceinline__ uint4 narrow(const float (&x)[P
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-// A block takes kRowThreads * kAhead pieces of a row (and the first of its row the single elements at both ends).
+// A block takes per_block pieces of a row (and the first of its row the single elements at both ends).
 template <typename T, bool kTop> __global__ void __launch_bounds__(kRowThreads) logprob_grad_kernel(const __grid_constant__ GradArgs A) {
-    constexpr int N = Pieces<T>::n;
-    __shared__ unsigned s_marked[kRowThreads];
+    constexpr int N = Pieces<T>::n, kLoads = 4;
+    __shared__ RowGrad s_row;
     __shared__ int s_id[kMaxTop];
     __shared__ float s_g[kMaxTop];
-    const int tid = threadIdx.x, lane = tid & 31, chunk = blockIdx.x % A.chunks;
-    const long long row = blockIdx.x / A.chunks;
+    const int tid = threadIdx.x;
+    const long long row = blockIdx.x;
     const T *z = reinterpret_cast<const T *>(A.logits) + row * A.row_ld;
     T *out = reinterpret_cast<T *>(A.d_logits) + row * A.d_ld;
     const Pieces<T> in(z, A.vocab);
-    const int at0 = chunk * kRowThreads * kAhead;
-    uint4 v[kAhead];
+    const int first = blockIdx.y * A.per_block, last = min(in.pieces, first + A.per_block);
+    uint4 v[kLoads];
+    auto fetch = [&](int at) {
 #pragma unroll
-    for (int u = 0; u < kAhead; ++u) {
-        const int i = at0 + u * kRowThreads + tid;
-        if (i < in.pieces) v[u] = in.piece(i);
-    }
-    const int one = chunk == 0 ? in.single() : -1;
-    const float single = one >= 0 ? to_f(in.p[one]) : 0.f;
-    const long long token = token_at(A.tokens, A.token_bytes, row * A.token_ld);
-    const bool has = token >= 0 && token < A.vocab;
-    const float g = A.g_logprob && has ? A.g_logprob[row * A.gl_ld] * A.inv_t : 0.f;
-    RowGrad r;
-    r.lse = A.lse[row];
-    r.entropy = A.entropy ? A.entropy[row] : 0.f;
-    r.ge = A.g_entropy ? A.g_entropy[row * A.ge_ld] * A.inv_t : 0.f;
-    r.total = g - (A.g_lse ? A.g_lse[row * A.gs_ld] * A.inv_t : 0.f);
-    r.inv_t = A.inv_t;
-    r.none = r.lse == -INFINITY;
-    const int t = has ? (int)token : -1;
-    // which of its pieces hold the token or an alternative, a bit each
-    unsigned marked = 0;
-    auto mark_of = [&](int id, int &owner) {
-        const int i = id - in.head, piece = i / N - at0;
-        owner = -1;
-        if (i < 0 || i >= in.pieces * N || piece < 0 || piece >= kRowThreads * kAhead) return 0u;
-        owner = piece % kRowThreads;
-        return 1u << (piece / kRowThreads);
-    };
-    if (kTop) {
-        const float gk = lane < A.top ? A.g_top[row * A.top + lane] * A.inv_t : 0.f;
-        r.total += warp_sum(gk);
-        s_marked[tid] = 0;
-        __syncthreads();
-        if (tid < A.top) {
-            const int id = A.top_ids[row * A.top + tid];
-            s_id[tid] = id;
-            s_g[tid] = gk;
-            int owner;
-            const unsigned bit = mark_of(id, owner);
-            if (owner >= 0) atomicOr(&s_marked[owner], bit);
+        for (int u = 0; u < kLoads; ++u) {
+            const int i = at + u * kRowThreads + tid;
+            if (i < last) v[u] = in.piece(i);
         }
-        __syncthreads();
-        marked = s_marked[tid];
+    };
+    fetch(first);
+    const int one = blockIdx.y == 0 ? in.single() : -1;
+    const float single = one >= 0 ? to_f(in.p[one]) : 0.f;
+    if (tid < 32) {
+        float more = 0.f;
+        if (kTop) {
+            if (tid < A.top) {
+                more = A.g_top[row * A.top + tid] * A.inv_t;
+                s_id[tid] = A.top_ids[row * A.top + tid];
+                s_g[tid] = more;
+            }
+            more = warp_sum(more);
+        }
+        if (tid == 0) {
+            const long long token = token_at(A.tokens, A.token_bytes, row * A.token_ld);
+            const bool has = token >= 0 && token < A.vocab;
+            const float lse = A.lse[row];
+            const bool none = lse == -INFINITY;
+            RowGrad r;
+            r.token = has ? (int)token : -1;
+            r.g = A.g_logprob && has && !none ? A.g_logprob[row * A.gl_ld] * A.inv_t : 0.f;
+            const float ge = A.g_entropy && !none ? A.g_entropy[row * A.ge_ld] * A.inv_t : 0.f;
+            r.ge = ge * 0.69314718055994531f;
+            r.total = none ? 0.f : r.g + more - (A.g_lse ? A.g_lse[row * A.gs_ld] * A.inv_t : 0.f) + (A.g_entropy ? ge * A.entropy[row] : 0.f);
+            r.lse = none ? INFINITY : lse * kLog2e;
+            r.c = A.inv_t * kLog2e;
+            s_row = r;
+        }
     }
-    if (t >= 0) {
-        int owner;
-        const unsigned bit = mark_of(t, owner);
-        if (owner == tid) marked |= bit;
-    }
+    __syncthreads();
+    const RowGrad r = s_row;
     auto full = [&](float x, int i) {             // of element i, with what falls on it directly
         float d = r.of(x);
-        if (i == t) d += g;
-        if (kTop) for (int k = 0; k < A.top; ++k) if (s_id[k] == i) d += s_g[k];
-        return r.none ? 0.f : d;
+        if (i == r.token) d += r.g;
+        if (kTop && r.lse != INFINITY) for (int k = 0; k < A.top; ++k) if (s_id[k] == i) d += s_g[k];
+        return d;
     };
     if (one >= 0) out[one] = rounded<T>(full(single, one));
     const bool alike = (((uintptr_t)z ^ (uintptr_t)out) & 15) == 0;
+    const Two cc = two(r.c, r.c), lse = two(-r.lse, -r.lse), ge = two(-r.ge, -r.ge), total = two(-r.total, -r.total);
+    for (int at = first; at < last; at += kRowThreads * kLoads) {
+        if (at != first) fetch(at);
+        // which of these pieces hold the token or an alternative, a bit each
+        unsigned marked = 0;
+        auto mark = [&](int id) {
+            if (id < in.head) return;
+            const int piece = (id - in.head) / N - at;
+            if ((piece & (kRowThreads - 1)) == tid && piece >= 0 && piece < kRowThreads * kLoads) marked |= 1u << (piece / kRowThreads);
+        };
+        mark(r.token);
+        if (kTop) for (int k = 0; k < A.top; ++k) mark(s_id[k]);
 #pragma unroll
-    for (int u = 0; u < kAhead; ++u) {
-        const int i = at0 + u * kRowThreads + tid, e = in.head + i * N;
-        if (i >= in.pieces) continue;
-        float x[N];
-        widen<T>(v[u], x);
-        if ((marked >> u) & 1u) {
+        for (int u = 0; u < kLoads; ++u) {
+            const int i = at + u * kRowThreads + tid, e = in.head + i * N;
+            if (i >= last) continue;
+            float d[N];
+            if ((marked >> u) & 1u) {
+                widen<T>(v[u], d);
 #pragma unroll 1
-            for (int k = 0; k < N; ++k) {         // (x stays in registers: the one element that counts is picked by comparison)
-                float y = 0.f;
+                for (int k = 0; k < N; ++k) {         // (they stay in registers: the one whose turn it is is picked by comparison)
+                    float y = 0.f;
 #pragma unroll
-                for (int q = 0; q < N; ++q) if (q == k) y = x[q];
-                y = full(y, e + k);
+                    for (int q = 0; q < N; ++q) if (q == k) y = d[q];
+                    y = full(y, e + k);
 #pragma unroll
-                for (int q = 0; q < N; ++q) if (q == k) x[q] = y;
+                    for (int q = 0; q < N; ++q) if (q == k) d[q] = y;
+                }
+            } else {
+#pragma unroll
+                for (int k = 0; k < N / 2; ++k) {
+                    const float2 y = pair<T>(v[u], k), x = apart(fma2(two(y.x, y.y), cc, lse));
+                    const Two w = fma2(ge, two(fmaxf(x.x, -1e3f), fmaxf(x.y, -1e3f)), total);
+                    const float2 f = apart(mul2(two(ex2(x.x), ex2(x.y)), w));
+                    d[2 * k] = f.x;
+                    d[2 * k + 1] = f.y;
+                }
             }
-        } else {
+            if (alike) {
+                *reinterpret_cast<uint4 *>(out + e) = narrow<T>(d);
+            } else {
 #pragma unroll
-            for (int k = 0; k < N; ++k) x[k] = r.none ? 0.f : r.of(x[k]);
-        }
-        if (alike) {
-            *reinterpret_cast<uint4 *>(out + e) = narrow<T>(x);
-        } else {
-#pragma unroll
-            for (int k = 0; k < N; ++k) out[e + k] = rounded<T>(x[k]);
+                for (int k = 0; k < N; ++k) out[e + k] = rounded<T>(d[k]);
+            }
         }
     }
 }
 
-// Blocks that share a row: as many as the chip takes at a time (four an SM) over the rows, each with 4096 logits at least.
-static int cuts_of(int rows, int vocab, int sms) {
-    int cuts = 1;
-    while (cuts < 8 && (long long)rows * cuts * 2 <= 4LL * sms && vocab / (2 * cuts) >= 4096) cuts *= 2;
-    return cuts;
+// Blocks that share a row, as a power of two: as many as the chip takes at a time (six an SM) over the rows, each with 4096 logits at least.
+static int cut_shift_of(int rows, int vocab, int sms) {
+    int shift = 0;
+    while (shift < 3 && ((long long)rows << (shift + 1)) <= 6LL * sms && (vocab >> (shift + 1)) >= 4096) ++shift;
+    return shift;
 }
 
 static cudaError_t sm_count(int *sms) {
@@ -513,8 +571,9 @@ xsm_status xsm_token_logprobs(const xsm_logprob_args *a, void *cuda_stream) {
     int sms = 0;
     const cudaError_t e = sm_count(&sms);
     if (e != cudaSuccess) return launched(e);
+    const int shift = cut_shift_of(a->rows, a->vocab, sms);
     const LogprobArgs A{a->logits, a->tokens, a->logprob, a->entropy, a->lse, a->top_ids, a->top_logprobs, a->row_stride, a->token_stride,
-                        a->vocab, a->token_bytes, a->top, cuts_of(a->rows, a->vocab, sms), 1.f / a->temperature};
+                        a->vocab, a->token_bytes, a->top, 1 << shift, shift, 1.f / a->temperature};
     const cudaStream_t st = (cudaStream_t)cuda_stream;
     cudaError_t r = cudaSuccess;
     with_dtype(a->dtype, [&](auto t) {
@@ -529,17 +588,19 @@ xsm_status xsm_token_logprobs_grad(const xsm_logprob_grad_args *a, void *cuda_st
     if (const char *m = check_logits(a->logits, a->tokens, a->rows, a->vocab, a->dtype, a->token_bytes, a->top, a->temperature)) return op_failed(XSM_ERR_INVALID_ARG, m);
     if (a->rows == 0) return XSM_OK;
     if (!a->lse || !a->d_logits || (a->g_entropy && !a->entropy) || (a->g_top && a->top && !a->top_ids)) return op_failed(XSM_ERR_INVALID_ARG, "null argument");
-    const int per = kRowThreads * kAhead * 16 / element_size(a->dtype), chunks = (a->vocab + per - 1) / per;
-    if ((long long)a->rows * chunks > 0x7fffffff) return op_failed(XSM_ERR_INVALID_ARG, "rows * vocab is too large");
+    // A block takes 2048 pieces of a row where there are rows enough to fill the chip, else 512.
+    const int pieces = (int)(((long long)a->vocab * element_size(a->dtype) + 15) / 16), per_block = a->rows >= 2048 ? 2048 : 512;
+    const int blocks = pieces > per_block ? (pieces + per_block - 1) / per_block : 1;
+    if (blocks > 65535) return op_failed(XSM_ERR_INVALID_ARG, "vocab is too large");
     const bool top = a->top && a->g_top;
     const GradArgs A{a->logits, a->tokens, a->lse, a->entropy, a->top_ids, a->g_logprob, a->g_entropy, a->g_lse, a->g_top, a->d_logits,
                      a->row_stride, a->token_stride, a->g_logprob_stride, a->g_entropy_stride, a->g_lse_stride, a->d_row_stride,
-                     a->vocab, a->token_bytes, a->top, chunks, 1.f / a->temperature};
+                     a->vocab, a->token_bytes, a->top, per_block, 1.f / a->temperature};
     const cudaStream_t st = (cudaStream_t)cuda_stream;
     with_dtype(a->dtype, [&](auto t) {
         using T = decltype(t);
-        if (top) logprob_grad_kernel<T, true><<<a->rows * chunks, kRowThreads, 0, st>>>(A);
-        else logprob_grad_kernel<T, false><<<a->rows * chunks, kRowThreads, 0, st>>>(A);
+        if (top) logprob_grad_kernel<T, true><<<dim3(a->rows, blocks), kRowThreads, 0, st>>>(A);
+        else logprob_grad_kernel<T, false><<<dim3(a->rows, blocks), kRowThreads, 0, st>>>(A);
     });
     return launched(cudaGetLastError());
 }
