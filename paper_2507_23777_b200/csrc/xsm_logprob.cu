@@ -15,9 +15,8 @@
 namespace xsm {
 
 constexpr int kMaxTop = 32;
-constexpr int kRowThreads = 128, kRowWarps = kRowThreads / 32;
-constexpr int kAhead = 4;                 // 16-byte pieces that a thread has under way
-constexpr int kCandidates = 512;
+constexpr int kBlock = 128;               // threads
+constexpr int kWarpRowBytes = 8192;       // rows up to this size are a warp's each, where there are many
 
 struct LogprobArgs {
     const void *logits, *tokens;
@@ -25,7 +24,7 @@ struct LogprobArgs {
     int *top_ids;
     float *top_logprobs;
     long long row_ld, token_ld;
-    int vocab, token_bytes, top;
+    int rows, vocab, token_bytes, top;
     int cuts, cut_shift;                  // blocks of a cluster, each with a part of the row: 2^cut_shift
     float inv_t;
 };
@@ -54,11 +53,8 @@ template <typename T> struct Pieces {
         tail = count - head - pieces * n;
     }
     __device__ __forceinline__ uint4 piece(int i) const { return reinterpret_cast<const uint4 *>(p + head)[i]; }
-    // this thread's single element, if it has one: its index in the run, or -1
-    __device__ __forceinline__ int single() const {
-        const int i = threadIdx.x;
-        return i < head ? i : i >= 32 && i < 32 + tail ? head + pieces * n + i - 32 : -1;
-    }
+    // thread i's single element, if it has one: its index in the run, or -1 (there are fewer than eight at each end)
+    __device__ __forceinline__ int single(int i) const { return i < head ? i : i >= 8 && i < 8 + tail ? head + pieces * n + i - 8 : -1; }
 };
 // two fp32 numbers that are worked on together
 typedef unsigned long long Two;
@@ -150,13 +146,18 @@ __device__ __forceinline__ void take(float2 z, Two minus_m, Two c, Two &s, Two &
     t = fma2(e, two(fmaxf(x.x, -1e30f), fmaxf(x.y, -1e30f)), t);
 }
 
-struct RowShared {
-    Part part[kRowWarps], joined;
-    unsigned bound[kRowWarps];
+// Warps that share a row: a block's four, or one, and the block has four rows.
+template <int W> __device__ __forceinline__ void meet() {
+    if (W == 1) __syncwarp();
+    else __syncthreads();
+}
+template <int W> struct RowShared {
+    static constexpr int room = W == 1 ? 256 : 512;
+    __align__(16) unsigned long long candidate[room + 8];
+    unsigned long long key[W], best[kMaxTop];
+    Part part[W], joined;
+    unsigned bound[W];
     int found;
-    unsigned long long key[kRowWarps];
-    __align__(16) unsigned long long candidate[kCandidates + 8];
-    unsigned long long best[kMaxTop];
 };
 
 // how many of n keys are larger than this one (what lies behind them up to a multiple of eight is zero)
@@ -174,11 +175,12 @@ __device__ __forceinline__ int larger(const unsigned long long *keys, int n, uns
 
 // The `top` largest of a run one after the other, each the largest below the one before: for rows whose bound collects too many (all
 // alike, or -infinity) or too few (NaN).
-template <typename T> __device__ __noinline__ void best_one_by_one(const T *z, int count, int index0, int top, RowShared &sh) {
+template <typename T, int W> __device__ __noinline__ void best_one_by_one(const T *z, int count, int index0, int top, RowShared<W> &sh) {
+    const int tid = W == 1 ? threadIdx.x & 31 : threadIdx.x;
     unsigned long long last = ~0ull;
     for (int k = 0; k < top; ++k) {
         unsigned long long best = 0;
-        for (int i = threadIdx.x; i < count; i += kRowThreads) {
+        for (int i = tid; i < count; i += 32 * W) {
             const unsigned long long key = rank_key(to_f(z[i]), index0 + i);
             if (key < last && key > best) best = key;
         }
@@ -187,24 +189,28 @@ template <typename T> __device__ __noinline__ void best_one_by_one(const T *z, i
             const unsigned long long w = __shfl_xor_sync(0xffffffffu, best, o);
             best = w > best ? w : best;
         }
-        __syncthreads();
-        if ((threadIdx.x & 31) == 0) sh.key[threadIdx.x >> 5] = best;
-        __syncthreads();
+        meet<W>();
+        if ((tid & 31) == 0) sh.key[tid >> 5] = best;
+        meet<W>();
         last = 0;
-        for (int w = 0; w < kRowWarps; ++w) last = sh.key[w] > last ? sh.key[w] : last;
-        if (threadIdx.x == 0) sh.best[k] = last;
+#pragma unroll
+        for (int w = 0; w < W; ++w) last = sh.key[w] > last ? sh.key[w] : last;
+        if (tid == 0) sh.best[k] = last;
     }
-    __syncthreads();
+    meet<W>();
 }
 
-template <typename T, bool kTop> __global__ void __launch_bounds__(kRowThreads, kTop ? 8 : 12) logprob_kernel(const __grid_constant__ LogprobArgs A) {
-    constexpr int N = Pieces<T>::n;
-    __shared__ RowShared sh;
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int cut = blockIdx.x & (A.cuts - 1);          // (clusters start at multiples of their size: this is the rank)
-    const long long row = blockIdx.x >> A.cut_shift;
+template <typename T, bool kTop, int W> __global__ void __launch_bounds__(kBlock, kTop || sizeof(T) == 4 ? 8 : 12) logprob_kernel(const __grid_constant__ LogprobArgs A) {
+    constexpr int N = Pieces<T>::n, kThreads = 32 * W, kAhead = 32 / N;      // pieces that a thread has under way: 32 logits
+    __shared__ RowShared<W> shared[W == 1 ? kBlock / 32 : 1];
+    RowShared<W> &sh = shared[W == 1 ? threadIdx.x >> 5 : 0];
+    const int tid = W == 1 ? threadIdx.x & 31 : threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int cut = W == 1 ? 0 : blockIdx.x & (A.cuts - 1);          // (clusters start at multiples of their size: this is the rank)
+    const long long row = W == 1 ? (long long)blockIdx.x * (kBlock / 32) + (threadIdx.x >> 5) : blockIdx.x >> A.cut_shift;
+    if (W == 1 && row >= A.rows) return;
     const T *z = reinterpret_cast<const T *>(A.logits) + row * A.row_ld;
-    const int i0 = (int)(((long long)A.vocab * cut) >> A.cut_shift), count = (int)(((long long)A.vocab * (cut + 1)) >> A.cut_shift) - i0;
+    const int i0 = W == 1 ? 0 : (int)(((long long)A.vocab * cut) >> A.cut_shift);
+    const int count = (W == 1 ? A.vocab : (int)(((long long)A.vocab * (cut + 1)) >> A.cut_shift)) - i0;
     const Pieces<T> in(z + i0, count);
     const float c = A.inv_t * kLog2e;
     if (kTop && tid == 0) sh.found = 0;
@@ -217,19 +223,33 @@ template <typename T, bool kTop> __global__ void __launch_bounds__(kRowThreads, 
     }
 
     Part a{-INFINITY, 0.f, 0.f};
-    const int one = in.single();
+    const int one = in.single(tid);
     const float single = one >= 0 ? to_f(in.p[one]) : -INFINITY;
     uint4 v[kAhead];
-    for (int at = 0; at == 0 || at < in.pieces; at += kRowThreads * kAhead) {
+    // kTop: the largest logits of this thread's best pieces, the best two's places
+    float best[3] = {-INFINITY, -INFINITY, -INFINITY};
+    int place[2] = {in.pieces, in.pieces};
+    for (int at = 0; at == 0 || at < in.pieces; at += kThreads * kAhead) {
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
-            const int i = at + u * kRowThreads + tid;
+            const int i = at + u * kThreads + tid;
             v[u] = i < in.pieces ? in.piece(i) : nothing<T>();
         }
         float top = at == 0 ? single : a.m;
         if (!(top == top)) top = a.m;
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u) top = fmaxf(top, largest<T>(v[u]));
+        for (int u = 0; u < kAhead; ++u) {
+            const float x = largest<T>(v[u]);
+            top = fmaxf(top, x);
+            if (kTop) {
+                const bool first = x > best[0], second = x > best[1];
+                best[2] = second ? best[1] : fmaxf(best[2], x);
+                place[1] = first ? place[0] : second ? at + u * kThreads + tid : place[1];
+                best[1] = first ? best[0] : fmaxf(best[1], x);
+                place[0] = first ? at + u * kThreads + tid : place[0];
+                best[0] = fmaxf(best[0], x);
+            }
+        }
         if (top > a.m) a.rebase(top, c);
         const float ref = a.m == -INFINITY ? 0.f : a.m;
         const Two cc = two(c, c), minus = two(-ref, -ref);
@@ -244,81 +264,98 @@ template <typename T, bool kTop> __global__ void __launch_bounds__(kRowThreads, 
         a.t += t2.x + t2.y;
     }
     const unsigned mine = kTop ? order_of(a.m) : 0u;
-    const int full_warps = min(kRowWarps, max(1, in.pieces / 32));
+    const int full_warps = min(W, max(1, in.pieces / 32));
     a.join(32, c);
+    unsigned bound = 0;
     if (kTop) {
         // the j-th largest of the maxima of a warp's threads, as many as make `top` over the warps that are full of pieces: at least `top` logits
         // reach the least of these warps' bounds
         bool in_play = true;
-        unsigned bound = 0;
         for (int j = 0; j < A.top; j += full_warps) {
             bound = __reduce_max_sync(0xffffffffu, in_play ? mine : 0u);
             const unsigned who = __ballot_sync(0xffffffffu, in_play && mine == bound);
             if (who && lane == __ffs(who) - 1) in_play = false;
         }
-        if (lane == 0) sh.bound[warp] = bound;
+        if (W > 1 && lane == 0) sh.bound[warp] = bound;
     }
-    if (lane == 0) sh.part[warp] = a;
-    __syncthreads();
-    if (warp == 0) {
-        a = lane < kRowWarps ? sh.part[lane] : Part{-INFINITY, 0.f, 0.f};
-        a.join(kRowWarps, c);
-        if (A.cuts > 1 && lane == 0) sh.joined = a;
+    if (W > 1) {
+        if (lane == 0) sh.part[warp] = a;
+        meet<W>();
+        if (warp == 0) {
+            a = lane < W ? sh.part[lane] : Part{-INFINITY, 0.f, 0.f};
+            a.join(W, c);
+            if (A.cuts > 1 && lane == 0) sh.joined = a;
+        }
+    } else {
+        meet<W>();
     }
     if (kTop) {
-        unsigned bound = sh.bound[0];
+        if (W > 1) {
+            bound = sh.bound[0];
 #pragma unroll
-        for (int w = 1; w < kRowWarps; ++w) if (w < full_warps) bound = min(bound, sh.bound[w]);
+            for (int w = 1; w < W; ++w) if (w < full_warps) bound = min(bound, sh.bound[w]);
+        }
         const float least = of_order(bound);
         const int want = min(A.top, count);
         int found = 0;
-        if (bound > order_of(-INFINITY) || count <= kCandidates) {
+        if (bound > order_of(-INFINITY) || count <= RowShared<W>::room) {
             auto offer = [&](float x, int i) {
                 if (x >= least) {
                     const int at = atomicAdd(&sh.found, 1);
-                    if (at < kCandidates) sh.candidate[at] = rank_key(x, i0 + i);
+                    if (at < RowShared<W>::room) sh.candidate[at] = rank_key(x, i0 + i);
                 }
             };
+            auto offer_piece = [&](const uint4 &w, int i) {
+                if (!(largest<T>(w) >= least)) return;
+                float x[N];
+                widen<T>(w, x);
+#pragma unroll
+                for (int k = 0; k < N; ++k) offer(x[k], in.head + i * N + k);
+            };
             if (one >= 0) offer(single, one);
-            const bool kept = in.pieces <= kRowThreads * kAhead;          // the row's pieces are still in registers
-            for (int at = 0; at < in.pieces; at += kRowThreads * kAhead) {
+            if (in.pieces <= kThreads * kAhead) {             // the row's pieces are still in registers
 #pragma unroll
                 for (int u = 0; u < kAhead; ++u) {
-                    const int i = at + u * kRowThreads + tid;
-                    if (i >= in.pieces) continue;
-                    if (!kept) v[u] = in.piece(i);
+                    const int i = u * kThreads + tid;
+                    if (i < in.pieces) offer_piece(v[u], i);
+                }
+            } else {
+                // a second look at the pieces that reach the bound: a thread's best two, and where there may be more all of its pieces, one for every lane
+#pragma unroll
+                for (int q = 0; q < 2; ++q) {
+                    const bool worth = best[q] >= least && best[2] < least && place[q] < in.pieces;
+                    v[q] = worth ? in.piece(place[q]) : nothing<T>();
                 }
 #pragma unroll
-                for (int u = 0; u < kAhead; ++u) {
-                    const int i = at + u * kRowThreads + tid;
-                    if (i >= in.pieces) continue;
-                    if (!(largest<T>(v[u]) >= least)) continue;
-                    float x[N];
-                    widen<T>(v[u], x);
-#pragma unroll
-                    for (int k = 0; k < N; ++k) offer(x[k], in.head + i * N + k);
+                for (int q = 0; q < 2; ++q)
+                    if (best[q] >= least && best[2] < least && place[q] < in.pieces) offer_piece(v[q], place[q]);
+                unsigned who = __ballot_sync(0xffffffffu, best[2] >= least);
+                while (who) {
+                    const int p = warp * 32 + __ffs(who) - 1;
+                    who &= who - 1;
+                    for (int at = lane * kThreads + p; at < in.pieces; at += 32 * kThreads) offer_piece(in.piece(at), at);
                 }
             }
-            __syncthreads();
+            meet<W>();
             found = sh.found;
-            if (found <= kCandidates) {
+            if (found <= RowShared<W>::room) {
                 if (tid < 8) sh.candidate[found + tid] = 0;
-                __syncthreads();
+                meet<W>();
             }
         }
-        if (found < want || found > kCandidates) {
-            best_one_by_one(z + i0, count, i0, want, sh);
+        if (found < want || found > RowShared<W>::room) {
+            best_one_by_one<T, W>(z + i0, count, i0, want, sh);
         } else {
-            for (int i = tid; i < found; i += kRowThreads) {
+            for (int i = tid; i < found; i += kThreads) {
                 const unsigned long long key = sh.candidate[i];
                 const int before = larger(sh.candidate, found, key);
                 if (before < want) sh.best[before] = key;
             }
         }
         if (tid < A.top && tid >= want) sh.best[tid] = 0;                 // a part of the row that is shorter than `top`
-        __syncthreads();
+        meet<W>();
     }
-    if (A.cuts > 1) {
+    if (W > 1 && A.cuts > 1) {
         __syncwarp();
         cluster_arrive();
         cluster_wait();
@@ -334,19 +371,19 @@ template <typename T, bool kTop> __global__ void __launch_bounds__(kRowThreads, 
             if (kTop) {
                 // the parts' best, in order, side by side; the first of them all
                 const int n = A.cuts * A.top;
-                for (int i = tid; i < n; i += kRowThreads) {
+                for (int i = tid; i < n; i += kThreads) {
                     const uint32_t at = map_rank(smem_u32(&sh.best[i % A.top]), i / A.top);
                     const unsigned lo = __float_as_uint(ld_cluster_f32(at)), hi = __float_as_uint(ld_cluster_f32(at + 4));
                     sh.candidate[i] = ((unsigned long long)hi << 32) | lo;
                 }
                 if (tid < 8) sh.candidate[n + tid] = 0;
-                __syncthreads();
-                for (int i = tid; i < n; i += kRowThreads) {
+                meet<W>();
+                for (int i = tid; i < n; i += kThreads) {
                     const unsigned long long key = sh.candidate[i];
                     const int before = larger(sh.candidate, n, key);
                     if (key != 0 && before < A.top) sh.best[before] = key;
                 }
-                __syncthreads();
+                meet<W>();
             }
         }
         __syncwarp();
@@ -354,20 +391,22 @@ template <typename T, bool kTop> __global__ void __launch_bounds__(kRowThreads, 
         cluster_wait();
         if (cut != 0) return;
     }
+    // lane 0 has the row's sums
+    const float log_s = logf(a.s), ref = a.m == -INFINITY ? 0.f : a.m;
+    const bool none = a.s == 0.f;                                     // nothing but -infinity
     if (tid == 0) {
-        const float log_s = logf(a.s), ref = a.m == -INFINITY ? 0.f : a.m;
-        const bool none = a.s == 0.f;                                     // nothing but -infinity
         A.logprob[row] = token < 0 ? 0.f : none ? -INFINITY : (given - ref) * A.inv_t - log_s;
         A.entropy[row] = none ? 0.f : log_s - a.t / a.s * 0.69314718055994531f;
         A.lse[row] = none ? -INFINITY : ref * A.inv_t + log_s;
-        if (kTop) sh.part[0] = Part{ref, log_s, none ? 1.f : 0.f};
     }
-    if (kTop) {
-        __syncthreads();
-        if (tid < A.top) {
-            const int id = (int)~(unsigned)sh.best[tid];
-            A.top_ids[row * A.top + tid] = id;
-            A.top_logprobs[row * A.top + tid] = sh.part[0].t != 0.f ? -INFINITY : (to_f(z[id]) - sh.part[0].m) * A.inv_t - sh.part[0].s;
+    if (kTop && warp == 0) {
+        const float m0 = __shfl_sync(0xffffffffu, ref, 0), log0 = __shfl_sync(0xffffffffu, none ? INFINITY : log_s, 0);
+        if (lane < A.top) {
+            const unsigned long long key = sh.best[lane];
+            A.top_ids[row * A.top + lane] = (int)~(unsigned)key;
+            // (its logit out of the key, where NaN has none)
+            const float x = (key >> 32) == 0 ? NAN : of_order((unsigned)(key >> 32));
+            A.top_logprobs[row * A.top + lane] = log0 == INFINITY ? -INFINITY : (x - m0) * A.inv_t - log0;
         }
     }
 }
@@ -379,15 +418,14 @@ struct GradArgs {
     const float *g_logprob, *g_entropy, *g_lse, *g_top;
     void *d_logits;
     long long row_ld, token_ld, gl_ld, ge_ld, gs_ld, d_ld;
-    int vocab, token_bytes, top, per_block;      // pieces of a row that a block takes
+    int rows, vocab, token_bytes, top, per_block;      // per_block: pieces of a row that a block takes
     float inv_t;
 };
 
 // The numbers of a row that its elements' gradients are made of: with x = log2 p = z c - lse', the gradient is -p (total' + ge' x), where
 // total' has the entropy's share and everything the factor 1/T.  A row with nothing left: lse' infinite, so p = 0, and the rest zero.
 struct RowGrad {
-    float c, lse, total, ge, g;
-    int token;
+    float c, lse, total, ge;
     __device__ __forceinline__ float of(float z) const {
         const float x = fmaf(z, c, -lse);
         return -ex2(x) * fmaf(ge, fmaxf(x, -1e3f), total);                // (p is zero below -150: the bound only keeps 0 * -infinity out)
@@ -410,14 +448,19 @@ template <typename T> __device__ __forceinline__ uint4 narrow(const float (&x)[P
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-// A block takes per_block pieces of a row (and the first of its row the single elements at both ends).
-template <typename T, bool kTop> __global__ void __launch_bounds__(kRowThreads) logprob_grad_kernel(const __grid_constant__ GradArgs A) {
-    constexpr int N = Pieces<T>::n, kLoads = 4;
-    __shared__ RowGrad s_row;
-    __shared__ int s_id[kMaxTop];
-    __shared__ float s_g[kMaxTop];
-    const int tid = threadIdx.x;
-    const long long row = blockIdx.x;
+// W warps take per_block pieces of a row (and the first of its row the single elements at both ends).  What falls on single logits directly,
+// the token's and the alternatives' gradients, is a list; when all elements are written, the listed ones among them are written again with
+// it, from logits that were read before (the gradient may take the place of the logits).
+template <typename T, bool kTop, int W> __global__ void __launch_bounds__(kBlock) logprob_grad_kernel(const __grid_constant__ GradArgs A) {
+    constexpr int N = Pieces<T>::n, kLoads = 4, kThreads = 32 * W, kGroups = W == 1 ? kBlock / 32 : 1;
+    __shared__ RowGrad rows[kGroups];
+    __shared__ int ids[kGroups][kMaxTop + 1];
+    __shared__ float gs[kGroups][kMaxTop + 1];
+    const int tid = W == 1 ? threadIdx.x & 31 : threadIdx.x, group = W == 1 ? threadIdx.x >> 5 : 0;
+    int *const s_id = ids[group];
+    float *const s_g = gs[group];
+    const long long row = (long long)blockIdx.x * kGroups + group;
+    if (W == 1 && row >= A.rows) return;
     const T *z = reinterpret_cast<const T *>(A.logits) + row * A.row_ld;
     T *out = reinterpret_cast<T *>(A.d_logits) + row * A.d_ld;
     const Pieces<T> in(z, A.vocab);
@@ -426,86 +469,80 @@ template <typename T, bool kTop> __global__ void __launch_bounds__(kRowThreads) 
     auto fetch = [&](int at) {
 #pragma unroll
         for (int u = 0; u < kLoads; ++u) {
-            const int i = at + u * kRowThreads + tid;
+            const int i = at + u * kThreads + tid;
             if (i < last) v[u] = in.piece(i);
         }
     };
     fetch(first);
-    const int one = blockIdx.y == 0 ? in.single() : -1;
+    const int one = blockIdx.y == 0 ? in.single(tid) : -1;
     const float single = one >= 0 ? to_f(in.p[one]) : 0.f;
+    const int listed = kTop ? A.top + 1 : 1;
     if (tid < 32) {
+        const float lse = A.lse[row];
+        const bool none = lse == -INFINITY;
         float more = 0.f;
         if (kTop) {
             if (tid < A.top) {
-                more = A.g_top[row * A.top + tid] * A.inv_t;
-                s_id[tid] = A.top_ids[row * A.top + tid];
-                s_g[tid] = more;
+                more = none ? 0.f : A.g_top[row * A.top + tid] * A.inv_t;
+                s_id[tid + 1] = A.top_ids[row * A.top + tid];
+                s_g[tid + 1] = more;
             }
             more = warp_sum(more);
         }
         if (tid == 0) {
             const long long token = token_at(A.tokens, A.token_bytes, row * A.token_ld);
             const bool has = token >= 0 && token < A.vocab;
-            const float lse = A.lse[row];
-            const bool none = lse == -INFINITY;
-            RowGrad r;
-            r.token = has ? (int)token : -1;
-            r.g = A.g_logprob && has && !none ? A.g_logprob[row * A.gl_ld] * A.inv_t : 0.f;
+            const float g = A.g_logprob && has && !none ? A.g_logprob[row * A.gl_ld] * A.inv_t : 0.f;
             const float ge = A.g_entropy && !none ? A.g_entropy[row * A.ge_ld] * A.inv_t : 0.f;
+            s_id[0] = has ? (int)token : -1;
+            s_g[0] = g;
+            RowGrad r;
             r.ge = ge * 0.69314718055994531f;
-            r.total = none ? 0.f : r.g + more - (A.g_lse ? A.g_lse[row * A.gs_ld] * A.inv_t : 0.f) + (A.g_entropy ? ge * A.entropy[row] : 0.f);
+            r.total = none ? 0.f : g + more - (A.g_lse ? A.g_lse[row * A.gs_ld] * A.inv_t : 0.f) + (A.g_entropy ? ge * A.entropy[row] : 0.f);
             r.lse = none ? INFINITY : lse * kLog2e;
             r.c = A.inv_t * kLog2e;
-            s_row = r;
+            rows[group] = r;
         }
     }
-    __syncthreads();
-    const RowGrad r = s_row;
-    auto full = [&](float x, int i) {             // of element i, with what falls on it directly
-        float d = r.of(x);
-        if (i == r.token) d += r.g;
-        if (kTop && r.lse != INFINITY) for (int k = 0; k < A.top; ++k) if (s_id[k] == i) d += s_g[k];
-        return d;
-    };
-    if (one >= 0) out[one] = rounded<T>(full(single, one));
+    meet<W>();
+    const RowGrad r = rows[group];
+    // this thread's entries of the list whose logits are of this block's part, and these
+    constexpr int kEntries = W == 1 ? 2 : 1;
+    static_assert(kEntries * kThreads > kMaxTop, "the list has a thread for every entry");
+    float listed_z[kEntries];
+    int listed_id[kEntries];
+#pragma unroll
+    for (int q = 0; q < kEntries; ++q) {
+        const int k = tid + q * kThreads;
+        int id = k < listed ? s_id[k] : -1;
+        if (id >= A.vocab) id = -1;
+        if (id >= in.head && id < in.head + in.pieces * N) {
+            const int piece = (id - in.head) / N;
+            if (piece < first || piece >= last) id = -1;
+        } else if (blockIdx.y != 0) {
+            id = -1;
+        }
+        listed_id[q] = id;
+        listed_z[q] = id >= 0 ? to_f(z[id]) : 0.f;
+    }
+    meet<W>();
+    if (one >= 0) out[one] = rounded<T>(r.of(single));
     const bool alike = (((uintptr_t)z ^ (uintptr_t)out) & 15) == 0;
     const Two cc = two(r.c, r.c), lse = two(-r.lse, -r.lse), ge = two(-r.ge, -r.ge), total = two(-r.total, -r.total);
-    for (int at = first; at < last; at += kRowThreads * kLoads) {
+    for (int at = first; at < last; at += kThreads * kLoads) {
         if (at != first) fetch(at);
-        // which of these pieces hold the token or an alternative, a bit each
-        unsigned marked = 0;
-        auto mark = [&](int id) {
-            if (id < in.head) return;
-            const int piece = (id - in.head) / N - at;
-            if ((piece & (kRowThreads - 1)) == tid && piece >= 0 && piece < kRowThreads * kLoads) marked |= 1u << (piece / kRowThreads);
-        };
-        mark(r.token);
-        if (kTop) for (int k = 0; k < A.top; ++k) mark(s_id[k]);
 #pragma unroll
         for (int u = 0; u < kLoads; ++u) {
-            const int i = at + u * kRowThreads + tid, e = in.head + i * N;
+            const int i = at + u * kThreads + tid, e = in.head + i * N;
             if (i >= last) continue;
             float d[N];
-            if ((marked >> u) & 1u) {
-                widen<T>(v[u], d);
-#pragma unroll 1
-                for (int k = 0; k < N; ++k) {         // (they stay in registers: the one whose turn it is is picked by comparison)
-                    float y = 0.f;
 #pragma unroll
-                    for (int q = 0; q < N; ++q) if (q == k) y = d[q];
-                    y = full(y, e + k);
-#pragma unroll
-                    for (int q = 0; q < N; ++q) if (q == k) d[q] = y;
-                }
-            } else {
-#pragma unroll
-                for (int k = 0; k < N / 2; ++k) {
-                    const float2 y = pair<T>(v[u], k), x = apart(fma2(two(y.x, y.y), cc, lse));
-                    const Two w = fma2(ge, two(fmaxf(x.x, -1e3f), fmaxf(x.y, -1e3f)), total);
-                    const float2 f = apart(mul2(two(ex2(x.x), ex2(x.y)), w));
-                    d[2 * k] = f.x;
-                    d[2 * k + 1] = f.y;
-                }
+            for (int k = 0; k < N / 2; ++k) {
+                const float2 y = pair<T>(v[u], k), x = apart(fma2(two(y.x, y.y), cc, lse));
+                const Two w = fma2(ge, two(fmaxf(x.x, -1e3f), fmaxf(x.y, -1e3f)), total);
+                const float2 f = apart(mul2(two(ex2(x.x), ex2(x.y)), w));
+                d[2 * k] = f.x;
+                d[2 * k + 1] = f.y;
             }
             if (alike) {
                 *reinterpret_cast<uint4 *>(out + e) = narrow<T>(d);
@@ -514,6 +551,15 @@ template <typename T, bool kTop> __global__ void __launch_bounds__(kRowThreads) 
                 for (int k = 0; k < N; ++k) out[e + k] = rounded<T>(d[k]);
             }
         }
+    }
+    meet<W>();
+#pragma unroll
+    for (int q = 0; q < kEntries; ++q) {
+        const int id = listed_id[q];
+        if (id < 0) continue;
+        float d = r.of(listed_z[q]);
+        for (int k = 0; k < listed; ++k) d += s_id[k] == id ? s_g[k] : 0.f;
+        out[id] = rounded<T>(d);
     }
 }
 
@@ -535,10 +581,17 @@ static cudaError_t sm_count(int *sms) {
     return cudaSuccess;
 }
 
-template <typename T, bool kTop> static cudaError_t launch_logprob(const LogprobArgs &A, int rows, cudaStream_t st) {
+// Short rows are a warp's each, where there are enough of them.
+static bool by_warp(int rows, long long row_bytes, int sms) { return row_bytes <= kWarpRowBytes && rows >= 4 * sms; }
+
+template <typename T, bool kTop> static cudaError_t launch_logprob(const LogprobArgs &A, bool warps, cudaStream_t st) {
+    if (warps) {
+        logprob_kernel<T, kTop, 1><<<(A.rows + kBlock / 32 - 1) / (kBlock / 32), kBlock, 0, st>>>(A);
+        return cudaGetLastError();
+    }
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(rows * A.cuts));
-    cfg.blockDim = dim3(kRowThreads);
+    cfg.gridDim = dim3((unsigned)(A.rows * A.cuts));
+    cfg.blockDim = dim3(kBlock);
     cfg.stream = st;
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeClusterDimension;
@@ -546,7 +599,12 @@ template <typename T, bool kTop> static cudaError_t launch_logprob(const Logprob
     at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
     cfg.attrs = at;
     cfg.numAttrs = A.cuts > 1 ? 1 : 0;
-    return cudaLaunchKernelEx(&cfg, logprob_kernel<T, kTop>, A);
+    return cudaLaunchKernelEx(&cfg, logprob_kernel<T, kTop, kBlock / 32>, A);
+}
+template <typename T, bool kTop> static cudaError_t launch_grad(const GradArgs &A, int blocks, bool warps, cudaStream_t st) {
+    if (warps) logprob_grad_kernel<T, kTop, 1><<<(A.rows + kBlock / 32 - 1) / (kBlock / 32), kBlock, 0, st>>>(A);
+    else logprob_grad_kernel<T, kTop, kBlock / 32><<<dim3(A.rows, blocks), kBlock, 0, st>>>(A);
+    return cudaGetLastError();
 }
 
 static const char *check_logits(const void *logits, const void *tokens, int rows, int vocab, int dtype, int token_bytes, int top, float temperature) {
@@ -571,14 +629,15 @@ xsm_status xsm_token_logprobs(const xsm_logprob_args *a, void *cuda_stream) {
     int sms = 0;
     const cudaError_t e = sm_count(&sms);
     if (e != cudaSuccess) return launched(e);
-    const int shift = cut_shift_of(a->rows, a->vocab, sms);
+    const bool warps = by_warp(a->rows, (long long)a->vocab * element_size(a->dtype), sms);
+    const int shift = warps ? 0 : cut_shift_of(a->rows, a->vocab, sms);
     const LogprobArgs A{a->logits, a->tokens, a->logprob, a->entropy, a->lse, a->top_ids, a->top_logprobs, a->row_stride, a->token_stride,
-                        a->vocab, a->token_bytes, a->top, 1 << shift, shift, 1.f / a->temperature};
+                        a->rows, a->vocab, a->token_bytes, a->top, 1 << shift, shift, 1.f / a->temperature};
     const cudaStream_t st = (cudaStream_t)cuda_stream;
     cudaError_t r = cudaSuccess;
     with_dtype(a->dtype, [&](auto t) {
         using T = decltype(t);
-        r = a->top ? launch_logprob<T, true>(A, a->rows, st) : launch_logprob<T, false>(A, a->rows, st);
+        r = a->top ? launch_logprob<T, true>(A, warps, st) : launch_logprob<T, false>(A, warps, st);
     });
     return launched(r);
 }
@@ -588,19 +647,23 @@ xsm_status xsm_token_logprobs_grad(const xsm_logprob_grad_args *a, void *cuda_st
     if (const char *m = check_logits(a->logits, a->tokens, a->rows, a->vocab, a->dtype, a->token_bytes, a->top, a->temperature)) return op_failed(XSM_ERR_INVALID_ARG, m);
     if (a->rows == 0) return XSM_OK;
     if (!a->lse || !a->d_logits || (a->g_entropy && !a->entropy) || (a->g_top && a->top && !a->top_ids)) return op_failed(XSM_ERR_INVALID_ARG, "null argument");
+    int sms = 0;
+    const cudaError_t e = sm_count(&sms);
+    if (e != cudaSuccess) return launched(e);
+    const long long row_bytes = (long long)a->vocab * element_size(a->dtype);
+    const bool warps = by_warp(a->rows, row_bytes, sms), top = a->top && a->g_top;
     // A block takes 2048 pieces of a row where there are rows enough to fill the chip, else 512.
-    const int pieces = (int)(((long long)a->vocab * element_size(a->dtype) + 15) / 16), per_block = a->rows >= 2048 ? 2048 : 512;
+    const int pieces = (int)((row_bytes + 15) / 16), per_block = warps ? pieces : a->rows >= 2048 ? 2048 : 512;
     const int blocks = pieces > per_block ? (pieces + per_block - 1) / per_block : 1;
     if (blocks > 65535) return op_failed(XSM_ERR_INVALID_ARG, "vocab is too large");
-    const bool top = a->top && a->g_top;
     const GradArgs A{a->logits, a->tokens, a->lse, a->entropy, a->top_ids, a->g_logprob, a->g_entropy, a->g_lse, a->g_top, a->d_logits,
                      a->row_stride, a->token_stride, a->g_logprob_stride, a->g_entropy_stride, a->g_lse_stride, a->d_row_stride,
-                     a->vocab, a->token_bytes, a->top, per_block, 1.f / a->temperature};
+                     a->rows, a->vocab, a->token_bytes, a->top, per_block, 1.f / a->temperature};
     const cudaStream_t st = (cudaStream_t)cuda_stream;
+    cudaError_t r = cudaSuccess;
     with_dtype(a->dtype, [&](auto t) {
         using T = decltype(t);
-        if (top) logprob_grad_kernel<T, true><<<dim3(a->rows, blocks), kRowThreads, 0, st>>>(A);
-        else logprob_grad_kernel<T, false><<<dim3(a->rows, blocks), kRowThreads, 0, st>>>(A);
+        r = top ? launch_grad<T, true>(A, blocks, warps, st) : launch_grad<T, false>(A, blocks, warps, st);
     });
-    return launched(cudaGetLastError());
+    return launched(r);
 }
