@@ -17,6 +17,7 @@ import torch
 from . import binding
 
 _DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+_TOKENS = {torch.int64: 8, torch.int32: 4}
 # the argument structures of include/xsm.h, packed in their order
 _APPEND = struct.Struct("8P13q8i")
 _ATTEND = struct.Struct("7P8q7if")
@@ -26,6 +27,9 @@ _GRAD = struct.Struct("10P6q5if")
 TokenLogprobs = namedtuple("TokenLogprobs", "logprob entropy lse top_ids top_logprobs")
 
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
+
+
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
 def _check(status: int):
@@ -38,23 +42,20 @@ def _need(ok, what: str):
         raise ValueError(what)
 
 
-def _ptr(t):
-    return 0 if t is None else t.data_ptr()
-
-
-def _here(t) -> int:
-    """The index of a tensor's device, which has to be the current one."""
+def _need_here(t):
+    """A tensor on the current device."""
     i = t.get_device()
-    if i < 0:
-        raise ValueError("the tensors must be on a CUDA device; there is no CPU path")
-    if i != torch.cuda.current_device():
-        raise ValueError(f"the tensors are on cuda:{i}, which is not the current device")
-    return i
+    _need(i >= 0, "the tensors must be on a CUDA device; there is no CPU path")
+    _need(i == _current_device(), f"the tensors are on cuda:{i}, which is not the current device")
 
 
-def _ints(t, n: int, device: int, what: str):
-    if t.dtype is not torch.int32 or t.shape != (n,) or t.stride(0) != 1 and n > 1 or t.get_device() != device:
-        raise ValueError(f"{what} must be a contiguous int32 tensor of {n} elements on cuda:{device}")
+def _need_ints(t, n: int, device: int, what: str):
+    _need(t.dtype is torch.int32 and tuple(t.shape) == (n,) and (n < 2 or t.stride(0) == 1) and t.get_device() == device,
+          f"{what} must be a contiguous int32 tensor of {n} elements on cuda:{device}")
+
+
+def _empty(shape, strides, dtype, device):
+    return torch.empty_strided(shape, strides, dtype=dtype, device=device)      # (the quickest of torch's ways to new memory)
 
 
 def rope_table(n_positions: int, dims: int, theta: float = 10000.0, device="cuda"):
@@ -80,12 +81,14 @@ class PagedCache:
         _need(k.dim() == 4 and k.dtype in _DTYPES, "the pools must be [n_pages, n_kv_heads, page_size, d_head] of fp32, bf16 or fp16")
         _need(v.shape == k.shape and v.dtype == k.dtype and v.stride() == k.stride() and v.device == k.device, "both pools must be alike")
         _need(k.stride(3) == 1, "the elements of a row must be neighbours")
-        self.device = _here(k)
+        _need_here(k)
+        self.device = k.get_device()
         self.k, self.v, self.dtype = k, v, k.dtype
         self.n_pages, self.n_kv_heads, self.page_size, self.d_head = k.shape
         cfg = binding.KvConfig(*(s if n > 1 else k.shape[3] for s, n in zip((k.stride(0), k.stride(1), k.stride(2)), k.shape)), *k.shape,
                                _DTYPES[k.dtype])
-        self._ws, self._ws_bytes = {}, {}
+        self.scale = self.d_head ** -0.5
+        self._ws, self._ws_bytes = {}, {}          # by stream: a workspace and its size; by shape of a call: what it needs
         _check(self.lib.xsm_kv_create(C.byref(cfg), k.data_ptr(), v.data_ptr(), C.byref(self._h)))
 
     def __del__(self):
@@ -93,56 +96,92 @@ class PagedCache:
         if h:
             self.lib.xsm_kv_destroy(h)
 
-    def _rows(self, x, what: str, heads=None):
-        """Checks [batch, m, heads, d_head]; the strides."""
-        if x.dim() != 4 or x.shape[3] != self.d_head or heads is not None and x.shape[2] != heads:
-            raise ValueError(f"{what} must be [batch, m, {'n_heads' if heads is None else heads}, {self.d_head}], not {list(x.shape)}")
-        if x.get_device() != self.device:
-            raise ValueError(f"{what} must be on cuda:{self.device}")
-        s = x.stride()
-        if s[3] != 1:
-            raise ValueError(f"the elements of a head of {what} must be neighbours")
-        return s[:3]
+    # What is wrong with a call's arguments, told one by one.  (The calls look at all of it at once and come here when something is.)
+    def _need_rows(self, x, what: str, heads=None):
+        _need(x.dim() == 4 and x.shape[3] == self.d_head and (heads is None or x.shape[2] == heads),
+              f"{what} must be [batch, m, {'n_heads' if heads is None else heads}, {self.d_head}], not {list(x.shape)}")
+        _need_here(x)
+        _need(x.get_device() == self.device, f"{what} must be on cuda:{self.device}")
+        _need(x.stride(3) == 1, f"the elements of a head of {what} must be neighbours")
 
-    def _table(self, table, batch: int):
-        if table.dtype is not torch.int32 or table.dim() != 2 or table.shape[0] != batch or table.get_device() != self.device or \
-                table.shape[1] > 1 and table.stride(1) != 1:
-            raise ValueError(f"the block table must be int32 [{batch}, max_pages] on cuda:{self.device}")
-        return table.stride(0), table.shape[1]
+    def _need_table(self, table, batch: int):
+        _need(table.dtype is torch.int32 and table.dim() == 2 and table.shape[0] == batch and table.get_device() == self.device and
+              (table.shape[1] < 2 or table.stride(1) == 1), f"the block table must be int32 [{batch}, max_pages] on cuda:{self.device}")
+
+    def _refuse_append(self, k, v, block_table, starts, counts, q, rope, out):
+        self._need_rows(k, "k", self.n_kv_heads)
+        self._need_rows(v, "v", self.n_kv_heads)
+        _need(v.shape == k.shape and v.dtype is k.dtype and k.dtype in _DTYPES, "k and v must be alike, of fp32, bf16 or fp16")
+        self._need_table(block_table, k.shape[0])
+        _need_ints(starts, k.shape[0], self.device, "starts")
+        if counts is not None:
+            _need_ints(counts, k.shape[0], self.device, "counts")
+        if q is not None:
+            self._need_rows(q, "q")
+            _need(q.shape[:2] == k.shape[:2] and q.dtype is k.dtype, "q must have the batch, the tokens and the type of k")
+            self._need_rows(out, "out", q.shape[2])
+            _need(out.shape == q.shape and out.dtype is q.dtype, "out must have the shape and the type of q")
+        _need(rope is None or rope.dtype is torch.float32 and rope.dim() == 3 and rope.shape[2] == 2 and rope.is_contiguous() and
+              rope.get_device() == self.device, f"rope must be contiguous float32 [positions, dims / 2, 2] on cuda:{self.device}")
+        raise ValueError("the arguments of append do not go together")
+
+    def _refuse_attend(self, q, block_table, lengths, counts, out, lse):
+        self._need_rows(q, "q")
+        _need(q.dtype in _DTYPES, "q must be of fp32, bf16 or fp16")
+        self._need_table(block_table, q.shape[0])
+        _need_ints(lengths, q.shape[0], self.device, "lengths")
+        if counts is not None:
+            _need_ints(counts, q.shape[0], self.device, "counts")
+        self._need_rows(out, "out")
+        _need(out.shape == q.shape and out.dtype is q.dtype, "out must have the shape and the type of q")
+        n = list(q.shape[:3])
+        _need(list(lse.shape) == n and lse.dtype is torch.float32 and lse.is_contiguous() and lse.get_device() == self.device,
+              f"lse must be contiguous float32 {n} on cuda:{self.device}")
+        raise ValueError("the arguments of attend do not go together")
 
     def append(self, k, v, block_table, starts, counts=None, q=None, rope=None, interleaved=False, out=None):
         """Writes k and v, [batch, m, n_kv_heads, d_head], to positions starts[b] + j (j < counts[b]) of every sequence; keys, and queries
         q [batch, m, n_heads, d_head], are rotated by `rope` (float32 [positions, dims / 2, 2], see rope_table).  Returns the rotated
         queries in `out` (a new tensor, or the one given; it may be q), or None without q."""
-        device = _here(k)
-        ks, vs = self._rows(k, "k", self.n_kv_heads), self._rows(v, "v", self.n_kv_heads)
-        batch, m = k.shape[:2]
-        if v.shape != k.shape or v.dtype is not k.dtype or k.dtype not in _DTYPES:
-            raise ValueError("k and v must be alike, of fp32, bf16 or fp16")
-        ld, pages = self._table(block_table, batch)
-        _ints(starts, batch, self.device, "starts")
-        if counts is not None:
-            _ints(counts, batch, self.device, "counts")
-        qs = os = (0, 0, 0)
-        heads = positions = dims = 0
-        if q is not None:
-            qs, heads = self._rows(q, "q"), q.shape[2]
-            if q.shape[:2] != k.shape[:2] or q.dtype is not k.dtype:
-                raise ValueError("q must have the batch, the tokens and the type of k")
+        device, dtype, shape, ks, vs, table = self.device, k.dtype, k.shape, k.stride(), v.stride(), block_table.shape
+        qs = os = (0, 0, 0, 1)
+        heads = positions = half = 0
+        ok = len(shape) == 4 and shape == v.shape and len(table) == 2 and dtype in _DTYPES
+        if ok:
+            batch, m, kv_heads, d = shape
+            ok = (kv_heads == self.n_kv_heads and d == self.d_head and ks[3] == vs[3] == 1 and v.dtype is dtype and table[0] == batch and
+                  starts.shape == (batch,) and block_table.dtype is starts.dtype is torch.int32 and k.get_device() == device == v.get_device() and
+                  block_table.get_device() == device == starts.get_device() == _current_device())
+        if ok and q is not None:
+            qs, q_shape = q.stride(), q.shape
             if out is None:
-                out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-            os = self._rows(out, "out", heads)
-            if out.shape != q.shape or out.dtype is not q.dtype:
-                raise ValueError("out must have the shape and the type of q")
+                out = torch.empty(q_shape, dtype=q.dtype, device=q.device)
+            os = out.stride()
+            ok = (len(q_shape) == 4 and q_shape == out.shape and qs[3] == os[3] == 1 and q_shape[0] == batch and q_shape[1] == m and q_shape[3] == d and
+                  q.dtype is dtype is out.dtype and q.get_device() == device == out.get_device())
+            if ok:
+                heads = q_shape[2]
         else:
-            out = None
-        if rope is not None:
-            if rope.dtype is not torch.float32 or rope.dim() != 3 or rope.shape[2] != 2 or not rope.is_contiguous() or rope.get_device() != self.device:
-                raise ValueError(f"rope must be contiguous float32 [positions, dims / 2, 2] on cuda:{self.device}")
-            positions, dims = rope.shape[0], 2 * rope.shape[1]
-        _check(self.lib.xsm_kv_append(self._h, _APPEND.pack(
-            _ptr(q), k.data_ptr(), v.data_ptr(), _ptr(out), block_table.data_ptr(), starts.data_ptr(), _ptr(counts), _ptr(rope),
-            *qs, *ks, *vs, *os, ld, batch, m, heads, _DTYPES[k.dtype], pages, positions, dims, bool(interleaved)), _raw_stream(device)))
+            out = None if q is None else out
+        if ok and rope is not None:
+            r = rope.shape
+            ok = len(r) == 3 and r[2] == 2 and rope.dtype is torch.float32 and rope.is_contiguous() and rope.get_device() == device
+            if ok:
+                positions, half, _ = r
+        if ok:
+            ts = block_table.stride()
+            ok = (table[1] < 2 or ts[1] == 1) and (batch < 2 or starts.stride(0) == 1)
+        if ok and counts is not None:
+            ok = counts.shape == (batch,) and counts.dtype is torch.int32 and counts.get_device() == device and (batch < 2 or counts.stride(0) == 1)
+        if not ok:
+            self._refuse_append(k, v, block_table, starts, counts, q, rope, out if out is not None else q)
+        status = self.lib.xsm_kv_append(self._h, _APPEND.pack(
+            0 if q is None else q.data_ptr(), k.data_ptr(), v.data_ptr(), 0 if out is None else out.data_ptr(), block_table.data_ptr(),
+            starts.data_ptr(), 0 if counts is None else counts.data_ptr(), 0 if rope is None else rope.data_ptr(),
+            qs[0], qs[1], qs[2], ks[0], ks[1], ks[2], vs[0], vs[1], vs[2], os[0], os[1], os[2], ts[0],
+            batch, m, heads, _DTYPES[dtype], table[1], positions, 2 * half, interleaved), _raw_stream(device))
+        if status:
+            _check(status)
         return out
 
     def _workspace(self, stream: int, batch: int, m: int, heads: int):
@@ -150,69 +189,80 @@ class PagedCache:
         need = self._ws_bytes.get((batch, m, heads))
         if need is None:
             need = self._ws_bytes[batch, m, heads] = max(16, self.lib.xsm_kv_attend_workspace(self._h, batch, m, heads))
-        ws = self._ws.get(stream)
-        if ws is None or ws.numel() < need:
-            ws = torch.zeros(need, dtype=torch.uint8, device=self.k.device)
-            if torch.cuda.is_current_stream_capturing():
-                return ws          # the graph's own: zeroed whenever it is replayed
-            self._ws[stream] = ws
-        return ws
+        ws, size = self._ws.get(stream, (None, 0))
+        if size < need:
+            ws, size = torch.zeros(need, dtype=torch.uint8, device=self.k.device), need
+            if not torch.cuda.is_current_stream_capturing():      # (a graph's own is zeroed whenever it is replayed)
+                self._ws[stream] = ws, size
+        return ws, size
 
     def attend(self, q, block_table, lengths, counts=None, causal=True, window=0, scale=None, out=None, lse=None):
         """Attention of the newest tokens: q [batch, m, n_heads, d_head] over the first lengths[b] positions of every sequence, the new ones
         included.  Query j of n = counts[b] (m without counts) sees positions up to lengths[b] - n + j (all with causal=False), and
         of these the last `window` (0: all).  Returns (out, lse): out like q, lse float32 [batch, m, n_heads], the logarithm of the sum
         of exp(scale q.k), -inf where nothing is seen."""
-        device = _here(q)
-        qs = self._rows(q, "q")
-        batch, m, heads, _ = q.shape
-        if q.dtype not in _DTYPES:
-            raise ValueError("q must be of fp32, bf16 or fp16")
+        device, shape, qs, dtype, table = self.device, q.shape, q.stride(), q.dtype, block_table.shape
         if q.requires_grad and torch.is_grad_enabled():
             raise ValueError("attend has no gradient: call it under torch.no_grad()")
-        ld, pages = self._table(block_table, batch)
-        _ints(lengths, batch, self.device, "lengths")
-        if counts is not None:
-            _ints(counts, batch, self.device, "counts")
         if out is None:
-            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        elif out.shape != q.shape or out.dtype is not q.dtype:
-            raise ValueError("out must have the shape and the type of q")
-        os = self._rows(out, "out")
+            out = torch.empty(shape, dtype=dtype, device=q.device)
+        rows = shape[:3]
         if lse is None:
-            lse = torch.empty((batch, m, heads), dtype=torch.float32, device=q.device)
-        elif lse.shape != (batch, m, heads) or lse.dtype is not torch.float32 or not lse.is_contiguous() or lse.get_device() != self.device:
-            raise ValueError(f"lse must be contiguous float32 [{batch}, {m}, {heads}] on cuda:{self.device}")
+            lse = torch.empty(rows, dtype=torch.float32, device=q.device)
+        os = out.stride()
+        ok = len(shape) == 4 and len(table) == 2 and shape == out.shape and lse.shape == rows and dtype in _DTYPES
+        if ok:
+            batch, m, heads, d = shape
+            ts = block_table.stride()
+            ok = (d == self.d_head and qs[3] == os[3] == 1 and table[0] == batch and (table[1] < 2 or ts[1] == 1) and lengths.shape == (batch,) and
+                  (batch < 2 or lengths.stride(0) == 1) and out.dtype is dtype and lse.dtype is torch.float32 and lse.is_contiguous() and
+                  block_table.dtype is lengths.dtype is torch.int32 and q.get_device() == device == out.get_device() == lse.get_device() and
+                  block_table.get_device() == device == lengths.get_device() == _current_device())
+        if ok and counts is not None:
+            ok = counts.shape == (batch,) and counts.dtype is torch.int32 and counts.get_device() == device and (batch < 2 or counts.stride(0) == 1)
+        if not ok:
+            self._refuse_attend(q, block_table, lengths, counts, out, lse)
         stream = _raw_stream(device)
-        ws = self._workspace(stream, batch, m, heads)
-        _check(self.lib.xsm_kv_attend(self._h, _ATTEND.pack(
-            q.data_ptr(), out.data_ptr(), lse.data_ptr(), block_table.data_ptr(), lengths.data_ptr(), _ptr(counts), ws.data_ptr(),
-            *qs, *os, ld, ws.numel(), batch, m, heads, _DTYPES[q.dtype], pages, bool(causal), window,
-            self.d_head ** -0.5 if scale is None else scale), stream))
+        ws, ws_bytes = self._workspace(stream, batch, m, heads)
+        status = self.lib.xsm_kv_attend(self._h, _ATTEND.pack(
+            q.data_ptr(), out.data_ptr(), lse.data_ptr(), block_table.data_ptr(), lengths.data_ptr(), 0 if counts is None else counts.data_ptr(),
+            ws.data_ptr(), qs[0], qs[1], qs[2], os[0], os[1], os[2], ts[0], ws_bytes, batch, m, heads, _DTYPES[dtype], table[1], causal, window,
+            self.scale if scale is None else scale), stream)
+        if status:
+            _check(status)
         return out, lse
 
 
 def _check_logits(logits, tokens):
-    device = _here(logits)
-    if logits.dim() != 2 or logits.dtype not in _DTYPES or logits.stride(1) != 1 and logits.shape[1] > 1:
-        raise ValueError("logits must be [rows, vocab] of fp32, bf16 or fp16 with neighbouring elements in a row")
-    if tokens.dim() != 1 or tokens.shape[0] != logits.shape[0] or tokens.get_device() != device or \
-            tokens.dtype is not torch.int64 and tokens.dtype is not torch.int32:
-        raise ValueError(f"tokens must be int32 or int64 [{logits.shape[0]}] on cuda:{device}")
-    return device
+    """(device, rows, vocab, row stride, token stride) of arguments that go together."""
+    device, shape = logits.get_device(), logits.shape
+    if len(shape) != 2 or logits.dtype not in _DTYPES:
+        raise ValueError("logits must be [rows, vocab] of fp32, bf16 or fp16")
+    rows, vocab = shape
+    ld, step = logits.stride()
+    if step != 1 and vocab > 1:
+        raise ValueError("the logits of a row must be neighbours")
+    if device < 0 or device != _current_device():
+        _need_here(logits)
+    if tokens.shape != (rows,) or tokens.get_device() != device or tokens.dtype not in _TOKENS:
+        raise ValueError(f"tokens must be int32 or int64 [{rows}] on cuda:{device}")
+    return device, rows, vocab, ld, tokens.stride(0)
 
 
 def _forward(logits, tokens, top, temperature):
-    device = _check_logits(logits, tokens)
-    rows, vocab = logits.shape
-    logprob, entropy, lse = torch.empty((3, rows), dtype=torch.float32, device=logits.device).unbind(0)
+    device, rows, vocab, ld, token_ld = _check_logits(logits, tokens)
+    where = logits.device
+    logprob, entropy, lse = (_empty((rows,), (1,), torch.float32, where) for _ in range(3))
     ids = alt = None
     if top > 0:
-        ids = torch.empty((rows, top), dtype=torch.int32, device=logits.device)
-        alt = torch.empty((rows, top), dtype=torch.float32, device=logits.device)
-    _check(binding.load().xsm_token_logprobs(_LOGPROB.pack(
-        logits.data_ptr(), tokens.data_ptr(), logprob.data_ptr(), entropy.data_ptr(), lse.data_ptr(), _ptr(ids), _ptr(alt),
-        logits.stride(0), tokens.stride(0), rows, vocab, _DTYPES[logits.dtype], tokens.element_size(), top, temperature), _raw_stream(device)))
+        ids = _empty((rows, top), (top, 1), torch.int32, where)
+        alt = _empty((rows, top), (top, 1), torch.float32, where)
+    status = binding.load().xsm_token_logprobs(_LOGPROB.pack(
+        logits.data_ptr(), tokens.data_ptr(), logprob.data_ptr(), entropy.data_ptr(), lse.data_ptr(), 0 if ids is None else ids.data_ptr(),
+        0 if ids is None else alt.data_ptr(), ld, token_ld, rows, vocab, _DTYPES[logits.dtype], _TOKENS[tokens.dtype], top, temperature),
+        _raw_stream(device))
+    if status:
+        _check(status)
     return TokenLogprobs(logprob, entropy, lse, ids, alt)
 
 
@@ -228,30 +278,32 @@ def token_logprobs_grad(logits, tokens, result, grad_logprob=None, grad_entropy=
     """The gradient by the logits, in their type, of sum(grad_logprob * logprob) + sum(grad_entropy * entropy) + ... of what token_logprobs
     returned as `result` for the same logits, tokens and temperature.  grad_*: float32 [rows], grad_top [rows, top]; each may be
     missing.  out: a tensor like logits for the gradient, which may be the logits themselves."""
-    device = _check_logits(logits, tokens)
-    rows, vocab = logits.shape
+    device, rows, vocab, ld, token_ld = _check_logits(logits, tokens)
     if out is None:
-        out = torch.empty((rows, vocab), dtype=logits.dtype, device=logits.device)
+        out = _empty((rows, vocab), (vocab, 1), logits.dtype, logits.device)
     elif out.shape != logits.shape or out.dtype is not logits.dtype or out.get_device() != device or out.stride(1) != 1 and vocab > 1 or \
             out.stride(0) < vocab and rows > 1:
         raise ValueError("out must be like logits, with rows of their own")
-    for t in (result.lse, result.entropy):
-        if t.shape != (rows,) or t.dtype is not torch.float32 or t.get_device() != device or t.stride(0) != 1 and rows > 1:
+    lse, entropy, ids = result.lse, result.entropy, result.top_ids
+    for t in (lse, entropy):
+        if t.shape != (rows,) or t.dtype is not torch.float32 or t.get_device() != device or rows > 1 and t.stride(0) != 1:
             raise ValueError("result must be what token_logprobs returned for these logits")
     gl, gl_ld = _row_grad(grad_logprob, rows, device, "grad_logprob")
     ge, ge_ld = _row_grad(grad_entropy, rows, device, "grad_entropy")
     gs, gs_ld = _row_grad(grad_lse, rows, device, "grad_lse")
-    top = ids = 0
+    top = alternatives = gt = 0
     if grad_top is not None:
-        ids = result.top_ids
         if ids is None or grad_top.shape != ids.shape or grad_top.dtype is not torch.float32 or not grad_top.is_contiguous() or \
-                grad_top.get_device() != device or ids.dtype is not torch.int32 or not ids.is_contiguous() or ids.get_device() != device:
+                grad_top.get_device() != device or ids.shape[0] != rows or ids.dtype is not torch.int32 or not ids.is_contiguous() or \
+                ids.get_device() != device:
             raise ValueError("grad_top must be contiguous float32 [rows, top] beside the result's top_ids")
-        top, ids = ids.shape[1], ids.data_ptr()
-    _check(binding.load().xsm_token_logprobs_grad(_GRAD.pack(
-        logits.data_ptr(), tokens.data_ptr(), result.lse.data_ptr(), result.entropy.data_ptr(), ids, gl, ge, gs, _ptr(grad_top),
-        out.data_ptr(), logits.stride(0), tokens.stride(0), gl_ld, ge_ld, gs_ld, out.stride(0), rows, vocab, _DTYPES[logits.dtype],
-        tokens.element_size(), top, temperature), _raw_stream(device)))
+        top, alternatives, gt = ids.shape[1], ids.data_ptr(), grad_top.data_ptr()
+    status = binding.load().xsm_token_logprobs_grad(_GRAD.pack(
+        logits.data_ptr(), tokens.data_ptr(), lse.data_ptr(), entropy.data_ptr(), alternatives, gl, ge, gs, gt, out.data_ptr(),
+        ld, token_ld, gl_ld, ge_ld, gs_ld, out.stride(0), rows, vocab, _DTYPES[logits.dtype], _TOKENS[tokens.dtype], top, temperature),
+        _raw_stream(device))
+    if status:
+        _check(status)
     return out
 
 
