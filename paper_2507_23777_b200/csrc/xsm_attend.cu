@@ -22,7 +22,10 @@
 namespace xsm {
 
 constexpr int kStage = 32;            // positions of a stage
-constexpr int kGranule = 4;           // stages that are never cut apart
+constexpr int kGranule = 4, kOpening = 3;      // stages that are never cut apart; granules that a unit counts for beside its stages
+// Units up to this many bytes of keys and values are not cut at all: a CTA reads 46 GB/s of a busy chip's and about 100 alone, and joining what two of
+// them have done takes 3 us.
+constexpr int kWholeBytes = 128 * 1024;
 constexpr int kAttendWarps = 8, kProducers = 4;
 constexpr int kRing = 16;             // most stages in shared memory
 // Workspace: status word and counters, which every call leaves at zero, in a place that does not depend on the call; then the partial results.
@@ -37,6 +40,7 @@ struct AttendArgs {
     float *partial;                   // two places for every CTA
     long long qs[3], os[3], table_ld;
     int batch, m, heads, group, kv_heads;
+    int whole, element;               // stages of a unit that is not cut, at most; bytes of a pool's element
     int rt, row_groups, n_rows;       // row tiles of a unit, units that share a key head, query rows of a key head
     int causal, window, page, max_pages, n_pages, box_rows;
     int parked;                       // warps that park their state at the end of a unit
@@ -79,11 +83,12 @@ __device__ __forceinline__ Span span_of(const AttendArgs &A, int b) {
     s.first_end = A.causal ? s.end - s.nq + 1 : s.end;
     s.first_begin = A.window > 0 ? max(0, s.first_end - A.window) : 0;
     s.last_begin = A.window > 0 ? max(0, s.end - A.window) : 0;
-    s.base = s.first_begin / A.box_rows * A.box_rows;
+    s.base = s.first_begin & ~(A.box_rows - 1);
     s.stages = max(1, (s.end - s.base + kStage - 1) / kStage);
     return s;
 }
-__device__ __forceinline__ int granules(const Span &s) { return (s.stages + kGranule - 1) / kGranule; }
+// (a unit takes a granule's time more than its stages do: queries, joining of warps, output)
+__device__ __forceinline__ int granules(int stages) { return (stages + kGranule - 1) / kGranule + kOpening; }
 
 // The run of granules of this CTA, and where it starts.  Every warp works it out for itself.  (The host has made sure that the granules
 // of all units fit 31 bits.)
@@ -99,15 +104,19 @@ struct Run {
 };
 __device__ __forceinline__ Run run_of(const AttendArgs &A, int units) {
     const int lane = threadIdx.x & 31;
-    int sum = 0, first = 0;                  // first: of the first 32 sequences, which most calls end with
+    int sum = 0, all = 0, first = 0;         // granules; stages; stages of the first 32 sequences, which most calls end with
     for (int b = lane; b < A.batch; b += 32) {
-        const int g = granules(span_of(A, b));
-        if (b == lane) first = g;
-        sum += g;
+        const int stages = span_of(A, b).stages;
+        if (b == lane) first = stages;
+        sum += granules(stages);
+        all += stages;
     }
     Run r;
     const int total = (int)__reduce_add_sync(0xffffffffu, (unsigned)sum) * units;
-    r.ctas = min((int)gridDim.x, total);     // every one of them has a granule at least
+    // Few long units: a unit's parts are read by their CTAs side by side, n stages of 32 * 2 * d_head elements, and joined by one, C rows of d_head
+    // sums, both at about the same bytes a second, so C = sqrt(16 * element size * n / rows) parts are the quickest.
+    const float parts = sqrtf(16.f * A.element * (float)__reduce_add_sync(0xffffffffu, (unsigned)all) / (float)A.batch / (float)min(A.n_rows, A.rt * 16));
+    r.ctas = min(min((int)gridDim.x, total), (int)fminf((float)A.batch * units * fmaxf(parts, 1.f), 65535.f));      // every one of them has a granule at least
     r.quot = total / r.ctas;
     r.rem = total - r.quot * r.ctas;
     r.at = r.start(blockIdx.x);
@@ -118,24 +127,32 @@ __device__ __forceinline__ Run run_of(const AttendArgs &A, int units) {
         r.end = r.at;
         return r;
     }
-    int before = 0;
-    for (int b0 = 0; b0 < A.batch; b0 += 32) {
-        const int b = b0 + lane, mine = b >= A.batch ? 0 : b0 == 0 ? first : granules(span_of(A, b));
+    // where both ends lie; one inside a unit that is not cut, or in front of a unit's first stage, goes to the unit's beginning
+    int ends[2] = {r.at, r.end};
+    int before = 0, open = 2;
+    for (int b0 = 0; b0 < A.batch && open; b0 += 32) {
+        const int b = b0 + lane, stages = b < A.batch ? b0 == 0 ? first : span_of(A, b).stages : 0, mine = b < A.batch ? granules(stages) : 0;
         int up = mine;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
             const int v = __shfl_up_sync(0xffffffffu, up, o);
             if (lane >= o) up += v;
         }
-        const unsigned past = __ballot_sync(0xffffffffu, b < A.batch && (before + up) * units > r.at);
-        if (past) {
-            const int l = __ffs(past) - 1;
-            r.b = b0 + l;
-            r.before = (before + __shfl_sync(0xffffffffu, up - mine, l)) * units;
-            break;
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const int at = e == 0 ? r.at : r.end;
+            const unsigned past = __ballot_sync(0xffffffffu, b < A.batch && (before + up) * units > at);
+            if (!past || before * units > at) continue;
+            const int l = __ffs(past) - 1, per = __shfl_sync(0xffffffffu, mine, l), start = (before + __shfl_sync(0xffffffffu, up - mine, l)) * units;
+            const int unit = start + (at - start) / per * per;
+            if (__shfl_sync(0xffffffffu, stages, l) <= A.whole || at - unit <= kOpening) ends[e] = unit;
+            if (e == 0) { r.b = b0 + l; r.before = start; }
+            --open;
         }
         before += __shfl_sync(0xffffffffu, up, 31);
     }
+    r.at = ends[0];
+    r.end = ends[1];
     return r;
 }
 
@@ -150,14 +167,14 @@ template <typename F> __device__ __forceinline__ void walk(const AttendArgs &A, 
     Run r = run_of(A, units);
     while (r.at < r.end) {
         const Span sp = span_of(A, r.b);
-        const int per = granules(sp), behind = r.before + per * units;
+        const int per = granules(sp.stages), behind = r.before + per * units;
         while (r.at < r.end && r.at < behind) {
             Segment s;
             const int rel = r.at - r.before;
             s.unit = rel / per;
             const int g0 = rel - s.unit * per, g1 = min(per, g0 + (r.end - r.at));
-            s.stage0 = g0 * kGranule;
-            s.stage1 = min(sp.stages, g1 * kGranule);
+            s.stage0 = max(0, g0 - kOpening) * kGranule;
+            s.stage1 = min(sp.stages, (g1 - kOpening) * kGranule);
             s.first = r.before + s.unit * per;
             s.last = s.first + per;
             s.whole = g0 == 0 && g1 == per;
@@ -321,9 +338,12 @@ __device__ __forceinline__ void attend_stage(uint32_t q_base, uint32_t stage, fl
                                              const int (&token)[2], RowState<DH> &st) {
     using S = Shape<T, DH>;
     const int lane = threadIdx.x & 31, t = lane & 3;
-    float s[4][4];
+    float s[4][4], small[4][4];               // fp32 operands, or queries in two parts: products of the smaller parts, in a chain of their own
 #pragma unroll
-    for (int nt = 0; nt < 4; ++nt) s[nt][0] = s[nt][1] = s[nt][2] = s[nt][3] = 0.f;
+    for (int nt = 0; nt < 4; ++nt) {
+        s[nt][0] = s[nt][1] = s[nt][2] = s[nt][3] = 0.f;
+        small[nt][0] = small[nt][1] = small[nt][2] = small[nt][3] = 0.f;
+    }
     const int row = (lane & 7) + ((lane >> 4) << 3);
 #pragma unroll
     for (int ks = 0; ks < S::steps; ++ks) {
@@ -340,14 +360,14 @@ __device__ __forceinline__ void attend_stage(uint32_t q_base, uint32_t stage, fl
                 for (int i = 0; i < 4; ++i) { h[i] = k[i] & 0xffffe000u; l[i] = tf32_rest_of(__uint_as_float(k[i]), h[i]); }
 #pragma unroll
                 for (int n = 0; n < 2; ++n) {
-                    mma1688_tf32(s[2 * kt + n], al.x, al.y, al.z, al.w, h[2 * n], h[2 * n + 1]);
-                    mma1688_tf32(s[2 * kt + n], a.x, a.y, a.z, a.w, l[2 * n], l[2 * n + 1]);
+                    mma1688_tf32(small[2 * kt + n], al.x, al.y, al.z, al.w, h[2 * n], h[2 * n + 1]);
+                    mma1688_tf32(small[2 * kt + n], a.x, a.y, a.z, a.w, l[2 * n], l[2 * n + 1]);
                     mma1688_tf32(s[2 * kt + n], a.x, a.y, a.z, a.w, h[2 * n], h[2 * n + 1]);
                 }
             } else {
 #pragma unroll
                 for (int n = 0; n < 2; ++n) {
-                    if (kSplitQ) mma16(s[2 * kt + n], al, k[2 * n], k[2 * n + 1], T());
+                    if (kSplitQ) mma16(small[2 * kt + n], al, k[2 * n], k[2 * n + 1], T());
                     mma16(s[2 * kt + n], a, k[2 * n], k[2 * n + 1], T());
                 }
             }
@@ -358,7 +378,7 @@ __device__ __forceinline__ void attend_stage(uint32_t q_base, uint32_t stage, fl
     for (int nt = 0; nt < 4; ++nt)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            s[nt][i] *= c;
+            s[nt][i] = kSplitQ || S::es == 4 ? (s[nt][i] + small[nt][i]) * c : s[nt][i] * c;
             if (kMask && !((mask.row[i >> 1] >> (nt * 8 + 2 * t + (i & 1))) & 1u)) s[nt][i] = -INFINITY;
             top[i >> 1] = fmaxf(top[i >> 1], s[nt][i]);
         }
@@ -434,11 +454,13 @@ attend_kernel(const __grid_constant__ TensorMap k_map, const __grid_constant__ T
     const uint32_t ring = smem_u32(smem), full = smem_u32(s_full), empty = smem_u32(s_empty);
     float *parked = reinterpret_cast<float *>(smem + A.ring * S::stage), *parked_ml = parked + A.parked * 16 * S::ld;
     unsigned char *queries = smem + A.ring * S::stage + parked_bytes(DH, A.parked);
+    chain_go();
     if (threadIdx.x == 0) {
         for (int i = 0; i < A.ring; ++i) { mbar_init(full + 8 * i, 1); mbar_init(empty + 8 * i, A.rt); }
         mbar_init_fence();
     }
     __syncthreads();
+    chain_wait();
     const int units = A.kv_heads * A.row_groups;
 
     if (warp >= kAttendWarps) {
@@ -638,13 +660,25 @@ attend_kernel(const __grid_constant__ TensorMap k_map, const __grid_constant__ T
             const int r = i / (DH / 4), d = (i - r * (DH / 4)) * 4;
             float m = -INFINITY, l = 0.f;
             float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-            for (int w = r >> 4; w < A.parked; w += tiles) m = fmaxf(m, parked_ml[w * 32 + 2 * (r & 15)]);
+            float2 ml[4];
+            float4 x[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int w = (r >> 4) + k * tiles;
+                ml[k] = make_float2(-INFINITY, 0.f);
+                x[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (w < A.parked) {
+                    ml[k] = *reinterpret_cast<const float2 *>(parked_ml + w * 32 + 2 * (r & 15));
+                    x[k] = *reinterpret_cast<const float4 *>(parked + (w * 16 + (r & 15)) * S::ld + d);
+                }
+                m = fmaxf(m, ml[k].x);
+            }
             const float ref = m == -INFINITY ? 0.f : m;
-            for (int w = r >> 4; w < A.parked; w += tiles) {
-                const float f = ex2(parked_ml[w * 32 + 2 * (r & 15)] - ref);
-                const float4 x = *reinterpret_cast<const float4 *>(parked + w * 16 * S::ld + (r & 15) * S::ld + d);
-                l += parked_ml[w * 32 + 2 * (r & 15) + 1] * f;
-                o.x += x.x * f; o.y += x.y * f; o.z += x.z * f; o.w += x.w * f;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const float f = ex2(ml[k].x - ref);
+                l += ml[k].y * f;
+                o.x += x[k].x * f; o.y += x[k].y * f; o.z += x[k].z * f; o.w += x[k].w * f;
             }
             if (seg.whole) {
                 finish<TQ>(A, sp, b, seg.unit, r, d, o, m, l);
@@ -657,7 +691,7 @@ attend_kernel(const __grid_constant__ TensorMap k_map, const __grid_constant__ T
             // CTAs whose runs meet this unit: the one with its first granule to the one with its last.  Whether this CTA is the last of them to
             // be there is asked at its end, when all its runs' writes are done.
             if (tid == 0) {
-                const int c0 = run.owner(seg.first), c1 = run.owner(seg.last - 1);
+                const int c0 = run.owner(seg.first + kOpening), c1 = run.owner(seg.last - 1);
                 s_left[pending] = Left{b, seg.unit, sp.nq, c0, c1, run.start(c0) < seg.first, false};
             }
             ++pending;
@@ -674,22 +708,26 @@ attend_kernel(const __grid_constant__ TensorMap k_map, const __grid_constant__ T
         s_left[tid].last = last;
     }
     bar_attend();
-    for (int u = 0; u < pending; ++u) {
+    // two of them: four warps each
+    const bool both = pending == 2 && s_left[0].last && s_left[1].last;
+    const int first = both ? tid & 127 : tid, step = both ? 128 : kAttendWarps * 32;
+    for (int u = both ? tid >> 7 : 0; u < (both ? (tid >> 7) + 1 : pending); ++u) {
         const Left left = s_left[u];
         if (!left.last) continue;
         Span sp;
         sp.nq = left.nq;
         const int rows = min(A.rt * 16, A.n_rows - (left.unit % A.row_groups) * A.rt * 16);
         auto place = [&](int c) { return A.partial + (2 * (long long)c + (c == left.c0 && left.second ? 1 : 0)) * slot_floats; };
-        for (int i = tid; i < rows * (DH / 4); i += kAttendWarps * 32) {
+        for (int i = first; i < rows * (DH / 4); i += step) {
             const int r = i / (DH / 4), d = (i - r * (DH / 4)) * 4;
             float m = -INFINITY, l = 0.f;
             float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-            for (int c = left.c0; c <= left.c1; c += 8) {           // eight of them on their way at a time
-                float2 ml[8];
-                float4 x[8];
+            constexpr int kWay = 16;
+            for (int c = left.c0; c <= left.c1; c += kWay) {       // so many of them on their way at a time
+                float2 ml[kWay];
+                float4 x[kWay];
 #pragma unroll
-                for (int k = 0; k < 8; ++k) {
+                for (int k = 0; k < kWay; ++k) {
                     ml[k] = make_float2(-INFINITY, 0.f);
                     x[k] = make_float4(0.f, 0.f, 0.f, 0.f);
                     if (c + k <= left.c1) {
@@ -699,12 +737,12 @@ attend_kernel(const __grid_constant__ TensorMap k_map, const __grid_constant__ T
                 }
                 float top = m;
 #pragma unroll
-                for (int k = 0; k < 8; ++k) top = fmaxf(top, ml[k].x);
+                for (int k = 0; k < kWay; ++k) top = fmaxf(top, ml[k].x);
                 const float ref = top == -INFINITY ? 0.f : top, f0 = ex2(m - ref);
                 l *= f0; o.x *= f0; o.y *= f0; o.z *= f0; o.w *= f0;
                 m = top;
 #pragma unroll
-                for (int k = 0; k < 8; ++k) {
+                for (int k = 0; k < kWay; ++k) {
                     const float f = ex2(ml[k].x - ref);
                     l += ml[k].y * f;
                     o.x += x[k].x * f; o.y += x[k].y * f; o.z += x[k].z * f; o.w += x[k].w * f;
@@ -757,8 +795,7 @@ static cudaError_t launch_attend(const xsm_kv &kv, const AttendArgs &A, const At
     const void *fn = (const void *)attend_kernel<T, TQ, DH>;
     const cudaError_t e = open_kernel(fn, p.smem, false);
     if (e != cudaSuccess) return e;
-    attend_kernel<T, TQ, DH><<<p.grid, (kAttendWarps + kProducers) * 32, p.smem, st>>>(kv.k_map, kv.v_map, A);
-    return cudaGetLastError();
+    return launch_early(attend_kernel<T, TQ, DH>, dim3(p.grid), dim3((kAttendWarps + kProducers) * 32), p.smem, st, kv.k_map, kv.v_map, A);
 }
 template <typename T, typename TQ> static cudaError_t launch_width(const xsm_kv &kv, const AttendArgs &A, const AttendPlan &p, cudaStream_t st) {
     switch (kv.cfg.d_head) {
@@ -793,7 +830,7 @@ xsm_status xsm_kv_attend(const xsm_kv *kv, const xsm_kv_attend_args *a, void *cu
     if (a->batch == 0) return XSM_OK;
     if (!a->q || !a->out || !a->block_table || !a->lengths || !a->workspace) return op_failed(XSM_ERR_INVALID_ARG, "null argument");
     const AttendPlan p = plan_attend(*kv, a->batch, a->m, a->n_heads, a->q_dtype);
-    if ((double)p.units * ((double)a->max_pages * c.page_size / (kStage * kGranule) + 2) > INT_MAX / 2) return op_failed(XSM_ERR_INVALID_ARG, "batch * heads * positions is too large");
+    if ((double)p.units * ((double)a->max_pages * c.page_size / (kStage * kGranule) + kOpening + 2) > INT_MAX / 2) return op_failed(XSM_ERR_INVALID_ARG, "batch * heads * positions is too large");
     if (a->workspace_bytes < (int64_t)p.workspace) return op_failed(XSM_ERR_CAPACITY, "the workspace is too small");
     const int per16 = 16 / element_size(a->q_dtype);
     for (int i = 0; i < 3; ++i)
@@ -806,7 +843,7 @@ xsm_status xsm_kv_attend(const xsm_kv *kv, const xsm_kv_attend_args *a, void *cu
     A.partial = reinterpret_cast<float *>((char *)a->workspace + kHeadBytes);
     for (int i = 0; i < 3; ++i) { A.qs[i] = a->q_stride[i]; A.os[i] = a->out_stride[i]; }
     A.batch = a->batch; A.m = a->m; A.heads = a->n_heads; A.group = a->n_heads / c.n_kv_heads; A.kv_heads = c.n_kv_heads;
-    A.rt = p.rt; A.row_groups = p.row_groups; A.n_rows = A.m * A.group; A.ring = p.ring; A.turns = p.turns; A.producers = p.producers; A.parked = p.parked;
+    A.whole = kWholeBytes / (2 * kStage * c.d_head * element_size(c.dtype)); A.element = element_size(c.dtype); A.rt = p.rt; A.row_groups = p.row_groups; A.n_rows = A.m * A.group; A.ring = p.ring; A.turns = p.turns; A.producers = p.producers; A.parked = p.parked;
     A.causal = a->causal != 0; A.window = a->window; A.page = c.page_size; A.max_pages = a->max_pages; A.n_pages = c.n_pages; A.box_rows = kv->box_rows;
     A.c = (float)((double)a->scale * 1.4426950408889634);
     const cudaStream_t st = (cudaStream_t)cuda_stream;

@@ -51,6 +51,23 @@ template <> __device__ __forceinline__ __half to_stored<__half>(float v) {
     return __float2half_rn(fabsf(v) > 65504.f ? copysignf(65504.f, v) : v);
 }
 
+// Launches a kernel that may start while the one before it on the stream still runs: it calls chain_wait before its first access to
+// memory, and chain_go to let the next one do the same.
+template <typename... P, typename... X>
+inline cudaError_t launch_early(void (*fn)(P...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, const X &...args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = block;
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, fn, args...);
+}
+
 // calls f with a value of the element type that `dtype` names
 template <typename F> inline void with_dtype(int dtype, F &&f) {
     if (dtype == XSM_F32) f(float());
