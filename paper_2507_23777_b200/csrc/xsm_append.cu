@@ -35,6 +35,8 @@ template <bool kPool, typename T, int N> __device__ __forceinline__ void store_f
 // part or the alignment does not allow that).  Items of a token: heads of q, of k, of v, d / 2N items each, the rotated ones first.
 template <typename TI, typename TC, int N>
 __global__ void __launch_bounds__(256) append_kernel(const __grid_constant__ AppendArgs A, const __grid_constant__ Pages P) {
+    chain_go();
+    chain_wait();
     const int b = blockIdx.x / A.m, j = blockIdx.x - b * A.m;
     const int per_head = A.d / (2 * N), rotated = A.rot / (2 * N), n = (A.heads + 2 * P.kv_heads) * per_head;
     const bool real = A.counts == nullptr || j < A.counts[b];
@@ -194,13 +196,13 @@ xsm_status xsm_kv_append(const xsm_kv *kv, const xsm_kv_append_args *a, void *cu
                       (a->n_heads == 0 || (aligned(a->q, a->q_stride, es) && aligned(a->q_out, a->q_out_stride, es)));
     const int items = (A.heads + 2 * P.kv_heads) * (A.d / (wide ? 16 : 2));
     const int threads = items >= 256 ? 256 : (items + 31) / 32 * 32;
+    cudaError_t e = cudaSuccess;
     with_dtype(a->in_dtype, [&](auto in) {
         with_dtype(kv->cfg.dtype, [&](auto stored) {
             using TI = decltype(in);
             using TC = decltype(stored);
-            if (wide) append_kernel<TI, TC, 8><<<(unsigned)tokens, threads, 0, (cudaStream_t)cuda_stream>>>(A, P);
-            else append_kernel<TI, TC, 1><<<(unsigned)tokens, threads, 0, (cudaStream_t)cuda_stream>>>(A, P);
+            e = launch_early(wide ? append_kernel<TI, TC, 8> : append_kernel<TI, TC, 1>, dim3((unsigned)tokens), dim3(threads), 0, (cudaStream_t)cuda_stream, A, P);
         });
     });
-    return launched(cudaGetLastError());
+    return launched(e);
 }

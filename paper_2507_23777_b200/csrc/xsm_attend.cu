@@ -28,6 +28,8 @@ constexpr int kGranule = 4, kOpening = 3;      // stages that are never cut apar
 constexpr int kWholeBytes = 128 * 1024;
 constexpr int kAttendWarps = 8, kProducers = 4;
 constexpr int kRing = 16;             // most stages in shared memory
+constexpr int kMaxRowTiles = 4;       // of a unit
+constexpr int kDeclared = 4096;       // shared memory that the kernel declares, at most
 // Workspace: status word and counters, which every call leaves at zero, in a place that does not depend on the call; then the partial results.
 constexpr int kHeadBytes = 4096, kMaxGrid = kHeadBytes / 4 - 4;
 
@@ -54,11 +56,17 @@ template <typename T, int DH> struct Shape {
     static constexpr int half = boxes * box_bytes, stage = 2 * half;                          // keys, then values
     static constexpr int steps = DH * es / 32;                                                // products over 32 bytes of a row
     static constexpr int ld = DH + 4;                                                         // rows of parked outputs
-    // shared-memory address of 16-byte chunk ch of row r
+    // Shared-memory address of 16-byte chunk ch of row r.  Rows are 128 (64) bytes, so a lane's row and the chunk that it begins with are one number
+    // (`lane_at`), and an even number of chunks further is an exclusive or of constants (`step`).
     static __device__ __forceinline__ uint32_t at(uint32_t base, int r, int ch) {
         constexpr int per = rb / 16;
         const int x = ch % per, s = rb == 128 ? r & 7 : (r >> 1) & 3;
         return base + (ch / per) * box_bytes + r * rb + ((x ^ s) << 4);
+    }
+    static __device__ __forceinline__ uint32_t lane_at(int r, int first) { return at(0, r, first); }
+    static __device__ __forceinline__ uint32_t step(uint32_t from, int ch) {
+        constexpr int per = rb / 16;
+        return (from ^ (uint32_t)((ch % per) << 4)) + (uint32_t)((ch / per) * box_bytes);
     }
 };
 __host__ __device__ constexpr int parked_bytes(int dh, int warps) { return warps * 16 * ((dh + 4) + 2) * 4; }
@@ -287,7 +295,7 @@ __device__ __forceinline__ void add_values(const float (&p)[4][4], uint32_t v_ba
             const uint4 a = make_uint4(pack2<T>(u[0], u[1]), pack2<T>(u[2], u[3]), pack2<T>(w[0], w[1]), pack2<T>(w[2], w[3]));
             uint4 r;
             if (kSplit) r = make_uint4(rest2<T>(u[0], u[1], a.x), rest2<T>(u[2], u[3], a.y), rest2<T>(w[0], w[1], a.z), rest2<T>(w[2], w[3], a.w));
-            const int row = kk * 16 + (lane & 7) + (((lane >> 3) & 1) << 3);
+            const uint32_t from = v_base + kk * 16 * S::rb + S::lane_at((lane & 7) + (((lane >> 3) & 1) << 3), lane >> 4);
             unsigned m0 = ~0u, m1 = ~0u;
             if (kMask) {
                 const unsigned b0 = kept >> (kk * 16 + 2 * t), b1 = kept >> (kk * 16 + 2 * t + 8);
@@ -297,7 +305,7 @@ __device__ __forceinline__ void add_values(const float (&p)[4][4], uint32_t v_ba
 #pragma unroll
             for (int j = 0; j < DH / 8; j += 2) {
                 unsigned v[4];
-                ldmatrix_x4_trans(v, S::at(v_base, row, j + (lane >> 4)));
+                ldmatrix_x4_trans(v, S::step(from, j));
                 if (kMask) { v[0] &= m0; v[1] &= m1; v[2] &= m0; v[3] &= m1; }
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
@@ -344,7 +352,7 @@ __device__ __forceinline__ void attend_stage(uint32_t q_base, uint32_t stage, fl
         s[nt][0] = s[nt][1] = s[nt][2] = s[nt][3] = 0.f;
         small[nt][0] = small[nt][1] = small[nt][2] = small[nt][3] = 0.f;
     }
-    const int row = (lane & 7) + ((lane >> 4) << 3);
+    const uint32_t from = stage + S::lane_at((lane & 7) + ((lane >> 4) << 3), (lane >> 3) & 1);
 #pragma unroll
     for (int ks = 0; ks < S::steps; ++ks) {
         const uint4 a = lds128(q_base + ks * 512 + lane * 16);
@@ -353,7 +361,7 @@ __device__ __forceinline__ void attend_stage(uint32_t q_base, uint32_t stage, fl
 #pragma unroll
         for (int kt = 0; kt < 2; ++kt) {
             unsigned k[4];
-            ldmatrix_x4(k, S::at(stage, kt * 16 + row, 2 * ks + ((lane >> 3) & 1)));
+            ldmatrix_x4(k, S::step(from, 2 * ks) + kt * 16 * S::rb);
             if constexpr (S::es == 4) {
                 unsigned h[4], l[4];
 #pragma unroll
@@ -429,14 +437,22 @@ template <typename TQ> __device__ __forceinline__ void store4(TQ *p, float4 v) {
     else *reinterpret_cast<uint2 *>(p) = make_uint2(pack2<TQ>(v.x, v.y), pack2<TQ>(v.z, v.w));
 }
 
+// Where a unit's rows come out.  Written by a thread a row: who needs them would divide.
+struct RowPlace {
+    long long out, lse;                       // elements; lse -1: not wanted
+    int token;                                // of the sequence's queries
+    bool real;                                // there is such a query
+};
+__device__ __forceinline__ void place_row(const AttendArgs &A, int b, int unit, int nq, int r, RowPlace *places) {
+    const int kvh = unit / A.row_groups, row = (unit - kvh * A.row_groups) * A.rt * 16 + r, j = row / A.group, h = kvh * A.group + (row - j * A.group);
+    places[r] = RowPlace{b * A.os[0] + j * A.os[1] + h * A.os[2], A.lse ? ((long long)b * A.m + j) * A.heads + h : -1, j, j < nq};
+}
 // output of one row's four elements and its lse, from the joined state
-template <typename TQ> __device__ __forceinline__ void finish(const AttendArgs &A, const Span &sp, int b, int unit, int row, int d, float4 o, float m, float l) {
-    const int kvh = unit / A.row_groups, r = (unit % A.row_groups) * A.rt * 16 + row, j = r / A.group, h = kvh * A.group + (r - j * A.group);
-    const bool none = j >= sp.nq || l == 0.f;
+template <typename TQ> __device__ __forceinline__ void finish(const AttendArgs &A, const RowPlace &p, int d, float4 o, float m, float l) {
+    const bool none = !p.real || l == 0.f;
     const float f = none ? 0.f : 1.f / l;
-    TQ *p = reinterpret_cast<TQ *>(A.out) + b * A.os[0] + j * A.os[1] + h * A.os[2] + d;
-    store4<TQ>(p, none ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(o.x * f, o.y * f, o.z * f, o.w * f));
-    if (d == 0 && A.lse) A.lse[((long long)b * A.m + j) * A.heads + h] = none ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
+    store4<TQ>(reinterpret_cast<TQ *>(A.out) + p.out + d, none ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(o.x * f, o.y * f, o.z * f, o.w * f));
+    if (d == 0 && p.lse >= 0) A.lse[p.lse] = none ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
 }
 
 template <typename T, typename TQ, int DH>
@@ -449,6 +465,7 @@ attend_kernel(const __grid_constant__ TensorMap k_map, const __grid_constant__ T
     __shared__ __align__(8) unsigned long long s_full[kRing], s_empty[kRing];
     __shared__ int2 s_info[kRing];            // first position of a stage, which halves exist
     struct Left { int b, unit, nq, c0, c1; bool second, last; };
+    __shared__ RowPlace s_rows[2][kMaxRowTiles * 16];      // of the unit at work; at the end of two that are joined
     __shared__ Left s_left[2];                // units that other CTAs share: at most the run's first and its last
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t ring = smem_u32(smem), full = smem_u32(s_full), empty = smem_u32(s_empty);
@@ -545,25 +562,30 @@ attend_kernel(const __grid_constant__ TensorMap k_map, const __grid_constant__ T
         opening = false;
         asm volatile("cp.async.wait_all;" ::: "memory");
         bar_attend();                            // the rows are here; what the segment before parked has been read
-        // a thread takes 32 bits (two elements, or one of fp32) at a time and puts them where the lanes of the products look for them
-        constexpr int per = S::es == 4 ? 1 : 2;
-        for (int i = tid; i < A.rt * 16 * (DH / per); i += kAttendWarps * 32) {
-            const int r = i / (DH / per), e = (i - r * (DH / per)) * per;
+        if (tid < rows) place_row(A, b, seg.unit, sp.nq, tid, s_rows[0]);
+        // A thread takes 16 bytes of the operands (eight elements, or four of fp32) at a time and puts their words where the lanes of the products
+        // look for them: 32 bytes of a row a step; lane 4 (row mod 8) + (word mod 4), register (row / 8) + 2 (word / 4).
+        constexpr int per = S::es == 4 ? 4 : 8, chunks = DH / per;
+        for (int i = tid; i < A.rt * 16 * chunks; i += kAttendWarps * 32) {
+            const int r = i / chunks, ch = i - r * chunks, in = r & 15;
+            struct __align__(16) Some { TQ e[per]; };
+            const Some some = *reinterpret_cast<const Some *>(raw + r * raw_ld + ch * per * (int)sizeof(TQ));
             float x[per];
 #pragma unroll
-            for (int k = 0; k < per; ++k) x[k] = r < rows ? to_f(reinterpret_cast<const TQ *>(raw + r * raw_ld)[e + k]) : 0.f;
-            // 32 bytes of a row a step; lane 4 (row mod 8) + (word mod 4), register (row / 8) + 2 (word / 4)
-            const int word = e / per, ks = word / 8, w = word % 8, in = r & 15;
-            unsigned *dst = reinterpret_cast<unsigned *>(queries + (r >> 4) * query_bytes(DH, S::es, kSplitQ || S::es == 4) + ks * 512 + ((in & 7) * 4 + (w & 3)) * 16) +
-                            (in >> 3) + 2 * (w >> 2);
-            if constexpr (S::es == 4) {
-                const unsigned hi = tf32_part(x[0]);
-                dst[0] = hi;
-                dst[S::steps * 128] = tf32_rest_of(x[0], hi);
-            } else {
-                const unsigned hi = pack2<T>(x[0], x[per - 1]);
-                dst[0] = hi;
-                if (kSplitQ) dst[S::steps * 128] = rest2<T>(x[0], x[per - 1], hi);
+            for (int k = 0; k < per; ++k) x[k] = r < rows ? to_f(some.e[k]) : 0.f;
+            unsigned *dst = reinterpret_cast<unsigned *>(queries + (r >> 4) * query_bytes(DH, S::es, kSplitQ || S::es == 4) + (ch >> 1) * 512 + (in & 7) * 64) +
+                            (in >> 3) + 2 * (ch & 1);
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                if constexpr (S::es == 4) {
+                    const unsigned hi = tf32_part(x[w]);
+                    dst[4 * w] = hi;
+                    dst[4 * w + S::steps * 128] = tf32_rest_of(x[w], hi);
+                } else {
+                    const unsigned hi = pack2<T>(x[2 * w], x[2 * w + 1]);
+                    dst[4 * w] = hi;
+                    if (kSplitQ) dst[4 * w + S::steps * 128] = rest2<T>(x[2 * w], x[2 * w + 1], hi);
+                }
             }
         }
         bar_attend();
@@ -581,8 +603,8 @@ attend_kernel(const __grid_constant__ TensorMap k_map, const __grid_constant__ T
         int token[2], begin[2], end[2];
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
-            const int row = row0 + tile * 16 + g + 8 * r;
-            token[r] = row / A.group;
+            const int row = tile * 16 + g + 8 * r;
+            token[r] = row < rows ? s_rows[0][row].token : sp.nq;
             end[r] = token[r] >= sp.nq ? 0 : A.causal ? sp.first_end + token[r] : sp.end;
             begin[r] = A.window > 0 ? max(0, end[r] - A.window) : 0;
         }
@@ -681,7 +703,7 @@ attend_kernel(const __grid_constant__ TensorMap k_map, const __grid_constant__ T
                 o.x += x[k].x * f; o.y += x[k].y * f; o.z += x[k].z * f; o.w += x[k].w * f;
             }
             if (seg.whole) {
-                finish<TQ>(A, sp, b, seg.unit, r, d, o, m, l);
+                finish<TQ>(A, s_rows[0][r], d, o, m, l);
             } else {
                 __stcg(reinterpret_cast<float4 *>(place + r * DH + d), o);
                 if (d == 0) __stcg(reinterpret_cast<float2 *>(place + A.rt * 16 * DH + 2 * r), make_float2(m, l));
@@ -711,45 +733,65 @@ attend_kernel(const __grid_constant__ TensorMap k_map, const __grid_constant__ T
     // two of them: four warps each
     const bool both = pending == 2 && s_left[0].last && s_left[1].last;
     const int first = both ? tid & 127 : tid, step = both ? 128 : kAttendWarps * 32;
+    for (int u = 0; u < pending; ++u) {
+        const Left &left = s_left[u];
+        if (left.last && tid < min(A.rt * 16, A.n_rows - (left.unit % A.row_groups) * A.rt * 16)) place_row(A, left.b, left.unit, left.nq, tid, s_rows[u]);
+    }
+    bar_attend();
     for (int u = both ? tid >> 7 : 0; u < (both ? (tid >> 7) + 1 : pending); ++u) {
         const Left left = s_left[u];
         if (!left.last) continue;
-        Span sp;
-        sp.nq = left.nq;
-        const int rows = min(A.rt * 16, A.n_rows - (left.unit % A.row_groups) * A.rt * 16);
-        auto place = [&](int c) { return A.partial + (2 * (long long)c + (c == left.c0 && left.second ? 1 : 0)) * slot_floats; };
-        for (int i = first; i < rows * (DH / 4); i += step) {
-            const int r = i / (DH / 4), d = (i - r * (DH / 4)) * 4;
-            float m = -INFINITY, l = 0.f;
-            float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-            constexpr int kWay = 16;
-            for (int c = left.c0; c <= left.c1; c += kWay) {       // so many of them on their way at a time
-                float2 ml[kWay];
-                float4 x[kWay];
+        const int n = min(A.rt * 16, A.n_rows - (left.unit % A.row_groups) * A.rt * 16) * (DH / 4);
+        // kItems pieces of the output times kWay parts on their way at a time
+        auto join = [&](auto items_, auto way_) {
+            constexpr int kItems = decltype(items_)::value, kWay = decltype(way_)::value;
+            for (int i0 = first; i0 < n; i0 += step * kItems) {
+                float m[kItems], l[kItems];
+                float4 o[kItems];
 #pragma unroll
-                for (int k = 0; k < kWay; ++k) {
-                    ml[k] = make_float2(-INFINITY, 0.f);
-                    x[k] = make_float4(0.f, 0.f, 0.f, 0.f);
-                    if (c + k <= left.c1) {
-                        ml[k] = __ldcg(reinterpret_cast<const float2 *>(place(c + k) + A.rt * 16 * DH + 2 * r));
-                        x[k] = __ldcg(reinterpret_cast<const float4 *>(place(c + k) + r * DH + d));
+                for (int q = 0; q < kItems; ++q) { m[q] = -INFINITY; l[q] = 0.f; o[q] = make_float4(0.f, 0.f, 0.f, 0.f); }
+                for (int c = left.c0; c <= left.c1; c += kWay) {
+                    float2 ml[kItems][kWay];
+                    float4 x[kItems][kWay];
+#pragma unroll
+                    for (int k = 0; k < kWay; ++k) {
+                        const float *from = A.partial + (2 * (long long)(c + k) + (c + k == left.c0 && left.second ? 1 : 0)) * slot_floats;
+#pragma unroll
+                        for (int q = 0; q < kItems; ++q) {
+                            const int i = i0 + q * step;
+                            ml[q][k] = make_float2(-INFINITY, 0.f);
+                            x[q][k] = make_float4(0.f, 0.f, 0.f, 0.f);
+                            if (c + k <= left.c1 && i < n) {
+                                ml[q][k] = __ldcg(reinterpret_cast<const float2 *>(from + A.rt * 16 * DH) + i / (DH / 4));
+                                x[q][k] = __ldcg(reinterpret_cast<const float4 *>(from) + i);
+                            }
+                        }
+                    }
+#pragma unroll
+                    for (int q = 0; q < kItems; ++q) {
+                        float top = m[q];
+#pragma unroll
+                        for (int k = 0; k < kWay; ++k) top = fmaxf(top, ml[q][k].x);
+                        const float ref = top == -INFINITY ? 0.f : top, f0 = ex2(m[q] - ref);
+                        l[q] *= f0; o[q].x *= f0; o[q].y *= f0; o[q].z *= f0; o[q].w *= f0;
+                        m[q] = top;
+#pragma unroll
+                        for (int k = 0; k < kWay; ++k) {
+                            const float f = ex2(ml[q][k].x - ref);
+                            l[q] += ml[q][k].y * f;
+                            o[q].x += x[q][k].x * f; o[q].y += x[q][k].y * f; o[q].z += x[q][k].z * f; o[q].w += x[q][k].w * f;
+                        }
                     }
                 }
-                float top = m;
 #pragma unroll
-                for (int k = 0; k < kWay; ++k) top = fmaxf(top, ml[k].x);
-                const float ref = top == -INFINITY ? 0.f : top, f0 = ex2(m - ref);
-                l *= f0; o.x *= f0; o.y *= f0; o.z *= f0; o.w *= f0;
-                m = top;
-#pragma unroll
-                for (int k = 0; k < kWay; ++k) {
-                    const float f = ex2(ml[k].x - ref);
-                    l += ml[k].y * f;
-                    o.x += x[k].x * f; o.y += x[k].y * f; o.z += x[k].z * f; o.w += x[k].w * f;
+                for (int q = 0; q < kItems; ++q) {
+                    const int i = i0 + q * step, r = i / (DH / 4);
+                    if (i < n) finish<TQ>(A, s_rows[u][r], (i - r * (DH / 4)) * 4, o[q], m[q], l[q]);
                 }
             }
-            finish<TQ>(A, sp, left.b, left.unit, r, d, o, m, l);
-        }
+        };
+        if (left.c1 - left.c0 < 4 && n > step) join(std::integral_constant<int, 2>(), std::integral_constant<int, 4>());
+        else join(std::integral_constant<int, 1>(), std::integral_constant<int, 8>());
     }
 }
 
@@ -769,7 +811,7 @@ static AttendPlan plan_attend(const xsm_kv &kv, int batch, int m, int n_heads, i
     p.rt = tiles >= 3 ? 4 : tiles;
     // Shared memory: the ring gets what the parked states and the queries leave.  A group of warps that takes stages wants two places, one to
     // work on and one that fills; so few groups that wide rows leave no room, then fewer row tiles.
-    auto left = [&](int rt, int turns) { return kCtaSmem - 1024 - parked_bytes(c.d_head, rt * turns < 4 ? rt * turns : 4) - rt * q; };
+    auto left = [&](int rt, int turns) { return kCtaSmem - kDeclared - parked_bytes(c.d_head, rt * turns < 4 ? rt * turns : 4) - rt * q; };
     for (;; p.rt /= 2) {
         p.turns = kAttendWarps / p.rt;
         while (p.turns > 1 && left(p.rt, p.turns) / stage < 2 * p.turns) p.turns /= 2;
