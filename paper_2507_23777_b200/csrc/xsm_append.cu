@@ -3,8 +3,10 @@
 #include "xsm_ops.h"
 
 #include <cuda.h>
+#include <limits.h>
 
 #include <new>
+#include <type_traits>
 
 namespace xsm {
 
@@ -14,16 +16,11 @@ struct AppendArgs {
     const int *starts, *counts;
     const float2 *rope;
     long long qs[3], ks[3], vs[3], os[3];       // strides of sequence, token, head
-    int m, heads, d, rope_n, rot, interleaved;
+    int m, heads, d, rope_n, rot;
 };
 
 template <typename T, int N> struct __align__(sizeof(T) * N > 16 ? 16 : sizeof(T) * N) Vec { T e[N]; };
 
-template <typename T, int N> __device__ __forceinline__ void load_f(const T *p, float (&x)[N]) {
-    const Vec<T, N> v = *reinterpret_cast<const Vec<T, N> *>(p);
-#pragma unroll
-    for (int i = 0; i < N; ++i) x[i] = to_f(v.e[i]);
-}
 template <bool kPool, typename T, int N> __device__ __forceinline__ void store_f(T *p, const float (&x)[N]) {
     Vec<T, N> v;
 #pragma unroll
@@ -32,58 +29,77 @@ template <bool kPool, typename T, int N> __device__ __forceinline__ void store_f
 }
 
 // A block for every token; a thread takes N pairs of elements of a head at a time (N = 8: whole 16-byte pieces; N = 1 where the rotated
-// part or the alignment does not allow that).  Items of a token: heads of q, of k, of v, d / 2N items each, the rotated ones first.
-template <typename TI, typename TC, int N>
-__global__ void __launch_bounds__(256) append_kernel(const __grid_constant__ AppendArgs A, const __grid_constant__ Pages P) {
+// part or the alignment does not allow that).  Items of a token: heads of q, of k, of v, d / 2N items each, the rotated ones first.  kOnce: there
+// is a thread for every item of the token; kNear: pairs are neighbours.
+template <typename TI, typename TC, int N, bool kNear, bool kOnce>
+__global__ void __launch_bounds__(kOnce ? 512 : 128) append_kernel(const __grid_constant__ AppendArgs A, const __grid_constant__ Pages P) {
     chain_go();
     chain_wait();
     const int b = blockIdx.x / A.m, j = blockIdx.x - b * A.m;
     const int per_head = A.d / (2 * N), rotated = A.rot / (2 * N), n = (A.heads + 2 * P.kv_heads) * per_head;
+    struct Item {
+        bool is_q, is_v, turn;
+        int head, c, e0, e1;                     // the two runs of N elements of the head
+    };
+    auto item_of = [&](int it) {
+        Item i;
+        const int slot = it / per_head;
+        i.c = it - slot * per_head;
+        i.is_q = slot < A.heads;
+        i.is_v = slot >= A.heads + P.kv_heads;
+        i.head = i.is_q ? slot : i.is_v ? slot - A.heads - P.kv_heads : slot - A.heads;
+        i.turn = !i.is_v && i.c < rotated;
+        i.e0 = i.turn && !kNear ? i.c * N : i.c * 2 * N;
+        i.e1 = i.turn && !kNear ? i.e0 + A.rot / 2 : i.e0 + N;
+        return i;
+    };
+    Vec<TI, N> in0, in1;
+    auto fetch = [&](const Item &i) {
+        const long long *s = i.is_q ? A.qs : i.is_v ? A.vs : A.ks;
+        const TI *src = reinterpret_cast<const TI *>(i.is_q ? A.q : i.is_v ? A.v : A.k) + b * s[0] + j * s[1] + i.head * s[2];
+        in0 = *reinterpret_cast<const Vec<TI, N> *>(src + i.e0);
+        in1 = *reinterpret_cast<const Vec<TI, N> *>(src + i.e1);
+    };
+    if (kOnce) fetch(item_of(min((int)threadIdx.x, n - 1)));        // on their way before anybody waits for the position and the page
     const bool real = A.counts == nullptr || j < A.counts[b];
     const long long pos = (long long)A.starts[b] + j;
     const bool has_angle = A.rope == nullptr || (pos >= 0 && pos < A.rope_n);
     long long place = -1;                        // of the row in head 0, in elements
-    if (real && has_angle && pos >= 0 && pos / P.size < P.max_pages) {
-        const int page = P.table[b * P.table_ld + pos / P.size];
-        if (page >= 0 && page < P.n_pages) place = page * P.page + (pos % P.size) * P.row;
+    if (real && has_angle && pos >= 0 && pos <= INT_MAX) {
+        const int at = (int)pos / P.size;
+        const int page = at < P.max_pages ? P.table[b * P.table_ld + at] : -1;
+        if (page >= 0 && page < P.n_pages) place = page * P.page + ((int)pos - at * P.size) * P.row;
     }
     for (int it = threadIdx.x; it < n; it += blockDim.x) {
-        const int slot = it / per_head, c = it - slot * per_head;
-        const bool is_q = slot < A.heads, is_v = slot >= A.heads + P.kv_heads;
-        const int head = is_q ? slot : is_v ? slot - A.heads - P.kv_heads : slot - A.heads;
-        const bool turn = !is_v && c < rotated;
-        // the two runs of N elements that this thread takes
-        const int e0 = turn && !A.interleaved ? c * N : c * 2 * N, e1 = turn && !A.interleaved ? e0 + A.rot / 2 : e0 + N;
-        if (!is_q && place < 0) continue;
-        const long long *s = is_q ? A.qs : is_v ? A.vs : A.ks;
-        const TI *src = reinterpret_cast<const TI *>(is_q ? A.q : is_v ? A.v : A.k) + b * s[0] + j * s[1] + head * s[2];
+        const Item i = item_of(it);
+        if (!i.is_q && place < 0) continue;
+        if (!kOnce) fetch(i);
+        const bool is_q = i.is_q, is_v = i.is_v, turn = i.turn;
+        const int head = i.head, c = i.c, e0 = i.e0, e1 = i.e1;
         float x[N], y[N];
-        load_f<TI, N>(src + e0, x);
-        load_f<TI, N>(src + e1, y);
-        if (turn && real && has_angle) {
-            const float2 *cs = A.rope + pos * (A.rot / 2) + c * N;
-            if (A.interleaved) {
 #pragma unroll
-                for (int i = 0; i < N; i += 2) {
-                    if (N == 1) {
-                        const float2 t = cs[0];
-                        const float u = x[0] * t.x - y[0] * t.y, w = x[0] * t.y + y[0] * t.x;
-                        x[0] = u; y[0] = w;
-                    } else {
-                        const float2 t = cs[i / 2], r = cs[N / 2 + i / 2];
-                        float u = x[i] * t.x - x[(i + 1) % N] * t.y, w = x[i] * t.y + x[(i + 1) % N] * t.x;
-                        x[i] = u; x[(i + 1) % N] = w;
-                        u = y[i] * r.x - y[(i + 1) % N] * r.y; w = y[i] * r.y + y[(i + 1) % N] * r.x;
-                        y[i] = u; y[(i + 1) % N] = w;
-                    }
+        for (int k = 0; k < N; ++k) { x[k] = to_f(in0.e[k]); y[k] = to_f(in1.e[k]); }
+        if (turn && real && has_angle) {
+            const float2 *from = A.rope + pos * (A.rot / 2) + c * N;
+            float2 cs[N];
+            if constexpr (N > 1) {
+#pragma unroll
+                for (int i = 0; i < N / 2; ++i) {
+                    const float4 t = reinterpret_cast<const float4 *>(from)[i];
+                    cs[2 * i] = make_float2(t.x, t.y);
+                    cs[2 * i + 1] = make_float2(t.z, t.w);
                 }
             } else {
+                cs[0] = from[0];
+            }
+            // pair i: elements i of both runs; interleaved: neighbours, the first half of the pairs in the first run
 #pragma unroll
-                for (int i = 0; i < N; ++i) {
-                    const float2 t = cs[i];
-                    const float u = x[i] * t.x - y[i] * t.y, w = x[i] * t.y + y[i] * t.x;
-                    x[i] = u; y[i] = w;
-                }
+            for (int i = 0; i < N; ++i) {
+                constexpr bool near = N > 1 && kNear;
+                float &a = near ? (i < N / 2 ? x[2 * i % N] : y[2 * i % N]) : x[i], &d = near ? (i < N / 2 ? x[(2 * i + 1) % N] : y[(2 * i + 1) % N]) : y[i];
+                const float u = a * cs[i].x - d * cs[i].y, w = a * cs[i].y + d * cs[i].x;
+                a = u;
+                d = w;
             }
         }
         if (is_q) {
@@ -188,20 +204,28 @@ xsm_status xsm_kv_append(const xsm_kv *kv, const xsm_kv_append_args *a, void *cu
     for (int i = 0; i < 3; ++i) { A.qs[i] = a->q_stride[i]; A.ks[i] = a->k_stride[i]; A.vs[i] = a->v_stride[i]; A.os[i] = a->q_out_stride[i]; }
     A.m = a->m; A.heads = a->n_heads; A.d = kv->cfg.d_head; A.rope_n = a->rope_positions;
     A.rot = a->rope ? a->rope_dims : 0;
-    A.interleaved = a->interleaved != 0;
     const Pages P = pages_of(*kv, a->block_table, a->table_stride, a->max_pages);
     const int es = element_size(a->in_dtype);
     if (((uintptr_t)a->rope) % 8) return op_failed(XSM_ERR_INVALID_ARG, "rope must be 8-byte aligned");
-    const bool wide = A.rot % 16 == 0 && aligned(a->k, a->k_stride, es) && aligned(a->v, a->v_stride, es) &&
+    const bool wide = A.rot % 16 == 0 && (uintptr_t)a->rope % 16 == 0 && aligned(a->k, a->k_stride, es) && aligned(a->v, a->v_stride, es) &&
                       (a->n_heads == 0 || (aligned(a->q, a->q_stride, es) && aligned(a->q_out, a->q_out_stride, es)));
     const int items = (A.heads + 2 * P.kv_heads) * (A.d / (wide ? 16 : 2));
-    const int threads = items >= 256 ? 256 : (items + 31) / 32 * 32;
+    // Few tokens: a thread for every item, whose elements are requested before the token's place is known (a window of five tokens 2.45 -> 2.1 us); many:
+    // 128 threads a token, fewer registers a thread (prompts of 8001 tokens 62 us, 73 the other way, 65 with 256 threads).
+    const bool once = tokens < 1024 && items <= 512;
+    const int threads = !once && items > 128 ? 128 : (items + 31) / 32 * 32;
     cudaError_t e = cudaSuccess;
     with_dtype(a->in_dtype, [&](auto in) {
         with_dtype(kv->cfg.dtype, [&](auto stored) {
             using TI = decltype(in);
             using TC = decltype(stored);
-            e = launch_early(wide ? append_kernel<TI, TC, 8> : append_kernel<TI, TC, 1>, dim3((unsigned)tokens), dim3(threads), 0, (cudaStream_t)cuda_stream, A, P);
+            auto go = [&](auto n, auto near, auto one) {
+                e = launch_early(append_kernel<TI, TC, decltype(n)::value, decltype(near)::value, decltype(one)::value>, dim3((unsigned)tokens), dim3(threads), 0,
+                                 (cudaStream_t)cuda_stream, A, P);
+            };
+            auto by_order = [&](auto n, auto near) { once ? go(n, near, std::true_type()) : go(n, near, std::false_type()); };
+            auto by_width = [&](auto n) { a->interleaved ? by_order(n, std::true_type()) : by_order(n, std::false_type()); };
+            wide ? by_width(std::integral_constant<int, 8>()) : by_width(std::integral_constant<int, 1>());
         });
     });
     return launched(e);
