@@ -203,6 +203,8 @@ template <typename T, int W> __device__ __noinline__ void best_one_by_one(const 
 template <typename T, bool kTop, int W> __global__ void __launch_bounds__(kBlock, kTop || sizeof(T) == 4 ? 8 : 12) logprob_kernel(const __grid_constant__ LogprobArgs A) {
     constexpr int N = Pieces<T>::n, kThreads = 32 * W, kAhead = 32 / N;      // pieces that a thread has under way: 32 logits
     __shared__ RowShared<W> shared[W == 1 ? kBlock / 32 : 1];
+    chain_go();
+    chain_wait();
     RowShared<W> &sh = shared[W == 1 ? threadIdx.x >> 5 : 0];
     const int tid = W == 1 ? threadIdx.x & 31 : threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int cut = W == 1 ? 0 : blockIdx.x & (A.cuts - 1);          // (clusters start at multiples of their size: this is the rank)
@@ -456,6 +458,8 @@ template <typename T, bool kTop, int W> __global__ void __launch_bounds__(kBlock
     __shared__ RowGrad rows[kGroups];
     __shared__ int ids[kGroups][kMaxTop + 1];
     __shared__ float gs[kGroups][kMaxTop + 1];
+    chain_go();
+    chain_wait();
     const int tid = W == 1 ? threadIdx.x & 31 : threadIdx.x, group = W == 1 ? threadIdx.x >> 5 : 0;
     int *const s_id = ids[group];
     float *const s_g = gs[group];
@@ -585,11 +589,9 @@ static cudaError_t sm_count(int *sms) {
 static bool by_warp(int rows, long long row_bytes, int sms) { return row_bytes <= kWarpRowBytes && rows >= 4 * sms; }
 
 template <typename T, bool kTop> static cudaError_t launch_logprob(const LogprobArgs &A, bool warps, cudaStream_t st) {
-    if (warps) {
-        logprob_kernel<T, kTop, 1><<<(A.rows + kBlock / 32 - 1) / (kBlock / 32), kBlock, 0, st>>>(A);
-        return cudaGetLastError();
-    }
-    cudaLaunchConfig_t cfg = {};
+    if (warps) return launch_early(logprob_kernel<T, kTop, 1>, dim3((A.rows + kBlock / 32 - 1) / (kBlock / 32)), dim3(kBlock), 0, st, A);
+    if (A.cuts == 1) return launch_early(logprob_kernel<T, kTop, kBlock / 32>, dim3(A.rows), dim3(kBlock), 0, st, A);
+    cudaLaunchConfig_t cfg = {};             // (clusters gain nothing by starting early: 96 x 131071 17.2 us without, 19.9 with)
     cfg.gridDim = dim3((unsigned)(A.rows * A.cuts));
     cfg.blockDim = dim3(kBlock);
     cfg.stream = st;
@@ -598,13 +600,12 @@ template <typename T, bool kTop> static cudaError_t launch_logprob(const Logprob
     at[0].val.clusterDim.x = A.cuts;
     at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
     cfg.attrs = at;
-    cfg.numAttrs = A.cuts > 1 ? 1 : 0;
+    cfg.numAttrs = 1;
     return cudaLaunchKernelEx(&cfg, logprob_kernel<T, kTop, kBlock / 32>, A);
 }
 template <typename T, bool kTop> static cudaError_t launch_grad(const GradArgs &A, int blocks, bool warps, cudaStream_t st) {
-    if (warps) logprob_grad_kernel<T, kTop, 1><<<(A.rows + kBlock / 32 - 1) / (kBlock / 32), kBlock, 0, st>>>(A);
-    else logprob_grad_kernel<T, kTop, kBlock / 32><<<dim3(A.rows, blocks), kBlock, 0, st>>>(A);
-    return cudaGetLastError();
+    if (warps) return launch_early(logprob_grad_kernel<T, kTop, 1>, dim3((A.rows + kBlock / 32 - 1) / (kBlock / 32)), dim3(kBlock), 0, st, A);
+    return launch_early(logprob_grad_kernel<T, kTop, kBlock / 32>, dim3(A.rows, blocks), dim3(kBlock), 0, st, A);
 }
 
 static const char *check_logits(const void *logits, const void *tokens, int rows, int vocab, int dtype, int token_bytes, int top, float temperature) {
