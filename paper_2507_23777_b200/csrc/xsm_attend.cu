@@ -26,7 +26,12 @@ constexpr int kGranule = 4, kOpening = 3;      // stages that are never cut apar
 // Units up to this many bytes of keys and values are not cut at all: a CTA reads 46 GB/s of a busy chip's and about 100 alone, and joining what two of
 // them have done takes 3 us.
 constexpr int kWholeBytes = 128 * 1024;
-constexpr int kAttendWarps = 8, kProducers = 4;
+constexpr int kProducers = 4;
+// Attending warps of a CTA: heads of 256 want 255 registers a thread, which eight warps and the producers do not have.
+__host__ __device__ constexpr int attend_warps(int dh) { return dh == 256 ? 4 : 8; }
+// Warps that share a stage's positions: where stages are so large that few fit, and a warp works on one for long (all that follows from a position's
+// key is a warp's own, so that the shares meet at the end of a unit like any others).
+__host__ __device__ constexpr int slices_of(int dh, int es) { return es == 4 ? dh >= 128 ? 4 : dh >= 64 ? 2 : 1 : dh == 256 ? 2 : 1; }
 constexpr int kRing = 16;             // most stages in shared memory
 constexpr int kMaxRowTiles = 4;       // of a unit
 constexpr int kDeclared = 4096;       // shared memory that the kernel declares, at most
@@ -259,15 +264,15 @@ __device__ __forceinline__ unsigned inside(int base, int begin, int end) {
     return (hi == 32 ? ~0u : (1u << hi) - 1u) & ~((1u << lo) - 1u);
 }
 
-// O += P V over the 32 positions of a stage.  kept: positions that take part; the others' values may be anything (kMask: they are
+// O += P V over 8 NT positions.  kept: positions that take part; the others' values may be anything (kMask: they are
 // read as zeros, so that zero weights do not meet infinities).  kSome: only rows of which `mine` is set get anything.
-template <typename T, int DH, bool kSplit, bool kMask, bool kSome>
-__device__ __forceinline__ void add_values(const float (&p)[4][4], uint32_t v_base, unsigned kept, const bool (&mine)[2], RowState<DH> &st) {
+template <typename T, int DH, int NT, bool kSplit, bool kMask, bool kSome>
+__device__ __forceinline__ void add_values(const float (&p)[NT][4], uint32_t v_base, unsigned kept, const bool (&mine)[2], RowState<DH> &st) {
     using S = Shape<T, DH>;
     const int lane = threadIdx.x & 31, t = lane & 3, g = lane >> 2;
     if constexpr (std::is_same<T, float>::value) {
 #pragma unroll
-        for (int nt = 0; nt < 4; ++nt) {
+        for (int nt = 0; nt < NT; ++nt) {
             const unsigned a0 = tf32_part(p[nt][0]), a1 = tf32_part(p[nt][2]), a2 = tf32_part(p[nt][1]), a3 = tf32_part(p[nt][3]);
             const unsigned r0 = tf32_rest(p[nt][0]), r1 = tf32_rest(p[nt][2]), r2 = tf32_rest(p[nt][1]), r3 = tf32_rest(p[nt][3]);
             const int k0 = nt * 8 + 2 * t;
@@ -290,7 +295,7 @@ __device__ __forceinline__ void add_values(const float (&p)[4][4], uint32_t v_ba
         }
     } else {
 #pragma unroll
-        for (int kk = 0; kk < 2; ++kk) {
+        for (int kk = 0; kk < NT / 2; ++kk) {
             const float (&u)[4] = p[2 * kk], (&w)[4] = p[2 * kk + 1];
             const uint4 a = make_uint4(pack2<T>(u[0], u[1]), pack2<T>(u[2], u[3]), pack2<T>(w[0], w[1]), pack2<T>(w[2], w[3]));
             uint4 r;
@@ -324,11 +329,11 @@ __device__ __forceinline__ void add_values(const float (&p)[4][4], uint32_t v_ba
 }
 
 // whether a position of `some` holds a value that is not finite
-template <typename T, int DH> __device__ __forceinline__ bool odd_values(uint32_t v_base, unsigned some) {
+template <typename T, int DH, int NT> __device__ __forceinline__ bool odd_values(uint32_t v_base, unsigned some) {
     using S = Shape<T, DH>;
     const int lane = threadIdx.x & 31;
     bool odd = false;
-    for (int r = 0; r < kStage; ++r) {
+    for (int r = 0; r < 8 * NT; ++r) {
         if (!((some >> r) & 1u)) continue;
         for (int w = lane; w < DH * S::es / 4; w += 32) odd |= not_finite<T>(lds32(S::at(v_base, r, w >> 2) + (w & 3) * 4));
     }
@@ -340,34 +345,35 @@ struct StageMask {
     unsigned row[2], any, all, valid;
 };
 
-// One stage for the sixteen rows of a warp.
-template <typename T, int DH, bool kSplitQ, bool kSplitP, bool kMask>
+// 8 NT positions of a stage (`stage`, masks and `base` begin with them) for the sixteen rows of a warp.
+template <typename T, int DH, int NT, bool kSplitQ, bool kSplitP, bool kMask>
 __device__ __forceinline__ void attend_stage(uint32_t q_base, uint32_t stage, float c, const StageMask &mask, const AttendArgs &A, const Span &sp, int base,
                                              const int (&token)[2], RowState<DH> &st) {
     using S = Shape<T, DH>;
     const int lane = threadIdx.x & 31, t = lane & 3;
-    float s[4][4], small[4][4];               // fp32 operands, or queries in two parts: products of the smaller parts, in a chain of their own
+    float s[NT][4], small[NT][4];             // fp32 operands, or queries in two parts: products of the smaller parts, in a chain of their own
 #pragma unroll
-    for (int nt = 0; nt < 4; ++nt) {
+    for (int nt = 0; nt < NT; ++nt) {
         s[nt][0] = s[nt][1] = s[nt][2] = s[nt][3] = 0.f;
         small[nt][0] = small[nt][1] = small[nt][2] = small[nt][3] = 0.f;
     }
-    const uint32_t from = stage + S::lane_at((lane & 7) + ((lane >> 4) << 3), (lane >> 3) & 1);
+    const uint32_t from = stage + (NT > 1 ? S::lane_at((lane & 7) + ((lane >> 4) << 3), (lane >> 3) & 1) : S::lane_at(lane & 7, (lane >> 3) & 1));
 #pragma unroll
     for (int ks = 0; ks < S::steps; ++ks) {
         const uint4 a = lds128(q_base + ks * 512 + lane * 16);
         uint4 al;
         if (kSplitQ || S::es == 4) al = lds128(q_base + (S::steps + ks) * 512 + lane * 16);
 #pragma unroll
-        for (int kt = 0; kt < 2; ++kt) {
+        for (int kt = 0; kt < (NT + 1) / 2; ++kt) {
             unsigned k[4];
-            ldmatrix_x4(k, S::step(from, 2 * ks) + kt * 16 * S::rb);
+            if constexpr (NT > 1) ldmatrix_x4(k, S::step(from, 2 * ks) + kt * 16 * S::rb);
+            else ldmatrix_x2(k, S::step(from, 2 * ks));
             if constexpr (S::es == 4) {
                 unsigned h[4], l[4];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) { h[i] = k[i] & 0xffffe000u; l[i] = tf32_rest_of(__uint_as_float(k[i]), h[i]); }
+                for (int i = 0; i < (NT > 1 ? 4 : 2); ++i) { h[i] = k[i] & 0xffffe000u; l[i] = tf32_rest_of(__uint_as_float(k[i]), h[i]); }
 #pragma unroll
-                for (int n = 0; n < 2; ++n) {
+                for (int n = 0; n < (NT > 1 ? 2 : 1); ++n) {
                     mma1688_tf32(small[2 * kt + n], al.x, al.y, al.z, al.w, h[2 * n], h[2 * n + 1]);
                     mma1688_tf32(small[2 * kt + n], a.x, a.y, a.z, a.w, l[2 * n], l[2 * n + 1]);
                     mma1688_tf32(s[2 * kt + n], a.x, a.y, a.z, a.w, h[2 * n], h[2 * n + 1]);
@@ -383,7 +389,7 @@ __device__ __forceinline__ void attend_stage(uint32_t q_base, uint32_t stage, fl
     }
     float top[2] = {st.m[0], st.m[1]};
 #pragma unroll
-    for (int nt = 0; nt < 4; ++nt)
+    for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             s[nt][i] = kSplitQ || S::es == 4 ? (s[nt][i] + small[nt][i]) * c : s[nt][i] * c;
@@ -405,7 +411,7 @@ __device__ __forceinline__ void attend_stage(uint32_t q_base, uint32_t stage, fl
         st.m[0] = top[0]; st.m[1] = top[1];
     }
 #pragma unroll
-    for (int nt = 0; nt < 4; ++nt) {
+    for (int nt = 0; nt < NT; ++nt) {
         s[nt][0] = ex2(s[nt][0] - ref0); s[nt][1] = ex2(s[nt][1] - ref0);
         s[nt][2] = ex2(s[nt][2] - ref1); s[nt][3] = ex2(s[nt][3] - ref1);
         st.l[0] += s[nt][0] + s[nt][1];
@@ -414,23 +420,23 @@ __device__ __forceinline__ void attend_stage(uint32_t q_base, uint32_t stage, fl
     const uint32_t v_base = stage + S::half;
     const bool all[2] = {true, true};
     if (!kMask) {
-        add_values<T, DH, kSplitP, false, false>(s, v_base, ~0u, all, st);
+        add_values<T, DH, NT, kSplitP, false, false>(s, v_base, ~0u, all, st);
     } else {
         const unsigned some = mask.any & ~mask.all;       // positions that some rows see and others do not
-        if (some == 0u || !odd_values<T, DH>(v_base, some)) {
-            add_values<T, DH, kSplitP, true, false>(s, v_base, mask.any, all, st);
+        if (some == 0u || !odd_values<T, DH, NT>(v_base, some)) {
+            add_values<T, DH, NT, kSplitP, true, false>(s, v_base, mask.any, all, st);
         } else {                                          // one of them holds an infinity or NaN: the rows of one token after the other
             for (int j = 0; j < sp.nq; ++j) {
                 const int end = A.causal ? sp.first_end + j : sp.end, begin = A.window > 0 ? max(0, end - A.window) : 0;
                 const bool mine[2] = {token[0] == j, token[1] == j};
-                add_values<T, DH, kSplitP, true, true>(s, v_base, inside(base, begin, end) & mask.valid, mine, st);
+                add_values<T, DH, NT, kSplitP, true, true>(s, v_base, inside(base, begin, end) & mask.valid, mine, st);
             }
         }
     }
 }
 
-// the eight attending warps
-__device__ __forceinline__ void bar_attend() { bar_sync<kAttendWarps * 32>(1); }
+// the attending warps
+template <int W> __device__ __forceinline__ void bar_attend() { bar_sync<W * 32>(1); }
 
 template <typename TQ> __device__ __forceinline__ void store4(TQ *p, float4 v) {
     if constexpr (sizeof(TQ) == 4) *reinterpret_cast<float4 *>(p) = v;
@@ -456,9 +462,10 @@ template <typename TQ> __device__ __forceinline__ void finish(const AttendArgs &
 }
 
 template <typename T, typename TQ, int DH>
-__global__ void __launch_bounds__((kAttendWarps + kProducers) * 32, 1)
+__global__ void __launch_bounds__((attend_warps(DH) + kProducers) * 32, 1)
 attend_kernel(const __grid_constant__ TensorMap k_map, const __grid_constant__ TensorMap v_map, const __grid_constant__ AttendArgs A) {
     using S = Shape<T, DH>;
+    constexpr int W = attend_warps(DH), kSlices = slices_of(DH, S::es), NT = 4 / kSlices;
     // queries with more bits than the pools' type enter as two parts; so do the weights, unless the output has fewer bits than they
     constexpr bool kSplitQ = S::es == 2 && sizeof(TQ) == 4, kSplitP = !(std::is_same<T, __half>::value && std::is_same<TQ, bf16>::value);
     extern __shared__ __align__(1024) unsigned char smem[];
@@ -473,16 +480,16 @@ attend_kernel(const __grid_constant__ TensorMap k_map, const __grid_constant__ T
     unsigned char *queries = smem + A.ring * S::stage + parked_bytes(DH, A.parked);
     chain_go();
     if (threadIdx.x == 0) {
-        for (int i = 0; i < A.ring; ++i) { mbar_init(full + 8 * i, 1); mbar_init(empty + 8 * i, A.rt); }
+        for (int i = 0; i < A.ring; ++i) { mbar_init(full + 8 * i, 1); mbar_init(empty + 8 * i, A.rt * kSlices); }
         mbar_init_fence();
     }
     __syncthreads();
     chain_wait();
     const int units = A.kv_heads * A.row_groups;
 
-    if (warp >= kAttendWarps) {
+    if (warp >= W) {
         // producer p of n takes stages p, p + n, ... of the CTA; slot and phase are those of its next one
-        const int p = warp - kAttendWarps;
+        const int p = warp - W;
         if (p >= A.producers) return;
         int it = 0, slot = 0, phase = 1, next = p;                    // it: stages of the segments before
         auto advance = [&](int by) {
@@ -533,12 +540,12 @@ attend_kernel(const __grid_constant__ TensorMap k_map, const __grid_constant__ T
             it += n;
         });
         // every copy lands before the CTA ends, also where an attending warp has given up
-        if (warp == kAttendWarps && lane == 0)
+        if (warp == W && lane == 0)
             for (int i = max(0, it - A.ring); i < it; ++i) mbar_wait(full + 8 * (i % A.ring), (i / A.ring) & 1, kMbarSpinLimit, A.status);
         return;
     }
 
-    const int tile = warp % A.rt, turns = A.turns, turn = warp / A.rt;      // row tile; groups that take stages, which of them (behind the last: none)
+    const int tile = warp % A.rt, share = warp / A.rt % kSlices * NT, turns = A.turns, turn = warp / (A.rt * kSlices);      // row tile; first eight positions of a stage; groups that take stages, which of them (behind the last: none)
     const int g = lane >> 2, t = lane & 3, tid = threadIdx.x;
     const int slot_floats = A.rt * 16 * (DH + 2);
     unsigned char *raw = queries + A.rt * query_bytes(DH, S::es, kSplitQ || S::es == 4);
@@ -547,7 +554,7 @@ attend_kernel(const __grid_constant__ TensorMap k_map, const __grid_constant__ T
     auto fetch_rows = [&](int b, int unit) {
         constexpr int chunks = DH * (int)sizeof(TQ) / 16;
         const int kvh = unit / A.row_groups, row0 = (unit % A.row_groups) * A.rt * 16, rows = min(A.rt * 16, A.n_rows - row0);
-        for (int i = tid; i < rows * chunks; i += kAttendWarps * 32) {
+        for (int i = tid; i < rows * chunks; i += W * 32) {
             const int r = i / chunks, c = i - r * chunks, j = (row0 + r) / A.group, h = kvh * A.group + (row0 + r - j * A.group);
             const TQ *p = reinterpret_cast<const TQ *>(A.q) + b * A.qs[0] + j * A.qs[1] + h * A.qs[2];
             asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"(smem_u32(raw) + r * raw_ld + c * 16), "l"(reinterpret_cast<const char *>(p) + c * 16) : "memory");
@@ -561,12 +568,12 @@ attend_kernel(const __grid_constant__ TensorMap k_map, const __grid_constant__ T
         if (opening) fetch_rows(b, seg.unit);
         opening = false;
         asm volatile("cp.async.wait_all;" ::: "memory");
-        bar_attend();                            // the rows are here; what the segment before parked has been read
+        bar_attend<W>();                            // the rows are here; what the segment before parked has been read
         if (tid < rows) place_row(A, b, seg.unit, sp.nq, tid, s_rows[0]);
         // A thread takes 16 bytes of the operands (eight elements, or four of fp32) at a time and puts their words where the lanes of the products
         // look for them: 32 bytes of a row a step; lane 4 (row mod 8) + (word mod 4), register (row / 8) + 2 (word / 4).
         constexpr int per = S::es == 4 ? 4 : 8, chunks = DH / per;
-        for (int i = tid; i < A.rt * 16 * chunks; i += kAttendWarps * 32) {
+        for (int i = tid; i < A.rt * 16 * chunks; i += W * 32) {
             const int r = i / chunks, ch = i - r * chunks, in = r & 15;
             struct __align__(16) Some { TQ e[per]; };
             const Some some = *reinterpret_cast<const Some *>(raw + r * raw_ld + ch * per * (int)sizeof(TQ));
@@ -588,7 +595,7 @@ attend_kernel(const __grid_constant__ TensorMap k_map, const __grid_constant__ T
                 }
             }
         }
-        bar_attend();
+        bar_attend<W>();
         if (seg.more) {
             const bool same = seg.unit + 1 < units;
             fetch_rows(same ? b : b + 1, same ? seg.unit + 1 : 0);
@@ -612,17 +619,19 @@ attend_kernel(const __grid_constant__ TensorMap k_map, const __grid_constant__ T
         for (; next < it0 + n; next += turns) {
             mbar_wait(full + 8 * slot, phase, kMbarSpinLimit, A.status);
             const int2 info = s_info[slot];
-            const uint32_t stage = ring + slot * S::stage;
+            const int base = info.x + share * 8;
+            const uint32_t stage = ring + slot * S::stage + share * 8 * S::rb;
             StageMask mask;
-            if (info.y == 3 && info.x >= sp.last_begin && info.x + kStage <= sp.first_end) {
-                attend_stage<T, DH, kSplitQ, kSplitP, false>(q_base, stage, A.c, mask, A, sp, info.x, token, st);
+            if (info.y == 3 && base >= sp.last_begin && base + 8 * NT <= sp.first_end) {
+                attend_stage<T, DH, NT, kSplitQ, kSplitP, false>(q_base, stage, A.c, mask, A, sp, base, token, st);
             } else {
-                mask.valid = (info.y & 1 ? 0xffffu : 0u) | (info.y & 2 ? 0xffff0000u : 0u);
-                mask.row[0] = inside(info.x, begin[0], end[0]) & mask.valid;
-                mask.row[1] = inside(info.x, begin[1], end[1]) & mask.valid;
-                mask.any = inside(info.x, sp.first_begin, sp.end) & mask.valid;
-                mask.all = inside(info.x, sp.last_begin, sp.first_end);
-                attend_stage<T, DH, kSplitQ, kSplitP, true>(q_base, stage, A.c, mask, A, sp, info.x, token, st);
+                constexpr unsigned mine = NT == 4 ? ~0u : (1u << (8 * NT)) - 1u;
+                mask.valid = (((info.y & 1 ? 0xffffu : 0u) | (info.y & 2 ? 0xffff0000u : 0u)) >> (share * 8)) & mine;
+                mask.row[0] = inside(base, begin[0], end[0]) & mask.valid;
+                mask.row[1] = inside(base, begin[1], end[1]) & mask.valid;
+                mask.any = inside(base, sp.first_begin, sp.end) & mask.valid;
+                mask.all = inside(base, sp.last_begin, sp.first_end);
+                attend_stage<T, DH, NT, kSplitQ, kSplitP, true>(q_base, stage, A.c, mask, A, sp, base, token, st);
             }
             __syncwarp();
             if (lane == 0) mbar_arrive(empty + 8 * slot);
@@ -631,13 +640,14 @@ attend_kernel(const __grid_constant__ TensorMap k_map, const __grid_constant__ T
         }
         it0 += n;
 
-        // the states of the warps: of eight, 4..7 hand theirs to 0..3, which park the joined ones
+        // the states of the warps: where they are more than have a place, the second half hand theirs to the first, which park the joined ones
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
             st.l[r] += __shfl_xor_sync(0xffffffffu, st.l[r], 1);
             st.l[r] += __shfl_xor_sync(0xffffffffu, st.l[r], 2);
         }
-        float *mine = parked + (warp & 3) * 16 * S::ld, *mine_ml = parked_ml + (warp & 3) * 32;
+        const int spot = warp & (A.parked - 1);
+        float *mine = parked + spot * 16 * S::ld, *mine_ml = parked_ml + spot * 32;
         auto park = [&] {
 #pragma unroll
             for (int j = 0; j < DH / 8; ++j) {
@@ -649,12 +659,12 @@ attend_kernel(const __grid_constant__ TensorMap k_map, const __grid_constant__ T
                 mine_ml[2 * g + 16] = st.m[1]; mine_ml[2 * g + 17] = st.l[1];
             }
         };
-        const bool eight = turns * A.rt == kAttendWarps;
-        if (eight) {
-            if (warp >= 4) park();
-            bar_attend();
+        const bool halved = turns * A.rt * kSlices == 2 * A.parked;
+        if (halved) {
+            if (warp >= A.parked && warp < 2 * A.parked) park();
+            bar_attend<W>();
         }
-        if (eight && warp < 4) {
+        if (halved && warp < A.parked) {
             float f[2], h[2];
 #pragma unroll
             for (int r = 0; r < 2; ++r) {
@@ -672,13 +682,13 @@ attend_kernel(const __grid_constant__ TensorMap k_map, const __grid_constant__ T
             __syncwarp();
         }
         if (warp < A.parked) park();
-        bar_attend();
+        bar_attend<W>();
         const int items = rows * (DH / 4), tiles = A.rt;
         float *place = A.partial;
         if (!seg.whole) {
             place += (2 * (long long)blockIdx.x + (run.start(blockIdx.x) < seg.first ? 1 : 0)) * slot_floats;
         }
-        for (int i = tid; i < items; i += kAttendWarps * 32) {
+        for (int i = tid; i < items; i += W * 32) {
             const int r = i / (DH / 4), d = (i - r * (DH / 4)) * 4;
             float m = -INFINITY, l = 0.f;
             float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -720,7 +730,7 @@ attend_kernel(const __grid_constant__ TensorMap k_map, const __grid_constant__ T
         }
     });
     if (pending == 0) return;
-    bar_attend();
+    bar_attend<W>();
     if (tid < pending) {
         // c0 is the first at no other unit that is cut: its counter is this unit's
         int *counter = A.counters + s_left[tid].c0, before;
@@ -729,16 +739,16 @@ attend_kernel(const __grid_constant__ TensorMap k_map, const __grid_constant__ T
         if (last) *counter = 0;                  // as the next call wants it
         s_left[tid].last = last;
     }
-    bar_attend();
-    // two of them: four warps each
+    bar_attend<W>();
+    // two of them: half of the warps each
     const bool both = pending == 2 && s_left[0].last && s_left[1].last;
-    const int first = both ? tid & 127 : tid, step = both ? 128 : kAttendWarps * 32;
+    const int first = both ? tid % (W * 16) : tid, step = both ? W * 16 : W * 32;
     for (int u = 0; u < pending; ++u) {
         const Left &left = s_left[u];
         if (left.last && tid < min(A.rt * 16, A.n_rows - (left.unit % A.row_groups) * A.rt * 16)) place_row(A, left.b, left.unit, left.nq, tid, s_rows[u]);
     }
-    bar_attend();
-    for (int u = both ? tid >> 7 : 0; u < (both ? (tid >> 7) + 1 : pending); ++u) {
+    bar_attend<W>();
+    for (int u = both ? tid / (W * 16) : 0; u < (both ? tid / (W * 16) + 1 : pending); ++u) {
         const Left left = s_left[u];
         if (!left.last) continue;
         const int n = min(A.rt * 16, A.n_rows - (left.unit % A.row_groups) * A.rt * 16) * (DH / 4);
@@ -808,16 +818,20 @@ static AttendPlan plan_attend(const xsm_kv &kv, int batch, int m, int n_heads, i
     const int es = element_size(c.dtype), rows = m * (n_heads / c.n_kv_heads), tiles = (rows + 15) / 16;
     AttendPlan p;
     const int q = query_bytes(c.d_head, es, es == 4 || q_dtype == XSM_F32) + raw_bytes(c.d_head, element_size(q_dtype)), stage = 2 * kStage * c.d_head * es;
+    const int warps = attend_warps(c.d_head) / slices_of(c.d_head, es);      // that could take stages of their own
     p.rt = tiles >= 3 ? 4 : tiles;
+    while (p.rt > warps) p.rt /= 2;
     // Shared memory: the ring gets what the parked states and the queries leave.  A group of warps that takes stages wants two places, one to
     // work on and one that fills; so few groups that wide rows leave no room, then fewer row tiles.
-    auto left = [&](int rt, int turns) { return kCtaSmem - kDeclared - parked_bytes(c.d_head, rt * turns < 4 ? rt * turns : 4) - rt * q; };
+    const int most = attend_warps(c.d_head) / 2;
+    auto parked = [&](int rt, int turns) { const int n = rt * turns * slices_of(c.d_head, es); return n < most ? n : most; };
+    auto left = [&](int rt, int turns) { return kCtaSmem - kDeclared - parked_bytes(c.d_head, parked(rt, turns)) - rt * q; };
     for (;; p.rt /= 2) {
-        p.turns = kAttendWarps / p.rt;
+        p.turns = warps / p.rt;
         while (p.turns > 1 && left(p.rt, p.turns) / stage < 2 * p.turns) p.turns /= 2;
         if (p.rt == 1 || left(p.rt, p.turns) / stage >= 2) break;
     }
-    p.parked = p.rt * p.turns < 4 ? p.rt * p.turns : 4;
+    p.parked = parked(p.rt, p.turns);
     p.ring = left(p.rt, p.turns) / stage < kRing ? left(p.rt, p.turns) / stage : kRing;
     // Whoever waits for a stage must have seen the one before it in the same place (a barrier tells one phase from the next, not from the
     // one after): groups of warps, and producers, have places of the ring of their own.  (All are powers of two, none larger than the ring.)
@@ -837,7 +851,7 @@ static cudaError_t launch_attend(const xsm_kv &kv, const AttendArgs &A, const At
     const void *fn = (const void *)attend_kernel<T, TQ, DH>;
     const cudaError_t e = open_kernel(fn, p.smem, false);
     if (e != cudaSuccess) return e;
-    return launch_early(attend_kernel<T, TQ, DH>, dim3(p.grid), dim3((kAttendWarps + kProducers) * 32), p.smem, st, kv.k_map, kv.v_map, A);
+    return launch_early(attend_kernel<T, TQ, DH>, dim3(p.grid), dim3((attend_warps(DH) + kProducers) * 32), p.smem, st, kv.k_map, kv.v_map, A);
 }
 template <typename T, typename TQ> static cudaError_t launch_width(const xsm_kv &kv, const AttendArgs &A, const AttendPlan &p, cudaStream_t st) {
     switch (kv.cfg.d_head) {
