@@ -211,11 +211,10 @@ __device__ __forceinline__ void mma1688_tf32(float (&c)[4], unsigned a0, unsigne
 __device__ __forceinline__ void mma16(float (&c)[4], const uint4 &a, unsigned b0, unsigned b1, __half) { mma16816_f16(c, a.x, a.y, a.z, a.w, b0, b1); }
 __device__ __forceinline__ void mma16(float (&c)[4], const uint4 &a, unsigned b0, unsigned b1, bf16) { mma16816_bf16(c, a.x, a.y, a.z, a.w, b0, b1); }
 
-// x = part + rest: part has the leading eleven bits (a tf32 operand), the rest keeps what a tf32 operand can of the others
-__device__ __forceinline__ unsigned tf32_part(float x) { return __float_as_uint(x) & 0xffffe000u; }
-__device__ __forceinline__ unsigned tf32_rest(float x) { return __float_as_uint(x - __uint_as_float(tf32_part(x))); }
-// (infinities and NaN: the difference of two infinities would be NaN where the product alone is right)
-__device__ __forceinline__ unsigned tf32_rest_of(float x, unsigned part) { return (part & 0x7f800000u) == 0x7f800000u ? 0u : __float_as_uint(x - __uint_as_float(part)); }
+// x = part + rest: part is x rounded to eleven bits (a tf32 operand), the rest is at most 2^-12 of it, of which a tf32 operand keeps eleven bits again
+__device__ __forceinline__ unsigned tf32_part(float x) { return (__float_as_uint(x) + 0x1000u) & 0xffffe000u; }
+// (infinities: the difference of two of them would be NaN where the product with the part is right; NaN comes back out of the rest)
+__device__ __forceinline__ unsigned tf32_rest(float x, unsigned part) { return (part & 0x7fffffffu) == 0x7f800000u ? 0u : __float_as_uint(x - __uint_as_float(part)); }
 
 // two values as 16-bit operands, first in the low half, and what the rounding took off
 template <typename T> __device__ __forceinline__ unsigned pack2(float a, float b);
@@ -271,27 +270,32 @@ __device__ __forceinline__ void add_values(const float (&p)[NT][4], uint32_t v_b
     using S = Shape<T, DH>;
     const int lane = threadIdx.x & 31, t = lane & 3, g = lane >> 2;
     if constexpr (std::is_same<T, float>::value) {
+        // The tensor core cuts off what its sum has no place for, towards zero: a stage's products are added up by themselves, and to the output by rounding.
+        unsigned a[NT][4], r[NT][4];
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-            const unsigned a0 = tf32_part(p[nt][0]), a1 = tf32_part(p[nt][2]), a2 = tf32_part(p[nt][1]), a3 = tf32_part(p[nt][3]);
-            const unsigned r0 = tf32_rest(p[nt][0]), r1 = tf32_rest(p[nt][2]), r2 = tf32_rest(p[nt][1]), r3 = tf32_rest(p[nt][3]);
-            const int k0 = nt * 8 + 2 * t;
+        for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-            for (int j = 0; j < DH / 8; ++j) {
+            for (int i = 0; i < 4; ++i) {
+                const float w = p[nt][(i & 1) * 2 + (i >> 1)];
+                a[nt][i] = tf32_part(w);
+                r[nt][i] = __float_as_uint(w - __uint_as_float(a[nt][i]));
+            }
+#pragma unroll
+        for (int j = 0; j < DH / 8; ++j) {
+            float add[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                const int k0 = nt * 8 + 2 * t;
                 unsigned x = lds32(S::at(v_base, k0, 2 * j + (g >> 2)) + (g & 3) * 4), y = lds32(S::at(v_base, k0 + 1, 2 * j + (g >> 2)) + (g & 3) * 4);
                 if (kMask) { x = (kept >> k0) & 1u ? x : 0u; y = (kept >> (k0 + 1)) & 1u ? y : 0u; }
-                const unsigned xh = x & 0xffffe000u, yh = y & 0xffffe000u;
-                const unsigned xl = tf32_rest_of(__uint_as_float(x), xh), yl = tf32_rest_of(__uint_as_float(y), yh);
-                float add[4] = {0.f, 0.f, 0.f, 0.f};
-                float (&o)[4] = kSome ? add : st.o[j];
-                mma1688_tf32(o, r0, r1, r2, r3, xh, yh);
-                mma1688_tf32(o, a0, a1, a2, a3, xl, yl);
-                mma1688_tf32(o, a0, a1, a2, a3, xh, yh);
-                if (kSome) {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) if (mine[i >> 1]) st.o[j][i] += add[i];
-                }
+                const unsigned xh = tf32_part(__uint_as_float(x)), yh = tf32_part(__uint_as_float(y));
+                const unsigned xl = tf32_rest(__uint_as_float(x), xh), yl = tf32_rest(__uint_as_float(y), yh);
+                mma1688_tf32(add, r[nt][0], r[nt][1], r[nt][2], r[nt][3], xh, yh);
+                mma1688_tf32(add, a[nt][0], a[nt][1], a[nt][2], a[nt][3], xl, yl);
+                mma1688_tf32(add, a[nt][0], a[nt][1], a[nt][2], a[nt][3], xh, yh);
             }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) if (!kSome || mine[i >> 1]) st.o[j][i] += add[i];
         }
     } else {
 #pragma unroll
@@ -351,11 +355,14 @@ __device__ __forceinline__ void attend_stage(uint32_t q_base, uint32_t stage, fl
                                              const int (&token)[2], RowState<DH> &st) {
     using S = Shape<T, DH>;
     const int lane = threadIdx.x & 31, t = lane & 3;
+    constexpr bool kHalves = S::es == 4 && NT <= 2;      // of fp32 the products of either half of the head are added up by themselves too
+    float half[kHalves ? NT : 1][4];
     float s[NT][4], small[NT][4];             // fp32 operands, or queries in two parts: products of the smaller parts, in a chain of their own
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
         s[nt][0] = s[nt][1] = s[nt][2] = s[nt][3] = 0.f;
         small[nt][0] = small[nt][1] = small[nt][2] = small[nt][3] = 0.f;
+        if (kHalves) half[nt][0] = half[nt][1] = half[nt][2] = half[nt][3] = 0.f;
     }
     const uint32_t from = stage + (NT > 1 ? S::lane_at((lane & 7) + ((lane >> 4) << 3), (lane >> 3) & 1) : S::lane_at(lane & 7, (lane >> 3) & 1));
 #pragma unroll
@@ -371,12 +378,12 @@ __device__ __forceinline__ void attend_stage(uint32_t q_base, uint32_t stage, fl
             if constexpr (S::es == 4) {
                 unsigned h[4], l[4];
 #pragma unroll
-                for (int i = 0; i < (NT > 1 ? 4 : 2); ++i) { h[i] = k[i] & 0xffffe000u; l[i] = tf32_rest_of(__uint_as_float(k[i]), h[i]); }
+                for (int i = 0; i < (NT > 1 ? 4 : 2); ++i) { h[i] = tf32_part(__uint_as_float(k[i])); l[i] = tf32_rest(__uint_as_float(k[i]), h[i]); }
 #pragma unroll
                 for (int n = 0; n < (NT > 1 ? 2 : 1); ++n) {
                     mma1688_tf32(small[2 * kt + n], al.x, al.y, al.z, al.w, h[2 * n], h[2 * n + 1]);
                     mma1688_tf32(small[2 * kt + n], a.x, a.y, a.z, a.w, l[2 * n], l[2 * n + 1]);
-                    mma1688_tf32(s[2 * kt + n], a.x, a.y, a.z, a.w, h[2 * n], h[2 * n + 1]);
+                    mma1688_tf32(kHalves && ks >= S::steps / 2 ? half[kHalves ? 2 * kt + n : 0] : s[2 * kt + n], a.x, a.y, a.z, a.w, h[2 * n], h[2 * n + 1]);
                 }
             } else {
 #pragma unroll
@@ -392,6 +399,7 @@ __device__ __forceinline__ void attend_stage(uint32_t q_base, uint32_t stage, fl
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
+            if (kHalves) s[nt][i] += half[nt][i];
             s[nt][i] = kSplitQ || S::es == 4 ? (s[nt][i] + small[nt][i]) * c : s[nt][i] * c;
             if (kMask && !((mask.row[i >> 1] >> (nt * 8 + 2 * t + (i & 1))) & 1u)) s[nt][i] = -INFINITY;
             top[i >> 1] = fmaxf(top[i >> 1], s[nt][i]);
@@ -587,7 +595,7 @@ attend_kernel(const __grid_constant__ TensorMap k_map, const __grid_constant__ T
                 if constexpr (S::es == 4) {
                     const unsigned hi = tf32_part(x[w]);
                     dst[4 * w] = hi;
-                    dst[4 * w + S::steps * 128] = tf32_rest_of(x[w], hi);
+                    dst[4 * w + S::steps * 128] = tf32_rest(x[w], hi);
                 } else {
                     const unsigned hi = pack2<T>(x[2 * w], x[2 * w + 1]);
                     dst[4 * w] = hi;
