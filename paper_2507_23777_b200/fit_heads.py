@@ -84,8 +84,9 @@ def backbone_hidden(cfg: dict, Wf, tokens: np.ndarray, cond: np.ndarray, device=
 
 
 def fit_from_corpus(cfg: dict, weights: np.ndarray, seqs, conds, iters=300, lr=2e-5, eval_every=25, holdout=0.125,
-                    batch=4096, device="cuda", seed=0):
+                    batch=4096, device="cuda", seed=0, library_loss=False):
     """seqs[i]: tokens x_0.. of mesh i (x_0 = BOS) generated by the backbone, conds[i]: its condition [C, d_cond].
+    library_loss: cross-entropy and its gradient by the library's operator (ops.token_logprobs, a GPU is needed) instead of torch's.
     Returns (weights with fitted heads, report)."""
     import torch
     import torch.nn.functional as F
@@ -116,8 +117,16 @@ def fit_from_corpus(cfg: dict, weights: np.ndarray, seqs, conds, iters=300, lr=2
     def head(g, i):
         return (g + F.silu(g @ W1[i].T)) @ Wo[i].T
 
+    if library_loss:
+        from . import ops
+
+        def entropy_of(z, t):
+            return -ops.token_logprobs(z, t).logprob.mean()
+    else:
+        entropy_of = F.cross_entropy
+
     def loss_of(g, y):      # Eq. 5 with w(d) = 0.8^d
-        return sum(0.8 ** (i + 1) * F.cross_entropy(head(g, i), y[:, i]) for i in range(K))
+        return sum(0.8 ** (i + 1) * entropy_of(head(g, i), y[:, i]) for i in range(K))
 
     curve, best, best_state, best_it = [], None, None, 0
     for it in range(iters + 1):
@@ -186,13 +195,14 @@ def main():
     ap.add_argument("--tokens", type=int, default=512, help="tokens per training mesh")
     ap.add_argument("--iters", type=int, default=300)
     ap.add_argument("--lr", type=float, default=2e-5)
+    ap.add_argument("--library-loss", action="store_true", help="cross-entropy and its gradient by the library's operator")
     ap.add_argument("--eval-tokens", type=int, default=4096)
     ap.add_argument("--eval-seeds", type=int, nargs="*", default=None, help="mesh seeds to decode (default: the configuration's)")
     args = ap.parse_args()
     build.build()
     cfg = inputs.config(args.config)
     w = inputs.make_weights(cfg)
-    fitted, report = fit(cfg, w, args.meshes, args.tokens, iters=args.iters, lr=args.lr)
+    fitted, report = fit(cfg, w, args.meshes, args.tokens, iters=args.iters, lr=args.lr, library_loss=args.library_loss)
     report.pop("curve")
     print(json.dumps({"fit": report}))
     cfg0 = dict(cfg, n_draft=0)
