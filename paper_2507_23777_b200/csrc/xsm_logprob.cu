@@ -155,9 +155,12 @@ template <int W> struct RowShared {
     static constexpr int room = W == 1 ? 256 : 512;
     __align__(16) unsigned long long candidate[room + 8];
     unsigned long long key[W], best[kMaxTop];
-    Part part[W], joined;
+    Part part[W];
     unsigned bound[W];
     int found;
+    // of a cluster's first block: what every block has found
+    __align__(16) unsigned long long gathered[W == 1 ? 1 : 8 * kMaxTop + 8];
+    Part parts[W == 1 ? 1 : 8];
 };
 
 // how many of n keys are larger than this one (what lies behind them up to a multiple of eight is zero)
@@ -215,6 +218,7 @@ template <typename T, bool kTop, int W> __global__ void __launch_bounds__(kBlock
     const int count = (W == 1 ? A.vocab : (int)(((long long)A.vocab * (cut + 1)) >> A.cut_shift)) - i0;
     const Pieces<T> in(z + i0, count);
     const float c = A.inv_t * kLog2e;
+    if (W > 1 && A.cuts > 1) cluster_arrive_relaxed();          // (nothing is told but that this block runs)
     if (kTop && tid == 0) sh.found = 0;
     float given = 0.f;
     long long token = -1;
@@ -286,7 +290,6 @@ template <typename T, bool kTop, int W> __global__ void __launch_bounds__(kBlock
         if (warp == 0) {
             a = lane < W ? sh.part[lane] : Part{-INFINITY, 0.f, 0.f};
             a.join(W, c);
-            if (A.cuts > 1 && lane == 0) sh.joined = a;
         }
     } else {
         meet<W>();
@@ -358,40 +361,35 @@ template <typename T, bool kTop, int W> __global__ void __launch_bounds__(kBlock
         meet<W>();
     }
     if (W > 1 && A.cuts > 1) {
+        // every block writes what it has found to the first one's shared memory
         __syncwarp();
-        cluster_arrive();
         cluster_wait();
-        if (cut == 0) {
-            if (warp == 0) {
-                a = Part{-INFINITY, 0.f, 0.f};
-                if (lane < A.cuts) {
-                    const uint32_t at = map_rank(smem_u32(&sh.joined), lane);
-                    a = Part{ld_cluster_f32(at), ld_cluster_f32(at + 4), ld_cluster_f32(at + 8)};
-                }
-                a.join(8, c);
-            }
-            if (kTop) {
-                // the parts' best, in order, side by side; the first of them all
-                const int n = A.cuts * A.top;
-                for (int i = tid; i < n; i += kThreads) {
-                    const uint32_t at = map_rank(smem_u32(&sh.best[i % A.top]), i / A.top);
-                    const unsigned lo = __float_as_uint(ld_cluster_f32(at)), hi = __float_as_uint(ld_cluster_f32(at + 4));
-                    sh.candidate[i] = ((unsigned long long)hi << 32) | lo;
-                }
-                if (tid < 8) sh.candidate[n + tid] = 0;
-                meet<W>();
-                for (int i = tid; i < n; i += kThreads) {
-                    const unsigned long long key = sh.candidate[i];
-                    const int before = larger(sh.candidate, n, key);
-                    if (key != 0 && before < A.top) sh.best[before] = key;
-                }
-                meet<W>();
-            }
+        if (kTop && tid < A.top) st_cluster_u64(map_rank(smem_u32(&sh.gathered[cut * A.top + tid]), 0), sh.best[tid]);
+        if (tid == 0) {
+            const uint32_t to = map_rank(smem_u32(&sh.parts[cut]), 0);
+            st_cluster_f32(to, a.m);
+            st_cluster_f32(to + 4, a.s);
+            st_cluster_f32(to + 8, a.t);
         }
         __syncwarp();
         cluster_arrive();
         cluster_wait();
         if (cut != 0) return;
+        if (warp == 0) {
+            a = lane < A.cuts ? sh.parts[lane] : Part{-INFINITY, 0.f, 0.f};
+            a.join(8, c);
+        }
+        if (kTop) {
+            const int n = A.cuts * A.top;
+            if (tid < 8) sh.gathered[n + tid] = 0;
+            meet<W>();
+            for (int i = tid; i < n; i += kThreads) {
+                const unsigned long long key = sh.gathered[i];
+                const int before = larger(sh.gathered, n, key);
+                if (key != 0 && before < A.top) sh.best[before] = key;
+            }
+            meet<W>();
+        }
     }
     // lane 0 has the row's sums
     const float log_s = logf(a.s), ref = a.m == -INFINITY ? 0.f : a.m;

@@ -196,6 +196,15 @@ class PagedCache:
                 self._ws[stream] = ws, size
         return ws, size
 
+    def check(self):
+        """Waits for the device and raises an XsmError if a bounded wait of an earlier attend ran out (its results are void)."""
+        torch.cuda.synchronize(self.device)
+        for ws, _ in self._ws.values():
+            status = int(ws[:4].view(torch.int32)[0])
+            if status:
+                ws[:4].zero_()
+                raise binding.XsmError(status, "a bounded device-side wait ran out of patience")
+
     def attend(self, q, block_table, lengths, counts=None, causal=True, window=0, scale=None, out=None, lse=None):
         """Attention of the newest tokens: q [batch, m, n_heads, d_head] over the first lengths[b] positions of every sequence, the new ones
         included.  Query j of n = counts[b] (m without counts) sees positions up to lengths[b] - n + j (all with causal=False), and

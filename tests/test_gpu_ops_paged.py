@@ -382,3 +382,41 @@ def test_refusals(ops):
     assert "q_dtype" in str(e.value)
     out, _ = cache.attend(q, table, one)          # and the cache is still good
     assert not out.any()
+
+
+def test_a_wait_that_ran_out_is_told(ops):
+    """The status word of a workspace, as a kernel would leave it."""
+    from paper_2507_23777_b200.binding import XSM_ERR_TIMEOUT, XsmError
+    kp = torch.zeros((4, 2, 32, 64), dtype=F16, device="cuda")
+    cache = ops.PagedCache(kp, kp.clone())
+    cache.check()
+    q, table, one = torch.zeros((1, 1, 2, 64), dtype=F16, device="cuda"), torch.zeros((1, 4), dtype=torch.int32, device="cuda"), torch.ones(1, dtype=torch.int32, device="cuda")
+    cache.attend(q, table, one)
+    cache.check()
+    (ws, _), = cache._ws.values()
+    ws[:4].view(torch.int32)[0] = XSM_ERR_TIMEOUT
+    with pytest.raises(XsmError) as e:
+        cache.check()
+    assert e.value.status == XSM_ERR_TIMEOUT
+    cache.check()
+
+
+@pytest.mark.parametrize("cache_t,q_t", TYPES)
+@pytest.mark.parametrize("d,m,group", [(256, 5, 7), (128, 16, 3), (96, 16, 4), (256, 1, 1), (128, 1, 1), (64, 3, 11)])
+def test_attend_wide_heads_with_many_rows_and_sliding_windows(ops, cache_t, q_t, d, m, group):
+    """Warps that share a stage, row tiles in groups, masked stages in each."""
+    for window in (0, 37):
+        check_attend(ops, cache_t, q_t, d, 1, group, m, 48, [m + 1, 300, 129], window=window, seed=d + m)
+
+
+@pytest.mark.parametrize("cache_t,q_t", TYPES)
+def test_attend_exactness(ops, cache_t, q_t):
+    """2-norm of the error against the norm of the result over 2500 keys: rounding to the output's type, 2^-9 and 2^-12 on average for numbers of eight
+    and eleven bits; fp32 outputs 2^-20, a few roundings of the scores (of a size of eight and more) and of the sums."""
+    g = gen(21)
+    k, v, table = ref.pools(g, [2500], 2, 64, 64, cache_t)
+    q = (2 * torch.randn((1, 3, 4, 64), generator=g)).to(q_t)
+    want = ref.attend(q, k, v, table, [2500])[0]
+    got, _ = ops.PagedCache(k.cuda(), v.cuda()).attend(q.cuda(), table.cuda(), torch.tensor([2500], dtype=torch.int32, device="cuda"))
+    off = float((got.cpu().double() - want).norm() / want.norm())
+    assert off < {F32: 2.0 ** -19, BF16: 2.0 ** -9, F16: 2.0 ** -12}[q_t], off
