@@ -11,6 +11,14 @@
 // groups as that leaves, which take the stages in turn.  A warp keeps its rows' output and running maximum in registers:
 // S = Q K^T, online softmax, O += P V with mma.sync; 16-bit weights enter as the sum of a rounded part and its remainder where
 // the output is to be as exact as the type allows, fp32 operands as parts of eleven bits whose three large products are added up.
+//
+// What bounds it.  Long contexts: the pools' bytes, at the rate of a copy (4 x 20000 positions of sixteen heads of 128 in fp16, 655 MB, 103 us = 98 %
+// of the measured rate; 48 ragged sequences of eight key heads in bf16, 804 MB, 126 us = 98 %).  A producer warp needs 0.4 to 0.6 us a stage: one
+// alone fed 33 GB/s an SM (158 us), four feed 46.  Short ones: a chain.  0.3 us to past the wait for the kernel before, 1.8 until lengths are
+// read and the cut is known, 0.6 for page numbers, 0.6 for the first stage, a microsecond a stage, 1.2 for joining the warps: 5.8 us for
+// 190 positions; where a unit is cut 1 us for the counter and 2 for adding up (12288 positions of sixteen heads of 64: 17 us of which the
+// bytes are 7.8).  Starting under the kernel before saves 1 us.  fp32: the chain too, with three products for one (12 us; the bytes 1.4).
+// Many rows a key head: mma.sync (8 x 4000 positions, 64 rows a key head: 44 us, the bytes 12).
 #include "xsm_ops.h"
 
 #include <limits.h>
@@ -22,9 +30,12 @@
 namespace xsm {
 
 constexpr int kStage = 32;            // positions of a stage
-constexpr int kGranule = 4, kOpening = 3;      // stages that are never cut apart; granules that a unit counts for beside its stages
-// Units up to this many bytes of keys and values are not cut at all: a CTA reads 46 GB/s of a busy chip's and about 100 alone, and joining what two of
-// them have done takes 3 us.
+// Stages that are never cut apart (2, 4, 8: 142, 138, 137 us on the ragged batch, 15.0, 15.0, 16.6 on fp32 with a window); granules that a unit counts for
+// beside its stages: its queries, the joining of its warps, its output (0, 2, 3: 133, 125, 126 us on the ragged batch, 18.2, 17.3, 16.4 on 12288
+// positions, 104.8, 103.8, 103.0 on 20000).
+constexpr int kGranule = 4, kOpening = 3;
+// Units up to this many bytes of keys and values are not cut at all: joining what two CTAs have done takes 3 us, in which one of them reads as much (190
+// positions 7.6 -> 5.9 us).
 constexpr int kWholeBytes = 128 * 1024;
 constexpr int kProducers = 4;
 // Attending warps of a CTA: heads of 256 want 255 registers a thread, which eight warps and the producers do not have.
@@ -127,7 +138,8 @@ __device__ __forceinline__ Run run_of(const AttendArgs &A, int units) {
     Run r;
     const int total = (int)__reduce_add_sync(0xffffffffu, (unsigned)sum) * units;
     // Few long units: a unit's parts are read by their CTAs side by side, n stages of 32 * 2 * d_head elements, and joined by one, C rows of d_head
-    // sums, both at about the same bytes a second, so C = sqrt(16 * element size * n / rows) parts are the quickest.
+    // sums, both at about the same bytes a second, so C = sqrt(16 * element size * n / rows) parts are the quickest (one key head at 20000 positions: 148
+    // parts 21.7 us, 50 parts 15.3).
     const float parts = sqrtf(16.f * A.element * (float)__reduce_add_sync(0xffffffffu, (unsigned)all) / (float)A.batch / (float)min(A.n_rows, A.rt * 16));
     r.ctas = min(min((int)gridDim.x, total), (int)fminf((float)A.batch * units * fmaxf(parts, 1.f), 65535.f));      // every one of them has a granule at least
     r.quot = total / r.ctas;

@@ -6,6 +6,12 @@
 // Alternatives: the largest logits of every thread bound the k-th largest of the row from below; what reaches the bound, usually little more
 // than k logits, is collected in a second look at the row (out of registers, or the caches) and sorted by counting.
 // Backward: one pass, every element from its own logit and a few numbers of its row.
+//
+// What bounds them.  Many rows: forward the instructions (8192 x 8192 of bf16 31 us where the bytes take 21: five and a half an element, of which
+// one is the exponential, and a row's 700 warp instructions of beginning and end), backward memory (41 us, as long as without any
+// arithmetic).  Two numbers an instruction (f32x2) took the pair from 111 to 78 us, blocks of 128 threads with four pieces of 16 bits
+// (eight of 32) under way to 72.  Few rows: a chain: 4.3 us for 5 x 4096 with 5 alternatives, of which a launch is 2; 96 x 131071 takes 8.0
+// without alternatives (the bytes 3.9) and 15.9 with 20, the parts' alternatives one behind the other: bound, second look, order, cluster, order.
 #include "xsm_ops.h"
 
 #include <math.h>
@@ -566,6 +572,7 @@ template <typename T, bool kTop, int W> __global__ void __launch_bounds__(kBlock
 }
 
 // Blocks that share a row, as a power of two: as many as the chip takes at a time (six an SM) over the rows, each with 4096 logits at least.
+// (96 x 131071 without alternatives: a block a row 13.5 us, two 11.5, four and eight 8.0.)
 static int cut_shift_of(int rows, int vocab, int sms) {
     int shift = 0;
     while (shift < 3 && ((long long)rows << (shift + 1)) <= 6LL * sms && (vocab >> (shift + 1)) >= 4096) ++shift;
@@ -583,7 +590,8 @@ static cudaError_t sm_count(int *sms) {
     return cudaSuccess;
 }
 
-// Short rows are a warp's each, where there are enough of them.
+// Short rows are a warp's each, where there are enough of them (16000 x 1000 with its gradient 56 us as blocks, 23 as warps; 16000 x 3001 78 and 57;
+// 8192 x 8192, past the line, 72 as blocks and 76 as warps).
 static bool by_warp(int rows, long long row_bytes, int sms) { return row_bytes <= kWarpRowBytes && rows >= 4 * sms; }
 
 template <typename T, bool kTop> static cudaError_t launch_logprob(const LogprobArgs &A, bool warps, cudaStream_t st) {
@@ -651,8 +659,9 @@ xsm_status xsm_token_logprobs_grad(const xsm_logprob_grad_args *a, void *cuda_st
     if (e != cudaSuccess) return launched(e);
     const long long row_bytes = (long long)a->vocab * element_size(a->dtype);
     const bool warps = by_warp(a->rows, row_bytes, sms), top = a->top && a->g_top;
-    // A block takes 2048 pieces of a row where there are rows enough to fill the chip, else 512.
-    const int pieces = (int)((row_bytes + 15) / 16), per_block = warps ? pieces : a->rows >= 2048 ? 2048 : 512;
+    // A block takes 2048 pieces of a row where there are rows enough for the eight blocks and more that an SM takes, else 512 (2045 rows of 1250 pieces
+    // 33.1 -> 32.6 us, 1300 of 5000 58.0 -> 56.1, 1300 of 1000 13.6 -> 14.5).
+    const int pieces = (int)((row_bytes + 15) / 16), per_block = warps ? pieces : a->rows >= 8 * sms ? 2048 : 512;
     const int blocks = pieces > per_block ? (pieces + per_block - 1) / per_block : 1;
     if (blocks > 65535) return op_failed(XSM_ERR_INVALID_ARG, "vocab is too large");
     const GradArgs A{a->logits, a->tokens, a->lse, a->entropy, a->top_ids, a->g_logprob, a->g_entropy, a->g_lse, a->g_top, a->d_logits,
