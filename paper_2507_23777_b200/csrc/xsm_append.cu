@@ -19,7 +19,8 @@ struct AppendArgs {
     const int *starts, *counts;
     const float2 *rope;
     long long qs[3], ks[3], vs[3], os[3];       // strides of sequence, token, head
-    int m, heads, d, rope_n, rot;
+    unsigned tokens, m;
+    int heads, d, rope_n, rot;
 };
 
 template <typename T, int N> struct __align__(sizeof(T) * N > 16 ? 16 : sizeof(T) * N) Vec { T e[N]; };
@@ -31,14 +32,16 @@ template <bool kPool, typename T, int N> __device__ __forceinline__ void store_f
     *reinterpret_cast<Vec<T, N> *>(p) = v;
 }
 
-// A block for every token; a thread takes N pairs of elements of a head at a time (N = 8: whole 16-byte pieces; N = 1 where the rotated
+// A block for every token (or, of tokens with few heads, for several); a thread takes N pairs of elements of a head at a time (N = 8: whole 16-byte pieces; N = 1 where the rotated
 // part or the alignment does not allow that).  Items of a token: heads of q, of k, of v, d / 2N items each, the rotated ones first.  kOnce: there
 // is a thread for every item of the token; kNear: pairs are neighbours.
 template <typename TI, typename TC, int N, bool kNear, bool kOnce>
 __global__ void __launch_bounds__(kOnce ? 512 : 128) append_kernel(const __grid_constant__ AppendArgs A, const __grid_constant__ Pages P) {
     chain_go();
     chain_wait();
-    const int b = blockIdx.x / A.m, j = blockIdx.x - b * A.m;
+    const unsigned token = kOnce ? blockIdx.x * blockDim.y + threadIdx.y : blockIdx.x;
+    if (kOnce && token >= A.tokens) return;
+    const int b = (int)(token / A.m), j = (int)(token - (unsigned)b * A.m);
     const int per_head = A.d / (2 * N), rotated = A.rot / (2 * N), n = (A.heads + 2 * P.kv_heads) * per_head;
     struct Item {
         bool is_q, is_v, turn;
@@ -205,25 +208,29 @@ xsm_status xsm_kv_append(const xsm_kv *kv, const xsm_kv_append_args *a, void *cu
     A.starts = a->starts; A.counts = a->counts;
     A.rope = reinterpret_cast<const float2 *>(a->rope);
     for (int i = 0; i < 3; ++i) { A.qs[i] = a->q_stride[i]; A.ks[i] = a->k_stride[i]; A.vs[i] = a->v_stride[i]; A.os[i] = a->q_out_stride[i]; }
-    A.m = a->m; A.heads = a->n_heads; A.d = kv->cfg.d_head; A.rope_n = a->rope_positions;
+    A.tokens = (unsigned)tokens; A.m = (unsigned)a->m; A.heads = a->n_heads; A.d = kv->cfg.d_head; A.rope_n = a->rope_positions;
     A.rot = a->rope ? a->rope_dims : 0;
     const Pages P = pages_of(*kv, a->block_table, a->table_stride, a->max_pages);
     const int es = element_size(a->in_dtype);
+    if (((uintptr_t)a->k | (uintptr_t)a->v | (uintptr_t)(a->n_heads ? a->q : nullptr) | (uintptr_t)(a->n_heads ? a->q_out : nullptr)) % es)
+        return op_failed(XSM_ERR_INVALID_ARG, "q, k, v and q_out must be aligned to their elements");
     if (((uintptr_t)a->rope) % 8) return op_failed(XSM_ERR_INVALID_ARG, "rope must be 8-byte aligned");
     const bool wide = A.rot % 16 == 0 && (uintptr_t)a->rope % 16 == 0 && aligned(a->k, a->k_stride, es) && aligned(a->v, a->v_stride, es) &&
                       (a->n_heads == 0 || (aligned(a->q, a->q_stride, es) && aligned(a->q_out, a->q_out_stride, es)));
     const int items = (A.heads + 2 * P.kv_heads) * (A.d / (wide ? 16 : 2));
     // Few tokens: a thread for every item, whose elements are requested before the token's place is known (a window of five tokens 2.45 -> 2.1 us); many:
     // 128 threads a token, fewer registers a thread (prompts of 8001 tokens 62 us, 73 the other way, 65 with 256 threads).
-    const bool once = tokens < 1024 && items <= 512;
+    const bool once = items <= 64 || (tokens < 1024 && items <= 512);
     const int threads = !once && items > 128 ? 128 : (items + 31) / 32 * 32;
+    // few items a token, many tokens: as many of them a block as make 128 threads (269790 tokens of four heads of 128: 281 us with one a block, 128 with four)
+    const int packed = tokens < 1024 || threads > 64 ? 1 : 128 / threads;
     cudaError_t e = cudaSuccess;
     with_dtype(a->in_dtype, [&](auto in) {
         with_dtype(kv->cfg.dtype, [&](auto stored) {
             using TI = decltype(in);
             using TC = decltype(stored);
             auto go = [&](auto n, auto near, auto one) {
-                e = launch_early(append_kernel<TI, TC, decltype(n)::value, decltype(near)::value, decltype(one)::value>, dim3((unsigned)tokens), dim3(threads), 0,
+                e = launch_early(append_kernel<TI, TC, decltype(n)::value, decltype(near)::value, decltype(one)::value>, dim3((unsigned)((tokens + packed - 1) / packed)), dim3(threads, packed), 0,
                                  (cudaStream_t)cuda_stream, A, P);
             };
             auto by_order = [&](auto n, auto near) { once ? go(n, near, std::true_type()) : go(n, near, std::false_type()); };

@@ -594,7 +594,7 @@ attend_kernel(const __grid_constant__ TensorMap k_map, const __grid_constant__ T
         // look for them: 32 bytes of a row a step; lane 4 (row mod 8) + (word mod 4), register (row / 8) + 2 (word / 4).
         constexpr int per = S::es == 4 ? 4 : 8, chunks = DH / per;
         for (int i = tid; i < A.rt * 16 * chunks; i += W * 32) {
-            const int r = i / chunks, ch = i - r * chunks, in = r & 15;
+            const int r = (i / (16 * chunks)) * 16 + i % 16, ch = i / 16 % chunks, in = r & 15;      // neighbouring lanes take neighbouring rows: fewer of them meet in a bank
             struct __align__(16) Some { TQ e[per]; };
             const Some some = *reinterpret_cast<const Some *>(raw + r * raw_ld + ch * per * (int)sizeof(TQ));
             float x[per];

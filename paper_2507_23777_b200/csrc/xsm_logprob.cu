@@ -621,6 +621,7 @@ static const char *check_logits(const void *logits, const void *tokens, int rows
     if (top < 0 || top > kMaxTop || top > vocab) return "top must be in [0, 32] and at most vocab";
     if (!(temperature > 0.f) || !(temperature < INFINITY) || !(1.f / temperature < INFINITY)) return "temperature must be positive and finite";
     if (rows > 0 && (!logits || !tokens)) return "null argument";
+    if ((uintptr_t)logits % element_size(dtype) || (uintptr_t)tokens % token_bytes) return "logits and tokens must be aligned to their elements";
     return nullptr;
 }
 
@@ -654,6 +655,7 @@ xsm_status xsm_token_logprobs_grad(const xsm_logprob_grad_args *a, void *cuda_st
     if (const char *m = check_logits(a->logits, a->tokens, a->rows, a->vocab, a->dtype, a->token_bytes, a->top, a->temperature)) return op_failed(XSM_ERR_INVALID_ARG, m);
     if (a->rows == 0) return XSM_OK;
     if (!a->lse || !a->d_logits || (a->g_entropy && !a->entropy) || (a->g_top && a->top && !a->top_ids)) return op_failed(XSM_ERR_INVALID_ARG, "null argument");
+    if ((uintptr_t)a->d_logits % element_size(a->dtype)) return op_failed(XSM_ERR_INVALID_ARG, "d_logits must be aligned to its elements");
     int sms = 0;
     const cudaError_t e = sm_count(&sms);
     if (e != cudaSuccess) return launched(e);

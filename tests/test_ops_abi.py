@@ -58,6 +58,16 @@ def test_pools_that_do_not_fit_are_refused(lib):
     assert b"aligned" in lib.xsm_last_error(None)
 
 
+def test_pointers_that_are_not_aligned_to_their_elements_are_refused(lib):
+    """(Before anything touches a device: the addresses lead nowhere.)"""
+    from paper_2507_23777_b200 import ops
+    for logits, tokens in ((4097, 4096), (4096, 4100)):
+        args = ops._LOGPROB.pack(logits, tokens, 4096, 4096, 4096, 0, 0, 64, 1, 2, 64, 1, 8, 0, 1.0)
+        assert lib.xsm_token_logprobs(args, None) == binding.XSM_ERR_INVALID_ARG and b"aligned" in lib.xsm_last_error(None)
+    args = ops._GRAD.pack(4096, 4096, 4096, 4096, 0, 4096, 0, 0, 0, 4097, 64, 1, 1, 0, 0, 64, 2, 64, 1, 8, 0, 1.0)
+    assert lib.xsm_token_logprobs_grad(args, None) == binding.XSM_ERR_INVALID_ARG and b"aligned" in lib.xsm_last_error(None)
+
+
 def test_no_cpu_path():
     import torch
     if torch.cuda.is_available():
