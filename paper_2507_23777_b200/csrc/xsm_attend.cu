@@ -246,12 +246,6 @@ template <> __device__ __forceinline__ unsigned rest2<__half>(float a, float b, 
 template <> __device__ __forceinline__ unsigned rest2<bf16>(float a, float b, unsigned p) {
     return pack2<bf16>(a - __uint_as_float(p << 16), b - __uint_as_float(p & 0xffff0000u));
 }
-// whether one of two 16-bit values (an fp32 value) is infinite or NaN
-template <typename T> __device__ __forceinline__ bool not_finite(unsigned v) {
-    if (std::is_same<T, float>::value) return (v & 0x7f800000u) == 0x7f800000u;
-    const unsigned e = std::is_same<T, bf16>::value ? 0x7f80u : 0x7c00u;
-    return (v & e) == e || (v & (e << 16)) == (e << 16);
-}
 __device__ __forceinline__ unsigned lds32(uint32_t a) {
     unsigned v;
     asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v) : "r"(a));
@@ -344,16 +338,23 @@ __device__ __forceinline__ void add_values(const float (&p)[NT][4], uint32_t v_b
     }
 }
 
-// whether a position of `some` holds a value that is not finite
+// Whether a position of `some` holds a value that is not finite.  (An exponent of ones and one more carry into the sign's place; the order of
+// a row's pieces does not matter.)
 template <typename T, int DH, int NT> __device__ __forceinline__ bool odd_values(uint32_t v_base, unsigned some) {
     using S = Shape<T, DH>;
-    const int lane = threadIdx.x & 31;
-    bool odd = false;
-    for (int r = 0; r < 8 * NT; ++r) {
-        if (!((some >> r) & 1u)) continue;
-        for (int w = lane; w < DH * S::es / 4; w += 32) odd |= not_finite<T>(lds32(S::at(v_base, r, w >> 2) + (w & 3) * 4));
+    constexpr unsigned ones = S::es == 4 ? 0x7f800000u : std::is_same<T, bf16>::value ? 0x7f807f80u : 0x7c007c00u;
+    constexpr unsigned more = S::es == 4 ? 0x00800000u : std::is_same<T, bf16>::value ? 0x00800080u : 0x04000400u;
+    constexpr int chunks = DH * S::es / 16, per = S::rb / 16;
+    const int lane = threadIdx.x & 31, first = __ffs(some) - 1, last = 32 - __clz(some);
+    unsigned odd = 0;
+#pragma unroll 4
+    for (int i = first * chunks + lane; i < last * chunks; i += 32) {
+        const int r = i / chunks, c = i - r * chunks;
+        const uint4 v = lds128(v_base + (c / per) * S::box_bytes + r * S::rb + c % per * 16);
+        const unsigned bits = ((v.x & ones) + more) | ((v.y & ones) + more) | ((v.z & ones) + more) | ((v.w & ones) + more);
+        odd |= (some >> r) & 1u ? bits : 0u;
     }
-    return __any_sync(0xffffffffu, odd);
+    return __any_sync(0xffffffffu, (odd & (S::es == 4 ? 0x80000000u : 0x80008000u)) != 0u);
 }
 
 // What masks a stage for a warp: positions that its two rows see, that any row of the sequence sees, that all of them do.
