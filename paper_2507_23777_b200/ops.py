@@ -54,8 +54,7 @@ def _need_ints(t, n: int, device: int, what: str):
           f"{what} must be a contiguous int32 tensor of {n} elements on cuda:{device}")
 
 
-def _empty(shape, strides, dtype, device):
-    return torch.empty_strided(shape, strides, dtype=dtype, device=device)      # (the quickest of torch's ways to new memory)
+_empty = torch.empty_strided      # the quickest of torch's ways to new memory
 
 
 def rope_table(n_positions: int, dims: int, theta: float = 10000.0, device="cuda"):
@@ -260,16 +259,19 @@ def _check_logits(logits, tokens):
 
 def _forward(logits, tokens, top, temperature):
     device, rows, vocab, ld, token_ld = _check_logits(logits, tokens)
-    where = logits.device
-    logprob, entropy, lse = (_empty((rows,), (1,), torch.float32, where) for _ in range(3))
+    where, f32, row = logits.device, torch.float32, (rows,)
+    logprob = _empty(row, (1,), dtype=f32, device=where)
+    entropy = _empty(row, (1,), dtype=f32, device=where)
+    lse = _empty(row, (1,), dtype=f32, device=where)
     ids = alt = None
+    to_ids = to_alt = 0
     if top > 0:
-        ids = _empty((rows, top), (top, 1), torch.int32, where)
-        alt = _empty((rows, top), (top, 1), torch.float32, where)
+        ids = _empty((rows, top), (top, 1), dtype=torch.int32, device=where)
+        alt = _empty((rows, top), (top, 1), dtype=f32, device=where)
+        to_ids, to_alt = ids.data_ptr(), alt.data_ptr()
     status = binding.load().xsm_token_logprobs(_LOGPROB.pack(
-        logits.data_ptr(), tokens.data_ptr(), logprob.data_ptr(), entropy.data_ptr(), lse.data_ptr(), 0 if ids is None else ids.data_ptr(),
-        0 if ids is None else alt.data_ptr(), ld, token_ld, rows, vocab, _DTYPES[logits.dtype], _TOKENS[tokens.dtype], top, temperature),
-        _raw_stream(device))
+        logits.data_ptr(), tokens.data_ptr(), logprob.data_ptr(), entropy.data_ptr(), lse.data_ptr(), to_ids, to_alt,
+        ld, token_ld, rows, vocab, _DTYPES[logits.dtype], _TOKENS[tokens.dtype], top, temperature), _raw_stream(device))
     if status:
         _check(status)
     return TokenLogprobs(logprob, entropy, lse, ids, alt)
@@ -289,14 +291,14 @@ def token_logprobs_grad(logits, tokens, result, grad_logprob=None, grad_entropy=
     missing.  out: a tensor like logits for the gradient, which may be the logits themselves."""
     device, rows, vocab, ld, token_ld = _check_logits(logits, tokens)
     if out is None:
-        out = _empty((rows, vocab), (vocab, 1), logits.dtype, logits.device)
+        out = _empty((rows, vocab), (vocab, 1), dtype=logits.dtype, device=logits.device)
     elif out.shape != logits.shape or out.dtype is not logits.dtype or out.get_device() != device or out.stride(1) != 1 and vocab > 1 or \
             out.stride(0) < vocab and rows > 1:
         raise ValueError("out must be like logits, with rows of their own")
-    lse, entropy, ids = result.lse, result.entropy, result.top_ids
-    for t in (lse, entropy):
-        if t.shape != (rows,) or t.dtype is not torch.float32 or t.get_device() != device or rows > 1 and t.stride(0) != 1:
-            raise ValueError("result must be what token_logprobs returned for these logits")
+    _, entropy, lse, ids, _ = result
+    if not (lse.shape == entropy.shape == (rows,) and lse.dtype is entropy.dtype is torch.float32 and lse.get_device() == device == entropy.get_device() and
+            lse.is_contiguous() and entropy.is_contiguous()):
+        raise ValueError("result must be what token_logprobs returned for these logits")
     gl, gl_ld = _row_grad(grad_logprob, rows, device, "grad_logprob")
     ge, ge_ld = _row_grad(grad_entropy, rows, device, "grad_entropy")
     gs, gs_ld = _row_grad(grad_lse, rows, device, "grad_lse")
