@@ -58,7 +58,8 @@ struct AttendArgs {
     float *partial;                   // two places for every CTA
     long long qs[3], os[3], table_ld;
     int batch, m, heads, group, kv_heads;
-    int whole, element;               // stages of a unit that is not cut, at most; bytes of a pool's element
+    int whole;                        // stages of a unit that is not cut, at most
+    float part_scale, all_units;      // see run_of
     int rt, row_groups, n_rows;       // row tiles of a unit, units that share a key head, query rows of a key head
     int causal, window, page, max_pages, n_pages, box_rows;
     int parked;                       // warps that park their state at the end of a unit
@@ -140,8 +141,10 @@ __device__ __forceinline__ Run run_of(const AttendArgs &A, int units) {
     // Few long units: a unit's parts are read by their CTAs side by side, n stages of 32 * 2 * d_head elements, and joined by one, C rows of d_head
     // sums, both at about the same bytes a second, so C = sqrt(16 * element size * n / rows) parts are the quickest (one key head at 20000 positions: 148
     // parts 21.7 us, 50 parts 15.3).
-    const float parts = sqrtf(16.f * A.element * (float)__reduce_add_sync(0xffffffffu, (unsigned)all) / (float)A.batch / (float)min(A.n_rows, A.rt * 16));
-    r.ctas = min(min((int)gridDim.x, total), (int)fminf((float)A.batch * units * fmaxf(parts, 1.f), 65535.f));      // every one of them has a granule at least
+    // (part_scale has what the lengths do not change: times all stages it is the square of C times the number of units.)
+    float parts;
+    asm("sqrt.approx.f32 %0, %1;" : "=f"(parts) : "f"(A.part_scale * (float)__reduce_add_sync(0xffffffffu, (unsigned)all)));
+    r.ctas = min(min((int)gridDim.x, total), (int)fminf(fmaxf(parts, A.all_units), 65535.f));      // every one of them has a granule at least
     r.quot = total / r.ctas;
     r.rem = total - r.quot * r.ctas;
     r.at = r.start(blockIdx.x);
@@ -920,9 +923,11 @@ xsm_status xsm_kv_attend(const xsm_kv *kv, const xsm_kv_attend_args *a, void *cu
     A.partial = reinterpret_cast<float *>((char *)a->workspace + kHeadBytes);
     for (int i = 0; i < 3; ++i) { A.qs[i] = a->q_stride[i]; A.os[i] = a->out_stride[i]; }
     A.batch = a->batch; A.m = a->m; A.heads = a->n_heads; A.group = a->n_heads / c.n_kv_heads; A.kv_heads = c.n_kv_heads;
-    A.whole = kWholeBytes / (2 * kStage * c.d_head * element_size(c.dtype)); A.element = element_size(c.dtype); A.rt = p.rt; A.row_groups = p.row_groups; A.n_rows = A.m * A.group; A.ring = p.ring; A.turns = p.turns; A.producers = p.producers; A.parked = p.parked;
+    A.whole = kWholeBytes / (2 * kStage * c.d_head * element_size(c.dtype)); A.rt = p.rt; A.row_groups = p.row_groups; A.n_rows = A.m * A.group; A.ring = p.ring; A.turns = p.turns; A.producers = p.producers; A.parked = p.parked;
     A.causal = a->causal != 0; A.window = a->window; A.page = c.page_size; A.max_pages = a->max_pages; A.n_pages = c.n_pages; A.box_rows = kv->box_rows;
     A.c = (float)((double)a->scale * 1.4426950408889634);
+    A.all_units = (float)p.units;
+    A.part_scale = A.all_units * A.all_units * 16.f * element_size(c.dtype) / ((float)A.batch * (float)(A.n_rows < 16 * A.rt ? A.n_rows : 16 * A.rt));
     const cudaStream_t st = (cudaStream_t)cuda_stream;
     if (c.dtype == XSM_F32) return launched(launch_width<float, float>(*kv, A, p, st));
     if (c.dtype == XSM_BF16) return launched(launch_width<bf16, bf16>(*kv, A, p, st));
