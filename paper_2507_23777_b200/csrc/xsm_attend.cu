@@ -15,10 +15,10 @@
 // What bounds it.  Long contexts: the pools' bytes, at the rate of a copy (4 x 20000 positions of sixteen heads of 128 in fp16, 655 MB, 103 us = 98 %
 // of the measured rate; 48 ragged sequences of eight key heads in bf16, 804 MB, 126 us = 98 %).  A producer warp needs 0.4 to 0.6 us a stage: one
 // alone fed 33 GB/s an SM (158 us), four feed 46.  Short ones: a chain.  0.3 us to past the wait for the kernel before, 1.8 until lengths are
-// read and the cut is known, 0.6 for page numbers, 0.6 for the first stage, a microsecond a stage, 1.2 for joining the warps: 5.8 us for
+// read and the cut is known, 0.6 for page numbers, 0.6 for the first stage, a microsecond a stage, 1.2 for joining the warps: 5.6 us for
 // 190 positions; where a unit is cut 1 us for the counter and 2 for adding up (12288 positions of sixteen heads of 64: 17 us of which the
 // bytes are 7.8).  Starting under the kernel before saves 1 us.  fp32: the chain too, with three products for one (12 us; the bytes 1.4).
-// Many rows a key head: mma.sync (8 x 4000 positions, 64 rows a key head: 44 us, the bytes 12).
+// Many rows a key head: mma.sync (8 x 4000 positions, 64 rows a key head: 42 us, the bytes 12).
 #include "xsm_ops.h"
 
 #include <limits.h>
