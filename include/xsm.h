@@ -274,7 +274,8 @@ XSM_API xsm_status xsm_kv_append(const xsm_kv *kv, const xsm_kv_append_args *a, 
  * positions t < lengths[b] and, with `causal`, t <= p = lengths[b] - n_b + j, with `window` > 0 also t > p - window.  For every query head,
  * which reads key head (head / (n_heads / n_kv_heads)):  out = sum_t softmax_t(scale q.k_t) v_t,  lse = log sum_t exp(scale q.k_t).
  * Where nothing is visible, and for j >= n_b, out is zero and lse -infinity.  What unseen positions hold does not matter, infinities and
- * NaN included.  Lengths beyond the table's end there; pages whose number lies outside the pool are not seen.
+ * NaN included; in what a row does see they may make that row's results NaN or infinite, never another row's.  Lengths beyond the table's
+ * end there; pages whose number lies outside the pool are not seen.
  * Sums and softmax in fp32.  q_dtype is the pool's type, or, over an fp16 pool, any: queries then enter as fp16 (fp32 ones as two parts), so
  * beyond +-65504 they are infinite.
  * workspace: DEVICE, xsm_kv_attend_workspace bytes, 16-byte aligned, zeroed by the caller before its first use; calls that share

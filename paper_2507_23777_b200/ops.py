@@ -70,7 +70,8 @@ class PagedCache:
     96, 128 or 256; page_size a multiple of 16.  The tensors stay the caller's and are used in place.
 
     A block table is int32 [batch, max_pages]: position p of a sequence is row p % page_size of page table[sequence, p // page_size].
-    Calls from several streams at a time are fine as far as the pools' contents allow it: every stream has a workspace of its own."""
+    Calls from several streams at a time are fine as far as the pools' contents allow it: every stream has a workspace of its own.  A
+    graph keeps the workspace that the stream it was recorded on had then: it is not replayed at the same time as that stream's calls."""
 
     def __init__(self, k, v):
         if not torch.cuda.is_available():
@@ -88,6 +89,7 @@ class PagedCache:
                                _DTYPES[k.dtype])
         self.scale = self.d_head ** -0.5
         self._ws, self._ws_bytes = {}, {}          # by stream: a workspace and its size; by shape of a call: what it needs
+        self._outgrown = []                        # workspaces that larger ones took the place of: a graph may still write to them
         _check(self.lib.xsm_kv_create(C.byref(cfg), k.data_ptr(), v.data_ptr(), C.byref(self._h)))
 
     def __del__(self):
@@ -190,15 +192,17 @@ class PagedCache:
             need = self._ws_bytes[batch, m, heads] = max(16, self.lib.xsm_kv_attend_workspace(self._h, batch, m, heads))
         ws, size = self._ws.get(stream, (None, 0))
         if size < need:
-            ws, size = torch.zeros(need, dtype=torch.uint8, device=self.k.device), need
+            old, (ws, size) = ws, (torch.zeros(need, dtype=torch.uint8, device=self.k.device), need)
             if not torch.cuda.is_current_stream_capturing():      # (a graph's own is zeroed whenever it is replayed)
                 self._ws[stream] = ws, size
+                if old is not None:
+                    self._outgrown.append(old)
         return ws, size
 
     def check(self):
         """Waits for the device and raises an XsmError if a bounded wait of an earlier attend ran out (its results are void)."""
         torch.cuda.synchronize(self.device)
-        for ws, _ in self._ws.values():
+        for ws in [ws for ws, _ in self._ws.values()] + self._outgrown:
             status = int(ws[:4].view(torch.int32)[0])
             if status:
                 ws[:4].zero_()

@@ -214,6 +214,37 @@ def test_attend_repeats_bit_for_bit_on_streams_and_in_a_graph(ops):
         assert torch.equal(out, want) and torch.equal(l2, lse)
 
 
+def test_graph_keeps_its_workspace(ops):
+    """A graph, then a call on the same stream that wants a larger workspace: the graph's is not handed out again."""
+    g = gen(31)
+    lens = [4000, 10, 2500, 900]
+    k, v, table = ref.pools(g, lens, 2, 64, 64, F16)
+    q = torch.randn((4, 16, 8, 64), generator=g).to(F16).cuda()
+    few = q[:, :1, :4].contiguous()
+    cache = ops.PagedCache(k.cuda(), v.cuda())
+    table, n = table.cuda(), torch.tensor(lens, dtype=torch.int32, device="cuda")
+    stream = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(stream):
+        want, _ = cache.attend(few, table, n)
+        small = cache._ws[stream.cuda_stream][0]
+        at, size = small.data_ptr(), small.numel()
+        del small
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=stream):
+        out, _ = cache.attend(few, table, n)
+    with torch.cuda.stream(stream):
+        cache.attend(q, table, n)
+        assert cache._ws[stream.cuda_stream][1] > size
+        others = [torch.full((size,), 85, dtype=torch.uint8, device="cuda") for _ in range(4)]
+        assert all(not o.data_ptr() <= at < o.data_ptr() + o.numel() for o in others)
+        graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(out, want) and all((o == 85).all() for o in others)
+    cache.check()
+
+
 def test_attend_offsets_beyond_32_bits(ops):
     """A pool of more than 2^32 elements: the pages at its end."""
     n_pages, page, d = 1100, 4096 * 4, 256
