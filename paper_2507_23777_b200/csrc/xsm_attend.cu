@@ -9,8 +9,8 @@
 // In a CTA a producer warp streams stages of 32 positions (boxes of the keys' and values' tensor maps; page numbers looked up 32
 // stages at a time) through a ring in shared memory.  Eight warps attend: row tiles of sixteen rows (one, two or four of them) times as many
 // groups as that leaves, which take the stages in turn.  A warp keeps its rows' output and running maximum in registers:
-// S = Q K^T, online softmax, O += P V with mma.sync; 16-bit weights enter as the sum of a rounded part and its remainder where
-// the output is to be as exact as the type allows, fp32 operands as parts of eleven bits whose three large products are added up.
+// S = Q K^T, online softmax, O += P V with mma.sync; over 16-bit pools weights enter as the sum of a rounded part and its remainder, fp32
+// operands as parts of eleven bits whose three large products are added up.
 //
 // What bounds it.  Long contexts: the pools' bytes, at the rate of a copy (4 x 20000 positions of sixteen heads of 128 in fp16, 655 MB, 103 us = 98 %
 // of the measured rate; 48 ragged sequences of eight key heads in bf16, 804 MB, 126 us = 98 %).  A producer warp needs 0.4 to 0.6 us a stage: one
@@ -274,7 +274,7 @@ __device__ __forceinline__ unsigned inside(int base, int begin, int end) {
 
 // O += P V over 8 NT positions.  kept: positions that take part; the others' values may be anything (kMask: they are
 // read as zeros, so that zero weights do not meet infinities).  kSome: only rows of which `mine` is set get anything.
-template <typename T, int DH, int NT, bool kSplit, bool kMask, bool kSome>
+template <typename T, int DH, int NT, bool kMask, bool kSome>
 __device__ __forceinline__ void add_values(const float (&p)[NT][4], uint32_t v_base, unsigned kept, const bool (&mine)[2], RowState<DH> &st) {
     using S = Shape<T, DH>;
     const int lane = threadIdx.x & 31, t = lane & 3, g = lane >> 2;
@@ -311,8 +311,7 @@ __device__ __forceinline__ void add_values(const float (&p)[NT][4], uint32_t v_b
         for (int kk = 0; kk < NT / 2; ++kk) {
             const float (&u)[4] = p[2 * kk], (&w)[4] = p[2 * kk + 1];
             const uint4 a = make_uint4(pack2<T>(u[0], u[1]), pack2<T>(u[2], u[3]), pack2<T>(w[0], w[1]), pack2<T>(w[2], w[3]));
-            uint4 r;
-            if (kSplit) r = make_uint4(rest2<T>(u[0], u[1], a.x), rest2<T>(u[2], u[3], a.y), rest2<T>(w[0], w[1], a.z), rest2<T>(w[2], w[3], a.w));
+            const uint4 r = make_uint4(rest2<T>(u[0], u[1], a.x), rest2<T>(u[2], u[3], a.y), rest2<T>(w[0], w[1], a.z), rest2<T>(w[2], w[3], a.w));
             const uint32_t from = v_base + kk * 16 * S::rb + S::lane_at((lane & 7) + (((lane >> 3) & 1) << 3), lane >> 4);
             unsigned m0 = ~0u, m1 = ~0u;
             if (kMask) {
@@ -329,7 +328,7 @@ __device__ __forceinline__ void add_values(const float (&p)[NT][4], uint32_t v_b
                 for (int h = 0; h < 2; ++h) {
                     float add[4] = {0.f, 0.f, 0.f, 0.f};
                     float (&o)[4] = kSome ? add : st.o[j + h];
-                    if (kSplit) mma16(o, r, v[2 * h], v[2 * h + 1], T());
+                    mma16(o, r, v[2 * h], v[2 * h + 1], T());
                     mma16(o, a, v[2 * h], v[2 * h + 1], T());
                     if (kSome) {
 #pragma unroll
@@ -366,7 +365,7 @@ struct StageMask {
 };
 
 // 8 NT positions of a stage (`stage`, masks and `base` begin with them) for the sixteen rows of a warp.
-template <typename T, int DH, int NT, bool kSplitQ, bool kSplitP, bool kMask>
+template <typename T, int DH, int NT, bool kSplitQ, bool kMask>
 __device__ __forceinline__ void attend_stage(uint32_t q_base, uint32_t stage, float c, const StageMask &mask, const AttendArgs &A, const Span &sp, int base,
                                              const int (&token)[2], RowState<DH> &st) {
     using S = Shape<T, DH>;
@@ -444,16 +443,16 @@ __device__ __forceinline__ void attend_stage(uint32_t q_base, uint32_t stage, fl
     const uint32_t v_base = stage + S::half;
     const bool all[2] = {true, true};
     if (!kMask) {
-        add_values<T, DH, NT, kSplitP, false, false>(s, v_base, ~0u, all, st);
+        add_values<T, DH, NT, false, false>(s, v_base, ~0u, all, st);
     } else {
         const unsigned some = mask.any & ~mask.all;       // positions that some rows see and others do not
         if (some == 0u || !odd_values<T, DH, NT>(v_base, some)) {
-            add_values<T, DH, NT, kSplitP, true, false>(s, v_base, mask.any, all, st);
+            add_values<T, DH, NT, true, false>(s, v_base, mask.any, all, st);
         } else {                                          // one of them holds an infinity or NaN: the rows of one token after the other
             for (int j = 0; j < sp.nq; ++j) {
                 const int end = A.causal ? sp.first_end + j : sp.end, begin = A.window > 0 ? max(0, end - A.window) : 0;
                 const bool mine[2] = {token[0] == j, token[1] == j};
-                add_values<T, DH, NT, kSplitP, true, true>(s, v_base, inside(base, begin, end) & mask.valid, mine, st);
+                add_values<T, DH, NT, true, true>(s, v_base, inside(base, begin, end) & mask.valid, mine, st);
             }
         }
     }
@@ -490,8 +489,8 @@ __global__ void __launch_bounds__((attend_warps(DH) + kProducers) * 32, 1)
 attend_kernel(const __grid_constant__ TensorMap k_map, const __grid_constant__ TensorMap v_map, const __grid_constant__ AttendArgs A) {
     using S = Shape<T, DH>;
     constexpr int W = attend_warps(DH), kSlices = slices_of(DH, S::es), NT = 4 / kSlices;
-    // queries with more bits than the pools' type enter as two parts; so do the weights, unless the output has fewer bits than they
-    constexpr bool kSplitQ = S::es == 2 && sizeof(TQ) == 4, kSplitP = !(std::is_same<T, __half>::value && std::is_same<TQ, bf16>::value);
+    // queries with more bits than the pools' type enter as two parts
+    constexpr bool kSplitQ = S::es == 2 && sizeof(TQ) == 4;
     extern __shared__ __align__(1024) unsigned char smem[];
     __shared__ __align__(8) unsigned long long s_full[kRing], s_empty[kRing];
     __shared__ int2 s_info[kRing];            // first position of a stage, which halves exist
@@ -647,7 +646,7 @@ attend_kernel(const __grid_constant__ TensorMap k_map, const __grid_constant__ T
             const uint32_t stage = ring + slot * S::stage + share * 8 * S::rb;
             StageMask mask;
             if (info.y == 3 && base >= sp.last_begin && base + 8 * NT <= sp.first_end) {
-                attend_stage<T, DH, NT, kSplitQ, kSplitP, false>(q_base, stage, A.c, mask, A, sp, base, token, st);
+                attend_stage<T, DH, NT, kSplitQ, false>(q_base, stage, A.c, mask, A, sp, base, token, st);
             } else {
                 constexpr unsigned mine = NT == 4 ? ~0u : (1u << (8 * NT)) - 1u;
                 mask.valid = (((info.y & 1 ? 0xffffu : 0u) | (info.y & 2 ? 0xffff0000u : 0u)) >> (share * 8)) & mine;
@@ -655,7 +654,7 @@ attend_kernel(const __grid_constant__ TensorMap k_map, const __grid_constant__ T
                 mask.row[1] = inside(base, begin[1], end[1]) & mask.valid;
                 mask.any = inside(base, sp.first_begin, sp.end) & mask.valid;
                 mask.all = inside(base, sp.last_begin, sp.first_end);
-                attend_stage<T, DH, NT, kSplitQ, kSplitP, true>(q_base, stage, A.c, mask, A, sp, base, token, st);
+                attend_stage<T, DH, NT, kSplitQ, true>(q_base, stage, A.c, mask, A, sp, base, token, st);
             }
             __syncwarp();
             if (lane == 0) mbar_arrive(empty + 8 * slot);

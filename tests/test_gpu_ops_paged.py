@@ -451,3 +451,16 @@ def test_attend_exactness(ops, cache_t, q_t):
     got, _ = ops.PagedCache(k.cuda(), v.cuda()).attend(q.cuda(), table.cuda(), torch.tensor([2500], dtype=torch.int32, device="cuda"))
     off = float((got.cpu().double() - want).norm() / want.norm())
     assert off < {F32: 2.0 ** -19, BF16: 2.0 ** -9, F16: 2.0 ** -12}[q_t], off
+
+
+def test_attend_of_bf16_queries_over_fp16_pages_is_rounded_once(ops):
+    """Against the 64-bit result rounded to bf16.  What is off by e (relative) before the rounding ends on the other side of a rounding's edge
+    in about one of 2^-8 / e numbers, which is then off by up to 2^-8: sqrt(2^8 e) 2^-8 in norm.  Scores and weights of 22 bits and more
+    leave e below 2^-18, 2^-13 in norm; weights of eleven bits 2^-13 over so many keys, 2^-10.5."""
+    g = gen(22)
+    k, v, table = ref.pools(g, [2500], 2, 64, 64, F16)
+    q = (2 * torch.randn((1, 5, 4, 64), generator=g)).to(BF16)
+    want = ref.attend(q, k, v, table, [2500])[0].float().to(BF16).double()
+    got, _ = ops.PagedCache(k.cuda(), v.cuda()).attend(q.cuda(), table.cuda(), torch.tensor([2500], dtype=torch.int32, device="cuda"))
+    off = float((got.cpu().double() - want).norm() / want.norm())
+    assert off < 2.0 ** -12, off
