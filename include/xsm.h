@@ -294,6 +294,9 @@ typedef struct {
 } xsm_kv_attend_args;
 XSM_API size_t xsm_kv_attend_workspace(const xsm_kv *kv, int batch, int m, int n_heads);
 XSM_API xsm_status xsm_kv_attend(const xsm_kv *kv, const xsm_kv_attend_args *a, void *cuda_stream);
+/* Tries of a shared-memory barrier before a wait of the following xsm_kv_attend calls gives up (0: the default, 2^22).  starve: these calls fetch no
+ * keys, so that their waits run out. */
+XSM_API xsm_status xsm_debug_kv_waits(xsm_kv *kv, uint32_t tries, int starve);
 
 /* Log probabilities under softmax(logits / temperature), of `rows` rows of `vocab` logits:
  *   lse = log sum_j exp(z_j),  logprob = z_token - lse,  entropy = -sum_j p_j log p_j,  z = logits / temperature, p = exp(z - lse),

@@ -166,6 +166,8 @@ xsm_status xsm_kv_create(const xsm_kv_config *cfg, void *d_k, void *d_v, xsm_kv 
     kv->k = d_k;
     kv->v = d_v;
     kv->box_rows = c.page_size % 32 ? 16 : 32;
+    kv->tries = kMbarSpinLimit;
+    kv->starve = 0;
     int dev = 0;
     void *encode = nullptr;
     cudaDriverEntryPointQueryResult q;
@@ -188,6 +190,13 @@ xsm_status xsm_kv_create(const xsm_kv_config *cfg, void *d_k, void *d_v, xsm_kv 
 xsm_status xsm_kv_destroy(xsm_kv *kv) {
     if (!kv) return op_failed(XSM_ERR_INVALID_ARG, "null argument");
     delete kv;
+    return XSM_OK;
+}
+
+xsm_status xsm_debug_kv_waits(xsm_kv *kv, uint32_t tries, int starve) {
+    if (!kv) return op_failed(XSM_ERR_INVALID_ARG, "null argument");
+    kv->tries = tries ? tries : kMbarSpinLimit;
+    kv->starve = starve != 0;
     return XSM_OK;
 }
 

@@ -65,6 +65,8 @@ struct AttendArgs {
     int parked;                       // warps that park their state at the end of a unit
     int ring, turns, producers;       // stages in shared memory; groups of warps that take them in turn, warps that fetch them: every place is one of each's
     float c;                          // scale * log2(e)
+    unsigned tries;                   // of a barrier, before whoever waits gives up
+    int starve;                       // nothing is fetched (a test of the waits)
 };
 
 template <typename T, int DH> struct Shape {
@@ -515,6 +517,9 @@ attend_kernel(const __grid_constant__ TensorMap k_map, const __grid_constant__ T
         const int p = warp - W;
         if (p >= A.producers) return;
         int it = 0, slot = 0, phase = 1, next = p;                    // it: stages of the segments before
+        // (lane 0) The stage behind the last that was requested: once a wait has run out, none is any more.  A place is filled again only when all its readers
+        // have said that they are through, which one that has given up never says: so no barrier is armed twice in a phase.
+        int past = A.starve ? -1 : p;
         auto advance = [&](int by) {
             slot += by;
             while (slot >= A.ring) { slot -= A.ring; phase ^= 1; }
@@ -541,9 +546,9 @@ attend_kernel(const __grid_constant__ TensorMap k_map, const __grid_constant__ T
 #pragma unroll
                     for (int h = 0; h < 2; ++h) { pg[h] = __shfl_sync(0xffffffffu, page[h], i); rw[h] = __shfl_sync(0xffffffffu, row[h], i); }
                     const int pos = __shfl_sync(0xffffffffu, first, i);
-                    if (lane == 0) {
+                    if (lane == 0 && next == past && (next < A.ring || mbar_wait(empty + 8 * slot, phase, A.tries, A.status))) {
                         const uint32_t bar = full + 8 * slot, dst = ring + slot * S::stage;
-                        if (next >= A.ring) mbar_wait(empty + 8 * slot, phase, kMbarSpinLimit, A.status);
+                        past += A.producers;
                         s_info[slot] = make_int2(pos, halves == 1 ? (pg[0] >= 0 ? 3 : 0) : (pg[0] >= 0 ? 1 : 0) | (pg[1] >= 0 ? 2 : 0));
                         mbar_arrive_expect_tx(bar, S::stage);
 #pragma unroll
@@ -562,9 +567,10 @@ attend_kernel(const __grid_constant__ TensorMap k_map, const __grid_constant__ T
             }
             it += n;
         });
-        // every copy lands before the CTA ends, also where an attending warp has given up
-        if (warp == W && lane == 0)
-            for (int i = max(0, it - A.ring); i < it; ++i) mbar_wait(full + 8 * (i % A.ring), (i / A.ring) & 1, kMbarSpinLimit, A.status);
+        // every copy lands before the CTA ends, also where an attending warp has given up: each producer looks at its own places, whose phases before it knows to
+        // be over
+        if (lane == 0)
+            for (int i = past - A.producers; i >= 0 && i > past - A.producers - A.ring; i -= A.producers) mbar_wait(full + 8 * (i % A.ring), (i / A.ring) & 1, A.tries, A.status);
         return;
     }
 
@@ -640,7 +646,11 @@ attend_kernel(const __grid_constant__ TensorMap k_map, const __grid_constant__ T
         }
         const int n = seg.stage1 - seg.stage0;
         for (; next < it0 + n; next += turns) {
-            mbar_wait(full + 8 * slot, phase, kMbarSpinLimit, A.status);
+            // (the results are void once a wait has run out: this warp waits for nothing more, and tells no producer to go on)
+            if (!__all_sync(0xffffffffu, mbar_wait(full + 8 * slot, phase, A.tries, A.status))) {
+                next = INT_MAX;
+                break;
+            }
             const int2 info = s_info[slot];
             const int base = info.x + share * 8;
             const uint32_t stage = ring + slot * S::stage + share * 8 * S::rb;
@@ -925,6 +935,8 @@ xsm_status xsm_kv_attend(const xsm_kv *kv, const xsm_kv_attend_args *a, void *cu
     A.whole = kWholeBytes / (2 * kStage * c.d_head * element_size(c.dtype)); A.rt = p.rt; A.row_groups = p.row_groups; A.n_rows = A.m * A.group; A.ring = p.ring; A.turns = p.turns; A.producers = p.producers; A.parked = p.parked;
     A.causal = a->causal != 0; A.window = a->window; A.page = c.page_size; A.max_pages = a->max_pages; A.n_pages = c.n_pages; A.box_rows = kv->box_rows;
     A.c = (float)((double)a->scale * 1.4426950408889634);
+    A.tries = kv->tries;
+    A.starve = kv->starve;
     A.all_units = (float)p.units;
     A.part_scale = A.all_units * A.all_units * 16.f * element_size(c.dtype) / ((float)A.batch * (float)(A.n_rows < 16 * A.rt ? A.n_rows : 16 * A.rt));
     const cudaStream_t st = (cudaStream_t)cuda_stream;

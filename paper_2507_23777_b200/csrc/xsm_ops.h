@@ -11,6 +11,8 @@ struct xsm_kv {
     // boxes of 16 or 32 positions of a head, as many elements wide as fill 128 (d_head 32 and 96 of 16 bits: 64) bytes, swizzled
     xsm::TensorMap k_map, v_map;
     int box_rows, sms;
+    unsigned tries;      // of a barrier of xsm_kv_attend, before a wait gives up
+    int starve;          // xsm_debug_kv_waits
 };
 
 namespace xsm {

@@ -464,3 +464,27 @@ def test_attend_of_bf16_queries_over_fp16_pages_is_rounded_once(ops):
     got, _ = ops.PagedCache(k.cuda(), v.cuda()).attend(q.cuda(), table.cuda(), torch.tensor([2500], dtype=torch.int32, device="cuda"))
     off = float((got.cpu().double() - want).norm() / want.norm())
     assert off < 2.0 ** -12, off
+
+
+@pytest.mark.parametrize("cache_t,q_t", TYPES)
+@pytest.mark.parametrize("d,lens,m", [(64, [4000, 10, 0, 900], 5), (256, [300], 16), (128, [40] * 200, 1)])
+def test_waits_that_run_out(ops, cache_t, q_t, d, lens, m):
+    """Keys that are never fetched: after a few tries every wait gives up, the call ends, its status is told once, and the next call (on counters
+    that have to be back at zero) is right."""
+    from paper_2507_23777_b200.binding import XSM_ERR_TIMEOUT, XsmError
+    g = gen(d)
+    k, v, table = ref.pools(g, lens, 2, 32, d, cache_t)
+    q = torch.randn((len(lens), m, 4, d), generator=g).to(q_t).cuda()
+    cache, table, n = ops.PagedCache(k.cuda(), v.cuda()), table.cuda(), torch.tensor(lens, dtype=torch.int32, device="cuda")
+    want, lse = cache.attend(q, table, n)
+    cache.check()
+    cache.lib.xsm_debug_kv_waits(cache._h, 20, 1)
+    cache.attend(q, table, n)
+    cache.lib.xsm_debug_kv_waits(cache._h, 0, 0)
+    with pytest.raises(XsmError) as e:
+        cache.check()
+    assert e.value.status == XSM_ERR_TIMEOUT
+    cache.check()
+    got, lse2 = cache.attend(q, table, n)
+    cache.check()
+    assert torch.equal(got, want) and torch.equal(lse, lse2)
