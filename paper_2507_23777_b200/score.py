@@ -58,10 +58,11 @@ class Scorer:
 
     @torch.no_grad()
     def logits(self, tokens, start: int):
-        """Logits behind tokens [batch, m] at positions start, start + 1, ...: [batch, m, vocab]; the caches hold the positions before."""
-        m = tokens.shape[1]
+        """Logits behind tokens [batch, m] at positions start, start + 1, ...: [batch, m, vocab]; the caches hold the positions before.  Behind a token
+        outside the vocabulary they are NaN."""
+        m, vocab = tokens.shape[1], self.cfg["vocab"]
         at = torch.full((self.batch,), start, dtype=torch.int32, device="cuda")
-        h = self.W("E")[tokens]
+        h = self.W("E")[tokens.clamp(0, vocab - 1)].masked_fill(((tokens < 0) | (tokens >= vocab))[..., None], float("nan"))
         for l in range(self.cfg["n_layers"]):
             p, cache, cond = f"l{l}.", self.cache[l], self.cond_cache[l]
             u = self._norm(h, p + "g1")
@@ -77,9 +78,12 @@ class Scorer:
     def score(self, cond, tokens, top: int = 0, temperature: float = 1.0) -> ops.TokenLogprobs:
         """tokens [batch, n], x_0 = BOS: (logprob, entropy, lse) [batch, n - 1] of x_1 .. x_{n-1}, and with `top` the best ids and their log
         probabilities [batch, n - 1, top] at every place."""
-        x = torch.as_tensor(np.asarray(tokens), dtype=torch.int64, device="cuda")
-        if x.shape[0] != self.batch or not 2 <= x.shape[1] <= self.max_tokens + 1:
+        tokens = np.asarray(tokens)
+        if tokens.ndim != 2 or tokens.shape[0] != self.batch or not 2 <= tokens.shape[1] <= self.max_tokens + 1:
             raise ValueError(f"tokens must be [{self.batch}, 2 to {self.max_tokens + 1}]")
+        if tokens.dtype.kind not in "iuf" or (tokens != np.floor(tokens)).any() or tokens.min() < 0 or tokens.max() >= self.cfg["vocab"]:
+            raise ValueError(f"tokens must be whole numbers in [0, {self.cfg['vocab']})")
+        x = torch.as_tensor(tokens.astype(np.int64), device="cuda")
         self.condition(cond)
         parts = []
         for a in range(0, x.shape[1] - 1, WINDOW):

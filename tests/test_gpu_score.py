@@ -78,3 +78,32 @@ def test_heads_fitted_with_the_operators_loss(score):
     a, b = ([c["held_out_loss"] for c in r["curve"]] for r in runs)
     assert len(a) == 4 and a[0] != a[-1]
     assert np.allclose(a, b, rtol=1e-4)
+
+
+def test_tokens_outside_the_vocabulary_are_refused(score):
+    """On the host, before anything is looked up by them; the scorer is as good as before."""
+    cfg = gpu_cfg(dtype=1)
+    s = score.Scorer(cfg, inputs.make_weights(cfg), 1, 20)
+    cond = inputs.make_cond(cfg, 1)
+    good = np.array([[cfg["bos_id"], 3, 7, cfg["vocab"] - 1]])
+    want = s.score(cond, good).logprob
+    for bad in (-1, cfg["vocab"], 2 ** 40, -(2 ** 40)):
+        for place in (0, 2, 3):
+            tokens = good.copy()
+            tokens[0, place] = bad
+            with pytest.raises(ValueError):
+                s.score(cond, tokens)
+    with pytest.raises(ValueError):
+        s.score(cond, good + 0.5)
+    assert torch.equal(s.score(cond, good).logprob, want)
+
+
+def test_logits_behind_tokens_outside_the_vocabulary_are_nan(score):
+    cfg = gpu_cfg(dtype=0)
+    s = score.Scorer(cfg, inputs.make_weights(cfg), 1, 20)
+    s.condition(inputs.make_cond(cfg, 1))
+    tokens = torch.tensor([[cfg["bos_id"], 3, cfg["vocab"], 4]], device="cuda")
+    z = s.logits(tokens, 0)
+    s.condition(inputs.make_cond(cfg, 1))
+    assert torch.equal(z[:, :2], s.logits(tokens.clamp(max=cfg["vocab"] - 1), 0)[:, :2]) and z[:, 2:].isnan().all()
+    assert s.logits(torch.tensor([[-1]], device="cuda"), 4).isnan().all()
