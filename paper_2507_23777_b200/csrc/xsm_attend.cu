@@ -372,6 +372,9 @@ __device__ __forceinline__ void attend_stage(uint32_t q_base, uint32_t stage, fl
                                              const int (&token)[2], RowState<DH> &st) {
     using S = Shape<T, DH>;
     const int lane = threadIdx.x & 31, t = lane & 3;
+    // Weights over fp16 pools are the type's numbers, of which 2^-24 is the least step: they are up to 2^15 instead of 1, so that a key whose weight is 2^-18 of
+    // the largest still has its 22 bits, and the error of any is below 2^-40 of the largest (17.5 nats below a key without a value: off by half, and by 2^-15 now).
+    constexpr int kHead = std::is_same<T, __half>::value ? 15 : 0;
     constexpr bool kHalves = S::es == 4 && NT <= 2;      // of fp32 the products of either half of the head are added up by themselves too
     float half[kHalves ? NT : 1][4];
     float s[NT][4], small[NT][4];             // fp32 operands, or queries in two parts: products of the smaller parts, in a chain of their own
@@ -411,7 +414,7 @@ __device__ __forceinline__ void attend_stage(uint32_t q_base, uint32_t stage, fl
             }
         }
     }
-    float top[2] = {st.m[0], st.m[1]};
+    float top[2] = {-INFINITY, -INFINITY};
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -425,6 +428,9 @@ __device__ __forceinline__ void attend_stage(uint32_t q_base, uint32_t stage, fl
     for (int r = 0; r < 2; ++r) {
         top[r] = fmaxf(top[r], __shfl_xor_sync(0xffffffffu, top[r], 1));
         top[r] = fmaxf(top[r], __shfl_xor_sync(0xffffffffu, top[r], 2));
+        // the reference that the weights are taken against (kHead below the largest score; rounded up, so that no weight is above 2^kHead however large the
+        // scores are)
+        top[r] = fmaxf(st.m[r], kHead > 0 ? __fadd_ru(top[r], (float)-kHead) : top[r]);
     }
     // nothing seen so far: any finite reference will do, the weights are zero
     const float ref0 = kMask && top[0] == -INFINITY ? 0.f : top[0], ref1 = kMask && top[1] == -INFINITY ? 0.f : top[1];

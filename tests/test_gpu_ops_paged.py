@@ -488,3 +488,45 @@ def test_waits_that_run_out(ops, cache_t, q_t, d, lens, m):
     got, lse2 = cache.attend(q, table, n)
     cache.check()
     assert torch.equal(got, want) and torch.equal(lse, lse2)
+
+
+@pytest.mark.parametrize("cache_t,q_t", TYPES)
+@pytest.mark.parametrize("nats", [8.0, 11.0, 15.0, 17.5, 18.0])
+def test_attend_keys_far_below_one_without_a_value(ops, cache_t, q_t, nats):
+    """A key that takes nearly all of the softmax and whose value is zero: what the others have is the whole result.  Over 16-bit pages a
+    weight enters as two parts of the type, over fp16 ones of which 2^-24 is the smallest step and 2^15 the largest weight's size."""
+    for n, at in ((201, 0), (201, 130), (201, 200), (2600, 5), (2600, 2599)):
+        g = gen(n + at)
+        k, v, table = ref.pools(g, [n], 1, 32, 64, cache_t)
+        k.zero_()
+        v.copy_(1 + torch.rand(v.shape, generator=g))
+        k[table[0, at // 32], 0, at % 32, 0] = nats
+        v[table[0, at // 32], 0, at % 32] = 0
+        q = torch.zeros((1, 1, 2, 64), dtype=q_t)
+        q[..., 0] = 1
+        want, lse, _, _ = ref.attend(q, k, v, table, [n], scale=1.0)
+        cache = ops.PagedCache(k.cuda(), v.cuda())
+        got, got_lse = cache.attend(q.cuda(), table.cuda(), torch.tensor([n], dtype=torch.int32, device="cuda"), scale=1.0)
+        part = {F16: max(2.0 ** -22, 2.0 ** -25 / (2.0 ** 15 * math.exp(-nats))), BF16: 2.0 ** -16, F32: 2.0 ** -20}[cache_t]
+        # the exponent of 26 at most, its rounding 2^-24 of it; exponentials 2^-22; sums
+        close(got, want, (UNIT[q_t] + part + 2.0 ** -18 + n * 2.0 ** -24) * want.abs() + TINY[q_t], "out")
+        close(got_lse, lse, 2.0 ** -22 * lse.abs() + n * 2.0 ** -24, "lse")
+
+
+@pytest.mark.parametrize("q_t", [F16, BF16, F32])
+@pytest.mark.parametrize("scale", [2.0 ** e for e in range(0, 101, 5)])
+def test_attend_scores_of_any_size_over_fp16_pages(ops, q_t, scale):
+    """The largest score's weight is far from the largest fp16 number, and the reference that it is taken against is a rounded one: two equal
+    keys above all others share the softmax evenly, whatever their score."""
+    g = gen(1)
+    k, v, table = ref.pools(g, [90], 1, 32, 64, F16)
+    k.zero_()
+    for at in (3, 77):
+        k[table[0, at // 32], 0, at % 32, 0] = 1023.0
+    q = torch.zeros((1, 1, 1, 64), dtype=q_t)
+    q[..., 0] = 1
+    cache = ops.PagedCache(k.cuda(), v.cuda())
+    got, lse = cache.attend(q.cuda(), table.cuda(), torch.tensor([90], dtype=torch.int32, device="cuda"), scale=scale)
+    a, b = (v[table[0, at // 32], 0, at % 32].double() for at in (3, 77))
+    close(got[0, 0, 0], (a + b) / 2, UNIT[q_t] * ((a + b) / 2).abs() + 2.0 ** -20 * (a.abs() + b.abs()) + TINY[q_t], "out")
+    close(lse[0, 0, 0], torch.tensor(1023.0 * scale + math.log(2.0), dtype=torch.float64), torch.tensor(1023.0 * scale * 2.0 ** -22 + 2.0 ** -20), "lse")
