@@ -939,10 +939,12 @@ xsm_status xsm_kv_attend(const xsm_kv *kv, const xsm_kv_attend_args *a, void *cu
     for (int i = 0; i < 3; ++i) { A.qs[i] = a->q_stride[i]; A.os[i] = a->out_stride[i]; }
     A.batch = a->batch; A.m = a->m; A.heads = a->n_heads; A.group = a->n_heads / c.n_kv_heads; A.kv_heads = c.n_kv_heads;
     A.whole = kWholeBytes / (2 * kStage * c.d_head * element_size(c.dtype)); A.rt = p.rt; A.row_groups = p.row_groups; A.n_rows = A.m * A.group; A.ring = p.ring; A.turns = p.turns; A.producers = p.producers; A.parked = p.parked;
-    A.causal = a->causal != 0; A.window = a->window; A.page = c.page_size; A.max_pages = a->max_pages; A.n_pages = c.n_pages; A.box_rows = kv->box_rows;
+    A.causal = a->causal != 0; A.page = c.page_size; A.max_pages = a->max_pages; A.n_pages = c.n_pages; A.box_rows = kv->box_rows;
     A.c = (float)((double)a->scale * 1.4426950408889634);
     A.tries = kv->tries;
     A.starve = kv->starve;
+    // (lengths end at INT_MAX - 2 kStage: a larger window sees no more, and would not go below a first end of -15)
+    A.window = a->window < INT_MAX - kStage ? a->window : INT_MAX - kStage;
     A.all_units = (float)p.units;
     A.part_scale = A.all_units * A.all_units * 16.f * element_size(c.dtype) / ((float)A.batch * (float)(A.n_rows < 16 * A.rt ? A.n_rows : 16 * A.rt));
     const cudaStream_t st = (cudaStream_t)cuda_stream;

@@ -530,3 +530,12 @@ def test_attend_scores_of_any_size_over_fp16_pages(ops, q_t, scale):
     a, b = (v[table[0, at // 32], 0, at % 32].double() for at in (3, 77))
     close(got[0, 0, 0], (a + b) / 2, UNIT[q_t] * ((a + b) / 2).abs() + 2.0 ** -20 * (a.abs() + b.abs()) + TINY[q_t], "out")
     close(lse[0, 0, 0], torch.tensor(1023.0 * scale + math.log(2.0), dtype=torch.float64), torch.tensor(1023.0 * scale * 2.0 ** -22 + 2.0 ** -20), "lse")
+
+
+@pytest.mark.parametrize("cache_t,q_t", TYPES)
+@pytest.mark.parametrize("window", [2 ** 31 - 1, 2 ** 31 - 2, 2 ** 31 - 10, 2 ** 31 - 40])
+def test_attend_window_at_the_end_of_its_type(ops, cache_t, q_t, window):
+    """A window that nothing lies before, over lengths below the number of new tokens too."""
+    check_attend(ops, cache_t, q_t, 64, 2, 2, 5, 32, [1, 2, 3, 0, 40], window=window, seed=3)
+    check_attend(ops, cache_t, q_t, 64, 1, 1, 16, 16, [1, 9, 16, 17], window=window, seed=4)
+    check_attend(ops, cache_t, q_t, 32, 1, 1, 16, 64, [2000, 3], window=window, counts=[16, 12], seed=5)
