@@ -262,7 +262,7 @@ XSM_API xsm_status xsm_kv_destroy(xsm_kv *kv);
 typedef struct {
     const void *q, *k, *v;                /* in_dtype [batch][m][n_heads or n_kv_heads][d_head]; q may be NULL */
     void *q_out;                          /* in_dtype [batch][m][n_heads][d_head] */
-    const int32_t *block_table;           /* DEVICE [batch][max_pages] */
+    const int32_t *block_table;           /* DEVICE [batch][max_pages]; may be NULL where max_pages is 0 */
     const int32_t *starts, *counts;       /* DEVICE [batch]; counts may be NULL: m each */
     const float *rope;                    /* DEVICE [rope_positions][rope_dims/2][2] cosine, sine; NULL: no rotation */
     int64_t q_stride[3], k_stride[3], v_stride[3], q_out_stride[3], table_stride;
@@ -286,7 +286,7 @@ typedef struct {
     const void *q;                        /* q_dtype [batch][m][n_heads][d_head], strides as above, 16-byte aligned */
     void *out;                            /* likewise */
     float *lse;                           /* [batch][m][n_heads], may be NULL */
-    const int32_t *block_table;           /* DEVICE [batch][max_pages] */
+    const int32_t *block_table;           /* DEVICE [batch][max_pages]; may be NULL where max_pages is 0 */
     const int32_t *lengths, *counts;      /* DEVICE [batch]: positions in the cache, the new ones included */
     void *workspace;
     int64_t q_stride[3], out_stride[3], table_stride, workspace_bytes;

@@ -210,7 +210,7 @@ xsm_status xsm_kv_append(const xsm_kv *kv, const xsm_kv_append_args *a, void *cu
     const long long tokens = (long long)a->batch * a->m;
     if (tokens == 0) return XSM_OK;
     if (tokens > 0x7fffffff) return op_failed(XSM_ERR_INVALID_ARG, "more than 2^31 - 1 tokens");
-    if (!a->k || !a->v || !a->block_table || !a->starts) return op_failed(XSM_ERR_INVALID_ARG, "null argument");
+    if (!a->k || !a->v || (!a->block_table && a->max_pages) || !a->starts) return op_failed(XSM_ERR_INVALID_ARG, "null argument");
     if (a->n_heads && (!a->q || !a->q_out)) return op_failed(XSM_ERR_INVALID_ARG, "n_heads without q or q_out");
     AppendArgs A;
     A.q = a->q; A.k = a->k; A.v = a->v; A.q_out = a->q_out;

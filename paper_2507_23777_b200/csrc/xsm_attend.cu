@@ -923,7 +923,7 @@ xsm_status xsm_kv_attend(const xsm_kv *kv, const xsm_kv_attend_args *a, void *cu
     if (a->window < 0 || (a->window && !a->causal)) return op_failed(XSM_ERR_INVALID_ARG, "window must not be negative, and needs causal");
     if (!(fabsf(a->scale) < INFINITY)) return op_failed(XSM_ERR_INVALID_ARG, "scale must be finite");
     if (a->batch == 0) return XSM_OK;
-    if (!a->q || !a->out || !a->block_table || !a->lengths || !a->workspace) return op_failed(XSM_ERR_INVALID_ARG, "null argument");
+    if (!a->q || !a->out || (!a->block_table && a->max_pages) || !a->lengths || !a->workspace) return op_failed(XSM_ERR_INVALID_ARG, "null argument");
     const AttendPlan p = plan_attend(*kv, a->batch, a->m, a->n_heads, a->q_dtype);
     if ((double)p.units * ((double)a->max_pages * c.page_size / (kStage * kGranule) + kOpening + 2) > INT_MAX / 2) return op_failed(XSM_ERR_INVALID_ARG, "batch * heads * positions is too large");
     if (a->workspace_bytes < (int64_t)p.workspace) return op_failed(XSM_ERR_CAPACITY, "the workspace is too small");

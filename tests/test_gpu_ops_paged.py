@@ -539,3 +539,19 @@ def test_attend_window_at_the_end_of_its_type(ops, cache_t, q_t, window):
     check_attend(ops, cache_t, q_t, 64, 2, 2, 5, 32, [1, 2, 3, 0, 40], window=window, seed=3)
     check_attend(ops, cache_t, q_t, 64, 1, 1, 16, 16, [1, 9, 16, 17], window=window, seed=4)
     check_attend(ops, cache_t, q_t, 32, 1, 1, 16, 64, [2000, 3], window=window, counts=[16, 12], seed=5)
+
+
+def test_a_table_without_pages(ops):
+    """Nothing has a place: nothing is written, nothing is seen, queries are rotated as ever."""
+    g = gen(14)
+    kp = torch.randn((4, 2, 16, 64), generator=g).to(F16).cuda()
+    cache = ops.PagedCache(kp, kp.clone())
+    before = kp.clone()
+    x = torch.randn((3, 2, 2, 64), generator=g).to(F16).cuda()
+    table, some, n = torch.zeros((3, 0), dtype=torch.int32, device="cuda"), torch.zeros((3, 1), dtype=torch.int32, device="cuda"), torch.tensor([0, 2, 9], dtype=torch.int32, device="cuda")
+    rope = ops.rope_table(32, 64)
+    q = cache.append(x, x, table, n, q=x, rope=rope)
+    out, lse = cache.attend(x, table, n)
+    assert torch.equal(kp, before) and torch.equal(cache.v, before)
+    assert not out.any() and (lse == -math.inf).all()
+    assert torch.equal(q, cache.append(x, x, some, n, q=x, rope=rope))
