@@ -229,7 +229,12 @@ __device__ __forceinline__ void mma16(float (&c)[4], const uint4 &a, unsigned b0
 __device__ __forceinline__ void mma16(float (&c)[4], const uint4 &a, unsigned b0, unsigned b1, bf16) { mma16816_bf16(c, a.x, a.y, a.z, a.w, b0, b1); }
 
 // x = part + rest: part is x rounded to eleven bits (a tf32 operand), the rest is at most 2^-12 of it, of which a tf32 operand keeps eleven bits again
-__device__ __forceinline__ unsigned tf32_part(float x) { return (__float_as_uint(x) + 0x1000u) & 0xffffe000u; }
+__device__ __forceinline__ unsigned tf32_weight(float x) { return (__float_as_uint(x) + 0x1000u) & 0xffffe000u; }      // (far from the largest number)
+// (the numbers next to the largest are cut off instead of rounded to an infinity)
+__device__ __forceinline__ unsigned tf32_part(float x) {
+    const unsigned u = __float_as_uint(x), up = (u + 0x1000u) & 0xffffe000u;
+    return (up & 0x7fffffffu) == 0x7f800000u ? u & 0xffffe000u : up;
+}
 // (infinities: the difference of two of them would be NaN where the product with the part is right; NaN comes back out of the rest)
 __device__ __forceinline__ unsigned tf32_rest(float x, unsigned part) { return (part & 0x7fffffffu) == 0x7f800000u ? 0u : __float_as_uint(x - __uint_as_float(part)); }
 
@@ -288,7 +293,7 @@ __device__ __forceinline__ void add_values(const float (&p)[NT][4], uint32_t v_b
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const float w = p[nt][(i & 1) * 2 + (i >> 1)];
-                a[nt][i] = tf32_part(w);
+                a[nt][i] = tf32_weight(w);
                 r[nt][i] = __float_as_uint(w - __uint_as_float(a[nt][i]));
             }
 #pragma unroll

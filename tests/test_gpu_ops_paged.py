@@ -555,3 +555,51 @@ def test_a_table_without_pages(ops):
     assert torch.equal(kp, before) and torch.equal(cache.v, before)
     assert not out.any() and (lse == -math.inf).all()
     assert torch.equal(q, cache.append(x, x, some, n, q=x, rope=rope))
+
+
+@pytest.mark.parametrize("cache_t,q_t", TYPES)
+@pytest.mark.parametrize("sign", [1, -1])
+def test_attend_largest_numbers_of_the_type(ops, cache_t, q_t, sign):
+    """Keys and values of the type's largest and lowest number: rows that do not see them are exact, a row that sees nothing else has them."""
+    d, m, n, page = 64, 4, 97, 32
+    bad = sign * torch.finfo(cache_t).max
+    g = gen(17)
+    k, v, table = ref.pools(g, [n, 1], 1, page, d, cache_t, fill=bad)
+    q = torch.randn((2, m, 2, d), generator=g).to(q_t)
+    want, _, weight, score = ref.attend(q, k, v, table, [n, 1])
+    s = (2.0 ** -21 + d * 2.0 ** -24) * score + 2.0 ** -22
+    bound = UNIT[q_t] * want.abs() + (2 * s[..., None] + 2.0 ** -11 + 100 * 2.0 ** -24) * weight + TINY[q_t]
+    for victim in (k, v):
+        kept = victim.clone()
+        for p in (n - 1, n - 2):
+            victim[table[0, p // page], 0, p % page, ::3] = bad
+        victim[table[1, 0], 0, 0] = bad
+        got, lse = ops.PagedCache(k.cuda(), v.cuda()).attend(q.cuda(), table.cuda(), torch.tensor([n, 1], dtype=torch.int32, device="cuda"))
+        close(got[0, :2], want[0, :2], bound[0, :2], "rows before")
+        if victim is v:
+            assert torch.isfinite(lse[:, 3]).all()
+            out = got[1, 3].cpu().double()
+            if q_t is cache_t:          # (else beyond the other type's range, or rounded to it)
+                assert ((out - bad).abs() <= 2.0 ** -20 * abs(bad)).all()
+        victim.copy_(kept)
+    # no part of a key that a query has nothing in
+    k.zero_()
+    k[..., 0] = bad
+    q.zero_()
+    q[..., 1] = 1
+    got, lse = ops.PagedCache(k.cuda(), v.cuda()).attend(q.cuda(), table.cuda(), torch.tensor([n, 1], dtype=torch.int32, device="cuda"))
+    want, want_lse, weight, _ = ref.attend(q, k, v, table, [n, 1])
+    close(got, want, UNIT[q_t] * want.abs() + (2.0 ** -11 + 2.0 ** -17) * weight + TINY[q_t], "queries of nothing")
+    close(lse, want_lse, 2.0 ** -20 * want_lse.abs().nan_to_num(posinf=1.0) + 2.0 ** -20, "lse of nothing")
+
+
+@pytest.mark.parametrize("bits", [0x7f800001, 0x7f800fff, 0x7fc00000, 0x7fffffff])
+def test_attend_any_nan_of_fp32_pages_is_one(ops, bits):
+    for victim in (0, 1):
+        pool = [torch.zeros((1, 1, 32, 64)), torch.ones((1, 1, 32, 64))]
+        pool[victim][0, 0, 4, 3] = torch.tensor(bits, dtype=torch.int32).view(F32)
+        q = torch.ones((1, 1, 1, 64), device="cuda")
+        got, _ = ops.PagedCache(pool[0].cuda(), pool[1].cuda()).attend(q, torch.zeros((1, 1), dtype=torch.int32, device="cuda"), torch.tensor([9], dtype=torch.int32, device="cuda"))
+        assert got[0, 0, 0, 3].isnan()
+        if victim:
+            assert (got[0, 0, 0, 4:] == 1).all()
