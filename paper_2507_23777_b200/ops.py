@@ -143,7 +143,11 @@ class PagedCache:
     def append(self, k, v, block_table, starts, counts=None, q=None, rope=None, interleaved=False, out=None):
         """Writes k and v, [batch, m, n_kv_heads, d_head], to positions starts[b] + j (j < counts[b]) of every sequence; keys, and queries
         q [batch, m, n_heads, d_head], are rotated by `rope` (float32 [positions, dims / 2, 2], see rope_table).  Returns the rotated
-        queries in `out` (a new tensor, or the one given; it may be q), or None without q."""
+        queries in `out` (a new tensor, or the one given; it may be q), or None without q.  Like attend it has no gradient, and refuses tensors that
+        want one unless torch.no_grad() says that it is not needed."""
+        if torch.is_grad_enabled() and (k.requires_grad or v.requires_grad or q is not None and q.requires_grad or rope is not None and rope.requires_grad or
+                                        out is not None and out.requires_grad):
+            raise ValueError("append has no gradient: call it under torch.no_grad()")
         device, dtype, shape, ks, vs, table = self.device, k.dtype, k.shape, k.stride(), v.stride(), block_table.shape
         qs = os = (0, 0, 0, 1)
         heads = positions = half = 0
@@ -214,7 +218,7 @@ class PagedCache:
         of these the last `window` (0: all).  Returns (out, lse): out like q, lse float32 [batch, m, n_heads], the logarithm of the sum
         of exp(scale q.k), -inf where nothing is seen."""
         device, shape, qs, dtype, table = self.device, q.shape, q.stride(), q.dtype, block_table.shape
-        if q.requires_grad and torch.is_grad_enabled():
+        if torch.is_grad_enabled() and (q.requires_grad or out is not None and out.requires_grad or lse is not None and lse.requires_grad):
             raise ValueError("attend has no gradient: call it under torch.no_grad()")
         if out is None:
             out = torch.empty(shape, dtype=dtype, device=q.device)

@@ -603,3 +603,22 @@ def test_attend_any_nan_of_fp32_pages_is_one(ops, bits):
         assert got[0, 0, 0, 3].isnan()
         if victim:
             assert (got[0, 0, 0, 4:] == 1).all()
+
+
+def test_calls_without_a_gradient_refuse_tensors_that_want_one(ops):
+    kp = torch.zeros((4, 2, 32, 64), dtype=BF16, device="cuda")
+    cache = ops.PagedCache(kp, kp.clone())
+    table, one = torch.zeros((1, 4), dtype=torch.int32, device="cuda"), torch.ones(1, dtype=torch.int32, device="cuda")
+    x = torch.zeros((1, 1, 2, 64), dtype=BF16, device="cuda")
+    leaf = x.clone().requires_grad_()
+    rope = ops.rope_table(8, 64)
+    for call in (lambda: cache.append(leaf, x, table, one), lambda: cache.append(x, leaf, table, one), lambda: cache.append(x, x, table, one, q=leaf),
+                 lambda: cache.append(x, x, table, one, q=2 * leaf, rope=rope), lambda: cache.append(x, x, table, one, q=x, out=2 * leaf),
+                 lambda: cache.append(x, x, table, one, q=x, rope=rope.clone().requires_grad_()), lambda: cache.attend(leaf, table, one),
+                 lambda: cache.attend(x, table, one, out=2 * leaf), lambda: cache.attend(cache.append(x, x, table, one, q=2 * leaf), table, one)):
+        with pytest.raises(ValueError) as e:
+            call()
+        assert "no_grad" in str(e.value)
+        with torch.no_grad():
+            call()
+    assert not cache.append(x, x, table, one, q=x).requires_grad
