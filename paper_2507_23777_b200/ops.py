@@ -13,6 +13,7 @@ import struct
 from collections import namedtuple
 
 import torch
+from torch.autograd import forward_ad
 
 from . import binding
 
@@ -40,6 +41,13 @@ def _check(status: int):
 def _need(ok, what: str):
     if not ok:
         raise ValueError(what)
+
+
+def _no_tangents(*tensors):
+    """Within a level of forward-mode differentiation: a tangent would get lost without a word."""
+    for t in tensors:
+        if t is not None and forward_ad.unpack_dual(t).tangent is not None:
+            raise ValueError("the operators have no forward-mode derivatives")
 
 
 def _need_here(t):
@@ -148,6 +156,8 @@ class PagedCache:
         if torch.is_grad_enabled() and (k.requires_grad or v.requires_grad or q is not None and q.requires_grad or rope is not None and rope.requires_grad or
                                         out is not None and out.requires_grad):
             raise ValueError("append has no gradient: call it under torch.no_grad()")
+        if forward_ad._current_level >= 0:
+            _no_tangents(k, v, q, rope)
         device, dtype, shape, ks, vs, table = self.device, k.dtype, k.shape, k.stride(), v.stride(), block_table.shape
         qs = os = (0, 0, 0, 1)
         heads = positions = half = 0
@@ -220,6 +230,8 @@ class PagedCache:
         device, shape, qs, dtype, table = self.device, q.shape, q.stride(), q.dtype, block_table.shape
         if torch.is_grad_enabled() and (q.requires_grad or out is not None and out.requires_grad or lse is not None and lse.requires_grad):
             raise ValueError("attend has no gradient: call it under torch.no_grad()")
+        if forward_ad._current_level >= 0:
+            _no_tangents(q, self.k, self.v)
         if out is None:
             out = torch.empty(shape, dtype=dtype, device=q.device)
         rows = shape[:3]
@@ -296,8 +308,15 @@ def _row_grad(g, rows, device, what):
 def token_logprobs_grad(logits, tokens, result, grad_logprob=None, grad_entropy=None, grad_lse=None, grad_top=None, temperature=1.0, out=None):
     """The gradient by the logits, in their type, of sum(grad_logprob * logprob) + sum(grad_entropy * entropy) + ... of what token_logprobs
     returned as `result` for the same logits, tokens and temperature.  grad_*: float32 [rows], grad_top [rows, top]; each may be
-    missing.  out: a tensor like logits for the gradient, which may be the logits themselves."""
+    missing.  out: a tensor like logits for the gradient, which may be the logits themselves.  There are no second derivatives: tensors that want a
+    gradient are refused unless torch.no_grad() says that it is not needed."""
     device, rows, vocab, ld, token_ld = _check_logits(logits, tokens)
+    if torch.is_grad_enabled():
+        for t in (logits, grad_logprob, grad_entropy, grad_lse, grad_top, out, *result):
+            if t is not None and t.requires_grad:
+                raise ValueError("token_logprobs_grad has no gradient of its own: call it under torch.no_grad()")
+    if forward_ad._current_level >= 0:
+        _no_tangents(logits, grad_logprob, grad_entropy, grad_lse, grad_top)
     if out is None:
         out = _empty((rows, vocab), (vocab, 1), dtype=logits.dtype, device=logits.device)
     elif out.shape != logits.shape or out.dtype is not logits.dtype or out.get_device() != device or out.stride(1) != 1 and vocab > 1 or \
@@ -351,7 +370,9 @@ class _TokenLogprobs(torch.autograd.Function):
 def token_logprobs(logits, tokens, top: int = 0, temperature: float = 1.0) -> TokenLogprobs:
     """Scores tokens [rows] (int32 or int64; one outside the vocabulary is none, and scores 0) under softmax(logits / temperature), logits
     [rows, vocab]: (logprob, entropy, lse) float32 [rows], and with `top` > 0 the ids (int32 [rows, top]) and log probabilities of the
-    largest logits, equal ones by the lower id first.  Differentiable by the logits."""
+    largest logits, equal ones by the lower id first.  Differentiable by the logits, once and backwards."""
+    if forward_ad._current_level >= 0:
+        _no_tangents(logits)
     if logits.requires_grad and torch.is_grad_enabled():
         return TokenLogprobs(*_TokenLogprobs.apply(logits, tokens, top, temperature))
     return _forward(logits, tokens, top, temperature)

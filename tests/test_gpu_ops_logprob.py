@@ -266,3 +266,37 @@ def test_refusals(ops):
     empty = ops.token_logprobs(z[:0], t[:0], top=2)
     assert empty.logprob.shape == (0,) and empty.top_ids.shape == (0, 2)
     assert ops.token_logprobs_grad(z[:0], t[:0], empty, grad_top=empty.top_logprobs).shape == (0, 10)
+
+
+def test_derivatives_that_no_call_has_are_refused(ops):
+    """Forward mode, and second derivatives: an error, not a result without its derivative."""
+    import torch.autograd.forward_ad as forward_ad
+    z, t = logits(3, 40, F32, 11)
+    z, t, g = z.cuda(), t.cuda(), torch.ones(3, device="cuda")
+    r = ops.token_logprobs(z, t, top=2)
+    leaf, gl = z.clone().requires_grad_(), g.clone().requires_grad_()
+    gt = torch.ones((3, 2), device="cuda", requires_grad=True)
+    for call in (lambda: ops.token_logprobs_grad(leaf, t, r, grad_logprob=g), lambda: ops.token_logprobs_grad(2 * leaf, t, r, grad_logprob=g),
+                 lambda: ops.token_logprobs_grad(z, t, r, grad_logprob=gl), lambda: ops.token_logprobs_grad(z, t, r, grad_entropy=gl),
+                 lambda: ops.token_logprobs_grad(z, t, r, grad_lse=gl), lambda: ops.token_logprobs_grad(z, t, r, grad_top=gt),
+                 lambda: ops.token_logprobs_grad(z, t, r, grad_logprob=g, out=2 * leaf),
+                 lambda: ops.token_logprobs_grad(z, t, ops.token_logprobs(leaf, t), grad_logprob=g)):
+        with pytest.raises(ValueError) as e:
+            call()
+        assert "no_grad" in str(e.value)
+        with torch.no_grad():
+            call()
+    kp = torch.zeros((4, 2, 32, 64), dtype=BF16, device="cuda")
+    cache = ops.PagedCache(kp, kp.clone())
+    table, one = torch.zeros((1, 4), dtype=torch.int32, device="cuda"), torch.ones(1, dtype=torch.int32, device="cuda")
+    x = torch.zeros((1, 1, 2, 64), dtype=BF16, device="cuda")
+    with forward_ad.dual_level():
+        dual, dual_x, dual_g = (forward_ad.make_dual(a, torch.ones_like(a)) for a in (z, x, g))
+        for call in (lambda: ops.token_logprobs(dual, t), lambda: ops.token_logprobs_grad(dual, t, r, grad_logprob=g), lambda: ops.token_logprobs_grad(z, t, r, grad_logprob=dual_g),
+                     lambda: cache.append(dual_x, x, table, one), lambda: cache.append(x, x, table, one, q=dual_x), lambda: cache.attend(dual_x, table, one)):
+            with pytest.raises(ValueError) as e:
+                call()
+            assert "forward" in str(e.value)
+        assert all(torch.equal(a, b) for a, b in zip(ops.token_logprobs(z, t, top=2), r))          # what has no tangent is as ever
+    with pytest.raises(Exception):
+        torch.func.jvp(lambda a: ops.token_logprobs(a, t).logprob, (z,), (z,))
