@@ -33,6 +33,9 @@ _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i:
 _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
+_BEYOND = struct.error, OverflowError      # what packing says of a number that its field does not hold
+
+
 def _check(status: int):
     if status:
         raise binding.XsmError(status, binding.load().xsm_last_error(None).decode())
@@ -190,11 +193,15 @@ class PagedCache:
             ok = counts.shape == (batch,) and counts.dtype is torch.int32 and counts.get_device() == device and (batch < 2 or counts.stride(0) == 1)
         if not ok:
             self._refuse_append(k, v, block_table, starts, counts, q, rope, out if out is not None else q)
-        status = self.lib.xsm_kv_append(self._h, _APPEND.pack(
-            0 if q is None else q.data_ptr(), k.data_ptr(), v.data_ptr(), 0 if out is None else out.data_ptr(), block_table.data_ptr(),
-            starts.data_ptr(), 0 if counts is None else counts.data_ptr(), 0 if rope is None else rope.data_ptr(),
-            qs[0], qs[1], qs[2], ks[0], ks[1], ks[2], vs[0], vs[1], vs[2], os[0], os[1], os[2], ts[0],
-            batch, m, heads, _DTYPES[dtype], table[1], positions, 2 * half, interleaved), _raw_stream(device))
+        try:
+            args = _APPEND.pack(
+                0 if q is None else q.data_ptr(), k.data_ptr(), v.data_ptr(), 0 if out is None else out.data_ptr(), block_table.data_ptr(),
+                starts.data_ptr(), 0 if counts is None else counts.data_ptr(), 0 if rope is None else rope.data_ptr(),
+                qs[0], qs[1], qs[2], ks[0], ks[1], ks[2], vs[0], vs[1], vs[2], os[0], os[1], os[2], ts[0],
+                batch, m, heads, _DTYPES[dtype], table[1], positions, 2 * half, interleaved)
+        except _BEYOND as e:
+            raise ValueError(f"an argument of append is beyond its type: {e}") from None
+        status = self.lib.xsm_kv_append(self._h, args, _raw_stream(device))
         if status:
             _check(status)
         return out
@@ -252,10 +259,14 @@ class PagedCache:
             self._refuse_attend(q, block_table, lengths, counts, out, lse)
         stream = _raw_stream(device)
         ws, ws_bytes = self._workspace(stream, batch, m, heads)
-        status = self.lib.xsm_kv_attend(self._h, _ATTEND.pack(
-            q.data_ptr(), out.data_ptr(), lse.data_ptr(), block_table.data_ptr(), lengths.data_ptr(), 0 if counts is None else counts.data_ptr(),
-            ws.data_ptr(), qs[0], qs[1], qs[2], os[0], os[1], os[2], ts[0], ws_bytes, batch, m, heads, _DTYPES[dtype], table[1], causal, window,
-            self.scale if scale is None else scale), stream)
+        try:
+            args = _ATTEND.pack(
+                q.data_ptr(), out.data_ptr(), lse.data_ptr(), block_table.data_ptr(), lengths.data_ptr(), 0 if counts is None else counts.data_ptr(),
+                ws.data_ptr(), qs[0], qs[1], qs[2], os[0], os[1], os[2], ts[0], ws_bytes, batch, m, heads, _DTYPES[dtype], table[1], causal, window,
+                self.scale if scale is None else scale)
+        except _BEYOND as e:
+            raise ValueError(f"an argument of attend is beyond its type: {e}") from None
+        status = self.lib.xsm_kv_attend(self._h, args, stream)
         if status:
             _check(status)
         return out, lse
@@ -286,12 +297,18 @@ def _forward(logits, tokens, top, temperature):
     ids = alt = None
     to_ids = to_alt = 0
     if top > 0:
+        if top > min(32, vocab) or top != int(top):
+            raise ValueError(f"top must be a whole number in [0, 32] and at most vocab, not {top}")
         ids = _empty((rows, top), (top, 1), dtype=torch.int32, device=where)
         alt = _empty((rows, top), (top, 1), dtype=f32, device=where)
         to_ids, to_alt = ids.data_ptr(), alt.data_ptr()
-    status = binding.load().xsm_token_logprobs(_LOGPROB.pack(
-        logits.data_ptr(), tokens.data_ptr(), logprob.data_ptr(), entropy.data_ptr(), lse.data_ptr(), to_ids, to_alt,
-        ld, token_ld, rows, vocab, _DTYPES[logits.dtype], _TOKENS[tokens.dtype], top, temperature), _raw_stream(device))
+    try:
+        args = _LOGPROB.pack(
+            logits.data_ptr(), tokens.data_ptr(), logprob.data_ptr(), entropy.data_ptr(), lse.data_ptr(), to_ids, to_alt,
+            ld, token_ld, rows, vocab, _DTYPES[logits.dtype], _TOKENS[tokens.dtype], top, temperature)
+    except _BEYOND as e:
+        raise ValueError(f"an argument of token_logprobs is beyond its type: {e}") from None
+    status = binding.load().xsm_token_logprobs(args, _raw_stream(device))
     if status:
         _check(status)
     return TokenLogprobs(logprob, entropy, lse, ids, alt)
@@ -336,10 +353,13 @@ def token_logprobs_grad(logits, tokens, result, grad_logprob=None, grad_entropy=
                 ids.get_device() != device:
             raise ValueError("grad_top must be contiguous float32 [rows, top] beside the result's top_ids")
         top, alternatives, gt = ids.shape[1], ids.data_ptr(), grad_top.data_ptr()
-    status = binding.load().xsm_token_logprobs_grad(_GRAD.pack(
-        logits.data_ptr(), tokens.data_ptr(), lse.data_ptr(), entropy.data_ptr(), alternatives, gl, ge, gs, gt, out.data_ptr(),
-        ld, token_ld, gl_ld, ge_ld, gs_ld, out.stride(0), rows, vocab, _DTYPES[logits.dtype], _TOKENS[tokens.dtype], top, temperature),
-        _raw_stream(device))
+    try:
+        args = _GRAD.pack(
+            logits.data_ptr(), tokens.data_ptr(), lse.data_ptr(), entropy.data_ptr(), alternatives, gl, ge, gs, gt, out.data_ptr(),
+            ld, token_ld, gl_ld, ge_ld, gs_ld, out.stride(0), rows, vocab, _DTYPES[logits.dtype], _TOKENS[tokens.dtype], top, temperature)
+    except _BEYOND as e:
+        raise ValueError(f"an argument of token_logprobs_grad is beyond its type: {e}") from None
+    status = binding.load().xsm_token_logprobs_grad(args, _raw_stream(device))
     if status:
         _check(status)
     return out

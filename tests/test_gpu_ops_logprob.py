@@ -300,3 +300,14 @@ def test_derivatives_that_no_call_has_are_refused(ops):
         assert all(torch.equal(a, b) for a, b in zip(ops.token_logprobs(z, t, top=2), r))          # what has no tangent is as ever
     with pytest.raises(Exception):
         torch.func.jvp(lambda a: ops.token_logprobs(a, t).logprob, (z,), (z,))
+
+
+def test_numbers_beyond_their_type_are_refused(ops):
+    """(Before any memory is asked for.)"""
+    from paper_2507_23777_b200.binding import XsmError
+    z, t = torch.zeros((2, 10), device="cuda"), torch.zeros(2, dtype=torch.int64, device="cuda")
+    r = ops.token_logprobs(z, t)
+    for call in (lambda: ops.token_logprobs(z, t, top=2 ** 40), lambda: ops.token_logprobs(z, t, top=2 ** 31), lambda: ops.token_logprobs(z, t, top=1.5),
+                 lambda: ops.token_logprobs(z, t, temperature=1e39), lambda: ops.token_logprobs_grad(z, t, r, temperature=1e39)):
+        with pytest.raises((ValueError, XsmError)):
+            call()

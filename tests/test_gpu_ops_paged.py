@@ -622,3 +622,14 @@ def test_calls_without_a_gradient_refuse_tensors_that_want_one(ops):
         with torch.no_grad():
             call()
     assert not cache.append(x, x, table, one, q=x).requires_grad
+
+
+def test_numbers_beyond_their_type_are_refused(ops):
+    from paper_2507_23777_b200.binding import XsmError
+    kp = torch.zeros((4, 2, 32, 64), dtype=F16, device="cuda")
+    cache = ops.PagedCache(kp, kp.clone())
+    table, one = torch.zeros((1, 4), dtype=torch.int32, device="cuda"), torch.ones(1, dtype=torch.int32, device="cuda")
+    q = torch.zeros((1, 1, 2, 64), dtype=F16, device="cuda")
+    for call in (lambda: cache.attend(q, table, one, window=2 ** 31), lambda: cache.attend(q, table, one, window=1.5), lambda: cache.attend(q, table, one, scale=1e39)):
+        with pytest.raises((ValueError, XsmError)):
+            call()
