@@ -30,6 +30,8 @@ TokenLogprobs = namedtuple("TokenLogprobs", "logprob entropy lse top_ids top_log
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
 
 
+# says to autograd that tensors have been written to: what keeps one of them for a backward pass notices
+_written = torch._C._increment_version
 _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
@@ -170,9 +172,12 @@ class PagedCache:
             ok = (kv_heads == self.n_kv_heads and d == self.d_head and ks[3] == vs[3] == 1 and v.dtype is dtype and table[0] == batch and
                   starts.shape == (batch,) and block_table.dtype is starts.dtype is torch.int32 and k.get_device() == device == v.get_device() and
                   block_table.get_device() == device == starts.get_device() == _current_device())
+        written = [self.k, self.v]
         if ok and q is not None:
             qs, q_shape = q.stride(), q.shape
-            if out is None:
+            if out is not None:
+                written.append(out)
+            else:
                 out = torch.empty(q_shape, dtype=q.dtype, device=q.device)
             os = out.stride()
             ok = (len(q_shape) == 4 and q_shape == out.shape and qs[3] == os[3] == 1 and q_shape[0] == batch and q_shape[1] == m and q_shape[3] == d and
@@ -201,6 +206,7 @@ class PagedCache:
                 batch, m, heads, _DTYPES[dtype], table[1], positions, 2 * half, interleaved)
         except _BEYOND as e:
             raise ValueError(f"an argument of append is beyond its type: {e}") from None
+        _written(written)
         status = self.lib.xsm_kv_append(self._h, args, _raw_stream(device))
         if status:
             _check(status)
@@ -239,11 +245,16 @@ class PagedCache:
             raise ValueError("attend has no gradient: call it under torch.no_grad()")
         if forward_ad._current_level >= 0:
             _no_tangents(q, self.k, self.v)
+        written = []
         if out is None:
             out = torch.empty(shape, dtype=dtype, device=q.device)
+        else:
+            written.append(out)
         rows = shape[:3]
         if lse is None:
             lse = torch.empty(rows, dtype=torch.float32, device=q.device)
+        else:
+            written.append(lse)
         os = out.stride()
         ok = len(shape) == 4 and len(table) == 2 and shape == out.shape and lse.shape == rows and dtype in _DTYPES
         if ok:
@@ -266,6 +277,8 @@ class PagedCache:
                 self.scale if scale is None else scale)
         except _BEYOND as e:
             raise ValueError(f"an argument of attend is beyond its type: {e}") from None
+        if written:
+            _written(written)
         status = self.lib.xsm_kv_attend(self._h, args, stream)
         if status:
             _check(status)
@@ -339,6 +352,8 @@ def token_logprobs_grad(logits, tokens, result, grad_logprob=None, grad_entropy=
     elif out.shape != logits.shape or out.dtype is not logits.dtype or out.get_device() != device or out.stride(1) != 1 and vocab > 1 or \
             out.stride(0) < vocab and rows > 1:
         raise ValueError("out must be like logits, with rows of their own")
+    else:
+        _written([out])
     _, entropy, lse, ids, _ = result
     if not (lse.shape == entropy.shape == (rows,) and lse.dtype is entropy.dtype is torch.float32 and lse.get_device() == device == entropy.get_device() and
             lse.is_contiguous() and entropy.is_contiguous()):

@@ -633,3 +633,27 @@ def test_numbers_beyond_their_type_are_refused(ops):
     for call in (lambda: cache.attend(q, table, one, window=2 ** 31), lambda: cache.attend(q, table, one, window=1.5), lambda: cache.attend(q, table, one, scale=1e39)):
         with pytest.raises((ValueError, XsmError)):
             call()
+
+
+def test_writes_in_place_are_seen_by_autograd(ops):
+    """A tensor that another step keeps for its backward pass, written by a call: torch says so, as with its own operators."""
+    kp = torch.zeros((4, 2, 32, 64), device="cuda")
+    table, one = torch.zeros((1, 4), dtype=torch.int32, device="cuda"), torch.ones(1, dtype=torch.int32, device="cuda")
+    w = torch.ones((), device="cuda", requires_grad=True)
+    x = torch.ones((1, 1, 2, 64), device="cuda")
+    z, t = torch.zeros((2, 10), device="cuda"), torch.zeros(2, dtype=torch.int64, device="cuda")
+
+    def fresh():
+        cache = ops.PagedCache(kp.clone(), kp.clone())
+        return cache, cache.k, cache.v, x.clone(), torch.ones((1, 1, 2), device="cuda"), z.clone()
+    for i, call in enumerate((lambda c, out, lse, d: c.append(x, x, table, one), lambda c, out, lse, d: c.append(x, x, table, one),
+                              lambda c, out, lse, d: c.append(x, x, table, one, q=x, out=out), lambda c, out, lse, d: c.attend(x, table, one, out=out),
+                              lambda c, out, lse, d: c.attend(x, table, one, lse=lse),
+                              lambda c, out, lse, d: ops.token_logprobs_grad(d, t, ops.token_logprobs(d, t), out=d))):
+        cache, k, v, out, lse, d = fresh()
+        kept = (k, v, out, out, lse, d)[i]
+        y = (w * kept).sum()
+        with torch.no_grad():
+            call(cache, out, lse, d)
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            y.backward()
