@@ -299,6 +299,16 @@ XSM_API xsm_status xsm_kv_attend(const xsm_kv *kv, const xsm_kv_attend_args *a, 
  * keys, so that their waits run out. */
 XSM_API xsm_status xsm_debug_kv_waits(xsm_kv *kv, uint32_t tries, int starve);
 
+/* For a caller that keeps a workspace for each graph that it records.  xsm_capture_id: the number of the capture that the stream takes part in, 0: none.
+ * xsm_capture_watch: *out belongs to the graph that is being recorded on the stream; xsm_capture_gone says 1, once, when that graph and all that was
+ * instantiated of it are destroyed, and frees it.  xsm_capture_mode: what the calling thread may do while streams are recorded (cudaStreamCaptureMode);
+ * returns the mode before, or -1. */
+typedef struct xsm_capture xsm_capture;
+XSM_API uint64_t xsm_capture_id(void *cuda_stream);
+XSM_API xsm_status xsm_capture_watch(void *cuda_stream, xsm_capture **out);
+XSM_API int xsm_capture_gone(xsm_capture *c);
+XSM_API int xsm_capture_mode(int mode);
+
 /* Log probabilities under softmax(logits / temperature), of `rows` rows of `vocab` logits:
  *   lse = log sum_j exp(z_j),  logprob = z_token - lse,  entropy = -sum_j p_j log p_j,  z = logits / temperature, p = exp(z - lse),
  * and the `top` (0 to 32) largest logits, equal ones by the lower index first: top_ids, top_logprobs = z - lse.

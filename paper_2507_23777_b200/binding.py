@@ -24,7 +24,8 @@ EXPORTS = [
     "xsm_debug_get_kv", "xsm_debug_set_drafts", "xsm_debug_get_state", "xsm_debug_set_phase_launch",
     "xsm_debug_trace_step", "xsm_spec_step_static", "xsm_debug_set_wait_limits", "xsm_debug_launch_stage",
     "xsm_debug_set_script", "xsm_debug_plan", "xsm_kv_create", "xsm_kv_destroy", "xsm_kv_append", "xsm_kv_attend_workspace",
-    "xsm_kv_attend", "xsm_debug_kv_waits", "xsm_token_logprobs", "xsm_token_logprobs_grad",
+    "xsm_kv_attend", "xsm_debug_kv_waits", "xsm_capture_id", "xsm_capture_watch", "xsm_capture_gone", "xsm_capture_mode",
+    "xsm_token_logprobs", "xsm_token_logprobs_grad",
 ]
 
 
@@ -101,6 +102,11 @@ def load(path: str | None = None):
     L.xsm_kv_append.argtypes = [vp, vp, vp]
     L.xsm_kv_attend.argtypes = [vp, vp, vp]
     L.xsm_debug_kv_waits.argtypes = [vp, C.c_uint32, C.c_int]
+    L.xsm_capture_id.restype = C.c_uint64
+    L.xsm_capture_id.argtypes = [vp]
+    L.xsm_capture_watch.argtypes = [vp, C.POINTER(vp)]
+    L.xsm_capture_gone.argtypes = [vp]
+    L.xsm_capture_mode.argtypes = [C.c_int]
     L.xsm_kv_attend_workspace.restype = C.c_size_t
     L.xsm_kv_attend_workspace.argtypes = [vp, C.c_int, C.c_int, C.c_int]
     L.xsm_token_logprobs.argtypes = [vp, vp]

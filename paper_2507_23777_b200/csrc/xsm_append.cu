@@ -8,6 +8,7 @@
 #include <cuda.h>
 #include <limits.h>
 
+#include <atomic>
 #include <new>
 #include <type_traits>
 
@@ -198,6 +199,62 @@ xsm_status xsm_debug_kv_waits(xsm_kv *kv, uint32_t tries, int starve) {
     kv->tries = tries ? tries : kMbarSpinLimit;
     kv->starve = starve != 0;
     return XSM_OK;
+}
+
+// One word that the graph's end sets, on a thread of the driver's: nothing of the caller's is touched there.
+struct xsm_capture {
+    std::atomic<int> gone{0};
+};
+static void CUDART_CB graph_gone(void *c) { static_cast<xsm_capture *>(c)->gone.store(1, std::memory_order_release); }
+
+uint64_t xsm_capture_id(void *cuda_stream) {
+    cudaStreamCaptureStatus status = cudaStreamCaptureStatusNone;
+    unsigned long long id = 0;
+    if (cudaStreamGetCaptureInfo((cudaStream_t)cuda_stream, &status, &id) != cudaSuccess) {
+        (void)cudaGetLastError();
+        return 0;
+    }
+    return status == cudaStreamCaptureStatusActive ? id : 0;
+}
+
+xsm_status xsm_capture_watch(void *cuda_stream, xsm_capture **out) {
+    if (!out) return op_failed(XSM_ERR_INVALID_ARG, "null argument");
+    cudaStreamCaptureStatus status = cudaStreamCaptureStatusNone;
+    unsigned long long id = 0;
+    cudaGraph_t graph = nullptr;
+    cudaError_t e = cudaStreamGetCaptureInfo((cudaStream_t)cuda_stream, &status, &id, &graph);
+    if (e != cudaSuccess) return launched(e);
+    if (status != cudaStreamCaptureStatusActive) return op_failed(XSM_ERR_INVALID_ARG, "the stream is not being recorded");
+    xsm_capture *c = new (std::nothrow) xsm_capture;
+    if (!c) return op_failed(XSM_ERR_CAPACITY, "out of host memory");
+    cudaUserObject_t object = nullptr;
+    e = cudaUserObjectCreate(&object, c, graph_gone, 1, cudaUserObjectNoDestructorSync);
+    if (e != cudaSuccess) {
+        delete c;
+        return launched(e);
+    }
+    e = cudaGraphRetainUserObject(graph, object, 1, cudaGraphUserObjectMove);
+    if (e != cudaSuccess) {
+        (void)cudaUserObjectRelease(object, 1);      // (its end may still be on its way: the word stays allocated)
+        return launched(e);
+    }
+    *out = c;
+    return XSM_OK;
+}
+
+int xsm_capture_gone(xsm_capture *c) {
+    if (!c || !c->gone.load(std::memory_order_acquire)) return 0;
+    delete c;
+    return 1;
+}
+
+int xsm_capture_mode(int mode) {
+    cudaStreamCaptureMode m = (cudaStreamCaptureMode)mode;
+    if (mode < 0 || mode > 2 || cudaThreadExchangeStreamCaptureMode(&m) != cudaSuccess) {
+        (void)cudaGetLastError();
+        return -1;
+    }
+    return (int)m;
 }
 
 xsm_status xsm_kv_append(const xsm_kv *kv, const xsm_kv_append_args *a, void *cuda_stream) {

@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import ctypes as C
 import struct
+import weakref
 from collections import namedtuple
 
 import torch
@@ -32,6 +33,7 @@ _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i:
 
 # says to autograd that tensors have been written to: what keeps one of them for a backward pass notices
 _written = torch._C._increment_version
+_capturing = torch._C._cuda_isCurrentStreamCapturing
 _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
@@ -77,14 +79,47 @@ def rope_table(n_positions: int, dims: int, theta: float = 10000.0, device="cuda
     return torch.stack([angle.cos(), angle.sin()], -1).float().contiguous()
 
 
+class _Recorded:
+    """The workspace of a graph's calls on one of its streams, outside of the graph's own memory: its status word outlasts a replay."""
+    __slots__ = "ws", "size", "outgrown", "watch", "__weakref__"
+
+
+_recorded = {}       # of graphs that exist: _Recorded by (device, number of the capture, stream)
+
+
+def _forget_graphs():
+    """Workspaces of graphs that are no more go back."""
+    gone = binding.load().xsm_capture_gone
+    for key in [key for key, r in list(_recorded.items()) if gone(r.watch)]:
+        del _recorded[key]
+
+
+def _zeros_while_recording(n: int, device: int):
+    """Zeroed memory that is no part of the graph that is being recorded, and ready when this returns."""
+    lib = binding.load()
+    with torch.cuda.device(device):
+        before = lib.xsm_capture_mode(2)           # (relaxed: other streams may be waited for, memory may be made)
+        try:
+            side = torch.cuda.Stream()
+            while lib.xsm_capture_id(side.cuda_stream):      # (torch hands its streams out in turn)
+                side = torch.cuda.Stream()
+            with torch.cuda.stream(side):
+                t = torch.zeros(n, dtype=torch.uint8, device=f"cuda:{device}")
+            side.synchronize()
+        finally:
+            lib.xsm_capture_mode(before)
+    return t
+
+
 class PagedCache:
     """Pools of keys and of values, [n_pages, n_kv_heads, page_size, d_head] (any strides with neighbouring elements in a row: a pool laid
     out [n_pages, page_size, n_kv_heads, d_head] is passed as its view `pool.transpose(1, 2)`).  fp32, bf16 or fp16; d_head 32, 64,
     96, 128 or 256; page_size a multiple of 16.  The tensors stay the caller's and are used in place.
 
     A block table is int32 [batch, max_pages]: position p of a sequence is row p % page_size of page table[sequence, p // page_size].
-    Calls from several streams at a time are fine as far as the pools' contents allow it: every stream has a workspace of its own.  A
-    graph keeps the workspace that the stream it was recorded on had then: it is not replayed at the same time as that stream's calls."""
+    Calls from several streams at a time are fine as far as the pools' contents allow it: every stream has a workspace of its own, and so has every
+    graph (one for each of its streams, which all caches share and which lasts as long as the graph).  The pools, and the other tensors of recorded
+    calls, are the caller's to keep."""
 
     def __init__(self, k, v):
         if not torch.cuda.is_available():
@@ -102,7 +137,8 @@ class PagedCache:
                                _DTYPES[k.dtype])
         self.scale = self.d_head ** -0.5
         self._ws, self._ws_bytes = {}, {}          # by stream: a workspace and its size; by shape of a call: what it needs
-        self._outgrown = []                        # workspaces that larger ones took the place of: a graph may still write to them
+        self._outgrown = []                        # workspaces that larger ones took the place of: calls on their way may still write to them
+        self._graphs = weakref.WeakSet()           # workspaces of graphs that calls of this cache were recorded in
         _check(self.lib.xsm_kv_create(C.byref(cfg), k.data_ptr(), v.data_ptr(), C.byref(self._h)))
 
     def __del__(self):
@@ -213,23 +249,42 @@ class PagedCache:
         return out
 
     def _workspace(self, stream: int, batch: int, m: int, heads: int):
-        """Zeroed memory for the calls of a stream, kept from call to call."""
+        """Zeroed memory for the calls of a stream, kept from call to call, or for those of a graph."""
         need = self._ws_bytes.get((batch, m, heads))
         if need is None:
             need = self._ws_bytes[batch, m, heads] = max(16, self.lib.xsm_kv_attend_workspace(self._h, batch, m, heads))
+        if _capturing():
+            return self._workspace_of_graph(stream, need)
         ws, size = self._ws.get(stream, (None, 0))
         if size < need:
             old, (ws, size) = ws, (torch.zeros(need, dtype=torch.uint8, device=self.k.device), need)
-            if not torch.cuda.is_current_stream_capturing():      # (a graph's own is zeroed whenever it is replayed)
-                self._ws[stream] = ws, size
-                if old is not None:
-                    self._outgrown.append(old)
+            self._ws[stream] = ws, size
+            if old is not None:
+                self._outgrown.append(old)
         return ws, size
 
+    def _workspace_of_graph(self, stream: int, need: int):
+        key = self.device, self.lib.xsm_capture_id(stream), stream
+        r = _recorded.get(key)
+        if r is None:
+            _forget_graphs()
+            r = _Recorded()
+            r.ws, r.size, r.outgrown, r.watch = None, 0, [], C.c_void_p()
+            _check(self.lib.xsm_capture_watch(stream, C.byref(r.watch)))
+            _recorded[key] = r
+        if r.size < need:
+            ws = _zeros_while_recording(need, self.device)
+            if r.ws is not None:
+                r.outgrown.append(r.ws)            # calls that are recorded already write to it
+            r.ws, r.size = ws, need
+        self._graphs.add(r)
+        return r.ws, r.size
+
     def check(self):
-        """Waits for the device and raises an XsmError if a bounded wait of an earlier attend ran out (its results are void)."""
+        """Waits for the device and raises an XsmError if a bounded wait of an earlier attend ran out (its results are void): one of this cache, or
+        one in a graph that calls of this cache were recorded in."""
         torch.cuda.synchronize(self.device)
-        for ws in [ws for ws, _ in self._ws.values()] + self._outgrown:
+        for ws in [ws for ws, _ in self._ws.values()] + self._outgrown + [ws for r in list(self._graphs) if r.ws is not None for ws in (r.ws, *r.outgrown)]:
             status = int(ws[:4].view(torch.int32)[0])
             if status:
                 ws[:4].zero_()

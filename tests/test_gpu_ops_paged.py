@@ -657,3 +657,115 @@ def test_writes_in_place_are_seen_by_autograd(ops):
             call(cache, out, lse, d)
         with pytest.raises(RuntimeError, match="modified by an inplace operation"):
             y.backward()
+
+
+def recorded(calls):
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = calls()
+    return graph, out
+
+
+def test_a_wait_that_ran_out_in_a_graph_is_told(ops):
+    """Status words of replays last until check, whichever of the recorded calls it was; good replays leave none."""
+    from paper_2507_23777_b200.binding import XSM_ERR_TIMEOUT, XsmError
+    g = gen(41)
+    k, v, table = ref.pools(g, [700, 90], 2, 32, 64, F16)
+    q = torch.randn((2, 3, 4, 64), generator=g).to(F16).cuda()
+    cache, table, n = ops.PagedCache(k.cuda(), v.cuda()), table.cuda(), torch.tensor([700, 90], dtype=torch.int32, device="cuda")
+    want, lse = cache.attend(q, table, n)
+    good, (out, l2) = recorded(lambda: cache.attend(q, table, n))
+
+    def bad_then_good():
+        cache.lib.xsm_debug_kv_waits(cache._h, 20, 1)
+        cache.attend(q, table, n)
+        cache.lib.xsm_debug_kv_waits(cache._h, 0, 0)
+        return cache.attend(q, table, n)
+    bad, (out2, l3) = recorded(bad_then_good)
+    good.replay()
+    cache.check()
+    assert torch.equal(out, want) and torch.equal(l2, lse)
+    for _ in range(2):
+        bad.replay()
+        good.replay()
+        with pytest.raises(XsmError) as e:
+            cache.check()
+        assert e.value.status == XSM_ERR_TIMEOUT
+        assert torch.equal(out2, want) and torch.equal(l3, lse)
+    good.replay()
+    cache.check()
+
+
+def test_recorded_calls_of_many_caches_share_a_workspace(ops):
+    """One for a graph's calls on a stream, as large as the largest wants, in no graph's own memory; another graph has another; gone with its graph."""
+    import gc
+    g = gen(42)
+    caches = []
+    for d, hk in ((64, 2), (128, 1), (64, 2)):
+        k, v, table = ref.pools(g, [1000, 90], hk, 32, d, F16)
+        q = torch.randn((2, 3, 4, d), generator=g).to(F16).cuda()
+        caches.append((ops.PagedCache(k.cuda(), v.cuda()), q, table.cuda()))
+    n = torch.tensor([1000, 90], dtype=torch.int32, device="cuda")
+    want = [c.attend(q, t, n)[0] for c, q, t in caches]
+    gc.collect()
+    before = set(ops._recorded)
+    graphs = [recorded(lambda: [c.attend(q, t, n)[0] for c, q, t in caches]) for _ in range(2)]
+    keys = [key for key in ops._recorded if key not in before]
+    one, two = (ops._recorded[key] for key in keys)
+    assert one.ws.data_ptr() != two.ws.data_ptr() and all(set(c._graphs) >= {one, two} for c, _, _ in caches)
+    for _ in range(3):
+        for graph, outs in graphs:
+            [o.zero_() for o in outs]
+            graph.replay()
+            torch.cuda.synchronize()
+            assert all(torch.equal(o, w) for o, w in zip(outs, want))
+    # a graph does not need the caches to be kept, only the tensors of the calls and the pools
+    kept = [(c.k, c.v, q, t) for c, q, t in caches]
+    caches.clear(), gc.collect()
+    others = [torch.full((one.size,), 85, dtype=torch.uint8, device="cuda") for _ in range(4)]
+    for graph, outs in graphs:
+        [o.zero_() for o in outs]
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(o, w) for o, w in zip(outs, want))
+    assert all((o == 85).all() for o in others) and len(kept) == 3
+    del one, two, graph, outs
+    graphs.clear(), gc.collect(), torch.cuda.synchronize()
+    import time
+    for _ in range(100):          # (the driver says so from a thread of its own)
+        ops._forget_graphs()
+        if not any(key in ops._recorded for key in keys):
+            break
+        time.sleep(0.05)
+    assert not any(key in ops._recorded for key in keys)
+
+
+def test_graphs_and_calls_of_the_stream_that_they_were_recorded_on_side_by_side(ops):
+    """Replays on other streams while the recording stream goes on with calls of its own, bit for bit."""
+    g = gen(43)
+    lens = [4000, 10, 2500, 900]
+    k, v, table = ref.pools(g, lens, 2, 64, 64, F16)
+    q = torch.randn((4, 5, 4, 64), generator=g).to(F16).cuda()
+    cache, table, n = ops.PagedCache(k.cuda(), v.cuda()), table.cuda(), torch.tensor(lens, dtype=torch.int32, device="cuda")
+    stream, other = torch.cuda.Stream(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(stream):
+        want, lse = cache.attend(q, table, n)
+    graphs = []
+    for _ in range(2):
+        graph = torch.cuda.CUDAGraph()
+        torch.cuda.synchronize()
+        with torch.cuda.graph(graph, stream=stream):
+            graphs.append((graph, [cache.attend(q, table, n) for _ in range(5)]))
+    torch.cuda.synchronize()
+    calls = []
+    for _ in range(10):
+        graphs[0][0].replay()
+        with torch.cuda.stream(other):
+            graphs[1][0].replay()
+        with torch.cuda.stream(stream):
+            calls += [cache.attend(q, table, n) for _ in range(5)]
+    torch.cuda.synchronize()
+    for out, l2 in calls + graphs[0][1] + graphs[1][1]:
+        assert torch.equal(out, want) and torch.equal(l2, lse)
+    cache.check()
