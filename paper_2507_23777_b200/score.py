@@ -16,7 +16,7 @@ import numpy as np
 import torch
 import torch.nn.functional as F
 
-from . import inputs, ops
+from . import binding, inputs, ops
 
 WINDOW = 16          # tokens of a sequence that go through the backbone at a time: what xsm_kv_attend takes
 
@@ -77,7 +77,7 @@ class Scorer:
     @torch.no_grad()
     def score(self, cond, tokens, top: int = 0, temperature: float = 1.0) -> ops.TokenLogprobs:
         """tokens [batch, n], x_0 = BOS: (logprob, entropy, lse) [batch, n - 1] of x_1 .. x_{n-1}, and with `top` the best ids and their log
-        probabilities [batch, n - 1, top] at every place."""
+        probabilities [batch, n - 1, top] at every place.  Waits for the device; an XsmError where a wait of the attention ran out."""
         tokens = np.asarray(tokens)
         if tokens.ndim != 2 or tokens.shape[0] != self.batch or not 2 <= tokens.shape[1] <= self.max_tokens + 1:
             raise ValueError(f"tokens must be [{self.batch}, 2 to {self.max_tokens + 1}]")
@@ -91,11 +91,19 @@ class Scorer:
             z = self.logits(x[:, a:a + m], a).flatten(0, 1)
             r = ops.token_logprobs(z, x[:, a + 1:a + 1 + m].flatten(), top=top, temperature=temperature)
             parts.append([None if t is None else t.view(self.batch, m, *t.shape[1:]) for t in r])
+        gave_up = None
+        for cache in self.cache + self.cond_cache:          # (all of them: none is to tell the next score of this one's)
+            try:
+                cache.check()
+            except binding.XsmError as e:
+                gave_up = e
+        if gave_up is not None:
+            raise gave_up
         return ops.TokenLogprobs(*(None if p[0] is None else torch.cat(p, 1) for p in zip(*parts)))
 
 
 def main():
-    from . import binding, build
+    from . import build
     ap = argparse.ArgumentParser(description=__doc__.splitlines()[0])
     ap.add_argument("--config", type=int, default=1)
     ap.add_argument("--tokens", type=int, default=256)

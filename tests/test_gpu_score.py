@@ -107,3 +107,21 @@ def test_logits_behind_tokens_outside_the_vocabulary_are_nan(score):
     s.condition(inputs.make_cond(cfg, 1))
     assert torch.equal(z[:, :2], s.logits(tokens.clamp(max=cfg["vocab"] - 1), 0)[:, :2]) and z[:, 2:].isnan().all()
     assert s.logits(torch.tensor([[-1]], device="cuda"), 4).isnan().all()
+
+
+@pytest.mark.parametrize("which", ["cache", "cond_cache"])
+def test_scores_of_an_attention_that_gave_up_are_not_returned(score, which):
+    from paper_2507_23777_b200 import binding
+    cfg = gpu_cfg(dtype=1)
+    s = score.Scorer(cfg, inputs.make_weights(cfg), 1, 40)
+    cond, tokens = inputs.make_cond(cfg, 1), np.arange(40)[None]
+    want = s.score(cond, tokens).logprob
+    some = getattr(s, which)
+    for c in some:
+        c.lib.xsm_debug_kv_waits(c._h, 20, 1)
+    with pytest.raises(binding.XsmError) as e:
+        s.score(cond, tokens)
+    assert e.value.status == binding.XSM_ERR_TIMEOUT
+    for c in some:
+        c.lib.xsm_debug_kv_waits(c._h, 0, 0)
+    assert torch.equal(s.score(cond, tokens).logprob, want)
