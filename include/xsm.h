@@ -342,6 +342,10 @@ typedef struct {
     float temperature;
 } xsm_logprob_grad_args;
 XSM_API xsm_status xsm_token_logprobs_grad(const xsm_logprob_grad_args *a, void *cuda_stream);
+/* The same with the log probabilities of the call above (DEVICE [rows], may be NULL): rows with a token take their probabilities from the differences to the
+ * token's logit, and what all logits of a row have in common does not matter.  Without them, in rows without a token, and where the gradient takes the place of
+ * rows of more than 8192 bytes, p is exp(z - lse) from an lse that is rounded to fp32: off by 2^-24 |lse| of itself. */
+XSM_API xsm_status xsm_token_logprobs_grad_near(const xsm_logprob_grad_args *a, const float *logprob, void *cuda_stream);
 
 #ifdef __cplusplus
 }

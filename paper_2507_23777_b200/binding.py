@@ -26,6 +26,7 @@ EXPORTS = [
     "xsm_debug_set_script", "xsm_debug_plan", "xsm_kv_create", "xsm_kv_destroy", "xsm_kv_append", "xsm_kv_attend_workspace",
     "xsm_kv_attend", "xsm_debug_kv_waits", "xsm_capture_id", "xsm_capture_watch", "xsm_capture_gone", "xsm_capture_mode",
     "xsm_token_logprobs", "xsm_token_logprobs_grad",
+    "xsm_token_logprobs_grad_near",
 ]
 
 
@@ -111,6 +112,7 @@ def load(path: str | None = None):
     L.xsm_kv_attend_workspace.argtypes = [vp, C.c_int, C.c_int, C.c_int]
     L.xsm_token_logprobs.argtypes = [vp, vp]
     L.xsm_token_logprobs_grad.argtypes = [vp, vp]
+    L.xsm_token_logprobs_grad_near.argtypes = [vp, vp, vp]
     if path is None:
         _lib = L
     return L

@@ -419,21 +419,23 @@ template <typename T, bool kTop, int W> __global__ void __launch_bounds__(kBlock
 
 struct GradArgs {
     const void *logits, *tokens;
-    const float *lse, *entropy;
+    const float *logprob, *lse, *entropy;      // logprob may be missing
     const int *top_ids;
     const float *g_logprob, *g_entropy, *g_lse, *g_top;
     void *d_logits;
     long long row_ld, token_ld, gl_ld, ge_ld, gs_ld, d_ld;
     int rows, vocab, token_bytes, top, per_block;      // per_block: pieces of a row that a block takes
-    float inv_t;
+    float inv_t, temperature;
 };
 
-// The numbers of a row that its elements' gradients are made of: with x = log2 p = z c - lse', the gradient is -p (total' + ge' x), where
-// total' has the entropy's share and everything the factor 1/T.  A row with nothing left: lse' infinite, so p = 0, and the rest zero.
+// The numbers of a row that its elements' gradients are made of: with x = log2 p = (z - ref) c + off, the gradient is -p (total' + ge' x), where
+// total' has the entropy's share and everything the factor 1/T.  The reference is the token's logit, which is known with its log probability, so that what all
+// logits have in common does not matter (an lse of 1000 is rounded to 3e-5, p to as much); where there is no token, or its log probability is larger than the lse
+// (a masked one's), it is lse T.  A row with nothing left: off = -infinity, so p = 0, and the rest zero.
 struct RowGrad {
-    float c, lse, total, ge;
+    float c, minus_ref, off, total, ge;
     __device__ __forceinline__ float of(float z) const {
-        const float x = fmaf(z, c, -lse);
+        const float x = fmaf(z + minus_ref, c, off);
         return -ex2(x) * fmaf(ge, fmaxf(x, -1e3f), total);                // (p is zero below -150: the bound only keeps 0 * -infinity out)
     }
 };
@@ -486,8 +488,11 @@ template <typename T, bool kTop, int W> __global__ void __launch_bounds__(kBlock
     const float single = one >= 0 ? to_f(in.p[one]) : 0.f;
     const int listed = kTop ? A.top + 1 : 1;
     if (tid < 32) {
-        const float lse = A.lse[row];
-        const bool none = lse == -INFINITY;
+        const float lse = A.lse[row], logprob = A.logprob ? A.logprob[row] : 0.f;
+        const long long token = token_at(A.tokens, A.token_bytes, row * A.token_ld);
+        const bool has = token >= 0 && token < A.vocab;
+        const bool by_token = A.logprob && has && fabsf(logprob) < fabsf(lse);      // (an lse may be beyond fp32 where the differences are not)
+        const bool none = lse == -INFINITY && !by_token;
         float more = 0.f;
         if (kTop) {
             if (tid < A.top) {
@@ -498,8 +503,6 @@ template <typename T, bool kTop, int W> __global__ void __launch_bounds__(kBlock
             more = warp_sum(more);
         }
         if (tid == 0) {
-            const long long token = token_at(A.tokens, A.token_bytes, row * A.token_ld);
-            const bool has = token >= 0 && token < A.vocab;
             const float g = A.g_logprob && has && !none ? A.g_logprob[row * A.gl_ld] * A.inv_t : 0.f;
             const float ge = A.g_entropy && !none ? A.g_entropy[row * A.ge_ld] * A.inv_t : 0.f;
             s_id[0] = has ? (int)token : -1;
@@ -507,7 +510,8 @@ template <typename T, bool kTop, int W> __global__ void __launch_bounds__(kBlock
             RowGrad r;
             r.ge = ge * 0.69314718055994531f;
             r.total = none ? 0.f : g + more - (A.g_lse ? A.g_lse[row * A.gs_ld] * A.inv_t : 0.f) + (A.g_entropy ? ge * A.entropy[row] : 0.f);
-            r.lse = none ? INFINITY : lse * kLog2e;
+            r.off = none ? -INFINITY : by_token ? logprob * kLog2e : 0.f;
+            r.minus_ref = by_token ? -to_f(z[token]) : none ? 0.f : -lse * A.temperature;
             r.c = A.inv_t * kLog2e;
             rows[group] = r;
         }
@@ -536,7 +540,7 @@ template <typename T, bool kTop, int W> __global__ void __launch_bounds__(kBlock
     meet<W>();
     if (one >= 0) out[one] = rounded<T>(r.of(single));
     const bool alike = (((uintptr_t)z ^ (uintptr_t)out) & 15) == 0;
-    const Two cc = two(r.c, r.c), lse = two(-r.lse, -r.lse), ge = two(-r.ge, -r.ge), total = two(-r.total, -r.total);
+    const Two cc = two(r.c, r.c), minus = two(r.minus_ref, r.minus_ref), off = two(r.off, r.off), ge = two(-r.ge, -r.ge), total = two(-r.total, -r.total);
     for (int at = first; at < last; at += kThreads * kLoads) {
         if (at != first) fetch(at);
 #pragma unroll
@@ -546,7 +550,7 @@ template <typename T, bool kTop, int W> __global__ void __launch_bounds__(kBlock
             float d[N];
 #pragma unroll
             for (int k = 0; k < N / 2; ++k) {
-                const float2 y = pair<T>(v[u], k), x = apart(fma2(two(y.x, y.y), cc, lse));
+                const float2 y = pair<T>(v[u], k), x = apart(fma2(add2(two(y.x, y.y), minus), cc, off));
                 const Two w = fma2(ge, two(fmaxf(x.x, -1e3f), fmaxf(x.y, -1e3f)), total);
                 const float2 f = apart(mul2(two(ex2(x.x), ex2(x.y)), w));
                 d[2 * k] = f.x;
@@ -650,7 +654,9 @@ xsm_status xsm_token_logprobs(const xsm_logprob_args *a, void *cuda_stream) {
     return launched(r);
 }
 
-xsm_status xsm_token_logprobs_grad(const xsm_logprob_grad_args *a, void *cuda_stream) {
+xsm_status xsm_token_logprobs_grad(const xsm_logprob_grad_args *a, void *cuda_stream) { return xsm_token_logprobs_grad_near(a, nullptr, cuda_stream); }
+
+xsm_status xsm_token_logprobs_grad_near(const xsm_logprob_grad_args *a, const float *logprob, void *cuda_stream) {
     if (!a) return op_failed(XSM_ERR_INVALID_ARG, "null argument");
     if (const char *m = check_logits(a->logits, a->tokens, a->rows, a->vocab, a->dtype, a->token_bytes, a->top, a->temperature)) return op_failed(XSM_ERR_INVALID_ARG, m);
     if (a->rows == 0) return XSM_OK;
@@ -666,9 +672,14 @@ xsm_status xsm_token_logprobs_grad(const xsm_logprob_grad_args *a, void *cuda_st
     const int pieces = (int)((row_bytes + 15) / 16), per_block = warps ? pieces : a->rows >= 8 * sms ? 2048 : 512;
     const int blocks = pieces > per_block ? (pieces + per_block - 1) / per_block : 1;
     if (blocks > 65535) return op_failed(XSM_ERR_INVALID_ARG, "vocab is too large");
-    const GradArgs A{a->logits, a->tokens, a->lse, a->entropy, a->top_ids, a->g_logprob, a->g_entropy, a->g_lse, a->g_top, a->d_logits,
+    // (every block of a row reads the token's logit: not where another one may have written the gradient to its place)
+    const int es = element_size(a->dtype);
+    const char *from = (const char *)a->logits, *to = (const char *)a->d_logits;
+    const long long ends_from = ((a->rows - 1) * a->row_stride + a->vocab) * es, ends_to = ((a->rows - 1) * a->d_row_stride + a->vocab) * es;
+    if (blocks > 1 && from < to + ends_to && to < from + ends_from) logprob = nullptr;
+    const GradArgs A{a->logits, a->tokens, logprob, a->lse, a->entropy, a->top_ids, a->g_logprob, a->g_entropy, a->g_lse, a->g_top, a->d_logits,
                      a->row_stride, a->token_stride, a->g_logprob_stride, a->g_entropy_stride, a->g_lse_stride, a->d_row_stride,
-                     a->rows, a->vocab, a->token_bytes, a->top, per_block, 1.f / a->temperature};
+                     a->rows, a->vocab, a->token_bytes, a->top, per_block, 1.f / a->temperature, a->temperature};
     const cudaStream_t st = (cudaStream_t)cuda_stream;
     cudaError_t r = cudaSuccess;
     with_dtype(a->dtype, [&](auto t) {

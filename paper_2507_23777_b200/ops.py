@@ -409,9 +409,10 @@ def token_logprobs_grad(logits, tokens, result, grad_logprob=None, grad_entropy=
         raise ValueError("out must be like logits, with rows of their own")
     else:
         _written([out])
-    _, entropy, lse, ids, _ = result
-    if not (lse.shape == entropy.shape == (rows,) and lse.dtype is entropy.dtype is torch.float32 and lse.get_device() == device == entropy.get_device() and
-            lse.is_contiguous() and entropy.is_contiguous()):
+    logprob, entropy, lse, ids, _ = result
+    if not (lse.shape == entropy.shape == logprob.shape == (rows,) and lse.dtype is entropy.dtype is logprob.dtype is torch.float32 and
+            lse.get_device() == device == entropy.get_device() and logprob.get_device() == device and
+            lse.is_contiguous() and entropy.is_contiguous() and logprob.is_contiguous()):
         raise ValueError("result must be what token_logprobs returned for these logits")
     gl, gl_ld = _row_grad(grad_logprob, rows, device, "grad_logprob")
     ge, ge_ld = _row_grad(grad_entropy, rows, device, "grad_entropy")
@@ -429,7 +430,7 @@ def token_logprobs_grad(logits, tokens, result, grad_logprob=None, grad_entropy=
             ld, token_ld, gl_ld, ge_ld, gs_ld, out.stride(0), rows, vocab, _DTYPES[logits.dtype], _TOKENS[tokens.dtype], top, temperature)
     except _BEYOND as e:
         raise ValueError(f"an argument of token_logprobs_grad is beyond its type: {e}") from None
-    status = binding.load().xsm_token_logprobs_grad(args, _raw_stream(device))
+    status = binding.load().xsm_token_logprobs_grad_near(args, logprob.data_ptr(), _raw_stream(device))
     if status:
         _check(status)
     return out

@@ -311,3 +311,45 @@ def test_numbers_beyond_their_type_are_refused(ops):
                  lambda: ops.token_logprobs(z, t, temperature=1e39), lambda: ops.token_logprobs_grad(z, t, r, temperature=1e39)):
         with pytest.raises((ValueError, XsmError)):
             call()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+@pytest.mark.parametrize("offset", [0.0, 100.0, -100.0, 1000.0, 10000.0, -10000.0])
+@pytest.mark.parametrize("rows,vocab", [(9, 50), (5, 3001), (700, 1000), (2, 40001)])
+def test_gradient_of_logits_with_an_offset(ops, dtype, offset, rows, vocab):
+    """What all logits of a row have in common does not matter, neither for a token that has nearly all of the probability (its gradient is what
+    it lacks) nor for one that has little.  Probabilities come from differences to the token's logit, their size times 2^-22; the
+    token's own gradient 1 - p is a difference of numbers next to one."""
+    z, t = logits(rows, vocab, F32, 12)
+    near = torch.arange(rows) % 3
+    z[torch.arange(rows), t] = torch.where(near == 0, 24.0, torch.where(near == 1, 12.0, z[torch.arange(rows), t]))
+    z = (z + offset).to(dtype)
+    g = torch.randn(rows, generator=torch.Generator().manual_seed(2))
+    zero = torch.zeros(rows)
+    for temperature in (1.0, 0.5):
+        gz = z.cuda()
+        r = ops.token_logprobs(gz, t.cuda(), temperature=temperature)
+        d = ops.token_logprobs_grad(gz, t.cuda(), r, grad_logprob=g.cuda(), temperature=temperature)
+        want, size = ref.logprobs_grad(z, t, None, g, zero, zero, None, temperature)
+        zd = z.double() / temperature
+        depth = (zd - zd.gather(1, t[:, None])).abs() + ref.logprobs(z, t, 0, temperature)[0].abs()[:, None]
+        own = torch.zeros_like(want).scatter_(1, t[:, None], g.abs().double()[:, None])
+        same(d, want, UNIT[dtype] * want.abs() + (depth * 2.0 ** -22 + (vocab / 256 + 40) * 2.0 ** -24 + 2.0 ** -20) * size + 2.0 ** -21 * own / temperature + TINY[dtype], "gradient")
+        leaf = z.cuda().requires_grad_()
+        (g.cuda() * ops.token_logprobs(leaf, t.cuda(), temperature=temperature).logprob).sum().backward()
+        assert torch.equal(leaf.grad, d)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+def test_gradient_where_the_token_is_masked_or_all_logits_are_the_lowest(ops, dtype):
+    """Tokens whose own logit says nothing about the others: -infinity, the type's lowest number; rows that hold nothing but that."""
+    z, t = logits(6, 300, dtype, 13)
+    z[0, t[0]], z[1, t[1]], z[2] = -math.inf, LOWEST[dtype], LOWEST[dtype]
+    t[3] = -1
+    r = ops.token_logprobs(z.cuda(), t.cuda(), top=4)
+    check_grad(ops, z, t, r, 4, 1.0)
+    r = ops.token_logprobs(z.cuda(), t.cuda(), top=4, temperature=0.5)
+    d = ops.token_logprobs_grad(z.cuda(), t.cuda(), r, grad_logprob=torch.ones(6, device="cuda"), temperature=0.5)
+    want = torch.full((300,), -2.0 / 300, dtype=torch.float64)
+    want[t[2]] += 2
+    same(d[2], want, UNIT[dtype] * want.abs() + 2.0 ** -20, "all the lowest")
