@@ -769,3 +769,47 @@ def test_graphs_and_calls_of_the_stream_that_they_were_recorded_on_side_by_side(
     for out, l2 in calls + graphs[0][1] + graphs[1][1]:
         assert torch.equal(out, want) and torch.equal(l2, lse)
     cache.check()
+
+
+def test_append_many_tokens_of_many_heads(ops):
+    """Prompts whose tokens have more elements than a block takes at once: 128 threads a token that go on to the next ones, in every type, width and
+    pairing; ragged counts, parts of heads rotated, strides, pages that are not there."""
+    def broken(table, n):
+        table[0, 1], table[1, 0], table[1, 3] = -1, n, 2 ** 31 - 1
+    for cache_t in (F32, BF16, F16):
+        for in_t in (F32, BF16, F16):
+            # (600 + 600 tokens; 24 heads of 64 are 96 items of sixteen elements, 768 pairs where the rotated part is no multiple of sixteen)
+            for rot, interleaved in ((32, False), (32, True), (10, False), (64, True)):
+                check_append(ops, cache_t, in_t, 64, 8, 8, 600, 64, [0, 37], rot=rot, interleaved=interleaved, counts=[600, 411], seed=rot + interleaved, break_table=broken)
+    check_append(ops, F16, BF16, 128, 4, 0, 1100, 48, [5], rot=128, layout="nhd", seed=3)
+    check_append(ops, BF16, BF16, 64, 16, 16, 513, 16, [0, 3], rot=None, seed=4, packed=False)
+
+
+def test_append_few_tokens_of_more_items_than_threads(ops):
+    """More than 512 items a token: 16 + 2 x 8 heads of 128 in pairs (2048), 64 + 2 x 8 heads of 128 in pieces (640)."""
+    for cache_t in (F32, BF16, F16):
+        for in_t in (F32, BF16, F16):
+            for interleaved in (False, True):
+                check_append(ops, cache_t, in_t, 128, 8, 16, 3, 32, [0, 31, 100], rot=10, interleaved=interleaved, counts=[3, 0, 2], seed=5)
+                check_append(ops, cache_t, in_t, 128, 8, 64, 3, 32, [9, 90], rot=64, interleaved=interleaved, seed=6)
+
+
+@pytest.mark.parametrize("m", [3, 600])
+@pytest.mark.parametrize("rot,interleaved", [(64, False), (64, True), (10, False), (10, True)])
+def test_append_queries_in_place(ops, m, rot, interleaved):
+    """q_out = q gives what a tensor of its own gives, also where a thread takes item after item; tokens without a place or a count included."""
+    g = gen(15)
+    x = torch.randn((2, m, 24, 64), generator=g).to(F16).cuda()
+    q, k, v = x.split([8, 8, 8], 2)
+    pages = 2 * (-(-(m + 40) // 32)) + 1
+    kp = torch.zeros((pages, 8, 32, 64), dtype=F16, device="cuda")
+    table = torch.arange(pages - 1, dtype=torch.int32, device="cuda").view(2, -1)
+    table[1, 0] = -1
+    starts, counts = torch.tensor([40, -2], dtype=torch.int32, device="cuda"), torch.tensor([m, m - 1], dtype=torch.int32, device="cuda")
+    rope = ops.rope_table(m + 39, rot)
+    a, b = ops.PagedCache(kp, kp.clone()), ops.PagedCache(kp.clone(), kp.clone())
+    want = a.append(k, v, table, starts, counts=counts, q=q, rope=rope, interleaved=interleaved)
+    mine = x.clone()
+    mq = mine[:, :, :8]
+    assert b.append(k, v, table, starts, counts=counts, q=mq, rope=rope, interleaved=interleaved, out=mq) is mq
+    assert torch.equal(mq, want) and torch.equal(mine[:, :, 8:], x[:, :, 8:]) and torch.equal(a.k, b.k) and torch.equal(a.v, b.v)
