@@ -33,6 +33,7 @@ _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i:
 
 # says to autograd that tensors have been written to: what keeps one of them for a backward pass notices
 _written = torch._C._increment_version
+_grad_enabled = torch.is_grad_enabled
 _capturing = torch._C._cuda_isCurrentStreamCapturing
 _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
@@ -194,7 +195,7 @@ class PagedCache:
         q [batch, m, n_heads, d_head], are rotated by `rope` (float32 [positions, dims / 2, 2], see rope_table).  Returns the rotated
         queries in `out` (a new tensor, or the one given; it may be q), or None without q.  Like attend it has no gradient, and refuses tensors that
         want one unless torch.no_grad() says that it is not needed."""
-        if torch.is_grad_enabled() and (k.requires_grad or v.requires_grad or q is not None and q.requires_grad or rope is not None and rope.requires_grad or
+        if _grad_enabled() and (k.requires_grad or v.requires_grad or q is not None and q.requires_grad or rope is not None and rope.requires_grad or
                                         out is not None and out.requires_grad):
             raise ValueError("append has no gradient: call it under torch.no_grad()")
         if forward_ad._current_level >= 0:
@@ -253,7 +254,7 @@ class PagedCache:
         need = self._ws_bytes.get((batch, m, heads))
         if need is None:
             need = self._ws_bytes[batch, m, heads] = max(16, self.lib.xsm_kv_attend_workspace(self._h, batch, m, heads))
-        if _capturing():
+        if stream and _capturing():               # (the default stream, 0, cannot be recorded)
             return self._workspace_of_graph(stream, need)
         ws, size = self._ws.get(stream, (None, 0))
         if size < need:
@@ -296,20 +297,16 @@ class PagedCache:
         of these the last `window` (0: all).  Returns (out, lse): out like q, lse float32 [batch, m, n_heads], the logarithm of the sum
         of exp(scale q.k), -inf where nothing is seen."""
         device, shape, qs, dtype, table = self.device, q.shape, q.stride(), q.dtype, block_table.shape
-        if torch.is_grad_enabled() and (q.requires_grad or out is not None and out.requires_grad or lse is not None and lse.requires_grad):
+        if _grad_enabled() and (q.requires_grad or out is not None and out.requires_grad or lse is not None and lse.requires_grad):
             raise ValueError("attend has no gradient: call it under torch.no_grad()")
         if forward_ad._current_level >= 0:
             _no_tangents(q, self.k, self.v)
-        written = []
+        written = [t for t in (out, lse) if t is not None]
         if out is None:
             out = torch.empty(shape, dtype=dtype, device=q.device)
-        else:
-            written.append(out)
         rows = shape[:3]
         if lse is None:
             lse = torch.empty(rows, dtype=torch.float32, device=q.device)
-        else:
-            written.append(lse)
         os = out.stride()
         ok = len(shape) == 4 and len(table) == 2 and shape == out.shape and lse.shape == rows and dtype in _DTYPES
         if ok:
@@ -396,8 +393,8 @@ def token_logprobs_grad(logits, tokens, result, grad_logprob=None, grad_entropy=
     missing.  out: a tensor like logits for the gradient, which may be the logits themselves.  There are no second derivatives: tensors that want a
     gradient are refused unless torch.no_grad() says that it is not needed."""
     device, rows, vocab, ld, token_ld = _check_logits(logits, tokens)
-    if torch.is_grad_enabled():
-        for t in (logits, grad_logprob, grad_entropy, grad_lse, grad_top, out, *result):
+    if _grad_enabled():
+        for t in (logits, result[2], grad_logprob, grad_entropy, grad_lse, grad_top, out):
             if t is not None and t.requires_grad:
                 raise ValueError("token_logprobs_grad has no gradient of its own: call it under torch.no_grad()")
     if forward_ad._current_level >= 0:
@@ -464,6 +461,6 @@ def token_logprobs(logits, tokens, top: int = 0, temperature: float = 1.0) -> To
     largest logits, equal ones by the lower id first.  Differentiable by the logits, once and backwards."""
     if forward_ad._current_level >= 0:
         _no_tangents(logits)
-    if logits.requires_grad and torch.is_grad_enabled():
+    if logits.requires_grad and _grad_enabled():
         return TokenLogprobs(*_TokenLogprobs.apply(logits, tokens, top, temperature))
     return _forward(logits, tokens, top, temperature)
