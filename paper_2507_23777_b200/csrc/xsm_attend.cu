@@ -230,13 +230,13 @@ __device__ __forceinline__ void mma16(float (&c)[4], const uint4 &a, unsigned b0
 
 // x = part + rest: part is x rounded to eleven bits (a tf32 operand), the rest is at most 2^-12 of it, of which a tf32 operand keeps eleven bits again
 __device__ __forceinline__ unsigned tf32_weight(float x) { return (__float_as_uint(x) + 0x1000u) & 0xffffe000u; }      // (far from the largest number)
-// (the numbers next to the largest are cut off instead of rounded to an infinity)
+// What would round to an infinity is cut off instead.  Infinities and NaN have a part of some finite number and are their own rest (the difference of two
+// infinities would be NaN where the products are right), so that the rest is a subtraction without a question.
 __device__ __forceinline__ unsigned tf32_part(float x) {
-    const unsigned u = __float_as_uint(x), up = (u + 0x1000u) & 0xffffe000u;
-    return (up & 0x7fffffffu) == 0x7f800000u ? u & 0xffffe000u : up;
+    const unsigned u = __float_as_uint(x), up = u + 0x1000u;
+    return (up & 0x7f800000u) == 0x7f800000u ? u & 0xff7fe000u : up & 0xffffe000u;
 }
-// (infinities: the difference of two of them would be NaN where the product with the part is right; NaN comes back out of the rest)
-__device__ __forceinline__ unsigned tf32_rest(float x, unsigned part) { return (part & 0x7fffffffu) == 0x7f800000u ? 0u : __float_as_uint(x - __uint_as_float(part)); }
+__device__ __forceinline__ unsigned tf32_rest(float x, unsigned part) { return __float_as_uint(x - __uint_as_float(part)); }
 
 // two values as 16-bit operands, first in the low half, and what the rounding took off
 template <typename T> __device__ __forceinline__ unsigned pack2(float a, float b);
