@@ -209,12 +209,9 @@ class PagedCache:
             ok = (kv_heads == self.n_kv_heads and d == self.d_head and ks[3] == vs[3] == 1 and v.dtype is dtype and table[0] == batch and
                   starts.shape == (batch,) and block_table.dtype is starts.dtype is torch.int32 and k.get_device() == device == v.get_device() and
                   block_table.get_device() == device == starts.get_device() == _current_device())
-        written = [self.k, self.v]
         if ok and q is not None:
             qs, q_shape = q.stride(), q.shape
-            if out is not None:
-                written.append(out)
-            else:
+            if out is None:
                 out = torch.empty(q_shape, dtype=q.dtype, device=q.device)
             os = out.stride()
             ok = (len(q_shape) == 4 and q_shape == out.shape and qs[3] == os[3] == 1 and q_shape[0] == batch and q_shape[1] == m and q_shape[3] == d and
@@ -243,7 +240,7 @@ class PagedCache:
                 batch, m, heads, _DTYPES[dtype], table[1], positions, 2 * half, interleaved)
         except _BEYOND as e:
             raise ValueError(f"an argument of append is beyond its type: {e}") from None
-        _written(written)
+        _written((self.k, self.v) if out is None else (self.k, self.v, out))
         status = self.lib.xsm_kv_append(self._h, args, _raw_stream(device))
         if status:
             _check(status)
@@ -301,7 +298,6 @@ class PagedCache:
             raise ValueError("attend has no gradient: call it under torch.no_grad()")
         if forward_ad._current_level >= 0:
             _no_tangents(q, self.k, self.v)
-        written = [t for t in (out, lse) if t is not None]
         if out is None:
             out = torch.empty(shape, dtype=dtype, device=q.device)
         rows = shape[:3]
@@ -329,8 +325,7 @@ class PagedCache:
                 self.scale if scale is None else scale)
         except _BEYOND as e:
             raise ValueError(f"an argument of attend is beyond its type: {e}") from None
-        if written:
-            _written(written)
+        _written((out, lse))
         status = self.lib.xsm_kv_attend(self._h, args, stream)
         if status:
             _check(status)
