@@ -277,8 +277,8 @@ XSM_API xsm_status xsm_kv_append(const xsm_kv *kv, const xsm_kv_append_args *a, 
  * NaN included; in what a row does see they may make that row's results NaN or infinite, never another row's.  Lengths beyond the table's
  * end there; pages whose number lies outside the pool are not seen.
  * Sums and softmax in fp32; the weights of 16-bit values enter as two parts of the pools' type, with an error of 2^-16 (bf16), 2^-22 and 2^-40 of the
- * row's largest weight (fp16).  q_dtype is the pool's type, or, over an fp16 pool, any: queries then enter as fp16 (fp32 ones as two parts), so
- * beyond +-65504 they are infinite.
+ * row's largest weight (fp16).  q_dtype is the pool's type, or, over an fp16 pool, any: queries then enter as fp16 (fp32 ones as two parts of it):
+ * beyond +-65504 they are infinite, and their smallest step is 2^-24 (bf16 ones below 2^-17 lose bits).
  * workspace: DEVICE, xsm_kv_attend_workspace bytes, 16-byte aligned, zeroed by the caller before its first use; calls that share
  * one follow each other on one stream.  Its first 32-bit word is XSM_ERR_TIMEOUT once a bounded wait of the device has run out, and the
  * results of that call are then void. */

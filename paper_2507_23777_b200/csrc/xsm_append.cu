@@ -33,9 +33,10 @@ template <bool kPool, typename T, int N> __device__ __forceinline__ void store_f
     *reinterpret_cast<Vec<T, N> *>(p) = v;
 }
 
-// A block for every token (or, of tokens with few heads, for several); a thread takes N pairs of elements of a head at a time (N = 8: whole 16-byte pieces; N = 1 where the rotated
-// part or the alignment does not allow that).  Items of a token: heads of q, of k, of v, d / 2N items each, the rotated ones first.  kOnce: there
-// is a thread for every item of the token; kNear: pairs are neighbours.
+// The items of a token are the heads of q, of k and of v in runs of N pairs of elements, d / 2N items a head, the rotated ones first.  N = 8 takes whole 16-byte
+// pieces; where the rotated part or the alignment does not allow that, N = 1.
+// kOnce: a block has a thread for every item of its token, or of several tokens where they have few; otherwise 128 threads go from item to item of one token.
+// kNear: pairs are neighbours.
 template <typename TI, typename TC, int N, bool kNear, bool kOnce>
 __global__ void __launch_bounds__(kOnce ? 512 : 128) append_kernel(const __grid_constant__ AppendArgs A, const __grid_constant__ Pages P) {
     chain_go();

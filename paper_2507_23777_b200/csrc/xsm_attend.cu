@@ -6,14 +6,14 @@
 // A unit that a cut goes through leaves partial results (maximum, sum, unnormalised output) in the workspace; the CTA that is the last
 // to arrive at the unit's counter adds them up in the order of the positions, so results do not depend on which one that is.
 //
-// In a CTA a producer warp streams stages of 32 positions (boxes of the keys' and values' tensor maps; page numbers looked up 32
-// stages at a time) through a ring in shared memory.  Eight warps attend: row tiles of sixteen rows (one, two or four of them) times as many
-// groups as that leaves, which take the stages in turn.  A warp keeps its rows' output and running maximum in registers:
+// In a CTA up to four producer warps stream stages of 32 positions (boxes of the keys' and values' tensor maps; page numbers looked up 32
+// stages at a time) through a ring in shared memory.  Eight warps attend (four where heads are 256 wide): row tiles of sixteen rows (one, two or four of
+// them) times as many groups as that leaves, which take the stages in turn.  A warp keeps its rows' output and running maximum in registers:
 // S = Q K^T, online softmax, O += P V with mma.sync; over 16-bit pools weights enter as the sum of a rounded part and its remainder, fp32
 // operands as parts of eleven bits whose three large products are added up.
 //
 // What bounds it.  Long contexts: the pools' bytes, at the rate of a copy (4 x 20000 positions of sixteen heads of 128 in fp16, 655 MB, 103 us = 98 %
-// of the measured rate; 48 ragged sequences of eight key heads in bf16, 804 MB, 126 us = 98 %).  A producer warp needs 0.4 to 0.6 us a stage: one
+// of the measured rate; 48 ragged sequences of eight key heads in bf16, 804 MB, 129 us = 97 %).  A producer warp needs 0.4 to 0.6 us a stage: one
 // alone fed 33 GB/s an SM (158 us), four feed 46.  Short ones: a chain.  0.3 us to past the wait for the kernel before, 1.8 until lengths are
 // read and the cut is known, 0.6 for page numbers, 0.6 for the first stage, a microsecond a stage, 1.2 for joining the warps: 5.6 us for
 // 190 positions; where a unit is cut 1 us for the counter and 2 for adding up (12288 positions of sixteen heads of 64: 17 us of which the

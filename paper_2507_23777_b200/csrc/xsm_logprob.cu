@@ -8,7 +8,7 @@
 // Backward: one pass, every element from its own logit and a few numbers of its row.
 //
 // What bounds them.  Many rows: forward the instructions (8192 x 8192 of bf16 31 us where the bytes take 21: five and a half an element, of which
-// one is the exponential, and a row's 700 warp instructions of beginning and end), backward memory (41 us, as long as without any
+// one is the exponential, and a row's 700 warp instructions of beginning and end), backward memory (42 us; 41 without any
 // arithmetic).  Two numbers an instruction (f32x2) took the pair from 111 to 78 us, blocks of 128 threads with four pieces of 16 bits
 // (eight of 32) under way to 72.  Few rows: a chain: 4.3 us for 5 x 4096 with 5 alternatives, of which a launch is 2; 96 x 131071 takes 8.0
 // without alternatives (the bytes 3.9) and 15.9 with 20, the parts' alternatives one behind the other: bound, second look, order, cluster, order.
