@@ -347,6 +347,116 @@ XSM_API xsm_status xsm_token_logprobs_grad(const xsm_logprob_grad_args *a, void 
  * rows of more than 8192 bytes, p is exp(z - lse) from an lse that is rounded to fp32: off by 2^-24 |lse| of itself. */
 XSM_API xsm_status xsm_token_logprobs_grad_near(const xsm_logprob_grad_args *a, const float *logprob, void *cuda_stream);
 
+/* ---- operators on a caller's own activations and weights ----
+ *
+ * Products on the tensor cores with what follows them in the same kernel: 16-bit elements (XSM_BF16, XSM_F16; rows 16-byte aligned, strides in elements), sums in
+ * fp32.  `d`, the summed axis of the forward products, is a multiple of 8; other sizes are any.  As above: the caller's stream of the current device, nothing is waited
+ * for, calls may be captured.  status: DEVICE, a 32-bit word, zeroed by the caller before its first use, which calls may share: XSM_ERR_TIMEOUT once a bounded wait of the
+ * device has run out, and the results of that call are then void.  workspace: DEVICE, 16-byte aligned, as many bytes as the function of that name says, of any
+ * content; calls that share one follow each other on one stream. */
+
+/* Log probabilities of given tokens under softmax(logits / temperature), logits = hidden . weight^T, which are never in memory:
+ *   z_rj = sum_i hidden[r][i] weight[j][i] / temperature,  lse_r = log sum_j exp(z_rj),  logprob_r = z_r,token - lse_r.
+ * Tokens outside [0, vocab), logits of -infinity and NaN as for xsm_token_logprobs. */
+typedef struct {
+    const void *hidden, *weight;          /* DEVICE dtype [rows][d], [vocab][d] */
+    const void *tokens;                   /* DEVICE int32 or int64 [rows], stride in elements */
+    float *logprob, *lse;                 /* DEVICE [rows] */
+    void *workspace;
+    int32_t *status;
+    int64_t hidden_stride, weight_stride, token_stride, workspace_bytes;
+    int32_t rows, vocab, d, dtype, token_bytes;
+    float temperature;
+} xsm_linear_logprobs_args;
+XSM_API size_t xsm_linear_logprobs_workspace(int rows, int vocab, int d);
+XSM_API xsm_status xsm_linear_logprobs(const xsm_linear_logprobs_args *a, void *cuda_stream);
+
+/* The gradient of sum_rows (g_logprob logprob + g_lse lse) by hidden and weight, in their type, from lse of the call above:
+ *   dz_rj = ([j = token_r] g_logprob_r - exp(z_rj - lse_r) (g_logprob_r - g_lse_r)) / temperature,  d_hidden = dz . weight,  d_weight = dz^T . hidden.
+ * g_logprob counts only where there is a token; rows with an lse of -infinity have none.  The logits are computed again, piece by piece of the vocabulary; dz is
+ * rounded to dtype once (fp16: scaled by a power of two that takes its largest possible element to 2^13, and back in the sums).  The workspace holds a
+ * piece of dz of at most 256 MiB (1024 tokens at least) and partial sums.  d_hidden or d_weight may be NULL. */
+typedef struct {
+    const void *hidden, *weight, *tokens; /* as above */
+    const float *lse;                     /* DEVICE [rows] */
+    const float *g_logprob, *g_lse;       /* DEVICE [rows], strides in elements; each may be NULL */
+    void *d_hidden, *d_weight;            /* DEVICE dtype [rows][d], [vocab][d] */
+    void *workspace;
+    int32_t *status;
+    int64_t hidden_stride, weight_stride, token_stride, g_logprob_stride, g_lse_stride, d_hidden_stride, d_weight_stride, workspace_bytes;
+    int32_t rows, vocab, d, dtype, token_bytes;
+    float temperature;
+} xsm_linear_logprobs_grad_args;
+XSM_API size_t xsm_linear_logprobs_grad_workspace(int rows, int vocab, int d);
+XSM_API xsm_status xsm_linear_logprobs_grad(const xsm_linear_logprobs_grad_args *a, void *cuda_stream);
+
+/* The gated feed-forward part of a block: out[r][f] = act(gate) up, gate = sum_i x[r][i] w_gate[f][i], up = sum_i x[r][i] w_up[f][i], gate and up in fp32;
+ * act(g) = g / (1 + exp(-g)) (activation 0, silu) or g (1 + erf(g / sqrt 2)) / 2 (1, gelu). */
+typedef struct {
+    const void *x, *w_gate, *w_up;        /* DEVICE dtype [rows][d], [ff][d], [ff][d] */
+    void *out;                            /* DEVICE dtype [rows][ff]; aligned to its elements */
+    int32_t *status;
+    int64_t x_stride, w_gate_stride, w_up_stride, out_stride;
+    int32_t rows, ff, d, dtype, activation;
+} xsm_gated_ff_args;
+XSM_API xsm_status xsm_gated_ff(const xsm_gated_ff_args *a, void *cuda_stream);
+
+/* The gradient of sum(g_out * out) by x, w_gate and w_up, in their type.  gate and up are computed again; their gradients g_out up act'(gate) and g_out act(gate) are
+ * rounded to dtype once (fp16: scaled by the power of two that takes the largest finite g_out to [1, 2)).  d_x, or d_w_gate and d_w_up, may be NULL. */
+typedef struct {
+    const void *x, *w_gate, *w_up;        /* as above */
+    const void *g_out;                    /* DEVICE dtype [rows][ff]; aligned to its elements */
+    void *d_x, *d_w_gate, *d_w_up;        /* DEVICE dtype [rows][d], [ff][d], [ff][d], the latter of one stride */
+    void *workspace;
+    int32_t *status;
+    int64_t x_stride, w_gate_stride, w_up_stride, g_out_stride, d_x_stride, d_w_stride, workspace_bytes;
+    int32_t rows, ff, d, dtype, activation;
+} xsm_gated_ff_grad_args;
+XSM_API size_t xsm_gated_ff_grad_workspace(int rows, int ff, int d);
+XSM_API xsm_status xsm_gated_ff_grad(const xsm_gated_ff_grad_args *a, void *cuda_stream);
+/* Tries of a shared-memory barrier before a wait of the following calls of the four above, in this process, gives up (0: the default, 2^22).  starve: these
+ * calls fetch no operands, so that their waits run out. */
+XSM_API xsm_status xsm_debug_product_waits(uint32_t tries, int starve);
+
+/* Norms of queries and keys for each head with the rotation of the positions:  y = R (gain x / sqrt(mean(x^2) + eps)), mean over the head, R as in xsm_kv_append.  fp32 within,
+ * rounded once.  The position of token j of a sequence is positions[sequence][j] (NULL: j); rows of a token whose position the rope does not have are zero, and
+ * so are their gradients.  d_head 32, 64, 96, 128 or 256; strides in elements of sequence, token, head, neighbouring elements of a head; q_out may be q, k_out k.
+ * n_heads or n_kv_heads may be 0. */
+typedef struct {
+    const void *q, *k;                    /* DEVICE dtype [batch][m][n_heads or n_kv_heads][d_head] */
+    void *q_out, *k_out;                  /* likewise */
+    const void *q_gain, *k_gain;          /* DEVICE gain_dtype [d_head] */
+    const int32_t *positions;             /* DEVICE [batch][m] */
+    const float *rope;                    /* as in xsm_kv_append_args */
+    int64_t q_stride[3], k_stride[3], q_out_stride[3], k_out_stride[3];
+    int32_t batch, m, n_heads, n_kv_heads, d_head, dtype, gain_dtype, rope_positions, rope_dims, interleaved;
+    float eps;
+} xsm_norm_rotate_args;
+XSM_API xsm_status xsm_norm_rotate(const xsm_norm_rotate_args *a, void *cuda_stream);
+
+/* The gradient of sum(g_q * q_out) + sum(g_k * k_out) by q, k and the gains (the latter in gain_dtype, added up in fp32 in an order of its own sizes' making). */
+typedef struct {
+    const void *q, *k, *q_gain, *k_gain;  /* as above */
+    const int32_t *positions;
+    const float *rope;
+    const void *g_q, *g_k;                /* DEVICE dtype, like q and k */
+    void *d_q, *d_k, *d_q_gain, *d_k_gain;
+    void *workspace;                      /* DEVICE, xsm_norm_rotate_grad_workspace bytes, of any content; calls that share one follow each other on one stream */
+    int64_t q_stride[3], k_stride[3], g_q_stride[3], g_k_stride[3], d_q_stride[3], d_k_stride[3], workspace_bytes;
+    int32_t batch, m, n_heads, n_kv_heads, d_head, dtype, gain_dtype, rope_positions, rope_dims, interleaved;
+    float eps;
+} xsm_norm_rotate_grad_args;
+XSM_API size_t xsm_norm_rotate_grad_workspace(int d_head);
+XSM_API xsm_status xsm_norm_rotate_grad(const xsm_norm_rotate_grad_args *a, void *cuda_stream);
+
+/* xsm_kv_append with the norms of keys, and of queries where there are any, before the rotation. */
+typedef struct {
+    const void *q_gain, *k_gain;          /* DEVICE gain_dtype [d_head] */
+    int32_t gain_dtype;
+    float eps;
+} xsm_head_norm;
+XSM_API xsm_status xsm_kv_append_norm(const xsm_kv *kv, const xsm_kv_append_args *a, const xsm_head_norm *n, void *cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

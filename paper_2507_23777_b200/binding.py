@@ -113,6 +113,14 @@ def load(path: str | None = None):
     L.xsm_token_logprobs.argtypes = [vp, vp]
     L.xsm_token_logprobs_grad.argtypes = [vp, vp]
     L.xsm_token_logprobs_grad_near.argtypes = [vp, vp, vp]
+    for name in ("linear_logprobs", "linear_logprobs_grad", "gated_ff", "gated_ff_grad", "norm_rotate", "norm_rotate_grad"):
+        getattr(L, "xsm_" + name).argtypes = [vp, vp]
+    for name in ("linear_logprobs", "linear_logprobs_grad", "gated_ff_grad"):
+        f = getattr(L, f"xsm_{name}_workspace")
+        f.restype, f.argtypes = C.c_size_t, [C.c_int, C.c_int, C.c_int]
+    L.xsm_norm_rotate_grad_workspace.restype, L.xsm_norm_rotate_grad_workspace.argtypes = C.c_size_t, [C.c_int]
+    L.xsm_kv_append_norm.argtypes = [vp, vp, vp, vp]
+    L.xsm_debug_product_waits.argtypes = [C.c_uint32, C.c_int]
     if path is None:
         _lib = L
     return L

@@ -9,8 +9,9 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libxsm.so")
 SOURCES = ["xsm_api.cu", "xsm_kernels.cu", "xsm_chain.cu", "xsm_proj_few.cu", "xsm_proj_umma.cu", "xsm_attn.cu", "xsm_f32.cu", "xsm_cond.cu", "xsm_tail.cu",
-           "xsm_append.cu", "xsm_attend.cu", "xsm_logprob.cu"]
-HEADERS = ["xsm_internal.h", "xsm_host.h", "xsm_common.cuh", "xsm_chain.cuh", "xsm_proj.cuh", "xsm_proj_few.cuh", "xsm_ops.h",
+           "xsm_append.cu", "xsm_attend.cu", "xsm_logprob.cu", "xsm_product.cu", "xsm_linear.cu", "xsm_gated.cu",
+           "xsm_norm.cu"]
+HEADERS = ["xsm_internal.h", "xsm_host.h", "xsm_common.cuh", "xsm_chain.cuh", "xsm_proj.cuh", "xsm_proj_few.cuh", "xsm_ops.h", "xsm_product.cuh",
            os.path.join("..", "..", "include", "xsm.h")]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC", "-Xcompiler", "-fvisibility=hidden"]

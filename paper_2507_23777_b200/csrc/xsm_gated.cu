@@ -1,0 +1,118 @@
+// The gated feed-forward part of a block: out = act(x . w_gate) * (x . w_up), both projections, the activation and the product in one kernel, and its gradients.
+//
+// A tile's columns are as many of gate as of up, so that both sums of an output lie in the same thread's tensor memory.  Backward: gate and up are computed
+// again and turned into their gradients where the products leave them (gate's and up's, rounded to the operands' type), then
+// dx = d_gate . w_gate + d_up . w_up is one product over both, d_w_gate = d_gate^T . x and d_w_up = d_up^T . x are one launch.
+#include "xsm_product.cuh"
+
+namespace xsm {
+
+static size_t up(size_t n) { return (n + 255) & ~(size_t)255; }
+static long long tiles_of(bool wide, long long m, long long n) { return wide ? ((m + 255) / 256) * ((n + 255) / 256) : ((m + 127) / 128) * ((n + 63) / 64); }
+static bool wide_tiles(long long m, long long n) { return m > 128 && n > 64; }
+
+struct GatedGradPlan {
+    bool wide, wide_x, wide_w;
+    int ld, splits_x, splits_w;
+    size_t amax, d_gate, d_up, part_x, part_w, bytes;
+};
+static GatedGradPlan plan_gated_grad(int rows, int ff, int d) {
+    GatedGradPlan p;
+    p.wide = wide_tiles(rows, ff);
+    p.wide_x = wide_tiles(rows, d);
+    p.wide_w = wide_tiles(ff, d);
+    p.ld = (ff + 7) / 8 * 8;
+    p.splits_x = product_splits(tiles_of(p.wide_x, rows, d), 2 * ((ff + 63) / 64), p.wide_x);
+    p.splits_w = product_splits(2 * tiles_of(p.wide_w, ff, d), (rows + 63) / 64, p.wide_w);
+    p.amax = 0;
+    p.d_gate = up(kAmaxBlocks * 4);
+    p.d_up = p.d_gate + up((size_t)rows * p.ld * 2);
+    p.part_x = p.d_up + up((size_t)rows * p.ld * 2);
+    p.part_w = p.part_x + (p.splits_x > 1 ? up((size_t)p.splits_x * rows * d * 4) : 0);
+    p.bytes = p.part_w + (p.splits_w > 1 ? up((size_t)2 * p.splits_w * ff * d * 4) : 0);
+    return p;
+}
+
+static const char *wrong_shape(int rows, int ff, int d, int dtype, int activation) {
+    if (dtype != XSM_BF16 && dtype != XSM_F16) return "dtype must be 1 (bf16) or 2 (fp16)";
+    if (rows < 0 || ff < 1 || d < 8 || d % 8) return "rows must not be negative, ff positive, d a positive multiple of 8";
+    if (activation != ACT_SILU && activation != ACT_GELU) return "activation must be 0 (silu) or 1 (gelu)";
+    return nullptr;
+}
+static bool rows_fit(const void *p, int64_t ld, int d) { return (uintptr_t)p % 16 == 0 && ld % 8 == 0 && ld >= d; }
+
+}  // namespace xsm
+
+using namespace xsm;
+
+xsm_status xsm_gated_ff(const xsm_gated_ff_args *a, void *cuda_stream) {
+    if (!a) return op_failed(XSM_ERR_INVALID_ARG, "null argument");
+    if (const char *w = wrong_shape(a->rows, a->ff, a->d, a->dtype, a->activation)) return op_failed(XSM_ERR_INVALID_ARG, w);
+    if (a->rows == 0) return XSM_OK;
+    if (!a->x || !a->w_gate || !a->w_up || !a->out || !a->status) return op_failed(XSM_ERR_INVALID_ARG, "null argument");
+    if (!rows_fit(a->x, a->x_stride, a->d) || !rows_fit(a->w_gate, a->w_gate_stride, a->d) || !rows_fit(a->w_up, a->w_up_stride, a->d))
+        return op_failed(XSM_ERR_INVALID_ARG, "rows of x, w_gate and w_up must be 16-byte aligned and must not overlap");
+    if ((uintptr_t)a->out % 2 || a->out_stride < a->ff || (uintptr_t)a->status % 4) return op_failed(XSM_ERR_INVALID_ARG, "out and status must be aligned to their elements, rows of out must not overlap");
+    ProductArgs A = {};
+    A.m = a->rows; A.n = a->ff; A.jobs = A.splits = 1;
+    A.status = a->status; A.activation = a->activation;
+    A.out[0] = a->out; A.out_ld = a->out_stride;
+    const Operand x[2] = {{a->x, a->rows, a->d, a->x_stride}, {}}, w[2] = {{a->w_gate, a->ff, a->d, a->w_gate_stride}, {a->w_up, a->ff, a->d, a->w_up_stride}};
+    return launched(launch_product(PR_GATED, a->dtype, wide_tiles(a->rows, a->ff), A, x, w, 1, (cudaStream_t)cuda_stream));
+}
+
+size_t xsm_gated_ff_grad_workspace(int rows, int ff, int d) { return rows < 1 || ff < 1 || d < 1 ? 0 : plan_gated_grad(rows, ff, d).bytes; }
+
+xsm_status xsm_gated_ff_grad(const xsm_gated_ff_grad_args *a, void *cuda_stream) {
+    if (!a) return op_failed(XSM_ERR_INVALID_ARG, "null argument");
+    if (const char *w = wrong_shape(a->rows, a->ff, a->d, a->dtype, a->activation)) return op_failed(XSM_ERR_INVALID_ARG, w);
+    if (!a->d_x && !a->d_w_gate && !a->d_w_up) return XSM_OK;
+    if (!a->d_w_gate != !a->d_w_up) return op_failed(XSM_ERR_INVALID_ARG, "d_w_gate and d_w_up go together");
+    const cudaStream_t st = (cudaStream_t)cuda_stream;
+    if (a->d_w_gate && (!rows_fit(a->d_w_gate, a->d_w_stride, a->d) || !rows_fit(a->d_w_up, a->d_w_stride, a->d)))
+        return op_failed(XSM_ERR_INVALID_ARG, "rows of d_w_gate and d_w_up must be 16-byte aligned and must not overlap");
+    if (a->rows == 0) {
+        cudaError_t e = cudaSuccess;
+        if (a->d_w_gate) e = cudaMemset2DAsync(a->d_w_gate, (size_t)a->d_w_stride * 2, 0, (size_t)a->d * 2, (size_t)a->ff, st);
+        if (a->d_w_gate && e == cudaSuccess) e = cudaMemset2DAsync(a->d_w_up, (size_t)a->d_w_stride * 2, 0, (size_t)a->d * 2, (size_t)a->ff, st);
+        return launched(e);
+    }
+    if (!a->x || !a->w_gate || !a->w_up || !a->g_out || !a->workspace || !a->status) return op_failed(XSM_ERR_INVALID_ARG, "null argument");
+    if (!rows_fit(a->x, a->x_stride, a->d) || !rows_fit(a->w_gate, a->w_gate_stride, a->d) || !rows_fit(a->w_up, a->w_up_stride, a->d) || (a->d_x && !rows_fit(a->d_x, a->d_x_stride, a->d)))
+        return op_failed(XSM_ERR_INVALID_ARG, "rows of x, w_gate, w_up and d_x must be 16-byte aligned and must not overlap");
+    if ((uintptr_t)a->g_out % 2 || a->g_out_stride < 0 || (uintptr_t)a->status % 4 || (uintptr_t)a->workspace % 16)
+        return op_failed(XSM_ERR_INVALID_ARG, "g_out and status must be aligned to their elements, workspace to 16 bytes");
+    const GatedGradPlan p = plan_gated_grad(a->rows, a->ff, a->d);
+    if (a->workspace_bytes < (int64_t)p.bytes) return op_failed(XSM_ERR_CAPACITY, "the workspace is too small");
+    char *ws = (char *)a->workspace;
+    ProductArgs A = {};
+    A.m = a->rows; A.n = a->ff; A.jobs = A.splits = 1;
+    A.status = a->status; A.activation = a->activation;
+    A.g_y = a->g_out; A.g_y_ld = a->g_out_stride;
+    A.out[0] = ws + p.d_gate; A.out[1] = ws + p.d_up; A.out_ld = p.ld;
+    cudaError_t e = cudaSuccess;
+    if (a->dtype == XSM_F16) {        // fp16 has no numbers below 2^-24: the largest gradient that comes in is taken to 1 and more, which leaves up to 2^15 for up
+        A.amax = (const float *)(ws + p.amax);
+        e = launch_amax_rows(a->g_out, a->dtype, a->rows, a->ff, a->g_out_stride, (float *)(ws + p.amax), st);
+    }
+    const Operand x[2] = {{a->x, a->rows, a->d, a->x_stride}, {}}, w[2] = {{a->w_gate, a->ff, a->d, a->w_gate_stride}, {a->w_up, a->ff, a->d, a->w_up_stride}};
+    const Operand g[2] = {{ws + p.d_gate, a->rows, a->ff, p.ld}, {ws + p.d_up, a->rows, a->ff, p.ld}};
+    if (e == cudaSuccess) e = launch_product(PR_GATED_GRAD, a->dtype, p.wide, A, x, w, 1, st);
+    ProductArgs G = {};
+    G.status = a->status; G.amax = A.amax; G.amax_to = A.amax_to; G.b_mn = 1;
+    if (a->d_x && e == cudaSuccess) {
+        G.m = a->rows; G.n = a->d; G.jobs = 1; G.splits = p.splits_x;
+        G.out[0] = a->d_x; G.out_ld = a->d_x_stride;
+        G.partial = p.splits_x > 1 ? (float *)(ws + p.part_x) : nullptr;
+        e = launch_product(PR_OUT, a->dtype, p.wide_x, G, g, w, 2, st);
+        if (G.partial && e == cudaSuccess) e = launch_join(G, a->dtype, st);
+    }
+    if (a->d_w_gate && e == cudaSuccess) {
+        G.m = a->ff; G.n = a->d; G.jobs = 2; G.splits = p.splits_w; G.a_mn = 1;
+        G.out[0] = a->d_w_gate; G.out[1] = a->d_w_up; G.out_ld = a->d_w_stride;
+        G.partial = p.splits_w > 1 ? (float *)(ws + p.part_w) : nullptr;
+        e = launch_product(PR_OUT, a->dtype, p.wide_w, G, g, x, 1, st);
+        if (G.partial && e == cudaSuccess) e = launch_join(G, a->dtype, st);
+    }
+    return launched(e);
+}

@@ -1,0 +1,194 @@
+// Log probabilities of given tokens straight from hidden states and the weights of an output projection, and their gradients: the logits of a tile are
+// worked on where the products leave them and are never in memory.
+//
+// Forward: z = hidden . weight / T; every tile of 256 (few rows: 64) tokens of the vocabulary gives a row two pairs (maximum, sum of exponentials), a second
+// kernel joins them: lse = max + log sum.  Backward, in pieces of the vocabulary: the logits once more, p = exp(z - lse), d = ([token] g - p (g - g_lse)) / T
+// rounded to the operands' type, then d_hidden = d . weight and d_weight = d^T . hidden.
+#include "xsm_product.cuh"
+
+#include <math.h>
+
+namespace xsm {
+
+constexpr long long kPieceBytes = 256ll << 20;      // of a piece's gradients by the logits
+
+// 32 rows a block; thread (row, y) joins parts y, y + 8, ...
+__global__ void __launch_bounds__(256) join_stats_kernel(const float2 *parts, const float *token_z, const void *tokens, long long token_ld, int token_bytes, int rows, int vocab,
+                                                         int n, float *logprob, float *lse) {
+    chain_go();
+    chain_wait();
+    __shared__ float2 s[8][32];
+    const int x = threadIdx.x & 31, y = threadIdx.x >> 5, row = blockIdx.x * 32 + x;
+    float m = -INFINITY, sum = 0.f;
+    auto take = [&](float2 p) {
+        const float was = m;
+        m = fmaxf(m, p.x);
+        const float base = m == -INFINITY ? 0.f : m;
+        sum = sum * ex2(was - base) + p.y * ex2(p.x - base);
+    };
+    if (row < rows) {
+#pragma unroll 4
+        for (int i = y; i < n; i += 8) take(parts[(long long)i * rows + row]);
+    }
+    s[y][x] = make_float2(m, sum);
+    __syncthreads();
+    if (y || row >= rows) return;
+    for (int i = 1; i < 8; ++i) take(s[i][x]);
+    const float l = m == -INFINITY && sum == 0.f ? -INFINITY : (m + log2f(sum)) * 0.69314718056f;
+    const long long t = token_bytes == 8 ? reinterpret_cast<const long long *>(tokens)[row * token_ld] : (long long)reinterpret_cast<const int *>(tokens)[row * token_ld];
+    lse[row] = l;
+    logprob[row] = t < 0 || t >= vocab ? 0.f : l == -INFINITY ? -INFINITY : token_z[row] - l;
+}
+
+struct LinearPlan { bool wide; int parts; };
+static LinearPlan plan_linear(int rows, int vocab) {
+    LinearPlan p;
+    p.wide = rows > 128;
+    p.parts = 2 * ((vocab + (p.wide ? 255 : 63)) / (p.wide ? 256 : 64));
+    return p;
+}
+
+static size_t up(size_t n) { return (n + 255) & ~(size_t)255; }
+
+struct LinearGradPlan {
+    bool wide_z, wide_h, wide_w;
+    int piece, pieces, splits_h, splits_w;
+    size_t amax, dz, part_h, part_w, bytes;      // offsets in the workspace
+};
+static bool wide_tiles(long long m, long long n) { return m > 128 && n > 64; }
+static LinearGradPlan plan_linear_grad(int rows, int vocab, int d) {
+    LinearGradPlan p;
+    long long piece = kPieceBytes / (2ll * rows) / 256 * 256;
+    if (piece < 1024) piece = 1024;
+    p.pieces = (int)((vocab + piece - 1) / piece);
+    p.piece = (int)(((vocab + p.pieces - 1) / p.pieces + 255) / 256 * 256);
+    if (p.piece > vocab) p.piece = (vocab + 63) / 64 * 64;
+    p.pieces = (vocab + p.piece - 1) / p.piece;
+    p.wide_z = wide_tiles(rows, p.piece);
+    p.wide_h = wide_tiles(rows, d);
+    p.wide_w = wide_tiles(p.piece, d);
+    auto tiles = [](bool wide, long long m, long long n) { return wide ? ((m + 255) / 256) * ((n + 255) / 256) : ((m + 127) / 128) * ((n + 63) / 64); };
+    p.splits_h = product_splits(tiles(p.wide_h, rows, d), p.piece / 64, p.wide_h);
+    const int last = vocab - (p.pieces - 1) * p.piece;            // (the shortest piece has to have a block for every part)
+    if (p.splits_h > (last + 63) / 64) p.splits_h = (last + 63) / 64;
+    p.splits_w = product_splits(tiles(p.wide_w, p.piece, d), (rows + 63) / 64, p.wide_w);
+    p.amax = 0;
+    p.dz = up(kAmaxBlocks * 4);
+    p.part_h = p.dz + up((size_t)rows * p.piece * 2);
+    p.part_w = p.part_h + (p.splits_h > 1 || p.pieces > 1 ? up((size_t)p.splits_h * rows * d * 4) : 0);
+    p.bytes = p.part_w + (p.splits_w > 1 ? up((size_t)p.splits_w * p.piece * d * 4) : 0);
+    return p;
+}
+
+static const char *wrong_shape(int rows, int vocab, int d, int dtype, int token_bytes, float temperature) {
+    if (dtype != XSM_BF16 && dtype != XSM_F16) return "dtype must be 1 (bf16) or 2 (fp16)";
+    if (rows < 0 || vocab < 1 || d < 8 || d % 8) return "rows must not be negative, vocab positive, d a positive multiple of 8";
+    if (token_bytes != 4 && token_bytes != 8) return "token_bytes must be 4 or 8";
+    if (!(temperature > 0.f) || !(temperature < INFINITY) || !(1.f / temperature < INFINITY)) return "temperature must be positive and finite, and its reciprocal finite";
+    return nullptr;
+}
+static bool rows_fit(const void *p, int64_t ld, int d) { return (uintptr_t)p % 16 == 0 && ld % 8 == 0 && ld >= d; }
+
+}  // namespace xsm
+
+using namespace xsm;
+
+size_t xsm_linear_logprobs_workspace(int rows, int vocab, int d) {
+    (void)d;
+    if (rows < 1 || vocab < 1) return 0;
+    return up((size_t)plan_linear(rows, vocab).parts * rows * 8) + up((size_t)rows * 4);
+}
+
+xsm_status xsm_linear_logprobs(const xsm_linear_logprobs_args *a, void *cuda_stream) {
+    if (!a) return op_failed(XSM_ERR_INVALID_ARG, "null argument");
+    if (const char *w = wrong_shape(a->rows, a->vocab, a->d, a->dtype, a->token_bytes, a->temperature)) return op_failed(XSM_ERR_INVALID_ARG, w);
+    if (a->rows == 0) return XSM_OK;
+    if (!a->hidden || !a->weight || !a->tokens || !a->logprob || !a->lse || !a->workspace || !a->status) return op_failed(XSM_ERR_INVALID_ARG, "null argument");
+    if (!rows_fit(a->hidden, a->hidden_stride, a->d) || !rows_fit(a->weight, a->weight_stride, a->d))
+        return op_failed(XSM_ERR_INVALID_ARG, "rows of hidden and weight must be 16-byte aligned and must not overlap");
+    if ((uintptr_t)a->tokens % a->token_bytes || ((uintptr_t)a->logprob | (uintptr_t)a->lse | (uintptr_t)a->status) % 4 || (uintptr_t)a->workspace % 16)
+        return op_failed(XSM_ERR_INVALID_ARG, "tokens, logprob, lse and status must be aligned to their elements, workspace to 16 bytes");
+    if (a->workspace_bytes < (int64_t)xsm_linear_logprobs_workspace(a->rows, a->vocab, a->d)) return op_failed(XSM_ERR_CAPACITY, "the workspace is too small");
+    const LinearPlan p = plan_linear(a->rows, a->vocab);
+    ProductArgs A = {};
+    A.m = a->rows; A.n = a->vocab; A.jobs = A.splits = 1;
+    A.status = a->status;
+    A.tokens = a->tokens; A.token_ld = a->token_stride; A.token_bytes = a->token_bytes; A.vocab = a->vocab;
+    A.inv_t = 1.f / a->temperature;
+    A.c = (float)(1.4426950408889634 / a->temperature);
+    A.parts = (float2 *)a->workspace;
+    A.token_z = (float *)((char *)a->workspace + up((size_t)p.parts * a->rows * 8));
+    const Operand h[2] = {{a->hidden, a->rows, a->d, a->hidden_stride}, {}}, w[2] = {{a->weight, a->vocab, a->d, a->weight_stride}, {}};
+    const cudaStream_t st = (cudaStream_t)cuda_stream;
+    cudaError_t e = launch_product(PR_STATS, a->dtype, p.wide, A, h, w, 1, st);
+    if (e == cudaSuccess)
+        e = launch_early(join_stats_kernel, dim3((unsigned)((a->rows + 31) / 32)), dim3(256), 0, st, (const float2 *)A.parts, (const float *)A.token_z, a->tokens, (long long)a->token_stride,
+                         (int)a->token_bytes, (int)a->rows, (int)a->vocab, (int)p.parts, a->logprob, a->lse);
+    return launched(e);
+}
+
+size_t xsm_linear_logprobs_grad_workspace(int rows, int vocab, int d) {
+    if (rows < 1 || vocab < 1 || d < 1) return 0;
+    return plan_linear_grad(rows, vocab, d).bytes;
+}
+
+xsm_status xsm_linear_logprobs_grad(const xsm_linear_logprobs_grad_args *a, void *cuda_stream) {
+    if (!a) return op_failed(XSM_ERR_INVALID_ARG, "null argument");
+    if (const char *w = wrong_shape(a->rows, a->vocab, a->d, a->dtype, a->token_bytes, a->temperature)) return op_failed(XSM_ERR_INVALID_ARG, w);
+    if (!a->d_hidden && !a->d_weight) return XSM_OK;
+    const cudaStream_t st = (cudaStream_t)cuda_stream;
+    if (a->d_weight && !rows_fit(a->d_weight, a->d_weight_stride, a->d)) return op_failed(XSM_ERR_INVALID_ARG, "rows of d_weight must be 16-byte aligned and must not overlap");
+    if (a->rows == 0)
+        return a->d_weight ? launched(cudaMemset2DAsync(a->d_weight, (size_t)a->d_weight_stride * 2, 0, (size_t)a->d * 2, (size_t)a->vocab, st)) : XSM_OK;
+    if (!a->hidden || !a->weight || !a->tokens || !a->lse || !a->workspace || !a->status) return op_failed(XSM_ERR_INVALID_ARG, "null argument");
+    if (!rows_fit(a->hidden, a->hidden_stride, a->d) || !rows_fit(a->weight, a->weight_stride, a->d) || (a->d_hidden && !rows_fit(a->d_hidden, a->d_hidden_stride, a->d)))
+        return op_failed(XSM_ERR_INVALID_ARG, "rows of hidden, weight and d_hidden must be 16-byte aligned and must not overlap");
+    if ((uintptr_t)a->tokens % a->token_bytes || ((uintptr_t)a->lse | (uintptr_t)a->g_logprob | (uintptr_t)a->g_lse | (uintptr_t)a->status) % 4 || (uintptr_t)a->workspace % 16)
+        return op_failed(XSM_ERR_INVALID_ARG, "tokens, lse, g_logprob, g_lse and status must be aligned to their elements, workspace to 16 bytes");
+    const LinearGradPlan p = plan_linear_grad(a->rows, a->vocab, a->d);
+    if (a->workspace_bytes < (int64_t)p.bytes) return op_failed(XSM_ERR_CAPACITY, "the workspace is too small");
+    char *ws = (char *)a->workspace;
+    ProductArgs Z = {};
+    Z.jobs = Z.splits = 1;
+    Z.status = a->status;
+    Z.m = a->rows;
+    Z.tokens = a->tokens; Z.token_ld = a->token_stride; Z.token_bytes = a->token_bytes; Z.vocab = a->vocab;
+    Z.inv_t = 1.f / a->temperature;
+    Z.c = (float)(1.4426950408889634 / a->temperature);
+    Z.lse = a->lse; Z.g = a->g_logprob; Z.g_ld = a->g_logprob_stride; Z.g_lse = a->g_lse; Z.g_lse_ld = a->g_lse_stride;
+    cudaError_t e = cudaSuccess;
+    if (a->dtype == XSM_F16) {        // fp16 has no numbers below 2^-24: the largest gradient by a logit is taken to 2^13 and more
+        Z.amax = (const float *)(ws + p.amax);
+        Z.amax_to = 13;
+        e = launch_amax_pairs(Z.g, Z.g_ld, Z.g_lse, Z.g_lse_ld, a->rows, Z.inv_t, (float *)(ws + p.amax), st);
+    }
+    for (int i = 0; i < p.pieces && e == cudaSuccess; ++i) {
+        const int v0 = i * p.piece, v = a->vocab - v0 < p.piece ? a->vocab - v0 : p.piece;
+        const void *weight = (const char *)a->weight + (long long)v0 * a->weight_stride * 2;
+        const Operand hidden[2] = {{a->hidden, a->rows, a->d, a->hidden_stride}, {}}, w[2] = {{weight, v, a->d, a->weight_stride}, {}}, dz[2] = {{ws + p.dz, a->rows, v, p.piece}, {}};
+        ProductArgs A = Z;
+        A.n = v; A.vocab0 = v0;
+        A.out[0] = ws + p.dz; A.out_ld = p.piece;
+        e = launch_product(PR_DLOGITS, a->dtype, p.wide_z, A, hidden, w, 1, st);
+        ProductArgs G = {};
+        G.jobs = 1;
+        G.status = a->status; G.amax = Z.amax; G.amax_to = Z.amax_to;
+        if (a->d_hidden && e == cudaSuccess) {
+            G.m = a->rows; G.n = a->d; G.splits = p.splits_h; G.a_mn = 0; G.b_mn = 1;
+            G.out[0] = a->d_hidden; G.out_ld = a->d_hidden_stride;
+            G.partial = p.splits_h > 1 || p.pieces > 1 ? (float *)(ws + p.part_h) : nullptr;
+            G.add = i > 0;
+            e = launch_product(PR_OUT, a->dtype, p.wide_h, G, dz, w, 1, st);
+            if (G.partial && i == p.pieces - 1 && e == cudaSuccess) e = launch_join(G, a->dtype, st);
+        }
+        if (a->d_weight && e == cudaSuccess) {
+            G.m = v; G.n = a->d; G.splits = p.splits_w; G.a_mn = 1; G.b_mn = 1;
+            G.out[0] = (char *)a->d_weight + (long long)v0 * a->d_weight_stride * 2; G.out_ld = a->d_weight_stride;
+            G.partial = p.splits_w > 1 ? (float *)(ws + p.part_w) : nullptr;
+            G.add = 0;
+            e = launch_product(PR_OUT, a->dtype, p.wide_w, G, dz, hidden, 1, st);
+            if (G.partial && e == cudaSuccess) e = launch_join(G, a->dtype, st);
+        }
+    }
+    return launched(e);
+}

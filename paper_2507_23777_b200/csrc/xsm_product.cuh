@@ -1,0 +1,79 @@
+// Tiled matrix products of the operators on a caller's own activations and weights, on tcgen05: one persistent kernel, several things that it
+// can do with a finished tile (xsm_product.cu, xsm_linear.cu, xsm_gated.cu).
+#pragma once
+#include "xsm_chain.cuh"
+#include "xsm_ops.h"
+
+#include <cuda.h>
+
+namespace xsm {
+
+enum ProductEpi {
+    PR_STATS,        // maximum and sum of exponentials of a row's logits, the token's logit
+    PR_DLOGITS,      // gradient by the logits
+    PR_GATED,        // act(gate) * up
+    PR_GATED_GRAD,   // gradients by gate and up
+    PR_OUT           // the sums themselves: rounded to the output's type, or fp32 partial sums
+};
+enum Activation { ACT_SILU = 0, ACT_GELU = 1 };
+
+constexpr int kAmaxBlocks = 256;
+
+struct __align__(64) ProductMaps { CUtensorMap a[2], b[2]; };
+
+struct ProductArgs {
+    int m, n;                       // rows and columns of the result (PR_GATED: n columns of gate and of up)
+    int tiles_m, tiles_n, jobs, splits, tiles;
+    int kb0, kb;                    // blocks of 64 along the summed axis: of the first pair of operands, of all
+    int a_mn, b_mn;                 // operands whose rows run along the summed axis
+    int a_rows;                     // rows of a box of A (not a_mn)
+    uint32_t stage_tx;              // bytes of a stage of all CTAs of a tile
+    unsigned tries;                 // of a barrier, before a wait gives up
+    int starve;                     // fetch nothing (xsm_debug_product_waits)
+    int *status;
+
+    // PR_STATS, PR_DLOGITS
+    const void *tokens;
+    long long token_ld;
+    int token_bytes, vocab0, vocab; // first token of this piece of the vocabulary, all tokens
+    float c, inv_t;                 // log2(e) / T, 1 / T
+    float2 *parts;                  // [part][m]: maximum, sum
+    float *token_z;                 // [m]
+    const float *lse, *g, *g_lse;
+    long long g_ld, g_lse_ld;
+
+    // PR_GATED_GRAD reads g_y, PR_GATED* and PR_DLOGITS write 16-bit rows
+    int activation;
+    const void *g_y;
+    long long g_y_ld;
+    void *out[2];                   // PR_OUT: of each job; PR_GATED_GRAD: gate's, up's
+    long long out_ld;
+    const float *amax;              // [kAmaxBlocks], NULL: scale 1
+    int amax_to;                    // the largest is scaled to [2^amax_to, 2^(amax_to + 1))
+    float *partial;                 // PR_OUT: fp32 [job][split][m][n] instead of out, where it is not NULL
+    int add;                        // to what partial holds
+};
+
+// How a product is cut: `wide`: two CTAs share tiles of 256 x 256; otherwise a CTA has tiles of 128 x 64.
+struct ProductCut { int group, bn; };
+inline ProductCut product_cut(bool wide) { return wide ? ProductCut{2, 256} : ProductCut{1, 64}; }
+
+// An operand in memory: `rows` rows of `row` elements, ld elements apart.
+struct Operand { const void *p; long long rows, row, ld; };
+
+// Fills in the cut (tiles, boxes, maps) of A and launches.  a, b: operands of the pairs or jobs; summed: which axis of each is summed over
+// (a_mn, b_mn: the rows).
+cudaError_t launch_product(ProductEpi epi, int dtype, bool wide, ProductArgs A, const Operand (&a)[2], const Operand (&b)[2], int pairs, cudaStream_t st);
+
+// |x| at most over rows of 16-bit elements, or of fp32 numbers 2|g| + |g_lse| times `by`; [kAmaxBlocks]
+cudaError_t launch_amax_rows(const void *x, int dtype, long long rows, long long cols, long long ld, float *amax, cudaStream_t st);
+cudaError_t launch_amax_pairs(const float *g, long long g_ld, const float *g_lse, long long g_lse_ld, int rows, float by, float *amax, cudaStream_t st);
+// out[job] = sum over splits of partial [job][split][m][n], times the scale back
+cudaError_t launch_join(const ProductArgs &A, int dtype, cudaStream_t st);
+
+// how many parts the summed axis is cut into so that `tiles` tiles keep the chip busy
+int product_splits(long long tiles, int kb, bool wide);
+int product_sms();
+void product_waits(unsigned *tries, int *starve);
+
+}  // namespace xsm

@@ -25,8 +25,16 @@ _APPEND = struct.Struct("8P13q8i")
 _ATTEND = struct.Struct("7P8q7if")
 _LOGPROB = struct.Struct("7P2q5if")
 _GRAD = struct.Struct("10P6q5if")
+_LINEAR = struct.Struct("7P4q5if")
+_LINEAR_GRAD = struct.Struct("10P8q5if")
+_GATED = struct.Struct("5P4q5i")
+_GATED_GRAD = struct.Struct("9P7q5i")
+_NORM = struct.Struct("8P12q10if")
+_NORM_GRAD = struct.Struct("13P19q10if")
+_HEAD_NORM = struct.Struct("2Pif")
 
 TokenLogprobs = namedtuple("TokenLogprobs", "logprob entropy lse top_ids top_logprobs")
+LinearLogprobs = namedtuple("LinearLogprobs", "logprob lse")
 
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
 
@@ -68,6 +76,11 @@ def _need_here(t):
 def _need_ints(t, n: int, device: int, what: str):
     _need(t.dtype is torch.int32 and tuple(t.shape) == (n,) and (n < 2 or t.stride(0) == 1) and t.get_device() == device,
           f"{what} must be a contiguous int32 tensor of {n} elements on cuda:{device}")
+
+
+def _need_gain(g, d: int, device: int, dtype):
+    _need(g.dim() == 1 and g.shape[0] == d and g.dtype is dtype and dtype in _DTYPES and g.stride(0) == 1 and g.get_device() == device,
+          f"gains must be contiguous [{d}] on cuda:{device}, of fp32, bf16 or fp16, both of one type")
 
 
 _empty = torch.empty_strided      # the quickest of torch's ways to new memory
@@ -190,11 +203,28 @@ class PagedCache:
               f"lse must be contiguous float32 {n} on cuda:{self.device}")
         raise ValueError("the arguments of attend do not go together")
 
-    def append(self, k, v, block_table, starts, counts=None, q=None, rope=None, interleaved=False, out=None):
+    def _gains(self, q, q_gain, k_gain, eps):
+        """The norm of an append as the library takes it."""
+        _need(k_gain is not None and (q is None) == (q_gain is None), "gains go together: k_gain, and q_gain where there is q")
+        for g in (k_gain, q_gain):
+            if g is not None:
+                _need_gain(g, self.d_head, self.device, k_gain.dtype)
+                _need(not (_grad_enabled() and g.requires_grad), "append has no gradient: call it under torch.no_grad()")
+                _no_tangents(g)
+        try:
+            return _HEAD_NORM.pack(0 if q_gain is None else q_gain.data_ptr(), k_gain.data_ptr(), _DTYPES[k_gain.dtype], eps)
+        except _BEYOND as e:
+            raise ValueError(f"an argument of append is beyond its type: {e}") from None
+
+    def append(self, k, v, block_table, starts, counts=None, q=None, rope=None, interleaved=False, out=None, q_gain=None, k_gain=None, eps=1e-6):
         """Writes k and v, [batch, m, n_kv_heads, d_head], to positions starts[b] + j (j < counts[b]) of every sequence; keys, and queries
         q [batch, m, n_heads, d_head], are rotated by `rope` (float32 [positions, dims / 2, 2], see rope_table).  Returns the rotated
-        queries in `out` (a new tensor, or the one given; it may be q), or None without q.  Like attend it has no gradient, and refuses tensors that
+        queries in `out` (a new tensor, or the one given; it may be q), or None without q.  With gains [d_head] (fp32, bf16 or fp16; q_gain where there is q)
+        every head of keys and queries is normed before, as norm_rotate does it.  Like attend it has no gradient, and refuses tensors that
         want one unless torch.no_grad() says that it is not needed."""
+        gains = None
+        if k_gain is not None or q_gain is not None:
+            gains = self._gains(q, q_gain, k_gain, eps)
         if _grad_enabled() and (k.requires_grad or v.requires_grad or q is not None and q.requires_grad or rope is not None and rope.requires_grad or
                                         out is not None and out.requires_grad):
             raise ValueError("append has no gradient: call it under torch.no_grad()")
@@ -241,7 +271,7 @@ class PagedCache:
         except _BEYOND as e:
             raise ValueError(f"an argument of append is beyond its type: {e}") from None
         _written((self.k, self.v) if out is None else (self.k, self.v, out))
-        status = self.lib.xsm_kv_append(self._h, args, _raw_stream(device))
+        status = self.lib.xsm_kv_append(self._h, args, _raw_stream(device)) if gains is None else self.lib.xsm_kv_append_norm(self._h, args, gains, _raw_stream(device))
         if status:
             _check(status)
         return out
@@ -459,3 +489,356 @@ def token_logprobs(logits, tokens, top: int = 0, temperature: float = 1.0) -> To
     if logits.requires_grad and _grad_enabled():
         return TokenLogprobs(*_TokenLogprobs.apply(logits, tokens, top, temperature))
     return _forward(logits, tokens, top, temperature)
+
+
+# ------------------------------------------------------------------------------------------ products with what follows them
+
+_ACTIVATIONS = {"silu": 0, "gelu": 1}
+_status_words = {}       # by device: a word that a wait that ran out leaves its status in
+
+
+def _status(device: int, stream: int) -> int:
+    """Address of the device's status word."""
+    t = _status_words.get(device)
+    if t is None:
+        t = _zeros_while_recording(16, device) if stream and _capturing() else torch.zeros(16, dtype=torch.uint8, device=f"cuda:{device}")
+        _status_words[device] = t
+    return t.data_ptr()
+
+
+def check(device=None):
+    """Waits for the device (the current one) and raises an XsmError if a bounded wait of an earlier linear_logprobs, gated_feed_forward or gradient of
+    theirs ran out there, replays of recorded ones among them (the results since the last check are void)."""
+    i = _current_device() if device is None else torch.device(device).index if not isinstance(device, int) else device
+    torch.cuda.synchronize(i)
+    t = _status_words.get(i)
+    if t is not None:
+        status = int(t[:4].view(torch.int32)[0])
+        if status:
+            t[:4].zero_()
+            raise binding.XsmError(status, "a bounded device-side wait ran out of patience")
+
+
+def _rows(t, what: str, device: int, dtype, width=None):
+    """Row stride of a matrix of 16-bit elements that the products can take as it lies."""
+    if t.dim() != 2 or t.dtype is not dtype or width is not None and t.shape[1] != width:
+        raise ValueError(f"{what} must be [rows, {'d' if width is None else width}] of {dtype}, not {list(t.shape)} of {t.dtype}")
+    if t.get_device() != device:
+        raise ValueError(f"{what} must be on cuda:{device}")
+    n, w = t.shape
+    ld, step = t.stride()
+    if n < 2 or w == 0:
+        ld = w
+    if step != 1 and w > 1 or ld < w or ld % 8 or t.data_ptr() % 16:
+        raise ValueError(f"rows of {what} must be of neighbouring elements, 16-byte aligned, and must not overlap")
+    return ld
+
+
+def _need_products(t, what: str):
+    """Device and type of a call's first operand."""
+    if t.dtype is not torch.bfloat16 and t.dtype is not torch.float16:
+        raise ValueError(f"{what} must be of bf16 or fp16")
+    device = t.get_device()
+    if device < 0 or device != _current_device():
+        _need_here(t)
+    return device, t.dtype
+
+
+def _no_gradient(what: str, *tensors):
+    if _grad_enabled():
+        for t in tensors:
+            if t is not None and t.requires_grad:
+                raise ValueError(f"{what} has no gradient of its own: call it under torch.no_grad()")
+    if forward_ad._current_level >= 0:
+        _no_tangents(*tensors)
+
+
+def _check_linear(hidden, weight, tokens):
+    device, dtype = _need_products(hidden, "hidden")
+    ld = _rows(hidden, "hidden", device, dtype)
+    rows, d = hidden.shape
+    w_ld = _rows(weight, "weight", device, dtype, d)
+    if d < 8 or d % 8 or weight.shape[0] < 1:
+        raise ValueError("the width of hidden must be a positive multiple of 8, and weight must have rows")
+    if tokens.shape != (rows,) or tokens.get_device() != device or tokens.dtype not in _TOKENS:
+        raise ValueError(f"tokens must be int32 or int64 [{rows}] on cuda:{device}")
+    return device, dtype, rows, d, ld, w_ld
+
+
+def _linear_forward(hidden, weight, tokens, temperature):
+    device, dtype, rows, d, ld, w_ld = _check_linear(hidden, weight, tokens)
+    lib, where, vocab, stream = binding.load(), hidden.device, weight.shape[0], _raw_stream(device)
+    logprob = _empty((rows,), (1,), dtype=torch.float32, device=where)
+    lse = _empty((rows,), (1,), dtype=torch.float32, device=where)
+    n = lib.xsm_linear_logprobs_workspace(rows, vocab, d)
+    ws = _empty((n,), (1,), dtype=torch.uint8, device=where)
+    try:
+        args = _LINEAR.pack(hidden.data_ptr(), weight.data_ptr(), tokens.data_ptr(), logprob.data_ptr(), lse.data_ptr(), ws.data_ptr(), _status(device, stream),
+                            ld, w_ld, tokens.stride(0), n, rows, vocab, d, _DTYPES[dtype], _TOKENS[tokens.dtype], temperature)
+    except _BEYOND as e:
+        raise ValueError(f"an argument of linear_logprobs is beyond its type: {e}") from None
+    status = lib.xsm_linear_logprobs(args, stream)
+    if status:
+        _check(status)
+    return LinearLogprobs(logprob, lse)
+
+
+def linear_logprobs_grad(hidden, weight, tokens, result, grad_logprob=None, grad_lse=None, temperature=1.0, need=(True, True)):
+    """The gradients (d_hidden, d_weight), in their type, of sum(grad_logprob * logprob) + sum(grad_lse * lse) of what linear_logprobs returned as `result` for the
+    same hidden, weight, tokens and temperature.  grad_*: float32 [rows]; each may be missing.  need: which of the two are wanted; the other is None.  The
+    logits are computed again, at most 256 MiB of their gradients are in memory at a time.  There are no second derivatives: tensors that want a gradient are
+    refused unless torch.no_grad() says that it is not needed."""
+    _no_gradient("linear_logprobs_grad", hidden, weight, result[1], grad_logprob, grad_lse)
+    device, dtype, rows, d, ld, w_ld = _check_linear(hidden, weight, tokens)
+    lse = result[1]
+    if lse.shape != (rows,) or lse.dtype is not torch.float32 or lse.get_device() != device or rows > 1 and lse.stride(0) != 1:
+        raise ValueError("result must be what linear_logprobs returned for these hidden states")
+    gl, gl_ld = _row_grad(grad_logprob, rows, device, "grad_logprob")
+    gs, gs_ld = _row_grad(grad_lse, rows, device, "grad_lse")
+    lib, where, vocab, stream = binding.load(), hidden.device, weight.shape[0], _raw_stream(device)
+    d_hidden = _empty((rows, d), (d, 1), dtype=dtype, device=where) if need[0] else None
+    d_weight = _empty((vocab, d), (d, 1), dtype=dtype, device=where) if need[1] else None
+    n = lib.xsm_linear_logprobs_grad_workspace(rows, vocab, d)
+    ws = _empty((n,), (1,), dtype=torch.uint8, device=where)
+    try:
+        args = _LINEAR_GRAD.pack(hidden.data_ptr(), weight.data_ptr(), tokens.data_ptr(), lse.data_ptr(), gl, gs, 0 if d_hidden is None else d_hidden.data_ptr(),
+                                 0 if d_weight is None else d_weight.data_ptr(), ws.data_ptr(), _status(device, stream), ld, w_ld, tokens.stride(0), gl_ld, gs_ld,
+                                 d, d, n, rows, vocab, d, _DTYPES[dtype], _TOKENS[tokens.dtype], temperature)
+    except _BEYOND as e:
+        raise ValueError(f"an argument of linear_logprobs_grad is beyond its type: {e}") from None
+    status = lib.xsm_linear_logprobs_grad(args, stream)
+    if status:
+        _check(status)
+    return d_hidden, d_weight
+
+
+class _LinearLogprobs(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, hidden, weight, tokens, temperature):
+        r = _linear_forward(hidden, weight, tokens, temperature)
+        ctx.save_for_backward(hidden, weight, tokens, r.lse)
+        ctx.temperature = temperature
+        ctx.set_materialize_grads(False)
+        return tuple(r)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, g_logprob, g_lse):
+        hidden, weight, tokens, lse = ctx.saved_tensors
+        need = ctx.needs_input_grad[:2]
+        if g_logprob is None and g_lse is None:
+            return None, None, None, None
+        return *linear_logprobs_grad(hidden, weight, tokens, (None, lse), g_logprob, g_lse, ctx.temperature, need), None, None
+
+
+def linear_logprobs(hidden, weight, tokens, temperature: float = 1.0) -> LinearLogprobs:
+    """Scores tokens [rows] (int32 or int64; one outside the vocabulary is none, and scores 0) under softmax(hidden weight^T / temperature) without keeping the
+    logits: (logprob, lse) float32 [rows].  hidden [rows, d] and weight [vocab, d] of bf16 or fp16, d a multiple of 8, rows 16-byte aligned.  Differentiable by
+    both, once and backwards."""
+    if forward_ad._current_level >= 0:
+        _no_tangents(hidden, weight)
+    if _grad_enabled() and (hidden.requires_grad or weight.requires_grad):
+        return LinearLogprobs(*_LinearLogprobs.apply(hidden, weight, tokens, temperature))
+    return _linear_forward(hidden, weight, tokens, temperature)
+
+
+def _check_gated(x, w_gate, w_up, activation):
+    device, dtype = _need_products(x, "x")
+    if x.dim() < 1 or w_gate.dim() != 2 or w_gate.shape != w_up.shape:
+        raise ValueError("x must be [..., d], w_gate and w_up [ff, d]")
+    d, ff = x.shape[-1], w_gate.shape[0]
+    if d < 8 or d % 8 or ff < 1:
+        raise ValueError("the width of x must be a positive multiple of 8, and w_gate and w_up must have rows")
+    if activation not in _ACTIVATIONS:
+        raise ValueError(f"activation must be one of {', '.join(_ACTIVATIONS)}, not {activation!r}")
+    flat = x if x.dim() == 2 else x.reshape(-1, d)
+    return device, dtype, flat, flat.shape[0], ff, d, _rows(flat, "x", device, dtype), _rows(w_gate, "w_gate", device, dtype, d), _rows(w_up, "w_up", device, dtype, d)
+
+
+def _gated_forward(x, w_gate, w_up, activation):
+    device, dtype, flat, rows, ff, d, ld, g_ld, u_ld = _check_gated(x, w_gate, w_up, activation)
+    stream = _raw_stream(device)
+    out = torch.empty((*x.shape[:-1], ff), dtype=dtype, device=x.device)
+    try:
+        args = _GATED.pack(flat.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), out.data_ptr(), _status(device, stream), ld, g_ld, u_ld, ff, rows, ff, d, _DTYPES[dtype],
+                           _ACTIVATIONS[activation])
+    except _BEYOND as e:
+        raise ValueError(f"an argument of gated_feed_forward is beyond its type: {e}") from None
+    status = binding.load().xsm_gated_ff(args, stream)
+    if status:
+        _check(status)
+    return out
+
+
+def gated_feed_forward_grad(x, w_gate, w_up, grad, activation: str = "silu", need=(True, True, True)):
+    """The gradients (d_x, d_w_gate, d_w_up), in their type, of sum(grad * out) of what gated_feed_forward returned for the same arguments.  grad: like out,
+    neighbouring elements in a row.  need: which are wanted (the last two go together); the others are None.  There are no second derivatives: tensors that want a
+    gradient are refused unless torch.no_grad() says that it is not needed."""
+    _no_gradient("gated_feed_forward_grad", x, w_gate, w_up, grad)
+    device, dtype, flat, rows, ff, d, ld, g_ld, u_ld = _check_gated(x, w_gate, w_up, activation)
+    if grad.shape != (*x.shape[:-1], ff) or grad.dtype is not dtype or grad.get_device() != device:
+        raise ValueError(f"grad must be {[*x.shape[:-1], ff]} of {dtype} on cuda:{device}")
+    g = grad if grad.dim() == 2 else grad.reshape(-1, ff)
+    if ff > 1 and rows and g.stride(1) != 1:
+        raise ValueError("the elements of a row of grad must be neighbours")
+    lib, where, stream = binding.load(), x.device, _raw_stream(device)
+    d_x = torch.empty(x.shape, dtype=dtype, device=where) if need[0] else None
+    d_gate = d_up = None
+    if need[1] or need[2]:
+        d_gate, d_up = (_empty((ff, d), (d, 1), dtype=dtype, device=where) for _ in range(2))
+    n = lib.xsm_gated_ff_grad_workspace(rows, ff, d)
+    ws = _empty((n,), (1,), dtype=torch.uint8, device=where)
+    try:
+        args = _GATED_GRAD.pack(flat.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), g.data_ptr(), 0 if d_x is None else d_x.data_ptr(), 0 if d_gate is None else d_gate.data_ptr(),
+                                0 if d_up is None else d_up.data_ptr(), ws.data_ptr(), _status(device, stream), ld, g_ld, u_ld, g.stride(0), d, d, n, rows, ff, d, _DTYPES[dtype],
+                                _ACTIVATIONS[activation])
+    except _BEYOND as e:
+        raise ValueError(f"an argument of gated_feed_forward_grad is beyond its type: {e}") from None
+    status = lib.xsm_gated_ff_grad(args, stream)
+    if status:
+        _check(status)
+    return d_x, d_gate if need[1] else None, d_up if need[2] else None
+
+
+class _GatedFeedForward(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, w_gate, w_up, activation):
+        ctx.save_for_backward(x, w_gate, w_up)
+        ctx.activation = activation
+        return _gated_forward(x, w_gate, w_up, activation)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, g):
+        x, w_gate, w_up = ctx.saved_tensors
+        if g.stride(-1) != 1 or g.dim() > 2:
+            g = g.contiguous()
+        return *gated_feed_forward_grad(x, w_gate, w_up, g, ctx.activation, ctx.needs_input_grad[:3]), None
+
+
+def gated_feed_forward(x, w_gate, w_up, activation: str = "silu"):
+    """act(x w_gate^T) * (x w_up^T), [..., ff]: both projections, the activation ("silu" or "gelu") and the product in one kernel.  x [..., d], w_gate and w_up [ff, d]
+    of bf16 or fp16, d a multiple of 8, rows 16-byte aligned; gate and up are held in fp32, the output is rounded once.  Differentiable by all three, once and
+    backwards; nothing but the arguments is kept for that."""
+    if forward_ad._current_level >= 0:
+        _no_tangents(x, w_gate, w_up)
+    if _grad_enabled() and (x.requires_grad or w_gate.requires_grad or w_up.requires_grad):
+        return _GatedFeedForward.apply(x, w_gate, w_up, activation)
+    return _gated_forward(x, w_gate, w_up, activation)
+
+
+# --------------------------------------------------------------------------------------- norms of heads with the rotation
+
+def _norm_layout(q, k, q_gain, k_gain, rope, positions):
+    """(device, type, type of the gains, batch, m, heads, kv heads, d_head, positions, half of the rotated) of arguments that go together."""
+    x, gain = (q, q_gain) if q is not None else (k, k_gain)
+    if x is None or (q is None) != (q_gain is None) or (k is None) != (k_gain is None):
+        raise ValueError("q and q_gain go together, k and k_gain too, and one of the pairs must be there")
+    device = x.get_device()
+    if device < 0 or device != _current_device():
+        _need_here(x)
+    if x.dim() != 4 or x.dtype not in _DTYPES:
+        raise ValueError("q and k must be [batch, m, heads, d_head] of fp32, bf16 or fp16")
+    batch, m, _, d = x.shape
+    for t, g in ((q, q_gain), (k, k_gain)):
+        if t is None:
+            continue
+        if t.dim() != 4 or t.shape[0] != batch or t.shape[1] != m or t.shape[3] != d or t.dtype is not x.dtype or t.get_device() != device or t.stride(3) != 1:
+            raise ValueError("q and k must have the same batch, tokens, d_head, type and device, and neighbouring elements of a head")
+        _need_gain(g, d, device, gain.dtype)
+    half = n = 0
+    if rope is not None:
+        if rope.dtype is not torch.float32 or rope.dim() != 3 or rope.shape[2] != 2 or not rope.is_contiguous() or rope.get_device() != device:
+            raise ValueError(f"rope must be contiguous float32 [positions, dims / 2, 2] on cuda:{device}")
+        n, half, _ = rope.shape
+    if positions is not None and (positions.shape != (batch, m) or positions.dtype is not torch.int32 or not positions.is_contiguous() or positions.get_device() != device):
+        raise ValueError(f"positions must be contiguous int32 [{batch}, {m}] on cuda:{device}")
+    return device, x.dtype, gain.dtype, batch, m, 0 if q is None else q.shape[2], 0 if k is None else k.shape[2], d, n, half
+
+
+def _address(t):
+    return 0 if t is None else t.data_ptr()
+
+
+def _strides(t):
+    return (0, 0, 0) if t is None else t.stride()[:3]
+
+
+def _norm_forward(q, k, q_gain, k_gain, rope, positions, eps, interleaved):
+    device, dtype, gain_dtype, batch, m, heads, kv_heads, d, n, half = _norm_layout(q, k, q_gain, k_gain, rope, positions)
+    q_out, k_out = (None if t is None else torch.empty(t.shape, dtype=dtype, device=t.device) for t in (q, k))
+    try:
+        args = _NORM.pack(_address(q), _address(k), _address(q_out), _address(k_out), _address(q_gain), _address(k_gain), _address(positions), _address(rope),
+                          *_strides(q), *_strides(k), *_strides(q_out), *_strides(k_out), batch, m, heads, kv_heads, d, _DTYPES[dtype], _DTYPES[gain_dtype], n, 2 * half,
+                          interleaved, eps)
+    except _BEYOND as e:
+        raise ValueError(f"an argument of norm_rotate is beyond its type: {e}") from None
+    status = binding.load().xsm_norm_rotate(args, _raw_stream(device))
+    if status:
+        _check(status)
+    return q_out, k_out
+
+
+def norm_rotate_grad(q, k, q_gain, k_gain, grad_q, grad_k, rope=None, positions=None, eps: float = 1e-6, interleaved: bool = False):
+    """The gradients (d_q, d_k, d_q_gain, d_k_gain), in their types, of sum(grad_q * q') + sum(grad_k * k') of what norm_rotate returned for the same arguments; None
+    beside what was not there.  There are no second derivatives: tensors that want a gradient are refused unless torch.no_grad() says that it is not
+    needed."""
+    _no_gradient("norm_rotate_grad", q, k, q_gain, k_gain, rope, grad_q, grad_k)
+    device, dtype, gain_dtype, batch, m, heads, kv_heads, d, n, half = _norm_layout(q, k, q_gain, k_gain, rope, positions)
+    for t, g in ((q, grad_q), (k, grad_k)):
+        if (t is None) != (g is None) or t is not None and (g.shape != t.shape or g.dtype is not dtype or g.get_device() != device or g.stride(3) != 1):
+            raise ValueError("grad_q and grad_k must be like q and k, with neighbouring elements of a head")
+    d_q, d_k = (None if t is None else torch.empty(t.shape, dtype=dtype, device=t.device) for t in (q, k))
+    d_q_gain, d_k_gain = (None if t is None else torch.empty(d, dtype=gain_dtype, device=t.device) for t in (q_gain, k_gain))
+    lib = binding.load()
+    size = lib.xsm_norm_rotate_grad_workspace(d)
+    ws = _empty((size,), (1,), dtype=torch.uint8, device=q_gain.device if q_gain is not None else k_gain.device)
+    try:
+        args = _NORM_GRAD.pack(_address(q), _address(k), _address(q_gain), _address(k_gain), _address(positions), _address(rope), _address(grad_q), _address(grad_k),
+                               _address(d_q), _address(d_k), _address(d_q_gain), _address(d_k_gain), ws.data_ptr(), *_strides(q), *_strides(k), *_strides(grad_q),
+                               *_strides(grad_k), *_strides(d_q), *_strides(d_k), size, batch, m, heads, kv_heads, d, _DTYPES[dtype], _DTYPES[gain_dtype], n, 2 * half,
+                               interleaved, eps)
+    except _BEYOND as e:
+        raise ValueError(f"an argument of norm_rotate_grad is beyond its type: {e}") from None
+    status = lib.xsm_norm_rotate_grad(args, _raw_stream(device))
+    if status:
+        _check(status)
+    return d_q, d_k, d_q_gain, d_k_gain
+
+
+class _NormRotate(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, q_gain, k_gain, rope, positions, eps, interleaved):
+        ctx.save_for_backward(q, k, q_gain, k_gain, rope, positions)
+        ctx.more = eps, interleaved
+        ctx.set_materialize_grads(False)
+        return _norm_forward(q, k, q_gain, k_gain, rope, positions, eps, interleaved)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, g_q, g_k):
+        q, k, q_gain, k_gain, rope, positions = ctx.saved_tensors
+        if g_q is None and q is not None or g_k is None and k is not None:        # (what nothing came back for has no gradient)
+            q, q_gain = (None, None) if g_q is None else (q, q_gain)
+            k, k_gain = (None, None) if g_k is None else (k, k_gain)
+        if q is None and k is None:
+            return (None,) * 8
+        g_q, g_k = (g if g is None or g.stride(3) == 1 else g.contiguous() for g in (g_q, g_k))
+        d = norm_rotate_grad(q, k, q_gain, k_gain, g_q, g_k, rope, positions, *ctx.more)
+        return *(x if need else None for x, need in zip(d, ctx.needs_input_grad)), None, None, None, None
+
+
+def norm_rotate(q, k, q_gain, k_gain, rope=None, positions=None, eps: float = 1e-6, interleaved: bool = False):
+    """Norms of queries and keys for each head with the rotation of the positions in the same pass: (q', k') with y = R (gain x / sqrt(mean(x^2) + eps)) over every head,
+    q [batch, m, n_heads, d_head], k [batch, m, n_kv_heads, d_head] of fp32, bf16 or fp16 with neighbouring elements of a head, gains [d_head].  Token j of a sequence
+    is at positions[sequence, j] (int32; without positions at j); rope (see rope_table) may be missing: no rotation.  Tokens at positions that the rope does not have
+    come out as zero.  q and q_gain, or k and k_gain, may be None.  Differentiable by q, k and the gains, once and backwards."""
+    if forward_ad._current_level >= 0:
+        _no_tangents(q, k, q_gain, k_gain, rope)
+    if _grad_enabled():
+        if rope is not None and rope.requires_grad:
+            raise ValueError("norm_rotate has no gradient by rope")
+        for t in (q, k, q_gain, k_gain):
+            if t is not None and t.requires_grad:
+                return _NormRotate.apply(q, k, q_gain, k_gain, rope, positions, eps, interleaved)
+    return _norm_forward(q, k, q_gain, k_gain, rope, positions, eps, interleaved)
