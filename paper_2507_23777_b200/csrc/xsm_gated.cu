@@ -8,22 +8,19 @@
 namespace xsm {
 
 static size_t up(size_t n) { return (n + 255) & ~(size_t)255; }
-static long long tiles_of(bool wide, long long m, long long n) { return wide ? ((m + 255) / 256) * ((n + 255) / 256) : ((m + 127) / 128) * ((n + 63) / 64); }
-static bool wide_tiles(long long m, long long n) { return m > 128 && n > 64; }
-
 struct GatedGradPlan {
-    bool wide, wide_x, wide_w;
+    ProductCut cut, cut_x, cut_w;
     int ld, splits_x, splits_w;
     size_t amax, d_gate, d_up, part_x, part_w, bytes;
 };
 static GatedGradPlan plan_gated_grad(int rows, int ff, int d) {
     GatedGradPlan p;
-    p.wide = wide_tiles(rows, ff);
-    p.wide_x = wide_tiles(rows, d);
-    p.wide_w = wide_tiles(ff, d);
+    p.cut = product_cut(PR_GATED_GRAD, rows, ff);
+    p.cut_x = product_cut(PR_OUT, rows, d);
+    p.cut_w = product_cut(PR_OUT, ff, d);
     p.ld = (ff + 7) / 8 * 8;
-    p.splits_x = product_splits(tiles_of(p.wide_x, rows, d), 2 * ((ff + 63) / 64), p.wide_x);
-    p.splits_w = product_splits(2 * tiles_of(p.wide_w, ff, d), (rows + 63) / 64, p.wide_w);
+    p.splits_x = product_splits(p.cut_x.tiles(rows, d, false), 2 * ((ff + 63) / 64), p.cut_x.wide);
+    p.splits_w = product_splits(2 * p.cut_w.tiles(ff, d, false), (rows + 63) / 64, p.cut_w.wide);
     p.amax = 0;
     p.d_gate = up(kAmaxBlocks * 4);
     p.d_up = p.d_gate + up((size_t)rows * p.ld * 2);
@@ -58,7 +55,7 @@ xsm_status xsm_gated_ff(const xsm_gated_ff_args *a, void *cuda_stream) {
     A.status = a->status; A.activation = a->activation;
     A.out[0] = a->out; A.out_ld = a->out_stride;
     const Operand x[2] = {{a->x, a->rows, a->d, a->x_stride}, {}}, w[2] = {{a->w_gate, a->ff, a->d, a->w_gate_stride}, {a->w_up, a->ff, a->d, a->w_up_stride}};
-    return launched(launch_product(PR_GATED, a->dtype, wide_tiles(a->rows, a->ff), A, x, w, 1, (cudaStream_t)cuda_stream));
+    return launched(launch_product(PR_GATED, a->dtype, product_cut(PR_GATED, a->rows, a->ff), A, x, w, 1, (cudaStream_t)cuda_stream));
 }
 
 size_t xsm_gated_ff_grad_workspace(int rows, int ff, int d) { return rows < 1 || ff < 1 || d < 1 ? 0 : plan_gated_grad(rows, ff, d).bytes; }
@@ -97,21 +94,21 @@ xsm_status xsm_gated_ff_grad(const xsm_gated_ff_grad_args *a, void *cuda_stream)
     }
     const Operand x[2] = {{a->x, a->rows, a->d, a->x_stride}, {}}, w[2] = {{a->w_gate, a->ff, a->d, a->w_gate_stride}, {a->w_up, a->ff, a->d, a->w_up_stride}};
     const Operand g[2] = {{ws + p.d_gate, a->rows, a->ff, p.ld}, {ws + p.d_up, a->rows, a->ff, p.ld}};
-    if (e == cudaSuccess) e = launch_product(PR_GATED_GRAD, a->dtype, p.wide, A, x, w, 1, st);
+    if (e == cudaSuccess) e = launch_product(PR_GATED_GRAD, a->dtype, p.cut, A, x, w, 1, st);
     ProductArgs G = {};
-    G.status = a->status; G.amax = A.amax; G.amax_to = A.amax_to; G.b_mn = 1;
+    G.status = a->status; G.amax = A.amax; G.amax_to = A.amax_to;
     if (a->d_x && e == cudaSuccess) {
         G.m = a->rows; G.n = a->d; G.jobs = 1; G.splits = p.splits_x;
         G.out[0] = a->d_x; G.out_ld = a->d_x_stride;
         G.partial = p.splits_x > 1 ? (float *)(ws + p.part_x) : nullptr;
-        e = launch_product(PR_OUT, a->dtype, p.wide_x, G, g, w, 2, st);
+        e = launch_product(PR_OUT, a->dtype, p.cut_x, G, g, w, 2, st);
         if (G.partial && e == cudaSuccess) e = launch_join(G, a->dtype, st);
     }
     if (a->d_w_gate && e == cudaSuccess) {
-        G.m = a->ff; G.n = a->d; G.jobs = 2; G.splits = p.splits_w; G.a_mn = 1;
+        G.m = a->ff; G.n = a->d; G.jobs = 2; G.splits = p.splits_w;
         G.out[0] = a->d_w_gate; G.out[1] = a->d_w_up; G.out_ld = a->d_w_stride;
         G.partial = p.splits_w > 1 ? (float *)(ws + p.part_w) : nullptr;
-        e = launch_product(PR_OUT, a->dtype, p.wide_w, G, g, x, 1, st);
+        e = launch_product(PR_OUT_ROWS, a->dtype, p.cut_w, G, g, x, 1, st);
         if (G.partial && e == cudaSuccess) e = launch_join(G, a->dtype, st);
     }
     return launched(e);

@@ -12,13 +12,13 @@ namespace xsm {
 
 constexpr long long kPieceBytes = 256ll << 20;      // of a piece's gradients by the logits
 
-// 32 rows a block; thread (row, y) joins parts y, y + 8, ...
+// Eight rows a block; thread (row, y) joins parts y, y + 32, ...  (32 rows a block, eight threads a row: 145 us for 96 rows of 4096 parts.)
 __global__ void __launch_bounds__(256) join_stats_kernel(const float2 *parts, const float *token_z, const void *tokens, long long token_ld, int token_bytes, int rows, int vocab,
                                                          int n, float *logprob, float *lse) {
     chain_go();
     chain_wait();
-    __shared__ float2 s[8][32];
-    const int x = threadIdx.x & 31, y = threadIdx.x >> 5, row = blockIdx.x * 32 + x;
+    __shared__ float2 s[32][9];
+    const int x = threadIdx.x & 7, y = threadIdx.x >> 3, row = blockIdx.x * 8 + x;
     float m = -INFINITY, sum = 0.f;
     auto take = [&](float2 p) {
         const float was = m;
@@ -28,34 +28,42 @@ __global__ void __launch_bounds__(256) join_stats_kernel(const float2 *parts, co
     };
     if (row < rows) {
 #pragma unroll 4
-        for (int i = y; i < n; i += 8) take(parts[(long long)i * rows + row]);
+        for (int i = y; i < n; i += 32) take(parts[(long long)i * rows + row]);
     }
     s[y][x] = make_float2(m, sum);
     __syncthreads();
-    if (y || row >= rows) return;
-    for (int i = 1; i < 8; ++i) take(s[i][x]);
+    // (a warp takes a row: lane = y)
+    const int r = threadIdx.x >> 5, lane = threadIdx.x & 31, at = blockIdx.x * 8 + r;
+    if (at >= rows) return;
+    m = s[lane][r].x;
+    sum = s[lane][r].y;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) take(make_float2(__shfl_xor_sync(0xffffffffu, m, o), __shfl_xor_sync(0xffffffffu, sum, o)));
+    if (lane) return;
     const float l = m == -INFINITY && sum == 0.f ? -INFINITY : (m + log2f(sum)) * 0.69314718056f;
-    const long long t = token_bytes == 8 ? reinterpret_cast<const long long *>(tokens)[row * token_ld] : (long long)reinterpret_cast<const int *>(tokens)[row * token_ld];
-    lse[row] = l;
-    logprob[row] = t < 0 || t >= vocab ? 0.f : l == -INFINITY ? -INFINITY : token_z[row] - l;
+    const long long t = token_bytes == 8 ? reinterpret_cast<const long long *>(tokens)[at * token_ld] : (long long)reinterpret_cast<const int *>(tokens)[at * token_ld];
+    lse[at] = l;
+    logprob[at] = t < 0 || t >= vocab ? 0.f : l == -INFINITY ? -INFINITY : token_z[at] - l;
 }
 
-struct LinearPlan { bool wide; int parts; };
+// One tile of rows: a CTA joins what its tiles find in its registers, and there are two parts for each CTA.
+struct LinearPlan { ProductCut cut; bool carry; int parts; };
 static LinearPlan plan_linear(int rows, int vocab) {
     LinearPlan p;
-    p.wide = rows > 128;
-    p.parts = 2 * ((vocab + (p.wide ? 255 : 63)) / (p.wide ? 256 : 64));
+    p.cut = product_cut(PR_STATS, rows, vocab);
+    p.carry = rows <= p.cut.tm();
+    const long long tiles = p.cut.tiles(p.cut.tm(), vocab, false);
+    p.parts = 2 * (p.carry ? product_ctas(tiles, p.cut.wide) / (p.cut.wide ? 2 : 1) : (int)tiles);
     return p;
 }
 
 static size_t up(size_t n) { return (n + 255) & ~(size_t)255; }
 
 struct LinearGradPlan {
-    bool wide_z, wide_h, wide_w;
+    ProductCut cut_z, cut_h, cut_w;
     int piece, pieces, splits_h, splits_w;
     size_t amax, dz, part_h, part_w, bytes;      // offsets in the workspace
 };
-static bool wide_tiles(long long m, long long n) { return m > 128 && n > 64; }
 static LinearGradPlan plan_linear_grad(int rows, int vocab, int d) {
     LinearGradPlan p;
     long long piece = kPieceBytes / (2ll * rows) / 256 * 256;
@@ -64,14 +72,13 @@ static LinearGradPlan plan_linear_grad(int rows, int vocab, int d) {
     p.piece = (int)(((vocab + p.pieces - 1) / p.pieces + 255) / 256 * 256);
     if (p.piece > vocab) p.piece = (vocab + 63) / 64 * 64;
     p.pieces = (vocab + p.piece - 1) / p.piece;
-    p.wide_z = wide_tiles(rows, p.piece);
-    p.wide_h = wide_tiles(rows, d);
-    p.wide_w = wide_tiles(p.piece, d);
-    auto tiles = [](bool wide, long long m, long long n) { return wide ? ((m + 255) / 256) * ((n + 255) / 256) : ((m + 127) / 128) * ((n + 63) / 64); };
-    p.splits_h = product_splits(tiles(p.wide_h, rows, d), p.piece / 64, p.wide_h);
+    p.cut_z = product_cut(PR_DLOGITS, rows, p.piece);
+    p.cut_h = product_cut(PR_OUT, rows, d);
+    p.cut_w = product_cut(PR_OUT, p.piece, d);
+    p.splits_h = product_splits(p.cut_h.tiles(rows, d, false), p.piece / 64, p.cut_h.wide);
     const int last = vocab - (p.pieces - 1) * p.piece;            // (the shortest piece has to have a block for every part)
     if (p.splits_h > (last + 63) / 64) p.splits_h = (last + 63) / 64;
-    p.splits_w = product_splits(tiles(p.wide_w, p.piece, d), (rows + 63) / 64, p.wide_w);
+    p.splits_w = product_splits(p.cut_w.tiles(p.piece, d, false), (rows + 63) / 64, p.cut_w.wide);
     p.amax = 0;
     p.dz = up(kAmaxBlocks * 4);
     p.part_h = p.dz + up((size_t)rows * p.piece * 2);
@@ -117,12 +124,13 @@ xsm_status xsm_linear_logprobs(const xsm_linear_logprobs_args *a, void *cuda_str
     A.inv_t = 1.f / a->temperature;
     A.c = (float)(1.4426950408889634 / a->temperature);
     A.parts = (float2 *)a->workspace;
+    A.carry = p.carry;
     A.token_z = (float *)((char *)a->workspace + up((size_t)p.parts * a->rows * 8));
     const Operand h[2] = {{a->hidden, a->rows, a->d, a->hidden_stride}, {}}, w[2] = {{a->weight, a->vocab, a->d, a->weight_stride}, {}};
     const cudaStream_t st = (cudaStream_t)cuda_stream;
-    cudaError_t e = launch_product(PR_STATS, a->dtype, p.wide, A, h, w, 1, st);
+    cudaError_t e = launch_product(PR_STATS, a->dtype, p.cut, A, h, w, 1, st);
     if (e == cudaSuccess)
-        e = launch_early(join_stats_kernel, dim3((unsigned)((a->rows + 31) / 32)), dim3(256), 0, st, (const float2 *)A.parts, (const float *)A.token_z, a->tokens, (long long)a->token_stride,
+        e = launch_early(join_stats_kernel, dim3((unsigned)((a->rows + 7) / 8)), dim3(256), 0, st, (const float2 *)A.parts, (const float *)A.token_z, a->tokens, (long long)a->token_stride,
                          (int)a->token_bytes, (int)a->rows, (int)a->vocab, (int)p.parts, a->logprob, a->lse);
     return launched(e);
 }
@@ -169,24 +177,24 @@ xsm_status xsm_linear_logprobs_grad(const xsm_linear_logprobs_grad_args *a, void
         ProductArgs A = Z;
         A.n = v; A.vocab0 = v0;
         A.out[0] = ws + p.dz; A.out_ld = p.piece;
-        e = launch_product(PR_DLOGITS, a->dtype, p.wide_z, A, hidden, w, 1, st);
+        e = launch_product(PR_DLOGITS, a->dtype, p.cut_z, A, hidden, w, 1, st);
         ProductArgs G = {};
         G.jobs = 1;
         G.status = a->status; G.amax = Z.amax; G.amax_to = Z.amax_to;
         if (a->d_hidden && e == cudaSuccess) {
-            G.m = a->rows; G.n = a->d; G.splits = p.splits_h; G.a_mn = 0; G.b_mn = 1;
+            G.m = a->rows; G.n = a->d; G.splits = p.splits_h;
             G.out[0] = a->d_hidden; G.out_ld = a->d_hidden_stride;
             G.partial = p.splits_h > 1 || p.pieces > 1 ? (float *)(ws + p.part_h) : nullptr;
             G.add = i > 0;
-            e = launch_product(PR_OUT, a->dtype, p.wide_h, G, dz, w, 1, st);
+            e = launch_product(PR_OUT, a->dtype, p.cut_h, G, dz, w, 1, st);
             if (G.partial && i == p.pieces - 1 && e == cudaSuccess) e = launch_join(G, a->dtype, st);
         }
         if (a->d_weight && e == cudaSuccess) {
-            G.m = v; G.n = a->d; G.splits = p.splits_w; G.a_mn = 1; G.b_mn = 1;
+            G.m = v; G.n = a->d; G.splits = p.splits_w;
             G.out[0] = (char *)a->d_weight + (long long)v0 * a->d_weight_stride * 2; G.out_ld = a->d_weight_stride;
             G.partial = p.splits_w > 1 ? (float *)(ws + p.part_w) : nullptr;
             G.add = 0;
-            e = launch_product(PR_OUT, a->dtype, p.wide_w, G, dz, hidden, 1, st);
+            e = launch_product(PR_OUT_ROWS, a->dtype, p.cut_w, G, dz, hidden, 1, st);
             if (G.partial && e == cudaSuccess) e = launch_join(G, a->dtype, st);
         }
     }

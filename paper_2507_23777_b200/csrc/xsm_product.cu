@@ -18,9 +18,7 @@ constexpr int kProductThreads = 64 + 32 * kEpiWarps;
 constexpr int kABytes = 128 * 128;              // of a stage and a CTA: 128 rows of A, 64 elements of the summed axis
 constexpr int kRingBytes = 192 * 1024;
 
-template <int CG, int BN> struct Cut {
-    static constexpr int stage = kABytes + BN / CG * 128, stages = kRingBytes / stage, tm = 128 * CG;
-};
+constexpr int kMaxStages = 24;
 
 // ------------------------------------------------------------------------------------------- instructions
 
@@ -79,16 +77,24 @@ template <int N> __device__ __forceinline__ void tmem_ld(uint32_t (&v)[N], uint3
 
 // ------------------------------------------------------------------------------------------------- numbers
 
-// act(g) and its derivative
-__device__ __forceinline__ void activate(int kind, float g, float &a, float &da) {
-    if (kind == ACT_SILU) {
-        const float s = __fdividef(1.f, 1.f + ex2(-g * kLog2e));
+__device__ __forceinline__ float rcp(float x) {
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+// act(g) and its derivative.  gelu: g Phi(g), Phi by the rational approximation 7.1.26 of Abramowitz and Stegun (erfc(x) = t p(t) exp(-x^2), t = 1 / (1 + 0.3275911 x); off by
+// 1.5e-7 at most, and by less where the exponential is small), whose exponential is the derivative's too.
+template <int KIND> __device__ __forceinline__ void activate(float g, float &a, float &da) {
+    if constexpr (KIND == ACT_SILU) {
+        const float s = rcp(1.f + ex2(-g * kLog2e));
         a = g * s;
-        da = s * (1.f + g * (1.f - s));
+        da = fmaf(a, 1.f - s, s);
     } else {
-        const float c = 0.5f * erfcf(-0.70710678f * g);
+        const float e = ex2(-0.5f * kLog2e * g * g), t = rcp(fmaf(0.3275911f * 0.70710678f, fabsf(g), 1.f));
+        const float q = 0.5f * e * t * fmaf(fmaf(fmaf(fmaf(1.061405429f, t, -1.453152027f), t, 1.421413741f), t, -0.284496736f), t, 0.254829592f);
+        const float c = g < 0.f ? q : 1.f - q;
         a = g * c;
-        da = c + g * 0.39894228f * ex2(-0.5f * kLog2e * g * g);
+        da = fmaf(0.39894228f * g, e, c);
     }
 }
 
@@ -124,41 +130,120 @@ template <typename T, int N> __device__ __forceinline__ void store_row(T *row, i
     }
 }
 
-// -------------------------------------------------------------------------------------------------- kernel
+// ----------------------------------------------------------------------------------------------------- tiles
 
+// Tiles in groups of `group_m` tiles of rows; in a group the rows first, then the columns: the tiles that run at a time then share both operands'
+// panels (63 x 8 tiles of 8192 steps rows first: every column of tiles fetched all of A again from memory).
 struct Tile { int m, n, split, job, k0, k1; };
-__device__ __forceinline__ Tile tile_of(const ProductArgs &A, int t) {
+__device__ __forceinline__ Tile tile_of(const ProductArgs &A, unsigned t) {
     Tile r;
-    r.m = t % A.tiles_m;
-    t /= A.tiles_m;
-    r.n = t % A.tiles_n;
-    t /= A.tiles_n;
-    r.split = t % A.splits;
-    r.job = t / A.splits;
-    r.k0 = (int)((long long)A.kb * r.split / A.splits);
-    r.k1 = (int)((long long)A.kb * (r.split + 1) / A.splits);
+    const unsigned z = A.by_plane.of(t);
+    t -= z * A.by_plane.d;
+    const unsigned g = A.by_group.of(t);
+    t -= g * A.by_group.d;
+    const bool last = (int)(g + 1) * A.group_m > A.tiles_m;
+    r.n = (int)(last ? A.by_last_rows.of(t) : A.by_rows.of(t));
+    r.m = (int)(g * (unsigned)A.group_m + t - (unsigned)r.n * (last ? A.by_last_rows.d : A.by_rows.d));
+    r.job = (int)A.by_splits.of(z);
+    r.split = (int)(z - (unsigned)r.job * A.by_splits.d);
+    r.k0 = r.split * A.kb_each + min(r.split, A.kb_more);
+    r.k1 = r.k0 + A.kb_each + (r.split < A.kb_more);
     return r;
 }
 
+// ---------------------------------------------------------------------------------------- rows in shared memory
+
+// A warp's 32 rows of 128 bytes (16-byte pieces permuted as TMA's 128-byte swizzle does) on their way between a thread's own row and memory.
+__device__ __forceinline__ uint32_t piece_at(uint32_t buf, int row, int piece) { return buf + (uint32_t)(row * 128 + ((piece ^ (row & 7)) << 4)); }
+__device__ __forceinline__ void sts128(uint32_t addr, uint4 v) {
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" :: "r"(addr), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
+__device__ __forceinline__ uint4 lds128(uint32_t addr) {
+    uint4 v;
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
+    return v;
+}
+// the buffer's last store has been read
+__device__ __forceinline__ void rows_free(int lane) {
+    if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+    __syncwarp();
+}
+__device__ __forceinline__ void rows_store(const void *map, uint32_t buf, int x, int y, int z, bool add, bool some, int lane) {
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    __syncwarp();
+    if (some && lane == 0) {
+        if (add) asm volatile("cp.reduce.async.bulk.tensor.3d.global.shared::cta.add.tile.bulk_group [%0, {%1, %2, %3}], [%4];" :: "l"(map), "r"(x), "r"(y), "r"(z), "r"(buf) : "memory");
+        else asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%1, %2, %3}], [%4];" :: "l"(map), "r"(x), "r"(y), "r"(z), "r"(buf) : "memory");
+        asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+    }
+}
+// the same by the warp itself, for rows that are not aligned: elements [col, n) of rows [row0, m)
+template <typename T> __device__ __forceinline__ void rows_copy_out(T *out, long long ld, int row0, int m, int col, int n, uint32_t buf, int lane) {
+    __syncwarp();
+    const bool has0 = col + 2 * lane < n, has1 = col + 2 * lane + 1 < n;
+#pragma unroll 4
+    for (int r = 0; r < 32; ++r) {
+        if (row0 + r >= m) break;
+        uint32_t v;
+        asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v) : "r"(piece_at(buf, r, lane >> 2) + (uint32_t)(lane & 3) * 4) : "memory");
+        T e[2];
+        memcpy(e, &v, 4);
+        T *p = out + (row0 + r) * ld + col + 2 * lane;
+        if (has0) p[0] = e[0];
+        if (has1) p[1] = e[1];
+    }
+    __syncwarp();
+}
+// rows [row0, m), elements [col, n) of a matrix into the buffer, zeros elsewhere; to be waited for with rows_landed
+template <typename T> __device__ __forceinline__ void rows_fetch(const T *x, long long ld, int row0, int m, int col, int n, bool aligned, uint32_t buf, int lane) {
+    if (aligned) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int r = i * 4 + (lane >> 3), c = lane & 7, left = (n - col - c * 8) * 2, bytes = row0 + r < m ? max(0, min(16, left)) : 0;
+            const T *p = bytes ? x + (row0 + r) * ld + col + c * 8 : x;
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" :: "r"(piece_at(buf, r, c)), "l"(p), "r"(bytes) : "memory");
+        }
+    } else {
+        const bool has0 = col + 2 * lane < n, has1 = col + 2 * lane + 1 < n;
+#pragma unroll 8
+        for (int r = 0; r < 32; ++r) {
+            T e[2] = {rounded<T>(0.f), rounded<T>(0.f)};
+            const T *p = x + (row0 + r) * ld + col + 2 * lane;
+            if (row0 + r < m && has0) e[0] = p[0];
+            if (row0 + r < m && has1) e[1] = p[1];
+            uint32_t v;
+            memcpy(&v, e, 4);
+            asm volatile("st.shared.b32 [%0], %1;" :: "r"(piece_at(buf, r, lane >> 2) + (uint32_t)(lane & 3) * 4), "r"(v) : "memory");
+        }
+    }
+}
+__device__ __forceinline__ void rows_landed() {
+    asm volatile("cp.async.wait_all;" ::: "memory");
+    __syncwarp();
+}
+// thirty-two numbers rounded to T, or sixteen bytes' worth of fp32 each, into a row: pieces from `first` on
+template <typename T> __device__ __forceinline__ void put_row(uint32_t buf, int row, int first, const float (&x)[32]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        sts128(piece_at(buf, row, first + i), make_uint4(pack2<T>(x[8 * i], x[8 * i + 1]), pack2<T>(x[8 * i + 2], x[8 * i + 3]), pack2<T>(x[8 * i + 4], x[8 * i + 5]), pack2<T>(x[8 * i + 6], x[8 * i + 7])));
+}
+
+// -------------------------------------------------------------------------------------------------- kernel
+
 template <int CG, int BN, int EPI, typename T>
 __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __grid_constant__ ProductMaps M, const __grid_constant__ ProductArgs A) {
-    using C = Cut<CG, BN>;
-    constexpr int S = C::stages;
+    constexpr int TM = 128 * CG;
+    constexpr bool kGated = EPI == PR_GATED || EPI == PR_GATED_GRAD, kOut = EPI == PR_OUT || EPI == PR_OUT_ROWS;
+    constexpr bool kRowsA = EPI == PR_OUT_ROWS, kRowsB = kOut;        // operands whose rows run along the summed axis
     extern __shared__ char smem_raw[];
-    __shared__ __align__(8) uint64_t full[S], empty[S], sums_full[2], sums_empty[2], last;
+    __shared__ __align__(8) uint64_t full[kMaxStages], empty[kMaxStages], sums_full[2], sums_empty[2], last;
     __shared__ uint32_t tmem_slot;
     __shared__ volatile int dead;           // a wait of this CTA has run out
+    __shared__ int fills;                   // stages that were asked for
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int rank = CG == 2 ? (int)cluster_rank() : 0, first = blockIdx.x / CG, step = gridDim.x / CG;
     const uint32_t ring = (smem_u32(smem_raw) + 1023u) & ~1023u;
     chain_go();
-    if (tid == 0) {
-        for (int i = 0; i < S; ++i) { mbar_init(smem_u32(&full[i]), 1u); mbar_init(smem_u32(&empty[i]), 1u); }
-        for (int i = 0; i < 2; ++i) { mbar_init(smem_u32(&sums_full[i]), 1u); mbar_init(smem_u32(&sums_empty[i]), kEpiWarps * CG); }
-        mbar_init(smem_u32(&last), 1u);
-        dead = 0;
-        mbar_init_fence();
-    }
     if (warp == 1) {
         if constexpr (CG == 1) {
             asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" :: "r"(smem_u32(&tmem_slot)), "n"(2 * BN) : "memory");
@@ -167,6 +252,12 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
             asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" :: "r"(smem_u32(&tmem_slot)), "n"(2 * BN) : "memory");
             asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
         }
+    } else if (warp == 0) {        // (a barrier each: one thread takes 30 cycles for each of them)
+        if (lane < A.stages) { mbar_init(smem_u32(&full[lane]), 1u); mbar_init(smem_u32(&empty[lane]), 1u); }
+        if (lane < 2) { mbar_init(smem_u32(&sums_full[lane]), 1u); mbar_init(smem_u32(&sums_empty[lane]), kEpiWarps * CG); }
+        if (lane == 2) mbar_init(smem_u32(&last), 1u);
+        if (lane == 3) { dead = 0; fills = 0; }
+        mbar_init_fence();
     }
     tcgen05_before_sync();
     __syncthreads();
@@ -176,9 +267,9 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
     chain_wait();
 
     // false: the limit ran out, here or elsewhere in the CTA; the results are void
-    auto wait = [&](uint64_t &b, uint32_t parity) {
-        const uint32_t bar = smem_u32(&b);
-        for (unsigned i = 0; i <= A.tries; ++i) {
+    auto wait = [&](uint32_t bar, uint32_t parity) {
+        if (mbar_try_wait(bar, parity)) return true;
+        for (unsigned i = 0; i < A.tries; ++i) {
             if (mbar_try_wait(bar, parity)) return true;
             if ((i & 63u) == 63u && dead) return false;
         }
@@ -186,129 +277,132 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
         atomicExch(A.status, XSM_STATUS_TIMEOUT);
         return false;
     };
+    auto wait_warp = [&](uint32_t bar, uint32_t parity) {        // (all lanes or none)
+        return __all_sync(0xffffffffu, mbar_try_wait(bar, parity)) || __all_sync(0xffffffffu, wait(bar, parity));
+    };
+    const uint32_t full0 = smem_u32(full), empty0 = smem_u32(empty), sums_full0 = smem_u32(sums_full), sums_empty0 = smem_u32(sums_empty);
 
-    auto wait_warp = [&](uint64_t &b, uint32_t parity) { return __all_sync(0xffffffffu, wait(b, parity)) != 0; };        // (all lanes or none)
-
+    // The two loops below run once for 64 steps of the summed axis, 512 cycles of the tensor cores: what does not change stands outside, and nothing
+    // branches that need not.  (With divisions, an operand's orientation and the barriers' addresses worked out within, 550 cycles a turn.)
     if (warp == 0) {
-        if (elect_one()) {
-            int fills = 0;        // stages asked for
+        if (elect_one() && !A.starve) {
+            const uint32_t full_at = CG == 2 ? map_rank(full0, 0) : full0;
+            int n = 0, s = 0;
+            uint32_t par = 1u, sa = ring;
             bool ok = true;
-            int s = 0;
-            uint32_t par = 1u;
             for (int t = first; ok && t < A.tiles; t += step) {
-                const Tile w = tile_of(A, t);
-                const int m0 = w.m * C::tm + rank * 128, n0 = EPI == PR_GATED || EPI == PR_GATED_GRAD ? w.n * (BN / 2) : w.n * BN + rank * (BN / CG);
+                const Tile w = tile_of(A, (unsigned)t);
+                const int m0 = w.m * TM + rank * 128, n0 = kGated ? w.n * (BN / 2) : w.n * BN + rank * (BN / CG);
+                const int second = kOut && w.k0 >= A.kb0;
+                const CUtensorMap *ma = &M.a[kOut ? second + w.job : 0], *mb = &M.b[kGated && CG == 2 ? rank : second];
+                int at = (w.k0 - (second ? A.kb0 : 0)) * 64;
                 for (int k = w.k0; k < w.k1; ++k) {
-                    if (!(ok = wait(empty[s], par))) break;
-                    if (!A.starve) {
-                        const uint32_t f = CG == 2 ? map_rank(smem_u32(&full[s]), 0) : smem_u32(&full[s]);
-                        if (rank == 0) mbar_arrive_expect_tx(smem_u32(&full[s]), A.stage_tx);
-                        const uint32_t sa = ring + (uint32_t)(s * C::stage), sb = sa + kABytes;
-                        const int pair = k >= A.kb0, at = (k - (pair ? A.kb0 : 0)) * 64;
-                        const void *ma = &M.a[pair + w.job], *mb = &M.b[pair];
-                        if (A.a_mn) {
-                            tma_2d<CG>(sa, ma, m0, at, f);
-                            tma_2d<CG>(sa + 8192, ma, m0 + 64, at, f);
-                        } else {
-                            tma_2d<CG>(sa, ma, at, m0, f);
-                        }
-                        if constexpr (EPI == PR_GATED || EPI == PR_GATED_GRAD) {
-                            if constexpr (CG == 2) {
-                                tma_2d<CG>(sb, &M.b[rank], at, n0, f);
-                            } else {
-                                tma_2d<CG>(sb, &M.b[0], at, n0, f);
-                                tma_2d<CG>(sb + BN / 2 * 128, &M.b[1], at, n0, f);
-                            }
-                        } else if (A.b_mn) {
-#pragma unroll
-                            for (int i = 0; i < BN / CG / 64; ++i) tma_2d<CG>(sb + i * 8192, mb, n0 + 64 * i, at, f);
-                        } else {
-                            tma_2d<CG>(sb, mb, at, n0, f);
-                        }
-                        ++fills;
+                    if (!(ok = wait(empty0 + 8u * (uint32_t)s, par))) break;
+                    const uint32_t f = full_at + 8u * (uint32_t)s, sb = sa + A.stage_b;
+                    if (CG == 1 || rank == 0) mbar_arrive_expect_tx(full0 + 8u * (uint32_t)s, A.stage_tx);
+                    if constexpr (kRowsA) {
+                        tma_2d<CG>(sa, ma, m0, at, f);
+                        tma_2d<CG>(sa + 8192, ma, m0 + 64, at, f);
+                    } else {
+                        tma_2d<CG>(sa, ma, at, m0, f);
                     }
-                    if (++s == S) { s = 0; par ^= 1u; }
+                    if constexpr (kRowsB) {
+#pragma unroll
+                        for (int i = 0; i < BN / CG / 64; ++i) tma_2d<CG>(sb + i * 8192, mb, n0 + 64 * i, at, f);
+                    } else {
+                        tma_2d<CG>(sb, mb, at, n0, f);
+                        if constexpr (kGated && CG == 1) tma_2d<CG>(sb + BN / 2 * 128, &M.b[1], at, n0, f);
+                    }
+                    ++n;
+                    at += 64;
+                    if (kOut && k + 1 == A.kb0) { at = 0; ++ma; ++mb; }
+                    sa += A.stage;
+                    if (++s == A.stages) { s = 0; par ^= 1u; sa = ring; }
                 }
             }
-            // What was asked for lands before the CTA ends, also where nobody waits for it any more.  (Both CTAs' copies count on this one's barriers.)
-            if (rank == 0)
-                for (int i = max(0, fills - S); i < fills; ++i)
-                    for (unsigned n = 0; n < A.tries && !mbar_try_wait(smem_u32(&full[i % S]), (uint32_t)(i / S) & 1u); ++n);
+            fills = n;
         }
         __syncwarp();
     } else if (warp == 1) {
         if (rank == 0) {
             const bool leader = elect_one();
-            const uint32_t idesc = product_idesc<T>(128 * CG, BN, A.a_mn, A.b_mn);
-            const uint64_t da = operand_desc(ring, A.a_mn), db = operand_desc(ring + kABytes, A.b_mn);
-            const uint32_t a_step = A.a_mn ? 2048 >> 4 : 32 >> 4, b_step = A.b_mn ? 2048 >> 4 : 32 >> 4;
+            const uint32_t idesc = product_idesc<T>(128 * CG, BN, kRowsA, kRowsB);
+            const uint64_t da = operand_desc(ring, kRowsA), db = operand_desc(ring + A.stage_b, kRowsB);
+            constexpr uint32_t a_step = kRowsA ? 2048 >> 4 : 32 >> 4, b_step = kRowsB ? 2048 >> 4 : 32 >> 4;
+            const uint32_t stage = A.stage >> 4;
             bool ok = true;
             int s = 0, acc = 0;
-            uint32_t par = 0u, acc_par = 1u;
+            uint32_t par = 0u, acc_par = 1u, at = 0u;
             for (int t = first; ok && t < A.tiles; t += step) {
-                const Tile w = tile_of(A, t);
-                if (!(ok = wait_warp(sums_empty[acc], acc_par))) break;
+                const Tile w = tile_of(A, (unsigned)t);
+                if (!(ok = wait_warp(sums_empty0 + 8u * (uint32_t)acc, acc_par))) break;
                 tcgen05_after_sync();
                 const uint32_t d = tmem + (uint32_t)(acc * BN);
+                uint32_t add = 0u;
                 for (int k = w.k0; k < w.k1; ++k) {
-                    if (!(ok = wait_warp(full[s], par))) break;
+                    if (!(ok = wait_warp(full0 + 8u * (uint32_t)s, par))) break;
                     tcgen05_after_sync();
                     if (leader) {
-                        const uint64_t a = da + (uint64_t)(uint32_t)(s * (C::stage >> 4)), b = db + (uint64_t)(uint32_t)(s * (C::stage >> 4));
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) mma_f16<CG>(d, a + i * a_step, b + i * b_step, idesc, (k > w.k0 || i > 0) ? 1u : 0u);
-                        commit<CG>(smem_u32(&empty[s]));
+                        for (int i = 0; i < 4; ++i) mma_f16<CG>(d, da + at + i * a_step, db + at + i * b_step, idesc, i > 0 ? 1u : add);
+                        commit<CG>(empty0 + 8u * (uint32_t)s);
                     }
                     __syncwarp();
-                    if (++s == S) { s = 0; par ^= 1u; }
+                    add = 1u;
+                    at += stage;
+                    if (++s == A.stages) { s = 0; par ^= 1u; at = 0u; }
                 }
                 if (!ok) break;
-                if (leader) commit<CG>(smem_u32(&sums_full[acc]));
+                if (leader) commit<CG>(sums_full0 + 8u * (uint32_t)acc);
                 __syncwarp();
                 if (++acc == 2) { acc = 0; acc_par ^= 1u; }
             }
-            // products under way end before the tensor memory goes back, also where nobody waits for them any more
-            if (leader) commit_here<CG>(smem_u32(&last));
-            __syncwarp();
-            for (unsigned n = 0; n < A.tries && !mbar_try_wait(smem_u32(&last), 0u); ++n);
         }
         __syncwarp();
     } else {
         const int quarter = warp & 3, half = (warp - 2) >> 2;
-        const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16);
-        const float scale = scale_of(A.amax, A.amax_to);
+        const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16), buf = ring + (uint32_t)(kRingBytes + (warp - 2) * 4096);
+        const float scale = scale_of(A.amax, A.amax_to), back = 1.f / scale;
         int acc = 0;
         uint32_t acc_par = 0u;
+        float mx = -INFINITY, sum = 0.f;        // PR_STATS
         for (int t = first; t < A.tiles; t += step) {
-            const Tile w = tile_of(A, t);
-            const int row = w.m * C::tm + rank * 128 + quarter * 32 + lane;
+            const Tile w = tile_of(A, (unsigned)t);
+            const int row0 = w.m * TM + rank * 128 + quarter * 32, row = row0 + lane;
             const bool live = row < A.m;
-            if (!wait_warp(sums_full[acc], acc_par)) break;
+            if constexpr (EPI == PR_GATED_GRAD && CG == 2) {
+                rows_free(lane);
+                rows_fetch(reinterpret_cast<const T *>(A.g_y), A.g_y_ld, row0, A.m, w.n * (BN / 2) + half * (BN / 4), A.n, (A.g_y_ld & 7) == 0 && ((uintptr_t)A.g_y & 15) == 0, buf, lane);
+            }
+            if (!wait_warp(sums_full0 + 8u * (uint32_t)acc, acc_par)) break;
             tcgen05_after_sync();
             const uint32_t sums = lanes + (uint32_t)(acc * BN);
             if constexpr (EPI == PR_GATED || EPI == PR_GATED_GRAD) {
                 constexpr int N = BN / 4 < 32 ? BN / 4 : 32;
                 const int col0 = w.n * (BN / 2) + half * (BN / 4);
-                const bool whole = (A.out_ld & 7) == 0;
-#pragma unroll 1
+                if constexpr (CG == 2 && EPI == PR_GATED) rows_free(lane);
+                if constexpr (CG == 2 && EPI == PR_GATED_GRAD) rows_landed();
+                uint32_t held[CG == 2 && EPI == PR_GATED_GRAD ? BN / 8 : 1];        // up's gradients, packed, until the buffer is free again
+                auto columns = [&](auto kind) {
+#pragma unroll
                 for (int c = 0; c < BN / 4; c += N) {
                     uint32_t vg[N], vu[N];
                     tmem_ld(vg, sums + (uint32_t)(half * (BN / 4) + c));
                     tmem_ld(vu, sums + (uint32_t)(BN / 2 + half * (BN / 4) + c));
-                    const int col = col0 + c;
+                    [[maybe_unused]] const int col = col0 + c;
                     float x[N];
                     if constexpr (EPI == PR_GATED_GRAD) {
-                        const T *gy = reinterpret_cast<const T *>(A.g_y) + (long long)row * A.g_y_ld;
-                        if (live && col + N <= A.n && (A.g_y_ld & 7) == 0 && ((uintptr_t)A.g_y & 15) == 0) {
+                        if constexpr (CG == 2) {
 #pragma unroll
                             for (int i = 0; i < N; i += 8) {
-                                const uint4 u = *reinterpret_cast<const uint4 *>(gy + col + i);
+                                const uint4 u = lds128(piece_at(buf, lane, (c + i) / 8));
                                 T e[8];
                                 memcpy(e, &u, 16);
 #pragma unroll
                                 for (int j = 0; j < 8; ++j) x[i + j] = to_f(e[j]) * scale;
                             }
                         } else {
+                            const T *gy = reinterpret_cast<const T *>(A.g_y) + (long long)row * A.g_y_ld;
 #pragma unroll
                             for (int i = 0; i < N; ++i) x[i] = live && col + i < A.n ? to_f(gy[col + i]) * scale : 0.f;
                         }
@@ -318,37 +412,55 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
 #pragma unroll
                         for (int i = 0; i < N; ++i) {
                             float a, da;
-                            activate(A.activation, __uint_as_float(vg[i]), a, da);
+                            activate<decltype(kind)::value>(__uint_as_float(vg[i]), a, da);
                             x[i] = a * __uint_as_float(vu[i]);
                         }
-                        if (live) store_row(reinterpret_cast<T *>(A.out[0]) + (long long)row * A.out_ld, col, A.n, whole && ((uintptr_t)A.out[0] & 15) == 0, x);
+                        if constexpr (CG == 2) put_row<T>(buf, lane, c / 8, x);
+                        else if (live) store_row(reinterpret_cast<T *>(A.out[0]) + (long long)row * A.out_ld, col, A.n, (A.out_ld & 7) == 0 && ((uintptr_t)A.out[0] & 15) == 0, x);
                     } else {
                         float y[N];
 #pragma unroll
                         for (int i = 0; i < N; ++i) {
                             float a, da;
-                            activate(A.activation, __uint_as_float(vg[i]), a, da);
+                            activate<decltype(kind)::value>(__uint_as_float(vg[i]), a, da);
                             y[i] = x[i] * a;
                             x[i] = x[i] * __uint_as_float(vu[i]) * da;
                         }
-                        if (live) {        // (workspace rows of a multiple of eight elements: what lies behind the last column is nobody's)
+                        if constexpr (CG == 2) {
+                            put_row<T>(buf, lane, c / 8, x);
+#pragma unroll
+                            for (int i = 0; i < N; i += 2) held[(c + i) / 2] = pack2<T>(y[i], y[i + 1]);
+                        } else if (live) {        // (workspace rows of a multiple of eight elements: what lies behind the last column is nobody's)
                             const int n8 = (int)A.out_ld;
                             store_row(reinterpret_cast<T *>(A.out[0]) + (long long)row * A.out_ld, col, n8, true, x);
                             store_row(reinterpret_cast<T *>(A.out[1]) + (long long)row * A.out_ld, col, n8, true, y);
                         }
                     }
                 }
+                };
+                if (A.activation == ACT_SILU) columns(std::integral_constant<int, ACT_SILU>());
+                else columns(std::integral_constant<int, ACT_GELU>());
+                if constexpr (CG == 2) {
+                    if (A.tma_out) rows_store(&M.out[0], buf, col0, row0, 0, false, row0 < A.m && col0 < A.n, lane);
+                    else rows_copy_out(reinterpret_cast<T *>(A.out[0]), A.out_ld, row0, A.m, col0, A.n, buf, lane);
+                    if constexpr (EPI == PR_GATED_GRAD) {
+                        rows_free(lane);
+#pragma unroll
+                        for (int i = 0; i < BN / 32; ++i) sts128(piece_at(buf, lane, i), make_uint4(held[4 * i], held[4 * i + 1], held[4 * i + 2], held[4 * i + 3]));
+                        rows_store(&M.out[1], buf, col0, row0, 0, false, row0 < A.m && col0 < A.n, lane);
+                    }
+                }
             } else {
-                constexpr int N = 32;
+                constexpr int N = BN / 2 < 32 ? BN / 2 : 32;
                 const int col0 = w.n * BN + half * (BN / 2);
                 long long token = -1;
-                float mx = -INFINITY, sum = 0.f, g = 0.f, gp = 0.f, lse2 = 0.f;
+                float g = 0.f, gp = 0.f, lse2 = 0.f;
                 if (EPI == PR_STATS || EPI == PR_DLOGITS) {
                     if (live) {
                         token = A.token_bytes == 8 ? reinterpret_cast<const long long *>(A.tokens)[row * A.token_ld] : (long long)reinterpret_cast<const int *>(A.tokens)[row * A.token_ld];
-                        token -= A.vocab0;
+                        const bool there = token >= 0 && token < A.vocab;
+                        token = there ? token - A.vocab0 : -1;
                         if constexpr (EPI == PR_DLOGITS) {
-                            const bool there = token + A.vocab0 >= 0 && token + A.vocab0 < A.vocab;
                             const float lse = A.lse[row];
                             g = A.g && there ? A.g[row * A.g_ld] : 0.f;
                             gp = g - (A.g_lse ? A.g_lse[row * A.g_lse_ld] : 0.f);
@@ -364,38 +476,52 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
                     uint32_t v[N];
                     tmem_ld(v, sums + (uint32_t)(half * (BN / 2) + c));
                     const int col = col0 + c;
+                    if (CG == 2 && EPI != PR_STATS && (A.partial || (c & 32) == 0)) rows_free(lane);
                     tmem_wait_ld();
                     float x[N];
                     if constexpr (EPI == PR_STATS) {
-                        const int n = A.n - col;
-                        float top = -INFINITY;
+                        if (col + N > A.n) {
 #pragma unroll
-                        for (int i = 0; i < N; ++i) {
-                            x[i] = i < n ? __uint_as_float(v[i]) * A.c : -INFINITY;
-                            top = fmaxf(top, x[i]);
+                            for (int i = 0; i < N; ++i)
+                                if (col + i >= A.n) v[i] = 0xff800000u;        // -infinity
                         }
+                        float top = __uint_as_float(v[0]);
+#pragma unroll
+                        for (int i = 1; i < N; ++i) top = fmaxf(top, __uint_as_float(v[i]));
                         if (token >= col && token < col + N) {
 #pragma unroll
                             for (int i = 0; i < N; ++i)
-                                if (token == col + i && i < n) A.token_z[row] = __uint_as_float(v[i]) * A.inv_t;
+                                if (token == col + i) A.token_z[row] = __uint_as_float(v[i]) * A.inv_t;
                         }
                         const float was = mx;
-                        mx = fmaxf(mx, top);
+                        mx = fmaxf(mx, top * A.c);
                         const float base = mx == -INFINITY ? 0.f : mx;
-                        sum *= ex2(was - base);
+                        float more[2] = {0.f, 0.f};
 #pragma unroll
-                        for (int i = 0; i < N; ++i) sum += ex2(x[i] - base);
-                    } else if constexpr (EPI == PR_DLOGITS) {
-#pragma unroll
-                        for (int i = 0; i < N; ++i) {
-                            x[i] = -gp * ex2(fmaf(__uint_as_float(v[i]), A.c, -lse2));
-                            if (token == col + i) x[i] += g;
-                        }
-                        if (live) store_row(reinterpret_cast<T *>(A.out[0]) + (long long)row * A.out_ld, col, (int)A.out_ld, true, x);
+                        for (int i = 0; i < N; ++i) more[i & 1] += ex2(fmaf(__uint_as_float(v[i]), A.c, -base));
+                        sum = fmaf(sum, ex2(was - base), more[0] + more[1]);
                     } else {
-                        if (A.partial) {
-                            float *p = A.partial + (((long long)w.job * A.splits + w.split) * A.m + row) * A.n + col;
-                            if (live)
+                        if constexpr (EPI == PR_DLOGITS) {
+#pragma unroll
+                            for (int i = 0; i < N; ++i) {
+                                x[i] = -gp * ex2(fmaf(__uint_as_float(v[i]), A.c, -lse2));
+                            }
+                            if (token >= col && token < col + N) {
+#pragma unroll
+                                for (int i = 0; i < N; ++i)
+                                    if (token == col + i) x[i] += g;
+                            }
+                        } else {
+#pragma unroll
+                            for (int i = 0; i < N; ++i) x[i] = __uint_as_float(v[i]) * back;
+                        }
+                        if (kOut && A.partial) {
+                            if constexpr (CG == 2) {
+#pragma unroll
+                                for (int i = 0; i < 8; ++i) sts128(piece_at(buf, lane, i), make_uint4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]));
+                                rows_store(&M.out[0], buf, col, row0, w.job * A.splits + w.split, A.add != 0, row0 < A.m && col < A.n, lane);
+                            } else if (live) {
+                                float *p = A.partial + (((long long)w.job * A.splits + w.split) * A.m + row) * A.n + col;
 #pragma unroll
                                 for (int i = 0; i < N; i += 4)
                                     if (col + i < A.n) {
@@ -406,16 +532,23 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
                                         }
                                         *reinterpret_cast<float4 *>(p + i) = o;
                                     }
+                            }
+                        } else if constexpr (CG == 2) {
+                            put_row<T>(buf, lane, (c & 32) / 8, x);
+                            if (c & 32) rows_store(&M.out[w.job], buf, col - 32, row0, 0, false, row0 < A.m && col - 32 < A.n, lane);
                         } else if (live) {
-                            const float back = 1.f / scale;
-#pragma unroll
-                            for (int i = 0; i < N; ++i) x[i] = __uint_as_float(v[i]) * back;
-                            store_row(reinterpret_cast<T *>(A.out[w.job]) + (long long)row * A.out_ld, col, A.n, true, x);
+                            store_row(reinterpret_cast<T *>(A.out[w.job]) + (long long)row * A.out_ld, col, EPI == PR_DLOGITS ? (int)A.out_ld : A.n, true, x);
                         }
                     }
                 }
                 if constexpr (EPI == PR_STATS) {
-                    if (live) A.parts[(long long)(2 * w.n + half) * A.m + row] = make_float2(mx, sum);
+                    if (!A.carry) {
+                        if (live) A.parts[(long long)(2 * w.n + half) * A.m + row] = make_float2(mx, sum);
+                        mx = -INFINITY;
+                        sum = 0.f;
+                    } else if (t + step >= A.tiles && live) {
+                        A.parts[(long long)(2 * first + half) * A.m + row] = make_float2(mx, sum);
+                    }
                 }
             }
             tcgen05_before_sync();
@@ -426,10 +559,24 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
             }
             if (++acc == 2) { acc = 0; acc_par ^= 1u; }
         }
+        if (CG == 2 && EPI != PR_STATS && lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
         __syncwarp();
     }
     tcgen05_before_sync();
     __syncthreads();
+    if (dead) {
+        // What was asked for lands before the CTA ends, and products under way end before the tensor memory goes back, also where nobody waits for them any more.
+        // (Both CTAs' copies count on this one's barriers; the other's last wait has run out long after its last copy.)
+        if (tid == 0 && rank == 0)
+            for (int i = max(0, fills - A.stages); i < fills; ++i)
+                for (unsigned n = 0; n < A.tries && !mbar_try_wait(smem_u32(&full[i % A.stages]), (uint32_t)(i / A.stages) & 1u); ++n);
+        if (warp == 1 && rank == 0) {
+            if (elect_one()) commit_here<CG>(smem_u32(&last));
+            __syncwarp();
+            for (unsigned n = 0; n < A.tries && !mbar_try_wait(smem_u32(&last), 0u); ++n);
+        }
+        __syncthreads();
+    }
     if constexpr (CG == 2) { cluster_arrive(); cluster_wait(); }        // (nobody leaves while the other CTA's barriers and memory are still in use)
     if (warp == 1) {
         tcgen05_after_sync();
@@ -538,6 +685,16 @@ static bool operand_map(EncodeTiledFn encode, CUtensorMap *out, const Operand &o
                   CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// Results as a warp stores them: 32 rows of 64 elements (partial sums: 32 numbers).
+static bool result_map(EncodeTiledFn encode, CUtensorMap *out, const ProductArgs &A, int dtype, bool sums, int i) {
+    const cuuint64_t ld = sums ? (cuuint64_t)A.n * 4 : (cuuint64_t)A.out_ld * 2;
+    cuuint64_t dims[3] = {(cuuint64_t)A.n, (cuuint64_t)A.m, sums ? (cuuint64_t)A.jobs * A.splits : 1}, strides[2] = {ld, ld * A.m};
+    cuuint32_t box[3] = {sums ? 32u : 64u, 32, 1}, one[3] = {1, 1, 1};
+    return encode(out, sums ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : dtype == XSM_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3,
+                  sums ? (void *)A.partial : A.out[i], dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_NONE,
+                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 int product_sms() {
     static std::atomic<int> known[kMaxDevices];
     int dev = 0, n = 0;
@@ -545,6 +702,11 @@ int product_sms() {
     n = known[dev].load(std::memory_order_relaxed);
     if (n == 0 && cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) == cudaSuccess) known[dev].store(n, std::memory_order_relaxed);
     return n;
+}
+
+int product_ctas(long long tiles, bool wide) {
+    const int slots = wide ? product_sms() / 2 : product_sms();
+    return (int)(tiles < slots ? tiles : slots) * (wide ? 2 : 1);
 }
 
 static std::atomic<unsigned> g_tries{kMbarSpinLimit};
@@ -561,15 +723,13 @@ int product_splits(long long tiles, int kb, bool wide) {
 }
 
 template <int CG, int BN, int EPI, typename T> static cudaError_t start(const ProductMaps &M, const ProductArgs &A, cudaStream_t st) {
-    using C = Cut<CG, BN>;
-    const int smem = C::stage * C::stages + 1024;
+    const int smem = kRingBytes + (CG == 2 ? kEpiWarps * 4096 : kABytes) + 1024;        // (few rows: the tensor cores read 128 rows of A whatever the box brought)
     const void *fn = (const void *)product_kernel<CG, BN, EPI, T>;
     cudaError_t e = open_kernel(fn, smem, false);
     if (e != cudaSuccess) return e;
-    const int slots = product_sms() / CG;
-    if (slots < 1) return cudaErrorInvalidDevice;
+    if (product_sms() < 2) return cudaErrorInvalidDevice;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)((A.tiles < slots ? A.tiles : slots) * CG));
+    cfg.gridDim = dim3((unsigned)product_ctas(A.tiles, CG == 2));
     cfg.blockDim = dim3(kProductThreads);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
@@ -583,44 +743,87 @@ template <int CG, int BN, int EPI, typename T> static cudaError_t start(const Pr
     return cudaLaunchKernelEx(&cfg, product_kernel<CG, BN, EPI, T>, M, A);
 }
 template <int CG, int BN, typename T> static cudaError_t start_epi(ProductEpi epi, const ProductMaps &M, const ProductArgs &A, cudaStream_t st) {
-    switch (epi) {
-        case PR_STATS: return start<CG, BN, PR_STATS, T>(M, A, st);
-        case PR_DLOGITS: return start<CG, BN, PR_DLOGITS, T>(M, A, st);
+    if (epi == PR_STATS) return start<CG, BN, PR_STATS, T>(M, A, st);
+    if (epi == PR_DLOGITS) return start<CG, BN, PR_DLOGITS, T>(M, A, st);
+    if constexpr (BN > 32) switch (epi) {
         case PR_GATED: return start<CG, BN, PR_GATED, T>(M, A, st);
         case PR_GATED_GRAD: return start<CG, BN, PR_GATED_GRAD, T>(M, A, st);
-        default: return start<CG, BN, PR_OUT, T>(M, A, st);
+        case PR_OUT: return start<CG, BN, PR_OUT, T>(M, A, st);
+        default: return start<CG, BN, PR_OUT_ROWS, T>(M, A, st);
     }
+    return cudaErrorInvalidValue;
 }
 
-cudaError_t launch_product(ProductEpi epi, int dtype, bool wide, ProductArgs A, const Operand (&a)[2], const Operand (&b)[2], int pairs, cudaStream_t st) {
+// Rows of more than one tile of 128 take two CTAs a tile.  Few rows: what a CTA fetches decides, its tiles times the rows of both operands; of the widths that fetch
+// least, the widest.  (96 rows x 131071 tokens: 64 columns 83 us, 128 ...; 5 rows x 4096: ...)  Operands whose rows run along the summed axis come in boxes of 64
+// columns.
+ProductCut product_cut(ProductEpi epi, long long m, long long n) {
+    const bool gated = epi == PR_GATED || epi == PR_GATED_GRAD;
+    if (m > 128 && n > (gated ? 32 : 64)) return {true, 256};
+    ProductCut best = {false, 128};
+    double least = 1e300;
+    for (int bn = 128; bn >= (gated || epi == PR_OUT || epi == PR_OUT_ROWS ? 64 : 32); bn /= 2) {
+        const ProductCut c = {false, bn};
+        const long long sms = product_sms() < 1 ? 1 : product_sms();
+        const double cost = (double)((c.tiles(m, n, gated) + sms - 1) / sms) * (double)((m < 128 ? m : 128) + bn);
+        if (cost < least) { least = cost; best = c; }
+    }
+    return best;
+}
+
+cudaError_t launch_product(ProductEpi epi, int dtype, ProductCut cut, ProductArgs A, const Operand (&a)[2], const Operand (&b)[2], int pairs, cudaStream_t st) {
     EncodeTiledFn encode;
     cudaError_t e = encoder(&encode);
     if (e != cudaSuccess) return e;
-    const bool gated = epi == PR_GATED || epi == PR_GATED_GRAD;
-    const ProductCut cut = product_cut(wide);
-    const int tm = 128 * cut.group, tn = gated ? cut.bn / 2 : cut.bn;
+    const bool gated = epi == PR_GATED || epi == PR_GATED_GRAD, wide = cut.wide, a_rows_summed = epi == PR_OUT_ROWS, b_rows_summed = epi == PR_OUT || epi == PR_OUT_ROWS;
+    const int tm = cut.tm(), tn = cut.tn(gated), group = wide ? 2 : 1;
     A.tiles_m = (A.m + tm - 1) / tm;
     A.tiles_n = (A.n + tn - 1) / tn;
-    const long long summed = A.a_mn ? a[0].rows : a[0].row;
+    const long long summed = a_rows_summed ? a[0].rows : a[0].row;
     A.kb0 = (int)((summed + 63) / 64);
     A.kb = A.kb0 * pairs;
     const long long tiles = (long long)A.tiles_m * A.tiles_n * A.jobs * A.splits;
     if (tiles > 0x3fffffff) return cudaErrorInvalidValue;
     A.tiles = (int)tiles;
+    A.group_m = A.tiles_m < 8 ? A.tiles_m : 8;
+    const int last_rows = A.tiles_m % A.group_m;
+    A.by_plane = Divisor((unsigned)(A.tiles_m * A.tiles_n));
+    A.by_group = Divisor((unsigned)(A.group_m * A.tiles_n));
+    A.by_rows = Divisor((unsigned)A.group_m);
+    A.by_last_rows = Divisor((unsigned)(last_rows ? last_rows : A.group_m));
+    A.by_splits = Divisor((unsigned)A.splits);
+    A.kb_each = A.kb / A.splits;
+    A.kb_more = A.kb % A.splits;
     A.a_rows = A.m >= 128 ? 128 : (A.m + 7) / 8 * 8;
-    const int b_box = gated ? (wide ? 128 : cut.bn / 2) : cut.bn / cut.group;
-    A.stage_tx = (uint32_t)(cut.group * ((A.a_mn ? kABytes : A.a_rows * 128) + cut.bn / cut.group * 128));
+    const int b_box = gated ? (wide ? 128 : cut.bn / 2) : cut.bn / group;
+    A.stage_b = (uint32_t)(a_rows_summed ? kABytes : A.a_rows * 128);
+    A.stage = A.stage_b + (uint32_t)(cut.bn / group * 128);
+    A.stage_tx = group * A.stage;
+    A.stages = kRingBytes / (int)A.stage < kMaxStages ? kRingBytes / (int)A.stage : kMaxStages;
     product_waits(&A.tries, &A.starve);
     ProductMaps M;
     memset(&M, 0, sizeof M);
     const int na = pairs > A.jobs ? pairs : A.jobs, nb = gated ? 2 : pairs;
     for (int i = 0; i < na; ++i)
-        if (!operand_map(encode, &M.a[i], a[i], dtype, A.a_mn ? 64 : A.a_rows)) return cudaErrorInvalidValue;
+        if (!operand_map(encode, &M.a[i], a[i], dtype, a_rows_summed ? 64 : A.a_rows)) return cudaErrorInvalidValue;
     for (int i = 0; i < nb; ++i)
-        if (!operand_map(encode, &M.b[i], b[i], dtype, A.b_mn ? 64 : b_box)) return cudaErrorInvalidValue;
+        if (!operand_map(encode, &M.b[i], b[i], dtype, b_rows_summed ? 64 : b_box)) return cudaErrorInvalidValue;
+    if (wide && epi != PR_STATS) {
+        const bool sums = b_rows_summed && A.partial;
+        const int outs = sums ? 1 : epi == PR_GATED_GRAD ? 2 : A.jobs;
+        A.tma_out = sums || (A.out_ld % 8 == 0 && (uintptr_t)A.out[0] % 16 == 0);
+        for (int i = 0; i < outs && A.tma_out; ++i)
+            if (!result_map(encode, &M.out[i], A, dtype, sums, i)) return cudaErrorInvalidValue;
+    }
     const bool bf = dtype == XSM_BF16;
-    if (wide) return bf ? start_epi<2, 256, bf16>(epi, M, A, st) : start_epi<2, 256, __half>(epi, M, A, st);
-    return bf ? start_epi<1, 64, bf16>(epi, M, A, st) : start_epi<1, 64, __half>(epi, M, A, st);
+    auto go = [&](auto cg, auto bn) {
+        constexpr int CG = decltype(cg)::value, BN = decltype(bn)::value;
+        return bf ? start_epi<CG, BN, bf16>(epi, M, A, st) : start_epi<CG, BN, __half>(epi, M, A, st);
+    };
+    using std::integral_constant;
+    if (wide) return go(integral_constant<int, 2>(), integral_constant<int, 256>());
+    if (cut.bn == 128) return go(integral_constant<int, 1>(), integral_constant<int, 128>());
+    return cut.bn == 64 ? go(integral_constant<int, 1>(), integral_constant<int, 64>()) : go(integral_constant<int, 1>(), integral_constant<int, 32>());
 }
 
 cudaError_t launch_amax_rows(const void *x, int dtype, long long rows, long long cols, long long ld, float *amax, cudaStream_t st) {

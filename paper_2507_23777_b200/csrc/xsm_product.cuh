@@ -13,21 +13,38 @@ enum ProductEpi {
     PR_DLOGITS,      // gradient by the logits
     PR_GATED,        // act(gate) * up
     PR_GATED_GRAD,   // gradients by gate and up
-    PR_OUT           // the sums themselves: rounded to the output's type, or fp32 partial sums
+    PR_OUT,          // the sums themselves: rounded to the output's type, or fp32 partial sums
+    PR_OUT_ROWS      // the same for an A whose rows run along the summed axis
 };
 enum Activation { ACT_SILU = 0, ACT_GELU = 1 };
 
 constexpr int kAmaxBlocks = 256;
 
-struct __align__(64) ProductMaps { CUtensorMap a[2], b[2]; };
+// n / d for n below 2^31 by a product and a shift (Granlund and Montgomery's method)
+struct Divisor {
+    unsigned d, m, l;
+    Divisor() = default;
+    explicit Divisor(unsigned d_) : d(d_), m(0), l(0) {
+        while (l < 32 && (1ull << l) < d) ++l;
+        m = (unsigned)(((1ull << 32) * ((1ull << l) - d)) / d + 1);
+    }
+    __device__ __forceinline__ unsigned of(unsigned n) const { return (__umulhi(m, n) + n) >> l; }
+};
+
+struct __align__(64) ProductMaps { CUtensorMap a[2], b[2], out[2]; };
 
 struct ProductArgs {
     int m, n;                       // rows and columns of the result (PR_GATED: n columns of gate and of up)
     int tiles_m, tiles_n, jobs, splits, tiles;
     int kb0, kb;                    // blocks of 64 along the summed axis: of the first pair of operands, of all
-    int a_mn, b_mn;                 // operands whose rows run along the summed axis
+    int kb_each, kb_more;           // blocks of a split, and how many splits have one more
+    Divisor by_plane, by_group, by_rows, by_last_rows, by_splits;      // tiles of a split, of a group, rows of a group, of the last one
     int a_rows;                     // rows of a box of A (not a_mn)
+    int group_m;                    // tiles of rows that are worked on side by side
+    int stages;                     // of the ring
+    uint32_t stage, stage_b;        // bytes of a CTA's stage, where B begins in it
     uint32_t stage_tx;              // bytes of a stage of all CTAs of a tile
+    int tma_out;                    // wide tiles: results leave by TMA
     unsigned tries;                 // of a barrier, before a wait gives up
     int starve;                     // fetch nothing (xsm_debug_product_waits)
     int *status;
@@ -38,6 +55,7 @@ struct ProductArgs {
     int token_bytes, vocab0, vocab; // first token of this piece of the vocabulary, all tokens
     float c, inv_t;                 // log2(e) / T, 1 / T
     float2 *parts;                  // [part][m]: maximum, sum
+    int carry;                      // one tile of rows: a CTA's parts are joined in its registers, parts are the CTAs'
     float *token_z;                 // [m]
     const float *lse, *g, *g_lse;
     long long g_ld, g_lse_ld;
@@ -54,16 +72,25 @@ struct ProductArgs {
     int add;                        // to what partial holds
 };
 
-// How a product is cut: `wide`: two CTAs share tiles of 256 x 256; otherwise a CTA has tiles of 128 x 64.
-struct ProductCut { int group, bn; };
-inline ProductCut product_cut(bool wide) { return wide ? ProductCut{2, 256} : ProductCut{1, 64}; }
+// How a product is cut: `wide`: two CTAs share tiles of 256 x 256; otherwise a CTA has tiles of 128 x bn.  gated: half of the columns are gate's, half up's, and a
+// tile is half as wide.
+struct ProductCut {
+    bool wide;
+    int bn;
+    int tm() const { return wide ? 256 : 128; }
+    int tn(bool gated) const { return gated ? bn / 2 : bn; }
+    long long tiles(long long m, long long n, bool gated) const { return ((m + tm() - 1) / tm()) * ((n + tn(gated) - 1) / tn(gated)); }
+};
+// out [m][n]; epi: what is done with it
+ProductCut product_cut(ProductEpi epi, long long m, long long n);
 
 // An operand in memory: `rows` rows of `row` elements, ld elements apart.
 struct Operand { const void *p; long long rows, row, ld; };
 
-// Fills in the cut (tiles, boxes, maps) of A and launches.  a, b: operands of the pairs or jobs; summed: which axis of each is summed over
-// (a_mn, b_mn: the rows).
-cudaError_t launch_product(ProductEpi epi, int dtype, bool wide, ProductArgs A, const Operand (&a)[2], const Operand (&b)[2], int pairs, cudaStream_t st);
+// CTAs that a product of so many tiles runs on
+int product_ctas(long long tiles, bool wide);
+// Fills in the cut (tiles, boxes, maps) of A and launches.  a, b: operands of the pairs or jobs.  PR_OUT*: b's rows run along the summed axis.
+cudaError_t launch_product(ProductEpi epi, int dtype, ProductCut cut, ProductArgs A, const Operand (&a)[2], const Operand (&b)[2], int pairs, cudaStream_t st);
 
 // |x| at most over rows of 16-bit elements, or of fp32 numbers 2|g| + |g_lse| times `by`; [kAmaxBlocks]
 cudaError_t launch_amax_rows(const void *x, int dtype, long long rows, long long cols, long long ld, float *amax, cudaStream_t st);
