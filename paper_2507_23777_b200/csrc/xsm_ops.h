@@ -40,6 +40,17 @@ inline Pages pages_of(const xsm_kv &kv, const int32_t *table, int64_t table_ld, 
     return Pages{(char *)kv.k, (char *)kv.v, table, c.page_stride, c.head_stride, c.row_stride, table_ld, c.n_pages, c.page_size, c.n_kv_heads, max_pages};
 }
 
+// n / d for n below 2^31 by a product and a shift (Granlund and Montgomery's method)
+struct Divisor {
+    unsigned d, m, l;
+    Divisor() = default;
+    explicit Divisor(unsigned d_) : d(d_), m(0), l(0) {
+        while (l < 32 && (1ull << l) < d) ++l;
+        m = (unsigned)(((1ull << 32) * ((1ull << l) - d)) / d + 1);
+    }
+    __device__ __forceinline__ unsigned of(unsigned n) const { return (__umulhi(m, n) + n) >> l; }
+};
+
 // ------------------------------------------------------------------------------------------- elements
 
 // rounding to the type, once: to the nearest, what is too large becomes infinite

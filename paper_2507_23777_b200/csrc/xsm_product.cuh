@@ -20,17 +20,6 @@ enum Activation { ACT_SILU = 0, ACT_GELU = 1 };
 
 constexpr int kAmaxBlocks = 256;
 
-// n / d for n below 2^31 by a product and a shift (Granlund and Montgomery's method)
-struct Divisor {
-    unsigned d, m, l;
-    Divisor() = default;
-    explicit Divisor(unsigned d_) : d(d_), m(0), l(0) {
-        while (l < 32 && (1ull << l) < d) ++l;
-        m = (unsigned)(((1ull << 32) * ((1ull << l) - d)) / d + 1);
-    }
-    __device__ __forceinline__ unsigned of(unsigned n) const { return (__umulhi(m, n) + n) >> l; }
-};
-
 struct __align__(64) ProductMaps { CUtensorMap a[2], b[2], out[2]; };
 
 struct ProductArgs {
