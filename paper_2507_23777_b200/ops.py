@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import ctypes as C
 import struct
+import threading
 import weakref
 from collections import namedtuple
 
@@ -506,6 +507,34 @@ def _status(device: int, stream: int) -> int:
     return t.data_ptr()
 
 
+_KEPT = 1 << 20          # bytes of a workspace that is kept from call to call
+_scratch_of = threading.local()
+_sizes = {}              # by operator and sizes: bytes of its workspace
+
+
+def _size_of(fn, *sizes) -> int:
+    n = _sizes.get((fn, sizes))
+    if n is None:
+        if len(_sizes) > 4096:
+            _sizes.clear()
+        n = _sizes[fn, sizes] = getattr(binding.load(), fn)(*sizes)
+    return n
+
+
+def _scratch(n: int, device: int, stream: int, where):
+    """Memory for one call on the stream, of any content: a small one is the thread's from call to call, while nothing is recorded."""
+    if n > _KEPT or stream and _capturing():
+        return _empty((n,), (1,), dtype=torch.uint8, device=where)
+    kept = _scratch_of.__dict__
+    t = kept.get((device, stream))
+    if t is None or t[1] < n:
+        if len(kept) > 64:
+            kept.clear()
+        size = max(n, 1 << 16)
+        t = kept[device, stream] = _empty((size,), (1,), dtype=torch.uint8, device=where), size
+    return t[0]
+
+
 def check(device=None):
     """Waits for the device (the current one) and raises an XsmError if a bounded wait of an earlier linear_logprobs, gated_feed_forward or gradient of
     theirs ran out there, replays of recorded ones among them (the results since the last check are void)."""
@@ -521,15 +550,16 @@ def check(device=None):
 
 def _rows(t, what: str, device: int, dtype, width=None):
     """Row stride of a matrix of 16-bit elements that the products can take as it lies."""
-    if t.dim() != 2 or t.dtype is not dtype or width is not None and t.shape[1] != width:
-        raise ValueError(f"{what} must be [rows, {'d' if width is None else width}] of {dtype}, not {list(t.shape)} of {t.dtype}")
+    shape = t.shape
+    if len(shape) != 2 or t.dtype is not dtype or width is not None and shape[1] != width:
+        raise ValueError(f"{what} must be [rows, {'d' if width is None else width}] of {dtype}, not {list(shape)} of {t.dtype}")
     if t.get_device() != device:
         raise ValueError(f"{what} must be on cuda:{device}")
-    n, w = t.shape
+    n, w = shape
     ld, step = t.stride()
-    if n < 2 or w == 0:
+    if n < 2:
         ld = w
-    if step != 1 and w > 1 or ld < w or ld % 8 or t.data_ptr() % 16:
+    if step != 1 and w > 1 or ld < w or ld & 7 or t.data_ptr() & 15:
         raise ValueError(f"rows of {what} must be of neighbouring elements, 16-byte aligned, and must not overlap")
     return ld
 
@@ -570,8 +600,8 @@ def _linear_forward(hidden, weight, tokens, temperature):
     lib, where, vocab, stream = binding.load(), hidden.device, weight.shape[0], _raw_stream(device)
     logprob = _empty((rows,), (1,), dtype=torch.float32, device=where)
     lse = _empty((rows,), (1,), dtype=torch.float32, device=where)
-    n = lib.xsm_linear_logprobs_workspace(rows, vocab, d)
-    ws = _empty((n,), (1,), dtype=torch.uint8, device=where)
+    n = _size_of("xsm_linear_logprobs_workspace", rows, vocab, d)
+    ws = _scratch(n, device, stream, where)
     try:
         args = _LINEAR.pack(hidden.data_ptr(), weight.data_ptr(), tokens.data_ptr(), logprob.data_ptr(), lse.data_ptr(), ws.data_ptr(), _status(device, stream),
                             ld, w_ld, tokens.stride(0), n, rows, vocab, d, _DTYPES[dtype], _TOKENS[tokens.dtype], temperature)
@@ -598,8 +628,8 @@ def linear_logprobs_grad(hidden, weight, tokens, result, grad_logprob=None, grad
     lib, where, vocab, stream = binding.load(), hidden.device, weight.shape[0], _raw_stream(device)
     d_hidden = _empty((rows, d), (d, 1), dtype=dtype, device=where) if need[0] else None
     d_weight = _empty((vocab, d), (d, 1), dtype=dtype, device=where) if need[1] else None
-    n = lib.xsm_linear_logprobs_grad_workspace(rows, vocab, d)
-    ws = _empty((n,), (1,), dtype=torch.uint8, device=where)
+    n = _size_of("xsm_linear_logprobs_grad_workspace", rows, vocab, d)
+    ws = _scratch(n, device, stream, where)
     try:
         args = _LINEAR_GRAD.pack(hidden.data_ptr(), weight.data_ptr(), tokens.data_ptr(), lse.data_ptr(), gl, gs, 0 if d_hidden is None else d_hidden.data_ptr(),
                                  0 if d_weight is None else d_weight.data_ptr(), ws.data_ptr(), _status(device, stream), ld, w_ld, tokens.stride(0), gl_ld, gs_ld,
@@ -658,7 +688,7 @@ def _check_gated(x, w_gate, w_up, activation):
 def _gated_forward(x, w_gate, w_up, activation):
     device, dtype, flat, rows, ff, d, ld, g_ld, u_ld = _check_gated(x, w_gate, w_up, activation)
     stream = _raw_stream(device)
-    out = torch.empty((*x.shape[:-1], ff), dtype=dtype, device=x.device)
+    out = _empty((rows, ff), (ff, 1), dtype=dtype, device=x.device) if flat is x else torch.empty((*x.shape[:-1], ff), dtype=dtype, device=x.device)
     try:
         args = _GATED.pack(flat.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), out.data_ptr(), _status(device, stream), ld, g_ld, u_ld, ff, rows, ff, d, _DTYPES[dtype],
                            _ACTIVATIONS[activation])
@@ -676,18 +706,18 @@ def gated_feed_forward_grad(x, w_gate, w_up, grad, activation: str = "silu", nee
     gradient are refused unless torch.no_grad() says that it is not needed."""
     _no_gradient("gated_feed_forward_grad", x, w_gate, w_up, grad)
     device, dtype, flat, rows, ff, d, ld, g_ld, u_ld = _check_gated(x, w_gate, w_up, activation)
-    if grad.shape != (*x.shape[:-1], ff) or grad.dtype is not dtype or grad.get_device() != device:
+    if grad.shape[:-1] != x.shape[:-1] or grad.dim() < 1 or grad.shape[-1] != ff or grad.dtype is not dtype or grad.get_device() != device:
         raise ValueError(f"grad must be {[*x.shape[:-1], ff]} of {dtype} on cuda:{device}")
     g = grad if grad.dim() == 2 else grad.reshape(-1, ff)
     if ff > 1 and rows and g.stride(1) != 1:
         raise ValueError("the elements of a row of grad must be neighbours")
     lib, where, stream = binding.load(), x.device, _raw_stream(device)
-    d_x = torch.empty(x.shape, dtype=dtype, device=where) if need[0] else None
+    d_x = _empty((rows, d), (d, 1), dtype=dtype, device=where).view(x.shape) if need[0] else None
     d_gate = d_up = None
     if need[1] or need[2]:
         d_gate, d_up = (_empty((ff, d), (d, 1), dtype=dtype, device=where) for _ in range(2))
-    n = lib.xsm_gated_ff_grad_workspace(rows, ff, d)
-    ws = _empty((n,), (1,), dtype=torch.uint8, device=where)
+    n = _size_of("xsm_gated_ff_grad_workspace", rows, ff, d)
+    ws = _scratch(n, device, stream, where)
     try:
         args = _GATED_GRAD.pack(flat.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), g.data_ptr(), 0 if d_x is None else d_x.data_ptr(), 0 if d_gate is None else d_gate.data_ptr(),
                                 0 if d_up is None else d_up.data_ptr(), ws.data_ptr(), _status(device, stream), ld, g_ld, u_ld, g.stride(0), d, d, n, rows, ff, d, _DTYPES[dtype],
@@ -729,48 +759,79 @@ def gated_feed_forward(x, w_gate, w_up, activation: str = "silu"):
 
 # --------------------------------------------------------------------------------------- norms of heads with the rotation
 
-def _norm_layout(q, k, q_gain, k_gain, rope, positions):
-    """(device, type, type of the gains, batch, m, heads, kv heads, d_head, positions, half of the rotated) of arguments that go together."""
+def _refuse_norm(q, k, q_gain, k_gain, rope, positions):
+    """What is wrong with the arguments, told one by one."""
+    _need((q is None) == (q_gain is None) and (k is None) == (k_gain is None) and (q is not None or k is not None),
+          "q and q_gain go together, k and k_gain too, and one of the pairs must be there")
     x, gain = (q, q_gain) if q is not None else (k, k_gain)
-    if x is None or (q is None) != (q_gain is None) or (k is None) != (k_gain is None):
-        raise ValueError("q and q_gain go together, k and k_gain too, and one of the pairs must be there")
+    _need(x.dim() == 4 and x.dtype in _DTYPES, "q and k must be [batch, m, heads, d_head] of fp32, bf16 or fp16")
+    _need_here(x)
     device = x.get_device()
-    if device < 0 or device != _current_device():
-        _need_here(x)
-    if x.dim() != 4 or x.dtype not in _DTYPES:
-        raise ValueError("q and k must be [batch, m, heads, d_head] of fp32, bf16 or fp16")
-    batch, m, _, d = x.shape
     for t, g in ((q, q_gain), (k, k_gain)):
-        if t is None:
-            continue
-        if t.dim() != 4 or t.shape[0] != batch or t.shape[1] != m or t.shape[3] != d or t.dtype is not x.dtype or t.get_device() != device or t.stride(3) != 1:
-            raise ValueError("q and k must have the same batch, tokens, d_head, type and device, and neighbouring elements of a head")
-        _need_gain(g, d, device, gain.dtype)
-    half = n = 0
+        if t is not None:
+            _need(t.dim() == 4 and t.shape[:2] == x.shape[:2] and t.shape[3] == x.shape[3] and t.dtype is x.dtype and t.get_device() == device and t.stride(3) == 1,
+                  "q and k must have the same batch, tokens, d_head, type and device, and neighbouring elements of a head")
+            _need_gain(g, x.shape[3], device, gain.dtype)
     if rope is not None:
-        if rope.dtype is not torch.float32 or rope.dim() != 3 or rope.shape[2] != 2 or not rope.is_contiguous() or rope.get_device() != device:
-            raise ValueError(f"rope must be contiguous float32 [positions, dims / 2, 2] on cuda:{device}")
-        n, half, _ = rope.shape
-    if positions is not None and (positions.shape != (batch, m) or positions.dtype is not torch.int32 or not positions.is_contiguous() or positions.get_device() != device):
-        raise ValueError(f"positions must be contiguous int32 [{batch}, {m}] on cuda:{device}")
-    return device, x.dtype, gain.dtype, batch, m, 0 if q is None else q.shape[2], 0 if k is None else k.shape[2], d, n, half
+        _need(rope.dtype is torch.float32 and rope.dim() == 3 and rope.shape[2] == 2 and rope.is_contiguous() and rope.get_device() == device,
+              f"rope must be contiguous float32 [positions, dims / 2, 2] on cuda:{device}")
+    if positions is not None:
+        _need(positions.shape == x.shape[:2] and positions.dtype is torch.int32 and positions.is_contiguous() and positions.get_device() == device,
+              f"positions must be contiguous int32 {list(x.shape[:2])} on cuda:{device}")
+    raise ValueError("the arguments of norm_rotate do not go together")
 
 
-def _address(t):
-    return 0 if t is None else t.data_ptr()
+_NONE = 0, 0, 0, 0
 
 
-def _strides(t):
-    return (0, 0, 0) if t is None else t.stride()[:3]
+def _norm_layout(q, k, q_gain, k_gain, rope, positions):
+    """What goes into the arguments' structures, all of it looked at at once: (device, strides of q and of k, addresses, sizes and types)."""
+    x, gain = (q, q_gain) if q is not None else (k, k_gain)
+    if x is None or gain is None:
+        _refuse_norm(q, k, q_gain, k_gain, rope, positions)
+    shape, dtype, gain_dtype, device = x.shape, x.dtype, gain.dtype, x.get_device()
+    ok = len(shape) == 4 and dtype in _DTYPES and gain_dtype in _DTYPES and device == _current_device()
+    heads = kv_heads = n = half = to_q = to_k = to_qg = to_kg = to_rope = to_at = 0
+    qs = ks = _NONE
+    if ok:
+        batch, m, _, d = shape
+        if q is not None:
+            qs, heads, to_q, to_qg = q.stride(), shape[2], q.data_ptr(), q_gain.data_ptr()
+            ok = qs[3] == 1 and q_gain.shape == (d,) and q_gain.stride(0) == 1 and q_gain.get_device() == device
+        if k is not None and k_gain is not None:
+            ks, other, to_k, to_kg = k.stride(), k.shape, k.data_ptr(), k_gain.data_ptr()
+            ok = (ok and len(other) == 4 and other[0] == batch and other[1] == m and other[3] == d and ks[3] == 1 and k.dtype is dtype and k.get_device() == device and
+                  k_gain.shape == (d,) and k_gain.stride(0) == 1 and k_gain.dtype is gain_dtype and k_gain.get_device() == device)
+            kv_heads = other[2] if ok else 0
+        elif k is not None or k_gain is not None:
+            ok = False
+        if rope is not None:
+            r = rope.shape
+            ok = ok and len(r) == 3 and r[2] == 2 and rope.dtype is torch.float32 and rope.is_contiguous() and rope.get_device() == device
+            if ok:
+                n, half, to_rope = r[0], r[1], rope.data_ptr()
+        if positions is not None:
+            ok = ok and positions.shape == (batch, m) and positions.dtype is torch.int32 and positions.is_contiguous() and positions.get_device() == device
+            to_at = positions.data_ptr()
+    if not ok:
+        _refuse_norm(q, k, q_gain, k_gain, rope, positions)
+    return device, qs, ks, (to_q, to_k, to_qg, to_kg, to_at, to_rope), (batch, m, heads, kv_heads, d, _DTYPES[dtype], _DTYPES[gain_dtype], n, 2 * half)
 
 
 def _norm_forward(q, k, q_gain, k_gain, rope, positions, eps, interleaved):
-    device, dtype, gain_dtype, batch, m, heads, kv_heads, d, n, half = _norm_layout(q, k, q_gain, k_gain, rope, positions)
-    q_out, k_out = (None if t is None else torch.empty(t.shape, dtype=dtype, device=t.device) for t in (q, k))
+    device, qs, ks, (to_q, to_k, to_qg, to_kg, to_at, to_rope), sizes = _norm_layout(q, k, q_gain, k_gain, rope, positions)
+    q_out = k_out = None
+    os = us = _NONE
+    to_qo = to_ko = 0
+    if q is not None:
+        q_out = torch.empty_like(q)
+        os, to_qo = q_out.stride(), q_out.data_ptr()
+    if k is not None:
+        k_out = torch.empty_like(k)
+        us, to_ko = k_out.stride(), k_out.data_ptr()
     try:
-        args = _NORM.pack(_address(q), _address(k), _address(q_out), _address(k_out), _address(q_gain), _address(k_gain), _address(positions), _address(rope),
-                          *_strides(q), *_strides(k), *_strides(q_out), *_strides(k_out), batch, m, heads, kv_heads, d, _DTYPES[dtype], _DTYPES[gain_dtype], n, 2 * half,
-                          interleaved, eps)
+        args = _NORM.pack(to_q, to_k, to_qo, to_ko, to_qg, to_kg, to_at, to_rope, qs[0], qs[1], qs[2], ks[0], ks[1], ks[2], os[0], os[1], os[2], us[0], us[1], us[2],
+                          *sizes, interleaved, eps)
     except _BEYOND as e:
         raise ValueError(f"an argument of norm_rotate is beyond its type: {e}") from None
     status = binding.load().xsm_norm_rotate(args, _raw_stream(device))
@@ -784,23 +845,32 @@ def norm_rotate_grad(q, k, q_gain, k_gain, grad_q, grad_k, rope=None, positions=
     beside what was not there.  There are no second derivatives: tensors that want a gradient are refused unless torch.no_grad() says that it is not
     needed."""
     _no_gradient("norm_rotate_grad", q, k, q_gain, k_gain, rope, grad_q, grad_k)
-    device, dtype, gain_dtype, batch, m, heads, kv_heads, d, n, half = _norm_layout(q, k, q_gain, k_gain, rope, positions)
-    for t, g in ((q, grad_q), (k, grad_k)):
-        if (t is None) != (g is None) or t is not None and (g.shape != t.shape or g.dtype is not dtype or g.get_device() != device or g.stride(3) != 1):
-            raise ValueError("grad_q and grad_k must be like q and k, with neighbouring elements of a head")
-    d_q, d_k = (None if t is None else torch.empty(t.shape, dtype=dtype, device=t.device) for t in (q, k))
-    d_q_gain, d_k_gain = (None if t is None else torch.empty(d, dtype=gain_dtype, device=t.device) for t in (q_gain, k_gain))
-    lib = binding.load()
-    size = lib.xsm_norm_rotate_grad_workspace(d)
-    ws = _empty((size,), (1,), dtype=torch.uint8, device=q_gain.device if q_gain is not None else k_gain.device)
+    device, qs, ks, (to_q, to_k, to_qg, to_kg, to_at, to_rope), sizes = _norm_layout(q, k, q_gain, k_gain, rope, positions)
+    stream = _raw_stream(device)
+    d_q = d_k = d_q_gain = d_k_gain = None
+    gs = hs = os = us = _NONE
+    to_g = to_h = to_dq = to_dk = to_dqg = to_dkg = 0
+    ok = (q is None) == (grad_q is None) and (k is None) == (grad_k is None)
+    if ok and q is not None:
+        gs = grad_q.stride()
+        ok = grad_q.shape == q.shape and grad_q.dtype is q.dtype and grad_q.get_device() == device and gs[3] == 1
+        d_q, d_q_gain = torch.empty_like(q), torch.empty_like(q_gain)
+        os, to_g, to_dq, to_dqg = d_q.stride(), grad_q.data_ptr(), d_q.data_ptr(), d_q_gain.data_ptr()
+    if ok and k is not None:
+        hs = grad_k.stride()
+        ok = grad_k.shape == k.shape and grad_k.dtype is k.dtype and grad_k.get_device() == device and hs[3] == 1
+        d_k, d_k_gain = torch.empty_like(k), torch.empty_like(k_gain)
+        us, to_h, to_dk, to_dkg = d_k.stride(), grad_k.data_ptr(), d_k.data_ptr(), d_k_gain.data_ptr()
+    if not ok:
+        raise ValueError("grad_q and grad_k must be like q and k, with neighbouring elements of a head")
+    size = _size_of("xsm_norm_rotate_grad_workspace", sizes[4])
+    ws = _scratch(size, device, stream, d_q.device if q is not None else d_k.device)
     try:
-        args = _NORM_GRAD.pack(_address(q), _address(k), _address(q_gain), _address(k_gain), _address(positions), _address(rope), _address(grad_q), _address(grad_k),
-                               _address(d_q), _address(d_k), _address(d_q_gain), _address(d_k_gain), ws.data_ptr(), *_strides(q), *_strides(k), *_strides(grad_q),
-                               *_strides(grad_k), *_strides(d_q), *_strides(d_k), size, batch, m, heads, kv_heads, d, _DTYPES[dtype], _DTYPES[gain_dtype], n, 2 * half,
-                               interleaved, eps)
+        args = _NORM_GRAD.pack(to_q, to_k, to_qg, to_kg, to_at, to_rope, to_g, to_h, to_dq, to_dk, to_dqg, to_dkg, ws.data_ptr(), qs[0], qs[1], qs[2], ks[0], ks[1], ks[2],
+                               gs[0], gs[1], gs[2], hs[0], hs[1], hs[2], os[0], os[1], os[2], us[0], us[1], us[2], size, *sizes, interleaved, eps)
     except _BEYOND as e:
         raise ValueError(f"an argument of norm_rotate_grad is beyond its type: {e}") from None
-    status = lib.xsm_norm_rotate_grad(args, _raw_stream(device))
+    status = binding.load().xsm_norm_rotate_grad(args, stream)
     if status:
         _check(status)
     return d_q, d_k, d_q_gain, d_k_gain
