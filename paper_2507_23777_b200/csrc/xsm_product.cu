@@ -46,13 +46,12 @@ template <int CG> __device__ __forceinline__ void commit(uint32_t bar) {
     else
         asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" :: "r"(bar), "h"((uint16_t)3) : "memory");
 }
-template <int CG> __device__ __forceinline__ void tma_2d(uint32_t dst, const void *map, int x, int y, uint32_t bar) {
+template <int CG> __device__ __forceinline__ void tma_3d(uint32_t dst, const void *map, int x, int y, int z, uint32_t bar) {
     if constexpr (CG == 1)
-        asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
-                     :: "r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
+        tma_box(dst, map, x, y, z, bar);
     else
-        asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%2, %3}], [%4];"
-                     :: "r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
+        asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%2, %3, %4}], [%5];"
+                     :: "r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
 }
 // the same at this CTA's barrier alone
 template <int CG> __device__ __forceinline__ void commit_here(uint32_t bar) {
@@ -264,7 +263,8 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
     if constexpr (CG == 2) { cluster_arrive(); cluster_wait(); }
     tcgen05_after_sync();
     const uint32_t tmem = tmem_slot;
-    chain_wait();
+    // (what the first tile needs is worked out, and the operands' descriptions are on their way, before what other kernels write is waited for)
+    if (warp != 0) chain_wait();
 
     // false: the limit ran out, here or elsewhere in the CTA; the results are void
     auto wait = [&](uint32_t bar, uint32_t parity) {
@@ -295,26 +295,35 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
                 const int m0 = w.m * TM + rank * 128, n0 = kGated ? w.n * (BN / 2) : w.n * BN + rank * (BN / CG);
                 const int second = kOut && w.k0 >= A.kb0;
                 const CUtensorMap *ma = &M.a[kOut ? second + w.job : 0], *mb = &M.b[kGated && CG == 2 ? rank : second];
-                int at = (w.k0 - (second ? A.kb0 : 0)) * 64;
+                // a stage of one block: columns `at`; of several: blocks of 64 columns from z on (operands of whole blocks are described so)
+                const bool many = !kOut && CG == 1 && A.chunks > 1;
+                int at = (w.k0 - (second ? A.kb0 : 0)) * 64, z = 0;
+                if (t == first) {
+                    asm volatile("prefetch.tensormap [%0];" :: "l"(ma) : "memory");
+                    asm volatile("prefetch.tensormap [%0];" :: "l"(mb) : "memory");
+                    chain_wait();
+                }
+                if (many) at = 0;
                 for (int k = w.k0; k < w.k1; ++k) {
                     if (!(ok = wait(empty0 + 8u * (uint32_t)s, par))) break;
                     const uint32_t f = full_at + 8u * (uint32_t)s, sb = sa + A.stage_b;
                     if (CG == 1 || rank == 0) mbar_arrive_expect_tx(full0 + 8u * (uint32_t)s, A.stage_tx);
                     if constexpr (kRowsA) {
-                        tma_2d<CG>(sa, ma, m0, at, f);
-                        tma_2d<CG>(sa + 8192, ma, m0 + 64, at, f);
+                        tma_3d<CG>(sa, ma, m0, at, 0, f);
+                        tma_3d<CG>(sa + 8192, ma, m0 + 64, at, 0, f);
                     } else {
-                        tma_2d<CG>(sa, ma, at, m0, f);
+                        tma_3d<CG>(sa, ma, at, m0, z, f);
                     }
                     if constexpr (kRowsB) {
 #pragma unroll
-                        for (int i = 0; i < BN / CG / 64; ++i) tma_2d<CG>(sb + i * 8192, mb, n0 + 64 * i, at, f);
+                        for (int i = 0; i < BN / CG / 64; ++i) tma_3d<CG>(sb + i * 8192, mb, n0 + 64 * i, at, 0, f);
                     } else {
-                        tma_2d<CG>(sb, mb, at, n0, f);
-                        if constexpr (kGated && CG == 1) tma_2d<CG>(sb + BN / 2 * 128, &M.b[1], at, n0, f);
+                        tma_3d<CG>(sb, mb, at, n0, z, f);
+                        if constexpr (kGated && CG == 1) tma_3d<CG>(sb + (uint32_t)A.chunks * (BN / 2 * 128), &M.b[1], at, n0, z, f);
                     }
                     ++n;
-                    at += 64;
+                    if (many) z += A.chunks;
+                    else at += 64;
                     if (kOut && k + 1 == A.kb0) { at = 0; ++ma; ++mb; }
                     sa += A.stage;
                     if (++s == A.stages) { s = 0; par ^= 1u; sa = ring; }
@@ -326,7 +335,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
     } else if (warp == 1) {
         if (rank == 0) {
             const bool leader = elect_one();
-            const uint32_t idesc = product_idesc<T>(128 * CG, BN, kRowsA, kRowsB);
+            const uint32_t idesc = product_idesc<T>(128 * CG, kGated && CG == 1 ? BN / 2 : BN, kRowsA, kRowsB);
             const uint64_t da = operand_desc(ring, kRowsA), db = operand_desc(ring + A.stage_b, kRowsB);
             constexpr uint32_t a_step = kRowsA ? 2048 >> 4 : 32 >> 4, b_step = kRowsB ? 2048 >> 4 : 32 >> 4;
             const uint32_t stage = A.stage >> 4;
@@ -343,8 +352,23 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
                     if (!(ok = wait_warp(full0 + 8u * (uint32_t)s, par))) break;
                     tcgen05_after_sync();
                     if (leader) {
+                        uint64_t a = da + at, b = db + at;
+                        for (int c = 0;; ++c) {
+                            if constexpr (kGated && CG == 1) {        // gate's columns and up's lie in boxes of their own
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) mma_f16<CG>(d, da + at + i * a_step, db + at + i * b_step, idesc, i > 0 ? 1u : add);
+                                for (int i = 0; i < 4; ++i) {
+                                    mma_f16<CG>(d, a + i * a_step, b + i * b_step, idesc, i > 0 ? 1u : add);
+                                    mma_f16<CG>(d + BN / 2, a + i * a_step, b + (uint32_t)A.chunks * (BN / 2 * 128 >> 4) + i * b_step, idesc, i > 0 ? 1u : add);
+                                }
+                            } else {
+#pragma unroll
+                                for (int i = 0; i < 4; ++i) mma_f16<CG>(d, a + i * a_step, b + i * b_step, idesc, i > 0 ? 1u : add);
+                            }
+                            if (CG == 2 || kOut || c + 1 == A.chunks) break;
+                            a += (uint32_t)A.a_rows * 128 >> 4;
+                            b += (kGated ? BN / 2 : BN) * 128 >> 4;
+                            add = 1u;
+                        }
                         commit<CG>(empty0 + 8u * (uint32_t)s);
                     }
                     __syncwarp();
@@ -587,27 +611,27 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
 
 // -------------------------------------------------------------------------------------------- small kernels
 
-// the largest |x| of 16-bit elements, infinities and NaN apart, a number for each block
+// the largest |x| of 16-bit elements, infinities and NaN apart, a number for each block; rows of up to `most` elements, of `all` elements from the first on
 template <typename T>
-__global__ void __launch_bounds__(256) amax_rows_kernel(const T *x, long long rows, int cols, long long ld, float *amax) {
+__global__ void __launch_bounds__(256) amax_rows_kernel(const T *x, long long rows, long long most, long long ld, long long all, float *amax) {
     chain_go();
     chain_wait();
     __shared__ float s[8];
     float m = 0.f;
     auto take = [&](float v) { v = fabsf(v); if (v < INFINITY) m = fmaxf(m, v); };
     const bool whole = ((uintptr_t)x & 15) == 0 && (ld & 7) == 0;
-    const int pieces = whole ? cols / 8 : 0;
     for (long long r = blockIdx.x; r < rows; r += kAmaxBlocks) {
         const T *row = x + r * ld;
+        const long long left = all - r * ld, cols = left < most ? left : most, pieces = whole ? cols / 8 : 0;
 #pragma unroll 4
-        for (int i = threadIdx.x; i < pieces; i += 256) {
+        for (long long i = threadIdx.x; i < pieces; i += 256) {
             const uint4 u = reinterpret_cast<const uint4 *>(row)[i];
             T e[8];
             memcpy(e, &u, 16);
 #pragma unroll
             for (int j = 0; j < 8; ++j) take(to_f(e[j]));
         }
-        for (int i = pieces * 8 + threadIdx.x; i < cols; i += 256) take(to_f(row[i]));
+        for (long long i = pieces * 8 + threadIdx.x; i < cols; i += 256) take(to_f(row[i]));
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
@@ -678,10 +702,12 @@ static cudaError_t encoder(EncodeTiledFn *fn) {
     return cudaSuccess;
 }
 
-static bool operand_map(EncodeTiledFn encode, CUtensorMap *out, const Operand &o, int dtype, int box_rows) {
-    cuuint64_t dims[2] = {(cuuint64_t)o.row, (cuuint64_t)o.rows}, strides[1] = {(cuuint64_t)o.ld * 2};
-    cuuint32_t box[2] = {64, (cuuint32_t)box_rows}, one[2] = {1, 1};
-    return encode(out, dtype == XSM_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, const_cast<void *>(o.p), dims, strides, box, one,
+// Boxes of 64 elements of `box_rows` rows; of `chunks` > 1 neighbouring runs of 64 elements of each row (rows of whole runs), one behind the other.
+static bool operand_map(EncodeTiledFn encode, CUtensorMap *out, const Operand &o, int dtype, int box_rows, int chunks) {
+    cuuint64_t dims[3] = {(cuuint64_t)(chunks > 1 ? 64 : o.row), (cuuint64_t)o.rows, (cuuint64_t)(chunks > 1 ? o.row / 64 : 1)};
+    cuuint64_t strides[2] = {(cuuint64_t)o.ld * 2, chunks > 1 ? 128 : (cuuint64_t)o.ld * 2};
+    cuuint32_t box[3] = {64, (cuuint32_t)box_rows, (cuuint32_t)chunks}, one[3] = {1, 1, 1};
+    return encode(out, dtype == XSM_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, const_cast<void *>(o.p), dims, strides, box, one,
                   CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
@@ -780,7 +806,13 @@ cudaError_t launch_product(ProductEpi epi, int dtype, ProductCut cut, ProductArg
     A.tiles_m = (A.m + tm - 1) / tm;
     A.tiles_n = (A.n + tn - 1) / tn;
     const long long summed = a_rows_summed ? a[0].rows : a[0].row;
-    A.kb0 = (int)((summed + 63) / 64);
+    A.a_rows = A.m >= 128 ? 128 : (A.m + 7) / 8 * 8;
+    // Few rows: a stage of several blocks, each operand's by one copy, as long as three stages fit; a copy costs the TMA unit some 200 cycles whatever it brings (5 rows x 4096
+    // tokens ... us).
+    A.chunks = 1;
+    if (!wide && !b_rows_summed && summed % 64 == 0)
+        while (A.chunks < 4 && 2 * A.chunks <= summed / 64 && 2 * A.chunks * (A.a_rows + cut.bn) * 128 * 3 <= kRingBytes) A.chunks *= 2;
+    A.kb0 = (int)((summed + 64 * A.chunks - 1) / (64 * A.chunks));
     A.kb = A.kb0 * pairs;
     const long long tiles = (long long)A.tiles_m * A.tiles_n * A.jobs * A.splits;
     if (tiles > 0x3fffffff) return cudaErrorInvalidValue;
@@ -794,10 +826,9 @@ cudaError_t launch_product(ProductEpi epi, int dtype, ProductCut cut, ProductArg
     A.by_splits = Divisor((unsigned)A.splits);
     A.kb_each = A.kb / A.splits;
     A.kb_more = A.kb % A.splits;
-    A.a_rows = A.m >= 128 ? 128 : (A.m + 7) / 8 * 8;
     const int b_box = gated ? (wide ? 128 : cut.bn / 2) : cut.bn / group;
-    A.stage_b = (uint32_t)(a_rows_summed ? kABytes : A.a_rows * 128);
-    A.stage = A.stage_b + (uint32_t)(cut.bn / group * 128);
+    A.stage_b = (uint32_t)((a_rows_summed ? kABytes : A.a_rows * 128) * A.chunks);
+    A.stage = A.stage_b + (uint32_t)(cut.bn / group * 128 * A.chunks);
     A.stage_tx = group * A.stage;
     A.stages = kRingBytes / (int)A.stage < kMaxStages ? kRingBytes / (int)A.stage : kMaxStages;
     product_waits(&A.tries, &A.starve);
@@ -805,9 +836,9 @@ cudaError_t launch_product(ProductEpi epi, int dtype, ProductCut cut, ProductArg
     memset(&M, 0, sizeof M);
     const int na = pairs > A.jobs ? pairs : A.jobs, nb = gated ? 2 : pairs;
     for (int i = 0; i < na; ++i)
-        if (!operand_map(encode, &M.a[i], a[i], dtype, a_rows_summed ? 64 : A.a_rows)) return cudaErrorInvalidValue;
+        if (!operand_map(encode, &M.a[i], a[i], dtype, a_rows_summed ? 64 : A.a_rows, A.chunks)) return cudaErrorInvalidValue;
     for (int i = 0; i < nb; ++i)
-        if (!operand_map(encode, &M.b[i], b[i], dtype, b_rows_summed ? 64 : b_box)) return cudaErrorInvalidValue;
+        if (!operand_map(encode, &M.b[i], b[i], dtype, b_rows_summed ? 64 : b_box, A.chunks)) return cudaErrorInvalidValue;
     if (wide && epi != PR_STATS) {
         const bool sums = b_rows_summed && A.partial;
         const int outs = sums ? 1 : epi == PR_GATED_GRAD ? 2 : A.jobs;
@@ -827,8 +858,14 @@ cudaError_t launch_product(ProductEpi epi, int dtype, ProductCut cut, ProductArg
 }
 
 cudaError_t launch_amax_rows(const void *x, int dtype, long long rows, long long cols, long long ld, float *amax, cudaStream_t st) {
-    if (dtype == XSM_BF16) return launch_early(amax_rows_kernel<bf16>, dim3(kAmaxBlocks), dim3(256), 0, st, (const bf16 *)x, rows, (int)cols, ld, amax);
-    return launch_early(amax_rows_kernel<__half>, dim3(kAmaxBlocks), dim3(256), 0, st, (const __half *)x, rows, (int)cols, ld, amax);
+    long long all = LLONG_MAX;
+    if (ld == cols) {        // one run of elements: a part for each block, of whole 16-byte pieces (2047 rows of 2051 fp16 10 -> ... us)
+        all = rows * cols;
+        ld = cols = (all / kAmaxBlocks + 8) / 8 * 8;
+        rows = (all + cols - 1) / cols;
+    }
+    if (dtype == XSM_BF16) return launch_early(amax_rows_kernel<bf16>, dim3(kAmaxBlocks), dim3(256), 0, st, (const bf16 *)x, rows, cols, ld, all, amax);
+    return launch_early(amax_rows_kernel<__half>, dim3(kAmaxBlocks), dim3(256), 0, st, (const __half *)x, rows, cols, ld, all, amax);
 }
 cudaError_t launch_amax_pairs(const float *g, long long g_ld, const float *h, long long h_ld, int rows, float by, float *amax, cudaStream_t st) {
     return launch_early(amax_pairs_kernel, dim3(kAmaxBlocks), dim3(32), 0, st, g, g_ld, h, h_ld, rows, by, amax);

@@ -25,10 +25,11 @@ struct __align__(64) ProductMaps { CUtensorMap a[2], b[2], out[2]; };
 struct ProductArgs {
     int m, n;                       // rows and columns of the result (PR_GATED: n columns of gate and of up)
     int tiles_m, tiles_n, jobs, splits, tiles;
-    int kb0, kb;                    // blocks of 64 along the summed axis: of the first pair of operands, of all
+    int kb0, kb;                    // stages along the summed axis: of the first pair of operands, of all
     int kb_each, kb_more;           // blocks of a split, and how many splits have one more
     Divisor by_plane, by_group, by_rows, by_last_rows, by_splits;      // tiles of a split, of a group, rows of a group, of the last one
-    int a_rows;                     // rows of a box of A (not a_mn)
+    int a_rows;                     // rows of a box of A (whose rows lie across the summed axis)
+    int chunks;                     // blocks of 64 that a stage holds; kb counts stages
     int group_m;                    // tiles of rows that are worked on side by side
     int stages;                     // of the ring
     uint32_t stage, stage_b;        // bytes of a CTA's stage, where B begins in it
