@@ -559,7 +559,7 @@ static cudaError_t launch_norm(const NormArgs &A, const Pages &P, int blocks, bo
     auto go = [&](auto l) {
         constexpr int L = decltype(l)::value, slots = NormSlots<MODE>::bytes, sums = MODE == NM_GRAD ? kNormThreads / L * (32 / (int)sizeof(TI) * L + 1) * 4 : 0, smem = slots > sums ? slots : sums;
         const void *fn = near ? (const void *)norm_kernel<TI, TC, L, true, MODE> : (const void *)norm_kernel<TI, TC, L, false, MODE>;
-        const cudaError_t e = smem > 48 * 1024 ? open_kernel(fn, smem, false) : cudaSuccess;
+        const cudaError_t e = smem > 48 * 1024 ? open_for(fn, smem) : cudaSuccess;
         if (e != cudaSuccess) return e;
         return near ? launch_early(norm_kernel<TI, TC, L, true, MODE>, dim3(blocks), dim3(kNormThreads), smem, st, A, P)
                     : launch_early(norm_kernel<TI, TC, L, false, MODE>, dim3(blocks), dim3(kNormThreads), smem, st, A, P);

@@ -28,6 +28,16 @@ inline xsm_status launched(cudaError_t e) noexcept {
 inline int element_size(int dtype) { return dtype == XSM_F32 ? 4 : 2; }
 inline bool is_dtype(int dtype) { return dtype == XSM_F32 || dtype == XSM_BF16 || dtype == XSM_F16; }
 
+// open_kernel, for callers of a C entry: what it keeps its notes in may run out of memory
+cudaError_t open_kernel(const void *fn, int smem, bool large_cluster);
+inline cudaError_t open_for(const void *fn, int smem) noexcept {
+    try {
+        return open_kernel(fn, smem, false);
+    } catch (...) {
+        return cudaErrorMemoryAllocation;
+    }
+}
+
 // The pools as the kernels see them.
 struct Pages {
     char *k, *v;

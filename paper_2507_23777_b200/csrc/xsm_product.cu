@@ -751,7 +751,7 @@ int product_splits(long long tiles, int kb, bool wide) {
 template <int CG, int BN, int EPI, typename T> static cudaError_t start(const ProductMaps &M, const ProductArgs &A, cudaStream_t st) {
     const int smem = kRingBytes + (CG == 2 ? kEpiWarps * 4096 : kABytes) + 1024;        // (few rows: the tensor cores read 128 rows of A whatever the box brought)
     const void *fn = (const void *)product_kernel<CG, BN, EPI, T>;
-    cudaError_t e = open_kernel(fn, smem, false);
+    cudaError_t e = open_for(fn, smem);
     if (e != cudaSuccess) return e;
     if (product_sms() < 2) return cudaErrorInvalidDevice;
     cudaLaunchConfig_t cfg = {};

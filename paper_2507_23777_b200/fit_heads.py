@@ -40,10 +40,11 @@ def _views(cfg: dict, Wf):
     return W
 
 
-def backbone_hidden(cfg: dict, Wf, tokens: np.ndarray, cond: np.ndarray, device="cuda"):
+def backbone_hidden(cfg: dict, Wf, tokens: np.ndarray, cond: np.ndarray, device="cuda", library_products=False):
     """Final hidden states g_s = RMSNorm_f(h^N_s) of a whole token sequence under the causal mask (Eq. 1; block
     order and norms as in Sec. 4.1 and the library header): tensor [len(tokens), d_model] on `device`.
-    Wf: all weights as one fp32 tensor on `device`."""
+    Wf: all weights as one fp32 tensor on `device`.  library_products: the gated feed-forward parts by the library's operator (ops.gated_feed_forward, a GPU is needed), on
+    activations and weights that are rounded to bf16."""
     import torch
     import torch.nn.functional as F
     W = _views(cfg, Wf)
@@ -79,14 +80,20 @@ def backbone_hidden(cfg: dict, Wf, tokens: np.ndarray, cond: np.ndarray, device=
             kc, vc = (c @ W(p + "Wkc").T).view(-1, H, dh), (c @ W(p + "Wvc").T).view(-1, H, dh)
             h = h + attend((u @ W(p + "Wqc").T).view(n, H, dh), kc, vc, False) @ W(p + "Woc").T
             u = rms(h, W(p + "g3"))
-            h = h + (F.silu(u @ W(p + "Wgate").T) * (u @ W(p + "Wup").T)) @ W(p + "Wdown").T
+            if library_products:
+                from . import ops
+                y = ops.gated_feed_forward(u.bfloat16(), W(p + "Wgate").bfloat16(), W(p + "Wup").bfloat16()).float()
+            else:
+                y = F.silu(u @ W(p + "Wgate").T) * (u @ W(p + "Wup").T)
+            h = h + y @ W(p + "Wdown").T
         return rms(h, W("gf"))
 
 
 def fit_from_corpus(cfg: dict, weights: np.ndarray, seqs, conds, iters=300, lr=2e-5, eval_every=25, holdout=0.125,
-                    batch=4096, device="cuda", seed=0, library_loss=False):
+                    batch=4096, device="cuda", seed=0, library_loss=False, library_products=False):
     """seqs[i]: tokens x_0.. of mesh i (x_0 = BOS) generated by the backbone, conds[i]: its condition [C, d_cond].
-    library_loss: cross-entropy and its gradient by the library's operator (ops.token_logprobs, a GPU is needed) instead of torch's.
+    library_loss: cross-entropy and its gradient by the library's operator (ops.token_logprobs, a GPU is needed) instead of torch's.  library_products: the backbone's gated
+    feed-forward parts, and the loss straight from the heads' hidden states without logits (ops.linear_logprobs), by the library's operators in bf16.
     Returns (weights with fitted heads, report)."""
     import torch
     import torch.nn.functional as F
@@ -95,7 +102,7 @@ def fit_from_corpus(cfg: dict, weights: np.ndarray, seqs, conds, iters=300, lr=2
     torch.manual_seed(seed)
     Wf = torch.from_numpy(inputs.weights_as_f32(cfg, weights).astype(np.float32, copy=True)).to(device)
     W = _views(cfg, Wf)
-    G = [backbone_hidden(cfg, Wf, s[:-1], c, device) for s, c in zip(seqs, conds)]
+    G = [backbone_hidden(cfg, Wf, s[:-1], c, device, library_products) for s, c in zip(seqs, conds)]
     X = [torch.as_tensor(np.asarray(s, dtype=np.int64), device=device) for s in seqs]
 
     def dataset(idx):       # input g_s; target of head d (1..K): x_{s+d+1}
@@ -114,8 +121,11 @@ def fit_from_corpus(cfg: dict, weights: np.ndarray, seqs, conds, iters=300, lr=2
     Wo = [W("W0").clone().requires_grad_(True) for _ in range(K)]
     opt = torch.optim.AdamW(W1 + Wo, lr=lr, weight_decay=0.0)
 
+    def states(g, i):
+        return g + F.silu(g @ W1[i].T)
+
     def head(g, i):
-        return (g + F.silu(g @ W1[i].T)) @ Wo[i].T
+        return states(g, i) @ Wo[i].T
 
     if library_loss:
         from . import ops
@@ -125,8 +135,17 @@ def fit_from_corpus(cfg: dict, weights: np.ndarray, seqs, conds, iters=300, lr=2
     else:
         entropy_of = F.cross_entropy
 
+    if library_products:
+        from . import ops
+
+        def loss_of_head(g, i, t):
+            return -ops.linear_logprobs(states(g, i).bfloat16(), Wo[i].bfloat16(), t).logprob.mean()
+    else:
+        def loss_of_head(g, i, t):
+            return entropy_of(head(g, i), t)
+
     def loss_of(g, y):      # Eq. 5 with w(d) = 0.8^d
-        return sum(0.8 ** (i + 1) * entropy_of(head(g, i), y[:, i]) for i in range(K))
+        return sum(0.8 ** (i + 1) * loss_of_head(g, i, y[:, i]) for i in range(K))
 
     curve, best, best_state, best_it = [], None, None, 0
     for it in range(iters + 1):
@@ -144,6 +163,8 @@ def fit_from_corpus(cfg: dict, weights: np.ndarray, seqs, conds, iters=300, lr=2
         opt.zero_grad()
         loss.backward()
         opt.step()
+    if library_products:
+        ops.check()
     out = inputs.weights_as_f32(cfg, weights).astype(np.float32, copy=True)
     offs = inputs.weight_offsets(cfg)
     for i in range(K):
@@ -196,13 +217,14 @@ def main():
     ap.add_argument("--iters", type=int, default=300)
     ap.add_argument("--lr", type=float, default=2e-5)
     ap.add_argument("--library-loss", action="store_true", help="cross-entropy and its gradient by the library's operator")
+    ap.add_argument("--library-products", action="store_true", help="gated feed-forward parts, and the loss without logits, by the library's operators in bf16")
     ap.add_argument("--eval-tokens", type=int, default=4096)
     ap.add_argument("--eval-seeds", type=int, nargs="*", default=None, help="mesh seeds to decode (default: the configuration's)")
     args = ap.parse_args()
     build.build()
     cfg = inputs.config(args.config)
     w = inputs.make_weights(cfg)
-    fitted, report = fit(cfg, w, args.meshes, args.tokens, iters=args.iters, lr=args.lr, library_loss=args.library_loss)
+    fitted, report = fit(cfg, w, args.meshes, args.tokens, iters=args.iters, lr=args.lr, library_loss=args.library_loss, library_products=args.library_products)
     report.pop("curve")
     print(json.dumps({"fit": report}))
     cfg0 = dict(cfg, n_draft=0)

@@ -204,8 +204,9 @@ class PagedCache:
               f"lse must be contiguous float32 {n} on cuda:{self.device}")
         raise ValueError("the arguments of attend do not go together")
 
-    def _gains(self, q, q_gain, k_gain, eps):
+    def _gains(self, q, q_gain, k_gain, eps, rope):
         """The norm of an append as the library takes it."""
+        _need(rope is None or rope.numel() > 0, "rope must not be empty")
         _need(k_gain is not None and (q is None) == (q_gain is None), "gains go together: k_gain, and q_gain where there is q")
         for g in (k_gain, q_gain):
             if g is not None:
@@ -225,7 +226,7 @@ class PagedCache:
         want one unless torch.no_grad() says that it is not needed."""
         gains = None
         if k_gain is not None or q_gain is not None:
-            gains = self._gains(q, q_gain, k_gain, eps)
+            gains = self._gains(q, q_gain, k_gain, eps, rope)
         if _grad_enabled() and (k.requires_grad or v.requires_grad or q is not None and q.requires_grad or rope is not None and rope.requires_grad or
                                         out is not None and out.requires_grad):
             raise ValueError("append has no gradient: call it under torch.no_grad()")
@@ -773,8 +774,8 @@ def _refuse_norm(q, k, q_gain, k_gain, rope, positions):
                   "q and k must have the same batch, tokens, d_head, type and device, and neighbouring elements of a head")
             _need_gain(g, x.shape[3], device, gain.dtype)
     if rope is not None:
-        _need(rope.dtype is torch.float32 and rope.dim() == 3 and rope.shape[2] == 2 and rope.is_contiguous() and rope.get_device() == device,
-              f"rope must be contiguous float32 [positions, dims / 2, 2] on cuda:{device}")
+        _need(rope.dtype is torch.float32 and rope.dim() == 3 and rope.shape[2] == 2 and rope.numel() > 0 and rope.is_contiguous() and rope.get_device() == device,
+              f"rope must be contiguous float32 [positions, dims / 2, 2] on cuda:{device}, and not empty")
     if positions is not None:
         _need(positions.shape == x.shape[:2] and positions.dtype is torch.int32 and positions.is_contiguous() and positions.get_device() == device,
               f"positions must be contiguous int32 {list(x.shape[:2])} on cuda:{device}")
@@ -805,9 +806,11 @@ def _norm_layout(q, k, q_gain, k_gain, rope, positions):
             kv_heads = other[2] if ok else 0
         elif k is not None or k_gain is not None:
             ok = False
+        if q is None and q_gain is not None:
+            ok = False
         if rope is not None:
             r = rope.shape
-            ok = ok and len(r) == 3 and r[2] == 2 and rope.dtype is torch.float32 and rope.is_contiguous() and rope.get_device() == device
+            ok = ok and len(r) == 3 and r[2] == 2 and r[0] > 0 and r[1] > 0 and rope.dtype is torch.float32 and rope.is_contiguous() and rope.get_device() == device
             if ok:
                 n, half, to_rope = r[0], r[1], rope.data_ptr()
         if positions is not None:
