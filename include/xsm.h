@@ -364,6 +364,8 @@ typedef struct {
     float *logprob, *lse;                 /* DEVICE [rows] */
     void *workspace;
     int32_t *status;
+    uint32_t *counter;                    /* DEVICE, a word that is zero before its first use and after every call; calls that share one follow each other on one stream.
+                                             With it up to 16 rows take one kernel instead of two; may be NULL */
     int64_t hidden_stride, weight_stride, token_stride, workspace_bytes;
     int32_t rows, vocab, d, dtype, token_bytes;
     float temperature;

@@ -571,7 +571,8 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
                         mx = -INFINITY;
                         sum = 0.f;
                     } else if (t + step >= A.tiles && live) {
-                        A.parts[(long long)(2 * first + half) * A.m + row] = make_float2(mx, sum);
+                        if (A.counter) A.parts[(long long)row * 2 * gridDim.x + 2 * first + half] = make_float2(mx, sum);
+                        else A.parts[(long long)(2 * first + half) * A.m + row] = make_float2(mx, sum);
                     }
                 }
             }
@@ -600,6 +601,25 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
             for (unsigned n = 0; n < A.tries && !mbar_try_wait(smem_u32(&last), 0u); ++n);
         }
         __syncthreads();
+    }
+    if constexpr (EPI == PR_STATS && CG == 1) {
+        if (A.counter) {
+            __shared__ int last_of_all;
+            if (tid == 0) {
+                __threadfence();
+                last_of_all = atomicInc(A.counter, gridDim.x - 1) == gridDim.x - 1;        // (back to zero with the last)
+                __threadfence();
+            }
+            __syncthreads();
+            if (last_of_all)
+                for (int row = warp; row < A.m; row += kProductThreads / 32) {
+                    RowSums r;
+#pragma unroll 4
+                    for (int i = lane; i < 2 * (int)gridDim.x; i += 32) r.take(__ldcg(&A.parts[(long long)row * 2 * gridDim.x + i]));
+                    r.across_lanes();
+                    if (lane == 0) r.finish(A.tokens, A.token_ld, A.token_bytes, A.vocab, row, A.token_z, A.logprob, A.lse_out);
+                }
+        }
     }
     if constexpr (CG == 2) { cluster_arrive(); cluster_wait(); }        // (nobody leaves while the other CTA's barriers and memory are still in use)
     if (warp == 1) {

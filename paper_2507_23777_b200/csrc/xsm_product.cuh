@@ -46,6 +46,8 @@ struct ProductArgs {
     float c, inv_t;                 // log2(e) / T, 1 / T
     float2 *parts;                  // [part][m]: maximum, sum
     int carry;                      // one tile of rows: a CTA's parts are joined in its registers, parts are the CTAs'
+    unsigned *counter;              // with carry: the CTA that comes last joins the CTAs' parts, [m][part], itself
+    float *logprob, *lse_out;
     float *token_z;                 // [m]
     const float *lse, *g, *g_lse;
     long long g_ld, g_lse_ld;
@@ -60,6 +62,27 @@ struct ProductArgs {
     int amax_to;                    // the largest is scaled to [2^amax_to, 2^(amax_to + 1))
     float *partial;                 // PR_OUT: fp32 [job][split][m][n] instead of out, where it is not NULL
     int add;                        // to what partial holds
+};
+
+// A row's maximum (times log2(e) / T) and sum of exponentials, joined part by part.
+struct RowSums {
+    float m = -INFINITY, sum = 0.f;
+    __device__ __forceinline__ void take(float2 p) {
+        const float was = m;
+        m = fmaxf(m, p.x);
+        const float base = m == -INFINITY ? 0.f : m;
+        sum = sum * ex2(was - base) + p.y * ex2(p.x - base);
+    }
+    __device__ __forceinline__ void across_lanes() {
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) take(make_float2(__shfl_xor_sync(0xffffffffu, m, o), __shfl_xor_sync(0xffffffffu, sum, o)));
+    }
+    __device__ __forceinline__ void finish(const void *tokens, long long token_ld, int token_bytes, int vocab, int row, const float *token_z, float *logprob, float *lse) const {
+        const float l = m == -INFINITY && sum == 0.f ? -INFINITY : (m + log2f(sum)) * 0.69314718056f;
+        const long long t = token_bytes == 8 ? reinterpret_cast<const long long *>(tokens)[row * token_ld] : (long long)reinterpret_cast<const int *>(tokens)[row * token_ld];
+        lse[row] = l;
+        logprob[row] = t < 0 || t >= vocab ? 0.f : l == -INFINITY ? -INFINITY : __ldcg(token_z + row) - l;
+    }
 };
 
 // How a product is cut: `wide`: two CTAs share tiles of 256 x 256; otherwise a CTA has tiles of 128 x bn.  gated: half of the columns are gate's, half up's, and a

@@ -26,7 +26,7 @@ _APPEND = struct.Struct("8P13q8i")
 _ATTEND = struct.Struct("7P8q7if")
 _LOGPROB = struct.Struct("7P2q5if")
 _GRAD = struct.Struct("10P6q5if")
-_LINEAR = struct.Struct("7P4q5if")
+_LINEAR = struct.Struct("8P4q5if")
 _LINEAR_GRAD = struct.Struct("10P8q5if")
 _GATED = struct.Struct("5P4q5i")
 _GATED_GRAD = struct.Struct("9P7q5i")
@@ -96,7 +96,7 @@ def rope_table(n_positions: int, dims: int, theta: float = 10000.0, device="cuda
 
 class _Recorded:
     """The workspace of a graph's calls on one of its streams, outside of the graph's own memory: its status word outlasts a replay."""
-    __slots__ = "ws", "size", "outgrown", "watch", "__weakref__"
+    __slots__ = "ws", "size", "outgrown", "watch", "counter", "__weakref__"
 
 
 _recorded = {}       # of graphs that exist: _Recorded by (device, number of the capture, stream)
@@ -124,6 +124,19 @@ def _zeros_while_recording(n: int, device: int):
         finally:
             lib.xsm_capture_mode(before)
     return t
+
+
+def _recorded_on(device: int, stream: int):
+    """What belongs to the graph that is being recorded on the stream."""
+    key = device, binding.load().xsm_capture_id(stream), stream
+    r = _recorded.get(key)
+    if r is None:
+        _forget_graphs()
+        r = _Recorded()
+        r.ws, r.size, r.outgrown, r.watch, r.counter = None, 0, [], C.c_void_p(), None
+        _check(binding.load().xsm_capture_watch(stream, C.byref(r.watch)))
+        _recorded[key] = r
+    return r
 
 
 class PagedCache:
@@ -206,15 +219,22 @@ class PagedCache:
 
     def _gains(self, q, q_gain, k_gain, eps, rope):
         """The norm of an append as the library takes it."""
-        _need(rope is None or rope.numel() > 0, "rope must not be empty")
         _need(k_gain is not None and (q is None) == (q_gain is None), "gains go together: k_gain, and q_gain where there is q")
-        for g in (k_gain, q_gain):
-            if g is not None:
-                _need_gain(g, self.d_head, self.device, k_gain.dtype)
-                _need(not (_grad_enabled() and g.requires_grad), "append has no gradient: call it under torch.no_grad()")
-                _no_tangents(g)
+        dtype, d, device = k_gain.dtype, (self.d_head,), self.device
+        ok = k_gain.shape == d and dtype in _DTYPES and k_gain.stride(0) == 1 and k_gain.get_device() == device
+        if q_gain is not None:
+            ok = ok and q_gain.shape == d and q_gain.dtype is dtype and q_gain.stride(0) == 1 and q_gain.get_device() == device
+        if not ok:
+            for g in (k_gain, q_gain):
+                if g is not None:
+                    _need_gain(g, self.d_head, device, dtype)
+        _need(rope is None or rope.numel() > 0, "rope must not be empty")
+        if _grad_enabled() and (k_gain.requires_grad or q_gain is not None and q_gain.requires_grad):
+            raise ValueError("append has no gradient: call it under torch.no_grad()")
+        if forward_ad._current_level >= 0:
+            _no_tangents(k_gain, q_gain)
         try:
-            return _HEAD_NORM.pack(0 if q_gain is None else q_gain.data_ptr(), k_gain.data_ptr(), _DTYPES[k_gain.dtype], eps)
+            return _HEAD_NORM.pack(0 if q_gain is None else q_gain.data_ptr(), k_gain.data_ptr(), _DTYPES[dtype], eps)
         except _BEYOND as e:
             raise ValueError(f"an argument of append is beyond its type: {e}") from None
 
@@ -294,14 +314,7 @@ class PagedCache:
         return ws, size
 
     def _workspace_of_graph(self, stream: int, need: int):
-        key = self.device, self.lib.xsm_capture_id(stream), stream
-        r = _recorded.get(key)
-        if r is None:
-            _forget_graphs()
-            r = _Recorded()
-            r.ws, r.size, r.outgrown, r.watch = None, 0, [], C.c_void_p()
-            _check(self.lib.xsm_capture_watch(stream, C.byref(r.watch)))
-            _recorded[key] = r
+        r = _recorded_on(self.device, stream)
         if r.size < need:
             ws = _zeros_while_recording(need, self.device)
             if r.ws is not None:
@@ -508,6 +521,22 @@ def _status(device: int, stream: int) -> int:
     return t.data_ptr()
 
 
+_counters = {}           # by (device, stream): a word that calls count their CTAs in
+
+
+def _counter(device: int, stream: int) -> int:
+    """Address of a word that is zero between the calls of a stream, or of a graph's on one of its streams."""
+    if stream and _capturing():
+        r = _recorded_on(device, stream)
+        if r.counter is None:
+            r.counter = _zeros_while_recording(16, device)
+        return r.counter.data_ptr()
+    t = _counters.get((device, stream))
+    if t is None:
+        t = _counters.setdefault((device, stream), torch.zeros(16, dtype=torch.uint8, device=f"cuda:{device}"))
+    return t.data_ptr()
+
+
 _KEPT = 1 << 20          # bytes of a workspace that is kept from call to call
 _scratch_of = threading.local()
 _sizes = {}              # by operator and sizes: bytes of its workspace
@@ -605,7 +634,7 @@ def _linear_forward(hidden, weight, tokens, temperature):
     ws = _scratch(n, device, stream, where)
     try:
         args = _LINEAR.pack(hidden.data_ptr(), weight.data_ptr(), tokens.data_ptr(), logprob.data_ptr(), lse.data_ptr(), ws.data_ptr(), _status(device, stream),
-                            ld, w_ld, tokens.stride(0), n, rows, vocab, d, _DTYPES[dtype], _TOKENS[tokens.dtype], temperature)
+                            _counter(device, stream) if rows <= 16 else 0, ld, w_ld, tokens.stride(0), n, rows, vocab, d, _DTYPES[dtype], _TOKENS[tokens.dtype], temperature)
     except _BEYOND as e:
         raise ValueError(f"an argument of linear_logprobs is beyond its type: {e}") from None
     status = lib.xsm_linear_logprobs(args, stream)

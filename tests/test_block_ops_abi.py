@@ -30,7 +30,7 @@ def test_structures_have_the_sizes_and_offsets_of_the_header(tmp_path):
 
     def up(n):
         return (n + 7) // 8 * 8
-    for name, s, pointers, strides in (("xsm_linear_logprobs_args", ops._LINEAR, 7, 4), ("xsm_linear_logprobs_grad_args", ops._LINEAR_GRAD, 10, 8), ("xsm_gated_ff_args", ops._GATED, 5, 4),
+    for name, s, pointers, strides in (("xsm_linear_logprobs_args", ops._LINEAR, 8, 4), ("xsm_linear_logprobs_grad_args", ops._LINEAR_GRAD, 10, 8), ("xsm_gated_ff_args", ops._GATED, 5, 4),
                                        ("xsm_gated_ff_grad_args", ops._GATED_GRAD, 9, 7)):
         assert got[name] == [up(s.size), 8 * pointers, 8 * (pointers + strides - 1), 8 * (pointers + strides), s.size - 4]
     assert got["xsm_norm_rotate_args"] == [up(ops._NORM.size), 64, 64 + 9 * 8, 64 + 12 * 8, ops._NORM.size - 4]
@@ -47,7 +47,7 @@ def test_calls_without_arguments_are_refused(lib):
     assert lib.xsm_norm_rotate_grad_workspace(0) == 0 and lib.xsm_norm_rotate_grad_workspace(512) == 0
 
 
-def linear(pointers=7 * [A], strides=(64, 64, 1), ws=1 << 30, rows=4, vocab=100, d=64, dtype=1, token_bytes=8, temperature=1.0):
+def linear(pointers=8 * [A], strides=(64, 64, 1), ws=1 << 30, rows=4, vocab=100, d=64, dtype=1, token_bytes=8, temperature=1.0):
     from paper_2507_23777_b200 import ops
     return ops._LINEAR.pack(*pointers, *strides, ws, rows, vocab, d, dtype, token_bytes, temperature)
 
@@ -55,8 +55,8 @@ def linear(pointers=7 * [A], strides=(64, 64, 1), ws=1 << 30, rows=4, vocab=100,
 @pytest.mark.parametrize("wrong,word", [(dict(dtype=0), b"dtype"), (dict(dtype=3), b"dtype"), (dict(rows=-1), b"rows"), (dict(vocab=0), b"vocab"), (dict(d=60, strides=(64, 64, 1)), b"d a positive"), (dict(d=0), b"d a positive"),
                                         (dict(token_bytes=2), b"token_bytes"), (dict(temperature=0.0), b"temperature"), (dict(temperature=float("nan")), b"temperature"),
                                         (dict(temperature=1e-45), b"temperature"), (dict(temperature=float("inf")), b"temperature"), (dict(strides=(60, 64, 1)), b"hidden"), (dict(strides=(64, 56, 1)), b"weight"),
-                                        (dict(strides=(64, 65, 1)), b"weight"), (dict(pointers=[A + 2] + 6 * [A]), b"aligned"), (dict(pointers=[A, A, A + 4, A, A, A, A]), b"aligned"),
-                                        (dict(pointers=5 * [A] + [A + 4, A]), b"aligned"), (dict(pointers=[0] + 6 * [A]), b"null"), (dict(pointers=6 * [A] + [0]), b"null")])
+                                        (dict(strides=(64, 65, 1)), b"weight"), (dict(pointers=[A + 2] + 7 * [A]), b"aligned"), (dict(pointers=[A, A, A + 4, A, A, A, A, A]), b"aligned"),
+                                        (dict(pointers=5 * [A] + [A + 4, A, A]), b"aligned"), (dict(pointers=[0] + 7 * [A]), b"null"), (dict(pointers=6 * [A] + [0, A]), b"null")])
 def test_wrong_arguments_of_linear_logprobs(lib, wrong, word):
     assert lib.xsm_linear_logprobs(linear(**wrong), None) == binding.XSM_ERR_INVALID_ARG
     assert word in lib.xsm_last_error(None)
