@@ -352,8 +352,11 @@ XSM_API xsm_status xsm_token_logprobs_grad_near(const xsm_logprob_grad_args *a, 
  * Products on the tensor cores with what follows them in the same kernel: 16-bit elements (XSM_BF16, XSM_F16; rows 16-byte aligned, strides in elements), sums in
  * fp32.  `d`, the summed axis of the forward products, is a multiple of 8; other sizes are any.  As above: the caller's stream of the current device, nothing is waited
  * for, calls may be captured.  status: DEVICE, a 32-bit word, zeroed by the caller before its first use, which calls may share: XSM_ERR_TIMEOUT once a bounded wait of the
- * device has run out, and the results of that call are then void.  workspace: DEVICE, 16-byte aligned, as many bytes as the function of that name says, of any
+ * device has run out, and the results of that call are then void.  counters: DEVICE, XSM_COUNTERS words, zero before their first use and again after every call, but for one whose
+ * wait ran out; calls that share them follow each other on one stream.  workspace: DEVICE, 16-byte aligned, as many bytes as the function of that name says, of any
  * content; calls that share one follow each other on one stream. */
+
+enum { XSM_COUNTERS = 2048 };
 
 /* Log probabilities of given tokens under softmax(logits / temperature), logits = hidden . weight^T, which are never in memory:
  *   z_rj = sum_i hidden[r][i] weight[j][i] / temperature,  lse_r = log sum_j exp(z_rj),  logprob_r = z_r,token - lse_r.
@@ -364,8 +367,7 @@ typedef struct {
     float *logprob, *lse;                 /* DEVICE [rows] */
     void *workspace;
     int32_t *status;
-    uint32_t *counter;                    /* DEVICE, a word that is zero before its first use and after every call; calls that share one follow each other on one stream.
-                                             With it up to 16 rows take one kernel instead of two; may be NULL */
+    uint32_t *counters;                   /* may be NULL; with them up to 16 rows take one kernel instead of two */
     int64_t hidden_stride, weight_stride, token_stride, workspace_bytes;
     int32_t rows, vocab, d, dtype, token_bytes;
     float temperature;
@@ -385,6 +387,7 @@ typedef struct {
     void *d_hidden, *d_weight;            /* DEVICE dtype [rows][d], [vocab][d] */
     void *workspace;
     int32_t *status;
+    uint32_t *counters;
     int64_t hidden_stride, weight_stride, token_stride, g_logprob_stride, g_lse_stride, d_hidden_stride, d_weight_stride, workspace_bytes;
     int32_t rows, vocab, d, dtype, token_bytes;
     float temperature;
@@ -411,6 +414,7 @@ typedef struct {
     void *d_x, *d_w_gate, *d_w_up;        /* DEVICE dtype [rows][d], [ff][d], [ff][d], the latter of one stride */
     void *workspace;
     int32_t *status;
+    uint32_t *counters;
     int64_t x_stride, w_gate_stride, w_up_stride, g_out_stride, d_x_stride, d_w_stride, workspace_bytes;
     int32_t rows, ff, d, dtype, activation;
 } xsm_gated_ff_grad_args;

@@ -17,6 +17,7 @@ LIB_PATH = os.path.join(_HERE, "libxsm.so")
 
 XSM_OK, XSM_ERR_INVALID_ARG, XSM_ERR_STATE, XSM_ERR_CAPACITY, XSM_ERR_CUDA, XSM_ERR_TIMEOUT = range(6)
 XSM_MAX_DRAFT = 16
+XSM_COUNTERS = 2048
 
 EXPORTS = [
     "xsm_weights_bytes", "xsm_workspace_bytes", "xsm_create", "xsm_prefill", "xsm_spec_step", "xsm_generate",
@@ -27,6 +28,9 @@ EXPORTS = [
     "xsm_kv_attend", "xsm_debug_kv_waits", "xsm_capture_id", "xsm_capture_watch", "xsm_capture_gone", "xsm_capture_mode",
     "xsm_token_logprobs", "xsm_token_logprobs_grad",
     "xsm_token_logprobs_grad_near",
+    "xsm_linear_logprobs_workspace", "xsm_linear_logprobs", "xsm_linear_logprobs_grad_workspace", "xsm_linear_logprobs_grad",
+    "xsm_gated_ff", "xsm_gated_ff_grad_workspace", "xsm_gated_ff_grad", "xsm_debug_product_waits",
+    "xsm_norm_rotate", "xsm_norm_rotate_grad_workspace", "xsm_norm_rotate_grad", "xsm_kv_append_norm",
 ]
 
 

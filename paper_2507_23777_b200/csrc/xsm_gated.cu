@@ -9,24 +9,21 @@ namespace xsm {
 
 static size_t up(size_t n) { return (n + 255) & ~(size_t)255; }
 struct GatedGradPlan {
-    ProductCut cut, cut_x, cut_w;
-    int ld, splits_x, splits_w;
-    size_t amax, d_gate, d_up, part_x, part_w, bytes;
+    ProductCut cut;
+    SumsPlan sums;
+    int ld;
+    size_t amax, d_gate, d_up, part, bytes;
 };
-static GatedGradPlan plan_gated_grad(int rows, int ff, int d) {
+static GatedGradPlan plan_gated_grad(int rows, int ff, int d, bool x, bool w) {
     GatedGradPlan p;
     p.cut = product_cut(PR_GATED_GRAD, rows, ff);
-    p.cut_x = product_cut(PR_OUT, rows, d);
-    p.cut_w = product_cut(PR_OUT, ff, d);
+    p.sums = plan_sums(rows, ff, d, 2, x, w);
     p.ld = (ff + 7) / 8 * 8;
-    p.splits_x = product_splits(p.cut_x.tiles(rows, d, false), 2 * ((ff + 63) / 64), p.cut_x.wide);
-    p.splits_w = product_splits(2 * p.cut_w.tiles(ff, d, false), (rows + 63) / 64, p.cut_w.wide);
     p.amax = 0;
     p.d_gate = up(kAmaxBlocks * 4);
     p.d_up = p.d_gate + up((size_t)rows * p.ld * 2);
-    p.part_x = p.d_up + up((size_t)rows * p.ld * 2);
-    p.part_w = p.part_x + (p.splits_x > 1 ? up((size_t)p.splits_x * rows * d * 4) : 0);
-    p.bytes = p.part_w + (p.splits_w > 1 ? up((size_t)2 * p.splits_w * ff * d * 4) : 0);
+    p.part = p.d_up + up((size_t)rows * p.ld * 2);
+    p.bytes = p.part + up(p.sums.bytes);
     return p;
 }
 
@@ -51,14 +48,17 @@ xsm_status xsm_gated_ff(const xsm_gated_ff_args *a, void *cuda_stream) {
         return op_failed(XSM_ERR_INVALID_ARG, "rows of x, w_gate and w_up must be 16-byte aligned and must not overlap");
     if ((uintptr_t)a->out % 2 || a->out_stride < a->ff || (uintptr_t)a->status % 4) return op_failed(XSM_ERR_INVALID_ARG, "out and status must be aligned to their elements, rows of out must not overlap");
     ProductArgs A = {};
-    A.m = a->rows; A.n = a->ff; A.jobs = A.splits = 1;
     A.status = a->status; A.activation = a->activation;
     A.out[0] = a->out; A.out_ld = a->out_stride;
-    const Operand x[2] = {{a->x, a->rows, a->d, a->x_stride}, {}}, w[2] = {{a->w_gate, a->ff, a->d, a->w_gate_stride}, {a->w_up, a->ff, a->d, a->w_up_stride}};
-    return launched(launch_product(PR_GATED, a->dtype, product_cut(PR_GATED, a->rows, a->ff), A, x, w, 1, (cudaStream_t)cuda_stream));
+    const Operand x = {a->x, a->rows, a->d, a->x_stride}, w[2] = {{a->w_gate, a->ff, a->d, a->w_gate_stride}, {a->w_up, a->ff, a->d, a->w_up_stride}};
+    return launched(launch_product(PR_GATED, a->dtype, product_cut(PR_GATED, a->rows, a->ff), A, a->rows, a->ff, x, w, (cudaStream_t)cuda_stream));
 }
 
-size_t xsm_gated_ff_grad_workspace(int rows, int ff, int d) { return rows < 1 || ff < 1 || d < 1 ? 0 : plan_gated_grad(rows, ff, d).bytes; }
+size_t xsm_gated_ff_grad_workspace(int rows, int ff, int d) {
+    if (rows < 1 || ff < 1 || d < 1) return 0;
+    const size_t a = plan_gated_grad(rows, ff, d, true, true).bytes, b = plan_gated_grad(rows, ff, d, true, false).bytes, c = plan_gated_grad(rows, ff, d, false, true).bytes;
+    return a > b ? (a > c ? a : c) : b > c ? b : c;
+}
 
 xsm_status xsm_gated_ff_grad(const xsm_gated_ff_grad_args *a, void *cuda_stream) {
     if (!a) return op_failed(XSM_ERR_INVALID_ARG, "null argument");
@@ -74,16 +74,15 @@ xsm_status xsm_gated_ff_grad(const xsm_gated_ff_grad_args *a, void *cuda_stream)
         if (a->d_w_gate && e == cudaSuccess) e = cudaMemset2DAsync(a->d_w_up, (size_t)a->d_w_stride * 2, 0, (size_t)a->d * 2, (size_t)a->ff, st);
         return launched(e);
     }
-    if (!a->x || !a->w_gate || !a->w_up || !a->g_out || !a->workspace || !a->status) return op_failed(XSM_ERR_INVALID_ARG, "null argument");
+    if (!a->x || !a->w_gate || !a->w_up || !a->g_out || !a->workspace || !a->status || !a->counters) return op_failed(XSM_ERR_INVALID_ARG, "null argument");
     if (!rows_fit(a->x, a->x_stride, a->d) || !rows_fit(a->w_gate, a->w_gate_stride, a->d) || !rows_fit(a->w_up, a->w_up_stride, a->d) || (a->d_x && !rows_fit(a->d_x, a->d_x_stride, a->d)))
         return op_failed(XSM_ERR_INVALID_ARG, "rows of x, w_gate, w_up and d_x must be 16-byte aligned and must not overlap");
-    if ((uintptr_t)a->g_out % 2 || a->g_out_stride < 0 || (uintptr_t)a->status % 4 || (uintptr_t)a->workspace % 16)
-        return op_failed(XSM_ERR_INVALID_ARG, "g_out and status must be aligned to their elements, workspace to 16 bytes");
-    const GatedGradPlan p = plan_gated_grad(a->rows, a->ff, a->d);
+    if ((uintptr_t)a->g_out % 2 || a->g_out_stride < 0 || ((uintptr_t)a->status | (uintptr_t)a->counters) % 4 || (uintptr_t)a->workspace % 16)
+        return op_failed(XSM_ERR_INVALID_ARG, "g_out, status and counters must be aligned to their elements, workspace to 16 bytes");
+    const GatedGradPlan p = plan_gated_grad(a->rows, a->ff, a->d, a->d_x, a->d_w_gate);
     if (a->workspace_bytes < (int64_t)p.bytes) return op_failed(XSM_ERR_CAPACITY, "the workspace is too small");
     char *ws = (char *)a->workspace;
     ProductArgs A = {};
-    A.m = a->rows; A.n = a->ff; A.jobs = A.splits = 1;
     A.status = a->status; A.activation = a->activation;
     A.g_y = a->g_out; A.g_y_ld = a->g_out_stride;
     A.out[0] = ws + p.d_gate; A.out[1] = ws + p.d_up; A.out_ld = p.ld;
@@ -92,24 +91,18 @@ xsm_status xsm_gated_ff_grad(const xsm_gated_ff_grad_args *a, void *cuda_stream)
         A.amax = (const float *)(ws + p.amax);
         e = launch_amax_rows(a->g_out, a->dtype, a->rows, a->ff, a->g_out_stride, (float *)(ws + p.amax), st);
     }
-    const Operand x[2] = {{a->x, a->rows, a->d, a->x_stride}, {}}, w[2] = {{a->w_gate, a->ff, a->d, a->w_gate_stride}, {a->w_up, a->ff, a->d, a->w_up_stride}};
-    const Operand g[2] = {{ws + p.d_gate, a->rows, a->ff, p.ld}, {ws + p.d_up, a->rows, a->ff, p.ld}};
-    if (e == cudaSuccess) e = launch_product(PR_GATED_GRAD, a->dtype, p.cut, A, x, w, 1, st);
-    ProductArgs G = {};
-    G.status = a->status; G.amax = A.amax; G.amax_to = A.amax_to;
-    if (a->d_x && e == cudaSuccess) {
-        G.m = a->rows; G.n = a->d; G.jobs = 1; G.splits = p.splits_x;
-        G.out[0] = a->d_x; G.out_ld = a->d_x_stride;
-        G.partial = p.splits_x > 1 ? (float *)(ws + p.part_x) : nullptr;
-        e = launch_product(PR_OUT, a->dtype, p.cut_x, G, g, w, 2, st);
-        if (G.partial && e == cudaSuccess) e = launch_join(G, a->dtype, st);
-    }
-    if (a->d_w_gate && e == cudaSuccess) {
-        G.m = a->ff; G.n = a->d; G.jobs = 2; G.splits = p.splits_w;
-        G.out[0] = a->d_w_gate; G.out[1] = a->d_w_up; G.out_ld = a->d_w_stride;
-        G.partial = p.splits_w > 1 ? (float *)(ws + p.part_w) : nullptr;
-        e = launch_product(PR_OUT_ROWS, a->dtype, p.cut_w, G, g, x, 1, st);
-        if (G.partial && e == cudaSuccess) e = launch_join(G, a->dtype, st);
-    }
+    const Operand x = {a->x, a->rows, a->d, a->x_stride}, w[2] = {{a->w_gate, a->ff, a->d, a->w_gate_stride}, {a->w_up, a->ff, a->d, a->w_up_stride}};
+    if (e == cudaSuccess) e = launch_product(PR_GATED_GRAD, a->dtype, p.cut, A, a->rows, a->ff, x, w, st);
+    Sums S = {};
+    S.pairs = 2;
+    S.h = x;
+    for (int i = 0; i < 2; ++i) { S.g[i] = {A.out[i], a->rows, a->ff, p.ld}; S.w[i] = w[i]; }
+    S.x = a->d_x; S.x_ld = a->d_x_stride;
+    S.y[0] = a->d_w_gate; S.y[1] = a->d_w_up; S.y_ld = a->d_w_stride;
+    S.end = 1;
+    S.partial = ws + p.part;
+    S.counters = a->counters; S.status = a->status;
+    S.amax = A.amax; S.amax_to = A.amax_to;
+    if (e == cudaSuccess) e = launch_sums(a->dtype, p.sums, S, st);
     return launched(e);
 }

@@ -11,6 +11,7 @@
 namespace xsm {
 
 constexpr long long kPieceBytes = 256ll << 20;      // of a piece's gradients by the logits
+constexpr int kRowsLookedThrough = 65536;           // so many rows every CTA looks through for the largest gradient
 
 // Eight rows a block; thread (row, y) joins parts y, y + 32, ...  (32 rows a block, eight threads a row: 145 us for 96 rows of 4096 parts.)
 __global__ void __launch_bounds__(256) join_stats_kernel(const float2 *parts, const float *token_z, const void *tokens, long long token_ld, int token_bytes, int rows, int vocab,
@@ -49,11 +50,12 @@ static LinearPlan plan_linear(int rows, int vocab) {
 static size_t up(size_t n) { return (n + 255) & ~(size_t)255; }
 
 struct LinearGradPlan {
-    ProductCut cut_z, cut_h, cut_w;
-    int piece, pieces, splits_h, splits_w;
-    size_t amax, dz, part_h, part_w, bytes;      // offsets in the workspace
+    ProductCut cut_z;
+    SumsPlan sums;
+    int piece, pieces;
+    size_t amax, dz, part, acc, bytes;      // offsets in the workspace
 };
-static LinearGradPlan plan_linear_grad(int rows, int vocab, int d) {
+static LinearGradPlan plan_linear_grad(int rows, int vocab, int d, bool h, bool w) {
     LinearGradPlan p;
     long long piece = kPieceBytes / (2ll * rows) / 256 * 256;
     if (piece < 1024) piece = 1024;
@@ -62,17 +64,12 @@ static LinearGradPlan plan_linear_grad(int rows, int vocab, int d) {
     if (p.piece > vocab) p.piece = (vocab + 63) / 64 * 64;
     p.pieces = (vocab + p.piece - 1) / p.piece;
     p.cut_z = product_cut(PR_DLOGITS, rows, p.piece);
-    p.cut_h = product_cut(PR_OUT, rows, d);
-    p.cut_w = product_cut(PR_OUT, p.piece, d);
-    p.splits_h = product_splits(p.cut_h.tiles(rows, d, false), p.piece / 64, p.cut_h.wide);
-    const int last = vocab - (p.pieces - 1) * p.piece;            // (the shortest piece has to have a block for every part)
-    if (p.splits_h > (last + 63) / 64) p.splits_h = (last + 63) / 64;
-    p.splits_w = product_splits(p.cut_w.tiles(p.piece, d, false), (rows + 63) / 64, p.cut_w.wide);
+    p.sums = plan_sums(rows, p.piece, d, 1, h, w);
     p.amax = 0;
     p.dz = up(kAmaxBlocks * 4);
-    p.part_h = p.dz + up((size_t)rows * p.piece * 2);
-    p.part_w = p.part_h + (p.splits_h > 1 || p.pieces > 1 ? up((size_t)p.splits_h * rows * d * 4) : 0);
-    p.bytes = p.part_w + (p.splits_w > 1 ? up((size_t)p.splits_w * p.piece * d * 4) : 0);
+    p.part = p.dz + up((size_t)rows * p.piece * 2);
+    p.acc = p.part + up(p.sums.bytes);
+    p.bytes = p.acc + (p.pieces > 1 && h ? up(sums_bytes(p.sums.cut, rows, d)) : 0);
     return p;
 }
 
@@ -102,12 +99,11 @@ xsm_status xsm_linear_logprobs(const xsm_linear_logprobs_args *a, void *cuda_str
     if (!a->hidden || !a->weight || !a->tokens || !a->logprob || !a->lse || !a->workspace || !a->status) return op_failed(XSM_ERR_INVALID_ARG, "null argument");
     if (!rows_fit(a->hidden, a->hidden_stride, a->d) || !rows_fit(a->weight, a->weight_stride, a->d))
         return op_failed(XSM_ERR_INVALID_ARG, "rows of hidden and weight must be 16-byte aligned and must not overlap");
-    if ((uintptr_t)a->tokens % a->token_bytes || ((uintptr_t)a->logprob | (uintptr_t)a->lse | (uintptr_t)a->status | (uintptr_t)a->counter) % 4 || (uintptr_t)a->workspace % 16)
-        return op_failed(XSM_ERR_INVALID_ARG, "tokens, logprob, lse, status and counter must be aligned to their elements, workspace to 16 bytes");
+    if ((uintptr_t)a->tokens % a->token_bytes || ((uintptr_t)a->logprob | (uintptr_t)a->lse | (uintptr_t)a->status | (uintptr_t)a->counters) % 4 || (uintptr_t)a->workspace % 16)
+        return op_failed(XSM_ERR_INVALID_ARG, "tokens, logprob, lse, status and counters must be aligned to their elements, workspace to 16 bytes");
     if (a->workspace_bytes < (int64_t)xsm_linear_logprobs_workspace(a->rows, a->vocab, a->d)) return op_failed(XSM_ERR_CAPACITY, "the workspace is too small");
     const LinearPlan p = plan_linear(a->rows, a->vocab);
     ProductArgs A = {};
-    A.m = a->rows; A.n = a->vocab; A.jobs = A.splits = 1;
     A.status = a->status;
     A.tokens = a->tokens; A.token_ld = a->token_stride; A.token_bytes = a->token_bytes; A.vocab = a->vocab;
     A.inv_t = 1.f / a->temperature;
@@ -115,12 +111,12 @@ xsm_status xsm_linear_logprobs(const xsm_linear_logprobs_args *a, void *cuda_str
     A.parts = (float2 *)a->workspace;
     A.carry = p.carry;
     // (few rows: the last CTA joins the parts itself, 5 x 4096 7.8 -> 7.3 us and a launch less; of 96 rows that takes one CTA 15 us)
-    if (p.carry && !p.cut.wide && a->rows <= 16) A.counter = a->counter;
+    if (p.carry && !p.cut.wide && a->rows <= 16) A.counter = a->counters;
     A.logprob = a->logprob; A.lse_out = a->lse;
     A.token_z = (float *)((char *)a->workspace + up((size_t)p.parts * a->rows * 8));
-    const Operand h[2] = {{a->hidden, a->rows, a->d, a->hidden_stride}, {}}, w[2] = {{a->weight, a->vocab, a->d, a->weight_stride}, {}};
+    const Operand h = {a->hidden, a->rows, a->d, a->hidden_stride}, w[2] = {{a->weight, a->vocab, a->d, a->weight_stride}, {}};
     const cudaStream_t st = (cudaStream_t)cuda_stream;
-    cudaError_t e = launch_product(PR_STATS, a->dtype, p.cut, A, h, w, 1, st);
+    cudaError_t e = launch_product(PR_STATS, a->dtype, p.cut, A, a->rows, a->vocab, h, w, st);
     if (e == cudaSuccess && !A.counter)
         e = launch_early(join_stats_kernel, dim3((unsigned)((a->rows + 7) / 8)), dim3(256), 0, st, (const float2 *)A.parts, (const float *)A.token_z, a->tokens, (long long)a->token_stride,
                          (int)a->token_bytes, (int)a->rows, (int)a->vocab, (int)p.parts, a->logprob, a->lse);
@@ -129,7 +125,8 @@ xsm_status xsm_linear_logprobs(const xsm_linear_logprobs_args *a, void *cuda_str
 
 size_t xsm_linear_logprobs_grad_workspace(int rows, int vocab, int d) {
     if (rows < 1 || vocab < 1 || d < 1) return 0;
-    return plan_linear_grad(rows, vocab, d).bytes;
+    const size_t a = plan_linear_grad(rows, vocab, d, true, true).bytes, b = plan_linear_grad(rows, vocab, d, true, false).bytes, c = plan_linear_grad(rows, vocab, d, false, true).bytes;
+    return a > b ? (a > c ? a : c) : b > c ? b : c;
 }
 
 xsm_status xsm_linear_logprobs_grad(const xsm_linear_logprobs_grad_args *a, void *cuda_stream) {
@@ -140,55 +137,50 @@ xsm_status xsm_linear_logprobs_grad(const xsm_linear_logprobs_grad_args *a, void
     if (a->d_weight && !rows_fit(a->d_weight, a->d_weight_stride, a->d)) return op_failed(XSM_ERR_INVALID_ARG, "rows of d_weight must be 16-byte aligned and must not overlap");
     if (a->rows == 0)
         return a->d_weight ? launched(cudaMemset2DAsync(a->d_weight, (size_t)a->d_weight_stride * 2, 0, (size_t)a->d * 2, (size_t)a->vocab, st)) : XSM_OK;
-    if (!a->hidden || !a->weight || !a->tokens || !a->lse || !a->workspace || !a->status) return op_failed(XSM_ERR_INVALID_ARG, "null argument");
+    if (!a->hidden || !a->weight || !a->tokens || !a->lse || !a->workspace || !a->status || !a->counters) return op_failed(XSM_ERR_INVALID_ARG, "null argument");
     if (!rows_fit(a->hidden, a->hidden_stride, a->d) || !rows_fit(a->weight, a->weight_stride, a->d) || (a->d_hidden && !rows_fit(a->d_hidden, a->d_hidden_stride, a->d)))
         return op_failed(XSM_ERR_INVALID_ARG, "rows of hidden, weight and d_hidden must be 16-byte aligned and must not overlap");
-    if ((uintptr_t)a->tokens % a->token_bytes || ((uintptr_t)a->lse | (uintptr_t)a->g_logprob | (uintptr_t)a->g_lse | (uintptr_t)a->status) % 4 || (uintptr_t)a->workspace % 16)
-        return op_failed(XSM_ERR_INVALID_ARG, "tokens, lse, g_logprob, g_lse and status must be aligned to their elements, workspace to 16 bytes");
-    const LinearGradPlan p = plan_linear_grad(a->rows, a->vocab, a->d);
+    if ((uintptr_t)a->tokens % a->token_bytes || ((uintptr_t)a->lse | (uintptr_t)a->g_logprob | (uintptr_t)a->g_lse | (uintptr_t)a->status | (uintptr_t)a->counters) % 4 || (uintptr_t)a->workspace % 16)
+        return op_failed(XSM_ERR_INVALID_ARG, "tokens, lse, g_logprob, g_lse, status and counters must be aligned to their elements, workspace to 16 bytes");
+    const LinearGradPlan p = plan_linear_grad(a->rows, a->vocab, a->d, a->d_hidden, a->d_weight);
     if (a->workspace_bytes < (int64_t)p.bytes) return op_failed(XSM_ERR_CAPACITY, "the workspace is too small");
     char *ws = (char *)a->workspace;
     ProductArgs Z = {};
-    Z.jobs = Z.splits = 1;
     Z.status = a->status;
-    Z.m = a->rows;
     Z.tokens = a->tokens; Z.token_ld = a->token_stride; Z.token_bytes = a->token_bytes; Z.vocab = a->vocab;
     Z.inv_t = 1.f / a->temperature;
     Z.c = (float)(1.4426950408889634 / a->temperature);
     Z.lse = a->lse; Z.g = a->g_logprob; Z.g_ld = a->g_logprob_stride; Z.g_lse = a->g_lse; Z.g_lse_ld = a->g_lse_stride;
+    Z.out[0] = ws + p.dz; Z.out_ld = p.piece;
+    Sums S = {};
+    S.pairs = 1;
+    S.h = {a->hidden, a->rows, a->d, a->hidden_stride};
+    S.x = a->d_hidden; S.x_ld = a->d_hidden_stride; S.y_ld = a->d_weight_stride;
+    S.x_sums = p.pieces > 1 ? (float *)(ws + p.acc) : nullptr;
+    S.partial = ws + p.part;
+    S.counters = a->counters; S.status = a->status;
     cudaError_t e = cudaSuccess;
     if (a->dtype == XSM_F16) {        // fp16 has no numbers below 2^-24: the largest gradient by a logit is taken to 2^13 and more
-        Z.amax = (const float *)(ws + p.amax);
-        Z.amax_to = 13;
-        e = launch_amax_pairs(Z.g, Z.g_ld, Z.g_lse, Z.g_lse_ld, a->rows, Z.inv_t, (float *)(ws + p.amax), st);
+        S.amax = (const float *)(ws + p.amax);
+        S.amax_to = Z.amax_to = 13;
+        if (a->rows <= kRowsLookedThrough) {
+            Z.amax_out = (float *)(ws + p.amax);
+        } else {
+            Z.amax = S.amax;
+            e = launch_amax_pairs(Z.g, Z.g_ld, Z.g_lse, Z.g_lse_ld, a->rows, Z.inv_t, (float *)(ws + p.amax), st);
+        }
     }
     for (int i = 0; i < p.pieces && e == cudaSuccess; ++i) {
         const int v0 = i * p.piece, v = a->vocab - v0 < p.piece ? a->vocab - v0 : p.piece;
-        const void *weight = (const char *)a->weight + (long long)v0 * a->weight_stride * 2;
-        const Operand hidden[2] = {{a->hidden, a->rows, a->d, a->hidden_stride}, {}}, w[2] = {{weight, v, a->d, a->weight_stride}, {}}, dz[2] = {{ws + p.dz, a->rows, v, p.piece}, {}};
-        ProductArgs A = Z;
-        A.n = v; A.vocab0 = v0;
-        A.out[0] = ws + p.dz; A.out_ld = p.piece;
-        e = launch_product(PR_DLOGITS, a->dtype, p.cut_z, A, hidden, w, 1, st);
-        ProductArgs G = {};
-        G.jobs = 1;
-        G.status = a->status; G.amax = Z.amax; G.amax_to = Z.amax_to;
-        if (a->d_hidden && e == cudaSuccess) {
-            G.m = a->rows; G.n = a->d; G.splits = p.splits_h;
-            G.out[0] = a->d_hidden; G.out_ld = a->d_hidden_stride;
-            G.partial = p.splits_h > 1 || p.pieces > 1 ? (float *)(ws + p.part_h) : nullptr;
-            G.add = i > 0;
-            e = launch_product(PR_OUT, a->dtype, p.cut_h, G, dz, w, 1, st);
-            if (G.partial && i == p.pieces - 1 && e == cudaSuccess) e = launch_join(G, a->dtype, st);
-        }
-        if (a->d_weight && e == cudaSuccess) {
-            G.m = v; G.n = a->d; G.splits = p.splits_w;
-            G.out[0] = (char *)a->d_weight + (long long)v0 * a->d_weight_stride * 2; G.out_ld = a->d_weight_stride;
-            G.partial = p.splits_w > 1 ? (float *)(ws + p.part_w) : nullptr;
-            G.add = 0;
-            e = launch_product(PR_OUT_ROWS, a->dtype, p.cut_w, G, dz, hidden, 1, st);
-            if (G.partial && e == cudaSuccess) e = launch_join(G, a->dtype, st);
-        }
+        const Operand w[2] = {{(const char *)a->weight + (long long)v0 * a->weight_stride * 2, v, a->d, a->weight_stride}, {}};
+        Z.vocab0 = v0;
+        e = launch_product(PR_DLOGITS, a->dtype, p.cut_z, Z, a->rows, v, S.h, w, st);
+        S.g[0] = {ws + p.dz, a->rows, v, p.piece};
+        S.w[0] = w[0];
+        S.y[0] = a->d_weight ? (char *)a->d_weight + (long long)v0 * a->d_weight_stride * 2 : nullptr;
+        S.go_on = i > 0;
+        S.end = i == p.pieces - 1;
+        if (e == cudaSuccess) e = launch_sums(a->dtype, p.sums, S, st);
     }
     return launched(e);
 }

@@ -97,17 +97,43 @@ template <int KIND> __device__ __forceinline__ void activate(float g, float &a, 
     }
 }
 
-// Power of two that takes the largest of kAmaxBlocks numbers to [2^to, 2^(to + 1)); 1 where there is none.
+// Power of two that takes `most` to [2^to, 2^(to + 1)); 1 where there is nothing.
+__device__ __forceinline__ float scale_for(float most, int to) {
+    if (!(most > 0.f)) return 1.f;
+    int e = (int)(__float_as_uint(most) >> 23) - 127;
+    e = max(-100, min(100, to - e));
+    return __uint_as_float((unsigned)(e + 127) << 23);
+}
+
+// the same of the largest of kAmaxBlocks numbers
 __device__ __forceinline__ float scale_of(const float *amax, int to) {
     if (amax == nullptr) return 1.f;
     float m = 0.f;
     for (int i = threadIdx.x & 31; i < kAmaxBlocks; i += 32) m = fmaxf(m, amax[i]);
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-    if (!(m > 0.f)) return 1.f;
-    int e = (int)(__float_as_uint(m) >> 23) - 127;
-    e = max(-100, min(100, to - e));
-    return __uint_as_float((unsigned)(e + 127) << 23);
+    return scale_for(m, to);
+}
+
+// The same of what the gradients by a row's logits may be, 2|g| + |g_lse| over T, over all rows: looked for by the eight warps of a finished tile while its products
+// run, infinities and NaN apart.
+__device__ __forceinline__ float scale_of_rows(const ProductArgs &A, int w, int lane) {
+    __shared__ float most[kEpiWarps];
+    float m = 0.f;
+    const int rows = A.part[0].m;
+#pragma unroll 4
+    for (long long r = w * 32 + lane; r < rows; r += 32 * kEpiWarps) {
+        const float v = (2.f * (A.g ? fabsf(A.g[r * A.g_ld]) : 0.f) + (A.g_lse ? fabsf(A.g_lse[r * A.g_lse_ld]) : 0.f)) * A.inv_t;
+        if (v < INFINITY) m = fmaxf(m, v);
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+    if (lane == 0) most[w] = m;
+    bar_sync<32 * kEpiWarps>(1);
+#pragma unroll
+    for (int i = 0; i < kEpiWarps; ++i) m = fmaxf(m, most[i]);
+    if (blockIdx.x == 0) A.amax_out[w * 32 + lane] = w + lane ? 0.f : m;
+    return scale_for(m, A.amax_to);
 }
 
 template <typename T> __device__ __forceinline__ uint32_t pack2(float a, float b) {
@@ -133,20 +159,22 @@ template <typename T, int N> __device__ __forceinline__ void store_row(T *row, i
 
 // Tiles in groups of `group_m` tiles of rows; in a group the rows first, then the columns: the tiles that run at a time then share both operands'
 // panels (63 x 8 tiles of 8192 steps rows first: every column of tiles fetched all of A again from memory).
-struct Tile { int m, n, split, job, k0, k1; };
-__device__ __forceinline__ Tile tile_of(const ProductArgs &A, unsigned t) {
+struct Tile { int m, n, split, job, k0, k1, at; };        // at: number of the tile of its job's and split's kind
+__device__ __forceinline__ Tile tile_of(const ProductPart &P, unsigned t) {
     Tile r;
-    const unsigned z = A.by_plane.of(t);
-    t -= z * A.by_plane.d;
-    const unsigned g = A.by_group.of(t);
-    t -= g * A.by_group.d;
-    const bool last = (int)(g + 1) * A.group_m > A.tiles_m;
-    r.n = (int)(last ? A.by_last_rows.of(t) : A.by_rows.of(t));
-    r.m = (int)(g * (unsigned)A.group_m + t - (unsigned)r.n * (last ? A.by_last_rows.d : A.by_rows.d));
-    r.job = (int)A.by_splits.of(z);
-    r.split = (int)(z - (unsigned)r.job * A.by_splits.d);
-    r.k0 = r.split * A.kb_each + min(r.split, A.kb_more);
-    r.k1 = r.k0 + A.kb_each + (r.split < A.kb_more);
+    t -= (unsigned)P.first;
+    const unsigned z = P.by_plane.of(t);
+    t -= z * P.by_plane.d;
+    r.job = (int)P.by_splits.of(z);
+    r.split = (int)(z - (unsigned)r.job * P.by_splits.d);
+    r.at = (int)(t + (unsigned)r.job * P.by_plane.d);
+    const unsigned g = P.by_group.of(t);
+    t -= g * P.by_group.d;
+    const bool last = (int)(g + 1) * P.group_m > P.tiles_m;
+    r.n = (int)(last ? P.by_last_rows.of(t) : P.by_rows.of(t));
+    r.m = (int)(g * (unsigned)P.group_m + t - (unsigned)r.n * (last ? P.by_last_rows.d : P.by_rows.d));
+    r.k0 = r.split * P.kb_each + min(r.split, P.kb_more);
+    r.k1 = r.k0 + P.kb_each + (r.split < P.kb_more);
     return r;
 }
 
@@ -167,12 +195,11 @@ __device__ __forceinline__ void rows_free(int lane) {
     if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
     __syncwarp();
 }
-__device__ __forceinline__ void rows_store(const void *map, uint32_t buf, int x, int y, int z, bool add, bool some, int lane) {
+__device__ __forceinline__ void rows_store(const void *map, uint32_t buf, int x, int y, int z, bool some, int lane) {
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     __syncwarp();
     if (some && lane == 0) {
-        if (add) asm volatile("cp.reduce.async.bulk.tensor.3d.global.shared::cta.add.tile.bulk_group [%0, {%1, %2, %3}], [%4];" :: "l"(map), "r"(x), "r"(y), "r"(z), "r"(buf) : "memory");
-        else asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%1, %2, %3}], [%4];" :: "l"(map), "r"(x), "r"(y), "r"(z), "r"(buf) : "memory");
+        asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%1, %2, %3}], [%4];" :: "l"(map), "r"(x), "r"(y), "r"(z), "r"(buf) : "memory");
         asm volatile("cp.async.bulk.commit_group;" ::: "memory");
     }
 }
@@ -232,8 +259,7 @@ template <typename T> __device__ __forceinline__ void put_row(uint32_t buf, int 
 template <int CG, int BN, int EPI, typename T>
 __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __grid_constant__ ProductMaps M, const __grid_constant__ ProductArgs A) {
     constexpr int TM = 128 * CG;
-    constexpr bool kGated = EPI == PR_GATED || EPI == PR_GATED_GRAD, kOut = EPI == PR_OUT || EPI == PR_OUT_ROWS;
-    constexpr bool kRowsA = EPI == PR_OUT_ROWS, kRowsB = kOut;        // operands whose rows run along the summed axis
+    constexpr bool kGated = EPI == PR_GATED || EPI == PR_GATED_GRAD, kOut = EPI == PR_OUT;
     extern __shared__ char smem_raw[];
     __shared__ __align__(8) uint64_t full[kMaxStages], empty[kMaxStages], sums_full[2], sums_empty[2], last;
     __shared__ uint32_t tmem_slot;
@@ -280,6 +306,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
     auto wait_warp = [&](uint32_t bar, uint32_t parity) {        // (all lanes or none)
         return __all_sync(0xffffffffu, mbar_try_wait(bar, parity)) || __all_sync(0xffffffffu, wait(bar, parity));
     };
+    auto part_of = [&](int t) -> const ProductPart & { return A.part[kOut && t >= A.part[1].first]; };
     const uint32_t full0 = smem_u32(full), empty0 = smem_u32(empty), sums_full0 = smem_u32(sums_full), sums_empty0 = smem_u32(sums_empty);
 
     // The two loops below run once for 64 steps of the summed axis, 512 cycles of the tensor cores: what does not change stands outside, and nothing
@@ -291,13 +318,15 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
             uint32_t par = 1u, sa = ring;
             bool ok = true;
             for (int t = first; ok && t < A.tiles; t += step) {
-                const Tile w = tile_of(A, (unsigned)t);
+                const ProductPart &P = part_of(t);
+                const Tile w = tile_of(P, (unsigned)t);
                 const int m0 = w.m * TM + rank * 128, n0 = kGated ? w.n * (BN / 2) : w.n * BN + rank * (BN / CG);
-                const int second = kOut && w.k0 >= A.kb0;
-                const CUtensorMap *ma = &M.a[kOut ? second + w.job : 0], *mb = &M.b[kGated && CG == 2 ? rank : second];
+                const int second = kOut && w.k0 >= P.kb0, rows_a = kOut && P.rows_a;
+                const uint32_t tx = P.stage_tx;
+                const CUtensorMap *ma = &M.a[kOut ? P.map_a + second + w.job : 0], *mb = &M.b[kOut ? P.map_b + second : kGated && CG == 2 ? rank : 0];
                 // a stage of one block: columns `at`; of several: blocks of 64 columns from z on (operands of whole blocks are described so)
                 const bool many = !kOut && CG == 1 && A.chunks > 1;
-                int at = (w.k0 - (second ? A.kb0 : 0)) * 64, z = 0;
+                int at = (w.k0 - (second ? P.kb0 : 0)) * 64, z = 0;
                 if (t == first) {
                     asm volatile("prefetch.tensormap [%0];" :: "l"(ma) : "memory");
                     asm volatile("prefetch.tensormap [%0];" :: "l"(mb) : "memory");
@@ -307,14 +336,14 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
                 for (int k = w.k0; k < w.k1; ++k) {
                     if (!(ok = wait(empty0 + 8u * (uint32_t)s, par))) break;
                     const uint32_t f = full_at + 8u * (uint32_t)s, sb = sa + A.stage_b;
-                    if (CG == 1 || rank == 0) mbar_arrive_expect_tx(full0 + 8u * (uint32_t)s, A.stage_tx);
-                    if constexpr (kRowsA) {
+                    if (CG == 1 || rank == 0) mbar_arrive_expect_tx(full0 + 8u * (uint32_t)s, tx);
+                    if (rows_a) {
                         tma_3d<CG>(sa, ma, m0, at, 0, f);
                         tma_3d<CG>(sa + 8192, ma, m0 + 64, at, 0, f);
                     } else {
                         tma_3d<CG>(sa, ma, at, m0, z, f);
                     }
-                    if constexpr (kRowsB) {
+                    if constexpr (kOut) {
 #pragma unroll
                         for (int i = 0; i < BN / CG / 64; ++i) tma_3d<CG>(sb + i * 8192, mb, n0 + 64 * i, at, 0, f);
                     } else {
@@ -324,7 +353,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
                     ++n;
                     if (many) z += A.chunks;
                     else at += 64;
-                    if (kOut && k + 1 == A.kb0) { at = 0; ++ma; ++mb; }
+                    if (kOut && k + 1 == P.kb0) { at = 0; ++ma; ++mb; }
                     sa += A.stage;
                     if (++s == A.stages) { s = 0; par ^= 1u; sa = ring; }
                 }
@@ -335,15 +364,18 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
     } else if (warp == 1) {
         if (rank == 0) {
             const bool leader = elect_one();
-            const uint32_t idesc = product_idesc<T>(128 * CG, kGated && CG == 1 ? BN / 2 : BN, kRowsA, kRowsB);
-            const uint64_t da = operand_desc(ring, kRowsA), db = operand_desc(ring + A.stage_b, kRowsB);
-            constexpr uint32_t a_step = kRowsA ? 2048 >> 4 : 32 >> 4, b_step = kRowsB ? 2048 >> 4 : 32 >> 4;
+            constexpr uint32_t b_step = kOut ? 2048 >> 4 : 32 >> 4;
+            const uint64_t db = operand_desc(ring + A.stage_b, kOut);
             const uint32_t stage = A.stage >> 4;
             bool ok = true;
             int s = 0, acc = 0;
             uint32_t par = 0u, acc_par = 1u, at = 0u;
             for (int t = first; ok && t < A.tiles; t += step) {
-                const Tile w = tile_of(A, (unsigned)t);
+                const ProductPart &P = part_of(t);
+                const Tile w = tile_of(P, (unsigned)t);
+                const bool rows_a = kOut && P.rows_a;
+                const uint32_t idesc = product_idesc<T>(128 * CG, kGated && CG == 1 ? BN / 2 : BN, rows_a, kOut), a_step = rows_a ? 2048 >> 4 : 32 >> 4, a_chunk = (uint32_t)P.a_rows * 128 >> 4;
+                const uint64_t da = operand_desc(ring, rows_a);
                 if (!(ok = wait_warp(sums_empty0 + 8u * (uint32_t)acc, acc_par))) break;
                 tcgen05_after_sync();
                 const uint32_t d = tmem + (uint32_t)(acc * BN);
@@ -365,7 +397,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
                                 for (int i = 0; i < 4; ++i) mma_f16<CG>(d, a + i * a_step, b + i * b_step, idesc, i > 0 ? 1u : add);
                             }
                             if (CG == 2 || kOut || c + 1 == A.chunks) break;
-                            a += (uint32_t)A.a_rows * 128 >> 4;
+                            a += a_chunk;
                             b += (kGated ? BN / 2 : BN) * 128 >> 4;
                             add = 1u;
                         }
@@ -386,17 +418,22 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
     } else {
         const int quarter = warp & 3, half = (warp - 2) >> 2;
         const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16), buf = ring + (uint32_t)(kRingBytes + (warp - 2) * 4096);
-        const float scale = scale_of(A.amax, A.amax_to), back = 1.f / scale;
+        float scale = scale_of(A.amax, A.amax_to);
+        if constexpr (EPI == PR_DLOGITS) {
+            if (A.amax_out) scale = scale_of_rows(A, warp - 2, lane);
+        }
+        const float back = 1.f / scale;
         int acc = 0;
         uint32_t acc_par = 0u;
         float mx = -INFINITY, sum = 0.f;        // PR_STATS
         for (int t = first; t < A.tiles; t += step) {
-            const Tile w = tile_of(A, (unsigned)t);
+            const ProductPart &P = part_of(t);
+            const Tile w = tile_of(P, (unsigned)t);
             const int row0 = w.m * TM + rank * 128 + quarter * 32, row = row0 + lane;
-            const bool live = row < A.m;
+            const bool live = row < P.m;
             if constexpr (EPI == PR_GATED_GRAD && CG == 2) {
                 rows_free(lane);
-                rows_fetch(reinterpret_cast<const T *>(A.g_y), A.g_y_ld, row0, A.m, w.n * (BN / 2) + half * (BN / 4), A.n, (A.g_y_ld & 7) == 0 && ((uintptr_t)A.g_y & 15) == 0, buf, lane);
+                rows_fetch(reinterpret_cast<const T *>(A.g_y), A.g_y_ld, row0, P.m, w.n * (BN / 2) + half * (BN / 4), P.n, (A.g_y_ld & 7) == 0 && ((uintptr_t)A.g_y & 15) == 0, buf, lane);
             }
             if (!wait_warp(sums_full0 + 8u * (uint32_t)acc, acc_par)) break;
             tcgen05_after_sync();
@@ -428,7 +465,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
                         } else {
                             const T *gy = reinterpret_cast<const T *>(A.g_y) + (long long)row * A.g_y_ld;
 #pragma unroll
-                            for (int i = 0; i < N; ++i) x[i] = live && col + i < A.n ? to_f(gy[col + i]) * scale : 0.f;
+                            for (int i = 0; i < N; ++i) x[i] = live && col + i < P.n ? to_f(gy[col + i]) * scale : 0.f;
                         }
                     }
                     tmem_wait_ld();
@@ -440,7 +477,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
                             x[i] = a * __uint_as_float(vu[i]);
                         }
                         if constexpr (CG == 2) put_row<T>(buf, lane, c / 8, x);
-                        else if (live) store_row(reinterpret_cast<T *>(A.out[0]) + (long long)row * A.out_ld, col, A.n, (A.out_ld & 7) == 0 && ((uintptr_t)A.out[0] & 15) == 0, x);
+                        else if (live) store_row(reinterpret_cast<T *>(A.out[0]) + (long long)row * A.out_ld, col, P.n, (A.out_ld & 7) == 0 && ((uintptr_t)A.out[0] & 15) == 0, x);
                     } else {
                         float y[N];
 #pragma unroll
@@ -465,13 +502,13 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
                 if (A.activation == ACT_SILU) columns(std::integral_constant<int, ACT_SILU>());
                 else columns(std::integral_constant<int, ACT_GELU>());
                 if constexpr (CG == 2) {
-                    if (A.tma_out) rows_store(&M.out[0], buf, col0, row0, 0, false, row0 < A.m && col0 < A.n, lane);
-                    else rows_copy_out(reinterpret_cast<T *>(A.out[0]), A.out_ld, row0, A.m, col0, A.n, buf, lane);
+                    if (A.tma_out) rows_store(&M.out[0], buf, col0, row0, 0, row0 < P.m && col0 < P.n, lane);
+                    else rows_copy_out(reinterpret_cast<T *>(A.out[0]), A.out_ld, row0, P.m, col0, P.n, buf, lane);
                     if constexpr (EPI == PR_GATED_GRAD) {
                         rows_free(lane);
 #pragma unroll
                         for (int i = 0; i < BN / 32; ++i) sts128(piece_at(buf, lane, i), make_uint4(held[4 * i], held[4 * i + 1], held[4 * i + 2], held[4 * i + 3]));
-                        rows_store(&M.out[1], buf, col0, row0, 0, false, row0 < A.m && col0 < A.n, lane);
+                        rows_store(&M.out[1], buf, col0, row0, 0, row0 < P.m && col0 < P.n, lane);
                     }
                 }
             } else {
@@ -495,19 +532,93 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
                         }
                     }
                 }
+                if constexpr (kOut) {
+                    constexpr int kPieces = BN / 64, kTile = CG * kEpiWarps * kPieces * 1024;        // of 32 columns a warp; fp32 sums of a tile
+                    // Sums in memory lie as the threads hold them: piece by piece, four columns of the 32 rows side by side.
+                    auto place = [&](float *p, long long tile) { return p + tile * kTile + ((rank * kEpiWarps + warp - 2) * kPieces) * 1024 + lane * 4; };
+                    bool mine = true;
+                    if (P.splits > 1) {
+                        // Every split leaves its sums; whoever comes last of a tile's and a warp's adds them up, in the order of the splits.
+                        float *p = place(P.partial, (long long)w.at * P.splits + w.split);
+#pragma unroll 1
+                        for (int c = 0; c < kPieces; ++c) {
+                            uint32_t v[32];
+                            tmem_ld(v, sums + (uint32_t)(half * (BN / 2) + c * 32));
+                            tmem_wait_ld();
+#pragma unroll
+                            for (int i = 0; i < 8; ++i)
+                                __stcg(reinterpret_cast<uint4 *>(p + c * 1024 + i * 128), make_uint4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]));
+                        }
+                        __threadfence();
+                        __syncwarp();
+                        unsigned before = 0;
+                        if (lane == 0) before = atomicInc(A.counter + P.counters + (unsigned)((w.at * CG + rank) * kEpiWarps + warp - 2), (unsigned)P.splits - 1u);
+                        mine = __shfl_sync(0xffffffffu, before, 0) == (unsigned)P.splits - 1u;
+                        __threadfence();
+                    }
+                    if (mine) {
+#pragma unroll 1
+                        for (int c = 0; c < kPieces; ++c) {
+                            const int col = col0 + c * 32;
+                            uint32_t v[32];
+                            float x[32];
+                            tmem_ld(v, sums + (uint32_t)(half * (BN / 2) + c * 32));
+                            tmem_wait_ld();
+                            if (P.splits > 1) {
+#pragma unroll 1
+                                for (int s = 0; s < P.splits; ++s) {
+                                    const float *p = place(P.partial, (long long)w.at * P.splits + s) + c * 1024;
+#pragma unroll
+                                    for (int i = 0; i < 8; ++i) {
+                                        const float4 q = s == w.split ? make_float4(__uint_as_float(v[4 * i]), __uint_as_float(v[4 * i + 1]), __uint_as_float(v[4 * i + 2]), __uint_as_float(v[4 * i + 3]))
+                                                                      : __ldcg(reinterpret_cast<const float4 *>(p + i * 128));
+                                        x[4 * i] = s ? x[4 * i] + q.x : q.x;
+                                        x[4 * i + 1] = s ? x[4 * i + 1] + q.y : q.y;
+                                        x[4 * i + 2] = s ? x[4 * i + 2] + q.z : q.z;
+                                        x[4 * i + 3] = s ? x[4 * i + 3] + q.w : q.w;
+                                    }
+                                }
+                            } else {
+#pragma unroll
+                                for (int i = 0; i < 32; ++i) x[i] = __uint_as_float(v[i]);
+                            }
+                            if (P.sums) {
+                                float *p = place(P.sums, w.at) + c * 1024;
+#pragma unroll
+                                for (int i = 0; i < 8; ++i) {
+                                    float4 *q = reinterpret_cast<float4 *>(p + i * 128);
+                                    if (P.go_on) {
+                                        const float4 o = *q;
+                                        x[4 * i] += o.x; x[4 * i + 1] += o.y; x[4 * i + 2] += o.z; x[4 * i + 3] += o.w;
+                                    }
+                                    if (!P.end) *q = make_float4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
+                                }
+                                if (!P.end) continue;
+                            }
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) x[i] *= back;
+                            if constexpr (CG == 2) {
+                                if ((c & 1) == 0) rows_free(lane);
+                                put_row<T>(buf, lane, (c & 1) * 4, x);
+                                if (c & 1) rows_store(&M.out[P.map_out + w.job], buf, col - 32, row0, 0, row0 < P.m && col - 32 < P.n, lane);
+                            } else if (live) {
+                                store_row(reinterpret_cast<T *>(P.out[w.job]) + (long long)row * P.out_ld, col, P.n, true, x);
+                            }
+                        }
+                    }
+                } else {
 #pragma unroll 1
                 for (int c = 0; c < BN / 2; c += N) {
                     uint32_t v[N];
                     tmem_ld(v, sums + (uint32_t)(half * (BN / 2) + c));
                     const int col = col0 + c;
-                    if (CG == 2 && EPI != PR_STATS && (A.partial || (c & 32) == 0)) rows_free(lane);
+                    if (CG == 2 && EPI == PR_DLOGITS && (c & 32) == 0) rows_free(lane);
                     tmem_wait_ld();
-                    float x[N];
                     if constexpr (EPI == PR_STATS) {
-                        if (col + N > A.n) {
+                        if (col + N > P.n) {
 #pragma unroll
                             for (int i = 0; i < N; ++i)
-                                if (col + i >= A.n) v[i] = 0xff800000u;        // -infinity
+                                if (col + i >= P.n) v[i] = 0xff800000u;        // -infinity
                         }
                         float top = __uint_as_float(v[0]);
 #pragma unroll
@@ -525,54 +636,31 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
                         for (int i = 0; i < N; ++i) more[i & 1] += ex2(fmaf(__uint_as_float(v[i]), A.c, -base));
                         sum = fmaf(sum, ex2(was - base), more[0] + more[1]);
                     } else {
-                        if constexpr (EPI == PR_DLOGITS) {
+                        float x[N];
 #pragma unroll
-                            for (int i = 0; i < N; ++i) {
-                                x[i] = -gp * ex2(fmaf(__uint_as_float(v[i]), A.c, -lse2));
-                            }
-                            if (token >= col && token < col + N) {
+                        for (int i = 0; i < N; ++i) x[i] = -gp * ex2(fmaf(__uint_as_float(v[i]), A.c, -lse2));
+                        if (token >= col && token < col + N) {
 #pragma unroll
-                                for (int i = 0; i < N; ++i)
-                                    if (token == col + i) x[i] += g;
-                            }
-                        } else {
-#pragma unroll
-                            for (int i = 0; i < N; ++i) x[i] = __uint_as_float(v[i]) * back;
+                            for (int i = 0; i < N; ++i)
+                                if (token == col + i) x[i] += g;
                         }
-                        if (kOut && A.partial) {
-                            if constexpr (CG == 2) {
-#pragma unroll
-                                for (int i = 0; i < 8; ++i) sts128(piece_at(buf, lane, i), make_uint4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]));
-                                rows_store(&M.out[0], buf, col, row0, w.job * A.splits + w.split, A.add != 0, row0 < A.m && col < A.n, lane);
-                            } else if (live) {
-                                float *p = A.partial + (((long long)w.job * A.splits + w.split) * A.m + row) * A.n + col;
-#pragma unroll
-                                for (int i = 0; i < N; i += 4)
-                                    if (col + i < A.n) {
-                                        float4 o = make_float4(__uint_as_float(v[i]), __uint_as_float(v[i + 1]), __uint_as_float(v[i + 2]), __uint_as_float(v[i + 3]));
-                                        if (A.add) {
-                                            const float4 q = *reinterpret_cast<const float4 *>(p + i);
-                                            o.x += q.x; o.y += q.y; o.z += q.z; o.w += q.w;
-                                        }
-                                        *reinterpret_cast<float4 *>(p + i) = o;
-                                    }
-                            }
-                        } else if constexpr (CG == 2) {
+                        if constexpr (CG == 2) {
                             put_row<T>(buf, lane, (c & 32) / 8, x);
-                            if (c & 32) rows_store(&M.out[w.job], buf, col - 32, row0, 0, false, row0 < A.m && col - 32 < A.n, lane);
+                            if (c & 32) rows_store(&M.out[0], buf, col - 32, row0, 0, row0 < P.m && col - 32 < P.n, lane);
                         } else if (live) {
-                            store_row(reinterpret_cast<T *>(A.out[w.job]) + (long long)row * A.out_ld, col, EPI == PR_DLOGITS ? (int)A.out_ld : A.n, true, x);
+                            store_row(reinterpret_cast<T *>(A.out[0]) + (long long)row * A.out_ld, col, (int)A.out_ld, true, x);
                         }
                     }
                 }
+                }
                 if constexpr (EPI == PR_STATS) {
                     if (!A.carry) {
-                        if (live) A.parts[(long long)(2 * w.n + half) * A.m + row] = make_float2(mx, sum);
+                        if (live) A.parts[(long long)(2 * w.n + half) * P.m + row] = make_float2(mx, sum);
                         mx = -INFINITY;
                         sum = 0.f;
                     } else if (t + step >= A.tiles && live) {
                         if (A.counter) A.parts[(long long)row * 2 * gridDim.x + 2 * first + half] = make_float2(mx, sum);
-                        else A.parts[(long long)(2 * first + half) * A.m + row] = make_float2(mx, sum);
+                        else A.parts[(long long)(2 * first + half) * P.m + row] = make_float2(mx, sum);
                     }
                 }
             }
@@ -612,7 +700,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
             }
             __syncthreads();
             if (last_of_all)
-                for (int row = warp; row < A.m; row += kProductThreads / 32) {
+                for (int row = warp; row < A.part[0].m; row += kProductThreads / 32) {
                     RowSums r;
 #pragma unroll 4
                     for (int i = lane; i < 2 * (int)gridDim.x; i += 32) r.take(__ldcg(&A.parts[(long long)row * 2 * gridDim.x + i]));
@@ -677,32 +765,6 @@ __global__ void __launch_bounds__(32) amax_pairs_kernel(const float *g, long lon
     if (threadIdx.x == 0) amax[blockIdx.x] = m;
 }
 
-struct JoinArgs {
-    const float *partial, *amax;
-    void *out[2];
-    long long out_ld, all;          // all: quads of a job
-    int m, n, splits, amax_to;
-};
-template <typename T> __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ JoinArgs A) {
-    chain_go();
-    chain_wait();
-    const float back = 1.f / scale_of(A.amax, A.amax_to);
-    const int quads = A.n / 4, job = blockIdx.y;
-    for (long long i = blockIdx.x * 256ll + threadIdx.x; i < A.all; i += gridDim.x * 256ll) {
-        const long long r = i / quads;
-        const int c = (int)(i - r * quads) * 4;
-        const float *p = A.partial + ((long long)job * A.splits * A.m + r) * A.n + c;
-        float4 s = *reinterpret_cast<const float4 *>(p);
-#pragma unroll 4
-        for (int k = 1; k < A.splits; ++k) {
-            const float4 q = *reinterpret_cast<const float4 *>(p + (long long)k * A.m * A.n);
-            s.x += q.x; s.y += q.y; s.z += q.z; s.w += q.w;
-        }
-        T *o = reinterpret_cast<T *>(A.out[job]) + r * A.out_ld + c;
-        *reinterpret_cast<uint2 *>(o) = make_uint2(pack2<T>(s.x * back, s.y * back), pack2<T>(s.z * back, s.w * back));
-    }
-}
-
 // ------------------------------------------------------------------------------------------------------ host
 
 typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
@@ -731,14 +793,12 @@ static bool operand_map(EncodeTiledFn encode, CUtensorMap *out, const Operand &o
                   CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// Results as a warp stores them: 32 rows of 64 elements (partial sums: 32 numbers).
-static bool result_map(EncodeTiledFn encode, CUtensorMap *out, const ProductArgs &A, int dtype, bool sums, int i) {
-    const cuuint64_t ld = sums ? (cuuint64_t)A.n * 4 : (cuuint64_t)A.out_ld * 2;
-    cuuint64_t dims[3] = {(cuuint64_t)A.n, (cuuint64_t)A.m, sums ? (cuuint64_t)A.jobs * A.splits : 1}, strides[2] = {ld, ld * A.m};
-    cuuint32_t box[3] = {sums ? 32u : 64u, 32, 1}, one[3] = {1, 1, 1};
-    return encode(out, sums ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : dtype == XSM_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3,
-                  sums ? (void *)A.partial : A.out[i], dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_NONE,
-                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+// Results as a warp stores them: 32 rows of 64 elements.
+static bool result_map(EncodeTiledFn encode, CUtensorMap *out, void *p, int m, int n, long long ld, int dtype) {
+    cuuint64_t dims[3] = {(cuuint64_t)n, (cuuint64_t)m, 1}, strides[2] = {(cuuint64_t)ld * 2, (cuuint64_t)ld * 2 * m};
+    cuuint32_t box[3] = {64, 32, 1}, one[3] = {1, 1, 1};
+    return encode(out, dtype == XSM_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, p, dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                  CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 int product_sms() {
@@ -762,12 +822,6 @@ void product_waits(unsigned *tries, int *starve) {
     *starve = g_starve.load(std::memory_order_relaxed);
 }
 
-int product_splits(long long tiles, int kb, bool wide) {
-    const int slots = wide ? product_sms() / 2 : product_sms();
-    const long long s = tiles > 0 ? slots / tiles : 1;
-    return (int)(s < 1 ? 1 : s > kb / 8 ? (kb / 8 < 1 ? 1 : kb / 8) : s);
-}
-
 template <int CG, int BN, int EPI, typename T> static cudaError_t start(const ProductMaps &M, const ProductArgs &A, cudaStream_t st) {
     const int smem = kRingBytes + (CG == 2 ? kEpiWarps * 4096 : kABytes) + 1024;        // (few rows: the tensor cores read 128 rows of A whatever the box brought)
     const void *fn = (const void *)product_kernel<CG, BN, EPI, T>;
@@ -788,27 +842,14 @@ template <int CG, int BN, int EPI, typename T> static cudaError_t start(const Pr
     cfg.numAttrs = CG == 2 ? 2 : 1;
     return cudaLaunchKernelEx(&cfg, product_kernel<CG, BN, EPI, T>, M, A);
 }
-template <int CG, int BN, typename T> static cudaError_t start_epi(ProductEpi epi, const ProductMaps &M, const ProductArgs &A, cudaStream_t st) {
-    if (epi == PR_STATS) return start<CG, BN, PR_STATS, T>(M, A, st);
-    if (epi == PR_DLOGITS) return start<CG, BN, PR_DLOGITS, T>(M, A, st);
-    if constexpr (BN > 32) switch (epi) {
-        case PR_GATED: return start<CG, BN, PR_GATED, T>(M, A, st);
-        case PR_GATED_GRAD: return start<CG, BN, PR_GATED_GRAD, T>(M, A, st);
-        case PR_OUT: return start<CG, BN, PR_OUT, T>(M, A, st);
-        default: return start<CG, BN, PR_OUT_ROWS, T>(M, A, st);
-    }
-    return cudaErrorInvalidValue;
-}
-
 // Rows of more than one tile of 128 take two CTAs a tile.  Few rows: what a CTA fetches decides, its tiles times the rows of both operands; of the widths that fetch
-// least, the widest.  (96 rows x 131071 tokens: 64 columns 83 us, 128 ...; 5 rows x 4096: ...)  Operands whose rows run along the summed axis come in boxes of 64
-// columns.
+// least, the widest.  (96 rows x 131071 tokens: 64 columns 83 us, 128 49; 5 rows x 4096: 64 columns 10.6, 32 9.8, before stages of several blocks.)
 ProductCut product_cut(ProductEpi epi, long long m, long long n) {
     const bool gated = epi == PR_GATED || epi == PR_GATED_GRAD;
     if (m > 128 && n > (gated ? 32 : 64)) return {true, 256};
     ProductCut best = {false, 128};
     double least = 1e300;
-    for (int bn = 128; bn >= (gated || epi == PR_OUT || epi == PR_OUT_ROWS ? 64 : 32); bn /= 2) {
+    for (int bn = 128; bn >= (gated ? 64 : 32); bn /= 2) {
         const ProductCut c = {false, bn};
         const long long sms = product_sms() < 1 ? 1 : product_sms();
         const double cost = (double)((c.tiles(m, n, gated) + sms - 1) / sms) * (double)((m < 128 ? m : 128) + bn);
@@ -817,64 +858,180 @@ ProductCut product_cut(ProductEpi epi, long long m, long long n) {
     return best;
 }
 
-cudaError_t launch_product(ProductEpi epi, int dtype, ProductCut cut, ProductArgs A, const Operand (&a)[2], const Operand (&b)[2], int pairs, cudaStream_t st) {
+// Tiles, splits and their divisors; false: too many
+static bool fill_part(ProductPart &P, const ProductCut &cut, bool gated, int m, int n, long long stages, int pairs, int jobs, int splits, long long first) {
+    P.m = m; P.n = n; P.jobs = jobs; P.splits = splits;
+    P.tiles_m = (m + cut.tm() - 1) / cut.tm();
+    const long long tiles_n = (n + cut.tn(gated) - 1) / cut.tn(gated), tiles = P.tiles_m * tiles_n * jobs * splits;
+    if (first + tiles > 0x3fffffff || stages * pairs > 0x3fffffff) return false;
+    P.first = (int)first;
+    P.tiles = (int)tiles;
+    P.kb0 = (int)stages;
+    P.kb = P.kb0 * pairs;
+    P.group_m = P.tiles_m < 8 ? P.tiles_m : 8;
+    const int last_rows = P.tiles_m % P.group_m;
+    P.by_plane = Divisor((unsigned)(P.tiles_m * tiles_n));
+    P.by_group = Divisor((unsigned)(P.group_m * tiles_n));
+    P.by_rows = Divisor((unsigned)P.group_m);
+    P.by_last_rows = Divisor((unsigned)(last_rows ? last_rows : P.group_m));
+    P.by_splits = Divisor((unsigned)splits);
+    P.kb_each = P.kb / splits;
+    P.kb_more = P.kb % splits;
+    return true;
+}
+
+template <int EPI> static cudaError_t start_cut(const ProductCut &cut, int dtype, const ProductMaps &M, const ProductArgs &A, cudaStream_t st) {
+    const bool bf = dtype == XSM_BF16;
+    auto go = [&](auto cg, auto bn) {
+        constexpr int CG = decltype(cg)::value, BN = decltype(bn)::value;
+        return bf ? start<CG, BN, EPI, bf16>(M, A, st) : start<CG, BN, EPI, __half>(M, A, st);
+    };
+    using std::integral_constant;
+    if (cut.wide) return go(integral_constant<int, 2>(), integral_constant<int, 256>());
+    if constexpr (EPI != PR_OUT) {
+        if (cut.bn == 128) return go(integral_constant<int, 1>(), integral_constant<int, 128>());
+    }
+    if constexpr (EPI == PR_STATS || EPI == PR_DLOGITS) {
+        if (cut.bn == 32) return go(integral_constant<int, 1>(), integral_constant<int, 32>());
+    }
+    return go(integral_constant<int, 1>(), integral_constant<int, 64>());
+}
+
+cudaError_t launch_product(ProductEpi epi, int dtype, ProductCut cut, ProductArgs A, int m, int n, const Operand &a, const Operand (&b)[2], cudaStream_t st) {
     EncodeTiledFn encode;
     cudaError_t e = encoder(&encode);
     if (e != cudaSuccess) return e;
-    const bool gated = epi == PR_GATED || epi == PR_GATED_GRAD, wide = cut.wide, a_rows_summed = epi == PR_OUT_ROWS, b_rows_summed = epi == PR_OUT || epi == PR_OUT_ROWS;
-    const int tm = cut.tm(), tn = cut.tn(gated), group = wide ? 2 : 1;
-    A.tiles_m = (A.m + tm - 1) / tm;
-    A.tiles_n = (A.n + tn - 1) / tn;
-    const long long summed = a_rows_summed ? a[0].rows : a[0].row;
-    A.a_rows = A.m >= 128 ? 128 : (A.m + 7) / 8 * 8;
+    const bool gated = epi == PR_GATED || epi == PR_GATED_GRAD, wide = cut.wide;
+    const int group = wide ? 2 : 1, a_rows = m >= 128 ? 128 : (m + 7) / 8 * 8;
     // Few rows: a stage of several blocks, each operand's by one copy, as long as three stages fit; a copy costs the TMA unit some 200 cycles whatever it brings (5 rows x 4096
-    // tokens ... us).
+    // tokens 9.8 -> 7.8 us).
     A.chunks = 1;
-    if (!wide && !b_rows_summed && summed % 64 == 0)
-        while (A.chunks < 4 && 2 * A.chunks <= summed / 64 && 2 * A.chunks * (A.a_rows + cut.bn) * 128 * 3 <= kRingBytes) A.chunks *= 2;
-    A.kb0 = (int)((summed + 64 * A.chunks - 1) / (64 * A.chunks));
-    A.kb = A.kb0 * pairs;
-    const long long tiles = (long long)A.tiles_m * A.tiles_n * A.jobs * A.splits;
-    if (tiles > 0x3fffffff) return cudaErrorInvalidValue;
-    A.tiles = (int)tiles;
-    A.group_m = A.tiles_m < 8 ? A.tiles_m : 8;
-    const int last_rows = A.tiles_m % A.group_m;
-    A.by_plane = Divisor((unsigned)(A.tiles_m * A.tiles_n));
-    A.by_group = Divisor((unsigned)(A.group_m * A.tiles_n));
-    A.by_rows = Divisor((unsigned)A.group_m);
-    A.by_last_rows = Divisor((unsigned)(last_rows ? last_rows : A.group_m));
-    A.by_splits = Divisor((unsigned)A.splits);
-    A.kb_each = A.kb / A.splits;
-    A.kb_more = A.kb % A.splits;
-    const int b_box = gated ? (wide ? 128 : cut.bn / 2) : cut.bn / group;
-    A.stage_b = (uint32_t)((a_rows_summed ? kABytes : A.a_rows * 128) * A.chunks);
+    if (!wide && a.row % 64 == 0)
+        while (A.chunks < 4 && 2 * A.chunks <= a.row / 64 && 2 * A.chunks * (a_rows + cut.bn) * 128 * 3 <= kRingBytes) A.chunks *= 2;
+    ProductPart &P = A.part[0];
+    if (!fill_part(P, cut, gated, m, n, (a.row + 64 * A.chunks - 1) / (64 * A.chunks), 1, 1, 1, 0)) return cudaErrorInvalidValue;
+    A.tiles = P.tiles;
+    P.a_rows = a_rows;
+    A.stage_b = (uint32_t)(a_rows * 128 * A.chunks);
     A.stage = A.stage_b + (uint32_t)(cut.bn / group * 128 * A.chunks);
-    A.stage_tx = group * A.stage;
+    P.stage_tx = group * A.stage;
     A.stages = kRingBytes / (int)A.stage < kMaxStages ? kRingBytes / (int)A.stage : kMaxStages;
     product_waits(&A.tries, &A.starve);
     ProductMaps M;
     memset(&M, 0, sizeof M);
-    const int na = pairs > A.jobs ? pairs : A.jobs, nb = gated ? 2 : pairs;
-    for (int i = 0; i < na; ++i)
-        if (!operand_map(encode, &M.a[i], a[i], dtype, a_rows_summed ? 64 : A.a_rows, A.chunks)) return cudaErrorInvalidValue;
-    for (int i = 0; i < nb; ++i)
-        if (!operand_map(encode, &M.b[i], b[i], dtype, b_rows_summed ? 64 : b_box, A.chunks)) return cudaErrorInvalidValue;
+    const int b_box = gated ? (wide ? 128 : cut.bn / 2) : cut.bn / group;
+    bool ok = operand_map(encode, &M.a[0], a, dtype, a_rows, A.chunks);
+    for (int i = 0; i < (gated ? 2 : 1); ++i) ok = ok && operand_map(encode, &M.b[i], b[i], dtype, b_box, A.chunks);
     if (wide && epi != PR_STATS) {
-        const bool sums = b_rows_summed && A.partial;
-        const int outs = sums ? 1 : epi == PR_GATED_GRAD ? 2 : A.jobs;
-        A.tma_out = sums || (A.out_ld % 8 == 0 && (uintptr_t)A.out[0] % 16 == 0);
-        for (int i = 0; i < outs && A.tma_out; ++i)
-            if (!result_map(encode, &M.out[i], A, dtype, sums, i)) return cudaErrorInvalidValue;
+        A.tma_out = A.out_ld % 8 == 0 && (uintptr_t)A.out[0] % 16 == 0;
+        for (int i = 0; i < (epi == PR_GATED_GRAD ? 2 : 1) && A.tma_out; ++i) ok = ok && result_map(encode, &M.out[i], A.out[i], m, n, A.out_ld, dtype);
     }
-    const bool bf = dtype == XSM_BF16;
-    auto go = [&](auto cg, auto bn) {
-        constexpr int CG = decltype(cg)::value, BN = decltype(bn)::value;
-        return bf ? start_epi<CG, BN, bf16>(epi, M, A, st) : start_epi<CG, BN, __half>(epi, M, A, st);
-    };
-    using std::integral_constant;
-    if (wide) return go(integral_constant<int, 2>(), integral_constant<int, 256>());
-    if (cut.bn == 128) return go(integral_constant<int, 1>(), integral_constant<int, 128>());
-    return cut.bn == 64 ? go(integral_constant<int, 1>(), integral_constant<int, 64>()) : go(integral_constant<int, 1>(), integral_constant<int, 32>());
+    if (!ok) return cudaErrorInvalidValue;
+    switch (epi) {
+        case PR_STATS: return start_cut<PR_STATS>(cut, dtype, M, A, st);
+        case PR_DLOGITS: return start_cut<PR_DLOGITS>(cut, dtype, M, A, st);
+        case PR_GATED: return start_cut<PR_GATED>(cut, dtype, M, A, st);
+        case PR_GATED_GRAD: return start_cut<PR_GATED_GRAD>(cut, dtype, M, A, st);
+        default: return cudaErrorInvalidValue;
+    }
+}
+
+static size_t tile_bytes(const ProductCut &cut) { return (size_t)cut.tm() * cut.bn * 4; }
+size_t sums_bytes(const ProductCut &cut, long long rows, long long d) { return (size_t)cut.tiles(rows, d, false) * tile_bytes(cut); }
+
+// Both products' tiles are dealt out in one row, x's first.  Tiles are as wide as the larger product asks for.  Where there are few of them the summed axes are cut: of the splits
+// that leave the CTAs with most to do least, in blocks of 64: a tile costs eight blocks on top (its last products, what is done with its sums), one that is cut sixteen, and two
+// for every split that is added up.
+SumsPlan plan_sums(long long rows, long long cols, long long d, int pairs, bool x, bool y) {
+    SumsPlan p = {};
+    p.cut = (x && rows > 128 && d > 64) || (y && cols > 128 && d > 64) ? ProductCut{true, 256} : ProductCut{false, 64};
+    const long long slots = product_sms() < 2 ? 1 : p.cut.wide ? product_sms() / 2 : product_sms(), kx = (cols + 63) / 64 * pairs, ky = (rows + 63) / 64;
+    const long long tx = x ? p.cut.tiles(rows, d, false) : 0, ty = y ? p.cut.tiles(cols, d, false) * pairs : 0, per = (p.cut.wide ? 2 : 1) * 8;
+    p.splits_x = p.splits_y = 1;
+    if (tx + ty < 4 * slots) {
+        static const int tries[] = {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 40, 48, 64, 96, 128};
+        auto cost = [&](long long k, int s) { return (double)((k + s - 1) / s) + (s > 1 ? 16 + 2 * s : 8); };
+        double least = 1e300;
+        for (int sx : tries) {
+            if (sx > 1 && (!x || sx * 4 > kx)) break;
+            for (int sy : tries) {
+                if (sy > 1 && (!y || sy * 4 > ky)) break;
+                if ((sx > 1 ? tx : 0) * per + (sy > 1 ? ty : 0) * per > kSumCounters) continue;
+                const long long nx = tx * sx, all = nx + ty * sy;
+                const double cx = cost(kx, sx), cy = cost(ky, sy);
+                double most = 0;
+                auto of = [&](long long c) {        // what CTA (pair) c has to do: tiles c, c + slots, ...
+                    if (c < 0 || c >= slots || c >= all) return;
+                    const long long mine = (all - 1 - c) / slots + 1, of_x = c < nx ? (nx - 1 - c) / slots + 1 : 0;
+                    const double t = of_x * cx + (mine - of_x) * cy;
+                    if (t > most) most = t;
+                };
+                of(0); of(nx % slots - 1); of(nx % slots); of(all % slots - 1); of(all % slots);
+                if (most < least - 1e-9) { least = most; p.splits_x = sx; p.splits_y = sy; }
+            }
+        }
+    }
+    p.partial_x = 0;
+    p.partial_y = p.splits_x > 1 ? (size_t)tx * p.splits_x * tile_bytes(p.cut) : 0;
+    p.bytes = p.partial_y + (p.splits_y > 1 ? (size_t)ty * p.splits_y * tile_bytes(p.cut) : 0);
+    return p;
+}
+
+cudaError_t launch_sums(int dtype, const SumsPlan &p, const Sums &s, cudaStream_t st) {
+    EncodeTiledFn encode;
+    cudaError_t e = encoder(&encode);
+    if (e != cudaSuccess) return e;
+    const int group = p.cut.wide ? 2 : 1;
+    const int rows = (int)s.g[0].rows, cols = (int)s.g[0].row, d = (int)s.h.row;
+    ProductArgs A = {};
+    A.status = s.status;
+    A.counter = s.counters;
+    A.amax = s.amax;
+    A.amax_to = s.amax_to;
+    A.chunks = 1;
+    A.stage_b = kABytes;
+    A.stage = kABytes + (uint32_t)(p.cut.bn / group * 128);
+    A.stages = kRingBytes / (int)A.stage < kMaxStages ? kRingBytes / (int)A.stage : kMaxStages;
+    product_waits(&A.tries, &A.starve);
+    ProductMaps M;
+    memset(&M, 0, sizeof M);
+    ProductPart &X = A.part[0], &Y = A.part[1];
+    bool ok = true;
+    const bool y = s.y[0] != nullptr;
+    if (s.x) {
+        const int splits = p.splits_x <= (cols + 63) / 64 * s.pairs ? p.splits_x : (cols + 63) / 64 * s.pairs;        // (the last piece of a vocabulary may be short)
+        if (!fill_part(X, p.cut, false, rows, d, (cols + 63) / 64, s.pairs, 1, splits, 0)) return cudaErrorInvalidValue;
+        X.a_rows = rows >= 128 ? 128 : (rows + 7) / 8 * 8;
+        X.stage_tx = (uint32_t)(group * (X.a_rows * 128 + p.cut.bn / group * 128));
+        X.partial = (float *)(s.partial + p.partial_x);
+        X.sums = s.x_sums; X.go_on = s.go_on; X.end = s.end;
+        X.out[0] = s.x; X.out_ld = s.x_ld;
+        for (int i = 0; i < s.pairs; ++i) {
+            ok = ok && operand_map(encode, &M.a[i], s.g[i], dtype, X.a_rows, 1) && operand_map(encode, &M.b[i], s.w[i], dtype, 64, 1);
+        }
+        if (p.cut.wide) ok = ok && result_map(encode, &M.out[0], s.x, rows, d, s.x_ld, dtype);
+    }
+    A.tiles = X.tiles;
+    Y.first = 0x7fffffff;
+    if (y) {
+        if (!fill_part(Y, p.cut, false, cols, d, (rows + 63) / 64, 1, s.pairs, p.splits_y, A.tiles)) return cudaErrorInvalidValue;
+        Y.rows_a = 1;
+        Y.a_rows = 128;
+        Y.stage_tx = group * A.stage;
+        Y.map_a = 2; Y.map_b = 2; Y.map_out = 1;
+        Y.partial = (float *)(s.partial + p.partial_y);
+        Y.counters = X.splits > 1 ? (unsigned)(X.by_plane.d * group * 8) : 0;
+        for (int i = 0; i < s.pairs; ++i) {
+            ok = ok && operand_map(encode, &M.a[2 + i], s.g[i], dtype, 64, 1);
+            Y.out[i] = s.y[i];
+            if (p.cut.wide) ok = ok && result_map(encode, &M.out[1 + i], s.y[i], cols, d, s.y_ld, dtype);
+        }
+        Y.out_ld = s.y_ld;
+        ok = ok && operand_map(encode, &M.b[2], s.h, dtype, 64, 1);
+        A.tiles += Y.tiles;
+    }
+    if (!ok) return cudaErrorInvalidValue;
+    return A.tiles ? start_cut<PR_OUT>(p.cut, dtype, M, A, st) : cudaSuccess;
 }
 
 cudaError_t launch_amax_rows(const void *x, int dtype, long long rows, long long cols, long long ld, float *amax, cudaStream_t st) {
@@ -889,18 +1046,6 @@ cudaError_t launch_amax_rows(const void *x, int dtype, long long rows, long long
 }
 cudaError_t launch_amax_pairs(const float *g, long long g_ld, const float *h, long long h_ld, int rows, float by, float *amax, cudaStream_t st) {
     return launch_early(amax_pairs_kernel, dim3(kAmaxBlocks), dim3(32), 0, st, g, g_ld, h, h_ld, rows, by, amax);
-}
-
-cudaError_t launch_join(const ProductArgs &A, int dtype, cudaStream_t st) {
-    JoinArgs J;
-    J.partial = A.partial; J.amax = A.amax;
-    J.out[0] = A.out[0]; J.out[1] = A.out[1];
-    J.out_ld = A.out_ld; J.all = (long long)A.m * (A.n / 4);
-    J.m = A.m; J.n = A.n; J.splits = A.splits; J.amax_to = A.amax_to;
-    const long long blocks = (J.all + 255) / 256, most = (long long)product_sms() * 8;
-    const dim3 grid((unsigned)(blocks < most ? blocks : most), (unsigned)A.jobs);
-    if (dtype == XSM_BF16) return launch_early(join_kernel<bf16>, grid, dim3(256), 0, st, J);
-    return launch_early(join_kernel<__half>, grid, dim3(256), 0, st, J);
 }
 
 }  // namespace xsm

@@ -13,27 +13,44 @@ enum ProductEpi {
     PR_DLOGITS,      // gradient by the logits
     PR_GATED,        // act(gate) * up
     PR_GATED_GRAD,   // gradients by gate and up
-    PR_OUT,          // the sums themselves: rounded to the output's type, or fp32 partial sums
-    PR_OUT_ROWS      // the same for an A whose rows run along the summed axis
+    PR_OUT           // the sums themselves: one or two products of B whose rows run along the summed axis
 };
 enum Activation { ACT_SILU = 0, ACT_GELU = 1 };
 
 constexpr int kAmaxBlocks = 256;
 
-struct __align__(64) ProductMaps { CUtensorMap a[2], b[2], out[2]; };
+constexpr int kSumCounters = 2048;      // words that PR_OUT counts in
 
-struct ProductArgs {
-    int m, n;                       // rows and columns of the result (PR_GATED: n columns of gate and of up)
-    int tiles_m, tiles_n, jobs, splits, tiles;
+// One product of a launch.
+struct ProductPart {
+    int m, n;                       // rows and columns of the result (PR_GATED*: n columns of gate and of up)
+    int first, tiles;               // number of its first tile, tiles of it
+    int tiles_m, group_m;           // tiles of rows, how many of them are worked on side by side
+    int jobs, splits;
     int kb0, kb;                    // stages along the summed axis: of the first pair of operands, of all
-    int kb_each, kb_more;           // blocks of a split, and how many splits have one more
+    int kb_each, kb_more;           // stages of a split, and how many splits have one more
     Divisor by_plane, by_group, by_rows, by_last_rows, by_splits;      // tiles of a split, of a group, rows of a group, of the last one
     int a_rows;                     // rows of a box of A (whose rows lie across the summed axis)
-    int chunks;                     // blocks of 64 that a stage holds; kb counts stages
-    int group_m;                    // tiles of rows that are worked on side by side
+    uint32_t stage_tx;              // bytes of a stage of all CTAs of a tile
+
+    // PR_OUT
+    int rows_a;                     // A's rows run along the summed axis
+    int map_a, map_b, map_out;      // the first of its descriptions
+    float *partial;                 // where there are splits: their sums
+    float *sums;                    // where the result is made in several launches: fp32 sums so far, NULL: made in this one
+    int go_on, end;                 // add to them; this is the last
+    unsigned counters;              // the first of its counters
+    void *out[2];                   // of each job
+    long long out_ld;
+};
+struct __align__(64) ProductMaps { CUtensorMap a[4], b[3], out[3]; };
+
+struct ProductArgs {
+    ProductPart part[2];
+    int tiles;
+    int chunks;                     // blocks of 64 that a stage holds
     int stages;                     // of the ring
     uint32_t stage, stage_b;        // bytes of a CTA's stage, where B begins in it
-    uint32_t stage_tx;              // bytes of a stage of all CTAs of a tile
     int tma_out;                    // wide tiles: results leave by TMA
     unsigned tries;                 // of a barrier, before a wait gives up
     int starve;                     // fetch nothing (xsm_debug_product_waits)
@@ -56,12 +73,11 @@ struct ProductArgs {
     int activation;
     const void *g_y;
     long long g_y_ld;
-    void *out[2];                   // PR_OUT: of each job; PR_GATED_GRAD: gate's, up's
+    void *out[2];                   // PR_GATED_GRAD: gate's, up's
     long long out_ld;
     const float *amax;              // [kAmaxBlocks], NULL: scale 1
+    float *amax_out;                // PR_DLOGITS: look for it in g and g_lse, and leave it here for the launches behind
     int amax_to;                    // the largest is scaled to [2^amax_to, 2^(amax_to + 1))
-    float *partial;                 // PR_OUT: fp32 [job][split][m][n] instead of out, where it is not NULL
-    int add;                        // to what partial holds
 };
 
 // A row's maximum (times log2(e) / T) and sum of exponentials, joined part by part.
@@ -94,7 +110,7 @@ struct ProductCut {
     int tn(bool gated) const { return gated ? bn / 2 : bn; }
     long long tiles(long long m, long long n, bool gated) const { return ((m + tm() - 1) / tm()) * ((n + tn(gated) - 1) / tn(gated)); }
 };
-// out [m][n]; epi: what is done with it
+// out [m][n]; epi: what is done with it (not PR_OUT: plan_sums)
 ProductCut product_cut(ProductEpi epi, long long m, long long n);
 
 // An operand in memory: `rows` rows of `row` elements, ld elements apart.
@@ -102,17 +118,36 @@ struct Operand { const void *p; long long rows, row, ld; };
 
 // CTAs that a product of so many tiles runs on
 int product_ctas(long long tiles, bool wide);
-// Fills in the cut (tiles, boxes, maps) of A and launches.  a, b: operands of the pairs or jobs.  PR_OUT*: b's rows run along the summed axis.
-cudaError_t launch_product(ProductEpi epi, int dtype, ProductCut cut, ProductArgs A, const Operand (&a)[2], const Operand (&b)[2], int pairs, cudaStream_t st);
+// Fills in the cut (tiles, boxes, descriptions) of A and launches: a . b^T [m][n], or with both b (PR_GATED*).
+cudaError_t launch_product(ProductEpi epi, int dtype, ProductCut cut, ProductArgs A, int m, int n, const Operand &a, const Operand (&b)[2], cudaStream_t st);
+
+// Two products in one launch, of each the results that are wanted:  x = sum over pairs of g[i] . w[i]  [rows][d],  y[i] = g[i]^T . h  [cols][d].
+struct SumsPlan {
+    ProductCut cut;
+    int splits_x, splits_y;
+    size_t partial_x, partial_y, bytes;      // fp32 sums of splits, in bytes from the beginning of their place
+};
+struct Sums {
+    int pairs;
+    Operand g[2], w[2], h;
+    void *x, *y[2];
+    long long x_ld, y_ld;
+    float *x_sums;                  // fp32 sums of x over several launches, NULL: one launch
+    int go_on, end;
+    char *partial;
+    unsigned *counters;             // kSumCounters words
+    const float *amax;
+    int amax_to;
+    int *status;
+};
+SumsPlan plan_sums(long long rows, long long cols, long long d, int pairs, bool x, bool y);
+size_t sums_bytes(const ProductCut &cut, long long rows, long long d);      // of x_sums
+cudaError_t launch_sums(int dtype, const SumsPlan &p, const Sums &s, cudaStream_t st);
 
 // |x| at most over rows of 16-bit elements, or of fp32 numbers 2|g| + |g_lse| times `by`; [kAmaxBlocks]
 cudaError_t launch_amax_rows(const void *x, int dtype, long long rows, long long cols, long long ld, float *amax, cudaStream_t st);
 cudaError_t launch_amax_pairs(const float *g, long long g_ld, const float *g_lse, long long g_lse_ld, int rows, float by, float *amax, cudaStream_t st);
-// out[job] = sum over splits of partial [job][split][m][n], times the scale back
-cudaError_t launch_join(const ProductArgs &A, int dtype, cudaStream_t st);
 
-// how many parts the summed axis is cut into so that `tiles` tiles keep the chip busy
-int product_splits(long long tiles, int kb, bool wide);
 int product_sms();
 void product_waits(unsigned *tries, int *starve);
 

@@ -27,9 +27,9 @@ _ATTEND = struct.Struct("7P8q7if")
 _LOGPROB = struct.Struct("7P2q5if")
 _GRAD = struct.Struct("10P6q5if")
 _LINEAR = struct.Struct("8P4q5if")
-_LINEAR_GRAD = struct.Struct("10P8q5if")
+_LINEAR_GRAD = struct.Struct("11P8q5if")
 _GATED = struct.Struct("5P4q5i")
-_GATED_GRAD = struct.Struct("9P7q5i")
+_GATED_GRAD = struct.Struct("10P7q5i")
 _NORM = struct.Struct("8P12q10if")
 _NORM_GRAD = struct.Struct("13P19q10if")
 _HEAD_NORM = struct.Struct("2Pif")
@@ -521,19 +521,19 @@ def _status(device: int, stream: int) -> int:
     return t.data_ptr()
 
 
-_counters = {}           # by (device, stream): a word that calls count their CTAs in
+_counters = {}           # by (device, stream): words that calls count their CTAs in
 
 
 def _counter(device: int, stream: int) -> int:
-    """Address of a word that is zero between the calls of a stream, or of a graph's on one of its streams."""
+    """Address of words that are zero between the calls of a stream, or of a graph's on one of its streams."""
     if stream and _capturing():
         r = _recorded_on(device, stream)
         if r.counter is None:
-            r.counter = _zeros_while_recording(16, device)
+            r.counter = _zeros_while_recording(4 * binding.XSM_COUNTERS, device)
         return r.counter.data_ptr()
     t = _counters.get((device, stream))
     if t is None:
-        t = _counters.setdefault((device, stream), torch.zeros(16, dtype=torch.uint8, device=f"cuda:{device}"))
+        t = _counters.setdefault((device, stream), torch.zeros(4 * binding.XSM_COUNTERS, dtype=torch.uint8, device=f"cuda:{device}"))
     return t.data_ptr()
 
 
@@ -575,6 +575,9 @@ def check(device=None):
         status = int(t[:4].view(torch.int32)[0])
         if status:
             t[:4].zero_()
+            for c in [c for (d, _), c in list(_counters.items()) if d == i] + [r.counter for (d, _, _), r in list(_recorded.items()) if d == i and r.counter is not None]:
+                c.zero_()          # (what gave up has not counted to the end)
+            torch.cuda.synchronize(i)
             raise binding.XsmError(status, "a bounded device-side wait ran out of patience")
 
 
@@ -662,7 +665,7 @@ def linear_logprobs_grad(hidden, weight, tokens, result, grad_logprob=None, grad
     ws = _scratch(n, device, stream, where)
     try:
         args = _LINEAR_GRAD.pack(hidden.data_ptr(), weight.data_ptr(), tokens.data_ptr(), lse.data_ptr(), gl, gs, 0 if d_hidden is None else d_hidden.data_ptr(),
-                                 0 if d_weight is None else d_weight.data_ptr(), ws.data_ptr(), _status(device, stream), ld, w_ld, tokens.stride(0), gl_ld, gs_ld,
+                                 0 if d_weight is None else d_weight.data_ptr(), ws.data_ptr(), _status(device, stream), _counter(device, stream), ld, w_ld, tokens.stride(0), gl_ld, gs_ld,
                                  d, d, n, rows, vocab, d, _DTYPES[dtype], _TOKENS[tokens.dtype], temperature)
     except _BEYOND as e:
         raise ValueError(f"an argument of linear_logprobs_grad is beyond its type: {e}") from None
@@ -750,7 +753,7 @@ def gated_feed_forward_grad(x, w_gate, w_up, grad, activation: str = "silu", nee
     ws = _scratch(n, device, stream, where)
     try:
         args = _GATED_GRAD.pack(flat.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), g.data_ptr(), 0 if d_x is None else d_x.data_ptr(), 0 if d_gate is None else d_gate.data_ptr(),
-                                0 if d_up is None else d_up.data_ptr(), ws.data_ptr(), _status(device, stream), ld, g_ld, u_ld, g.stride(0), d, d, n, rows, ff, d, _DTYPES[dtype],
+                                0 if d_up is None else d_up.data_ptr(), ws.data_ptr(), _status(device, stream), _counter(device, stream), ld, g_ld, u_ld, g.stride(0), d, d, n, rows, ff, d, _DTYPES[dtype],
                                 _ACTIVATIONS[activation])
     except _BEYOND as e:
         raise ValueError(f"an argument of gated_feed_forward_grad is beyond its type: {e}") from None

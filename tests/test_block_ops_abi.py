@@ -30,8 +30,8 @@ def test_structures_have_the_sizes_and_offsets_of_the_header(tmp_path):
 
     def up(n):
         return (n + 7) // 8 * 8
-    for name, s, pointers, strides in (("xsm_linear_logprobs_args", ops._LINEAR, 8, 4), ("xsm_linear_logprobs_grad_args", ops._LINEAR_GRAD, 10, 8), ("xsm_gated_ff_args", ops._GATED, 5, 4),
-                                       ("xsm_gated_ff_grad_args", ops._GATED_GRAD, 9, 7)):
+    for name, s, pointers, strides in (("xsm_linear_logprobs_args", ops._LINEAR, 8, 4), ("xsm_linear_logprobs_grad_args", ops._LINEAR_GRAD, 11, 8), ("xsm_gated_ff_args", ops._GATED, 5, 4),
+                                       ("xsm_gated_ff_grad_args", ops._GATED_GRAD, 10, 7)):
         assert got[name] == [up(s.size), 8 * pointers, 8 * (pointers + strides - 1), 8 * (pointers + strides), s.size - 4]
     assert got["xsm_norm_rotate_args"] == [up(ops._NORM.size), 64, 64 + 9 * 8, 64 + 12 * 8, ops._NORM.size - 4]
     assert got["xsm_norm_rotate_grad_args"] == [up(ops._NORM_GRAD.size), 104, 104 + 18 * 8, 104 + 19 * 8, ops._NORM_GRAD.size - 4]
@@ -67,9 +67,9 @@ def test_workspaces_that_are_too_small(lib):
     if lib.xsm_linear_logprobs_workspace(4, 100, 64) == 0:
         pytest.skip("sizes of workspaces go by the device")
     assert lib.xsm_linear_logprobs(linear(ws=0), None) == binding.XSM_ERR_CAPACITY
-    args = ops._LINEAR_GRAD.pack(*10 * [A], 64, 64, 1, 1, 1, 64, 64, 0, 4, 100, 64, 1, 8, 1.0)
+    args = ops._LINEAR_GRAD.pack(*11 * [A], 64, 64, 1, 1, 1, 64, 64, 0, 4, 100, 64, 1, 8, 1.0)
     assert lib.xsm_linear_logprobs_grad(args, None) == binding.XSM_ERR_CAPACITY
-    args = ops._GATED_GRAD.pack(*9 * [A], 64, 64, 64, 100, 64, 64, 0, 4, 100, 64, 1, 0)
+    args = ops._GATED_GRAD.pack(*10 * [A], 64, 64, 64, 100, 64, 64, 0, 4, 100, 64, 1, 0)
     assert lib.xsm_gated_ff_grad(args, None) == binding.XSM_ERR_CAPACITY
 
 
@@ -86,9 +86,9 @@ def test_wrong_arguments_of_gated_ff(lib, wrong, word):
 
 def test_gradients_that_go_together(lib):
     from paper_2507_23777_b200 import ops
-    args = ops._GATED_GRAD.pack(A, A, A, A, A, A, 0, A, A, 64, 64, 64, 100, 64, 64, 1 << 30, 4, 100, 64, 1, 0)
+    args = ops._GATED_GRAD.pack(A, A, A, A, A, A, 0, A, A, A, 64, 64, 64, 100, 64, 64, 1 << 30, 4, 100, 64, 1, 0)
     assert lib.xsm_gated_ff_grad(args, None) == binding.XSM_ERR_INVALID_ARG and b"together" in lib.xsm_last_error(None)
-    args = ops._GATED_GRAD.pack(A, A, A, A, 0, 0, 0, A, A, 64, 64, 64, 100, 64, 64, 1 << 30, 4, 100, 64, 1, 0)
+    args = ops._GATED_GRAD.pack(A, A, A, A, 0, 0, 0, A, A, A, 64, 64, 64, 100, 64, 64, 1 << 30, 4, 100, 64, 1, 0)
     assert lib.xsm_gated_ff_grad(args, None) == 0          # nothing is wanted
 
 
