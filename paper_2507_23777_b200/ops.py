@@ -616,15 +616,33 @@ def _no_gradient(what: str, *tensors):
         _no_tangents(*tensors)
 
 
-def _check_linear(hidden, weight, tokens):
+def _refuse_linear(hidden, weight, tokens):
+    """What is wrong with the arguments, told one by one."""
     device, dtype = _need_products(hidden, "hidden")
-    ld = _rows(hidden, "hidden", device, dtype)
+    _rows(hidden, "hidden", device, dtype)
     rows, d = hidden.shape
-    w_ld = _rows(weight, "weight", device, dtype, d)
-    if d < 8 or d % 8 or weight.shape[0] < 1:
-        raise ValueError("the width of hidden must be a positive multiple of 8, and weight must have rows")
-    if tokens.shape != (rows,) or tokens.get_device() != device or tokens.dtype not in _TOKENS:
-        raise ValueError(f"tokens must be int32 or int64 [{rows}] on cuda:{device}")
+    _rows(weight, "weight", device, dtype, d)
+    _need(d >= 8 and d % 8 == 0 and weight.shape[0] >= 1, "the width of hidden must be a positive multiple of 8, and weight must have rows")
+    _need(tokens.shape == (rows,) and tokens.get_device() == device and tokens.dtype in _TOKENS, f"tokens must be int32 or int64 [{rows}] on cuda:{device}")
+    raise ValueError("the arguments of linear_logprobs do not go together")
+
+
+def _check_linear(hidden, weight, tokens):
+    """(device, type, rows, d, row strides) of arguments that go together, all of it looked at at once."""
+    shape, w_shape, dtype, device = hidden.shape, weight.shape, hidden.dtype, hidden.get_device()
+    ok = len(shape) == 2 == len(w_shape) and (dtype is torch.bfloat16 or dtype is torch.float16)
+    if ok:
+        rows, d = shape
+        (ld, a), (w_ld, b) = hidden.stride(), weight.stride()
+        if rows < 2:
+            ld = d
+        if w_shape[0] < 2:
+            w_ld = d
+        ok = (w_shape[1] == d and d >= 8 and w_shape[0] >= 1 and (d | ld | w_ld) & 7 == 0 and a == b == 1 and ld >= d and w_ld >= d and weight.dtype is dtype and
+              device == weight.get_device() == tokens.get_device() == _current_device() and tokens.shape == (rows,) and tokens.dtype in _TOKENS and
+              (hidden.data_ptr() | weight.data_ptr()) & 15 == 0)
+    if not ok:
+        _refuse_linear(hidden, weight, tokens)
     return device, dtype, rows, d, ld, w_ld
 
 
@@ -705,26 +723,46 @@ def linear_logprobs(hidden, weight, tokens, temperature: float = 1.0) -> LinearL
     return _linear_forward(hidden, weight, tokens, temperature)
 
 
-def _check_gated(x, w_gate, w_up, activation):
+def _refuse_gated(x, w_gate, w_up, activation):
+    """What is wrong with the arguments, told one by one."""
     device, dtype = _need_products(x, "x")
-    if x.dim() < 1 or w_gate.dim() != 2 or w_gate.shape != w_up.shape:
-        raise ValueError("x must be [..., d], w_gate and w_up [ff, d]")
-    d, ff = x.shape[-1], w_gate.shape[0]
-    if d < 8 or d % 8 or ff < 1:
-        raise ValueError("the width of x must be a positive multiple of 8, and w_gate and w_up must have rows")
+    _need(x.dim() >= 1 and w_gate.dim() == 2 and w_gate.shape == w_up.shape, "x must be [..., d], w_gate and w_up [ff, d]")
+    d = x.shape[-1]
+    _need(d >= 8 and d % 8 == 0 and w_gate.shape[0] >= 1, "the width of x must be a positive multiple of 8, and w_gate and w_up must have rows")
     if activation not in _ACTIVATIONS:
         raise ValueError(f"activation must be one of {', '.join(_ACTIVATIONS)}, not {activation!r}")
-    flat = x if x.dim() == 2 else x.reshape(-1, d)
-    return device, dtype, flat, flat.shape[0], ff, d, _rows(flat, "x", device, dtype), _rows(w_gate, "w_gate", device, dtype, d), _rows(w_up, "w_up", device, dtype, d)
+    _rows(x.reshape(-1, d), "x", device, dtype)
+    _rows(w_gate, "w_gate", device, dtype, d)
+    _rows(w_up, "w_up", device, dtype, d)
+    raise ValueError("the arguments of gated_feed_forward do not go together")
+
+
+def _check_gated(x, w_gate, w_up, activation):
+    """(device, type, x as a matrix, rows, ff, d, row strides) of arguments that go together, all of it looked at at once."""
+    dtype, device, w_shape, kind = x.dtype, x.get_device(), w_gate.shape, _ACTIVATIONS.get(activation)
+    ok = kind is not None and len(w_shape) == 2 and w_shape == w_up.shape and (dtype is torch.bfloat16 or dtype is torch.float16) and x.dim() >= 1
+    if ok:
+        flat = x if x.dim() == 2 else x.reshape(-1, x.shape[-1])
+        (rows, d), ff = flat.shape, w_shape[0]
+        (ld, a), (g_ld, b), (u_ld, c) = flat.stride(), w_gate.stride(), w_up.stride()
+        if rows < 2:
+            ld = d
+        if ff < 2:
+            g_ld = u_ld = d
+        ok = (w_shape[1] == d and d >= 8 and ff >= 1 and (d | ld | g_ld | u_ld) & 7 == 0 and a == b == c == 1 and ld >= d and g_ld >= d and u_ld >= d and
+              w_gate.dtype is dtype is w_up.dtype and device == w_gate.get_device() == w_up.get_device() == _current_device() and
+              (flat.data_ptr() | w_gate.data_ptr() | w_up.data_ptr()) & 15 == 0)
+    if not ok:
+        _refuse_gated(x, w_gate, w_up, activation)
+    return device, dtype, flat, rows, ff, d, ld, g_ld, u_ld, kind
 
 
 def _gated_forward(x, w_gate, w_up, activation):
-    device, dtype, flat, rows, ff, d, ld, g_ld, u_ld = _check_gated(x, w_gate, w_up, activation)
+    device, dtype, flat, rows, ff, d, ld, g_ld, u_ld, kind = _check_gated(x, w_gate, w_up, activation)
     stream = _raw_stream(device)
     out = _empty((rows, ff), (ff, 1), dtype=dtype, device=x.device) if flat is x else torch.empty((*x.shape[:-1], ff), dtype=dtype, device=x.device)
     try:
-        args = _GATED.pack(flat.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), out.data_ptr(), _status(device, stream), ld, g_ld, u_ld, ff, rows, ff, d, _DTYPES[dtype],
-                           _ACTIVATIONS[activation])
+        args = _GATED.pack(flat.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), out.data_ptr(), _status(device, stream), ld, g_ld, u_ld, ff, rows, ff, d, _DTYPES[dtype], kind)
     except _BEYOND as e:
         raise ValueError(f"an argument of gated_feed_forward is beyond its type: {e}") from None
     status = binding.load().xsm_gated_ff(args, stream)
@@ -738,29 +776,39 @@ def gated_feed_forward_grad(x, w_gate, w_up, grad, activation: str = "silu", nee
     neighbouring elements in a row.  need: which are wanted (the last two go together); the others are None.  There are no second derivatives: tensors that want a
     gradient are refused unless torch.no_grad() says that it is not needed."""
     _no_gradient("gated_feed_forward_grad", x, w_gate, w_up, grad)
-    device, dtype, flat, rows, ff, d, ld, g_ld, u_ld = _check_gated(x, w_gate, w_up, activation)
-    if grad.shape[:-1] != x.shape[:-1] or grad.dim() < 1 or grad.shape[-1] != ff or grad.dtype is not dtype or grad.get_device() != device:
+    device, dtype, flat, rows, ff, d, ld, g_ld, u_ld, kind = _check_gated(x, w_gate, w_up, activation)
+    g = grad
+    if flat is not x:
+        _need(grad.dim() >= 1 and grad.shape[:-1] == x.shape[:-1] and grad.shape[-1] == ff, f"grad must be {[*x.shape[:-1], ff]}")
+        g = grad.reshape(-1, ff)
+    if g.shape != (rows, ff) or g.dtype is not dtype or g.get_device() != device:
         raise ValueError(f"grad must be {[*x.shape[:-1], ff]} of {dtype} on cuda:{device}")
-    g = grad if grad.dim() == 2 else grad.reshape(-1, ff)
-    if ff > 1 and rows and g.stride(1) != 1:
+    gy_ld, step = g.stride()
+    if step != 1 and ff > 1 and rows:
         raise ValueError("the elements of a row of grad must be neighbours")
-    lib, where, stream = binding.load(), x.device, _raw_stream(device)
-    d_x = _empty((rows, d), (d, 1), dtype=dtype, device=where).view(x.shape) if need[0] else None
-    d_gate = d_up = None
-    if need[1] or need[2]:
-        d_gate, d_up = (_empty((ff, d), (d, 1), dtype=dtype, device=where) for _ in range(2))
+    where, stream = x.device, _raw_stream(device)
+    d_x = d_gate = d_up = None
+    to_x = to_gate = to_up = 0
+    need_x, need_gate, need_up = need
+    if need_x:
+        d_x = _empty((rows, d), (d, 1), dtype=dtype, device=where)
+        to_x = d_x.data_ptr()
+        if flat is not x:
+            d_x = d_x.view(x.shape)
+    if need_gate or need_up:
+        d_gate, d_up = _empty((ff, d), (d, 1), dtype=dtype, device=where), _empty((ff, d), (d, 1), dtype=dtype, device=where)
+        to_gate, to_up = d_gate.data_ptr(), d_up.data_ptr()
     n = _size_of("xsm_gated_ff_grad_workspace", rows, ff, d)
     ws = _scratch(n, device, stream, where)
     try:
-        args = _GATED_GRAD.pack(flat.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), g.data_ptr(), 0 if d_x is None else d_x.data_ptr(), 0 if d_gate is None else d_gate.data_ptr(),
-                                0 if d_up is None else d_up.data_ptr(), ws.data_ptr(), _status(device, stream), _counter(device, stream), ld, g_ld, u_ld, g.stride(0), d, d, n, rows, ff, d, _DTYPES[dtype],
-                                _ACTIVATIONS[activation])
+        args = _GATED_GRAD.pack(flat.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), g.data_ptr(), to_x, to_gate, to_up, ws.data_ptr(), _status(device, stream), _counter(device, stream),
+                                ld, g_ld, u_ld, gy_ld, d, d, n, rows, ff, d, _DTYPES[dtype], kind)
     except _BEYOND as e:
         raise ValueError(f"an argument of gated_feed_forward_grad is beyond its type: {e}") from None
-    status = lib.xsm_gated_ff_grad(args, stream)
+    status = binding.load().xsm_gated_ff_grad(args, stream)
     if status:
         _check(status)
-    return d_x, d_gate if need[1] else None, d_up if need[2] else None
+    return d_x, d_gate if need_gate else None, d_up if need_up else None
 
 
 class _GatedFeedForward(torch.autograd.Function):
