@@ -448,6 +448,7 @@ typedef struct {
     const void *g_q, *g_k;                /* DEVICE dtype, like q and k */
     void *d_q, *d_k, *d_q_gain, *d_k_gain;
     void *workspace;                      /* DEVICE, xsm_norm_rotate_grad_workspace bytes, of any content; calls that share one follow each other on one stream */
+    uint32_t *counters;                   /* as for the products above */
     int64_t q_stride[3], k_stride[3], g_q_stride[3], g_k_stride[3], d_q_stride[3], d_k_stride[3], workspace_bytes;
     int32_t batch, m, n_heads, n_kv_heads, d_head, dtype, gain_dtype, rope_positions, rope_dims, interleaved;
     float eps;

@@ -5,7 +5,8 @@
 // A head is 2 to 16 neighbouring lanes, which hold two runs of eight elements each, the two halves of eight pairs, so that norm and rotation need nothing but
 // the lanes' own registers and a sum over them.  A group of lanes takes some heads of a token one behind the other, what the token's angles and the gains have to do with an
 // element in registers; the heads to come are on their way to slots of shared memory that each lane has for itself, so that neither registers nor barriers limit
-// how many.  d_gain is added up in registers over all rows of a group, then over a block, then over blocks in their order: no atomics.
+// how many.  d_gain is added up in registers over all rows of a group, then over a block, then over blocks in a fixed order: no result hangs on who
+// comes first.
 #include "xsm_ops.h"
 #include "xsm_chain.cuh"
 
@@ -25,6 +26,7 @@ struct NormTensor {
     void *out;                      // result, or gradient by x
     const void *gain;
     float *part;                    // NM_GRAD: [block][d]
+    void *d_gain;
     long long xs[3], gs[3], os[3];  // strides of sequence, token, head
     int heads, blocks;              // heads, blocks that work on the tensor
     Divisor by_chunks;              // units of a token
@@ -37,6 +39,7 @@ struct NormArgs {
     Divisor by_m;
     int d, rope_n, rot, hp, gain_dtype;      // hp: heads of a unit
     float eps, inv_d;
+    unsigned *counter;              // NM_GRAD: of blocks that have ended
 };
 
 template <typename T, int N> struct __align__(sizeof(T) * N > 16 ? 16 : sizeof(T) * N) Run { T e[N]; };
@@ -123,10 +126,54 @@ template <bool kPool, typename T, int H> __device__ __forceinline__ void store_r
     }
 }
 
+// Adds up the d_gain of a few blocks where the last of them ends: 8 to 32 threads a quad of elements, each every so-many-th block, then these; nothing hangs on which is the last.
+__device__ __forceinline__ void finish_gains(const NormArgs &A) {
+    __shared__ int last;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        __threadfence();
+        last = atomicInc(A.counter, gridDim.x - 1) == gridDim.x - 1;
+        __threadfence();
+    }
+    __syncthreads();
+    if (!last) return;
+    const int quads = A.d / 4, parts = quads <= 8 ? 32 : quads <= 16 ? 16 : 8, part = (int)threadIdx.x % parts;
+    for (int t = 0; t < 2; ++t) {
+        const NormTensor &T = A.t[t];
+        if (!T.heads) continue;
+        for (int q0 = 0; q0 < quads; q0 += kNormThreads / parts) {
+            const int q = q0 + (int)threadIdx.x / parts;
+            float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (q < quads) {
+                const float *from = T.part + 4 * q;
+#pragma unroll 4
+                for (int b = part; b < T.blocks; b += parts) {
+                    const float4 x = __ldcg(reinterpret_cast<const float4 *>(from + (long long)b * A.d));
+                    v.x += x.x; v.y += x.y; v.z += x.z; v.w += x.w;
+                }
+            }
+            for (int o = parts / 2; o > 0; o >>= 1) {
+                v.x += __shfl_xor_sync(0xffffffffu, v.x, o);
+                v.y += __shfl_xor_sync(0xffffffffu, v.y, o);
+                v.z += __shfl_xor_sync(0xffffffffu, v.z, o);
+                v.w += __shfl_xor_sync(0xffffffffu, v.w, o);
+            }
+            if (q < quads && part < 4) {
+                const float f = part == 0 ? v.x : part == 1 ? v.y : part == 2 ? v.z : v.w;
+                const int e = 4 * q + part;
+                if (A.gain_dtype == XSM_F32) reinterpret_cast<float *>(T.d_gain)[e] = f;
+                else if (A.gain_dtype == XSM_BF16) reinterpret_cast<bf16 *>(T.d_gain)[e] = rounded<bf16>(f);
+                else reinterpret_cast<__half *>(T.d_gain)[e] = rounded<__half>(f);
+            }
+        }
+    }
+}
+
 // Rows and angles in 16-byte pieces.  L lanes a head; the lanes' first runs lie side by side, and so do the second ones, half of the turned (of the other) part of the head
 // further: with half-split pairs a lane then has both elements of each, with neighbouring ones (kNear) anyway.  (Two runs of a lane side by side made accesses of half
 // sectors: 20 us instead of ... for 3003 tokens of 32 heads of 64 in fp32.)
-template <typename TI, typename TC, int L, bool kNear, int MODE>
+// kFinish: the block that ends last adds up the blocks' d_gain (a kernel of its own: the code for it costs the loop 3 us of 20).
+template <typename TI, typename TC, int L, bool kNear, int MODE, bool kFinish>
 __global__ void __launch_bounds__(kNormThreads, kNormBlocks) norm_kernel(const __grid_constant__ NormArgs A, const __grid_constant__ Pages P) {
     constexpr int G = kNormThreads / L, N = 16 / (int)sizeof(TI), H = N / 2;        // N elements a run
     using Slots = NormSlots<MODE>;
@@ -380,11 +427,12 @@ __global__ void __launch_bounds__(kNormThreads, kNormBlocks) norm_kernel(const _
             for (int g = 0; g < G; ++g) v += s[g * W + e];
             T.part[(long long)blk * A.d + e] = v;
         }
+        if constexpr (kFinish) finish_gains(A);
     }
 }
 
 // The same for rows or angles of any alignment: a warp a head, up to four pairs of elements a lane.
-template <typename TI, typename TC, bool kNear, int MODE>
+template <typename TI, typename TC, bool kNear, int MODE, bool kFinish>
 __global__ void __launch_bounds__(kNormThreads) norm_any_kernel(const __grid_constant__ NormArgs A, const __grid_constant__ Pages P) {
     constexpr int I = 4, G = kNormThreads / 32;
     __shared__ float s[MODE == NM_GRAD ? G : 1][257];
@@ -488,6 +536,7 @@ __global__ void __launch_bounds__(kNormThreads) norm_any_kernel(const __grid_con
             for (int g = 0; g < G; ++g) v += s[g][e];
             T.part[(long long)blk * A.d + e] = v;
         }
+        if constexpr (kFinish) finish_gains(A);
     }
 }
 
@@ -553,16 +602,23 @@ static int cut_norm(NormArgs &A, int lanes) {
 
 template <typename TI, typename TC, int MODE>
 static cudaError_t launch_norm(const NormArgs &A, const Pages &P, int blocks, bool wide, bool near, cudaStream_t st) {
+    auto start = [&](auto fn, int smem) {
+        const cudaError_t e = smem > 48 * 1024 ? open_for((const void *)fn, smem) : cudaSuccess;
+        return e != cudaSuccess ? e : launch_early(fn, dim3(blocks), dim3(kNormThreads), smem, st, A, P);
+    };
+    auto finish = [&](auto f) {        // f(whether the last block adds up)
+        if constexpr (MODE == NM_GRAD) return A.counter ? f(std::true_type()) : f(std::false_type());
+        else return f(std::false_type());
+    };
     if (!wide)
-        return near ? launch_early(norm_any_kernel<TI, TC, true, MODE>, dim3(blocks), dim3(kNormThreads), 0, st, A, P)
-                    : launch_early(norm_any_kernel<TI, TC, false, MODE>, dim3(blocks), dim3(kNormThreads), 0, st, A, P);
+        return finish([&](auto fin) {
+            return near ? start(norm_any_kernel<TI, TC, true, MODE, decltype(fin)::value>, 0) : start(norm_any_kernel<TI, TC, false, MODE, decltype(fin)::value>, 0);
+        });
     auto go = [&](auto l) {
         constexpr int L = decltype(l)::value, slots = NormSlots<MODE>::bytes, sums = MODE == NM_GRAD ? kNormThreads / L * (32 / (int)sizeof(TI) * L + 1) * 4 : 0, smem = slots > sums ? slots : sums;
-        const void *fn = near ? (const void *)norm_kernel<TI, TC, L, true, MODE> : (const void *)norm_kernel<TI, TC, L, false, MODE>;
-        const cudaError_t e = smem > 48 * 1024 ? open_for(fn, smem) : cudaSuccess;
-        if (e != cudaSuccess) return e;
-        return near ? launch_early(norm_kernel<TI, TC, L, true, MODE>, dim3(blocks), dim3(kNormThreads), smem, st, A, P)
-                    : launch_early(norm_kernel<TI, TC, L, false, MODE>, dim3(blocks), dim3(kNormThreads), smem, st, A, P);
+        return finish([&](auto fin) {
+            return near ? start(norm_kernel<TI, TC, L, true, MODE, decltype(fin)::value>, smem) : start(norm_kernel<TI, TC, L, false, MODE, decltype(fin)::value>, smem);
+        });
     };
     using std::integral_constant;
     const int lanes = lanes_of(A.d, (int)sizeof(TI), true);
@@ -665,8 +721,8 @@ xsm_status xsm_norm_rotate_grad(const xsm_norm_rotate_grad_args *a, void *cuda_s
         if (e == cudaSuccess && a->n_kv_heads) e = cudaMemsetAsync(a->d_k_gain, 0, (size_t)a->d_head * gs, st);
         return launched(e);
     }
-    if ((a->n_heads && (!a->q || !a->g_q || !a->d_q)) || (a->n_kv_heads && (!a->k || !a->g_k || !a->d_k)) || !a->workspace) return op_failed(XSM_ERR_INVALID_ARG, "null argument");
-    if ((uintptr_t)a->workspace % 16) return op_failed(XSM_ERR_INVALID_ARG, "workspace must be 16-byte aligned");
+    if ((a->n_heads && (!a->q || !a->g_q || !a->d_q)) || (a->n_kv_heads && (!a->k || !a->g_k || !a->d_k)) || !a->workspace || !a->counters) return op_failed(XSM_ERR_INVALID_ARG, "null argument");
+    if ((uintptr_t)a->workspace % 16 || (uintptr_t)a->counters % 4) return op_failed(XSM_ERR_INVALID_ARG, "workspace must be 16-byte aligned, counters to their elements");
     if (a->workspace_bytes < (int64_t)gain_parts(a->d_head)) return op_failed(XSM_ERR_CAPACITY, "the workspace is too small");
     NormArgs A = norm_args(s, a->positions, a->rope);
     const void *x[2] = {a->q, a->k}, *g[2] = {a->g_q, a->g_k}, *gain[2] = {a->q_gain, a->k_gain};
@@ -685,10 +741,13 @@ xsm_status xsm_norm_rotate_grad(const xsm_norm_rotate_grad_args *a, void *cuda_s
     const int blocks = cut_norm(A, lanes_of(A.d, es, wide));
     A.t[0].part = (float *)a->workspace;
     A.t[1].part = A.t[0].part + (size_t)A.t[0].blocks * A.d;
+    for (int i = 0; i < 2; ++i) A.t[i].d_gain = d_gain[i];
+    // (few blocks: the last one adds up; of 296 that is 6 us longer than a kernel of its own)
+    A.counter = blocks <= 64 ? a->counters : nullptr;
     const Pages P = {};
     cudaError_t e = cudaSuccess;
     with_dtype(a->dtype, [&](auto in) { e = launch_norm<decltype(in), decltype(in), NM_GRAD>(A, P, blocks, wide, a->interleaved != 0, st); });
-    if (e == cudaSuccess) {
+    if (e == cudaSuccess && !A.counter) {
         GainArgs R;
         for (int i = 0; i < 2; ++i) { R.part[i] = A.t[i].part; R.out[i] = A.t[i].heads ? d_gain[i] : nullptr; R.blocks[i] = A.t[i].blocks; }
         R.d = A.d; R.dtype = A.gain_dtype;

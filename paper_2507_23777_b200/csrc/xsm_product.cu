@@ -536,12 +536,13 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
                     constexpr int kPieces = BN / 64, kTile = CG * kEpiWarps * kPieces * 1024;        // of 32 columns a warp; fp32 sums of a tile
                     // Sums in memory lie as the threads hold them: piece by piece, four columns of the 32 rows side by side.
                     auto place = [&](float *p, long long tile) { return p + tile * kTile + ((rank * kEpiWarps + warp - 2) * kPieces) * 1024 + lane * 4; };
-                    bool mine = true;
-                    if (P.splits > 1) {
+                    const int pieces = min(kPieces, (P.n - col0 + 31) / 32);        // (that have columns)
+                    bool mine = row0 < P.m;
+                    if (P.splits > 1 && mine) {
                         // Every split leaves its sums; whoever comes last of a tile's and a warp's adds them up, in the order of the splits.
                         float *p = place(P.partial, (long long)w.at * P.splits + w.split);
 #pragma unroll 1
-                        for (int c = 0; c < kPieces; ++c) {
+                        for (int c = 0; c < pieces; ++c) {
                             uint32_t v[32];
                             tmem_ld(v, sums + (uint32_t)(half * (BN / 2) + c * 32));
                             tmem_wait_ld();
@@ -558,27 +559,35 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
                     }
                     if (mine) {
 #pragma unroll 1
-                        for (int c = 0; c < kPieces; ++c) {
+                        for (int c = 0; c < pieces; ++c) {
                             const int col = col0 + c * 32;
-                            uint32_t v[32];
                             float x[32];
-                            tmem_ld(v, sums + (uint32_t)(half * (BN / 2) + c * 32));
-                            tmem_wait_ld();
                             if (P.splits > 1) {
+                                const float *p = place(P.partial, (long long)w.at * P.splits) + c * 1024;
+#pragma unroll
+                                for (int i = 0; i < 32; ++i) x[i] = 0.f;
+                                // (two splits' on their way at a time: their latency is most of this)
 #pragma unroll 1
-                                for (int s = 0; s < P.splits; ++s) {
-                                    const float *p = place(P.partial, (long long)w.at * P.splits + s) + c * 1024;
+                                for (int s = 0; s < P.splits; s += 2, p += 2 * kTile) {
+                                    const bool two = s + 1 < P.splits;
+                                    float4 q[8], r[8];
 #pragma unroll
                                     for (int i = 0; i < 8; ++i) {
-                                        const float4 q = s == w.split ? make_float4(__uint_as_float(v[4 * i]), __uint_as_float(v[4 * i + 1]), __uint_as_float(v[4 * i + 2]), __uint_as_float(v[4 * i + 3]))
-                                                                      : __ldcg(reinterpret_cast<const float4 *>(p + i * 128));
-                                        x[4 * i] = s ? x[4 * i] + q.x : q.x;
-                                        x[4 * i + 1] = s ? x[4 * i + 1] + q.y : q.y;
-                                        x[4 * i + 2] = s ? x[4 * i + 2] + q.z : q.z;
-                                        x[4 * i + 3] = s ? x[4 * i + 3] + q.w : q.w;
+                                        q[i] = __ldcg(reinterpret_cast<const float4 *>(p + i * 128));
+                                        r[i] = two ? __ldcg(reinterpret_cast<const float4 *>(p + kTile + i * 128)) : make_float4(0.f, 0.f, 0.f, 0.f);
+                                    }
+#pragma unroll
+                                    for (int i = 0; i < 8; ++i) {
+                                        x[4 * i] = x[4 * i] + q[i].x + r[i].x;
+                                        x[4 * i + 1] = x[4 * i + 1] + q[i].y + r[i].y;
+                                        x[4 * i + 2] = x[4 * i + 2] + q[i].z + r[i].z;
+                                        x[4 * i + 3] = x[4 * i + 3] + q[i].w + r[i].w;
                                     }
                                 }
                             } else {
+                                uint32_t v[32];
+                                tmem_ld(v, sums + (uint32_t)(half * (BN / 2) + c * 32));
+                                tmem_wait_ld();
 #pragma unroll
                                 for (int i = 0; i < 32; ++i) x[i] = __uint_as_float(v[i]);
                             }
@@ -600,7 +609,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
                             if constexpr (CG == 2) {
                                 if ((c & 1) == 0) rows_free(lane);
                                 put_row<T>(buf, lane, (c & 1) * 4, x);
-                                if (c & 1) rows_store(&M.out[P.map_out + w.job], buf, col - 32, row0, 0, row0 < P.m && col - 32 < P.n, lane);
+                                if ((c & 1) || c + 1 == pieces) rows_store(&M.out[P.map_out + w.job], buf, col - (c & 1) * 32, row0, 0, true, lane);
                             } else if (live) {
                                 store_row(reinterpret_cast<T *>(P.out[w.job]) + (long long)row * P.out_ld, col, P.n, true, x);
                             }
@@ -940,8 +949,8 @@ static size_t tile_bytes(const ProductCut &cut) { return (size_t)cut.tm() * cut.
 size_t sums_bytes(const ProductCut &cut, long long rows, long long d) { return (size_t)cut.tiles(rows, d, false) * tile_bytes(cut); }
 
 // Both products' tiles are dealt out in one row, x's first.  Tiles are as wide as the larger product asks for.  Where there are few of them the summed axes are cut: of the splits
-// that leave the CTAs with most to do least, in blocks of 64: a tile costs eight blocks on top (its last products, what is done with its sums), one that is cut sixteen, and two
-// for every split that is added up.
+// that leave the CTAs with most to do least, in blocks of 64: a tile costs eight blocks on top (its last products, what is done with its sums), one that is cut sixteen, and for every
+// split that is added up three (one piece of 32 columns: one).
 SumsPlan plan_sums(long long rows, long long cols, long long d, int pairs, bool x, bool y) {
     SumsPlan p = {};
     p.cut = (x && rows > 128 && d > 64) || (y && cols > 128 && d > 64) ? ProductCut{true, 256} : ProductCut{false, 64};
@@ -950,7 +959,8 @@ SumsPlan plan_sums(long long rows, long long cols, long long d, int pairs, bool 
     p.splits_x = p.splits_y = 1;
     if (tx + ty < 4 * slots) {
         static const int tries[] = {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 40, 48, 64, 96, 128};
-        auto cost = [&](long long k, int s) { return (double)((k + s - 1) / s) + (s > 1 ? 16 + 2 * s : 8); };
+        const double each = !p.cut.wide || d <= 32 ? 1 : d <= 64 ? 2 : 3;
+        auto cost = [&](long long k, int s) { return (double)((k + s - 1) / s) + (s > 1 ? 16 + each * s : 8); };
         double least = 1e300;
         for (int sx : tries) {
             if (sx > 1 && (!x || sx * 4 > kx)) break;

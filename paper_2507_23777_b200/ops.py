@@ -31,7 +31,7 @@ _LINEAR_GRAD = struct.Struct("11P8q5if")
 _GATED = struct.Struct("5P4q5i")
 _GATED_GRAD = struct.Struct("10P7q5i")
 _NORM = struct.Struct("8P12q10if")
-_NORM_GRAD = struct.Struct("13P19q10if")
+_NORM_GRAD = struct.Struct("14P19q10if")
 _HEAD_NORM = struct.Struct("2Pif")
 
 TokenLogprobs = namedtuple("TokenLogprobs", "logprob entropy lse top_ids top_logprobs")
@@ -949,7 +949,7 @@ def norm_rotate_grad(q, k, q_gain, k_gain, grad_q, grad_k, rope=None, positions=
     size = _size_of("xsm_norm_rotate_grad_workspace", sizes[4])
     ws = _scratch(size, device, stream, d_q.device if q is not None else d_k.device)
     try:
-        args = _NORM_GRAD.pack(to_q, to_k, to_qg, to_kg, to_at, to_rope, to_g, to_h, to_dq, to_dk, to_dqg, to_dkg, ws.data_ptr(), qs[0], qs[1], qs[2], ks[0], ks[1], ks[2],
+        args = _NORM_GRAD.pack(to_q, to_k, to_qg, to_kg, to_at, to_rope, to_g, to_h, to_dq, to_dk, to_dqg, to_dkg, ws.data_ptr(), _counter(device, stream), qs[0], qs[1], qs[2], ks[0], ks[1], ks[2],
                                gs[0], gs[1], gs[2], hs[0], hs[1], hs[2], os[0], os[1], os[2], us[0], us[1], us[2], size, *sizes, interleaved, eps)
     except _BEYOND as e:
         raise ValueError(f"an argument of norm_rotate_grad is beyond its type: {e}") from None

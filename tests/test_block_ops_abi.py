@@ -34,7 +34,7 @@ def test_structures_have_the_sizes_and_offsets_of_the_header(tmp_path):
                                        ("xsm_gated_ff_grad_args", ops._GATED_GRAD, 10, 7)):
         assert got[name] == [up(s.size), 8 * pointers, 8 * (pointers + strides - 1), 8 * (pointers + strides), s.size - 4]
     assert got["xsm_norm_rotate_args"] == [up(ops._NORM.size), 64, 64 + 9 * 8, 64 + 12 * 8, ops._NORM.size - 4]
-    assert got["xsm_norm_rotate_grad_args"] == [up(ops._NORM_GRAD.size), 104, 104 + 18 * 8, 104 + 19 * 8, ops._NORM_GRAD.size - 4]
+    assert got["xsm_norm_rotate_grad_args"] == [up(ops._NORM_GRAD.size), 112, 112 + 18 * 8, 112 + 19 * 8, ops._NORM_GRAD.size - 4]
     assert got["xsm_head_norm"] == [ops._HEAD_NORM.size, 16, 20]
 
 
@@ -102,7 +102,7 @@ def test_wrong_arguments_of_norm_rotate(lib, wrong, word):
     args = ops._NORM.pack(c["q"], A, A, A, A, A, 0, c["rope"], *4 * (768, 256, 64), c["batch"], c["m"], c["heads"], 2, c["d"], c["dtype"], c["gain_dtype"], c["positions"], c["dims"], 0, c["eps"])
     assert lib.xsm_norm_rotate(args, None) == binding.XSM_ERR_INVALID_ARG
     assert word in lib.xsm_last_error(None)
-    args = ops._NORM_GRAD.pack(c["q"], A, A, A, 0, c["rope"], *7 * [A], *6 * (768, 256, 64), 1 << 30, c["batch"], c["m"], c["heads"], 2, c["d"], c["dtype"], c["gain_dtype"], c["positions"], c["dims"], 0, c["eps"])
+    args = ops._NORM_GRAD.pack(c["q"], A, A, A, 0, c["rope"], *8 * [A], *6 * (768, 256, 64), 1 << 30, c["batch"], c["m"], c["heads"], 2, c["d"], c["dtype"], c["gain_dtype"], c["positions"], c["dims"], 0, c["eps"])
     assert lib.xsm_norm_rotate_grad(args, None) == binding.XSM_ERR_INVALID_ARG
     assert word in lib.xsm_last_error(None)
 
