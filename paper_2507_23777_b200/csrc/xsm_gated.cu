@@ -17,7 +17,7 @@ struct GatedGradPlan {
 static GatedGradPlan plan_gated_grad(int rows, int ff, int d, bool x, bool w) {
     GatedGradPlan p;
     p.cut = product_cut(PR_GATED_GRAD, rows, ff);
-    p.sums = plan_sums(rows, ff, d, 2, x, w);
+    p.sums = plan_sums(rows, ff, d, 2, x, w, true);
     p.ld = (ff + 7) / 8 * 8;
     p.amax = 0;
     p.d_gate = up(kAmaxBlocks * 4);

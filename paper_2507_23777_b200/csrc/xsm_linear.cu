@@ -64,7 +64,7 @@ static LinearGradPlan plan_linear_grad(int rows, int vocab, int d, bool h, bool 
     if (p.piece > vocab) p.piece = (vocab + 63) / 64 * 64;
     p.pieces = (vocab + p.piece - 1) / p.piece;
     p.cut_z = product_cut(PR_DLOGITS, rows, p.piece);
-    p.sums = plan_sums(rows, p.piece, d, 1, h, w);
+    p.sums = plan_sums(rows, p.piece, d, 1, h, w, p.pieces == 1);
     p.amax = 0;
     p.dz = up(kAmaxBlocks * 4);
     p.part = p.dz + up((size_t)rows * p.piece * 2);

@@ -550,12 +550,15 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
                             for (int i = 0; i < 8; ++i)
                                 __stcg(reinterpret_cast<uint4 *>(p + c * 1024 + i * 128), make_uint4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]));
                         }
+                        if (P.apart) mine = false;
+                        else {
                         __threadfence();
                         __syncwarp();
                         unsigned before = 0;
                         if (lane == 0) before = atomicInc(A.counter + P.counters + (unsigned)((w.at * CG + rank) * kEpiWarps + warp - 2), (unsigned)P.splits - 1u);
                         mine = __shfl_sync(0xffffffffu, before, 0) == (unsigned)P.splits - 1u;
                         __threadfence();
+                        }
                     }
                     if (mine) {
 #pragma unroll 1
@@ -774,6 +777,32 @@ __global__ void __launch_bounds__(32) amax_pairs_kernel(const float *g, long lon
     if (threadIdx.x == 0) amax[blockIdx.x] = m;
 }
 
+// Adds up the sums of many splits, which lie as the threads of product_kernel left them: a quad of columns a thread.  (Where the last split adds them up itself, one CTA of a tile
+// reads them all: 24 splits of a tile of 256 x 256 take it 20 us.)
+template <int CG, int BN, typename T>
+__global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ ProductPart P, const float *amax, int amax_to) {
+    constexpr int kPieces = BN / 64, kTile = CG * kEpiWarps * kPieces * 1024;
+    chain_go();
+    chain_wait();
+    const float back = 1.f / scale_of(amax, amax_to);
+    const long long quads = (long long)P.by_plane.d * P.jobs * (kTile / 4);
+    for (long long i = blockIdx.x * 256ll + threadIdx.x; i < quads; i += gridDim.x * 256ll) {
+        const int at = (int)(i / (kTile / 4)), q = (int)(i - (long long)at * (kTile / 4)), lane = q & 31, four = q >> 5 & 7, piece = (q >> 8) % kPieces, w = (q >> 8) / kPieces % kEpiWarps,
+                  rank = (q >> 8) / (kPieces * kEpiWarps), job = at / (int)P.by_plane.d;
+        const Tile t = tile_of(P, (unsigned)P.first + (unsigned)(at - job * (int)P.by_plane.d));
+        const int row = t.m * 128 * CG + rank * 128 + ((w + 2) & 3) * 32 + lane, col = t.n * BN + (w >> 2) * (BN / 2) + piece * 32 + four * 4;
+        if (row >= P.m || col >= P.n) continue;
+        const float4 *p = reinterpret_cast<const float4 *>(P.partial) + (long long)at * P.splits * (kTile / 4) + q;
+        float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 8
+        for (int k = 0; k < P.splits; ++k) {
+            const float4 x = __ldcg(p + (long long)k * (kTile / 4));
+            s.x += x.x; s.y += x.y; s.z += x.z; s.w += x.w;
+        }
+        *reinterpret_cast<uint2 *>(reinterpret_cast<T *>(P.out[job]) + (long long)row * P.out_ld + col) = make_uint2(pack2<T>(s.x * back, s.y * back), pack2<T>(s.z * back, s.w * back));
+    }
+}
+
 // ------------------------------------------------------------------------------------------------------ host
 
 typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
@@ -948,10 +977,13 @@ cudaError_t launch_product(ProductEpi epi, int dtype, ProductCut cut, ProductArg
 static size_t tile_bytes(const ProductCut &cut) { return (size_t)cut.tm() * cut.bn * 4; }
 size_t sums_bytes(const ProductCut &cut, long long rows, long long d) { return (size_t)cut.tiles(rows, d, false) * tile_bytes(cut); }
 
+// Splits that the last of them adds up itself; more are added up by a kernel of its own.
+constexpr int kJoinedHere = 6;
+
 // Both products' tiles are dealt out in one row, x's first.  Tiles are as wide as the larger product asks for.  Where there are few of them the summed axes are cut: of the splits
 // that leave the CTAs with most to do least, in blocks of 64: a tile costs eight blocks on top (its last products, what is done with its sums), one that is cut sixteen, and for every
-// split that is added up three (one piece of 32 columns: one).
-SumsPlan plan_sums(long long rows, long long cols, long long d, int pairs, bool x, bool y) {
+// split that is added up three (one piece of 32 columns: one), or ten and a launch of ten more.
+SumsPlan plan_sums(long long rows, long long cols, long long d, int pairs, bool x, bool y, bool once) {
     SumsPlan p = {};
     p.cut = (x && rows > 128 && d > 64) || (y && cols > 128 && d > 64) ? ProductCut{true, 256} : ProductCut{false, 64};
     const long long slots = product_sms() < 2 ? 1 : p.cut.wide ? product_sms() / 2 : product_sms(), kx = (cols + 63) / 64 * pairs, ky = (rows + 63) / 64;
@@ -960,13 +992,13 @@ SumsPlan plan_sums(long long rows, long long cols, long long d, int pairs, bool 
     if (tx + ty < 4 * slots) {
         static const int tries[] = {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 40, 48, 64, 96, 128};
         const double each = !p.cut.wide || d <= 32 ? 1 : d <= 64 ? 2 : 3;
-        auto cost = [&](long long k, int s) { return (double)((k + s - 1) / s) + (s > 1 ? 16 + each * s : 8); };
+        auto cost = [&](long long k, int s) { return (double)((k + s - 1) / s) + (s == 1 ? 8 : s <= kJoinedHere ? 16 + each * s : 16); };
         double least = 1e300;
         for (int sx : tries) {
-            if (sx > 1 && (!x || sx * 4 > kx)) break;
+            if (sx > 1 && (!x || sx * 4 > kx || (!once && sx > kJoinedHere))) break;
             for (int sy : tries) {
                 if (sy > 1 && (!y || sy * 4 > ky)) break;
-                if ((sx > 1 ? tx : 0) * per + (sy > 1 ? ty : 0) * per > kSumCounters) continue;
+                if ((sx > 1 && sx <= kJoinedHere ? tx : 0) * per + (sy > 1 && sy <= kJoinedHere ? ty : 0) * per > kSumCounters) continue;
                 const long long nx = tx * sx, all = nx + ty * sy;
                 const double cx = cost(kx, sx), cy = cost(ky, sy);
                 double most = 0;
@@ -977,6 +1009,7 @@ SumsPlan plan_sums(long long rows, long long cols, long long d, int pairs, bool 
                     if (t > most) most = t;
                 };
                 of(0); of(nx % slots - 1); of(nx % slots); of(all % slots - 1); of(all % slots);
+                most += (sx > kJoinedHere ? 20 : 0) + (sy > kJoinedHere ? 20 : 0);
                 if (most < least - 1e-9) { least = most; p.splits_x = sx; p.splits_y = sy; }
             }
         }
@@ -985,6 +1018,14 @@ SumsPlan plan_sums(long long rows, long long cols, long long d, int pairs, bool 
     p.partial_y = p.splits_x > 1 ? (size_t)tx * p.splits_x * tile_bytes(p.cut) : 0;
     p.bytes = p.partial_y + (p.splits_y > 1 ? (size_t)ty * p.splits_y * tile_bytes(p.cut) : 0);
     return p;
+}
+
+static cudaError_t launch_join(const ProductCut &cut, int dtype, const ProductPart &P, const ProductArgs &A, cudaStream_t st) {
+    const long long blocks = (long long)P.by_plane.d * P.jobs * (long long)(tile_bytes(cut) / 16 / 256), most = (long long)product_sms() * 8;
+    const dim3 grid((unsigned)(blocks < most ? blocks : most));
+    if (cut.wide)
+        return dtype == XSM_BF16 ? launch_early(join_kernel<2, 256, bf16>, grid, dim3(256), 0, st, P, A.amax, A.amax_to) : launch_early(join_kernel<2, 256, __half>, grid, dim3(256), 0, st, P, A.amax, A.amax_to);
+    return dtype == XSM_BF16 ? launch_early(join_kernel<1, 64, bf16>, grid, dim3(256), 0, st, P, A.amax, A.amax_to) : launch_early(join_kernel<1, 64, __half>, grid, dim3(256), 0, st, P, A.amax, A.amax_to);
 }
 
 cudaError_t launch_sums(int dtype, const SumsPlan &p, const Sums &s, cudaStream_t st) {
@@ -1014,6 +1055,7 @@ cudaError_t launch_sums(int dtype, const SumsPlan &p, const Sums &s, cudaStream_
         X.a_rows = rows >= 128 ? 128 : (rows + 7) / 8 * 8;
         X.stage_tx = (uint32_t)(group * (X.a_rows * 128 + p.cut.bn / group * 128));
         X.partial = (float *)(s.partial + p.partial_x);
+        X.apart = X.splits > kJoinedHere;
         X.sums = s.x_sums; X.go_on = s.go_on; X.end = s.end;
         X.out[0] = s.x; X.out_ld = s.x_ld;
         for (int i = 0; i < s.pairs; ++i) {
@@ -1030,7 +1072,8 @@ cudaError_t launch_sums(int dtype, const SumsPlan &p, const Sums &s, cudaStream_
         Y.stage_tx = group * A.stage;
         Y.map_a = 2; Y.map_b = 2; Y.map_out = 1;
         Y.partial = (float *)(s.partial + p.partial_y);
-        Y.counters = X.splits > 1 ? (unsigned)(X.by_plane.d * group * 8) : 0;
+        Y.apart = Y.splits > kJoinedHere;
+        Y.counters = X.splits > 1 && !X.apart ? (unsigned)(X.by_plane.d * group * 8) : 0;
         for (int i = 0; i < s.pairs; ++i) {
             ok = ok && operand_map(encode, &M.a[2 + i], s.g[i], dtype, 64, 1);
             Y.out[i] = s.y[i];
@@ -1041,7 +1084,10 @@ cudaError_t launch_sums(int dtype, const SumsPlan &p, const Sums &s, cudaStream_
         A.tiles += Y.tiles;
     }
     if (!ok) return cudaErrorInvalidValue;
-    return A.tiles ? start_cut<PR_OUT>(p.cut, dtype, M, A, st) : cudaSuccess;
+    if (A.tiles) e = start_cut<PR_OUT>(p.cut, dtype, M, A, st);
+    for (const ProductPart &P : A.part)
+        if (e == cudaSuccess && P.tiles && P.apart) e = launch_join(p.cut, dtype, P, A, st);
+    return e;
 }
 
 cudaError_t launch_amax_rows(const void *x, int dtype, long long rows, long long cols, long long ld, float *amax, cudaStream_t st) {

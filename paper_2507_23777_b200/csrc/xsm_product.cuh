@@ -37,6 +37,7 @@ struct ProductPart {
     int rows_a;                     // A's rows run along the summed axis
     int map_a, map_b, map_out;      // the first of its descriptions
     float *partial;                 // where there are splits: their sums
+    int apart;                      // so many splits that a kernel of its own adds them up
     float *sums;                    // where the result is made in several launches: fp32 sums so far, NULL: made in this one
     int go_on, end;                 // add to them; this is the last
     unsigned counters;              // the first of its counters
@@ -140,7 +141,7 @@ struct Sums {
     int amax_to;
     int *status;
 };
-SumsPlan plan_sums(long long rows, long long cols, long long d, int pairs, bool x, bool y);
+SumsPlan plan_sums(long long rows, long long cols, long long d, int pairs, bool x, bool y, bool once);      // once: x is made in one launch
 size_t sums_bytes(const ProductCut &cut, long long rows, long long d);      // of x_sums
 cudaError_t launch_sums(int dtype, const SumsPlan &p, const Sums &s, cudaStream_t st);
 
