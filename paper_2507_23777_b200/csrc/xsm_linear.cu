@@ -1,9 +1,13 @@
 // Log probabilities of given tokens straight from hidden states and the weights of an output projection, and their gradients: the logits of a tile are
 // worked on where the products leave them and are never in memory.
 //
-// Forward: z = hidden . weight / T; every tile of 256 (few rows: 64) tokens of the vocabulary gives a row two pairs (maximum, sum of exponentials), a second
-// kernel joins them: lse = max + log sum.  Backward, in pieces of the vocabulary: the logits once more, p = exp(z - lse), d = ([token] g - p (g - g_lse)) / T
-// rounded to the operands' type, then d_hidden = d . weight and d_weight = d^T . hidden.
+// Forward: z = hidden . weight / T; every tile of 256 (few rows: a CTA's tiles) tokens of the vocabulary gives a row two pairs (maximum, sum of exponentials), which a second
+// kernel joins, or, of few rows, the CTA that ends last: lse = max + log sum.  Backward, in pieces of the vocabulary: the logits once more, p = exp(z - lse),
+// d = ([token] g - p (g - g_lse)) / T rounded to the operands' type, then d_hidden = d . weight and d_weight = d^T . hidden in one launch.  d in 16 bits: that product
+// is two thirds of the work; it doubles the square of the gradients' error (a rounding before the sum next to the one behind it).
+//
+// What bounds it.  8192 rows, 32003 tokens, 2048 wide: 3.1 ms for four products of 1.07 TFLOP (three without the logits again), 1.39 PFLOP/s under the power limit, what the
+// library's own product sustains.  4096 x 4096 x 1024: 28 + 76 us, three launches' beginnings and ends in it.  1999 x 5003 x 768: 21 + 46.
 #include "xsm_product.cuh"
 
 #include <math.h>

@@ -2,11 +2,15 @@
 // tokens on their way to the pages of a cache.
 //
 // y = R(position) (gain x r), r = (mean x^2 + eps)^(-1/2) over a head.  Gradient: u = R^-1 dy, d_gain = sum over rows of u x r, dx = r (w - x r^2 mean(w x)), w = gain u.
-// A head is 2 to 16 neighbouring lanes, which hold two runs of eight elements each, the two halves of eight pairs, so that norm and rotation need nothing but
+// A head is 2 to 32 neighbouring lanes, which hold two runs of 16 bytes each, the two halves of their pairs, so that norm and rotation need nothing but
 // the lanes' own registers and a sum over them.  A group of lanes takes some heads of a token one behind the other, what the token's angles and the gains have to do with an
 // element in registers; the heads to come are on their way to slots of shared memory that each lane has for itself, so that neither registers nor barriers limit
 // how many.  d_gain is added up in registers over all rows of a group, then over a block, then over blocks in a fixed order: no result hangs on who
 // comes first.
+//
+// What bounds it.  8192 tokens of 32 + 8 heads of 128 in bf16: forward 33 us where its bytes take 26 at the copy rate, gradient 54 and a kernel of 5 where they take 39: memory at 77 and
+// 66 %, half of the issue slots (two numbers an instruction), four warps a scheduler, which the registers allow (three blocks an SM instead of two: 33 -> 43 us).  Four rows
+// on their way are enough (six, eight: no faster).  A window of five tokens into the pages: 3.2 us, two latencies behind a launch.
 #include "xsm_ops.h"
 #include "xsm_chain.cuh"
 
@@ -171,7 +175,7 @@ __device__ __forceinline__ void finish_gains(const NormArgs &A) {
 
 // Rows and angles in 16-byte pieces.  L lanes a head; the lanes' first runs lie side by side, and so do the second ones, half of the turned (of the other) part of the head
 // further: with half-split pairs a lane then has both elements of each, with neighbouring ones (kNear) anyway.  (Two runs of a lane side by side made accesses of half
-// sectors: 20 us instead of ... for 3003 tokens of 32 heads of 64 in fp32.)
+// sectors: 20 us instead of 13 for 3003 tokens of 32 heads of 64 in fp32.)
 // kFinish: the block that ends last adds up the blocks' d_gain (a kernel of its own: the code for it costs the loop 3 us of 20).
 template <typename TI, typename TC, int L, bool kNear, int MODE, bool kFinish>
 __global__ void __launch_bounds__(kNormThreads, kNormBlocks) norm_kernel(const __grid_constant__ NormArgs A, const __grid_constant__ Pages P) {
@@ -576,7 +580,7 @@ static int norm_sms() {
 }
 static int lanes_of(int d, int es, bool wide) { return !wide ? 32 : d == 96 ? 128 * es / 32 : d * es / 32; }
 
-// Heads of a unit and blocks of each tensor.  No more blocks than run at a time (one more cost 41 us instead of ...), shared out by the tensors' heads; of 8, 4, 2 and 1 heads a
+// Heads of a unit and blocks of each tensor.  No more blocks than run at a time (one more: 41 us instead of 33 for 8192 tokens of 32 + 8 heads of 128), shared out by the tensors' heads; of 8, 4, 2 and 1 heads a
 // unit those with which the groups that have most to do have least: a unit costs a group as much as one and a half heads before the first of them.
 static int cut_norm(NormArgs &A, int lanes) {
     const int groups = kNormThreads / lanes, most = norm_sms() * kNormBlocks;

@@ -3,6 +3,12 @@
 // One persistent kernel.  A warp fetches blocks of 64 along the summed axis of both operands by TMA into a ring, a warp issues the products,
 // eight warps work on finished tiles out of tensor memory while the products of the next one run (two accumulators).  Operands may lie either
 // way: rows along the summed axis (boxes of 64 rows of 64 elements, "MN-major") or across it ("K-major"); nothing is transposed in memory.
+//
+// What bounds it.  Many rows, two CTAs a tile of 256 x 256: the tensor cores.  8192 x 32003 x 2048 takes 983,000 cycles of 901,000 that the products alone take in their
+// 55 rounds of 74 tiles, 660 us at the 1.49 GHz that the power limit leaves: 1.63 PFLOP/s.  Summed axes below some 800 would be bound by what is done with a tile
+// (4,000 cycles; act(gate) up 2,650) where these are not the products' 4 cycles a step.  A launch's first products come 3,400 cycles after its beginning, its end 6,000
+// after its last products.  Few rows: the bytes of the weights (96 x 131071 x 1024: 49 us, 41 at the copy rate), very few a chain (5 x 4096 x 1024: 7.5 us: 2,000 cycles
+// to the first copy, 3,700 for the bytes, 1,600 for the tile, then the last CTA's sums).
 #include "xsm_product.cuh"
 
 #include <limits.h>
@@ -17,7 +23,6 @@ constexpr int kEpiWarps = 8;
 constexpr int kProductThreads = 64 + 32 * kEpiWarps;
 constexpr int kABytes = 128 * 128;              // of a stage and a CTA: 128 rows of A, 64 elements of the summed axis
 constexpr int kRingBytes = 192 * 1024;
-
 constexpr int kMaxStages = 24;
 
 // ------------------------------------------------------------------------------------------- instructions
@@ -446,58 +451,58 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
                 uint32_t held[CG == 2 && EPI == PR_GATED_GRAD ? BN / 8 : 1];        // up's gradients, packed, until the buffer is free again
                 auto columns = [&](auto kind) {
 #pragma unroll
-                for (int c = 0; c < BN / 4; c += N) {
-                    uint32_t vg[N], vu[N];
-                    tmem_ld(vg, sums + (uint32_t)(half * (BN / 4) + c));
-                    tmem_ld(vu, sums + (uint32_t)(BN / 2 + half * (BN / 4) + c));
-                    [[maybe_unused]] const int col = col0 + c;
-                    float x[N];
-                    if constexpr (EPI == PR_GATED_GRAD) {
-                        if constexpr (CG == 2) {
+                    for (int c = 0; c < BN / 4; c += N) {
+                        uint32_t vg[N], vu[N];
+                        tmem_ld(vg, sums + (uint32_t)(half * (BN / 4) + c));
+                        tmem_ld(vu, sums + (uint32_t)(BN / 2 + half * (BN / 4) + c));
+                        [[maybe_unused]] const int col = col0 + c;
+                        float x[N];
+                        if constexpr (EPI == PR_GATED_GRAD) {
+                            if constexpr (CG == 2) {
 #pragma unroll
-                            for (int i = 0; i < N; i += 8) {
-                                const uint4 u = lds128(piece_at(buf, lane, (c + i) / 8));
-                                T e[8];
-                                memcpy(e, &u, 16);
+                                for (int i = 0; i < N; i += 8) {
+                                    const uint4 u = lds128(piece_at(buf, lane, (c + i) / 8));
+                                    T e[8];
+                                    memcpy(e, &u, 16);
 #pragma unroll
-                                for (int j = 0; j < 8; ++j) x[i + j] = to_f(e[j]) * scale;
+                                    for (int j = 0; j < 8; ++j) x[i + j] = to_f(e[j]) * scale;
+                                }
+                            } else {
+                                const T *gy = reinterpret_cast<const T *>(A.g_y) + (long long)row * A.g_y_ld;
+#pragma unroll
+                                for (int i = 0; i < N; ++i) x[i] = live && col + i < P.n ? to_f(gy[col + i]) * scale : 0.f;
                             }
+                        }
+                        tmem_wait_ld();
+                        if constexpr (EPI == PR_GATED) {
+#pragma unroll
+                            for (int i = 0; i < N; ++i) {
+                                float a, da;
+                                activate<decltype(kind)::value>(__uint_as_float(vg[i]), a, da);
+                                x[i] = a * __uint_as_float(vu[i]);
+                            }
+                            if constexpr (CG == 2) put_row<T>(buf, lane, c / 8, x);
+                            else if (live) store_row(reinterpret_cast<T *>(A.out[0]) + (long long)row * A.out_ld, col, P.n, (A.out_ld & 7) == 0 && ((uintptr_t)A.out[0] & 15) == 0, x);
                         } else {
-                            const T *gy = reinterpret_cast<const T *>(A.g_y) + (long long)row * A.g_y_ld;
+                            float y[N];
 #pragma unroll
-                            for (int i = 0; i < N; ++i) x[i] = live && col + i < P.n ? to_f(gy[col + i]) * scale : 0.f;
+                            for (int i = 0; i < N; ++i) {
+                                float a, da;
+                                activate<decltype(kind)::value>(__uint_as_float(vg[i]), a, da);
+                                y[i] = x[i] * a;
+                                x[i] = x[i] * __uint_as_float(vu[i]) * da;
+                            }
+                            if constexpr (CG == 2) {
+                                put_row<T>(buf, lane, c / 8, x);
+#pragma unroll
+                                for (int i = 0; i < N; i += 2) held[(c + i) / 2] = pack2<T>(y[i], y[i + 1]);
+                            } else if (live) {        // (workspace rows of a multiple of eight elements: what lies behind the last column is nobody's)
+                                const int n8 = (int)A.out_ld;
+                                store_row(reinterpret_cast<T *>(A.out[0]) + (long long)row * A.out_ld, col, n8, true, x);
+                                store_row(reinterpret_cast<T *>(A.out[1]) + (long long)row * A.out_ld, col, n8, true, y);
+                            }
                         }
                     }
-                    tmem_wait_ld();
-                    if constexpr (EPI == PR_GATED) {
-#pragma unroll
-                        for (int i = 0; i < N; ++i) {
-                            float a, da;
-                            activate<decltype(kind)::value>(__uint_as_float(vg[i]), a, da);
-                            x[i] = a * __uint_as_float(vu[i]);
-                        }
-                        if constexpr (CG == 2) put_row<T>(buf, lane, c / 8, x);
-                        else if (live) store_row(reinterpret_cast<T *>(A.out[0]) + (long long)row * A.out_ld, col, P.n, (A.out_ld & 7) == 0 && ((uintptr_t)A.out[0] & 15) == 0, x);
-                    } else {
-                        float y[N];
-#pragma unroll
-                        for (int i = 0; i < N; ++i) {
-                            float a, da;
-                            activate<decltype(kind)::value>(__uint_as_float(vg[i]), a, da);
-                            y[i] = x[i] * a;
-                            x[i] = x[i] * __uint_as_float(vu[i]) * da;
-                        }
-                        if constexpr (CG == 2) {
-                            put_row<T>(buf, lane, c / 8, x);
-#pragma unroll
-                            for (int i = 0; i < N; i += 2) held[(c + i) / 2] = pack2<T>(y[i], y[i + 1]);
-                        } else if (live) {        // (workspace rows of a multiple of eight elements: what lies behind the last column is nobody's)
-                            const int n8 = (int)A.out_ld;
-                            store_row(reinterpret_cast<T *>(A.out[0]) + (long long)row * A.out_ld, col, n8, true, x);
-                            store_row(reinterpret_cast<T *>(A.out[1]) + (long long)row * A.out_ld, col, n8, true, y);
-                        }
-                    }
-                }
                 };
                 if (A.activation == ACT_SILU) columns(std::integral_constant<int, ACT_SILU>());
                 else columns(std::integral_constant<int, ACT_GELU>());
@@ -550,14 +555,15 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
                             for (int i = 0; i < 8; ++i)
                                 __stcg(reinterpret_cast<uint4 *>(p + c * 1024 + i * 128), make_uint4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]));
                         }
-                        if (P.apart) mine = false;
-                        else {
-                        __threadfence();
-                        __syncwarp();
-                        unsigned before = 0;
-                        if (lane == 0) before = atomicInc(A.counter + P.counters + (unsigned)((w.at * CG + rank) * kEpiWarps + warp - 2), (unsigned)P.splits - 1u);
-                        mine = __shfl_sync(0xffffffffu, before, 0) == (unsigned)P.splits - 1u;
-                        __threadfence();
+                        if (P.apart) {
+                            mine = false;
+                        } else {
+                            __threadfence();
+                            __syncwarp();
+                            unsigned before = 0;
+                            if (lane == 0) before = atomicInc(A.counter + P.counters + (unsigned)((w.at * CG + rank) * kEpiWarps + warp - 2), (unsigned)P.splits - 1u);
+                            mine = __shfl_sync(0xffffffffu, before, 0) == (unsigned)P.splits - 1u;
+                            __threadfence();
                         }
                     }
                     if (mine) {
@@ -620,50 +626,50 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
                     }
                 } else {
 #pragma unroll 1
-                for (int c = 0; c < BN / 2; c += N) {
-                    uint32_t v[N];
-                    tmem_ld(v, sums + (uint32_t)(half * (BN / 2) + c));
-                    const int col = col0 + c;
-                    if (CG == 2 && EPI == PR_DLOGITS && (c & 32) == 0) rows_free(lane);
-                    tmem_wait_ld();
-                    if constexpr (EPI == PR_STATS) {
-                        if (col + N > P.n) {
+                    for (int c = 0; c < BN / 2; c += N) {
+                        uint32_t v[N];
+                        tmem_ld(v, sums + (uint32_t)(half * (BN / 2) + c));
+                        const int col = col0 + c;
+                        if (CG == 2 && EPI == PR_DLOGITS && (c & 32) == 0) rows_free(lane);
+                        tmem_wait_ld();
+                        if constexpr (EPI == PR_STATS) {
+                            if (col + N > P.n) {
 #pragma unroll
-                            for (int i = 0; i < N; ++i)
-                                if (col + i >= P.n) v[i] = 0xff800000u;        // -infinity
-                        }
-                        float top = __uint_as_float(v[0]);
+                                for (int i = 0; i < N; ++i)
+                                    if (col + i >= P.n) v[i] = 0xff800000u;        // -infinity
+                            }
+                            float top = __uint_as_float(v[0]);
 #pragma unroll
-                        for (int i = 1; i < N; ++i) top = fmaxf(top, __uint_as_float(v[i]));
-                        if (token >= col && token < col + N) {
+                            for (int i = 1; i < N; ++i) top = fmaxf(top, __uint_as_float(v[i]));
+                            if (token >= col && token < col + N) {
 #pragma unroll
-                            for (int i = 0; i < N; ++i)
-                                if (token == col + i) A.token_z[row] = __uint_as_float(v[i]) * A.inv_t;
-                        }
-                        const float was = mx;
-                        mx = fmaxf(mx, top * A.c);
-                        const float base = mx == -INFINITY ? 0.f : mx;
-                        float more[2] = {0.f, 0.f};
+                                for (int i = 0; i < N; ++i)
+                                    if (token == col + i) A.token_z[row] = __uint_as_float(v[i]) * A.inv_t;
+                            }
+                            const float was = mx;
+                            mx = fmaxf(mx, top * A.c);
+                            const float base = mx == -INFINITY ? 0.f : mx;
+                            float more[2] = {0.f, 0.f};
 #pragma unroll
-                        for (int i = 0; i < N; ++i) more[i & 1] += ex2(fmaf(__uint_as_float(v[i]), A.c, -base));
-                        sum = fmaf(sum, ex2(was - base), more[0] + more[1]);
-                    } else {
-                        float x[N];
+                            for (int i = 0; i < N; ++i) more[i & 1] += ex2(fmaf(__uint_as_float(v[i]), A.c, -base));
+                            sum = fmaf(sum, ex2(was - base), more[0] + more[1]);
+                        } else {
+                            float x[N];
 #pragma unroll
-                        for (int i = 0; i < N; ++i) x[i] = -gp * ex2(fmaf(__uint_as_float(v[i]), A.c, -lse2));
-                        if (token >= col && token < col + N) {
+                            for (int i = 0; i < N; ++i) x[i] = -gp * ex2(fmaf(__uint_as_float(v[i]), A.c, -lse2));
+                            if (token >= col && token < col + N) {
 #pragma unroll
-                            for (int i = 0; i < N; ++i)
-                                if (token == col + i) x[i] += g;
-                        }
-                        if constexpr (CG == 2) {
-                            put_row<T>(buf, lane, (c & 32) / 8, x);
-                            if (c & 32) rows_store(&M.out[0], buf, col - 32, row0, 0, row0 < P.m && col - 32 < P.n, lane);
-                        } else if (live) {
-                            store_row(reinterpret_cast<T *>(A.out[0]) + (long long)row * A.out_ld, col, (int)A.out_ld, true, x);
+                                for (int i = 0; i < N; ++i)
+                                    if (token == col + i) x[i] += g;
+                            }
+                            if constexpr (CG == 2) {
+                                put_row<T>(buf, lane, (c & 32) / 8, x);
+                                if (c & 32) rows_store(&M.out[0], buf, col - 32, row0, 0, row0 < P.m && col - 32 < P.n, lane);
+                            } else if (live) {
+                                store_row(reinterpret_cast<T *>(A.out[0]) + (long long)row * A.out_ld, col, (int)A.out_ld, true, x);
+                            }
                         }
                     }
-                }
                 }
                 if constexpr (EPI == PR_STATS) {
                     if (!A.carry) {
@@ -1092,7 +1098,7 @@ cudaError_t launch_sums(int dtype, const SumsPlan &p, const Sums &s, cudaStream_
 
 cudaError_t launch_amax_rows(const void *x, int dtype, long long rows, long long cols, long long ld, float *amax, cudaStream_t st) {
     long long all = LLONG_MAX;
-    if (ld == cols) {        // one run of elements: a part for each block, of whole 16-byte pieces (2047 rows of 2051 fp16 10 -> ... us)
+    if (ld == cols) {        // one run of elements: a part for each block, of whole 16-byte pieces (2047 rows of 2051 fp16: 10 us row by row, 7 so)
         all = rows * cols;
         ld = cols = (all / kAmaxBlocks + 8) / 8 * 8;
         rows = (all + cols - 1) / cols;
