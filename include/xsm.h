@@ -350,7 +350,7 @@ XSM_API xsm_status xsm_token_logprobs_grad_near(const xsm_logprob_grad_args *a, 
 /* ---- operators on a caller's own activations and weights ----
  *
  * Products on the tensor cores with what follows them in the same kernel: 16-bit elements (XSM_BF16, XSM_F16; rows 16-byte aligned, strides in elements), sums in
- * fp32.  `d`, the summed axis of the forward products, is a multiple of 8; other sizes are any.  As above: the caller's stream of the current device, nothing is waited
+ * fp32.  `d`, the summed axis of the forward products, is a multiple of 8; other sizes are any, up to 2^30.  As above: the caller's stream of the current device, nothing is waited
  * for, calls may be captured.  status: DEVICE, a 32-bit word, zeroed by the caller before its first use, which calls may share: XSM_ERR_TIMEOUT once a bounded wait of the
  * device has run out, and the results of that call are then void.  counters: DEVICE, XSM_COUNTERS words, zero before their first use and again after every call, but for one whose
  * wait ran out; calls that share them follow each other on one stream.  workspace: DEVICE, 16-byte aligned, as many bytes as the function of that name says, of any
@@ -407,7 +407,7 @@ typedef struct {
 XSM_API xsm_status xsm_gated_ff(const xsm_gated_ff_args *a, void *cuda_stream);
 
 /* The gradient of sum(g_out * out) by x, w_gate and w_up, in their type.  gate and up are computed again; their gradients g_out up act'(gate) and g_out act(gate) are
- * rounded to dtype once (fp16: scaled by the power of two that takes the largest finite g_out to [1, 2)).  d_x, or d_w_gate and d_w_up, may be NULL. */
+ * rounded to dtype once (fp16: scaled by the power of two that takes the largest finite g_out to [1, 2): up act'(gate) beyond 2^15 is infinite, what is below 2^-25 zero).  d_x, or d_w_gate and d_w_up, may be NULL. */
 typedef struct {
     const void *x, *w_gate, *w_up;        /* as above */
     const void *g_out;                    /* DEVICE dtype [rows][ff]; aligned to its elements */

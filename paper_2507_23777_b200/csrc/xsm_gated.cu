@@ -35,6 +35,7 @@ static GatedGradPlan plan_gated_grad(int rows, int ff, int d, bool x, bool w) {
 static const char *wrong_shape(int rows, int ff, int d, int dtype, int activation) {
     if (dtype != XSM_BF16 && dtype != XSM_F16) return "dtype must be 1 (bf16) or 2 (fp16)";
     if (rows < 0 || ff < 1 || d < 8 || d % 8) return "rows must not be negative, ff positive, d a positive multiple of 8";
+    if (rows > kMostRows || ff > kMostRows || d > kMostRows) return "rows, ff and d must not exceed 2^30";
     if (activation != ACT_SILU && activation != ACT_GELU) return "activation must be 0 (silu) or 1 (gelu)";
     return nullptr;
 }
@@ -60,7 +61,7 @@ xsm_status xsm_gated_ff(const xsm_gated_ff_args *a, void *cuda_stream) {
 }
 
 size_t xsm_gated_ff_grad_workspace(int rows, int ff, int d) {
-    if (rows < 1 || ff < 1 || d < 1) return 0;
+    if (rows < 1 || ff < 1 || d < 1 || rows > kMostRows || ff > kMostRows || d > kMostRows) return 0;
     const size_t a = plan_gated_grad(rows, ff, d, true, true).bytes, b = plan_gated_grad(rows, ff, d, true, false).bytes, c = plan_gated_grad(rows, ff, d, false, true).bytes;
     return a > b ? (a > c ? a : c) : b > c ? b : c;
 }

@@ -80,6 +80,7 @@ static LinearGradPlan plan_linear_grad(int rows, int vocab, int d, bool h, bool 
 static const char *wrong_shape(int rows, int vocab, int d, int dtype, int token_bytes, float temperature) {
     if (dtype != XSM_BF16 && dtype != XSM_F16) return "dtype must be 1 (bf16) or 2 (fp16)";
     if (rows < 0 || vocab < 1 || d < 8 || d % 8) return "rows must not be negative, vocab positive, d a positive multiple of 8";
+    if (rows > kMostRows || vocab > kMostRows || d > kMostRows) return "rows, vocab and d must not exceed 2^30";
     if (token_bytes != 4 && token_bytes != 8) return "token_bytes must be 4 or 8";
     if (!(temperature > 0.f) || !(temperature < INFINITY) || !(1.f / temperature < INFINITY)) return "temperature must be positive and finite, and its reciprocal finite";
     return nullptr;
@@ -92,7 +93,7 @@ using namespace xsm;
 
 size_t xsm_linear_logprobs_workspace(int rows, int vocab, int d) {
     (void)d;
-    if (rows < 1 || vocab < 1) return 0;
+    if (rows < 1 || vocab < 1 || rows > kMostRows || vocab > kMostRows) return 0;
     return up((size_t)plan_linear(rows, vocab).parts * rows * 8) + up((size_t)rows * 4);
 }
 
@@ -128,7 +129,7 @@ xsm_status xsm_linear_logprobs(const xsm_linear_logprobs_args *a, void *cuda_str
 }
 
 size_t xsm_linear_logprobs_grad_workspace(int rows, int vocab, int d) {
-    if (rows < 1 || vocab < 1 || d < 1) return 0;
+    if (rows < 1 || vocab < 1 || d < 1 || rows > kMostRows || vocab > kMostRows || d > kMostRows) return 0;
     const size_t a = plan_linear_grad(rows, vocab, d, true, true).bytes, b = plan_linear_grad(rows, vocab, d, true, false).bytes, c = plan_linear_grad(rows, vocab, d, false, true).bytes;
     return a > b ? (a > c ? a : c) : b > c ? b : c;
 }

@@ -18,6 +18,7 @@ enum ProductEpi {
 enum Activation { ACT_SILU = 0, ACT_GELU = 1 };
 
 constexpr int kAmaxBlocks = 256;
+constexpr int kMostRows = 1 << 30;      // of an operand, and elements of one: a tile's last row and column are then ints too
 
 constexpr int kSumCounters = 2048;      // words that PR_OUT counts in
 

@@ -84,6 +84,18 @@ def test_wrong_arguments_of_gated_ff(lib, wrong, word):
     assert word in lib.xsm_last_error(None)
 
 
+def test_sizes_beyond_what_tiles_are_counted_in(lib):
+    from paper_2507_23777_b200 import ops
+    big = (1 << 30) + 8
+    for sizes in (dict(rows=big), dict(vocab=big), dict(d=big, strides=(big, big, 1))):
+        assert lib.xsm_linear_logprobs(linear(**sizes), None) == binding.XSM_ERR_INVALID_ARG and b"2^30" in lib.xsm_last_error(None)
+    for rows, ff, d in ((big, 8, 8), (8, big, 8), (8, 8, big)):
+        args = ops._GATED.pack(*5 * [A], d, d, d, ff, rows, ff, d, 1, 0)
+        assert lib.xsm_gated_ff(args, None) == binding.XSM_ERR_INVALID_ARG and b"2^30" in lib.xsm_last_error(None)
+        assert lib.xsm_gated_ff_grad_workspace(rows, ff, d) == 0 == lib.xsm_linear_logprobs_grad_workspace(rows, ff, d)
+    assert lib.xsm_linear_logprobs_workspace(big, 8, 8) == 0 == lib.xsm_linear_logprobs_workspace(8, big, 8)
+
+
 def test_gradients_that_go_together(lib):
     from paper_2507_23777_b200 import ops
     args = ops._GATED_GRAD.pack(A, A, A, A, A, A, 0, A, A, A, 64, 64, 64, 100, 64, 64, 1 << 30, 4, 100, 64, 1, 0)
