@@ -667,7 +667,7 @@ def _linear_forward(hidden, weight, tokens, temperature):
 def linear_logprobs_grad(hidden, weight, tokens, result, grad_logprob=None, grad_lse=None, temperature=1.0, need=(True, True)):
     """The gradients (d_hidden, d_weight), in their type, of sum(grad_logprob * logprob) + sum(grad_lse * lse) of what linear_logprobs returned as `result` for the
     same hidden, weight, tokens and temperature.  grad_*: float32 [rows]; each may be missing.  need: which of the two are wanted; the other is None.  The
-    logits are computed again, at most 256 MiB of their gradients are in memory at a time.  There are no second derivatives: tensors that want a gradient are
+    logits are computed again, at most 256 MiB of their gradients (or 1024 tokens' of each row) are in memory at a time.  There are no second derivatives: tensors that want a gradient are
     refused unless torch.no_grad() says that it is not needed."""
     _no_gradient("linear_logprobs_grad", hidden, weight, result[1], grad_logprob, grad_lse)
     device, dtype, rows, d, ld, w_ld = _check_linear(hidden, weight, tokens)
@@ -741,7 +741,7 @@ def _check_gated(x, w_gate, w_up, activation):
     """(device, type, x as a matrix, rows, ff, d, row strides) of arguments that go together, all of it looked at at once."""
     dtype, device, w_shape, kind = x.dtype, x.get_device(), w_gate.shape, _ACTIVATIONS.get(activation)
     ok = kind is not None and len(w_shape) == 2 and w_shape == w_up.shape and (dtype is torch.bfloat16 or dtype is torch.float16) and x.dim() >= 1
-    if ok:
+    if ok and x.shape[-1]:
         flat = x if x.dim() == 2 else x.reshape(-1, x.shape[-1])
         (rows, d), ff = flat.shape, w_shape[0]
         (ld, a), (g_ld, b), (u_ld, c) = flat.stride(), w_gate.stride(), w_up.stride()
@@ -752,6 +752,8 @@ def _check_gated(x, w_gate, w_up, activation):
         ok = (w_shape[1] == d and d >= 8 and ff >= 1 and (d | ld | g_ld | u_ld) & 7 == 0 and a == b == c == 1 and ld >= d and g_ld >= d and u_ld >= d and
               w_gate.dtype is dtype is w_up.dtype and device == w_gate.get_device() == w_up.get_device() == _current_device() and
               (flat.data_ptr() | w_gate.data_ptr() | w_up.data_ptr()) & 15 == 0)
+    else:
+        ok = False
     if not ok:
         _refuse_gated(x, w_gate, w_up, activation)
     return device, dtype, flat, rows, ff, d, ld, g_ld, u_ld, kind
@@ -901,16 +903,22 @@ def _norm_layout(q, k, q_gain, k_gain, rope, positions):
     return device, qs, ks, (to_q, to_k, to_qg, to_kg, to_at, to_rope), (batch, m, heads, kv_heads, d, _DTYPES[dtype], _DTYPES[gain_dtype], n, 2 * half)
 
 
+def _like(t):
+    """A tensor like t whose heads' elements are neighbours, also where t's rows overlap."""
+    r = torch.empty_like(t)
+    return r if r.stride(3) == 1 else torch.empty(t.shape, dtype=t.dtype, device=t.device)
+
+
 def _norm_forward(q, k, q_gain, k_gain, rope, positions, eps, interleaved):
     device, qs, ks, (to_q, to_k, to_qg, to_kg, to_at, to_rope), sizes = _norm_layout(q, k, q_gain, k_gain, rope, positions)
     q_out = k_out = None
     os = us = _NONE
     to_qo = to_ko = 0
     if q is not None:
-        q_out = torch.empty_like(q)
+        q_out = _like(q)
         os, to_qo = q_out.stride(), q_out.data_ptr()
     if k is not None:
-        k_out = torch.empty_like(k)
+        k_out = _like(k)
         us, to_ko = k_out.stride(), k_out.data_ptr()
     try:
         args = _NORM.pack(to_q, to_k, to_qo, to_ko, to_qg, to_kg, to_at, to_rope, qs[0], qs[1], qs[2], ks[0], ks[1], ks[2], os[0], os[1], os[2], us[0], us[1], us[2],
@@ -937,12 +945,12 @@ def norm_rotate_grad(q, k, q_gain, k_gain, grad_q, grad_k, rope=None, positions=
     if ok and q is not None:
         gs = grad_q.stride()
         ok = grad_q.shape == q.shape and grad_q.dtype is q.dtype and grad_q.get_device() == device and gs[3] == 1
-        d_q, d_q_gain = torch.empty_like(q), torch.empty_like(q_gain)
+        d_q, d_q_gain = _like(q), torch.empty_like(q_gain)
         os, to_g, to_dq, to_dqg = d_q.stride(), grad_q.data_ptr(), d_q.data_ptr(), d_q_gain.data_ptr()
     if ok and k is not None:
         hs = grad_k.stride()
         ok = grad_k.shape == k.shape and grad_k.dtype is k.dtype and grad_k.get_device() == device and hs[3] == 1
-        d_k, d_k_gain = torch.empty_like(k), torch.empty_like(k_gain)
+        d_k, d_k_gain = _like(k), torch.empty_like(k_gain)
         us, to_h, to_dk, to_dkg = d_k.stride(), grad_k.data_ptr(), d_k.data_ptr(), d_k_gain.data_ptr()
     if not ok:
         raise ValueError("grad_q and grad_k must be like q and k, with neighbouring elements of a head")

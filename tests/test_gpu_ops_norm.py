@@ -122,6 +122,25 @@ def test_rows_of_any_stride_and_alignment(ops, dtype, interleaved):
     assert torch.equal(ops.norm_rotate(one, None, gains[0], None, rope=rope)[0], ops.norm_rotate(one.contiguous(), None, gains[0], None, rope=rope)[0])
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_rows_that_overlap(ops, dtype):
+    """Windows of a longer row, a step of one element apart; and the same head for all.  (Rows that are not aligned have a kernel of their own, which adds the 64 squares up
+    two a lane where the other has 8 or 16: equal within NORM's count of roundings, not bit by bit.)"""
+    g = torch.Generator(device="cuda").manual_seed(30)
+    base = torch.randn(4000, generator=g, device="cuda").to(dtype)
+    rope = ops.rope_table(33, 64)
+    gain, grad = torch.randn(64, generator=g, device="cuda"), torch.randn((2, 33, 3, 64), generator=g, device="cuda").to(dtype)
+    for strides in ((1000, 1, 300, 1), (0, 1, 0, 1), (1, 64, 0, 1), (0, 0, 0, 1)):
+        x = base.as_strided((2, 33, 3, 64), strides)
+        out = ops.norm_rotate(x, None, gain, None, rope=rope)[0]
+        near(out, *ref.norm(x, gain, rope, None, 1e-6, False), "norm")
+        d, _, d_gain, _ = ops.norm_rotate_grad(x, None, gain, None, grad, None, rope=rope)
+        (dx, b), (dg, bg) = ref.norm_grad(x, gain, grad, rope, None, 1e-6, False)
+        near(d, dx, b, "dx")
+        near(d_gain, dg, bg, "d_gain")
+        assert out.stride(3) == 1 == d.stride(3)
+
+
 @pytest.mark.parametrize("dtype", [F32, BF16, F16])
 def test_zero_large_and_odd_rows(ops, dtype):
     q, k, _, gains, grads = inputs(1, 8, 2, 2, 64, dtype, seed=5)
