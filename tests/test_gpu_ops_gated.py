@@ -86,6 +86,32 @@ def test_shapes_strides_and_slices(ops, rows):
         assert torch.equal(v, y)
 
 
+@pytest.mark.parametrize("rows,ff", [(7, 123), (300, 123), (300, 128), (2047, 2051)])
+@pytest.mark.parametrize("size", [1.0, 2.0 ** -14])
+def test_gradients_in_fp16_lie_anywhere(ops, rows, ff, size):
+    """The largest gradient is looked for where the rows are: at odd places, of odd length, the same row for all; what lies between them is not looked at."""
+    x, wg, wu, gy = inputs(rows, ff, 64, F16, seed=20)
+    gy = (gy.float() * size).half()
+    want = ops.gated_feed_forward_grad(x, wg, wu, gy)
+    for v, (w, b) in zip(want, ref.gated_grad(x, wg, wu, gy, "silu")):
+        near(v, w, b, "gradient")
+    for left, right in ((0, 5), (3, 2), (8, 8)):
+        g2 = torch.full((rows, left + ff + right), 60000.0, device="cuda", dtype=F16)
+        g2[:, left:left + ff] = gy
+        for v, y in zip(ops.gated_feed_forward_grad(x, wg, wu, g2[:, left:left + ff]), want):
+            assert torch.equal(v, y)
+    row = gy[:1].expand(rows, ff)
+    for v, y in zip(ops.gated_feed_forward_grad(x, wg, wu, row), ops.gated_feed_forward_grad(x, wg, wu, row.contiguous())):
+        assert torch.equal(v, y)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("rows,ff,d", [(9000, 40, 72), (9001, 130, 128), (20, 20011, 64), (300, 20001, 128), (20001, 4, 8)])
+def test_long_sums_of_few_tiles(ops, dtype, rows, ff, d):
+    """Sums that are cut into many, of either kind of gradient."""
+    check(ops, *inputs(rows, ff, d, dtype, seed=21), "silu")
+
+
 @pytest.mark.parametrize("dtype", [BF16, F16])
 @pytest.mark.parametrize("rows", [5, 280])
 def test_infinities_and_nan_stay_in_their_rows(ops, dtype, rows):

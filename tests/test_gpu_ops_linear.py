@@ -73,6 +73,30 @@ def test_vocabulary_in_pieces(ops, rows, d):
     near(d_weight, want, bound * (rows / 30000 + 1), "d_weight")        # (the accumulator holds all rows' sum while it takes the last of them)
 
 
+@pytest.mark.parametrize("size", [1.0, 2.0 ** -30])
+def test_many_rows_in_fp16(ops, size):
+    """More rows than every CTA looks through for the largest gradient, and a vocabulary in pieces (gradients of one size: the scale is then every row's)."""
+    rows = 70001
+    h, w, t, gl, gs = inputs(rows, 2500, 64, F16, seed=20)
+    w = w * 8
+    gl, gs = 2 * size * gl.sign(), size * gs.sign()
+    r = ops.linear_logprobs(h, w, t)
+    d_hidden, d_weight = ops.linear_logprobs_grad(h, w, t, r, gl, gs)
+    some = torch.cat([torch.arange(300, device="cuda"), torch.arange(rows - 300, rows, device="cuda")])
+    t[:5] = 3
+    (want, bound), _ = ref.linear_grad(h[some[5:]], w, t[some[5:]], 1.0, gl[some[5:]], gs[some[5:]])
+    near(d_hidden[some[5:]], want, bound + want.abs() * 2.0 ** -22, "d_hidden")
+    alone = ops.linear_logprobs_grad(h, w, t, r, gl, gs, need=(False, True))
+    assert alone[0] is None and alone[1].isfinite().all()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("rows,vocab,d", [(9000, 40, 72), (9001, 150, 128), (20, 30011, 64), (300, 60001, 256), (20001, 8, 8)])
+def test_long_sums_of_few_tiles(ops, dtype, rows, vocab, d):
+    """Sums that are cut into many, of either gradient."""
+    check(ops, *inputs(rows, vocab, d, dtype, seed=21))
+
+
 @pytest.mark.parametrize("dtype", [BF16, F16])
 @pytest.mark.parametrize("rows", [4, 260])
 def test_only_some_gradients(ops, dtype, rows):
