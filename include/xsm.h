@@ -378,7 +378,7 @@ XSM_API xsm_status xsm_linear_logprobs(const xsm_linear_logprobs_args *a, void *
 /* The gradient of sum_rows (g_logprob logprob + g_lse lse) by hidden and weight, in their type, from lse of the call above:
  *   dz_rj = ([j = token_r] g_logprob_r - exp(z_rj - lse_r) (g_logprob_r - g_lse_r)) / temperature,  d_hidden = dz . weight,  d_weight = dz^T . hidden.
  * g_logprob counts only where there is a token; rows with an lse of -infinity have none.  The logits are computed again, piece by piece of the vocabulary; dz is
- * rounded to dtype once (fp16: scaled by a power of two that takes its largest possible element to 2^13, and back in the sums).  The workspace holds a
+ * rounded to dtype once (up to 128 rows or 64 tokens: held in two parts of it; fp16: scaled by a power of two that takes its largest possible element to 2^13, and back in the sums).  The workspace holds a
  * piece of dz of at most 256 MiB (1024 tokens at least) and partial sums.  d_hidden or d_weight may be NULL. */
 typedef struct {
     const void *hidden, *weight, *tokens; /* as above */
@@ -407,7 +407,7 @@ typedef struct {
 XSM_API xsm_status xsm_gated_ff(const xsm_gated_ff_args *a, void *cuda_stream);
 
 /* The gradient of sum(g_out * out) by x, w_gate and w_up, in their type.  gate and up are computed again; their gradients g_out up act'(gate) and g_out act(gate) are
- * rounded to dtype once (fp16: scaled by the power of two that takes the largest finite g_out to [1, 2): up act'(gate) beyond 2^15 is infinite, what is below 2^-25 zero).  d_x, or d_w_gate and d_w_up, may be NULL. */
+ * rounded to dtype once (up to 128 rows or 32 columns: held in two parts of it; fp16: scaled by the power of two that takes the largest finite g_out to [1, 2): up act'(gate) beyond 2^15 is infinite, what is below 2^-25 zero).  d_x, or d_w_gate and d_w_up, may be NULL. */
 typedef struct {
     const void *x, *w_gate, *w_up;        /* as above */
     const void *g_out;                    /* DEVICE dtype [rows][ff]; aligned to its elements */

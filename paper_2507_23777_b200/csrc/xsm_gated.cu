@@ -1,7 +1,7 @@
 // The gated feed-forward part of a block: out = act(x . w_gate) * (x . w_up), both projections, the activation and the product in one kernel, and its gradients.
 //
 // A tile's columns are as many of gate as of up, so that both sums of an output lie in the same thread's tensor memory.  Backward: gate and up are computed
-// again and turned into their gradients where the products leave them (gate's and up's, rounded to the operands' type), then
+// again and turned into their gradients where the products leave them (gate's and up's, rounded to the operands' type, of few rows in two parts), then
 // dx = d_gate . w_gate + d_up . w_up is one product over both, d_w_gate = d_gate^T . x and d_w_up = d_up^T . x: one launch for all three.  (Gate and up kept in 16 bits
 // would spare a quarter of the work and double the gradients' error; kept in fp32 they cost as much to move as to compute.)
 //
@@ -17,17 +17,20 @@ struct GatedGradPlan {
     ProductCut cut;
     SumsPlan sums;
     int ld;
+    long long low;
     size_t amax, d_gate, d_up, part, bytes;
 };
 static GatedGradPlan plan_gated_grad(int rows, int ff, int d, bool x, bool w) {
     GatedGradPlan p;
     p.cut = product_cut(PR_GATED_GRAD, rows, ff);
-    p.sums = plan_sums(rows, ff, d, 2, x, w, true);
+    p.sums = plan_sums(rows, ff, d, 2, x, w, true, !p.cut.wide);
     p.ld = (ff + 7) / 8 * 8;
     p.amax = 0;
     p.d_gate = up(kAmaxBlocks * 4);
-    p.d_up = p.d_gate + up((size_t)rows * p.ld * 2);
-    p.part = p.d_up + up((size_t)rows * p.ld * 2);
+    const size_t one = up((size_t)rows * p.ld * 2);
+    p.low = p.cut.wide ? 0 : (long long)one;        // (in elements: behind both)
+    p.d_up = p.d_gate + one;
+    p.part = p.d_up + (p.cut.wide ? 1 : 3) * one;
     p.bytes = p.part + up(p.sums.bytes);
     return p;
 }
@@ -91,7 +94,7 @@ xsm_status xsm_gated_ff_grad(const xsm_gated_ff_grad_args *a, void *cuda_stream)
     ProductArgs A = {};
     A.status = a->status; A.activation = a->activation;
     A.g_y = a->g_out; A.g_y_ld = a->g_out_stride;
-    A.out[0] = ws + p.d_gate; A.out[1] = ws + p.d_up; A.out_ld = p.ld;
+    A.out[0] = ws + p.d_gate; A.out[1] = ws + p.d_up; A.out_ld = p.ld; A.low = p.low;
     cudaError_t e = cudaSuccess;
     if (a->dtype == XSM_F16) {        // fp16 has no numbers below 2^-24: the largest gradient that comes in is taken to 1 and more, which leaves up to 2^15 for up
         A.amax = (const float *)(ws + p.amax);
@@ -100,7 +103,7 @@ xsm_status xsm_gated_ff_grad(const xsm_gated_ff_grad_args *a, void *cuda_stream)
     const Operand x = {a->x, a->rows, a->d, a->x_stride}, w[2] = {{a->w_gate, a->ff, a->d, a->w_gate_stride}, {a->w_up, a->ff, a->d, a->w_up_stride}};
     if (e == cudaSuccess) e = launch_product(PR_GATED_GRAD, a->dtype, p.cut, A, a->rows, a->ff, x, w, st);
     Sums S = {};
-    S.pairs = 2;
+    S.pairs = 2; S.low = p.low;
     S.h = x;
     for (int i = 0; i < 2; ++i) { S.g[i] = {A.out[i], a->rows, a->ff, p.ld}; S.w[i] = w[i]; }
     S.x = a->d_x; S.x_ld = a->d_x_stride;

@@ -3,8 +3,9 @@
 //
 // Forward: z = hidden . weight / T; every tile of 256 (few rows: a CTA's tiles) tokens of the vocabulary gives a row two pairs (maximum, sum of exponentials), which a second
 // kernel joins, or, of few rows, the CTA that ends last: lse = max + log sum.  Backward, in pieces of the vocabulary: the logits once more, p = exp(z - lse),
-// d = ([token] g - p (g - g_lse)) / T rounded to the operands' type, then d_hidden = d . weight and d_weight = d^T . hidden in one launch.  d in 16 bits: that product
-// is two thirds of the work; it doubles the square of the gradients' error (a rounding before the sum next to the one behind it).
+// d = ([token] g - p (g - g_lse)) / T rounded to the operands' type, then d_hidden = d . weight and d_weight = d^T . hidden in one launch.  d in 16 bits: these products
+// are two thirds of the work; it doubles the square of the gradients' error (a rounding before the sum next to the one behind it).  Few rows, where the weights' bytes are the
+// time and single elements of d the gradient, also have what the rounding left.
 //
 // What bounds it.  8192 rows, 32003 tokens, 2048 wide: 3.1 ms for four products of 1.07 TFLOP (three without the logits again), 1.39 PFLOP/s under the power limit, what the
 // library's own product sustains.  4096 x 4096 x 1024: 28 + 76 us, three launches' beginnings and ends in it.  1999 x 5003 x 768: 21 + 46.
@@ -57,21 +58,25 @@ struct LinearGradPlan {
     ProductCut cut_z;
     SumsPlan sums;
     int piece, pieces;
+    long long low;
     size_t amax, dz, part, acc, bytes;      // offsets in the workspace
 };
 static LinearGradPlan plan_linear_grad(int rows, int vocab, int d, bool h, bool w) {
     LinearGradPlan p;
-    long long piece = kPieceBytes / (2ll * rows) / 256 * 256;
+    const int each = product_cut(PR_DLOGITS, rows, vocab).wide ? 2 : 4;
+    long long piece = kPieceBytes / each / rows / 256 * 256;
     if (piece < 1024) piece = 1024;
     p.pieces = (int)((vocab + piece - 1) / piece);
     p.piece = (int)(((vocab + p.pieces - 1) / p.pieces + 255) / 256 * 256);
     if (p.piece > vocab) p.piece = (vocab + 63) / 64 * 64;
     p.pieces = (vocab + p.piece - 1) / p.piece;
     p.cut_z = product_cut(PR_DLOGITS, rows, p.piece);
-    p.sums = plan_sums(rows, p.piece, d, 1, h, w, p.pieces == 1);
+    p.sums = plan_sums(rows, p.piece, d, 1, h, w, p.pieces == 1, !p.cut_z.wide);
     p.amax = 0;
     p.dz = up(kAmaxBlocks * 4);
-    p.part = p.dz + up((size_t)rows * p.piece * 2);
+    const size_t dz = up((size_t)rows * p.piece * 2);
+    p.low = p.cut_z.wide ? 0 : (long long)(dz / 2);
+    p.part = p.dz + (p.cut_z.wide ? 1 : 2) * dz;
     p.acc = p.part + up(p.sums.bytes);
     p.bytes = p.acc + (p.pieces > 1 && h ? up(sums_bytes(p.sums.cut, rows, d)) : 0);
     return p;
@@ -156,9 +161,9 @@ xsm_status xsm_linear_logprobs_grad(const xsm_linear_logprobs_grad_args *a, void
     Z.inv_t = 1.f / a->temperature;
     Z.c = (float)(1.4426950408889634 / a->temperature);
     Z.lse = a->lse; Z.g = a->g_logprob; Z.g_ld = a->g_logprob_stride; Z.g_lse = a->g_lse; Z.g_lse_ld = a->g_lse_stride;
-    Z.out[0] = ws + p.dz; Z.out_ld = p.piece;
+    Z.out[0] = ws + p.dz; Z.out_ld = p.piece; Z.low = p.low;
     Sums S = {};
-    S.pairs = 1;
+    S.pairs = 1; S.low = p.low;
     S.h = {a->hidden, a->rows, a->d, a->hidden_stride};
     S.x = a->d_hidden; S.x_ld = a->d_hidden_stride; S.y_ld = a->d_weight_stride;
     S.x_sums = p.pieces > 1 ? (float *)(ws + p.acc) : nullptr;

@@ -28,9 +28,9 @@ constexpr int kMaxStages = 24;
 // ------------------------------------------------------------------------------------------- instructions
 
 // Descriptor of an operand tile with the 128-byte swizzle.  K-major: rows of 64 elements, groups of 8 rows 1024 bytes apart.  MN-major: rows of
-// 64 elements across the summed axis, groups of 8 steps of it 1024 bytes apart, the next 64 elements a box (8 KB) further.
-__device__ __forceinline__ uint64_t operand_desc(uint32_t addr, bool mn) {
-    return (uint64_t)((addr >> 4) & 0x3FFFu) | ((uint64_t)(mn ? 8192 >> 4 : 1) << 16) | ((uint64_t)(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61);
+// 64 elements across the summed axis, groups of 8 steps of it 1024 bytes apart, the next 64 elements `next` bytes (a box of 8 KB, or two) further.
+__device__ __forceinline__ uint64_t operand_desc(uint32_t addr, bool mn, uint32_t next = 8192) {
+    return (uint64_t)((addr >> 4) & 0x3FFFu) | ((uint64_t)(mn ? next >> 4 : 1) << 16) | ((uint64_t)(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61);
 }
 template <typename T> __device__ __forceinline__ uint32_t product_idesc(int m, int n, bool a_mn, bool b_mn) {
     const uint32_t f = std::is_same<T, bf16>::value ? 1u : 0u;
@@ -160,6 +160,18 @@ template <typename T, int N> __device__ __forceinline__ void store_row(T *row, i
     }
 }
 
+// The same twice: numbers rounded to T, and, `low` elements further, what the rounding left.
+template <typename T, int N> __device__ __forceinline__ void store_both(T *row, long long low, int col, int n, const float (&x)[N]) {
+    store_row(row, col, n, true, x);
+    float rest[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const float r = x[i] - to_f(rounded<T>(x[i]));
+        rest[i] = fabsf(r) < INFINITY ? r : 0.f;
+    }
+    store_row(row + low, col, n, true, rest);
+}
+
 // ----------------------------------------------------------------------------------------------------- tiles
 
 // Tiles in groups of `group_m` tiles of rows; in a group the rows first, then the columns: the tiles that run at a time then share both operands'
@@ -264,7 +276,7 @@ template <typename T> __device__ __forceinline__ void put_row(uint32_t buf, int 
 template <int CG, int BN, int EPI, typename T>
 __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __grid_constant__ ProductMaps M, const __grid_constant__ ProductArgs A) {
     constexpr int TM = 128 * CG;
-    constexpr bool kGated = EPI == PR_GATED || EPI == PR_GATED_GRAD, kOut = EPI == PR_OUT;
+    constexpr bool kGated = EPI == PR_GATED || EPI == PR_GATED_GRAD, kOut = EPI == PR_OUT, kRounds = EPI == PR_STATS && CG == 1;
     extern __shared__ char smem_raw[];
     __shared__ __align__(8) uint64_t full[kMaxStages], empty[kMaxStages], sums_full[2], sums_empty[2], last;
     __shared__ uint32_t tmem_slot;
@@ -321,6 +333,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
             const uint32_t full_at = CG == 2 ? map_rank(full0, 0) : full0;
             int n = 0, s = 0;
             uint32_t par = 1u, sa = ring;
+            const uint32_t a_next = kOut && A.low ? 16384 : 8192;        // (A's rows and what their rounding left come by one copy, one behind the other)
             bool ok = true;
             for (int t = first; ok && t < A.tiles; t += step) {
                 const ProductPart &P = part_of(t);
@@ -344,7 +357,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
                     if (CG == 1 || rank == 0) mbar_arrive_expect_tx(full0 + 8u * (uint32_t)s, tx);
                     if (rows_a) {
                         tma_3d<CG>(sa, ma, m0, at, 0, f);
-                        tma_3d<CG>(sa + 8192, ma, m0 + 64, at, 0, f);
+                        tma_3d<CG>(sa + a_next, ma, m0 + 64, at, 0, f);
                     } else {
                         tma_3d<CG>(sa, ma, at, m0, z, f);
                     }
@@ -372,6 +385,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
             constexpr uint32_t b_step = kOut ? 2048 >> 4 : 32 >> 4;
             const uint64_t db = operand_desc(ring + A.stage_b, kOut);
             const uint32_t stage = A.stage >> 4;
+            const bool low = kOut && A.low != 0;
             bool ok = true;
             int s = 0, acc = 0;
             uint32_t par = 0u, acc_par = 1u, at = 0u;
@@ -380,11 +394,12 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
                 const Tile w = tile_of(P, (unsigned)t);
                 const bool rows_a = kOut && P.rows_a;
                 const uint32_t idesc = product_idesc<T>(128 * CG, kGated && CG == 1 ? BN / 2 : BN, rows_a, kOut), a_step = rows_a ? 2048 >> 4 : 32 >> 4, a_chunk = (uint32_t)P.a_rows * 128 >> 4;
-                const uint64_t da = operand_desc(ring, rows_a);
+                const uint64_t da = operand_desc(ring, rows_a, low ? 16384 : 8192);
+                const uint32_t a_low = (rows_a ? 8192u : (uint32_t)P.a_rows * 128u) >> 4;
                 if (!(ok = wait_warp(sums_empty0 + 8u * (uint32_t)acc, acc_par))) break;
                 tcgen05_after_sync();
-                const uint32_t d = tmem + (uint32_t)(acc * BN);
-                uint32_t add = 0u;
+                uint32_t d = tmem + (uint32_t)(acc * BN), add = 0u;
+                int left = kRounds ? A.round : 0;
                 for (int k = w.k0; k < w.k1; ++k) {
                     if (!(ok = wait_warp(full0 + 8u * (uint32_t)s, par))) break;
                     tcgen05_after_sync();
@@ -400,6 +415,10 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
                             } else {
 #pragma unroll
                                 for (int i = 0; i < 4; ++i) mma_f16<CG>(d, a + i * a_step, b + i * b_step, idesc, i > 0 ? 1u : add);
+                                if (low) {
+#pragma unroll
+                                    for (int i = 0; i < 4; ++i) mma_f16<CG>(d, a + a_low + i * a_step, b + i * b_step, idesc, 1u);
+                                }
                             }
                             if (CG == 2 || kOut || c + 1 == A.chunks) break;
                             a += a_chunk;
@@ -412,6 +431,18 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
                     add = 1u;
                     at += stage;
                     if (++s == A.stages) { s = 0; par ^= 1u; at = 0u; }
+                    if constexpr (kRounds) {
+                        if (--left == 0 && k + 1 < w.k1) {
+                            if (leader) commit<CG>(sums_full0 + 8u * (uint32_t)acc);
+                            __syncwarp();
+                            if (++acc == 2) { acc = 0; acc_par ^= 1u; }
+                            if (!(ok = wait_warp(sums_empty0 + 8u * (uint32_t)acc, acc_par))) break;
+                            tcgen05_after_sync();
+                            d = tmem + (uint32_t)(acc * BN);
+                            add = 0u;
+                            left = A.round;
+                        }
+                    }
                 }
                 if (!ok) break;
                 if (leader) commit<CG>(sums_full0 + 8u * (uint32_t)acc);
@@ -431,6 +462,15 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
         int acc = 0;
         uint32_t acc_par = 0u;
         float mx = -INFINITY, sum = 0.f;        // PR_STATS
+        auto release = [&] {        // the products may have the accumulator again
+            tcgen05_before_sync();
+            __syncwarp();
+            if (lane == 0) {
+                if constexpr (CG == 2) arrive_cluster(map_rank(smem_u32(&sums_empty[acc]), 0));
+                else mbar_arrive(smem_u32(&sums_empty[acc]));
+            }
+            if (++acc == 2) { acc = 0; acc_par ^= 1u; }
+        };
         for (int t = first; t < A.tiles; t += step) {
             const ProductPart &P = part_of(t);
             const Tile w = tile_of(P, (unsigned)t);
@@ -498,8 +538,8 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
                                 for (int i = 0; i < N; i += 2) held[(c + i) / 2] = pack2<T>(y[i], y[i + 1]);
                             } else if (live) {        // (workspace rows of a multiple of eight elements: what lies behind the last column is nobody's)
                                 const int n8 = (int)A.out_ld;
-                                store_row(reinterpret_cast<T *>(A.out[0]) + (long long)row * A.out_ld, col, n8, true, x);
-                                store_row(reinterpret_cast<T *>(A.out[1]) + (long long)row * A.out_ld, col, n8, true, y);
+                                store_both(reinterpret_cast<T *>(A.out[0]) + (long long)row * A.out_ld, A.low, col, n8, x);
+                                store_both(reinterpret_cast<T *>(A.out[1]) + (long long)row * A.out_ld, A.low, col, n8, y);
                             }
                         }
                     }
@@ -615,23 +655,45 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
                             }
 #pragma unroll
                             for (int i = 0; i < 32; ++i) x[i] *= back;
-                            if constexpr (CG == 2) {
-                                if ((c & 1) == 0) rows_free(lane);
-                                put_row<T>(buf, lane, (c & 1) * 4, x);
-                                if ((c & 1) || c + 1 == pieces) rows_store(&M.out[P.map_out + w.job], buf, col - (c & 1) * 32, row0, 0, true, lane);
-                            } else if (live) {
-                                store_row(reinterpret_cast<T *>(P.out[w.job]) + (long long)row * P.out_ld, col, P.n, true, x);
-                            }
+                            if ((c & 1) == 0) rows_free(lane);
+                            put_row<T>(buf, lane, (c & 1) * 4, x);
+                            if ((c & 1) || c + 1 == pieces) rows_store(&M.out[P.map_out + w.job], buf, col - (c & 1) * 32, row0, 0, true, lane);
                         }
                     }
                 } else {
-#pragma unroll 1
+                    // The tensor core cuts its sums off where they are added to: of few rows, where there is time for it, no more than 256 steps are added up there, and these here.
+                    // (13 x 24000 x 1824: lse off by 1.2e-6 of itself otherwise.)
+                    [[maybe_unused]] float z[kRounds ? BN / 2 : 1];
+                    if constexpr (kRounds) {
+                        bool ok = true;
+                        for (int k = w.k0;;) {
+#pragma unroll
+                            for (int c = 0; c < BN / 2; c += N) {
+                                uint32_t v[N];
+                                tmem_ld(v, lanes + (uint32_t)(acc * BN + half * (BN / 2) + c));
+                                tmem_wait_ld();
+#pragma unroll
+                                for (int i = 0; i < N; ++i) z[c + i] = (k > w.k0 ? z[c + i] : 0.f) + __uint_as_float(v[i]);
+                            }
+                            release();
+                            if ((k += A.round) >= w.k1) break;
+                            if (!(ok = wait_warp(sums_full0 + 8u * (uint32_t)acc, acc_par))) break;
+                            tcgen05_after_sync();
+                        }
+                        if (!ok) break;
+                    }
+#pragma unroll(kRounds ? BN / 2 / N : 1)
                     for (int c = 0; c < BN / 2; c += N) {
                         uint32_t v[N];
-                        tmem_ld(v, sums + (uint32_t)(half * (BN / 2) + c));
+                        if constexpr (kRounds) {
+#pragma unroll
+                            for (int i = 0; i < N; ++i) v[i] = __float_as_uint(z[c + i]);
+                        } else {
+                            tmem_ld(v, sums + (uint32_t)(half * (BN / 2) + c));
+                        }
                         const int col = col0 + c;
                         if (CG == 2 && EPI == PR_DLOGITS && (c & 32) == 0) rows_free(lane);
-                        tmem_wait_ld();
+                        if constexpr (!kRounds) tmem_wait_ld();
                         if constexpr (EPI == PR_STATS) {
                             if (col + N > P.n) {
 #pragma unroll
@@ -666,7 +728,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
                                 put_row<T>(buf, lane, (c & 32) / 8, x);
                                 if (c & 32) rows_store(&M.out[0], buf, col - 32, row0, 0, row0 < P.m && col - 32 < P.n, lane);
                             } else if (live) {
-                                store_row(reinterpret_cast<T *>(A.out[0]) + (long long)row * A.out_ld, col, (int)A.out_ld, true, x);
+                                store_both(reinterpret_cast<T *>(A.out[0]) + (long long)row * A.out_ld, A.low, col, (int)A.out_ld, x);
                             }
                         }
                     }
@@ -682,15 +744,9 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
                     }
                 }
             }
-            tcgen05_before_sync();
-            __syncwarp();
-            if (lane == 0) {
-                if constexpr (CG == 2) arrive_cluster(map_rank(smem_u32(&sums_empty[acc]), 0));
-                else mbar_arrive(smem_u32(&sums_empty[acc]));
-            }
-            if (++acc == 2) { acc = 0; acc_par ^= 1u; }
+            if constexpr (!kRounds) release();
         }
-        if (CG == 2 && EPI != PR_STATS && lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+        if ((CG == 2 || kOut) && EPI != PR_STATS && lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
         __syncwarp();
     }
     tcgen05_before_sync();
@@ -829,10 +885,11 @@ static cudaError_t encoder(EncodeTiledFn *fn) {
 }
 
 // Boxes of 64 elements of `box_rows` rows; of `chunks` > 1 neighbouring runs of 64 elements of each row (rows of whole runs), one behind the other.
-static bool operand_map(EncodeTiledFn encode, CUtensorMap *out, const Operand &o, int dtype, int box_rows, int chunks) {
-    cuuint64_t dims[3] = {(cuuint64_t)(chunks > 1 ? 64 : o.row), (cuuint64_t)o.rows, (cuuint64_t)(chunks > 1 ? o.row / 64 : 1)};
-    cuuint64_t strides[2] = {(cuuint64_t)o.ld * 2, chunks > 1 ? 128 : (cuuint64_t)o.ld * 2};
-    cuuint32_t box[3] = {64, (cuuint32_t)box_rows, (cuuint32_t)chunks}, one[3] = {1, 1, 1};
+// low: the boxes of a second matrix, so many elements further, come behind the first's.
+static bool operand_map(EncodeTiledFn encode, CUtensorMap *out, const Operand &o, int dtype, int box_rows, int chunks, long long low = 0) {
+    cuuint64_t dims[3] = {(cuuint64_t)(chunks > 1 ? 64 : o.row), (cuuint64_t)o.rows, (cuuint64_t)(chunks > 1 ? o.row / 64 : low ? 2 : 1)};
+    cuuint64_t strides[2] = {(cuuint64_t)o.ld * 2, chunks > 1 ? 128 : low ? (cuuint64_t)low * 2 : (cuuint64_t)o.ld * 2};
+    cuuint32_t box[3] = {64, (cuuint32_t)box_rows, low ? 2 : (cuuint32_t)chunks}, one[3] = {1, 1, 1};
     return encode(out, dtype == XSM_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, const_cast<void *>(o.p), dims, strides, box, one,
                   CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
@@ -867,7 +924,7 @@ void product_waits(unsigned *tries, int *starve) {
 }
 
 template <int CG, int BN, int EPI, typename T> static cudaError_t start(const ProductMaps &M, const ProductArgs &A, cudaStream_t st) {
-    const int smem = kRingBytes + (CG == 2 ? kEpiWarps * 4096 : kABytes) + 1024;        // (few rows: the tensor cores read 128 rows of A whatever the box brought)
+    const int smem = kRingBytes + (CG == 2 || EPI == PR_OUT ? kEpiWarps * 4096 : kABytes) + 1024;        // (few rows: the tensor cores read 128 rows of A whatever the box brought)
     const void *fn = (const void *)product_kernel<CG, BN, EPI, T>;
     cudaError_t e = open_for(fn, smem);
     if (e != cudaSuccess) return e;
@@ -933,12 +990,12 @@ template <int EPI> static cudaError_t start_cut(const ProductCut &cut, int dtype
     using std::integral_constant;
     if (cut.wide) return go(integral_constant<int, 2>(), integral_constant<int, 256>());
     if constexpr (EPI != PR_OUT) {
-        if (cut.bn == 128) return go(integral_constant<int, 1>(), integral_constant<int, 128>());
+        if (cut.bn == 64) return go(integral_constant<int, 1>(), integral_constant<int, 64>());
     }
     if constexpr (EPI == PR_STATS || EPI == PR_DLOGITS) {
         if (cut.bn == 32) return go(integral_constant<int, 1>(), integral_constant<int, 32>());
     }
-    return go(integral_constant<int, 1>(), integral_constant<int, 64>());
+    return go(integral_constant<int, 1>(), integral_constant<int, 128>());
 }
 
 cudaError_t launch_product(ProductEpi epi, int dtype, ProductCut cut, ProductArgs A, int m, int n, const Operand &a, const Operand (&b)[2], cudaStream_t st) {
@@ -960,6 +1017,7 @@ cudaError_t launch_product(ProductEpi epi, int dtype, ProductCut cut, ProductArg
     A.stage = A.stage_b + (uint32_t)(cut.bn / group * 128 * A.chunks);
     P.stage_tx = group * A.stage;
     A.stages = kRingBytes / (int)A.stage < kMaxStages ? kRingBytes / (int)A.stage : kMaxStages;
+    A.round = 4 / A.chunks;
     product_waits(&A.tries, &A.starve);
     ProductMaps M;
     memset(&M, 0, sizeof M);
@@ -986,44 +1044,49 @@ size_t sums_bytes(const ProductCut &cut, long long rows, long long d) { return (
 // Splits that the last of them adds up itself; more are added up by a kernel of its own.
 constexpr int kJoinedHere = 6;
 
-// Both products' tiles are dealt out in one row, x's first.  Tiles are as wide as the larger product asks for.  Where there are few of them the summed axes are cut: of the splits
-// that leave the CTAs with most to do least, in blocks of 64: a tile costs eight blocks on top (its last products, what is done with its sums), one that is cut sixteen, and for every
-// split that is added up three (one piece of 32 columns: one), or ten and a launch of ten more.
-SumsPlan plan_sums(long long rows, long long cols, long long d, int pairs, bool x, bool y, bool once) {
+// Both products' tiles are dealt out in one row, x's first; where a CTA would have too much to do the summed axes are cut.  Of both widths of tiles and of the splits, those that
+// leave the CTAs with most to do least, in cycles: a block of 64 of the summed axis is 512 of the tensor cores in tiles of 256 x 256 (256 in those of 128 x 128, whose operands
+// take longer to come), twice that in two parts; a tile has its last products and what is done with its sums on top, more where it is cut, and for each split that is added up (a piece
+// of 32 columns at a time), or a launch for all.
+static SumsPlan cut_sums(ProductCut cut, long long rows, long long cols, long long d, int pairs, bool x, bool y, bool once, bool low, double *least) {
     SumsPlan p = {};
-    p.cut = (x && rows > 128 && d > 64) || (y && cols > 128 && d > 64) ? ProductCut{true, 256} : ProductCut{false, 64};
-    const long long slots = product_sms() < 2 ? 1 : p.cut.wide ? product_sms() / 2 : product_sms(), kx = (cols + 63) / 64 * pairs, ky = (rows + 63) / 64;
-    const long long tx = x ? p.cut.tiles(rows, d, false) : 0, ty = y ? p.cut.tiles(cols, d, false) * pairs : 0, per = (p.cut.wide ? 2 : 1) * 8;
+    p.cut = cut;
     p.splits_x = p.splits_y = 1;
-    if (tx + ty < 4 * slots) {
-        static const int tries[] = {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 40, 48, 64, 96, 128};
-        const double each = !p.cut.wide || d <= 32 ? 1 : d <= 64 ? 2 : 3;
-        auto cost = [&](long long k, int s) { return (double)((k + s - 1) / s) + (s == 1 ? 8 : s <= kJoinedHere ? 16 + each * s : 16); };
-        double least = 1e300;
-        for (int sx : tries) {
-            if (sx > 1 && (!x || sx * 4 > kx || (!once && sx > kJoinedHere))) break;
-            for (int sy : tries) {
-                if (sy > 1 && (!y || sy * 4 > ky)) break;
-                if ((sx > 1 && sx <= kJoinedHere ? tx : 0) * per + (sy > 1 && sy <= kJoinedHere ? ty : 0) * per > kSumCounters) continue;
-                const long long nx = tx * sx, all = nx + ty * sy;
-                const double cx = cost(kx, sx), cy = cost(ky, sy);
-                double most = 0;
-                auto of = [&](long long c) {        // what CTA (pair) c has to do: tiles c, c + slots, ...
-                    if (c < 0 || c >= slots || c >= all) return;
-                    const long long mine = (all - 1 - c) / slots + 1, of_x = c < nx ? (nx - 1 - c) / slots + 1 : 0;
-                    const double t = of_x * cx + (mine - of_x) * cy;
-                    if (t > most) most = t;
-                };
-                of(0); of(nx % slots - 1); of(nx % slots); of(all % slots - 1); of(all % slots);
-                most += (sx > kJoinedHere ? 20 : 0) + (sy > kJoinedHere ? 20 : 0);
-                if (most < least - 1e-9) { least = most; p.splits_x = sx; p.splits_y = sy; }
-            }
+    const long long slots = product_sms() < 2 ? 1 : cut.wide ? product_sms() / 2 : product_sms(), kx = (cols + 63) / 64 * pairs, ky = (rows + 63) / 64;
+    const long long tx = x ? cut.tiles(rows, d, false) : 0, ty = y ? cut.tiles(cols, d, false) * pairs : 0, per = (cut.wide ? 2 : 1) * 8;
+    static const int tries[] = {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 40, 48, 64, 96, 128};
+    const double stage = (cut.wide ? 512 : 400) * (low ? cut.wide ? 2 : 1.5 : 1), tile = cut.wide ? 4096 : 2048, each = d <= 32 ? 512 : d <= 64 || !cut.wide ? 1024 : 1536;
+    auto cost = [&](long long k, int s) { return (double)((k + s - 1) / s) * stage + (s == 1 ? tile : s <= kJoinedHere ? 2 * tile + each * s : 2 * tile); };
+    *least = 1e300;
+    for (int sx : tries) {
+        if (sx > 1 && (!x || sx * 4 > kx || tx * (sx - 1) > 2 * slots || (!once && sx > kJoinedHere))) break;
+        for (int sy : tries) {
+            if (sy > 1 && (!y || sy * 4 > ky || ty * (sy - 1) > 2 * slots)) break;
+            if ((sx > 1 && sx <= kJoinedHere ? tx : 0) * per + (sy > 1 && sy <= kJoinedHere ? ty : 0) * per > kSumCounters) continue;
+            const long long nx = tx * sx, all = nx + ty * sy;
+            const double cx = cost(kx, sx), cy = cost(ky, sy);
+            double most = 0;
+            auto of = [&](long long c) {        // what CTA (pair) c has to do: tiles c, c + slots, ...
+                if (c < 0 || c >= slots || c >= all) return;
+                const long long mine = (all - 1 - c) / slots + 1, of_x = c < nx ? (nx - 1 - c) / slots + 1 : 0;
+                const double t = of_x * cx + (mine - of_x) * cy;
+                if (t > most) most = t;
+            };
+            of(0); of(nx % slots - 1); of(nx % slots); of(all % slots - 1); of(all % slots);
+            most += (sx > kJoinedHere ? 10240 : 0) + (sy > kJoinedHere ? 10240 : 0);
+            if (most < *least - 1e-9) { *least = most; p.splits_x = sx; p.splits_y = sy; }
         }
     }
     p.partial_x = 0;
-    p.partial_y = p.splits_x > 1 ? (size_t)tx * p.splits_x * tile_bytes(p.cut) : 0;
-    p.bytes = p.partial_y + (p.splits_y > 1 ? (size_t)ty * p.splits_y * tile_bytes(p.cut) : 0);
+    p.partial_y = p.splits_x > 1 ? (size_t)tx * p.splits_x * tile_bytes(cut) : 0;
+    p.bytes = p.partial_y + (p.splits_y > 1 ? (size_t)ty * p.splits_y * tile_bytes(cut) : 0);
     return p;
+}
+
+SumsPlan plan_sums(long long rows, long long cols, long long d, int pairs, bool x, bool y, bool once, bool low) {
+    double wide, narrow;
+    const SumsPlan p = cut_sums({true, 256}, rows, cols, d, pairs, x, y, once, low, &wide), q = cut_sums({false, 128}, rows, cols, d, pairs, x, y, once, low, &narrow);
+    return wide <= narrow ? p : q;
 }
 
 static cudaError_t launch_join(const ProductCut &cut, int dtype, const ProductPart &P, const ProductArgs &A, cudaStream_t st) {
@@ -1031,7 +1094,7 @@ static cudaError_t launch_join(const ProductCut &cut, int dtype, const ProductPa
     const dim3 grid((unsigned)(blocks < most ? blocks : most));
     if (cut.wide)
         return dtype == XSM_BF16 ? launch_early(join_kernel<2, 256, bf16>, grid, dim3(256), 0, st, P, A.amax, A.amax_to) : launch_early(join_kernel<2, 256, __half>, grid, dim3(256), 0, st, P, A.amax, A.amax_to);
-    return dtype == XSM_BF16 ? launch_early(join_kernel<1, 64, bf16>, grid, dim3(256), 0, st, P, A.amax, A.amax_to) : launch_early(join_kernel<1, 64, __half>, grid, dim3(256), 0, st, P, A.amax, A.amax_to);
+    return dtype == XSM_BF16 ? launch_early(join_kernel<1, 128, bf16>, grid, dim3(256), 0, st, P, A.amax, A.amax_to) : launch_early(join_kernel<1, 128, __half>, grid, dim3(256), 0, st, P, A.amax, A.amax_to);
 }
 
 cudaError_t launch_sums(int dtype, const SumsPlan &p, const Sums &s, cudaStream_t st) {
@@ -1046,8 +1109,10 @@ cudaError_t launch_sums(int dtype, const SumsPlan &p, const Sums &s, cudaStream_
     A.amax = s.amax;
     A.amax_to = s.amax_to;
     A.chunks = 1;
-    A.stage_b = kABytes;
-    A.stage = kABytes + (uint32_t)(p.cut.bn / group * 128);
+    A.low = s.low;
+    const int parts = s.low ? 2 : 1;
+    A.stage_b = (uint32_t)(kABytes * parts);
+    A.stage = A.stage_b + (uint32_t)(p.cut.bn / group * 128);
     A.stages = kRingBytes / (int)A.stage < kMaxStages ? kRingBytes / (int)A.stage : kMaxStages;
     product_waits(&A.tries, &A.starve);
     ProductMaps M;
@@ -1059,15 +1124,15 @@ cudaError_t launch_sums(int dtype, const SumsPlan &p, const Sums &s, cudaStream_
         const int splits = p.splits_x <= (cols + 63) / 64 * s.pairs ? p.splits_x : (cols + 63) / 64 * s.pairs;        // (the last piece of a vocabulary may be short)
         if (!fill_part(X, p.cut, false, rows, d, (cols + 63) / 64, s.pairs, 1, splits, 0)) return cudaErrorInvalidValue;
         X.a_rows = rows >= 128 ? 128 : (rows + 7) / 8 * 8;
-        X.stage_tx = (uint32_t)(group * (X.a_rows * 128 + p.cut.bn / group * 128));
+        X.stage_tx = (uint32_t)(group * (X.a_rows * 128 * parts + p.cut.bn / group * 128));
         X.partial = (float *)(s.partial + p.partial_x);
         X.apart = X.splits > kJoinedHere;
         X.sums = s.x_sums; X.go_on = s.go_on; X.end = s.end;
         X.out[0] = s.x; X.out_ld = s.x_ld;
         for (int i = 0; i < s.pairs; ++i) {
-            ok = ok && operand_map(encode, &M.a[i], s.g[i], dtype, X.a_rows, 1) && operand_map(encode, &M.b[i], s.w[i], dtype, 64, 1);
+            ok = ok && operand_map(encode, &M.a[i], s.g[i], dtype, X.a_rows, 1, s.low) && operand_map(encode, &M.b[i], s.w[i], dtype, 64, 1);
         }
-        if (p.cut.wide) ok = ok && result_map(encode, &M.out[0], s.x, rows, d, s.x_ld, dtype);
+        ok = ok && result_map(encode, &M.out[0], s.x, rows, d, s.x_ld, dtype);
     }
     A.tiles = X.tiles;
     Y.first = 0x7fffffff;
@@ -1081,9 +1146,9 @@ cudaError_t launch_sums(int dtype, const SumsPlan &p, const Sums &s, cudaStream_
         Y.apart = Y.splits > kJoinedHere;
         Y.counters = X.splits > 1 && !X.apart ? (unsigned)(X.by_plane.d * group * 8) : 0;
         for (int i = 0; i < s.pairs; ++i) {
-            ok = ok && operand_map(encode, &M.a[2 + i], s.g[i], dtype, 64, 1);
+            ok = ok && operand_map(encode, &M.a[2 + i], s.g[i], dtype, 64, 1, s.low);
             Y.out[i] = s.y[i];
-            if (p.cut.wide) ok = ok && result_map(encode, &M.out[1 + i], s.y[i], cols, d, s.y_ld, dtype);
+            ok = ok && result_map(encode, &M.out[1 + i], s.y[i], cols, d, s.y_ld, dtype);
         }
         Y.out_ld = s.y_ld;
         ok = ok && operand_map(encode, &M.b[2], s.h, dtype, 64, 1);

@@ -54,6 +54,8 @@ struct ProductArgs {
     int stages;                     // of the ring
     uint32_t stage, stage_b;        // bytes of a CTA's stage, where B begins in it
     int tma_out;                    // wide tiles: results leave by TMA
+    int round;                      // PR_STATS, one CTA a tile: stages after which the sums so far are added up outside the tensor core
+    long long low;                  // elements from a gradient (PR_OUT: from A) to what its rounding left, of few rows; 0: that is let go
     unsigned tries;                 // of a barrier, before a wait gives up
     int starve;                     // fetch nothing (xsm_debug_product_waits)
     int *status;
@@ -132,6 +134,7 @@ struct SumsPlan {
 struct Sums {
     int pairs;
     Operand g[2], w[2], h;
+    long long low;                  // elements from g to what its rounding left, 0: nothing
     void *x, *y[2];
     long long x_ld, y_ld;
     float *x_sums;                  // fp32 sums of x over several launches, NULL: one launch
@@ -142,7 +145,7 @@ struct Sums {
     int amax_to;
     int *status;
 };
-SumsPlan plan_sums(long long rows, long long cols, long long d, int pairs, bool x, bool y, bool once);      // once: x is made in one launch
+SumsPlan plan_sums(long long rows, long long cols, long long d, int pairs, bool x, bool y, bool once, bool low);      // once: x is made in one launch; low: g in two parts
 size_t sums_bytes(const ProductCut &cut, long long rows, long long d);      // of x_sums
 cudaError_t launch_sums(int dtype, const SumsPlan &p, const Sums &s, cudaStream_t st);
 

@@ -10,10 +10,10 @@ from ops_reference import TINY, UNIT
 F32, BF16, F16 = torch.float32, torch.bfloat16, torch.float16
 
 
-def product(a, b):
-    """a b^T in 64 bits, and what a sum of its products on the tensor core may be off."""
-    s = a.abs() @ b.abs().T
-    return a @ b.T, s * (-(-a.shape[1] // 16) + 2) * 2.0 ** -23
+def product(a, b, few=False):
+    """a b^T in 64 bits, and what a sum of its products on the tensor core may be off; few: 256 products there at most, these sums in fp32."""
+    s, steps = a.abs() @ b.abs().T, -(-a.shape[1] // 16)
+    return a @ b.T, s * (min(steps, 16) + steps / 32 + 3 if few else steps + 2) * 2.0 ** -23
 
 
 def near(got, want, bound, what):
@@ -36,9 +36,9 @@ def stored(x, slack, dtype):
 
 # ------------------------------------------------------------------------------------------ log probabilities from hidden states
 
-def linear(hidden, weight, tokens, temperature):
-    """(logprob, lse, z, bound of the first, of the second, of z)"""
-    z, slack = product(hidden.double(), weight.double())
+def linear(hidden, weight, tokens, temperature, few=False):
+    """(logprob, lse, z, bound of the first, of the second, of z); few: rows or tokens that one CTA's tiles are as many as."""
+    z, slack = product(hidden.double(), weight.double(), few)
     z, slack = z / temperature, slack / temperature
     size = torch.where(torch.isfinite(z), z.abs(), 0.0)
     # z log2(e) / T and its difference to the maximum, the exponential, a sum of v of them (by threads, parts and joins: at most v / 64 + 40 one after the other)
@@ -52,8 +52,8 @@ def linear(hidden, weight, tokens, temperature):
     return logprob, lse, z, torch.where(have, slack.gather(1, at)[:, 0] + off_lse + logprob.abs() * 2.0 ** -24, 0.0), off_lse, slack
 
 
-def linear_grad(hidden, weight, tokens, temperature, g, g_lse):
-    """((d_hidden, bound), (d_weight, bound))"""
+def linear_grad(hidden, weight, tokens, temperature, g, g_lse, parts=1):
+    """((d_hidden, bound), (d_weight, bound)); parts: of dtype that the gradients by the logits are held in"""
     dtype = hidden.dtype
     logprob, lse, z, _, off_lse, off_z = linear(hidden, weight, tokens, temperature)
     rows = z.shape[0]
@@ -69,13 +69,14 @@ def linear_grad(hidden, weight, tokens, temperature, g, g_lse):
     slack = dz.abs() * rel.expm1() + 2.0 ** -126 * (g - s).abs()[:, None]
     dz[have.nonzero()[:, 0], tokens[have].long()] += g[have]
     dz, slack = dz / temperature, slack / temperature + dz.abs() / temperature * 2.0 ** -22
-    # once rounded to dtype; fp16 scaled so that the largest possible element is 2^13 at least
+    # rounded to dtype, and with two parts what that left again; fp16 scaled so that the largest possible element is 2^13 at least
     most = float(((2 * g.abs() + s.abs()) / temperature).nan_to_num(0, 0, 0).amax()) if rows else 0.0
     floor = TINY[dtype] * (max(most, 2.0 ** -100) * 2.0 ** -13 if dtype is F16 else 1.0)
-    slack = slack + UNIT[dtype] * (dz.abs() + slack) + floor
+    slack = slack + UNIT[dtype] ** parts * (dz.abs() + slack) + floor
     out = []
     for a, b, bound in ((dz, weight.double().T, slack), (dz.T, hidden.double().T, slack.T)):
         x, more = product(a, b)
+        more = more * (2 if parts > 1 else 1)        # (both parts' products, one after the other)
         out.append((x, stored(x, more + bound @ b.abs().T, dtype)))
     return out
 
@@ -106,7 +107,7 @@ def gated(x, w_gate, w_up, kind):
     return out, stored(out, off_a * up.abs() + (a.abs() + off_a) * off_u + out.abs() * 2.0 ** -22, x.dtype), (gate, up, a, da, off_g, off_u, off_a)
 
 
-def gated_grad(x, w_gate, w_up, grad, kind):
+def gated_grad(x, w_gate, w_up, grad, kind, parts=1):
     dtype = x.dtype
     _, _, (gate, up, a, da, off_g, off_u, off_a) = gated(x, w_gate, w_up, kind)
     gy = grad.double()
@@ -117,13 +118,13 @@ def gated_grad(x, w_gate, w_up, grad, kind):
     fine = gy[torch.isfinite(gy)].abs()
     most = float(fine.max()) if fine.numel() else 0.0
     floor = TINY[dtype] * (max(most, 2.0 ** -100) if dtype is F16 else 1.0)        # (scaled so that the largest is 1 or more)
-    slack_g, slack_u = (s + UNIT[dtype] * (d.abs() + s) + floor for s, d in ((slack_g, d_gate), (slack_u, d_up)))
+    slack_g, slack_u = (s + UNIT[dtype] ** parts * (d.abs() + s) + floor for s, d in ((slack_g, d_gate), (slack_u, d_up)))
     wg, wu, xx = w_gate.double(), w_up.double(), x.double()
     both, off = product(torch.cat([d_gate, d_up], 1), torch.cat([wg, wu], 0).T)
-    out = [(both, stored(both, off + slack_g @ wg.abs() + slack_u @ wu.abs(), dtype))]
+    out = [(both, stored(both, off * parts + slack_g @ wg.abs() + slack_u @ wu.abs(), dtype))]
     for d, s in ((d_gate, slack_g), (d_up, slack_u)):
         v, off = product(d.T, xx.T)
-        out.append((v, stored(v, off + s.T @ xx.abs(), dtype)))
+        out.append((v, stored(v, off * parts + s.T @ xx.abs(), dtype)))
     return out
 
 

@@ -32,7 +32,8 @@ def check(ops, x, wg, wu, gy, kind):
     assert out.dtype is x.dtype and out.is_contiguous()
     near(out, want, bound, "out")
     got = ops.gated_feed_forward_grad(x, wg, wu, gy, kind)
-    for v, (want, bound), what in zip(got, ref.gated_grad(x, wg, wu, gy, kind), ("d_x", "d_w_gate", "d_w_up")):
+    parts = 2 if x.shape[0] <= 128 or wg.shape[0] <= 32 else 1        # (a CTA a tile)
+    for v, (want, bound), what in zip(got, ref.gated_grad(x, wg, wu, gy, kind, parts), ("d_x", "d_w_gate", "d_w_up")):
         assert v.dtype is x.dtype and v.is_contiguous()
         near(v, want, bound, what)
     return out, got
