@@ -11,9 +11,9 @@ F32, BF16, F16 = torch.float32, torch.bfloat16, torch.float16
 
 
 def product(a, b, few=False):
-    """a b^T in 64 bits, and what a sum of its products on the tensor core may be off; few: 256 products there at most, these sums in fp32."""
+    """a b^T in 64 bits, and what a sum of its products on the tensor core may be off; few: 512 products there at most, these sums in fp32."""
     s, steps = a.abs() @ b.abs().T, -(-a.shape[1] // 16)
-    return a @ b.T, s * (min(steps, 16) + steps / 32 + 3 if few else steps + 2) * 2.0 ** -23
+    return a @ b.T, s * (min(steps, 32) + steps / 64 + 3 if few else steps + 2) * 2.0 ** -23
 
 
 def near(got, want, bound, what):
