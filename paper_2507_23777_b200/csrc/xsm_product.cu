@@ -120,17 +120,9 @@ __device__ __forceinline__ float scale_of(const float *amax, int to) {
     return scale_for(m, to);
 }
 
-// The same of what the gradients by a row's logits may be, 2|g| + |g_lse| over T, over all rows: looked for by the eight warps of a finished tile while its products
-// run, infinities and NaN apart.
-__device__ __forceinline__ float scale_of_rows(const ProductArgs &A, int w, int lane) {
+// The same of the largest of 256 threads' numbers, those of the eight warps of a finished tile, which look for it while its products run; left in memory for the kernels behind.
+__device__ __forceinline__ float scale_of_warps(const ProductArgs &A, float m, int w, int lane) {
     __shared__ float most[kEpiWarps];
-    float m = 0.f;
-    const int rows = A.part[0].m;
-#pragma unroll 4
-    for (long long r = w * 32 + lane; r < rows; r += 32 * kEpiWarps) {
-        const float v = (2.f * (A.g ? fabsf(A.g[r * A.g_ld]) : 0.f) + (A.g_lse ? fabsf(A.g_lse[r * A.g_lse_ld]) : 0.f)) * A.inv_t;
-        if (v < INFINITY) m = fmaxf(m, v);
-    }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
     if (lane == 0) most[w] = m;
@@ -139,6 +131,34 @@ __device__ __forceinline__ float scale_of_rows(const ProductArgs &A, int w, int 
     for (int i = 0; i < kEpiWarps; ++i) m = fmaxf(m, most[i]);
     if (blockIdx.x == 0) A.amax_out[w * 32 + lane] = w + lane ? 0.f : m;
     return scale_for(m, A.amax_to);
+}
+// ... of what the gradients by a row's logits may be, 2|g| + |g_lse| over T, over all rows, infinities and NaN apart
+__device__ __forceinline__ float scale_of_rows(const ProductArgs &A, int w, int lane) {
+    float m = 0.f;
+    const int rows = A.part[0].m;
+#pragma unroll 4
+    for (long long r = w * 32 + lane; r < rows; r += 32 * kEpiWarps) {
+        const float v = (2.f * (A.g ? fabsf(A.g[r * A.g_ld]) : 0.f) + (A.g_lse ? fabsf(A.g_lse[r * A.g_lse_ld]) : 0.f)) * A.inv_t;
+        if (v < INFINITY) m = fmaxf(m, v);
+    }
+    return scale_of_warps(A, m, w, lane);
+}
+// ... of the gradients that come in, rows without a gap
+template <typename T> __device__ __forceinline__ float scale_of_grads(const ProductArgs &A, int w, int lane) {
+    float m = 0.f;
+    const int n = A.part[0].m * A.part[0].n;
+    const T *g = reinterpret_cast<const T *>(A.g_y);
+    auto take = [&](float v) { v = fabsf(v); if (v < INFINITY) m = fmaxf(m, v); };
+#pragma unroll 4
+    for (int i = w * 32 + lane; i < n / 8; i += 32 * kEpiWarps) {
+        const uint4 u = reinterpret_cast<const uint4 *>(g)[i];
+        T e[8];
+        memcpy(e, &u, 16);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) take(to_f(e[j]));
+    }
+    if (w * 32 + lane < n % 8) take(to_f(g[n / 8 * 8 + w * 32 + lane]));
+    return scale_of_warps(A, m, w, lane);
 }
 
 template <typename T> __device__ __forceinline__ uint32_t pack2(float a, float b) {
@@ -457,6 +477,9 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
         float scale = scale_of(A.amax, A.amax_to);
         if constexpr (EPI == PR_DLOGITS) {
             if (A.amax_out) scale = scale_of_rows(A, warp - 2, lane);
+        }
+        if constexpr (EPI == PR_GATED_GRAD && std::is_same<T, __half>::value) {
+            if (A.amax_out) scale = scale_of_grads<T>(A, warp - 2, lane);
         }
         const float back = 1.f / scale;
         int acc = 0;

@@ -80,7 +80,7 @@ struct ProductArgs {
     void *out[2];                   // PR_GATED_GRAD: gate's, up's
     long long out_ld;
     const float *amax;              // [kAmaxBlocks], NULL: scale 1
-    float *amax_out;                // PR_DLOGITS: look for it in g and g_lse, and leave it here for the launches behind
+    float *amax_out;                // PR_DLOGITS: look for it in g and g_lse, PR_GATED_GRAD: in g_y, and leave it here for the launches behind
     int amax_to;                    // the largest is scaled to [2^amax_to, 2^(amax_to + 1))
 };
 
