@@ -362,7 +362,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
                 const int second = kOut && w.k0 >= P.kb0, rows_a = kOut && P.rows_a;
                 const uint32_t tx = P.stage_tx;
                 const CUtensorMap *ma = &M.a[kOut ? P.map_a + second + w.job : 0], *mb = &M.b[kOut ? P.map_b + second : kGated && CG == 2 ? rank : 0];
-                // a stage of one block: columns `at`; of several: blocks of 64 columns from z on (operands of whole blocks are described so)
+                // a stage of one block: columns `at`; of several: blocks of 64 columns from z on, what is left of the rows in a stage of its own
                 const bool many = !kOut && CG == 1 && A.chunks > 1;
                 int at = (w.k0 - (second ? P.kb0 : 0)) * 64, z = 0;
                 if (t == first) {
@@ -373,6 +373,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
                 if (many) at = 0;
                 for (int k = w.k0; k < w.k1; ++k) {
                     if (!(ok = wait(empty0 + 8u * (uint32_t)s, par))) break;
+                    if (many && A.tail && k + 1 == w.k1) { ++ma; mb += 2; z = 0; }
                     const uint32_t f = full_at + 8u * (uint32_t)s, sb = sa + A.stage_b;
                     if (CG == 1 || rank == 0) mbar_arrive_expect_tx(full0 + 8u * (uint32_t)s, tx);
                     if (rows_a) {
@@ -386,7 +387,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
                         for (int i = 0; i < BN / CG / 64; ++i) tma_3d<CG>(sb + i * 8192, mb, n0 + 64 * i, at, 0, f);
                     } else {
                         tma_3d<CG>(sb, mb, at, n0, z, f);
-                        if constexpr (kGated && CG == 1) tma_3d<CG>(sb + (uint32_t)A.chunks * (BN / 2 * 128), &M.b[1], at, n0, z, f);
+                        if constexpr (kGated && CG == 1) tma_3d<CG>(sb + (uint32_t)A.chunks * (BN / 2 * 128), mb + 1, at, n0, z, f);
                     }
                     ++n;
                     if (many) z += A.chunks;
@@ -908,10 +909,12 @@ static cudaError_t encoder(EncodeTiledFn *fn) {
     return cudaSuccess;
 }
 
-// Boxes of 64 elements of `box_rows` rows; of `chunks` > 1 neighbouring runs of 64 elements of each row (rows of whole runs), one behind the other.
+// Boxes of 64 elements of `box_rows` rows; of `chunks` > 1 neighbouring runs of 64 elements of each row, one behind the other: of the whole runs, or (rest) of the one that is left, as if
+// there were more.
 // low: the boxes of a second matrix, so many elements further, come behind the first's.
-static bool operand_map(EncodeTiledFn encode, CUtensorMap *out, const Operand &o, int dtype, int box_rows, int chunks, long long low = 0) {
-    cuuint64_t dims[3] = {(cuuint64_t)(chunks > 1 ? 64 : o.row), (cuuint64_t)o.rows, (cuuint64_t)(chunks > 1 ? o.row / 64 : low ? 2 : 1)};
+static bool operand_map(EncodeTiledFn encode, CUtensorMap *out, Operand o, int dtype, int box_rows, int chunks, long long low = 0, bool rest = false) {
+    cuuint64_t dims[3] = {(cuuint64_t)(rest ? o.row % 64 : chunks > 1 ? 64 : o.row), (cuuint64_t)o.rows, (cuuint64_t)(rest ? 1 : chunks > 1 ? o.row / 64 : low ? 2 : 1)};
+    if (rest) o.p = (const char *)o.p + o.row / 64 * 128;
     cuuint64_t strides[2] = {(cuuint64_t)o.ld * 2, chunks > 1 ? 128 : low ? (cuuint64_t)low * 2 : (cuuint64_t)o.ld * 2};
     cuuint32_t box[3] = {64, (cuuint32_t)box_rows, low ? 2 : (cuuint32_t)chunks}, one[3] = {1, 1, 1};
     return encode(out, dtype == XSM_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, const_cast<void *>(o.p), dims, strides, box, one,
@@ -1029,12 +1032,15 @@ cudaError_t launch_product(ProductEpi epi, int dtype, ProductCut cut, ProductArg
     const bool gated = epi == PR_GATED || epi == PR_GATED_GRAD, wide = cut.wide;
     const int group = wide ? 2 : 1, a_rows = m >= 128 ? 128 : (m + 7) / 8 * 8;
     // Few rows: a stage of several blocks, each operand's by one copy, as long as three stages fit; a copy costs the TMA unit some 200 cycles whatever it brings (5 rows x 4096
-    // tokens 9.8 -> 7.8 us).
+    // tokens 9.8 -> 7.8 us).  What is left of rows that are no whole blocks has a stage of its own, which long rows are worth (us: 3 x 11421 of 1552 26.5 -> 21.1, 2 x 1056 of
+    // 1848 13.4 -> 11.4; 8 x 139 of 1312 8.9 -> 7.8; but 3 x 1607 of 840 7.3 -> 7.8, 43 x 5344 of 328 8.4 -> 9.2).
     A.chunks = 1;
-    if (!wide && a.row % 64 == 0)
+    if (!wide && (a.row % 64 == 0 || a.row >= 1024))
         while (A.chunks < 4 && 2 * A.chunks <= a.row / 64 && 2 * A.chunks * (a_rows + cut.bn) * 128 * 3 <= kRingBytes) A.chunks *= 2;
+    A.tail = A.chunks > 1 && a.row % 64 != 0;
     ProductPart &P = A.part[0];
-    if (!fill_part(P, cut, gated, m, n, (a.row + 64 * A.chunks - 1) / (64 * A.chunks), 1, 1, 1, 0)) return cudaErrorInvalidValue;
+    const long long stages = A.chunks > 1 ? (a.row / 64 + A.chunks - 1) / A.chunks + A.tail : (a.row + 63) / 64;
+    if (!fill_part(P, cut, gated, m, n, stages, 1, 1, 1, 0)) return cudaErrorInvalidValue;
     A.tiles = P.tiles;
     P.a_rows = a_rows;
     A.stage_b = (uint32_t)(a_rows * 128 * A.chunks);
@@ -1048,6 +1054,10 @@ cudaError_t launch_product(ProductEpi epi, int dtype, ProductCut cut, ProductArg
     const int b_box = gated ? (wide ? 128 : cut.bn / 2) : cut.bn / group;
     bool ok = operand_map(encode, &M.a[0], a, dtype, a_rows, A.chunks);
     for (int i = 0; i < (gated ? 2 : 1); ++i) ok = ok && operand_map(encode, &M.b[i], b[i], dtype, b_box, A.chunks);
+    if (A.tail) {
+        ok = ok && operand_map(encode, &M.a[1], a, dtype, a_rows, A.chunks, 0, true);
+        for (int i = 0; i < (gated ? 2 : 1); ++i) ok = ok && operand_map(encode, &M.b[2 + i], b[i], dtype, b_box, A.chunks, 0, true);
+    }
     if (wide && epi != PR_STATS) {
         A.tma_out = A.out_ld % 8 == 0 && (uintptr_t)A.out[0] % 16 == 0;
         for (int i = 0; i < (epi == PR_GATED_GRAD ? 2 : 1) && A.tma_out; ++i) ok = ok && result_map(encode, &M.out[i], A.out[i], m, n, A.out_ld, dtype);

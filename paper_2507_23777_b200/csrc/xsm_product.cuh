@@ -45,12 +45,13 @@ struct ProductPart {
     void *out[2];                   // of each job
     long long out_ld;
 };
-struct __align__(64) ProductMaps { CUtensorMap a[4], b[3], out[3]; };
+struct __align__(64) ProductMaps { CUtensorMap a[4], b[4], out[3]; };      // (stages of several blocks: a[1], b[2], b[3] are what is left of the rows)
 
 struct ProductArgs {
     ProductPart part[2];
     int tiles;
     int chunks;                     // blocks of 64 that a stage holds
+    int tail;                       // with several: the last stage holds what is left of the rows behind whole blocks
     int stages;                     // of the ring
     uint32_t stage, stage_b;        // bytes of a CTA's stage, where B begins in it
     int tma_out;                    // wide tiles: results leave by TMA

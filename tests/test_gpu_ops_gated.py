@@ -41,7 +41,7 @@ def check(ops, x, wg, wu, gy, kind):
 
 @pytest.mark.parametrize("dtype,kind", [(BF16, "silu"), (F16, "silu"), (BF16, "gelu"), (F16, "gelu")])
 @pytest.mark.parametrize("rows,ff,d", [(1, 1, 8), (1, 64, 64), (5, 33, 72), (8, 4096, 256), (16, 1000, 768), (33, 250, 512), (96, 2051, 128), (128, 64, 24), (129, 33, 64), (129, 31, 72),
-                                       (200, 64, 1024), (256, 256, 96), (300, 515, 768), (513, 130, 320), (1000, 2000, 1024), (2049, 100, 136)])
+                                       (200, 64, 1024), (256, 256, 96), (300, 515, 768), (513, 130, 320), (1000, 2000, 1024), (2049, 100, 136), (7, 130, 1032), (100, 70, 1272)])
 def test_sizes(ops, dtype, kind, rows, ff, d):
     check(ops, *inputs(rows, ff, d, dtype, seed=rows + ff + d), kind)
 

@@ -46,7 +46,7 @@ def check(ops, h, w, t, gl, gs, temperature=1.0, forward_only=False):
 
 @pytest.mark.parametrize("dtype", [BF16, F16])
 @pytest.mark.parametrize("rows,vocab,d", [(1, 1, 8), (1, 50, 64), (5, 64, 72), (7, 65, 24), (8, 4096, 256), (16, 1000, 768), (33, 257, 512), (96, 20011, 128), (127, 300, 200), (128, 129, 64),
-                                          (129, 256, 64), (129, 65, 72), (200, 64, 1024), (256, 257, 96), (300, 5003, 768), (513, 511, 320), (1000, 2000, 1024), (2049, 100, 136), (2, 300, 4104), (90, 400, 4096)])
+                                          (129, 256, 64), (129, 65, 72), (200, 64, 1024), (256, 257, 96), (300, 5003, 768), (513, 511, 320), (1000, 2000, 1024), (2049, 100, 136), (2, 300, 4104), (90, 400, 4096), (7, 130, 1032), (128, 70, 1272), (31, 5000, 2040)])
 def test_sizes(ops, dtype, rows, vocab, d):
     check(ops, *inputs(rows, vocab, d, dtype, seed=rows + vocab + d))
 
