@@ -864,29 +864,43 @@ __global__ void __launch_bounds__(32) amax_pairs_kernel(const float *g, long lon
     if (threadIdx.x == 0) amax[blockIdx.x] = m;
 }
 
-// Adds up the sums of many splits, which lie as the threads of product_kernel left them: a quad of columns a thread.  (Where the last split adds them up itself, one CTA of a tile
-// reads them all: 24 splits of a tile of 256 x 256 take it 20 us.)
+// Adds up the sums of many splits, which lie as the threads of product_kernel left them: four columns of 32 rows a block, of which every warp takes each eighth split, then the first
+// the warps' sums.  (Where the last split adds them up itself, one CTA of a tile reads them all: 24 splits of a tile of 256 x 256 take it 20 us.  A thread that adds up all splits waits for
+// one batch of them after the other: 40 of them 11 us, so 5.)
 template <int CG, int BN, typename T>
 __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ ProductPart P, const float *amax, int amax_to) {
     constexpr int kPieces = BN / 64, kTile = CG * kEpiWarps * kPieces * 1024;
+    __shared__ float4 sums[7][32];
     chain_go();
     chain_wait();
-    const float back = 1.f / scale_of(amax, amax_to);
-    const long long quads = (long long)P.by_plane.d * P.jobs * (kTile / 4);
-    for (long long i = blockIdx.x * 256ll + threadIdx.x; i < quads; i += gridDim.x * 256ll) {
-        const int at = (int)(i / (kTile / 4)), q = (int)(i - (long long)at * (kTile / 4)), lane = q & 31, four = q >> 5 & 7, piece = (q >> 8) % kPieces, w = (q >> 8) / kPieces % kEpiWarps,
-                  rank = (q >> 8) / (kPieces * kEpiWarps), job = at / (int)P.by_plane.d;
+    const int lane = threadIdx.x & 31, slice = threadIdx.x >> 5;
+    const float back = slice ? 1.f : 1.f / scale_of(amax, amax_to);
+    const int groups = (int)(P.by_plane.d * (unsigned)P.jobs) * (kTile / 128);
+    for (int i = blockIdx.x; i < groups; i += gridDim.x) {
+        const int at = i / (kTile / 128), q = i - at * (kTile / 128), four = q & 7, piece = (q >> 3) % kPieces, w = (q >> 3) / kPieces % kEpiWarps, rank = (q >> 3) / (kPieces * kEpiWarps),
+                  job = at / (int)P.by_plane.d;
         const Tile t = tile_of(P, (unsigned)P.first + (unsigned)(at - job * (int)P.by_plane.d));
         const int row = t.m * 128 * CG + rank * 128 + ((w + 2) & 3) * 32 + lane, col = t.n * BN + (w >> 2) * (BN / 2) + piece * 32 + four * 4;
-        if (row >= P.m || col >= P.n) continue;
-        const float4 *p = reinterpret_cast<const float4 *>(P.partial) + (long long)at * P.splits * (kTile / 4) + q;
+        if (row - lane >= P.m || col >= P.n) continue;        // (the whole block)
+        const float4 *p = reinterpret_cast<const float4 *>(P.partial) + (long long)at * P.splits * (kTile / 4) + q * 32 + lane;
         float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 8
-        for (int k = 0; k < P.splits; ++k) {
+#pragma unroll 4
+        for (int k = slice; k < P.splits; k += 8) {
             const float4 x = __ldcg(p + (long long)k * (kTile / 4));
             s.x += x.x; s.y += x.y; s.z += x.z; s.w += x.w;
         }
-        *reinterpret_cast<uint2 *>(reinterpret_cast<T *>(P.out[job]) + (long long)row * P.out_ld + col) = make_uint2(pack2<T>(s.x * back, s.y * back), pack2<T>(s.z * back, s.w * back));
+        if (slice) sums[slice - 1][lane] = s;
+        __syncthreads();
+        if (slice == 0) {
+#pragma unroll
+            for (int k = 0; k < 7; ++k) {
+                const float4 x = sums[k][lane];
+                s.x += x.x; s.y += x.y; s.z += x.z; s.w += x.w;
+            }
+            if (row < P.m)
+                *reinterpret_cast<uint2 *>(reinterpret_cast<T *>(P.out[job]) + (long long)row * P.out_ld + col) = make_uint2(pack2<T>(s.x * back, s.y * back), pack2<T>(s.z * back, s.w * back));
+        }
+        __syncthreads();
     }
 }
 
@@ -1126,7 +1140,7 @@ SumsPlan plan_sums(long long rows, long long cols, long long d, int pairs, bool 
 }
 
 static cudaError_t launch_join(const ProductCut &cut, int dtype, const ProductPart &P, const ProductArgs &A, cudaStream_t st) {
-    const long long blocks = (long long)P.by_plane.d * P.jobs * (long long)(tile_bytes(cut) / 16 / 256), most = (long long)product_sms() * 8;
+    const long long blocks = (long long)P.by_plane.d * P.jobs * (long long)(tile_bytes(cut) / 512), most = (long long)product_sms() * 8;
     const dim3 grid((unsigned)(blocks < most ? blocks : most));
     if (cut.wide)
         return dtype == XSM_BF16 ? launch_early(join_kernel<2, 256, bf16>, grid, dim3(256), 0, st, P, A.amax, A.amax_to) : launch_early(join_kernel<2, 256, __half>, grid, dim3(256), 0, st, P, A.amax, A.amax_to);
