@@ -1132,7 +1132,7 @@ static SumsPlan cut_sums(ProductCut cut, long long rows, long long cols, long lo
 }
 
 // (us, in tiles of 256 and of 128: gradients of a loss over 96 rows of 131071 tokens, 1024 wide, 245 and 214; 5 x 11436 x 80 18 and 16; gated, 1125 x 2259 x 1296 62 and 72; 1162 x 2899 x 600
-// 49 and 61; of 43 drawn cases the rule takes the slower one in 2, by 1 and 3 %.)
+// 49 and 61; of 43 drawn cases the rule takes the slower one in 2, by 1 and 3 %.  300 or 550 cycles a narrow block: 1.8 and 0.4 % slower over 50.)
 SumsPlan plan_sums(long long rows, long long cols, long long d, int pairs, bool x, bool y, bool once, bool low) {
     double wide, narrow;
     const SumsPlan p = cut_sums({true, 256}, rows, cols, d, pairs, x, y, once, low, &wide), q = cut_sums({false, 128}, rows, cols, d, pairs, x, y, once, low, &narrow);
