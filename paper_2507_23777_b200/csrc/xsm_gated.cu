@@ -24,15 +24,16 @@ struct GatedGradPlan {
 };
 static GatedGradPlan plan_gated_grad(int rows, int ff, int d, bool x, bool w) {
     GatedGradPlan p;
-    p.cut = product_cut(PR_GATED_GRAD, rows, ff);
-    p.sums = plan_sums(rows, ff, d, 2, x, w, true, !p.cut.wide);
+    const bool few = product_few(PR_GATED_GRAD, rows, ff);
+    p.cut = product_cut(PR_GATED_GRAD, rows, ff, d);
+    p.sums = plan_sums(rows, ff, d, 2, x, w, true, few);
     p.ld = (ff + 7) / 8 * 8;
     p.amax = 0;
     p.d_gate = up(kAmaxBlocks * 4);
     const size_t one = up((size_t)rows * p.ld * 2);
-    p.low = p.cut.wide ? 0 : (long long)one;        // (in elements: behind both)
+    p.low = few ? (long long)one : 0;        // (in elements: behind both)
     p.d_up = p.d_gate + one;
-    p.part = p.d_up + (p.cut.wide ? 1 : 3) * one;
+    p.part = p.d_up + (few ? 3 : 1) * one;
     p.bytes = p.part + up(p.sums.bytes);
     return p;
 }
@@ -62,7 +63,7 @@ xsm_status xsm_gated_ff(const xsm_gated_ff_args *a, void *cuda_stream) {
     A.status = a->status; A.activation = a->activation;
     A.out[0] = a->out; A.out_ld = a->out_stride;
     const Operand x = {a->x, a->rows, a->d, a->x_stride}, w[2] = {{a->w_gate, a->ff, a->d, a->w_gate_stride}, {a->w_up, a->ff, a->d, a->w_up_stride}};
-    return launched(launch_product(PR_GATED, a->dtype, product_cut(PR_GATED, a->rows, a->ff), A, a->rows, a->ff, x, w, (cudaStream_t)cuda_stream));
+    return launched(launch_product(PR_GATED, a->dtype, product_cut(PR_GATED, a->rows, a->ff, a->d), A, a->rows, a->ff, x, w, (cudaStream_t)cuda_stream));
 }
 
 size_t xsm_gated_ff_grad_workspace(int rows, int ff, int d) {

@@ -43,9 +43,9 @@ __global__ void __launch_bounds__(256) join_stats_kernel(const float2 *parts, co
 
 // One tile of rows: a CTA joins what its tiles find in its registers, and there are two parts for each CTA.
 struct LinearPlan { ProductCut cut; bool carry; int parts; };
-static LinearPlan plan_linear(int rows, int vocab) {
+static LinearPlan plan_linear(int rows, int vocab, int d) {
     LinearPlan p;
-    p.cut = product_cut(PR_STATS, rows, vocab);
+    p.cut = product_cut(PR_STATS, rows, vocab, d);
     p.carry = rows <= p.cut.tm();
     const long long tiles = p.cut.tiles(p.cut.tm(), vocab, false);
     p.parts = 2 * (p.carry ? product_ctas(tiles, p.cut.wide) / (p.cut.wide ? 2 : 1) : (int)tiles);
@@ -63,20 +63,21 @@ struct LinearGradPlan {
 };
 static LinearGradPlan plan_linear_grad(int rows, int vocab, int d, bool h, bool w) {
     LinearGradPlan p;
-    const int each = product_cut(PR_DLOGITS, rows, vocab).wide ? 2 : 4;
+    const bool few = product_few(PR_DLOGITS, rows, vocab);
+    const int each = few ? 4 : 2;
     long long piece = kPieceBytes / each / rows / 256 * 256;
     if (piece < 1024) piece = 1024;
     p.pieces = (int)((vocab + piece - 1) / piece);
     p.piece = (int)(((vocab + p.pieces - 1) / p.pieces + 255) / 256 * 256);
     if (p.piece > vocab) p.piece = (vocab + 63) / 64 * 64;
     p.pieces = (vocab + p.piece - 1) / p.piece;
-    p.cut_z = product_cut(PR_DLOGITS, rows, p.piece);
-    p.sums = plan_sums(rows, p.piece, d, 1, h, w, p.pieces == 1, !p.cut_z.wide);
+    p.cut_z = product_cut(PR_DLOGITS, rows, p.piece, d);
+    p.sums = plan_sums(rows, p.piece, d, 1, h, w, p.pieces == 1, few);
     p.amax = 0;
     p.dz = up(kAmaxBlocks * 4);
     const size_t dz = up((size_t)rows * p.piece * 2);
-    p.low = p.cut_z.wide ? 0 : (long long)(dz / 2);
-    p.part = p.dz + (p.cut_z.wide ? 1 : 2) * dz;
+    p.low = few ? (long long)(dz / 2) : 0;
+    p.part = p.dz + (few ? 2 : 1) * dz;
     p.acc = p.part + up(p.sums.bytes);
     p.bytes = p.acc + (p.pieces > 1 && h ? up(sums_bytes(p.sums.cut, rows, d)) : 0);
     return p;
@@ -97,9 +98,8 @@ static bool rows_fit(const void *p, int64_t ld, int d) { return (uintptr_t)p % 1
 using namespace xsm;
 
 size_t xsm_linear_logprobs_workspace(int rows, int vocab, int d) {
-    (void)d;
-    if (rows < 1 || vocab < 1 || rows > kMostRows || vocab > kMostRows) return 0;
-    return up((size_t)plan_linear(rows, vocab).parts * rows * 8) + up((size_t)rows * 4);
+    if (rows < 1 || vocab < 1 || d < 1 || rows > kMostRows || vocab > kMostRows || d > kMostRows) return 0;
+    return up((size_t)plan_linear(rows, vocab, d).parts * rows * 8) + up((size_t)rows * 4);
 }
 
 xsm_status xsm_linear_logprobs(const xsm_linear_logprobs_args *a, void *cuda_stream) {
@@ -112,7 +112,7 @@ xsm_status xsm_linear_logprobs(const xsm_linear_logprobs_args *a, void *cuda_str
     if ((uintptr_t)a->tokens % a->token_bytes || ((uintptr_t)a->logprob | (uintptr_t)a->lse | (uintptr_t)a->status | (uintptr_t)a->counters) % 4 || (uintptr_t)a->workspace % 16)
         return op_failed(XSM_ERR_INVALID_ARG, "tokens, logprob, lse, status and counters must be aligned to their elements, workspace to 16 bytes");
     if (a->workspace_bytes < (int64_t)xsm_linear_logprobs_workspace(a->rows, a->vocab, a->d)) return op_failed(XSM_ERR_CAPACITY, "the workspace is too small");
-    const LinearPlan p = plan_linear(a->rows, a->vocab);
+    const LinearPlan p = plan_linear(a->rows, a->vocab, a->d);
     ProductArgs A = {};
     A.status = a->status;
     A.tokens = a->tokens; A.token_ld = a->token_stride; A.token_bytes = a->token_bytes; A.vocab = a->vocab;

@@ -180,9 +180,10 @@ template <typename T, int N> __device__ __forceinline__ void store_row(T *row, i
     }
 }
 
-// The same twice: numbers rounded to T, and, `low` elements further, what the rounding left.
+// The same twice: numbers rounded to T, and, `low` elements further (0: not), what the rounding left.
 template <typename T, int N> __device__ __forceinline__ void store_both(T *row, long long low, int col, int n, const float (&x)[N]) {
     store_row(row, col, n, true, x);
+    if (low == 0) return;
     float rest[N];
 #pragma unroll
     for (int i = 0; i < N; ++i) {
@@ -510,6 +511,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
             if constexpr (EPI == PR_GATED || EPI == PR_GATED_GRAD) {
                 constexpr int N = BN / 4 < 32 ? BN / 4 : 32;
                 const int col0 = w.n * (BN / 2) + half * (BN / 4);
+                [[maybe_unused]] const bool whole = EPI == PR_GATED_GRAD && (A.g_y_ld & 7) == 0 && ((uintptr_t)A.g_y & 15) == 0;
                 if constexpr (CG == 2 && EPI == PR_GATED) rows_free(lane);
                 if constexpr (CG == 2 && EPI == PR_GATED_GRAD) rows_landed();
                 uint32_t held[CG == 2 && EPI == PR_GATED_GRAD ? BN / 8 : 1];        // up's gradients, packed, until the buffer is free again
@@ -533,8 +535,19 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
                                 }
                             } else {
                                 const T *gy = reinterpret_cast<const T *>(A.g_y) + (long long)row * A.g_y_ld;
+                                if (live && whole && col + N <= P.n) {
 #pragma unroll
-                                for (int i = 0; i < N; ++i) x[i] = live && col + i < P.n ? to_f(gy[col + i]) * scale : 0.f;
+                                    for (int i = 0; i < N; i += 8) {
+                                        const uint4 u = *reinterpret_cast<const uint4 *>(gy + col + i);
+                                        T e[8];
+                                        memcpy(e, &u, 16);
+#pragma unroll
+                                        for (int j = 0; j < 8; ++j) x[i + j] = to_f(e[j]) * scale;
+                                    }
+                                } else {
+#pragma unroll
+                                    for (int i = 0; i < N; ++i) x[i] = live && col + i < P.n ? to_f(gy[col + i]) * scale : 0.f;
+                                }
                             }
                         }
                         tmem_wait_ld();
@@ -984,17 +997,23 @@ template <int CG, int BN, int EPI, typename T> static cudaError_t start(const Pr
     cfg.numAttrs = CG == 2 ? 2 : 1;
     return cudaLaunchKernelEx(&cfg, product_kernel<CG, BN, EPI, T>, M, A);
 }
-// Rows of more than one tile of 128 take two CTAs a tile.  Few rows: what a CTA fetches decides, its tiles times the rows of both operands; of the widths that fetch
-// least, the widest.  (96 rows x 131071 tokens: 64 columns 83 us, 128 49; 5 rows x 4096: 64 columns 10.6, 32 9.8, before stages of several blocks.)
-ProductCut product_cut(ProductEpi epi, long long m, long long n) {
-    const bool gated = epi == PR_GATED || epi == PR_GATED_GRAD;
-    if (m > 128 && n > (gated ? 32 : 64)) return {true, 256};
-    ProductCut best = {false, 128};
-    double least = 1e300;
+bool product_few(ProductEpi epi, long long m, long long n) { return m <= 128 || n <= (epi == PR_GATED || epi == PR_GATED_GRAD ? 32 : 64); }
+
+// Few rows or columns: what a CTA fetches decides, its tiles times the rows of both operands; of the widths that fetch least, the widest.  (96 rows x 131071 tokens: 64 columns 83 us,
+// 128 49; 5 rows x 4096: 64 columns 10.6, 32 9.8, before stages of several blocks.)  Otherwise two CTAs a tile, but where there are too few such tiles for all of them: of what the rounds of
+// tiles take, in cycles, the least: a block of 64 is 512 of the tensor cores, or what its operands' bytes are from the L2 (64 a cycle and CTA), a tile has its last products and what is done
+// with its sums on top, more where outputs of odd length leave number by number.  (us, forward + gradient: loss 195 x 684 of 344 10.8 + 16.0 -> 7.3 + 12.0, 161 x 131 of 1472 14.0 + 18.5 ->
+// 9.3 + 12.4, 1697 x 332 of 1952 17.1 + 28.9 -> 12.2 + 22.9; gated 486 x 532 of 1080 12.9 + 26.8 -> 12.4 + 23.4; 665 x 111 of 392 8.4 + 16.7 -> 9.3 + 14.0, whose forward stays wide.)
+ProductCut product_cut(ProductEpi epi, long long m, long long n, long long d) {
+    const bool gated = epi == PR_GATED || epi == PR_GATED_GRAD, few = product_few(epi, m, n);
+    const long long sms = product_sms() < 2 ? 2 : product_sms(), blocks = (d + 63) / 64;
+    const int odd = epi == PR_GATED && n % 8 ? 6144 : 0;
+    ProductCut best = {!few, few ? 128 : 256};
+    double least = few ? 1e300 : (double)((best.tiles(m, n, gated) + sms / 2 - 1) / (sms / 2)) * (double)(blocks * 512 + 4096);
     for (int bn = 128; bn >= (gated ? 64 : 32); bn /= 2) {
         const ProductCut c = {false, bn};
-        const long long sms = product_sms() < 1 ? 1 : product_sms();
-        const double cost = (double)((c.tiles(m, n, gated) + sms - 1) / sms) * (double)((m < 128 ? m : 128) + bn);
+        const double rounds = (double)((c.tiles(m, n, gated) + sms - 1) / sms);
+        const double cost = few ? rounds * (double)((m < 128 ? m : 128) + bn) : rounds * (double)(blocks * (256 + 2 * bn) + 1024 + 16 * bn + odd);
         if (cost < least) { least = cost; best = c; }
     }
     return best;

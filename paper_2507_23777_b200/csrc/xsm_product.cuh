@@ -115,8 +115,10 @@ struct ProductCut {
     int tn(bool gated) const { return gated ? bn / 2 : bn; }
     long long tiles(long long m, long long n, bool gated) const { return ((m + tm() - 1) / tm()) * ((n + tn(gated) - 1) / tn(gated)); }
 };
-// out [m][n]; epi: what is done with it (not PR_OUT: plan_sums)
-ProductCut product_cut(ProductEpi epi, long long m, long long n);
+// few rows, or few columns: gradients by logits, gate and up are held in two parts
+bool product_few(ProductEpi epi, long long m, long long n);
+// out [m][n] over rows of d; epi: what is done with it (not PR_OUT: plan_sums)
+ProductCut product_cut(ProductEpi epi, long long m, long long n, long long d);
 
 // An operand in memory: `rows` rows of `row` elements, ld elements apart.
 struct Operand { const void *p; long long rows, row, ld; };
