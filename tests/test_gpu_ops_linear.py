@@ -306,6 +306,37 @@ def test_offsets_beyond_32_bits(ops):
         near(r.logprob[:3], z.gather(1, t[:3, None])[:, 0] - want, torch.full_like(want, 2 * bound), "logprob")
 
 
+@pytest.mark.parametrize("rows", [3, 130])
+def test_gradients_beyond_32_bits(ops, rows):
+    """The last rows of a weight gradient of 2^31 elements and more, and the gradient by hidden, to which they add."""
+    d, vocab, last = 8192, 270_001, 40
+    g = torch.Generator(device="cuda").manual_seed(22)
+    w = torch.empty((vocab, d), dtype=BF16, device="cuda").normal_(0.0, 0.02, generator=g)
+    h = torch.randn((rows, d), generator=g, device="cuda").to(BF16)
+    t = torch.randint(vocab - last, vocab, (rows,), generator=g, device="cuda")
+    gl, gs = (torch.randn(rows, generator=g, device="cuda") for _ in range(2))
+    r = ops.linear_logprobs(h, w, t)
+    d_hidden, d_weight = ops.linear_logprobs_grad(h, w, t, r, gl, gs)
+    tail = w[-last:].double()
+    dz = -torch.exp(h.double() @ tail.T - r.lse.double()[:, None]) * (gl - gs).double()[:, None]
+    dz[torch.arange(rows, device="cuda"), t - (vocab - last)] += gl.double()
+    want = dz.T @ h.double()
+    size = dz.abs().T @ h.double().abs()
+    # the middle part's rounding, the exponent's error (512 sums cut off, sizes to 20), the result's rounding
+    near(d_weight[-last:], want, size * (2.0 ** -8 + 2.0 ** -9) + want.abs() * 2.0 ** -8 + 1e-30, "d_weight")
+    dh = torch.zeros((3, d), dtype=torch.float64, device="cuda")
+    size = torch.zeros_like(dh)
+    for a in range(0, vocab, 20000):
+        x = w[a:a + 20000].double()
+        p = -torch.exp(h[:3].double() @ x.T - r.lse[:3].double()[:, None]) * (gl - gs)[:3].double()[:, None]
+        at = t[:3] - a
+        here = (at >= 0) & (at < x.shape[0])
+        p[here.nonzero()[:, 0], at[here]] += gl[:3][here].double()
+        dh += p @ x
+        size += p.abs() @ x.abs()
+    near(d_hidden[:3], dh, size * (2.0 ** -8 + 2.0 ** -9) + dh.abs() * 2.0 ** -8, "d_hidden")
+
+
 @pytest.mark.parametrize("rows", [5, 300])
 def test_a_wait_that_runs_out_is_told(ops, rows):
     h, w, t, gl, gs = inputs(rows, 500, 256, BF16, seed=13)
