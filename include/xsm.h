@@ -378,7 +378,9 @@ XSM_API xsm_status xsm_linear_logprobs(const xsm_linear_logprobs_args *a, void *
 /* The gradient of sum_rows (g_logprob logprob + g_lse lse) by hidden and weight, in their type, from lse of the call above:
  *   dz_rj = ([j = token_r] g_logprob_r - exp(z_rj - lse_r) (g_logprob_r - g_lse_r)) / temperature,  d_hidden = dz . weight,  d_weight = dz^T . hidden.
  * g_logprob counts only where there is a token; rows with an lse of -infinity have none.  The logits are computed again, piece by piece of the vocabulary; dz is
- * rounded to dtype once (up to 128 rows or 64 tokens: held in two parts of it; fp16: scaled by a power of two that takes its largest possible element to 2^13, and back in the sums).  The workspace holds a
+ * rounded to dtype once (up to 128 rows or 64 tokens: held in two parts of it; fp16: scaled by
+ * a power of two that takes its largest possible element to 2^13, rows whose elements are below 2^-12 of that by up to 2^14 more, and back in the sums; g_logprob of rows without a token
+ * does not count, nor what rows with an lse of -infinity have).  The workspace holds a
  * piece of dz of at most 256 MiB (1024 tokens at least) and partial sums.  d_hidden or d_weight may be NULL. */
 typedef struct {
     const void *hidden, *weight, *tokens; /* as above */

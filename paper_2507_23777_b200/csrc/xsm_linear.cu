@@ -16,7 +16,7 @@
 namespace xsm {
 
 constexpr long long kPieceBytes = 256ll << 20;      // of a piece's gradients by the logits
-constexpr int kRowsLookedThrough = 65536;           // so many rows every CTA looks through for the largest gradient
+constexpr int kRowsLookedThrough = 8192;            // so many rows every CTA looks through for the largest gradient, beside its first products
 
 // Eight rows a block; thread (row, y) joins parts y, y + 32, ...  (32 rows a block, eight threads a row: 145 us for 96 rows of 4096 parts.)
 __global__ void __launch_bounds__(256) join_stats_kernel(const float2 *parts, const float *token_z, const void *tokens, long long token_ld, int token_bytes, int rows, int vocab,
@@ -59,7 +59,7 @@ struct LinearGradPlan {
     SumsPlan sums;
     int piece, pieces;
     long long low;
-    size_t amax, dz, part, acc, bytes;      // offsets in the workspace
+    size_t amax, all, scale, hidden, dz, part, acc, bytes;      // offsets in the workspace
 };
 static LinearGradPlan plan_linear_grad(int rows, int vocab, int d, bool h, bool w) {
     LinearGradPlan p;
@@ -74,7 +74,10 @@ static LinearGradPlan plan_linear_grad(int rows, int vocab, int d, bool h, bool 
     p.cut_z = product_cut(PR_DLOGITS, rows, p.piece, d);
     p.sums = plan_sums(rows, p.piece, d, 1, h, w, p.pieces == 1, few);
     p.amax = 0;
-    p.dz = up(kAmaxBlocks * 4);
+    p.all = up(kAmaxBlocks * 4);
+    p.scale = p.all + 256;
+    p.hidden = p.scale + up((size_t)rows * 4);
+    p.dz = p.hidden + (w ? up((size_t)rows * d * 2) : 0);
     const size_t dz = up((size_t)rows * p.piece * 2);
     p.low = few ? (long long)(dz / 2) : 0;
     p.part = p.dz + (few ? 2 : 1) * dz;
@@ -164,27 +167,33 @@ xsm_status xsm_linear_logprobs_grad(const xsm_linear_logprobs_grad_args *a, void
     Z.out[0] = ws + p.dz; Z.out_ld = p.piece; Z.low = p.low;
     Sums S = {};
     S.pairs = 1; S.low = p.low;
-    S.h = {a->hidden, a->rows, a->d, a->hidden_stride};
+    const Operand hidden = {a->hidden, a->rows, a->d, a->hidden_stride};
+    S.h = hidden;
     S.x = a->d_hidden; S.x_ld = a->d_hidden_stride; S.y_ld = a->d_weight_stride;
     S.x_sums = p.pieces > 1 ? (float *)(ws + p.acc) : nullptr;
     S.partial = ws + p.part;
     S.counters = a->counters; S.status = a->status;
     cudaError_t e = cudaSuccess;
-    if (a->dtype == XSM_F16) {        // fp16 has no numbers below 2^-24: the largest gradient by a logit is taken to 2^13 and more
-        S.amax = (const float *)(ws + p.amax);
-        S.amax_to = Z.amax_to = 13;
-        if (a->rows <= kRowsLookedThrough) {
-            Z.amax_out = (float *)(ws + p.amax);
-        } else {
-            Z.amax = S.amax;
-            e = launch_amax_pairs(Z.g, Z.g_ld, Z.g_lse, Z.g_lse_ld, a->rows, Z.inv_t, (float *)(ws + p.amax), st);
+    if (a->dtype == XSM_F16) {        // fp16 has no numbers below 2^-24: a row's largest possible gradient by a logit is taken to 2^13 and more
+        Z.amax_to = 13;
+        S.row_scale = Z.row_scale = (float *)(ws + p.scale);
+        S.all_scale = Z.all_scale = (float *)(ws + p.all);
+        if (a->d_weight) {
+            Z.h = a->hidden; Z.h_ld = a->hidden_stride; Z.h_out = ws + p.hidden; Z.h_out_ld = Z.d = a->d;
+            S.h = {ws + p.hidden, a->rows, a->d, a->d};
+        }
+        Z.look = a->rows <= kRowsLookedThrough;
+        if (!Z.look) {
+            Z.amax = (const float *)(ws + p.amax);
+            e = launch_amax_losses(Z, a->rows, (float *)(ws + p.amax), st);
         }
     }
     for (int i = 0; i < p.pieces && e == cudaSuccess; ++i) {
         const int v0 = i * p.piece, v = a->vocab - v0 < p.piece ? a->vocab - v0 : p.piece;
         const Operand w[2] = {{(const char *)a->weight + (long long)v0 * a->weight_stride * 2, v, a->d, a->weight_stride}, {}};
         Z.vocab0 = v0;
-        e = launch_product(PR_DLOGITS, a->dtype, p.cut_z, Z, a->rows, v, S.h, w, st);
+        e = launch_product(PR_DLOGITS, a->dtype, p.cut_z, Z, a->rows, v, hidden, w, st);
+        Z.h_out = nullptr;        // (the first one's stay)
         S.g[0] = {ws + p.dz, a->rows, v, p.piece};
         S.w[0] = w[0];
         S.y[0] = a->d_weight ? (char *)a->d_weight + (long long)v0 * a->d_weight_stride * 2 : nullptr;

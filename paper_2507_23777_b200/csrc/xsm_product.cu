@@ -121,7 +121,7 @@ __device__ __forceinline__ float scale_of(const float *amax, int to) {
 }
 
 // The same of the largest of 256 threads' numbers, those of the eight warps of a finished tile, which look for it while its products run; left in memory for the kernels behind.
-__device__ __forceinline__ float scale_of_warps(const ProductArgs &A, float m, int w, int lane) {
+template <int EPI> __device__ __forceinline__ float scale_of_warps(const ProductArgs &A, float m, int w, int lane) {
     __shared__ float most[kEpiWarps];
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
@@ -129,20 +129,28 @@ __device__ __forceinline__ float scale_of_warps(const ProductArgs &A, float m, i
     bar_sync<32 * kEpiWarps>(1);
 #pragma unroll
     for (int i = 0; i < kEpiWarps; ++i) m = fmaxf(m, most[i]);
-    if (blockIdx.x == 0) A.amax_out[w * 32 + lane] = w + lane ? 0.f : m;
+    if (EPI == PR_GATED_GRAD && blockIdx.x == 0) A.amax_out[w * 32 + lane] = w + lane ? 0.f : m;
     return scale_for(m, A.amax_to);
 }
-// ... of what the gradients by a row's logits may be, 2|g| + |g_lse| over T, over all rows, infinities and NaN apart
+// What the gradients by a row's logits may be: 2|g| + |g_lse| over T, g where there is a token, both where there is an lse; infinities and NaN: nothing.
+__device__ __forceinline__ float row_bound(const ProductArgs &A, long long r) {
+    const long long t = A.token_bytes == 8 ? reinterpret_cast<const long long *>(A.tokens)[r * A.token_ld] : (long long)reinterpret_cast<const int *>(A.tokens)[r * A.token_ld];
+    const float lse = A.lse[r], g = A.g ? A.g[r * A.g_ld] : 0.f, h = A.g_lse ? A.g_lse[r * A.g_lse_ld] : 0.f;
+    const float v = (2.f * (t >= 0 && t < A.vocab ? fabsf(g) : 0.f) + fabsf(h)) * A.inv_t;
+    return lse > -INFINITY && v < INFINITY ? v : 0.f;
+}
+// ... of all rows' bounds
 __device__ __forceinline__ float scale_of_rows(const ProductArgs &A, int w, int lane) {
     float m = 0.f;
     const int rows = A.part[0].m;
 #pragma unroll 4
-    for (long long r = w * 32 + lane; r < rows; r += 32 * kEpiWarps) {
-        const float v = (2.f * (A.g ? fabsf(A.g[r * A.g_ld]) : 0.f) + (A.g_lse ? fabsf(A.g_lse[r * A.g_lse_ld]) : 0.f)) * A.inv_t;
-        if (v < INFINITY) m = fmaxf(m, v);
-    }
-    return scale_of_warps(A, m, w, lane);
+    for (long long r = w * 32 + lane; r < rows; r += 32 * kEpiWarps) m = fmaxf(m, row_bound(A, r));
+    return scale_of_warps<PR_DLOGITS>(A, m, w, lane);
 }
+// A row's own power of two.  Rows down to 2^-12 of the largest have the one for all: fp16's smallest number is off by 2^-26 of their bound at most.  Smaller ones, which would lose bits to
+// it, are taken to 2^-12 of the largest too, by up to 2^14; the row of the weights' gradients' other operand is as much smaller, and its elements off by up to 2^-11 (of rows below 2^-26
+// of the largest).  Larger powers would cost these sums what they give the others.
+__device__ __forceinline__ float row_scale(float bound, float all) { return bound > 0.f ? fminf(fmaxf(scale_for(bound, 13) * 0x1p-12f, all), all * 0x1p14f) : all; }
 // ... of the gradients that come in, rows without a gap
 template <typename T> __device__ __forceinline__ float scale_of_grads(const ProductArgs &A, int w, int lane) {
     float m = 0.f;
@@ -158,7 +166,7 @@ template <typename T> __device__ __forceinline__ float scale_of_grads(const Prod
         for (int j = 0; j < 8; ++j) take(to_f(e[j]));
     }
     if (w * 32 + lane < n % 8) take(to_f(g[n / 8 * 8 + w * 32 + lane]));
-    return scale_of_warps(A, m, w, lane);
+    return scale_of_warps<PR_GATED_GRAD>(A, m, w, lane);
 }
 
 template <typename T> __device__ __forceinline__ uint32_t pack2(float a, float b) {
@@ -167,6 +175,22 @@ template <typename T> __device__ __forceinline__ uint32_t pack2(float a, float b
     memcpy(&r, p, 4);
     return r;
 }
+// A.h's rows, scaled, to A.h_out: by the warps of finished tiles while their first products run
+template <typename T> __device__ __forceinline__ void scale_rows(const ProductArgs &A, float all, int w, int lane) {
+    for (long long r = (long long)blockIdx.x * kEpiWarps + w; r < A.part[0].m; r += (long long)gridDim.x * kEpiWarps) {
+        const float f = all / row_scale(row_bound(A, r), all);
+        const uint4 *from = reinterpret_cast<const uint4 *>(reinterpret_cast<const T *>(A.h) + r * A.h_ld);
+        uint4 *to = reinterpret_cast<uint4 *>(reinterpret_cast<T *>(A.h_out) + r * A.h_out_ld);
+#pragma unroll 4
+        for (int i = lane; i < A.d / 8; i += 32) {
+            const uint4 u = from[i];
+            T e[8];
+            memcpy(e, &u, 16);
+            to[i] = make_uint4(pack2<T>(to_f(e[0]) * f, to_f(e[1]) * f), pack2<T>(to_f(e[2]) * f, to_f(e[3]) * f), pack2<T>(to_f(e[4]) * f, to_f(e[5]) * f), pack2<T>(to_f(e[6]) * f, to_f(e[7]) * f));
+        }
+    }
+}
+
 // N numbers to a row's columns from `col` on, of `n`; whole: 16-byte pieces fit
 template <typename T, int N> __device__ __forceinline__ void store_row(T *row, int col, int n, bool whole, const float (&x)[N]) {
     if (whole && col + N <= n) {
@@ -477,13 +501,17 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
         const int quarter = warp & 3, half = (warp - 2) >> 2;
         const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16), buf = ring + (uint32_t)(kRingBytes + (warp - 2) * 4096);
         float scale = scale_of(A.amax, A.amax_to);
-        if constexpr (EPI == PR_DLOGITS) {
-            if (A.amax_out) scale = scale_of_rows(A, warp - 2, lane);
+        constexpr bool kRowScales = std::is_same<T, __half>::value && (EPI == PR_DLOGITS || kOut);
+        if constexpr (kRowScales && EPI == PR_DLOGITS) {
+            if (A.look) scale = scale_of_rows(A, warp - 2, lane);
+            if (A.h_out) scale_rows<T>(A, scale, warp - 2, lane);
+            if (blockIdx.x == 0 && tid == 64) *A.all_scale = scale;
         }
+        [[maybe_unused]] const float all = scale;
         if constexpr (EPI == PR_GATED_GRAD && std::is_same<T, __half>::value) {
             if (A.amax_out) scale = scale_of_grads<T>(A, warp - 2, lane);
         }
-        const float back = 1.f / scale;
+        const float back = 1.f / (kRowScales && kOut && A.all_scale ? *A.all_scale : scale);
         int acc = 0;
         uint32_t acc_par = 0u;
         float mx = -INFINITY, sum = 0.f;        // PR_STATS
@@ -605,6 +633,10 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
                         token = there ? token - A.vocab0 : -1;
                         if constexpr (EPI == PR_DLOGITS) {
                             const float lse = A.lse[row];
+                            if constexpr (kRowScales) {
+                                scale = row_scale(row_bound(A, row), all);
+                                if (w.n == 0 && half == 0) A.row_scale[row] = scale;
+                            }
                             g = A.g && there ? A.g[row * A.g_ld] : 0.f;
                             gp = g - (A.g_lse ? A.g_lse[row * A.g_lse_ld] : 0.f);
                             g *= A.inv_t * scale;
@@ -690,8 +722,12 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
                                 }
                                 if (!P.end) continue;
                             }
+                            float by = back;
+                            if constexpr (kRowScales) {
+                                if (A.row_scale && !P.rows_a) by = live ? 1.f / A.row_scale[row] : 0.f;
+                            }
 #pragma unroll
-                            for (int i = 0; i < 32; ++i) x[i] *= back;
+                            for (int i = 0; i < 32; ++i) x[i] *= by;
                             if ((c & 1) == 0) rows_free(lane);
                             put_row<T>(buf, lane, (c & 1) * 4, x);
                             if ((c & 1) || c + 1 == pieces) rows_store(&M.out[P.map_out + w.job], buf, col - (c & 1) * 32, row0, 0, true, lane);
@@ -863,15 +899,12 @@ __global__ void __launch_bounds__(256) amax_rows_kernel(const T *x, long long ro
     }
 }
 
-__global__ void __launch_bounds__(32) amax_pairs_kernel(const float *g, long long g_ld, const float *h, long long h_ld, int rows, float by, float *amax) {
+__global__ void __launch_bounds__(32) amax_losses_kernel(const __grid_constant__ ProductArgs A, int rows, float *amax) {
     chain_go();
     chain_wait();
     float m = 0.f;
-    for (int r = blockIdx.x * 32 + threadIdx.x; r < rows; r += kAmaxBlocks * 32) {
-        const float v = (2.f * (g ? fabsf(g[r * g_ld]) : 0.f) + (h ? fabsf(h[r * h_ld]) : 0.f)) * by;
-        if (v < INFINITY) m = fmaxf(m, v);
-        if (r > INT_MAX - kAmaxBlocks * 32) break;
-    }
+#pragma unroll 4
+    for (long long r = blockIdx.x * 32 + threadIdx.x; r < rows; r += kAmaxBlocks * 32) m = fmaxf(m, row_bound(A, r));
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
     if (threadIdx.x == 0) amax[blockIdx.x] = m;
@@ -881,13 +914,13 @@ __global__ void __launch_bounds__(32) amax_pairs_kernel(const float *g, long lon
 // the warps' sums.  (Where the last split adds them up itself, one CTA of a tile reads them all: 24 splits of a tile of 256 x 256 take it 20 us.  A thread that adds up all splits waits for
 // one batch of them after the other: 40 of them 11 us, so 5.)
 template <int CG, int BN, typename T>
-__global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ ProductPart P, const float *amax, int amax_to) {
+__global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ ProductPart P, const __grid_constant__ ProductArgs A) {
     constexpr int kPieces = BN / 64, kTile = CG * kEpiWarps * kPieces * 1024;
     __shared__ float4 sums[7][32];
     chain_go();
     chain_wait();
     const int lane = threadIdx.x & 31, slice = threadIdx.x >> 5;
-    const float back = slice ? 1.f : 1.f / scale_of(amax, amax_to);
+    const float back = slice ? 1.f : 1.f / (A.all_scale ? *A.all_scale : scale_of(A.amax, A.amax_to));
     const int groups = (int)(P.by_plane.d * (unsigned)P.jobs) * (kTile / 128);
     for (int i = blockIdx.x; i < groups; i += gridDim.x) {
         const int at = i / (kTile / 128), q = i - at * (kTile / 128), four = q & 7, piece = (q >> 3) % kPieces, w = (q >> 3) / kPieces % kEpiWarps, rank = (q >> 3) / (kPieces * kEpiWarps),
@@ -910,8 +943,10 @@ __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ Produ
                 const float4 x = sums[k][lane];
                 s.x += x.x; s.y += x.y; s.z += x.z; s.w += x.w;
             }
-            if (row < P.m)
-                *reinterpret_cast<uint2 *>(reinterpret_cast<T *>(P.out[job]) + (long long)row * P.out_ld + col) = make_uint2(pack2<T>(s.x * back, s.y * back), pack2<T>(s.z * back, s.w * back));
+            if (row < P.m) {
+                const float by = A.row_scale && !P.rows_a ? 1.f / A.row_scale[row] : back;
+                *reinterpret_cast<uint2 *>(reinterpret_cast<T *>(P.out[job]) + (long long)row * P.out_ld + col) = make_uint2(pack2<T>(s.x * by, s.y * by), pack2<T>(s.z * by, s.w * by));
+            }
         }
         __syncthreads();
     }
@@ -1162,8 +1197,8 @@ static cudaError_t launch_join(const ProductCut &cut, int dtype, const ProductPa
     const long long blocks = (long long)P.by_plane.d * P.jobs * (long long)(tile_bytes(cut) / 512), most = (long long)product_sms() * 8;
     const dim3 grid((unsigned)(blocks < most ? blocks : most));
     if (cut.wide)
-        return dtype == XSM_BF16 ? launch_early(join_kernel<2, 256, bf16>, grid, dim3(256), 0, st, P, A.amax, A.amax_to) : launch_early(join_kernel<2, 256, __half>, grid, dim3(256), 0, st, P, A.amax, A.amax_to);
-    return dtype == XSM_BF16 ? launch_early(join_kernel<1, 128, bf16>, grid, dim3(256), 0, st, P, A.amax, A.amax_to) : launch_early(join_kernel<1, 128, __half>, grid, dim3(256), 0, st, P, A.amax, A.amax_to);
+        return dtype == XSM_BF16 ? launch_early(join_kernel<2, 256, bf16>, grid, dim3(256), 0, st, P, A) : launch_early(join_kernel<2, 256, __half>, grid, dim3(256), 0, st, P, A);
+    return dtype == XSM_BF16 ? launch_early(join_kernel<1, 128, bf16>, grid, dim3(256), 0, st, P, A) : launch_early(join_kernel<1, 128, __half>, grid, dim3(256), 0, st, P, A);
 }
 
 cudaError_t launch_sums(int dtype, const SumsPlan &p, const Sums &s, cudaStream_t st) {
@@ -1177,6 +1212,8 @@ cudaError_t launch_sums(int dtype, const SumsPlan &p, const Sums &s, cudaStream_
     A.counter = s.counters;
     A.amax = s.amax;
     A.amax_to = s.amax_to;
+    A.row_scale = s.row_scale;
+    A.all_scale = s.all_scale;
     A.chunks = 1;
     A.low = s.low;
     const int parts = s.low ? 2 : 1;
@@ -1240,9 +1277,7 @@ cudaError_t launch_amax_rows(const void *x, int dtype, long long rows, long long
     if (dtype == XSM_BF16) return launch_early(amax_rows_kernel<bf16>, dim3(kAmaxBlocks), dim3(256), 0, st, (const bf16 *)x, rows, cols, ld, all, amax);
     return launch_early(amax_rows_kernel<__half>, dim3(kAmaxBlocks), dim3(256), 0, st, (const __half *)x, rows, cols, ld, all, amax);
 }
-cudaError_t launch_amax_pairs(const float *g, long long g_ld, const float *h, long long h_ld, int rows, float by, float *amax, cudaStream_t st) {
-    return launch_early(amax_pairs_kernel, dim3(kAmaxBlocks), dim3(32), 0, st, g, g_ld, h, h_ld, rows, by, amax);
-}
+cudaError_t launch_amax_losses(const ProductArgs &A, int rows, float *amax, cudaStream_t st) { return launch_early(amax_losses_kernel, dim3(kAmaxBlocks), dim3(32), 0, st, A, rows, amax); }
 
 }  // namespace xsm
 

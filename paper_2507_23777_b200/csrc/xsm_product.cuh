@@ -81,8 +81,17 @@ struct ProductArgs {
     void *out[2];                   // PR_GATED_GRAD: gate's, up's
     long long out_ld;
     const float *amax;              // [kAmaxBlocks], NULL: scale 1
-    float *amax_out;                // PR_DLOGITS: look for it in g and g_lse, PR_GATED_GRAD: in g_y, and leave it here for the launches behind
+    float *amax_out;                // PR_GATED_GRAD: look for it in g_y, and leave it here for the launches behind
     int amax_to;                    // the largest is scaled to [2^amax_to, 2^(amax_to + 1))
+
+    // fp16, whose smallest number is 2^-24: a power of two of every row's gradients, [m], and one of all; NULL: none.  PR_DLOGITS leaves them for PR_OUT, and the operand of the
+    // weights' gradients with rows scaled by the power of all over their own (h_out; NULL: nobody needs it).
+    float *row_scale, *all_scale;
+    int look;                       // PR_DLOGITS: the largest of the rows is looked for here; otherwise it is that of amax
+    const void *h;                  // [m][d]
+    void *h_out;
+    long long h_ld, h_out_ld;
+    int d;
 };
 
 // A row's maximum (times log2(e) / T) and sum of exponentials, joined part by part.
@@ -146,15 +155,16 @@ struct Sums {
     unsigned *counters;             // kSumCounters words
     const float *amax;
     int amax_to;
+    float *row_scale, *all_scale;   // of g's rows, fp16; h's rows are scaled by the latter over the former
     int *status;
 };
 SumsPlan plan_sums(long long rows, long long cols, long long d, int pairs, bool x, bool y, bool once, bool low);      // once: x is made in one launch; low: g in two parts
 size_t sums_bytes(const ProductCut &cut, long long rows, long long d);      // of x_sums
 cudaError_t launch_sums(int dtype, const SumsPlan &p, const Sums &s, cudaStream_t st);
 
-// |x| at most over rows of 16-bit elements, or of fp32 numbers 2|g| + |g_lse| times `by`; [kAmaxBlocks]
+// the largest |x| of rows of 16-bit elements, or of what the gradients by a row's logits may be; [kAmaxBlocks]
 cudaError_t launch_amax_rows(const void *x, int dtype, long long rows, long long cols, long long ld, float *amax, cudaStream_t st);
-cudaError_t launch_amax_pairs(const float *g, long long g_ld, const float *g_lse, long long g_lse_ld, int rows, float by, float *amax, cudaStream_t st);
+cudaError_t launch_amax_losses(const ProductArgs &A, int rows, float *amax, cudaStream_t st);
 
 int product_sms();
 void product_waits(unsigned *tries, int *starve);
