@@ -409,7 +409,9 @@ typedef struct {
 XSM_API xsm_status xsm_gated_ff(const xsm_gated_ff_args *a, void *cuda_stream);
 
 /* The gradient of sum(g_out * out) by x, w_gate and w_up, in their type.  gate and up are computed again; their gradients g_out up act'(gate) and g_out act(gate) are
- * rounded to dtype once (up to 128 rows or 32 columns: held in two parts of it; fp16: scaled by the power of two that takes the largest finite g_out to [1, 2): up act'(gate) beyond 2^15 is infinite, what is below 2^-25 zero).  d_x, or d_w_gate and d_w_up, may be NULL. */
+ * rounded to dtype once (up to 128 rows or 32 columns: held in two parts of it; fp16: scaled by
+ * powers of two, which take a row's bound |g_out| |x| max(1.13 |w_up|, |w_gate|), over the largest finite elements and rows, to 2^13 for the largest row and to 2 at least for rows down to
+ * 2^-26 of it, and back in the sums: nothing finite becomes infinite on the way).  d_x, or d_w_gate and d_w_up, may be NULL. */
 typedef struct {
     const void *x, *w_gate, *w_up;        /* as above */
     const void *g_out;                    /* DEVICE dtype [rows][ff]; aligned to its elements */

@@ -11,8 +11,6 @@
 
 namespace xsm {
 
-constexpr long long kLookedThrough = 1 << 16;      // so many gradients every CTA looks through for the largest (27 x 243 14.0 -> 11.0 us, 55 x 1133 18.4 -> 17.5)
-
 static size_t up(size_t n) { return (n + 255) & ~(size_t)255; }
 
 struct GatedGradPlan {
@@ -20,7 +18,7 @@ struct GatedGradPlan {
     SumsPlan sums;
     int ld;
     long long low;
-    size_t amax, d_gate, d_up, part, bytes;
+    size_t amax, all, scale, bounds, x, d_gate, d_up, part, bytes;
 };
 static GatedGradPlan plan_gated_grad(int rows, int ff, int d, bool x, bool w) {
     GatedGradPlan p;
@@ -29,7 +27,11 @@ static GatedGradPlan plan_gated_grad(int rows, int ff, int d, bool x, bool w) {
     p.sums = plan_sums(rows, ff, d, 2, x, w, true, few);
     p.ld = (ff + 7) / 8 * 8;
     p.amax = 0;
-    p.d_gate = up(kAmaxBlocks * 4);
+    p.all = up(2 * kAmaxBlocks * 4);
+    p.scale = p.all + 256;
+    p.bounds = p.scale + up((size_t)rows * 4);
+    p.x = p.bounds + up((size_t)rows * 4);
+    p.d_gate = p.x + (w ? up((size_t)rows * d * 2) : 0);
     const size_t one = up((size_t)rows * p.ld * 2);
     p.low = few ? (long long)one : 0;        // (in elements: behind both)
     p.d_up = p.d_gate + one;
@@ -99,24 +101,28 @@ xsm_status xsm_gated_ff_grad(const xsm_gated_ff_grad_args *a, void *cuda_stream)
     A.g_y = a->g_out; A.g_y_ld = a->g_out_stride;
     A.out[0] = ws + p.d_gate; A.out[1] = ws + p.d_up; A.out_ld = p.ld; A.low = p.low;
     cudaError_t e = cudaSuccess;
-    if (a->dtype == XSM_F16) {        // fp16 has no numbers below 2^-24: the largest gradient that comes in is taken to 1 and more, which leaves up to 2^15 for up
-        // (few elements without gaps: every CTA looks through them while its first products run; a launch costs 2 us from the host and 3 on the device)
-        if (a->g_out_stride == a->ff && (uintptr_t)a->g_out % 16 == 0 && (long long)a->rows * a->ff <= kLookedThrough) A.amax_out = (float *)(ws + p.amax);
-        else A.amax = (const float *)(ws + p.amax);
-        if (A.amax) e = launch_amax_rows(a->g_out, a->dtype, a->rows, a->ff, a->g_out_stride, (float *)(ws + p.amax), st);
-    }
     const Operand x = {a->x, a->rows, a->d, a->x_stride}, w[2] = {{a->w_gate, a->ff, a->d, a->w_gate_stride}, {a->w_up, a->ff, a->d, a->w_up_stride}};
-    if (e == cudaSuccess) e = launch_product(PR_GATED_GRAD, a->dtype, p.cut, A, a->rows, a->ff, x, w, st);
     Sums S = {};
     S.pairs = 2; S.low = p.low;
     S.h = x;
+    if (a->dtype == XSM_F16) {        // fp16 has no numbers below 2^-24 and none above 65504: a row's largest possible gradient by gate or up is taken to 2^13 and more
+        S.row_scale = A.row_scale = (float *)(ws + p.scale);
+        S.all_scale = A.all_scale = (float *)(ws + p.all);
+        A.bounds = (const float *)(ws + p.bounds);
+        A.amax = (const float *)(ws + p.amax);
+        if (a->d_w_gate) {
+            A.h = a->x; A.h_ld = a->x_stride; A.h_out = ws + p.x; A.h_out_ld = A.d = a->d;
+            S.h = {ws + p.x, a->rows, a->d, a->d};
+        }
+        e = launch_gated_sizes({x, {a->g_out, a->rows, a->ff, a->g_out_stride}, {w[0], w[1]}, (float *)(ws + p.bounds), (float *)(ws + p.amax)}, st);
+    }
+    if (e == cudaSuccess) e = launch_product(PR_GATED_GRAD, a->dtype, p.cut, A, a->rows, a->ff, x, w, st);
     for (int i = 0; i < 2; ++i) { S.g[i] = {A.out[i], a->rows, a->ff, p.ld}; S.w[i] = w[i]; }
     S.x = a->d_x; S.x_ld = a->d_x_stride;
     S.y[0] = a->d_w_gate; S.y[1] = a->d_w_up; S.y_ld = a->d_w_stride;
     S.end = 1;
     S.partial = ws + p.part;
     S.counters = a->counters; S.status = a->status;
-    S.amax = a->dtype == XSM_F16 ? (const float *)(ws + p.amax) : nullptr; S.amax_to = A.amax_to;
     if (e == cudaSuccess) e = launch_sums(a->dtype, p.sums, S, st);
     return launched(e);
 }

@@ -175,7 +175,6 @@ xsm_status xsm_linear_logprobs_grad(const xsm_linear_logprobs_grad_args *a, void
     S.counters = a->counters; S.status = a->status;
     cudaError_t e = cudaSuccess;
     if (a->dtype == XSM_F16) {        // fp16 has no numbers below 2^-24: a row's largest possible gradient by a logit is taken to 2^13 and more
-        Z.amax_to = 13;
         S.row_scale = Z.row_scale = (float *)(ws + p.scale);
         S.all_scale = Z.all_scale = (float *)(ws + p.all);
         if (a->d_weight) {

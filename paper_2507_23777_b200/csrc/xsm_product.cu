@@ -11,7 +11,6 @@
 // to the first copy, 3,700 for the bytes, 1,600 for the tile, then the last CTA's sums).
 #include "xsm_product.cuh"
 
-#include <limits.h>
 #include <string.h>
 
 #include <atomic>
@@ -110,28 +109,17 @@ __device__ __forceinline__ float scale_for(float most, int to) {
     return __uint_as_float((unsigned)(e + 127) << 23);
 }
 
-// the same of the largest of kAmaxBlocks numbers
-__device__ __forceinline__ float scale_of(const float *amax, int to) {
-    if (amax == nullptr) return 1.f;
+// the largest of kAmaxBlocks numbers
+__device__ __forceinline__ float most_of(const float *amax) {
     float m = 0.f;
-    for (int i = threadIdx.x & 31; i < kAmaxBlocks; i += 32) m = fmaxf(m, amax[i]);
+#pragma unroll
+    for (int i = 0; i < kAmaxBlocks; i += 32) m = fmaxf(m, amax[i + (threadIdx.x & 31)]);
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-    return scale_for(m, to);
+    return m;
 }
+constexpr int kScaleTo = 13;        // the largest gradient that may be is taken to [2^13, 2^14)
 
-// The same of the largest of 256 threads' numbers, those of the eight warps of a finished tile, which look for it while its products run; left in memory for the kernels behind.
-template <int EPI> __device__ __forceinline__ float scale_of_warps(const ProductArgs &A, float m, int w, int lane) {
-    __shared__ float most[kEpiWarps];
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-    if (lane == 0) most[w] = m;
-    bar_sync<32 * kEpiWarps>(1);
-#pragma unroll
-    for (int i = 0; i < kEpiWarps; ++i) m = fmaxf(m, most[i]);
-    if (EPI == PR_GATED_GRAD && blockIdx.x == 0) A.amax_out[w * 32 + lane] = w + lane ? 0.f : m;
-    return scale_for(m, A.amax_to);
-}
 // What the gradients by a row's logits may be: 2|g| + |g_lse| over T, g where there is a token, both where there is an lse; infinities and NaN: nothing.
 __device__ __forceinline__ float row_bound(const ProductArgs &A, long long r) {
     const long long t = A.token_bytes == 8 ? reinterpret_cast<const long long *>(A.tokens)[r * A.token_ld] : (long long)reinterpret_cast<const int *>(A.tokens)[r * A.token_ld];
@@ -139,46 +127,35 @@ __device__ __forceinline__ float row_bound(const ProductArgs &A, long long r) {
     const float v = (2.f * (t >= 0 && t < A.vocab ? fabsf(g) : 0.f) + fabsf(h)) * A.inv_t;
     return lse > -INFINITY && v < INFINITY ? v : 0.f;
 }
-// ... of all rows' bounds
-__device__ __forceinline__ float scale_of_rows(const ProductArgs &A, int w, int lane) {
+// ... of all rows at most, looked for by the warps of finished tiles while their first products run
+__device__ __forceinline__ float most_of_rows(const ProductArgs &A, int w, int lane) {
+    __shared__ float most[kEpiWarps];
     float m = 0.f;
     const int rows = A.part[0].m;
 #pragma unroll 4
     for (long long r = w * 32 + lane; r < rows; r += 32 * kEpiWarps) m = fmaxf(m, row_bound(A, r));
-    return scale_of_warps<PR_DLOGITS>(A, m, w, lane);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+    if (lane == 0) most[w] = m;
+    bar_sync<32 * kEpiWarps>(1);
+#pragma unroll
+    for (int i = 0; i < kEpiWarps; ++i) m = fmaxf(m, most[i]);
+    return m;
 }
 // A row's own power of two.  Rows down to 2^-12 of the largest have the one for all: fp16's smallest number is off by 2^-26 of their bound at most.  Smaller ones, which would lose bits to
 // it, are taken to 2^-12 of the largest too, by up to 2^14; the row of the weights' gradients' other operand is as much smaller, and its elements off by up to 2^-11 (of rows below 2^-26
 // of the largest).  Larger powers would cost these sums what they give the others.
-__device__ __forceinline__ float row_scale(float bound, float all) { return bound > 0.f ? fminf(fmaxf(scale_for(bound, 13) * 0x1p-12f, all), all * 0x1p14f) : all; }
-// ... of the gradients that come in, rows without a gap
-template <typename T> __device__ __forceinline__ float scale_of_grads(const ProductArgs &A, int w, int lane) {
-    float m = 0.f;
-    const int n = A.part[0].m * A.part[0].n;
-    const T *g = reinterpret_cast<const T *>(A.g_y);
-    auto take = [&](float v) { v = fabsf(v); if (v < INFINITY) m = fmaxf(m, v); };
-#pragma unroll 4
-    for (int i = w * 32 + lane; i < n / 8; i += 32 * kEpiWarps) {
-        const uint4 u = reinterpret_cast<const uint4 *>(g)[i];
-        T e[8];
-        memcpy(e, &u, 16);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) take(to_f(e[j]));
-    }
-    if (w * 32 + lane < n % 8) take(to_f(g[n / 8 * 8 + w * 32 + lane]));
-    return scale_of_warps<PR_GATED_GRAD>(A, m, w, lane);
-}
-
+__device__ __forceinline__ float row_scale(float bound, float all) { return bound > 0.f ? fminf(fmaxf(scale_for(bound, kScaleTo) * 0x1p-12f, all), all * 0x1p14f) : all; }
 template <typename T> __device__ __forceinline__ uint32_t pack2(float a, float b) {
     T p[2] = {rounded<T>(a), rounded<T>(b)};
     uint32_t r;
     memcpy(&r, p, 4);
     return r;
 }
-// A.h's rows, scaled, to A.h_out: by the warps of finished tiles while their first products run
-template <typename T> __device__ __forceinline__ void scale_rows(const ProductArgs &A, float all, int w, int lane) {
+// A.h's rows, scaled by the power of all over their own (own(row)), to A.h_out: by the same warps
+template <typename T, typename F> __device__ __forceinline__ void scale_rows(const ProductArgs &A, float all, F own, int w, int lane) {
     for (long long r = (long long)blockIdx.x * kEpiWarps + w; r < A.part[0].m; r += (long long)gridDim.x * kEpiWarps) {
-        const float f = all / row_scale(row_bound(A, r), all);
+        const float f = all / own(r);
         const uint4 *from = reinterpret_cast<const uint4 *>(reinterpret_cast<const T *>(A.h) + r * A.h_ld);
         uint4 *to = reinterpret_cast<uint4 *>(reinterpret_cast<T *>(A.h_out) + r * A.h_out_ld);
 #pragma unroll 4
@@ -500,18 +477,25 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
     } else {
         const int quarter = warp & 3, half = (warp - 2) >> 2;
         const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16), buf = ring + (uint32_t)(kRingBytes + (warp - 2) * 4096);
-        float scale = scale_of(A.amax, A.amax_to);
-        constexpr bool kRowScales = std::is_same<T, __half>::value && (EPI == PR_DLOGITS || kOut);
-        if constexpr (kRowScales && EPI == PR_DLOGITS) {
-            if (A.look) scale = scale_of_rows(A, warp - 2, lane);
-            if (A.h_out) scale_rows<T>(A, scale, warp - 2, lane);
-            if (blockIdx.x == 0 && tid == 64) *A.all_scale = scale;
+        constexpr bool kScaled = std::is_same<T, __half>::value && (EPI == PR_DLOGITS || EPI == PR_GATED_GRAD || kOut);
+        float all = 1.f;
+        [[maybe_unused]] float factor = 1.f;        // of the rows' bounds
+        if constexpr (kScaled && kOut) all = *A.all_scale;
+        if constexpr (kScaled && !kOut) {
+            if constexpr (EPI == PR_GATED_GRAD) factor = most_of(A.amax + kAmaxBlocks);
+            if constexpr (EPI == PR_DLOGITS) all = scale_for(A.look ? most_of_rows(A, warp - 2, lane) : most_of(A.amax), kScaleTo);
+            else all = scale_for(most_of(A.amax) * factor, kScaleTo);
+            if (blockIdx.x == 0 && tid == 64) *A.all_scale = all;
         }
-        [[maybe_unused]] const float all = scale;
-        if constexpr (EPI == PR_GATED_GRAD && std::is_same<T, __half>::value) {
-            if (A.amax_out) scale = scale_of_grads<T>(A, warp - 2, lane);
+        [[maybe_unused]] auto own_scale = [&](long long r) {
+            if constexpr (EPI == PR_DLOGITS) return row_scale(row_bound(A, r), all);
+            else return row_scale(A.bounds[r] * factor, all);
+        };
+        if constexpr (kScaled && !kOut) {
+            if (A.h_out) scale_rows<T>(A, all, own_scale, warp - 2, lane);
         }
-        const float back = 1.f / (kRowScales && kOut && A.all_scale ? *A.all_scale : scale);
+        float scale = 1.f;
+        const float back = 1.f / all;
         int acc = 0;
         uint32_t acc_par = 0u;
         float mx = -INFINITY, sum = 0.f;        // PR_STATS
@@ -529,6 +513,10 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
             const Tile w = tile_of(P, (unsigned)t);
             const int row0 = w.m * TM + rank * 128 + quarter * 32, row = row0 + lane;
             const bool live = row < P.m;
+            if constexpr (kScaled && EPI == PR_GATED_GRAD) {
+                scale = live ? own_scale(row) : 0.f;
+                if (live && w.n == 0 && half == 0) A.row_scale[row] = scale;
+            }
             if constexpr (EPI == PR_GATED_GRAD && CG == 2) {
                 rows_free(lane);
                 rows_fetch(reinterpret_cast<const T *>(A.g_y), A.g_y_ld, row0, P.m, w.n * (BN / 2) + half * (BN / 4), P.n, (A.g_y_ld & 7) == 0 && ((uintptr_t)A.g_y & 15) == 0, buf, lane);
@@ -633,8 +621,8 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
                         token = there ? token - A.vocab0 : -1;
                         if constexpr (EPI == PR_DLOGITS) {
                             const float lse = A.lse[row];
-                            if constexpr (kRowScales) {
-                                scale = row_scale(row_bound(A, row), all);
+                            if constexpr (kScaled) {
+                                scale = own_scale(row);
                                 if (w.n == 0 && half == 0) A.row_scale[row] = scale;
                             }
                             g = A.g && there ? A.g[row * A.g_ld] : 0.f;
@@ -723,8 +711,8 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
                                 if (!P.end) continue;
                             }
                             float by = back;
-                            if constexpr (kRowScales) {
-                                if (A.row_scale && !P.rows_a) by = live ? 1.f / A.row_scale[row] : 0.f;
+                            if constexpr (kScaled) {
+                                if (!P.rows_a) by = live ? 1.f / A.row_scale[row] : 0.f;
                             }
 #pragma unroll
                             for (int i = 0; i < 32; ++i) x[i] *= by;
@@ -867,35 +855,78 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
 
 // -------------------------------------------------------------------------------------------- small kernels
 
-// the largest |x| of 16-bit elements, infinities and NaN apart, a number for each block; rows of up to `most` elements, of `all` elements from the first on
-template <typename T>
-__global__ void __launch_bounds__(256) amax_rows_kernel(const T *x, long long rows, long long most, long long ld, long long all, float *amax) {
+// The largest of n elements, or the sum of their squares (kSquares), by a warp, each lane's own.  Elements up to the first 16-byte boundary and behind the last one by one; eight loads of a
+// lane on their way, which the compiler would put beside their uses otherwise (64 rows, 8192 of 2048: 38 us, 19 so; 2047 x 2051 of 768 12.5 and 8.8).
+template <bool kSquares, bool kFinite> __device__ __forceinline__ float row_size_of(const __half *p, long long n, int lane) {
+    float m = 0.f;
+    auto take = [&](float v) {
+        if (kFinite && !(fabsf(v) < INFINITY)) v = 0.f;
+        m = kSquares ? fmaf(v, v, m) : fmaxf(m, fabsf(v));
+    };
+    const long long before = min(n, (long long)((16 - ((uintptr_t)p & 15)) / 2 & 7)), pieces = (n - before) / 8, behind = before + pieces * 8;
+    const float first = lane < before ? to_f(p[lane]) : 0.f, last = lane < n - behind ? to_f(p[behind + lane]) : 0.f;
+    const uint4 *body = reinterpret_cast<const uint4 *>(p + before);
+    for (long long i = lane; i < pieces; i += 256) {
+        uint4 u[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            asm volatile("ld.global.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(u[k].x), "=r"(u[k].y), "=r"(u[k].z), "=r"(u[k].w) : "l"(body + (i + 32 * k < pieces ? i + 32 * k : i)));
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            if (i + 32 * k >= pieces) u[k] = make_uint4(0u, 0u, 0u, 0u);
+            __half2 e[4];
+            memcpy(e, &u[k], 16);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float2 f = __half22float2(e[j]);
+                take(f.x);
+                take(f.y);
+            }
+        }
+    }
+    take(first);
+    take(last);
+    return m;
+}
+// ... infinities and NaN apart
+template <bool kSquares> __device__ __forceinline__ float row_size(const __half *p, long long n, int lane) {
+    auto all = [](float m) {
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) m = kSquares ? m + __shfl_xor_sync(0xffffffffu, m, o) : fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+        return m;
+    };
+    const float m = all(row_size_of<kSquares, false>(p, n, lane));
+    return m < INFINITY ? m : all(row_size_of<kSquares, true>(p, n, lane));
+}
+// GatedSizes: a warp a row, x's with g's, then the weights'.  The weights' bytes bound it where rows are few: 64 rows, 8192 of 2048 61 -> 78 us with it, 2047 x 2051 of 768 53 -> 57.
+constexpr int kSizeThreads = 512;
+__global__ void __launch_bounds__(kSizeThreads, 2) gated_sizes_kernel(const __grid_constant__ GatedSizes A) {
     chain_go();
     chain_wait();
-    __shared__ float s[8];
-    float m = 0.f;
-    auto take = [&](float v) { v = fabsf(v); if (v < INFINITY) m = fmaxf(m, v); };
-    const bool whole = ((uintptr_t)x & 15) == 0 && (ld & 7) == 0;
-    for (long long r = blockIdx.x; r < rows; r += kAmaxBlocks) {
-        const T *row = x + r * ld;
-        const long long left = all - r * ld, cols = left < most ? left : most, pieces = whole ? cols / 8 : 0;
-#pragma unroll 4
-        for (long long i = threadIdx.x; i < pieces; i += 256) {
-            const uint4 u = reinterpret_cast<const uint4 *>(row)[i];
-            T e[8];
-            memcpy(e, &u, 16);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) take(to_f(e[j]));
+    __shared__ float most[2][kSizeThreads / 32];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const long long rows = A.x.rows, ff = A.w[0].rows;
+    float bounds = 0.f, factors = 0.f;
+    for (long long t = (long long)blockIdx.x * (kSizeThreads / 32) + warp; t < rows + 2 * ff; t += kAmaxBlocks * (kSizeThreads / 32)) {
+        const long long f = t - rows;
+        const Operand &O = f < 0 ? A.x : A.w[f >= ff];
+        float bound = sqrtf(row_size<true>(reinterpret_cast<const __half *>(O.p) + (f < 0 ? t : f >= ff ? f - ff : f) * O.ld, O.row, lane));
+        if (f < 0) bound *= row_size<false>(reinterpret_cast<const __half *>(A.g.p) + t * A.g.ld, A.g.row, lane);
+        else if (f >= ff) bound *= 1.13f;
+        if (f < 0) {
+            bounds = fmaxf(bounds, bound);
+            if (lane == 0) A.bounds[t] = bound;
+        } else {
+            factors = fmaxf(factors, bound);
         }
-        for (long long i = pieces * 8 + threadIdx.x; i < cols; i += 256) take(to_f(row[i]));
     }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-    if ((threadIdx.x & 31) == 0) s[threadIdx.x >> 5] = m;
+    if (lane == 0) { most[0][warp] = bounds; most[1][warp] = factors; }
     __syncthreads();
-    if (threadIdx.x == 0) {
-        for (int i = 1; i < 8; ++i) m = fmaxf(m, s[i]);
-        amax[blockIdx.x] = m;
+    if (warp < 2) {
+        float m = lane < kSizeThreads / 32 ? most[warp][lane] : 0.f;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+        if (lane == 0) A.amax[warp * kAmaxBlocks + blockIdx.x] = m;
     }
 }
 
@@ -920,7 +951,7 @@ __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ Produ
     chain_go();
     chain_wait();
     const int lane = threadIdx.x & 31, slice = threadIdx.x >> 5;
-    const float back = slice ? 1.f : 1.f / (A.all_scale ? *A.all_scale : scale_of(A.amax, A.amax_to));
+    const float back = A.all_scale ? 1.f / *A.all_scale : 1.f;
     const int groups = (int)(P.by_plane.d * (unsigned)P.jobs) * (kTile / 128);
     for (int i = blockIdx.x; i < groups; i += gridDim.x) {
         const int at = i / (kTile / 128), q = i - at * (kTile / 128), four = q & 7, piece = (q >> 3) % kPieces, w = (q >> 3) / kPieces % kEpiWarps, rank = (q >> 3) / (kPieces * kEpiWarps),
@@ -1210,8 +1241,6 @@ cudaError_t launch_sums(int dtype, const SumsPlan &p, const Sums &s, cudaStream_
     ProductArgs A = {};
     A.status = s.status;
     A.counter = s.counters;
-    A.amax = s.amax;
-    A.amax_to = s.amax_to;
     A.row_scale = s.row_scale;
     A.all_scale = s.all_scale;
     A.chunks = 1;
@@ -1267,16 +1296,7 @@ cudaError_t launch_sums(int dtype, const SumsPlan &p, const Sums &s, cudaStream_
     return e;
 }
 
-cudaError_t launch_amax_rows(const void *x, int dtype, long long rows, long long cols, long long ld, float *amax, cudaStream_t st) {
-    long long all = LLONG_MAX;
-    if (ld == cols) {        // one run of elements: a part for each block, of whole 16-byte pieces (2047 rows of 2051 fp16: 10 us row by row, 7 so)
-        all = rows * cols;
-        ld = cols = (all / kAmaxBlocks + 8) / 8 * 8;
-        rows = (all + cols - 1) / cols;
-    }
-    if (dtype == XSM_BF16) return launch_early(amax_rows_kernel<bf16>, dim3(kAmaxBlocks), dim3(256), 0, st, (const bf16 *)x, rows, cols, ld, all, amax);
-    return launch_early(amax_rows_kernel<__half>, dim3(kAmaxBlocks), dim3(256), 0, st, (const __half *)x, rows, cols, ld, all, amax);
-}
+cudaError_t launch_gated_sizes(const GatedSizes &s, cudaStream_t st) { return launch_early(gated_sizes_kernel, dim3(kAmaxBlocks), dim3(kSizeThreads), 0, st, s); }
 cudaError_t launch_amax_losses(const ProductArgs &A, int rows, float *amax, cudaStream_t st) { return launch_early(amax_losses_kernel, dim3(kAmaxBlocks), dim3(32), 0, st, A, rows, amax); }
 
 }  // namespace xsm

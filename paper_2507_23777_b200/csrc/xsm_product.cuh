@@ -80,14 +80,12 @@ struct ProductArgs {
     long long g_y_ld;
     void *out[2];                   // PR_GATED_GRAD: gate's, up's
     long long out_ld;
-    const float *amax;              // [kAmaxBlocks], NULL: scale 1
-    float *amax_out;                // PR_GATED_GRAD: look for it in g_y, and leave it here for the launches behind
-    int amax_to;                    // the largest is scaled to [2^amax_to, 2^(amax_to + 1))
-
-    // fp16, whose smallest number is 2^-24: a power of two of every row's gradients, [m], and one of all; NULL: none.  PR_DLOGITS leaves them for PR_OUT, and the operand of the
-    // weights' gradients with rows scaled by the power of all over their own (h_out; NULL: nobody needs it).
+    // fp16, whose smallest number is 2^-24: a power of two of every row's gradients, [m], and one of all; NULL: none.  PR_DLOGITS and PR_GATED_GRAD leave them for PR_OUT, and the operand
+    // of the weights' gradients with rows scaled by the power of all over their own (h_out; NULL: nobody needs it).
     float *row_scale, *all_scale;
-    int look;                       // PR_DLOGITS: the largest of the rows is looked for here; otherwise it is that of amax
+    const float *bounds;            // PR_GATED_GRAD: [m], times the largest of amax's second kAmaxBlocks numbers no less than any element of a row's gradients
+    const float *amax;              // the largest of rows' bounds is that of the first kAmaxBlocks
+    int look;                       // PR_DLOGITS: it is looked for here instead
     const void *h;                  // [m][d]
     void *h_out;
     long long h_ld, h_out_ld;
@@ -153,8 +151,6 @@ struct Sums {
     int go_on, end;
     char *partial;
     unsigned *counters;             // kSumCounters words
-    const float *amax;
-    int amax_to;
     float *row_scale, *all_scale;   // of g's rows, fp16; h's rows are scaled by the latter over the former
     int *status;
 };
@@ -162,9 +158,17 @@ SumsPlan plan_sums(long long rows, long long cols, long long d, int pairs, bool 
 size_t sums_bytes(const ProductCut &cut, long long rows, long long d);      // of x_sums
 cudaError_t launch_sums(int dtype, const SumsPlan &p, const Sums &s, cudaStream_t st);
 
-// the largest |x| of rows of 16-bit elements, or of what the gradients by a row's logits may be; [kAmaxBlocks]
-cudaError_t launch_amax_rows(const void *x, int dtype, long long rows, long long cols, long long ld, float *amax, cudaStream_t st);
+// What the gradients by rows' logits may be at most; [kAmaxBlocks].
 cudaError_t launch_amax_losses(const ProductArgs &A, int rows, float *amax, cudaStream_t st);
+
+// What gate's and up's gradients of fp16 rows may be at most, infinities and NaN apart: |up act'(gate)| <= 1.13 |x| |w_up|, |act(gate)| <= |x| |w_gate| (Cauchy and Schwarz; no derivative of silu or
+// gelu is above 1.13).
+struct GatedSizes {
+    Operand x, g, w[2];             // w: gate's, up's
+    float *bounds;                  // [rows]: the largest |g| times |x|
+    float *amax;                    // [2][kAmaxBlocks]: of bounds, of the weights' factor
+};
+cudaError_t launch_gated_sizes(const GatedSizes &s, cudaStream_t st);
 
 int product_sms();
 void product_waits(unsigned *tries, int *starve);

@@ -61,8 +61,9 @@ def test_rows_in_which_nothing_has_a_part_do_not_count(ops, rows):
 
 
 def loss_by_size(h, w, t, temperature, gl, gs, sizes, parts):
-    """linear_grad of rows of one size after the other: every row's bound goes by its own size.  The weights' gradient: the rows of each size, and what fp16 steps of 2^-24 leave of a
-    scaled operand next to the largest row's 2^13: for each row 2^-25 times 2^-12 of the largest |hidden| (2|g| + |g_lse|)."""
+    """linear_grad of rows of one size after the other: every row's bound goes by its own size.  The weights' gradient: the rows of each size, and for every row what fp16's steps leave of it next
+    to the largest: of its gradients 2^-25, these 2^13 of the largest's, and of its hidden states, 2^-12 of which a row of 2^-12 of the largest keeps as 2^-25 at worst: with |hidden| above
+    two both are less than 2^-37 of the largest |hidden| (2|g| + |g_lse|)."""
     dh, bh = torch.zeros(h.shape, dtype=torch.float64, device="cuda"), torch.zeros(h.shape, dtype=torch.float64, device="cuda")
     dw, bw = 0.0, 0.0
     kinds = sizes.unique()
@@ -109,3 +110,97 @@ def test_weights_gradient_of_many_rows_in_fp16(ops, size):
         want, bound = want + y, bound + c
     for x in (d_weight, alone):
         near(x, want, bound * (rows / chunk + 1), "d_weight")
+
+
+# ------------------------------------------------------------------------------------------------- the gated feed-forward part
+
+def gated_inputs(rows, ff, d, dtype, seed):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    x = torch.randn((rows, d), generator=g, device="cuda").to(dtype)
+    wg, wu = ((1.5 * d ** -0.5 * torch.randn((ff, d), generator=g, device="cuda")).to(dtype) for _ in range(2))
+    return x, wg, wu, torch.randn((rows, ff), generator=g, device="cuda").to(dtype)
+
+
+def gated_by_size(x, wg, wu, gy, kind, sizes, parts):
+    """gated_grad of rows of one size after the other, each with its own bound.  What fp16's steps leave of a row next to the largest, as for the losses, by the bound of its gradients:
+    |g| |x| max(1.13 |w_up|, |w_gate|); of the row itself 2^-26 of that."""
+    kinds = sizes.unique()
+    norm = x.double().norm(dim=-1)
+    factor = max(1.13 * float(wu.double().norm(dim=-1).max()), float(wg.double().norm(dim=-1).max()))
+    bounds = gy.double().abs().amax(-1) * norm * factor
+    dx, bx = torch.zeros(x.shape, dtype=torch.float64, device="cuda"), torch.zeros(x.shape, dtype=torch.float64, device="cuda")
+    out = [[dx, bx], [0.0, 0.0], [0.0, 0.0]]
+    for s in kinds:
+        at = sizes == s
+        (v, b), *more = ref.gated_grad(x[at], wg, wu, gy[at], kind, parts)
+        dx[at] = v
+        bx[at] = b + 2.0 ** -26 * bounds[at][:, None] * (wg.double().abs().sum(0) + wu.double().abs().sum(0))
+        for o, (v, b) in zip(out[1:], more):
+            o[0], o[1] = o[0] + v, o[1] + b * len(kinds)
+    for o in out[1:]:
+        o[1] = o[1] + x.shape[0] * 2.0 ** -37 * (1 + float(x.abs().max())) * float(bounds.max())
+    return out
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("kind", ["silu", "gelu"])
+@pytest.mark.parametrize("rows,ff,d", [(40, 700, 64), (300, 30, 64), (700, 515, 128)])
+@pytest.mark.parametrize("top", [0, 10])
+def test_gated_gradients_of_rows_of_unequal_size(ops, dtype, kind, rows, ff, d, top):
+    """Rows 2^24 apart, each as near as if it were alone; rows of zeros between them."""
+    x, wg, wu, gy = gated_inputs(rows, ff, d, dtype, seed=5)
+    sizes = 2.0 ** (top - 6.0 * (torch.arange(rows, device="cuda") % 5))
+    gy = (gy.float().clamp(-4, 4) * sizes[:, None]).to(dtype)
+    gy[3::7] = 0
+    got = ops.gated_feed_forward_grad(x, wg, wu, gy, kind)
+    few = rows <= 128 or ff <= 32
+    for v, (want, bound), what in zip(got, gated_by_size(x, wg, wu, gy, kind, sizes, 2 if few else 1), ("d_x", "d_w_gate", "d_w_up")):
+        sure = want.abs() + bound < 65000
+        near(torch.where(sure, v.double(), 0.0), torch.where(sure, want, 0.0), bound, what)
+    assert (got[0][3::7] == 0).all()
+
+
+@pytest.mark.parametrize("rows", [1, 6, 300])
+@pytest.mark.parametrize("ff", [24, 200])
+@pytest.mark.parametrize("size", [300.0, 30000.0])
+def test_gated_gradients_of_large_up_in_fp16(ops, rows, ff, size):
+    """up beyond the type's range beside a gate of ordinary size: the gradients of small g_out are finite, and are returned."""
+    x, wg, wu, gy = gated_inputs(rows, ff, 64, F16, seed=6)
+    x[:, 0] = size
+    wg[:, 0], wu[:, 0] = 0.0, 400.0
+    assert float((x.double() @ wu.double().T).abs().min()) > 2.0 ** 16
+    gy = (gy.float() * 1e-4).half()
+    wu[1:] *= 0.25
+    got = ops.gated_feed_forward_grad(x, wg, wu, gy)
+    few = rows <= 128 or ff <= 32
+    some = 0
+    for v, (want, bound), what in zip(got, gated_by_size(x, wg, wu, gy, "silu", torch.ones(rows, device="cuda"), 2 if few else 1), ("d_x", "d_w_gate", "d_w_up")):
+        sure = want.abs() + bound < 65000
+        some += int(sure.sum())
+        near(torch.where(sure, v.double(), 0.0), torch.where(sure, want, 0.0), bound, what)
+    assert some > 0
+
+
+def test_gated_gradients_of_ends_of_the_type(ops):
+    """The largest and the smallest numbers of fp16 in every place, weights of zeros, one weight that is infinite."""
+    x, wg, wu, gy = gated_inputs(140, 72, 64, F16, seed=7)
+    for scale_x, scale_w, scale_g in ((2.0 ** -24, 1.0, 1.0), (1.0, 2.0 ** -24, 1.0), (1.0, 1.0, 2.0 ** -24), (2.0 ** 13, 2.0 ** -13, 2.0 ** 13), (2.0 ** -13, 2.0 ** 13, 1.0)):
+        a = [(t.float() * s).half() for t, s in ((x, scale_x), (wg, scale_w), (wu, scale_w), (gy, scale_g))]
+        for v, (want, bound), what in zip(ops.gated_feed_forward_grad(*a), gated_by_size(*a, "silu", torch.ones(140, device="cuda"), 1), ("d_x", "d_w_gate", "d_w_up")):
+            sure = want.abs() + bound < 65000
+            near(torch.where(sure, v.double(), 0.0), torch.where(sure, want, 0.0), bound, what)
+    zero = torch.zeros_like(wg)
+    for v in ops.gated_feed_forward_grad(x, zero, zero, gy):
+        assert (v == 0).all()
+    for v in ops.gated_feed_forward_grad(torch.zeros_like(x), wg, wu, gy):
+        assert (v == 0).all()
+    w2 = wu.clone()
+    w2[5, 3] = math.inf
+    d = ops.gated_feed_forward_grad(x, wg, w2, gy)
+    clean = ops.gated_feed_forward_grad(x, wg, wu, gy)
+    keep = torch.arange(72, device="cuda") != 5
+    bound = gated_by_size(x, wg, wu, gy, "silu", torch.ones(140, device="cuda"), 1)
+    assert not d[1][5].isfinite().any()
+    for i in (1, 2):
+        near(d[i][keep], bound[i][0][keep], bound[i][1][keep], "d_w")
+        assert clean[i].isfinite().all()
