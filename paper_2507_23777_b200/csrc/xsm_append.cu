@@ -173,7 +173,8 @@ xsm_status xsm_kv_create(const xsm_kv_config *cfg, void *d_k, void *d_v, xsm_kv 
     int dev = 0;
     void *encode = nullptr;
     cudaDriverEntryPointQueryResult q;
-    cudaError_t e = cudaGetDevice(&dev);
+    cudaError_t e = bind_device();
+    if (e == cudaSuccess) e = cudaGetDevice(&dev);
     if (e == cudaSuccess) e = cudaDeviceGetAttribute(&kv->sms, cudaDevAttrMultiProcessorCount, dev);
     if (e == cudaSuccess) e = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &encode, cudaEnableDefault, &q);
     if (e != cudaSuccess) {

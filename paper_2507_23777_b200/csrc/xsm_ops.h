@@ -38,6 +38,19 @@ inline cudaError_t open_for(const void *fn, int smem) noexcept {
     }
 }
 
+// The current device's context for this thread, before a call of the driver's: a thread has none before its first call of the runtime that needs one, as where a framework's memory comes
+// from a pool of its own.
+inline cudaError_t bind_device() noexcept {
+    static thread_local int bound = -1;
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e == cudaSuccess && dev != bound) {
+        e = cudaSetDevice(dev);
+        if (e == cudaSuccess) bound = dev;
+    }
+    return e;
+}
+
 // The pools as the kernels see them.
 struct Pages {
     char *k, *v;

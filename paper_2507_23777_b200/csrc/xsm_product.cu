@@ -990,6 +990,8 @@ typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t
                                   CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 static std::atomic<EncodeTiledFn> g_encode{nullptr};
 static cudaError_t encoder(EncodeTiledFn *fn) {
+    const cudaError_t bound = bind_device();
+    if (bound != cudaSuccess) return bound;
     *fn = g_encode.load(std::memory_order_acquire);
     if (*fn) return cudaSuccess;
     void *p = nullptr;

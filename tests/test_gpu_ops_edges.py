@@ -1,0 +1,75 @@
+"""Calls of the operators on a caller's own activations and weights that are seldom made: from new threads, of nothing, on devices by their names."""
+import threading
+
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def ops():
+    assert torch.cuda.is_available(), "this test needs a B200"
+    from paper_2507_23777_b200 import build, ops
+    build.build()
+    yield ops
+    ops.check()
+
+
+def on_a_new_thread(f):
+    """What f returns on a thread that has made no call to the device yet; what it raises is raised here."""
+    out = {}
+
+    def run():
+        try:
+            out["r"] = f()
+        except Exception as e:
+            out["e"] = e
+    t = threading.Thread(target=run)
+    t.start()
+    t.join()
+    if "e" in out:
+        raise out["e"]
+    return out["r"]
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("rows", [5, 300])
+def test_first_calls_of_a_thread(ops, dtype, rows):
+    """Nothing of the thread's has called the device before: the memory comes from torch's pool."""
+    g = torch.Generator(device="cuda").manual_seed(0)
+    x, gy = (torch.randn((rows, 64), generator=g, device="cuda").to(dtype) for _ in range(2))
+    w = torch.randn((64, 64), generator=g, device="cuda").to(dtype)
+    t = torch.randint(0, 64, (rows,), generator=g, device="cuda")
+    gl = torch.randn(rows, generator=g, device="cuda")
+    q, gain = torch.randn((1, rows, 2, 64), generator=g, device="cuda").to(dtype), torch.ones(64, device="cuda")
+    pools = [torch.zeros((3, 2, 16, 64), device="cuda", dtype=dtype) for _ in range(2)]
+    r = ops.linear_logprobs(x, w, t)
+    calls = [lambda: ops.linear_logprobs(x, w, t), lambda: ops.linear_logprobs_grad(x, w, t, r, gl), lambda: [ops.gated_feed_forward(x, w, w)], lambda: ops.gated_feed_forward_grad(x, w, w, gy),
+             lambda: ops.norm_rotate(q, q, gain, gain), lambda: ops.norm_rotate_grad(q, q, gain, gain, q, q), lambda: ops.PagedCache(*pools) and []]
+    for f in calls:
+        want = f()
+        for _ in range(2):
+            for a, b in zip(on_a_new_thread(f), want):
+                assert torch.equal(a, b)
+
+
+def test_a_backward_pass_that_is_the_first_call_of_autograds_thread():
+    """In a process of its own: autograd's thread has not called the device before the gradient of the gated part."""
+    import os
+    import subprocess
+    import sys
+    code = """
+import torch
+from paper_2507_23777_b200 import ops
+x, w = torch.randn(300, 64, device="cuda").bfloat16(), torch.randn(200, 64, device="cuda").bfloat16()
+gy = torch.randn(300, 200, device="cuda").bfloat16()
+want = [ops.gated_feed_forward_grad(x, w, w, gy) for _ in range(3)].pop()
+x.requires_grad_()
+out = ops.gated_feed_forward(x, w, w)
+del want
+got, = torch.autograd.grad(out, x, gy)
+with torch.no_grad():
+    assert torch.equal(got, ops.gated_feed_forward_grad(x, w, w, gy)[0])
+"""
+    subprocess.run([sys.executable, "-c", code], check=True, cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))), timeout=300)
