@@ -396,6 +396,9 @@ typedef struct {
 } xsm_linear_logprobs_grad_args;
 XSM_API size_t xsm_linear_logprobs_grad_workspace(int rows, int vocab, int d);
 XSM_API xsm_status xsm_linear_logprobs_grad(const xsm_linear_logprobs_grad_args *a, void *cuda_stream);
+/* The same with the log probabilities of the call above (DEVICE [rows], may be NULL): the token's own element is g_logprob (1 - p) + g_lse p with p = exp(logprob), which next to p = 1 an lse that
+ * is rounded to fp32 does not tell: otherwise p is exp(z - lse), off by 2^-24 |lse| of itself. */
+XSM_API xsm_status xsm_linear_logprobs_grad_near(const xsm_linear_logprobs_grad_args *a, const float *logprob, void *cuda_stream);
 
 /* The gated feed-forward part of a block: out[r][f] = act(gate) up, gate = sum_i x[r][i] w_gate[f][i], up = sum_i x[r][i] w_up[f][i], gate and up in fp32;
  * act(g) = g / (1 + exp(-g)) (activation 0, silu) or g (1 + erf(g / sqrt 2)) / 2 (1, gelu). */

@@ -20,7 +20,7 @@ constexpr int kRowsLookedThrough = 8192;            // so many rows every CTA lo
 
 // Eight rows a block; thread (row, y) joins parts y, y + 32, ...  (32 rows a block, eight threads a row: 145 us for 96 rows of 4096 parts.)
 __global__ void __launch_bounds__(256) join_stats_kernel(const float2 *parts, const float *token_z, const void *tokens, long long token_ld, int token_bytes, int rows, int vocab,
-                                                         int n, float *logprob, float *lse) {
+                                                         int n, float c, double to_lse, float *logprob, float *lse) {
     chain_go();
     chain_wait();
     __shared__ float2 s[32][9];
@@ -38,7 +38,7 @@ __global__ void __launch_bounds__(256) join_stats_kernel(const float2 *parts, co
     r.m = s[lane][threadIdx.x >> 5].x;
     r.sum = s[lane][threadIdx.x >> 5].y;
     r.across_lanes();
-    if (lane == 0) r.finish(tokens, token_ld, token_bytes, vocab, at, token_z, logprob, lse);
+    if (lane == 0) r.finish(tokens, token_ld, token_bytes, vocab, at, token_z, c, to_lse, logprob, lse);
 }
 
 // One tile of rows: a CTA joins what its tiles find in its registers, and there are two parts for each CTA.
@@ -121,6 +121,7 @@ xsm_status xsm_linear_logprobs(const xsm_linear_logprobs_args *a, void *cuda_str
     A.tokens = a->tokens; A.token_ld = a->token_stride; A.token_bytes = a->token_bytes; A.vocab = a->vocab;
     A.inv_t = 1.f / a->temperature;
     A.c = (float)(1.4426950408889634 / a->temperature);
+    A.to_lse = 1.0 / ((double)A.c * a->temperature);
     A.parts = (float2 *)a->workspace;
     A.carry = p.carry;
     // (few rows: the last CTA joins the parts itself, 5 x 4096 7.8 -> 7.3 us and a launch less; of 96 rows that takes one CTA 15 us)
@@ -132,7 +133,7 @@ xsm_status xsm_linear_logprobs(const xsm_linear_logprobs_args *a, void *cuda_str
     cudaError_t e = launch_product(PR_STATS, a->dtype, p.cut, A, a->rows, a->vocab, h, w, st);
     if (e == cudaSuccess && !A.counter)
         e = launch_early(join_stats_kernel, dim3((unsigned)((a->rows + 7) / 8)), dim3(256), 0, st, (const float2 *)A.parts, (const float *)A.token_z, a->tokens, (long long)a->token_stride,
-                         (int)a->token_bytes, (int)a->rows, (int)a->vocab, (int)p.parts, a->logprob, a->lse);
+                         (int)a->token_bytes, (int)a->rows, (int)a->vocab, (int)p.parts, A.c, A.to_lse, a->logprob, a->lse);
     return launched(e);
 }
 
@@ -142,7 +143,9 @@ size_t xsm_linear_logprobs_grad_workspace(int rows, int vocab, int d) {
     return a > b ? (a > c ? a : c) : b > c ? b : c;
 }
 
-xsm_status xsm_linear_logprobs_grad(const xsm_linear_logprobs_grad_args *a, void *cuda_stream) {
+xsm_status xsm_linear_logprobs_grad(const xsm_linear_logprobs_grad_args *a, void *cuda_stream) { return xsm_linear_logprobs_grad_near(a, nullptr, cuda_stream); }
+
+xsm_status xsm_linear_logprobs_grad_near(const xsm_linear_logprobs_grad_args *a, const float *logprob, void *cuda_stream) {
     if (!a) return op_failed(XSM_ERR_INVALID_ARG, "null argument");
     if (const char *w = wrong_shape(a->rows, a->vocab, a->d, a->dtype, a->token_bytes, a->temperature)) return op_failed(XSM_ERR_INVALID_ARG, w);
     if (!a->d_hidden && !a->d_weight) return XSM_OK;
@@ -153,8 +156,8 @@ xsm_status xsm_linear_logprobs_grad(const xsm_linear_logprobs_grad_args *a, void
     if (!a->hidden || !a->weight || !a->tokens || !a->lse || !a->workspace || !a->status || !a->counters) return op_failed(XSM_ERR_INVALID_ARG, "null argument");
     if (!rows_fit(a->hidden, a->hidden_stride, a->d) || !rows_fit(a->weight, a->weight_stride, a->d) || (a->d_hidden && !rows_fit(a->d_hidden, a->d_hidden_stride, a->d)))
         return op_failed(XSM_ERR_INVALID_ARG, "rows of hidden, weight and d_hidden must be 16-byte aligned and must not overlap");
-    if ((uintptr_t)a->tokens % a->token_bytes || ((uintptr_t)a->lse | (uintptr_t)a->g_logprob | (uintptr_t)a->g_lse | (uintptr_t)a->status | (uintptr_t)a->counters) % 4 || (uintptr_t)a->workspace % 16)
-        return op_failed(XSM_ERR_INVALID_ARG, "tokens, lse, g_logprob, g_lse, status and counters must be aligned to their elements, workspace to 16 bytes");
+    if ((uintptr_t)a->tokens % a->token_bytes || ((uintptr_t)a->lse | (uintptr_t)logprob | (uintptr_t)a->g_logprob | (uintptr_t)a->g_lse | (uintptr_t)a->status | (uintptr_t)a->counters) % 4 || (uintptr_t)a->workspace % 16)
+        return op_failed(XSM_ERR_INVALID_ARG, "tokens, lse, logprob, g_logprob, g_lse, status and counters must be aligned to their elements, workspace to 16 bytes");
     const LinearGradPlan p = plan_linear_grad(a->rows, a->vocab, a->d, a->d_hidden, a->d_weight);
     if (a->workspace_bytes < (int64_t)p.bytes) return op_failed(XSM_ERR_CAPACITY, "the workspace is too small");
     char *ws = (char *)a->workspace;
@@ -163,7 +166,7 @@ xsm_status xsm_linear_logprobs_grad(const xsm_linear_logprobs_grad_args *a, void
     Z.tokens = a->tokens; Z.token_ld = a->token_stride; Z.token_bytes = a->token_bytes; Z.vocab = a->vocab;
     Z.inv_t = 1.f / a->temperature;
     Z.c = (float)(1.4426950408889634 / a->temperature);
-    Z.lse = a->lse; Z.g = a->g_logprob; Z.g_ld = a->g_logprob_stride; Z.g_lse = a->g_lse; Z.g_lse_ld = a->g_lse_stride;
+    Z.lse = a->lse; Z.given = logprob; Z.g = a->g_logprob; Z.g_ld = a->g_logprob_stride; Z.g_lse = a->g_lse; Z.g_lse_ld = a->g_lse_stride;
     Z.out[0] = ws + p.dz; Z.out_ld = p.piece; Z.low = p.low;
     Sums S = {};
     S.pairs = 1; S.low = p.low;

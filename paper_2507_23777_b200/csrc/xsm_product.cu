@@ -613,7 +613,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
                 constexpr int N = BN / 2 < 32 ? BN / 2 : 32;
                 const int col0 = w.n * BN + half * (BN / 2);
                 long long token = -1;
-                float g = 0.f, gp = 0.f, lse2 = 0.f;
+                float g = 0.f, gp = 0.f, gl = 0.f, lse2 = 0.f;
                 if (EPI == PR_STATS || EPI == PR_DLOGITS) {
                     if (live) {
                         token = A.token_bytes == 8 ? reinterpret_cast<const long long *>(A.tokens)[row * A.token_ld] : (long long)reinterpret_cast<const int *>(A.tokens)[row * A.token_ld];
@@ -626,11 +626,13 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
                                 if (w.n == 0 && half == 0) A.row_scale[row] = scale;
                             }
                             g = A.g && there ? A.g[row * A.g_ld] : 0.f;
-                            gp = g - (A.g_lse ? A.g_lse[row * A.g_lse_ld] : 0.f);
+                            gl = A.g_lse ? A.g_lse[row * A.g_lse_ld] : 0.f;
+                            gp = g - gl;
                             g *= A.inv_t * scale;
+                            gl *= A.inv_t * scale;
                             gp *= A.inv_t * scale;
                             lse2 = lse * kLog2e;
-                            if (lse == -INFINITY) g = gp = lse2 = 0.f;
+                            if (lse == -INFINITY) g = gl = gp = lse2 = 0.f;
                         }
                     }
                 }
@@ -768,7 +770,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
                             if (token >= col && token < col + N) {
 #pragma unroll
                                 for (int i = 0; i < N; ++i)
-                                    if (token == col + i) A.token_z[row] = __uint_as_float(v[i]) * A.inv_t;
+                                    if (token == col + i) A.token_z[row] = __uint_as_float(v[i]);
                             }
                             const float was = mx;
                             mx = fmaxf(mx, top * A.c);
@@ -782,9 +784,11 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
 #pragma unroll
                             for (int i = 0; i < N; ++i) x[i] = -gp * ex2(fmaf(__uint_as_float(v[i]), A.c, -lse2));
                             if (token >= col && token < col + N) {
+                                // g (1 - p) + g_lse p; 1 - p from the log probability: next to 1, z - lse has none of it left
+                                const float lp = A.given ? A.given[row] : 0.f, own = fmaf(gl, expf(lp), -g * expm1f(lp));
 #pragma unroll
                                 for (int i = 0; i < N; ++i)
-                                    if (token == col + i) x[i] += g;
+                                    if (token == col + i) x[i] = A.given ? own : x[i] + g;
                             }
                             if constexpr (CG == 2) {
                                 put_row<T>(buf, lane, (c & 32) / 8, x);
@@ -841,7 +845,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
 #pragma unroll 4
                     for (int i = lane; i < 2 * (int)gridDim.x; i += 32) r.take(__ldcg(&A.parts[(long long)row * 2 * gridDim.x + i]));
                     r.across_lanes();
-                    if (lane == 0) r.finish(A.tokens, A.token_ld, A.token_bytes, A.vocab, row, A.token_z, A.logprob, A.lse_out);
+                    if (lane == 0) r.finish(A.tokens, A.token_ld, A.token_bytes, A.vocab, row, A.token_z, A.c, A.to_lse, A.logprob, A.lse_out);
                 }
         }
     }

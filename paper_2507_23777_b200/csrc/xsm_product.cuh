@@ -66,12 +66,14 @@ struct ProductArgs {
     long long token_ld;
     int token_bytes, vocab0, vocab; // first token of this piece of the vocabulary, all tokens
     float c, inv_t;                 // log2(e) / T, 1 / T
+    double to_lse;                  // 1 / (c T)
     float2 *parts;                  // [part][m]: maximum, sum
     int carry;                      // one tile of rows: a CTA's parts are joined in its registers, parts are the CTAs'
     unsigned *counter;              // with carry: the CTA that comes last joins the CTAs' parts, [m][part], itself
     float *logprob, *lse_out;
-    float *token_z;                 // [m]
+    float *token_z;                 // [m], the token's sum
     const float *lse, *g, *g_lse;
+    const float *given;             // PR_DLOGITS: the forward pass' logprob, may be NULL
     long long g_ld, g_lse_ld;
 
     // PR_GATED_GRAD reads g_y, PR_GATED* and PR_DLOGITS write 16-bit rows
@@ -105,11 +107,18 @@ struct RowSums {
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) take(make_float2(__shfl_xor_sync(0xffffffffu, m, o), __shfl_xor_sync(0xffffffffu, sum, o)));
     }
-    __device__ __forceinline__ void finish(const void *tokens, long long token_ld, int token_bytes, int vocab, int row, const float *token_z, float *logprob, float *lse) const {
-        const float l = m == -INFINITY && sum == 0.f ? -INFINITY : (m + log2f(sum)) * 0.69314718056f;
+    // The maximum and the sums share what rounding c x maximum left, and all logits what they have in common: the token's logit less the maximum, less the logarithm of the sum, is off by
+    // its own size's rounding.  (z - lse is off by that of the logits: 3e-5 at 300, and above zero as often as below.)
+    __device__ __forceinline__ void finish(const void *tokens, long long token_ld, int token_bytes, int vocab, int row, const float *token_z, float c, double to_lse, float *logprob, float *lse) const {
+        const float s = log2f(sum), l = m == -INFINITY && sum == 0.f ? -INFINITY : (float)(((double)m + s) * to_lse);
         const long long t = token_bytes == 8 ? reinterpret_cast<const long long *>(tokens)[row * token_ld] : (long long)reinterpret_cast<const int *>(tokens)[row * token_ld];
         lse[row] = l;
-        logprob[row] = t < 0 || t >= vocab ? 0.f : l == -INFINITY ? -INFINITY : __ldcg(token_z + row) - l;
+        float p = 0.f;
+        if (t >= 0 && t < vocab) {
+            p = l == -INFINITY ? l : (fmaf(__ldcg(token_z + row), c, -m) - s) * 0.69314718056f;
+            if (p > 0.f) p = 0.f;
+        }
+        logprob[row] = p;
     }
 };
 

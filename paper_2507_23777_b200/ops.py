@@ -666,14 +666,15 @@ def _linear_forward(hidden, weight, tokens, temperature):
 
 def linear_logprobs_grad(hidden, weight, tokens, result, grad_logprob=None, grad_lse=None, temperature=1.0, need=(True, True)):
     """The gradients (d_hidden, d_weight), in their type, of sum(grad_logprob * logprob) + sum(grad_lse * lse) of what linear_logprobs returned as `result` for the
-    same hidden, weight, tokens and temperature.  grad_*: float32 [rows]; each may be missing.  need: which of the two are wanted; the other is None.  The
+    same hidden, weight, tokens and temperature (the log probabilities may be None: a token's element of a probability next to 1 is then as good as lse tells).  grad_*: float32 [rows]; each may be missing.  need: which of the two are wanted; the other is None.  The
     logits are computed again, at most 256 MiB of their gradients (or 1024 tokens' of each row) are in memory at a time.  There are no second derivatives: tensors that want a gradient are
     refused unless torch.no_grad() says that it is not needed."""
-    _no_gradient("linear_logprobs_grad", hidden, weight, result[1], grad_logprob, grad_lse)
+    _no_gradient("linear_logprobs_grad", hidden, weight, *result, grad_logprob, grad_lse)
     device, dtype, rows, d, ld, w_ld = _check_linear(hidden, weight, tokens)
-    lse = result[1]
-    if lse.shape != (rows,) or lse.dtype is not torch.float32 or lse.get_device() != device or rows > 1 and lse.stride(0) != 1:
-        raise ValueError("result must be what linear_logprobs returned for these hidden states")
+    logprob, lse = result
+    for t in (lse,) if logprob is None else (lse, logprob):
+        if t.shape != (rows,) or t.dtype is not torch.float32 or t.get_device() != device or rows > 1 and t.stride(0) != 1:
+            raise ValueError("result must be what linear_logprobs returned for these hidden states")
     gl, gl_ld = _row_grad(grad_logprob, rows, device, "grad_logprob")
     gs, gs_ld = _row_grad(grad_lse, rows, device, "grad_lse")
     lib, where, vocab, stream = binding.load(), hidden.device, weight.shape[0], _raw_stream(device)
@@ -687,7 +688,7 @@ def linear_logprobs_grad(hidden, weight, tokens, result, grad_logprob=None, grad
                                  d, d, n, rows, vocab, d, _DTYPES[dtype], _TOKENS[tokens.dtype], temperature)
     except _BEYOND as e:
         raise ValueError(f"an argument of linear_logprobs_grad is beyond its type: {e}") from None
-    status = lib.xsm_linear_logprobs_grad(args, stream)
+    status = lib.xsm_linear_logprobs_grad_near(args, 0 if logprob is None else logprob.data_ptr(), stream)
     if status:
         _check(status)
     return d_hidden, d_weight
@@ -697,7 +698,7 @@ class _LinearLogprobs(torch.autograd.Function):
     @staticmethod
     def forward(ctx, hidden, weight, tokens, temperature):
         r = _linear_forward(hidden, weight, tokens, temperature)
-        ctx.save_for_backward(hidden, weight, tokens, r.lse)
+        ctx.save_for_backward(hidden, weight, tokens, *r)
         ctx.temperature = temperature
         ctx.set_materialize_grads(False)
         return tuple(r)
@@ -705,11 +706,11 @@ class _LinearLogprobs(torch.autograd.Function):
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, g_logprob, g_lse):
-        hidden, weight, tokens, lse = ctx.saved_tensors
+        hidden, weight, tokens, *r = ctx.saved_tensors
         need = ctx.needs_input_grad[:2]
         if g_logprob is None and g_lse is None:
             return None, None, None, None
-        return *linear_logprobs_grad(hidden, weight, tokens, (None, lse), g_logprob, g_lse, ctx.temperature, need), None, None
+        return *linear_logprobs_grad(hidden, weight, tokens, r, g_logprob, g_lse, ctx.temperature, need), None, None
 
 
 def linear_logprobs(hidden, weight, tokens, temperature: float = 1.0) -> LinearLogprobs:

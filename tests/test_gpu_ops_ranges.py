@@ -204,3 +204,47 @@ def test_gated_gradients_of_ends_of_the_type(ops):
     for i in (1, 2):
         near(d[i][keep], bound[i][0][keep], bound[i][1][keep], "d_w")
         assert clean[i].isfinite().all()
+
+
+# --------------------------------------------------------------------------------------------------- logits in the hundreds
+
+def shifted(rows, vocab, dtype, common, seed, apart=0.0):
+    """Logits that are `common` and some eighths, exactly: whole numbers of hidden states and weights; the given token's is `apart` above.  The third column is the token's own."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    h, w = torch.zeros((rows, 64), device="cuda"), torch.zeros((vocab, 64), device="cuda")
+    h[:, 0], w[:, 0] = common, 1.0
+    h[:, 1], w[:, 1] = 1.0, torch.randint(-16, 17, (vocab,), generator=g, device="cuda") / 8
+    w[0, 1] += apart
+    w[0, 2] = 1.0
+    return h.to(dtype), w.to(dtype), torch.zeros(rows, dtype=torch.int64, device="cuda")
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("rows", [3, 40, 300])
+@pytest.mark.parametrize("vocab,apart", [(1, 0.0), (2, 0.0), (50, 12.0), (5000, 24.0), (5000, 0.0)])
+@pytest.mark.parametrize("common,temperature", [(240.0, 1.0), (-112.0, 0.7), (240.0, 0.25)])
+def test_what_all_logits_have_in_common_does_not_matter(ops, dtype, rows, vocab, apart, common, temperature):
+    """Log probabilities are no larger than zero and off by their own size's roundings, whatever the logits' size: differences to the maximum by 2^-23 (the factor's, the product's), exponentials
+    by 2^-22, their sum by one rounding for each 64 and 40 more, its logarithm by 2^-23 of itself.  lse is off by that and its own rounding.  A token's gradient is g (1 - p)."""
+    h, w, t = shifted(rows, vocab, dtype, common, 8, apart)
+    z = h.double() @ w.double().T / temperature
+    lse = torch.logsumexp(z, -1)
+    top = z.amax(-1)
+    want = (z - top[:, None])[:, 0] - torch.log(torch.exp(z - top[:, None]).sum(-1))
+    # (of the sum, 2^-22 for the exponentials but the maximum's, whose argument is what a rounding of 432 left)
+    slack = (1 - want.exp()) * ((z.max() - z.min()) * 2.0 ** -23 + 2.0 ** -22) + (vocab / 64 + 40) * 2.0 ** -24 * (vocab > 1) + 2.0 ** -22 + want.abs() * 2.0 ** -22
+    r = ops.linear_logprobs(h, w, t, temperature)
+    assert (r.logprob <= 0).all()
+    near(r.logprob, want, slack, "logprob")
+    near(r.lse, lse, slack + (lse - top).abs() * 2.0 ** -22 + lse.abs() * 2.0 ** -24, "lse")
+    g = torch.linspace(0.5, 2.0, rows, device="cuda")
+    gs = torch.linspace(-0.25, 0.25, rows, device="cuda")
+    with torch.no_grad():
+        d = ops.linear_logprobs_grad(h, w, t, r, g, gs, temperature, need=(True, False))[0]
+    p = want.exp()
+    own = (-torch.expm1(want) * g + p * gs) / temperature
+    # the element: logprob's error, the exponentials' 2^-23, the products'; rounded to dtype (in two parts of up to 128 rows) in the middle and in the end; fp16's steps next to 2^13
+    parts = 2 if rows <= 128 or vocab <= 64 else 1
+    bound = ((slack + 2.0 ** -22) * (p * (g + gs.abs())) + own.abs() * temperature * 2.0 ** -22) / temperature
+    bound = bound + ref.UNIT[dtype] ** parts * own.abs() + 2.0 ** -26 * (2 * g + gs.abs()) / temperature * (dtype is F16) + ref.UNIT[dtype] * own.abs() + ref.TINY[dtype]
+    near(d[:, 2], own, bound * 1.01, "d_hidden")
