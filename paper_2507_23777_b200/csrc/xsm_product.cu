@@ -298,7 +298,7 @@ template <typename T> __device__ __forceinline__ void put_row(uint32_t buf, int 
 template <int CG, int BN, int EPI, typename T>
 __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __grid_constant__ ProductMaps M, const __grid_constant__ ProductArgs A) {
     constexpr int TM = 128 * CG;
-    constexpr bool kGated = EPI == PR_GATED || EPI == PR_GATED_GRAD, kOut = EPI == PR_OUT, kRounds = EPI == PR_STATS && CG == 1;
+    constexpr bool kGated = EPI == PR_GATED || EPI == PR_GATED_GRAD, kOut = EPI == PR_OUT, kRounds = (EPI == PR_STATS || EPI == PR_DLOGITS) && CG == 1;
     extern __shared__ char smem_raw[];
     __shared__ __align__(8) uint64_t full[kMaxStages], empty[kMaxStages], sums_full[2], sums_empty[2], last;
     __shared__ uint32_t tmem_slot;
@@ -725,7 +725,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
                     }
                 } else {
                     // The tensor core cuts its sums off where they are added to: of few rows, where there is time for it, no more than 512 steps are added up there, and these here.
-                    // (13 x 24000 x 1824: lse off by 1.2e-6 of itself otherwise.)
+                    // (13 x 24000 x 1824: lse off by 1.2e-6 of itself otherwise; and the gradient's probabilities are those of the same sums.)
                     [[maybe_unused]] float z[kRounds ? BN / 2 : 1];
                     const bool more_z = kRounds && w.k1 - w.k0 > A.round;
                     if constexpr (kRounds) {

@@ -55,7 +55,7 @@ struct ProductArgs {
     int stages;                     // of the ring
     uint32_t stage, stage_b;        // bytes of a CTA's stage, where B begins in it
     int tma_out;                    // wide tiles: results leave by TMA
-    int round;                      // PR_STATS, one CTA a tile: stages after which the sums so far are added up outside the tensor core
+    int round;                      // PR_STATS, PR_DLOGITS, one CTA a tile: stages after which the sums so far are added up outside the tensor core
     long long low;                  // elements from a gradient (PR_OUT: from A) to what its rounding left, of few rows; 0: that is let go
     unsigned tries;                 // of a barrier, before a wait gives up
     int starve;                     // fetch nothing (xsm_debug_product_waits)

@@ -248,3 +248,27 @@ def test_what_all_logits_have_in_common_does_not_matter(ops, dtype, rows, vocab,
     bound = ((slack + 2.0 ** -22) * (p * (g + gs.abs())) + own.abs() * temperature * 2.0 ** -22) / temperature
     bound = bound + ref.UNIT[dtype] ** parts * own.abs() + 2.0 ** -26 * (2 * g + gs.abs()) / temperature * (dtype is F16) + ref.UNIT[dtype] * own.abs() + ref.TINY[dtype]
     near(d[:, 2], own, bound * 1.01, "d_hidden")
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("rows,vocab,d", [(3, 300, 2048), (100, 700, 4096), (300, 60, 4096), (7, 130, 8200)])
+def test_probabilities_of_long_sums_of_few_rows_add_up_to_one(ops, dtype, rows, vocab, d):
+    """Products of one sign, whose sums are cut off the same way step after step: the gradient by the logits adds up to g_lse, as near as sums of 512 steps at a time are (the first column of the
+    weights, which no hidden state meets, adds it up)."""
+    g = torch.Generator(device="cuda").manual_seed(9)
+    h, w = (torch.rand(s, generator=g, device="cuda") + 0.5 for s in ((rows, d), (vocab, d)))
+    h, w = h.to(dtype), (w * 20 / d).to(dtype)
+    h[:, 0], w[:, 0] = 0.0, 1.0
+    t = torch.randint(0, vocab, (rows,), generator=g, device="cuda")
+    gl, gs = torch.rand(rows, generator=g, device="cuda") + 0.5, torch.zeros(rows, device="cuda")
+    r = ops.linear_logprobs(h, w, t)
+    logprob, lse, z, b_logprob, b_lse, off = ref.linear(h, w, t, 1.0, few=True)
+    near(r.lse, lse, b_lse, "lse")
+    with torch.no_grad():
+        d_hidden = ops.linear_logprobs_grad(h, w, t, r, gl, gs, need=(True, False))[0]
+    # dz by what z and lse are off, two parts of the type, fp16's steps next to 2^13; their sum on the tensor core, both parts
+    p = (z - lse[:, None]).exp()
+    size = (p.sum(-1) + 1) * gl
+    slack = (p * (off + b_lse[:, None] + 2.0 ** -20).expm1()).sum(-1) * gl + ref.UNIT[dtype] ** 2 * size + vocab * 2.0 ** -26 * 2 * gl * (dtype is F16)
+    slack = slack + size * (-(-vocab // 16) + 2) * 2.0 ** -23 * 2
+    near(d_hidden[:, 0], torch.zeros(rows, device="cuda"), slack, "sum of the gradient by the logits")
