@@ -539,15 +539,16 @@ def _counter(device: int, stream: int) -> int:
 
 _KEPT = 1 << 20          # bytes of a workspace that is kept from call to call
 _scratch_of = threading.local()
-_sizes = {}              # by operator and sizes: bytes of its workspace
+_sizes = {}              # by operator, device and sizes: bytes of its workspace, which go by the device's SMs
 
 
-def _size_of(fn, *sizes) -> int:
-    n = _sizes.get((fn, sizes))
+def _size_of(fn, device: int, *sizes) -> int:
+    """What the library says of the current device."""
+    n = _sizes.get((fn, device, sizes))
     if n is None:
         if len(_sizes) > 4096:
             _sizes.clear()
-        n = _sizes[fn, sizes] = getattr(binding.load(), fn)(*sizes)
+        n = _sizes[fn, device, sizes] = getattr(binding.load(), fn)(*sizes)
     return n
 
 
@@ -651,7 +652,7 @@ def _linear_forward(hidden, weight, tokens, temperature):
     lib, where, vocab, stream = binding.load(), hidden.device, weight.shape[0], _raw_stream(device)
     logprob = _empty((rows,), (1,), dtype=torch.float32, device=where)
     lse = _empty((rows,), (1,), dtype=torch.float32, device=where)
-    n = _size_of("xsm_linear_logprobs_workspace", rows, vocab, d)
+    n = _size_of("xsm_linear_logprobs_workspace", device, rows, vocab, d)
     ws = _scratch(n, device, stream, where)
     try:
         args = _LINEAR.pack(hidden.data_ptr(), weight.data_ptr(), tokens.data_ptr(), logprob.data_ptr(), lse.data_ptr(), ws.data_ptr(), _status(device, stream),
@@ -680,7 +681,7 @@ def linear_logprobs_grad(hidden, weight, tokens, result, grad_logprob=None, grad
     lib, where, vocab, stream = binding.load(), hidden.device, weight.shape[0], _raw_stream(device)
     d_hidden = _empty((rows, d), (d, 1), dtype=dtype, device=where) if need[0] else None
     d_weight = _empty((vocab, d), (d, 1), dtype=dtype, device=where) if need[1] else None
-    n = _size_of("xsm_linear_logprobs_grad_workspace", rows, vocab, d)
+    n = _size_of("xsm_linear_logprobs_grad_workspace", device, rows, vocab, d)
     ws = _scratch(n, device, stream, where)
     try:
         args = _LINEAR_GRAD.pack(hidden.data_ptr(), weight.data_ptr(), tokens.data_ptr(), lse.data_ptr(), gl, gs, 0 if d_hidden is None else d_hidden.data_ptr(),
@@ -801,7 +802,7 @@ def gated_feed_forward_grad(x, w_gate, w_up, grad, activation: str = "silu", nee
     if need_gate or need_up:
         d_gate, d_up = _empty((ff, d), (d, 1), dtype=dtype, device=where), _empty((ff, d), (d, 1), dtype=dtype, device=where)
         to_gate, to_up = d_gate.data_ptr(), d_up.data_ptr()
-    n = _size_of("xsm_gated_ff_grad_workspace", rows, ff, d)
+    n = _size_of("xsm_gated_ff_grad_workspace", device, rows, ff, d)
     ws = _scratch(n, device, stream, where)
     try:
         args = _GATED_GRAD.pack(flat.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), g.data_ptr(), to_x, to_gate, to_up, ws.data_ptr(), _status(device, stream), _counter(device, stream),
@@ -955,7 +956,7 @@ def norm_rotate_grad(q, k, q_gain, k_gain, grad_q, grad_k, rope=None, positions=
         us, to_h, to_dk, to_dkg = d_k.stride(), grad_k.data_ptr(), d_k.data_ptr(), d_k_gain.data_ptr()
     if not ok:
         raise ValueError("grad_q and grad_k must be like q and k, with neighbouring elements of a head")
-    size = _size_of("xsm_norm_rotate_grad_workspace", sizes[4])
+    size = _size_of("xsm_norm_rotate_grad_workspace", device, sizes[4])
     ws = _scratch(size, device, stream, d_q.device if q is not None else d_k.device)
     try:
         args = _NORM_GRAD.pack(to_q, to_k, to_qg, to_kg, to_at, to_rope, to_g, to_h, to_dq, to_dk, to_dqg, to_dkg, ws.data_ptr(), _counter(device, stream), qs[0], qs[1], qs[2], ks[0], ks[1], ks[2],

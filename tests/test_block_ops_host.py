@@ -1,0 +1,26 @@
+"""The torch side of the operators on a caller's own activations and weights, and the paths that call them, where no device is needed."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2507_23777_b200 import binding, build, ops
+
+
+@pytest.fixture(scope="module")
+def lib():
+    build.build()
+    return binding.load()
+
+
+def test_sizes_of_workspaces_are_each_devices_own(monkeypatch):
+    """Devices of unequal numbers of SMs need workspaces of unequal sizes."""
+    class Lib:
+        current = 0
+
+        def xsm_linear_logprobs_workspace(self, rows, vocab, d):
+            return 1000 + self.current
+    fake = Lib()
+    monkeypatch.setattr(ops, "_sizes", {})
+    monkeypatch.setattr(ops.binding, "load", lambda: fake)
+    for fake.current in (0, 3, 0, 3):
+        assert ops._size_of("xsm_linear_logprobs_workspace", fake.current, 4, 100, 64) == 1000 + fake.current
