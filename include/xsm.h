@@ -447,7 +447,8 @@ typedef struct {
 } xsm_norm_rotate_args;
 XSM_API xsm_status xsm_norm_rotate(const xsm_norm_rotate_args *a, void *cuda_stream);
 
-/* The gradient of sum(g_q * q_out) + sum(g_k * k_out) by q, k and the gains (the latter in gain_dtype, added up in fp32 in an order of its own sizes' making). */
+/* The gradient of sum(g_q * q_out) + sum(g_k * k_out) by q, k and the gains (the latter in gain_dtype, added up in fp32 in an order of its own sizes' making; without heads they are not
+ * written). */
 typedef struct {
     const void *q, *k, *q_gain, *k_gain;  /* as above */
     const int32_t *positions;

@@ -73,3 +73,21 @@ with torch.no_grad():
     assert torch.equal(got, ops.gated_feed_forward_grad(x, w, w, gy)[0])
 """
     subprocess.run([sys.executable, "-c", code], check=True, cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))), timeout=300)
+
+
+@pytest.mark.parametrize("heads,kv_heads", [(0, 2), (2, 0), (0, 0), (0, None), (None, 0)])
+@pytest.mark.parametrize("batch,m", [(2, 3), (0, 3), (2, 0)])
+def test_gains_of_no_heads_have_gradients_of_zero(ops, heads, kv_heads, batch, m):
+    gains = [torch.ones(64, device="cuda"), torch.ones(64, device="cuda")]
+    torch.full((8, 64), float("nan"), device="cuda")          # (what new memory may hold)
+    x = [None if n is None else torch.ones((batch, m, n, 64), device="cuda") for n in (heads, kv_heads)]
+    gains = [None if t is None else g for t, g in zip(x, gains)]
+    for _ in range(3):
+        d = ops.norm_rotate_grad(*x, *gains, *x)
+        for n, t, dt, dg in zip((heads, kv_heads), x, d[:2], d[2:]):
+            assert dt is None if t is None else dt.shape == t.shape
+            if n == 0 or t is not None and batch * m == 0:
+                assert (dg == 0).all()
+            if dg is not None:
+                dg.fill_(float("nan"))                         # (so does the memory of the next)
+        del d, dt, dg
