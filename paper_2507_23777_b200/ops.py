@@ -946,12 +946,12 @@ def norm_rotate_grad(q, k, q_gain, k_gain, grad_q, grad_k, rope=None, positions=
     ok = (q is None) == (grad_q is None) and (k is None) == (grad_k is None)
     if ok and q is not None:
         gs = grad_q.stride()
-        ok = grad_q.shape == q.shape and grad_q.dtype is q.dtype and grad_q.get_device() == device and gs[3] == 1
+        ok = grad_q.shape == q.shape and grad_q.dtype is q.dtype and grad_q.get_device() == device and (gs[3] == 1 or grad_q.numel() == 0)
         d_q, d_q_gain = _like(q), torch.empty_like(q_gain) if sizes[2] else torch.zeros_like(q_gain)        # (heads: of none the library makes no sum)
         os, to_g, to_dq, to_dqg = d_q.stride(), grad_q.data_ptr(), d_q.data_ptr(), d_q_gain.data_ptr()
     if ok and k is not None:
         hs = grad_k.stride()
-        ok = grad_k.shape == k.shape and grad_k.dtype is k.dtype and grad_k.get_device() == device and hs[3] == 1
+        ok = grad_k.shape == k.shape and grad_k.dtype is k.dtype and grad_k.get_device() == device and (hs[3] == 1 or grad_k.numel() == 0)
         d_k, d_k_gain = _like(k), torch.empty_like(k_gain) if sizes[3] else torch.zeros_like(k_gain)
         us, to_h, to_dk, to_dkg = d_k.stride(), grad_k.data_ptr(), d_k.data_ptr(), d_k_gain.data_ptr()
     if not ok:

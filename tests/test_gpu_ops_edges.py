@@ -91,3 +91,19 @@ def test_gains_of_no_heads_have_gradients_of_zero(ops, heads, kv_heads, batch, m
             if dg is not None:
                 dg.fill_(float("nan"))                         # (so does the memory of the next)
         del d, dt, dg
+
+
+@pytest.mark.parametrize("shape", [(0, 3, 2, 64), (2, 0, 2, 64), (2, 3, 0, 64)])
+def test_empty_batches_are_trained(ops, shape):
+    """The gradient of a sum over nothing comes with strides of zero, which a copy of nothing keeps."""
+    q, k = (torch.ones(shape, device="cuda", requires_grad=True) for _ in range(2))
+    gains = [torch.ones(64, device="cuda", requires_grad=True) for _ in range(2)]
+    a, b = ops.norm_rotate(q, k, *gains)
+    d = torch.autograd.grad(a.sum() + b.sum(), [q, k, *gains])
+    assert d[0].shape == d[1].shape == shape and (d[2] == 0).all() and (d[3] == 0).all()
+    x = torch.ones((0, 4, 64), device="cuda", dtype=torch.bfloat16, requires_grad=True)
+    w = torch.ones((72, 64), device="cuda", dtype=torch.bfloat16, requires_grad=True)
+    d = torch.autograd.grad(ops.gated_feed_forward(x, w, w).sum(), [x, w])
+    assert d[0].shape == x.shape and (d[1] == 0).all()
+    d = torch.autograd.grad(ops.linear_logprobs(x.view(0, 64), w, torch.zeros(0, dtype=torch.int64, device="cuda")).logprob.sum(), [x, w])
+    assert d[0].shape == x.shape and (d[1] == 0).all()
