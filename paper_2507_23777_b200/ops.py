@@ -517,7 +517,7 @@ def _status(device: int, stream: int) -> int:
     t = _status_words.get(device)
     if t is None:
         t = _zeros_while_recording(16, device) if stream and _capturing() else torch.zeros(16, dtype=torch.uint8, device=f"cuda:{device}")
-        _status_words[device] = t
+        t = _status_words.setdefault(device, t)          # (another thread may have been first)
     return t.data_ptr()
 
 

@@ -24,3 +24,16 @@ def test_sizes_of_workspaces_are_each_devices_own(monkeypatch):
     monkeypatch.setattr(ops.binding, "load", lambda: fake)
     for fake.current in (0, 3, 0, 3):
         assert ops._size_of("xsm_linear_logprobs_workspace", fake.current, 4, 100, 64) == 1000 + fake.current
+
+
+def test_threads_share_a_devices_status_word(monkeypatch):
+    """Another thread makes the word while this one does: both use the first, which is the one that check reads."""
+    theirs = torch.zeros(16, dtype=torch.uint8)
+    words = {}
+
+    def zeros(*args, **kw):
+        words[2] = theirs
+        return torch.ones(16, dtype=torch.uint8)
+    monkeypatch.setattr(ops, "_status_words", words)
+    monkeypatch.setattr(ops.torch, "zeros", zeros)
+    assert ops._status(2, 0) == theirs.data_ptr() and words[2] is theirs
