@@ -91,7 +91,7 @@ static const char *wrong_shape(int rows, int vocab, int d, int dtype, int token_
     if (rows < 0 || vocab < 1 || d < 8 || d % 8) return "rows must not be negative, vocab positive, d a positive multiple of 8";
     if (rows > kMostRows || vocab > kMostRows || d > kMostRows) return "rows, vocab and d must not exceed 2^30";
     if (token_bytes != 4 && token_bytes != 8) return "token_bytes must be 4 or 8";
-    if (!(temperature > 0.f) || !(temperature < INFINITY) || !(1.f / temperature < INFINITY)) return "temperature must be positive and finite, and its reciprocal finite";
+    if (!(temperature > 0.f) || !(temperature < INFINITY) || !((float)(1.4426950408889634 / temperature) < INFINITY)) return "temperature must be positive and finite, and log2(e) times its reciprocal finite";
     return nullptr;
 }
 static bool rows_fit(const void *p, int64_t ld, int d) { return (uintptr_t)p % 16 == 0 && ld % 8 == 0 && ld >= d; }

@@ -37,3 +37,13 @@ def test_threads_share_a_devices_status_word(monkeypatch):
     monkeypatch.setattr(ops, "_status_words", words)
     monkeypatch.setattr(ops.torch, "zeros", zeros)
     assert ops._status(2, 0) == theirs.data_ptr() and words[2] is theirs
+
+
+@pytest.mark.parametrize("temperature", [4.2e-39, 3e-39])
+def test_temperatures_whose_factor_is_infinite_are_refused(lib, temperature):
+    """log2(e) / T is what logits are multiplied by: infinite, it makes NaN of every zero.  (1 / T is finite here.)"""
+    A = 4096
+    args = ops._LINEAR.pack(*8 * [A], 64, 64, 1, 1 << 30, 4, 100, 64, 1, 8, temperature)
+    assert lib.xsm_linear_logprobs(args, None) == binding.XSM_ERR_INVALID_ARG and b"temperature" in lib.xsm_last_error(None)
+    args = ops._LINEAR_GRAD.pack(*11 * [A], 64, 64, 1, 1, 1, 64, 64, 1 << 30, 4, 100, 64, 1, 8, temperature)
+    assert lib.xsm_linear_logprobs_grad(args, None) == binding.XSM_ERR_INVALID_ARG and b"temperature" in lib.xsm_last_error(None)
