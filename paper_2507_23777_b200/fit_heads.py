@@ -40,13 +40,20 @@ def _views(cfg: dict, Wf):
     return W
 
 
+def _need_bf16(cfg: dict):
+    if cfg["dtype"] != 1:
+        raise ValueError("the library's products are of 16-bit weights: the model must be a bf16 one")
+
+
 def backbone_hidden(cfg: dict, Wf, tokens: np.ndarray, cond: np.ndarray, device="cuda", library_products=False):
     """Final hidden states g_s = RMSNorm_f(h^N_s) of a whole token sequence under the causal mask (Eq. 1; block
     order and norms as in Sec. 4.1 and the library header): tensor [len(tokens), d_model] on `device`.
     Wf: all weights as one fp32 tensor on `device`.  library_products: the gated feed-forward parts by the library's operator (ops.gated_feed_forward, a GPU is needed), on
-    activations and weights that are rounded to bf16."""
+    activations and weights that are rounded to bf16; the model must be a bf16 one."""
     import torch
     import torch.nn.functional as F
+    if library_products:
+        _need_bf16(cfg)
     W = _views(cfg, Wf)
     L, d, H, dh = cfg["n_layers"], cfg["d_model"], cfg["n_heads"], cfg["d_head"]
     n, half = len(tokens), dh // 2
@@ -93,8 +100,10 @@ def fit_from_corpus(cfg: dict, weights: np.ndarray, seqs, conds, iters=300, lr=2
                     batch=4096, device="cuda", seed=0, library_loss=False, library_products=False):
     """seqs[i]: tokens x_0.. of mesh i (x_0 = BOS) generated by the backbone, conds[i]: its condition [C, d_cond].
     library_loss: cross-entropy and its gradient by the library's operator (ops.token_logprobs, a GPU is needed) instead of torch's.  library_products: the backbone's gated
-    feed-forward parts, and the loss straight from the heads' hidden states without logits (ops.linear_logprobs), by the library's operators in bf16.
+    feed-forward parts, and the loss straight from the heads' hidden states without logits (ops.linear_logprobs), by the library's operators in bf16 (bf16 models).
     Returns (weights with fitted heads, report)."""
+    if library_products:
+        _need_bf16(cfg)
     import torch
     import torch.nn.functional as F
     K, d, V = cfg["n_draft"], cfg["d_model"], cfg["vocab"]
@@ -217,7 +226,7 @@ def main():
     ap.add_argument("--iters", type=int, default=300)
     ap.add_argument("--lr", type=float, default=2e-5)
     ap.add_argument("--library-loss", action="store_true", help="cross-entropy and its gradient by the library's operator")
-    ap.add_argument("--library-products", action="store_true", help="gated feed-forward parts, and the loss without logits, by the library's operators in bf16")
+    ap.add_argument("--library-products", action="store_true", help="gated feed-forward parts, and the loss without logits, by the library's operators (bf16 models)")
     ap.add_argument("--eval-tokens", type=int, default=4096)
     ap.add_argument("--eval-seeds", type=int, nargs="*", default=None, help="mesh seeds to decode (default: the configuration's)")
     args = ap.parse_args()

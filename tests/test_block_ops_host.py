@@ -47,3 +47,15 @@ def test_temperatures_whose_factor_is_infinite_are_refused(lib, temperature):
     assert lib.xsm_linear_logprobs(args, None) == binding.XSM_ERR_INVALID_ARG and b"temperature" in lib.xsm_last_error(None)
     args = ops._LINEAR_GRAD.pack(*11 * [A], 64, 64, 1, 1, 1, 64, 64, 1 << 30, 4, 100, 64, 1, 8, temperature)
     assert lib.xsm_linear_logprobs_grad(args, None) == binding.XSM_ERR_INVALID_ARG and b"temperature" in lib.xsm_last_error(None)
+
+
+def test_heads_of_fp32_models_are_not_fitted_in_bf16():
+    """As scoring refuses it: the library's products would round weights that the model holds in 32 bits."""
+    from paper_2507_23777_b200 import fit_heads, inputs
+    cfg = inputs.config(0)
+    w = inputs.make_weights(cfg)
+    seqs, conds = [np.arange(4)] * 2, list(inputs.make_cond(cfg, 2))
+    with pytest.raises(ValueError, match="bf16"):
+        fit_heads.fit_from_corpus(cfg, w, seqs, conds, iters=0, device="cpu", library_products=True)
+    with pytest.raises(ValueError, match="bf16"):
+        fit_heads.backbone_hidden(cfg, torch.from_numpy(inputs.weights_as_f32(cfg, w).astype(np.float32)), seqs[0], conds[0], "cpu", library_products=True)
