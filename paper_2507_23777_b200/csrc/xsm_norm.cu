@@ -46,8 +46,6 @@ struct NormArgs {
     unsigned *counter;              // NM_GRAD: of blocks that have ended
 };
 
-template <typename T, int N> struct __align__(sizeof(T) * N > 16 ? 16 : sizeof(T) * N) Run { T e[N]; };
-
 __device__ __forceinline__ float gain_at(const void *p, int dtype, int i) {
     return dtype == XSM_F32 ? reinterpret_cast<const float *>(p)[i] : dtype == XSM_BF16 ? to_f(reinterpret_cast<const bf16 *>(p)[i]) : to_f(reinterpret_cast<const __half *>(p)[i]);
 }
