@@ -569,7 +569,9 @@ def _scratch(n: int, device: int, stream: int, where):
 def check(device=None):
     """Waits for the device (the current one) and raises an XsmError if a bounded wait of an earlier linear_logprobs, gated_feed_forward or gradient of
     theirs ran out there, replays of recorded ones among them (the results since the last check are void)."""
-    i = _current_device() if device is None else torch.device(device).index if not isinstance(device, int) else device
+    i = device if device is None or isinstance(device, int) else torch.device(device).index
+    if i is None:             # ("cuda" is the current one too)
+        i = _current_device()
     torch.cuda.synchronize(i)
     t = _status_words.get(i)
     if t is not None:

@@ -107,3 +107,19 @@ def test_empty_batches_are_trained(ops, shape):
     assert d[0].shape == x.shape and (d[1] == 0).all()
     d = torch.autograd.grad(ops.linear_logprobs(x.view(0, 64), w, torch.zeros(0, dtype=torch.int64, device="cuda")).logprob.sum(), [x, w])
     assert d[0].shape == x.shape and (d[1] == 0).all()
+
+
+@pytest.mark.parametrize("device", [None, 0, "cuda", "cuda:0", torch.device("cuda"), torch.device("cuda", 0)])
+def test_checks_of_a_device_by_any_of_its_names(ops, device):
+    from paper_2507_23777_b200 import binding
+    x = torch.ones((5, 64), device="cuda", dtype=torch.bfloat16)
+    lib = binding.load()
+    ops.check(device)
+    try:
+        lib.xsm_debug_product_waits(2000, 1)
+        ops.gated_feed_forward(x, x, x)
+        with pytest.raises(binding.XsmError, match="patience"):
+            ops.check(device)
+    finally:
+        lib.xsm_debug_product_waits(0, 0)
+    ops.check(device)
