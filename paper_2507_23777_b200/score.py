@@ -105,17 +105,20 @@ class Scorer:
             raise ValueError(f"tokens must be whole numbers in [0, {self.cfg['vocab']})")
         return torch.as_tensor(tokens.astype(np.int64), device="cuda")
 
-    def _check_waits(self):
+    def _check_waits(self, products: bool):
         gave_up = None
         for cache in self.cache + self.cond_cache:          # (all of them: none is to tell the next score of this one's)
             try:
                 cache.check()
             except binding.XsmError as e:
                 gave_up = e
+        if products:
+            try:
+                ops.check()
+            except binding.XsmError as e:
+                gave_up = e
         if gave_up is not None:
             raise gave_up
-        if self.library_products:
-            ops.check()
 
     @torch.no_grad()
     def score(self, cond, tokens, top: int = 0, temperature: float = 1.0) -> ops.TokenLogprobs:
@@ -129,7 +132,7 @@ class Scorer:
             z = self.logits(x[:, a:a + m], a).flatten(0, 1)
             r = ops.token_logprobs(z, x[:, a + 1:a + 1 + m].flatten(), top=top, temperature=temperature)
             parts.append([None if t is None else t.view(self.batch, m, *t.shape[1:]) for t in r])
-        self._check_waits()
+        self._check_waits(self.library_products)
         return ops.TokenLogprobs(*(None if p[0] is None else torch.cat(p, 1) for p in zip(*parts)))
 
     @torch.no_grad()
@@ -142,8 +145,7 @@ class Scorer:
         self.condition(cond)
         hidden = [self.hidden(x[:, a:min(a + WINDOW, x.shape[1] - 1)], a) for a in range(0, x.shape[1] - 1, WINDOW)]
         r = ops.linear_logprobs(torch.cat(hidden, 1).flatten(0, 1).bfloat16(), self._bf16("W0"), x[:, 1:].flatten(), temperature=temperature)
-        self._check_waits()
-        ops.check()
+        self._check_waits(True)
         return ops.LinearLogprobs(*(t.view(self.batch, -1) for t in r))
 
 

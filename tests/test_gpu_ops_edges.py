@@ -123,3 +123,28 @@ def test_checks_of_a_device_by_any_of_its_names(ops, device):
     finally:
         lib.xsm_debug_product_waits(0, 0)
     ops.check(device)
+
+
+@pytest.mark.parametrize("first", ["score", "likelihood"])
+def test_a_score_that_gave_up_says_nothing_of_the_next(ops, first):
+    """Attention and products give up in the same score: the next one, of either kind, is told of neither."""
+    import numpy as np
+
+    from conftest import gpu_cfg
+    from paper_2507_23777_b200 import binding, inputs, score
+    cfg = gpu_cfg(dtype=1)
+    s = score.Scorer(cfg, inputs.make_weights(cfg), 1, 40, library_products=True)
+    cond, tokens = inputs.make_cond(cfg, 1), np.arange(40)[None]
+    want = s.likelihood(cond, tokens).logprob
+    lib = binding.load()
+    try:
+        lib.xsm_debug_product_waits(2000, 1)
+        for c in s.cache:
+            lib.xsm_debug_kv_waits(c._h, 2000, 1)
+        with pytest.raises(binding.XsmError):
+            getattr(s, first)(cond, tokens)
+    finally:
+        lib.xsm_debug_product_waits(0, 0)
+        for c in s.cache:
+            lib.xsm_debug_kv_waits(c._h, 0, 0)
+    assert torch.equal(s.likelihood(cond, tokens).logprob, want)
