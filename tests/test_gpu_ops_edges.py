@@ -148,3 +148,56 @@ def test_a_score_that_gave_up_says_nothing_of_the_next(ops, first):
         for c in s.cache:
             lib.xsm_debug_kv_waits(c._h, 0, 0)
     assert torch.equal(s.likelihood(cond, tokens).logprob, want)
+
+
+def test_threads_that_share_a_stream(ops):
+    """Counters are the stream's, scratch is a thread's: four threads' calls follow each other on one stream in any order."""
+    stream = torch.cuda.Stream()
+    work = []
+    for i, dtype in enumerate((torch.bfloat16, torch.float16, torch.bfloat16, torch.float16)):
+        g = torch.Generator(device="cuda").manual_seed(i)
+        rows = (5, 300, 9000, 40)[i]
+        h, w = (torch.randn((n, 64), generator=g, device="cuda").to(dtype) for n in (rows, 520))
+        t = torch.randint(0, 520, (rows,), generator=g, device="cuda")
+        gl, gy = torch.randn(rows, generator=g, device="cuda"), torch.randn((rows, 520), generator=g, device="cuda").to(dtype)
+        q, gain = torch.randn((1, rows, 3, 64), generator=g, device="cuda").to(dtype), torch.ones(64, device="cuda")
+
+        def calls(h=h, w=w, t=t, gl=gl, gy=gy, q=q, gain=gain):
+            r = ops.linear_logprobs(h, w, t)
+            return [*r, *ops.linear_logprobs_grad(h, w, t, r, gl), *ops.gated_feed_forward_grad(h, w, w, gy), *ops.norm_rotate_grad(q, q, gain, gain, q, q)]
+        work.append((calls, calls()))
+    torch.cuda.synchronize()
+    go, out = threading.Barrier(len(work)), [None] * len(work)
+
+    def run(i):
+        try:
+            with torch.cuda.stream(stream):
+                go.wait()
+                out[i] = [work[i][0]() for _ in range(20)]
+        except Exception as e:
+            out[i] = e
+    threads = [threading.Thread(target=run, args=(i,)) for i in range(len(work))]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    for got, (_, want) in zip(out, work):
+        assert not isinstance(got, Exception), got
+        for x in got:
+            assert all(torch.equal(a, b) for a, b in zip(x, want))
+
+
+def test_gradients_of_a_decoding_heads_loss(ops):
+    """A head's loss as its fitting takes it, hidden states and weights rounded to bf16 on the way: five tensors are rounded by 2^-8 of an element at most each, which bounds a gradient's norm, twice
+    where it comes through both factors."""
+    g = torch.Generator(device="cuda").manual_seed(3)
+    x, w1, wo = torch.randn((500, 96), generator=g, device="cuda"), torch.randn((96, 96), generator=g, device="cuda") / 10, torch.randn((300, 96), generator=g, device="cuda") / 10
+    t = torch.randint(0, 300, (500,), generator=g, device="cuda")
+    leaves = [w1.clone().requires_grad_(), wo.clone().requires_grad_()]
+    silu = torch.nn.functional.silu
+    got = torch.autograd.grad(-ops.linear_logprobs((x + silu(x @ leaves[0].T)).bfloat16(), leaves[1].bfloat16(), t).logprob.mean(), leaves)
+    wide = [v.double().requires_grad_() for v in (w1, wo)]
+    want = torch.autograd.grad(torch.nn.functional.cross_entropy((x.double() + silu(x.double() @ wide[0].T)) @ wide[1].T, t), wide)
+    for a, b in zip(got, want):
+        assert float((a.double() - b).norm()) <= 10 * 2.0 ** -8 * float(b.norm())
