@@ -109,6 +109,12 @@ def _forget_graphs():
         del _recorded[key]
 
 
+def _zeros(n: int, device: int):
+    """Zeroed memory that is kept from call to call; it may be written to in any mode, inference mode or not, whichever it is made in."""
+    with torch.inference_mode(False):
+        return torch.zeros(n, dtype=torch.uint8, device=f"cuda:{device}")
+
+
 def _zeros_while_recording(n: int, device: int):
     """Zeroed memory that is no part of the graph that is being recorded, and ready when this returns."""
     lib = binding.load()
@@ -119,7 +125,7 @@ def _zeros_while_recording(n: int, device: int):
             while lib.xsm_capture_id(side.cuda_stream):      # (torch hands its streams out in turn)
                 side = torch.cuda.Stream()
             with torch.cuda.stream(side):
-                t = torch.zeros(n, dtype=torch.uint8, device=f"cuda:{device}")
+                t = _zeros(n, device)
             side.synchronize()
         finally:
             lib.xsm_capture_mode(before)
@@ -307,7 +313,7 @@ class PagedCache:
             return self._workspace_of_graph(stream, need)
         ws, size = self._ws.get(stream, (None, 0))
         if size < need:
-            old, (ws, size) = ws, (torch.zeros(need, dtype=torch.uint8, device=self.k.device), need)
+            old, (ws, size) = ws, (_zeros(need, self.device), need)
             self._ws[stream] = ws, size
             if old is not None:
                 self._outgrown.append(old)
@@ -516,7 +522,7 @@ def _status(device: int, stream: int) -> int:
     """Address of the device's status word."""
     t = _status_words.get(device)
     if t is None:
-        t = _zeros_while_recording(16, device) if stream and _capturing() else torch.zeros(16, dtype=torch.uint8, device=f"cuda:{device}")
+        t = _zeros_while_recording(16, device) if stream and _capturing() else _zeros(16, device)
         t = _status_words.setdefault(device, t)          # (another thread may have been first)
     return t.data_ptr()
 
@@ -533,7 +539,7 @@ def _counter(device: int, stream: int) -> int:
         return r.counter.data_ptr()
     t = _counters.get((device, stream))
     if t is None:
-        t = _counters.setdefault((device, stream), torch.zeros(4 * binding.XSM_COUNTERS, dtype=torch.uint8, device=f"cuda:{device}"))
+        t = _counters.setdefault((device, stream), _zeros(4 * binding.XSM_COUNTERS, device))
     return t.data_ptr()
 
 

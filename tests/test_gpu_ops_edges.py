@@ -201,3 +201,38 @@ def test_gradients_of_a_decoding_heads_loss(ops):
     want = torch.autograd.grad(torch.nn.functional.cross_entropy((x.double() + silu(x.double() @ wide[0].T)) @ wide[1].T, t), wide)
     for a, b in zip(got, want):
         assert float((a.double() - b).norm()) <= 10 * 2.0 ** -8 * float(b.norm())
+
+
+@pytest.mark.parametrize("recorded", [False, True])
+def test_waits_that_ran_out_in_inference_mode_are_told_outside(ops, monkeypatch, recorded):
+    """What calls keep is made in inference mode here, and cleared outside of it."""
+    from paper_2507_23777_b200 import binding
+    monkeypatch.setattr(ops, "_status_words", {})
+    monkeypatch.setattr(ops, "_counters", {})
+    lib = binding.load()
+    x = torch.ones((5, 64), device="cuda", dtype=torch.bfloat16)
+    q = torch.ones((1, 2, 2, 64), device="cuda", dtype=torch.bfloat16)
+    table, length = torch.zeros((1, 1), dtype=torch.int32, device="cuda"), torch.full((1,), 16, dtype=torch.int32, device="cuda")
+    cache = ops.PagedCache(*(torch.ones((1, 2, 16, 64), device="cuda", dtype=torch.bfloat16) for _ in range(2)))
+
+    def calls():
+        ops.gated_feed_forward_grad(x, x, x, x[:, :5].contiguous())
+        cache.attend(q, table, length)
+    try:
+        lib.xsm_debug_product_waits(2000, 1)
+        lib.xsm_debug_kv_waits(cache._h, 2000, 1)
+        with torch.inference_mode():
+            if recorded:
+                graph = torch.cuda.CUDAGraph()
+                with torch.cuda.graph(graph):
+                    calls()
+                graph.replay()
+            else:
+                calls()
+        for check in (ops.check, cache.check):
+            with pytest.raises(binding.XsmError, match="patience"):
+                check()
+            check()
+    finally:
+        lib.xsm_debug_product_waits(0, 0)
+        lib.xsm_debug_kv_waits(cache._h, 0, 0)
