@@ -374,6 +374,8 @@ typedef struct {
 } xsm_linear_logprobs_args;
 XSM_API size_t xsm_linear_logprobs_workspace(int rows, int vocab, int d);
 XSM_API xsm_status xsm_linear_logprobs(const xsm_linear_logprobs_args *a, void *cuda_stream);
+/* The same, and logprob once more (DEVICE [rows], may be NULL), for a gradient that is to find it whatever becomes of the first. */
+XSM_API xsm_status xsm_linear_logprobs_keep(const xsm_linear_logprobs_args *a, float *kept, void *cuda_stream);
 
 /* The gradient of sum_rows (g_logprob logprob + g_lse lse) by hidden and weight, in their type, from lse of the call above:
  *   dz_rj = ([j = token_r] g_logprob_r - exp(z_rj - lse_r) (g_logprob_r - g_lse_r)) / temperature,  d_hidden = dz . weight,  d_weight = dz^T . hidden.

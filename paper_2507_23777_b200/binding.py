@@ -28,7 +28,7 @@ EXPORTS = [
     "xsm_kv_attend", "xsm_debug_kv_waits", "xsm_capture_id", "xsm_capture_watch", "xsm_capture_gone", "xsm_capture_mode",
     "xsm_token_logprobs", "xsm_token_logprobs_grad",
     "xsm_token_logprobs_grad_near",
-    "xsm_linear_logprobs_workspace", "xsm_linear_logprobs", "xsm_linear_logprobs_grad_workspace", "xsm_linear_logprobs_grad", "xsm_linear_logprobs_grad_near",
+    "xsm_linear_logprobs_workspace", "xsm_linear_logprobs", "xsm_linear_logprobs_keep", "xsm_linear_logprobs_grad_workspace", "xsm_linear_logprobs_grad", "xsm_linear_logprobs_grad_near",
     "xsm_gated_ff", "xsm_gated_ff_grad_workspace", "xsm_gated_ff_grad", "xsm_debug_product_waits",
     "xsm_norm_rotate", "xsm_norm_rotate_grad_workspace", "xsm_norm_rotate_grad", "xsm_kv_append_norm",
 ]
@@ -122,6 +122,7 @@ def load(path: str | None = None):
     for name in ("linear_logprobs", "linear_logprobs_grad", "gated_ff_grad"):
         f = getattr(L, f"xsm_{name}_workspace")
         f.restype, f.argtypes = C.c_size_t, [C.c_int, C.c_int, C.c_int]
+    L.xsm_linear_logprobs_keep.argtypes = [vp, vp, vp]
     L.xsm_linear_logprobs_grad_near.argtypes = [vp, vp, vp]
     L.xsm_norm_rotate_grad_workspace.restype, L.xsm_norm_rotate_grad_workspace.argtypes = C.c_size_t, [C.c_int]
     L.xsm_kv_append_norm.argtypes = [vp, vp, vp, vp]

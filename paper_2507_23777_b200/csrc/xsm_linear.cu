@@ -20,7 +20,7 @@ constexpr int kRowsLookedThrough = 8192;            // so many rows every CTA lo
 
 // Eight rows a block; thread (row, y) joins parts y, y + 32, ...  (32 rows a block, eight threads a row: 145 us for 96 rows of 4096 parts.)
 __global__ void __launch_bounds__(256) join_stats_kernel(const float2 *parts, const float *token_z, const void *tokens, long long token_ld, int token_bytes, int rows, int vocab,
-                                                         int n, float c, double to_lse, float *logprob, float *lse) {
+                                                         int n, float c, double to_lse, float *logprob, float *lse, float *kept) {
     chain_go();
     chain_wait();
     __shared__ float2 s[32][9];
@@ -38,7 +38,7 @@ __global__ void __launch_bounds__(256) join_stats_kernel(const float2 *parts, co
     r.m = s[lane][threadIdx.x >> 5].x;
     r.sum = s[lane][threadIdx.x >> 5].y;
     r.across_lanes();
-    if (lane == 0) r.finish(tokens, token_ld, token_bytes, vocab, at, token_z, c, to_lse, logprob, lse);
+    if (lane == 0) r.finish(tokens, token_ld, token_bytes, vocab, at, token_z, c, to_lse, logprob, lse, kept);
 }
 
 // One tile of rows: a CTA joins what its tiles find in its registers, and there are two parts for each CTA.
@@ -105,14 +105,16 @@ size_t xsm_linear_logprobs_workspace(int rows, int vocab, int d) {
     return up((size_t)plan_linear(rows, vocab, d).parts * rows * 8) + up((size_t)rows * 4);
 }
 
-xsm_status xsm_linear_logprobs(const xsm_linear_logprobs_args *a, void *cuda_stream) {
+xsm_status xsm_linear_logprobs(const xsm_linear_logprobs_args *a, void *cuda_stream) { return xsm_linear_logprobs_keep(a, nullptr, cuda_stream); }
+
+xsm_status xsm_linear_logprobs_keep(const xsm_linear_logprobs_args *a, float *kept, void *cuda_stream) {
     if (!a) return op_failed(XSM_ERR_INVALID_ARG, "null argument");
     if (const char *w = wrong_shape(a->rows, a->vocab, a->d, a->dtype, a->token_bytes, a->temperature)) return op_failed(XSM_ERR_INVALID_ARG, w);
     if (a->rows == 0) return XSM_OK;
     if (!a->hidden || !a->weight || !a->tokens || !a->logprob || !a->lse || !a->workspace || !a->status) return op_failed(XSM_ERR_INVALID_ARG, "null argument");
     if (!rows_fit(a->hidden, a->hidden_stride, a->d) || !rows_fit(a->weight, a->weight_stride, a->d))
         return op_failed(XSM_ERR_INVALID_ARG, "rows of hidden and weight must be 16-byte aligned and must not overlap");
-    if ((uintptr_t)a->tokens % a->token_bytes || ((uintptr_t)a->logprob | (uintptr_t)a->lse | (uintptr_t)a->status | (uintptr_t)a->counters) % 4 || (uintptr_t)a->workspace % 16)
+    if ((uintptr_t)a->tokens % a->token_bytes || ((uintptr_t)a->logprob | (uintptr_t)kept | (uintptr_t)a->lse | (uintptr_t)a->status | (uintptr_t)a->counters) % 4 || (uintptr_t)a->workspace % 16)
         return op_failed(XSM_ERR_INVALID_ARG, "tokens, logprob, lse, status and counters must be aligned to their elements, workspace to 16 bytes");
     if (a->workspace_bytes < (int64_t)xsm_linear_logprobs_workspace(a->rows, a->vocab, a->d)) return op_failed(XSM_ERR_CAPACITY, "the workspace is too small");
     const LinearPlan p = plan_linear(a->rows, a->vocab, a->d);
@@ -126,14 +128,14 @@ xsm_status xsm_linear_logprobs(const xsm_linear_logprobs_args *a, void *cuda_str
     A.carry = p.carry;
     // (few rows: the last CTA joins the parts itself, 5 x 4096 7.8 -> 7.3 us and a launch less; of 96 rows that takes one CTA 15 us)
     if (p.carry && !p.cut.wide && a->rows <= 16) A.counter = a->counters;
-    A.logprob = a->logprob; A.lse_out = a->lse;
+    A.logprob = a->logprob; A.lse_out = a->lse; A.kept = kept;
     A.token_z = (float *)((char *)a->workspace + up((size_t)p.parts * a->rows * 8));
     const Operand h = {a->hidden, a->rows, a->d, a->hidden_stride}, w[2] = {{a->weight, a->vocab, a->d, a->weight_stride}, {}};
     const cudaStream_t st = (cudaStream_t)cuda_stream;
     cudaError_t e = launch_product(PR_STATS, a->dtype, p.cut, A, a->rows, a->vocab, h, w, st);
     if (e == cudaSuccess && !A.counter)
         e = launch_early(join_stats_kernel, dim3((unsigned)((a->rows + 7) / 8)), dim3(256), 0, st, (const float2 *)A.parts, (const float *)A.token_z, a->tokens, (long long)a->token_stride,
-                         (int)a->token_bytes, (int)a->rows, (int)a->vocab, (int)p.parts, A.c, A.to_lse, a->logprob, a->lse);
+                         (int)a->token_bytes, (int)a->rows, (int)a->vocab, (int)p.parts, A.c, A.to_lse, a->logprob, a->lse, kept);
     return launched(e);
 }
 

@@ -845,7 +845,7 @@ __global__ void __launch_bounds__(kProductThreads, 1) product_kernel(const __gri
 #pragma unroll 4
                     for (int i = lane; i < 2 * (int)gridDim.x; i += 32) r.take(__ldcg(&A.parts[(long long)row * 2 * gridDim.x + i]));
                     r.across_lanes();
-                    if (lane == 0) r.finish(A.tokens, A.token_ld, A.token_bytes, A.vocab, row, A.token_z, A.c, A.to_lse, A.logprob, A.lse_out);
+                    if (lane == 0) r.finish(A.tokens, A.token_ld, A.token_bytes, A.vocab, row, A.token_z, A.c, A.to_lse, A.logprob, A.lse_out, A.kept);
                 }
         }
     }

@@ -70,7 +70,7 @@ struct ProductArgs {
     float2 *parts;                  // [part][m]: maximum, sum
     int carry;                      // one tile of rows: a CTA's parts are joined in its registers, parts are the CTAs'
     unsigned *counter;              // with carry: the CTA that comes last joins the CTAs' parts, [m][part], itself
-    float *logprob, *lse_out;
+    float *logprob, *lse_out, *kept;        // kept: logprob once more, may be NULL
     float *token_z;                 // [m], the token's sum
     const float *lse, *g, *g_lse;
     const float *given;             // PR_DLOGITS: the forward pass' logprob, may be NULL
@@ -109,7 +109,7 @@ struct RowSums {
     }
     // The maximum and the sums share what rounding c x maximum left, and all logits what they have in common: the token's logit less the maximum, less the logarithm of the sum, is off by
     // its own size's rounding.  (z - lse is off by that of the logits: 3e-5 at 300, and above zero as often as below.)
-    __device__ __forceinline__ void finish(const void *tokens, long long token_ld, int token_bytes, int vocab, int row, const float *token_z, float c, double to_lse, float *logprob, float *lse) const {
+    __device__ __forceinline__ void finish(const void *tokens, long long token_ld, int token_bytes, int vocab, int row, const float *token_z, float c, double to_lse, float *logprob, float *lse, float *kept) const {
         const float s = log2f(sum), l = m == -INFINITY && sum == 0.f ? -INFINITY : (float)(((double)m + s) * to_lse);
         const long long t = token_bytes == 8 ? reinterpret_cast<const long long *>(tokens)[row * token_ld] : (long long)reinterpret_cast<const int *>(tokens)[row * token_ld];
         lse[row] = l;
@@ -119,6 +119,7 @@ struct RowSums {
             if (p > 0.f) p = 0.f;
         }
         logprob[row] = p;
+        if (kept) kept[row] = p;
     }
 };
 

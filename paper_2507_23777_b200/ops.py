@@ -655,7 +655,8 @@ def _check_linear(hidden, weight, tokens):
     return device, dtype, rows, d, ld, w_ld
 
 
-def _linear_forward(hidden, weight, tokens, temperature):
+def _linear_forward(hidden, weight, tokens, temperature, kept=None):
+    """kept: a place for the log probabilities once more"""
     device, dtype, rows, d, ld, w_ld = _check_linear(hidden, weight, tokens)
     lib, where, vocab, stream = binding.load(), hidden.device, weight.shape[0], _raw_stream(device)
     logprob = _empty((rows,), (1,), dtype=torch.float32, device=where)
@@ -667,7 +668,7 @@ def _linear_forward(hidden, weight, tokens, temperature):
                             _counter(device, stream) if rows <= 16 else 0, ld, w_ld, tokens.stride(0), n, rows, vocab, d, _DTYPES[dtype], _TOKENS[tokens.dtype], temperature)
     except _BEYOND as e:
         raise ValueError(f"an argument of linear_logprobs is beyond its type: {e}") from None
-    status = lib.xsm_linear_logprobs(args, stream)
+    status = lib.xsm_linear_logprobs_keep(args, 0 if kept is None else kept.data_ptr(), stream)
     if status:
         _check(status)
     return LinearLogprobs(logprob, lse)
@@ -706,8 +707,9 @@ def linear_logprobs_grad(hidden, weight, tokens, result, grad_logprob=None, grad
 class _LinearLogprobs(torch.autograd.Function):
     @staticmethod
     def forward(ctx, hidden, weight, tokens, temperature):
-        r = _linear_forward(hidden, weight, tokens, temperature)
-        ctx.save_for_backward(hidden, weight, tokens, *r)
+        kept = torch.empty(hidden.shape[:1], dtype=torch.float32, device=hidden.device)        # (the caller may write to the log probabilities, to mask them for one)
+        r = _linear_forward(hidden, weight, tokens, temperature, kept)
+        ctx.save_for_backward(hidden, weight, tokens, kept, r.lse)
         ctx.temperature = temperature
         ctx.set_materialize_grads(False)
         return tuple(r)

@@ -272,3 +272,18 @@ def test_probabilities_of_long_sums_of_few_rows_add_up_to_one(ops, dtype, rows, 
     slack = (p * (off + b_lse[:, None] + 2.0 ** -20).expm1()).sum(-1) * gl + ref.UNIT[dtype] ** 2 * size + vocab * 2.0 ** -26 * 2 * gl * (dtype is F16)
     slack = slack + size * (-(-vocab // 16) + 2) * 2.0 ** -23 * 2
     near(d_hidden[:, 0], torch.zeros(rows, device="cuda"), slack, "sum of the gradient by the logits")
+
+
+@pytest.mark.parametrize("rows", [5, 40, 300])
+def test_log_probabilities_may_be_masked_in_place(ops, rows):
+    """The backward pass needs none of what the caller writes to."""
+    h, w, t, gl, _ = loss_inputs(rows, 300, 64, BF16, seed=10)
+    h.requires_grad_()
+    w.requires_grad_()
+    mask = (torch.arange(rows, device="cuda") % 3 > 0).float()
+    r = ops.linear_logprobs(h, w, t)
+    want = torch.autograd.grad((r.logprob * mask * gl).sum(), [h, w])
+    r = ops.linear_logprobs(h, w, t)
+    r.logprob.mul_(mask * gl)
+    got = torch.autograd.grad(r.logprob.sum(), [h, w])
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
