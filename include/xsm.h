@@ -383,7 +383,7 @@ XSM_API xsm_status xsm_linear_logprobs_keep(const xsm_linear_logprobs_args *a, f
  * rounded to dtype once (up to 128 rows or 64 tokens: held in two parts of it; fp16: scaled by
  * a power of two that takes its largest possible element to 2^13, rows whose elements are below 2^-12 of that by up to 2^14 more, and back in the sums; g_logprob of rows without a token
  * does not count, nor what rows with an lse of -infinity have).  The workspace holds a
- * piece of dz of at most 256 MiB (1024 tokens at least) and partial sums.  d_hidden or d_weight may be NULL. */
+ * piece of dz of at most 256 MiB (1024 tokens at least), fp16's scaled rows of hidden and partial sums.  d_hidden or d_weight may be NULL. */
 typedef struct {
     const void *hidden, *weight, *tokens; /* as above */
     const float *lse;                     /* DEVICE [rows] */

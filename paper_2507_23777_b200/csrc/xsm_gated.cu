@@ -6,7 +6,7 @@
 // would spare a quarter of the work and double the gradients' error; kept in fp32 they cost as much to move as to compute.)
 //
 // What bounds it.  8192 rows, 4096 of 1024: forward 91 us = 1.51 PFLOP/s, gradient 307 = 1.34: 104 us for gate and up again, 190 for 256 tiles of 74 at a time, which
-// leave the last round half empty.  4001 rows, 8192 of 2048: 186 us, 1.44 PFLOP/s.  Five rows, 4096 of 1024: 8 us, of which the weights' bytes are 2.6.
+// leave the last round half empty.  4001 rows, 8192 of 2048: 191 us, 1.41 PFLOP/s.  Five rows, 4096 of 1024: 8 us, of which the weights' bytes are 2.6.
 #include "xsm_product.cuh"
 
 namespace xsm {

@@ -676,9 +676,10 @@ def _linear_forward(hidden, weight, tokens, temperature, kept=None):
 
 def linear_logprobs_grad(hidden, weight, tokens, result, grad_logprob=None, grad_lse=None, temperature=1.0, need=(True, True)):
     """The gradients (d_hidden, d_weight), in their type, of sum(grad_logprob * logprob) + sum(grad_lse * lse) of what linear_logprobs returned as `result` for the
-    same hidden, weight, tokens and temperature (the log probabilities may be None: a token's element of a probability next to 1 is then as good as lse tells).  grad_*: float32 [rows]; each may be missing.  need: which of the two are wanted; the other is None.  The
-    logits are computed again, at most 256 MiB of their gradients (or 1024 tokens' of each row) are in memory at a time.  There are no second derivatives: tensors that want a gradient are
-    refused unless torch.no_grad() says that it is not needed."""
+    same hidden, weight, tokens and temperature (the log probabilities may be None: a token's element of a probability next to 1 is then as good as lse tells).  grad_*: float32 [rows]; each
+    may be missing.  need: which of the two are wanted; the other is None.  The logits are computed again, at most 256 MiB of their gradients (or 1024 tokens' of each row) are in memory at a
+    time, rounded to the type (up to 128 rows or 64 tokens: held in two parts of it); in fp16 every row is scaled into its range there, rows 2^26 and more below the largest lose bits.  There
+    are no second derivatives: tensors that want a gradient are refused unless torch.no_grad() says that it is not needed."""
     _no_gradient("linear_logprobs_grad", hidden, weight, *result, grad_logprob, grad_lse)
     device, dtype, rows, d, ld, w_ld = _check_linear(hidden, weight, tokens)
     logprob, lse = result
@@ -787,8 +788,9 @@ def _gated_forward(x, w_gate, w_up, activation):
 
 def gated_feed_forward_grad(x, w_gate, w_up, grad, activation: str = "silu", need=(True, True, True)):
     """The gradients (d_x, d_w_gate, d_w_up), in their type, of sum(grad * out) of what gated_feed_forward returned for the same arguments.  grad: like out,
-    neighbouring elements in a row.  need: which are wanted (the last two go together); the others are None.  There are no second derivatives: tensors that want a
-    gradient are refused unless torch.no_grad() says that it is not needed."""
+    neighbouring elements in a row.  need: which are wanted (the last two go together); the others are None.  The gradients by gate and up are rounded to the type in the middle (up to
+    128 rows or 32 columns: held in two parts of it); in fp16 every row is scaled into its range there, rows 2^26 and more below the largest lose bits.  There are no second derivatives: tensors that
+    want a gradient are refused unless torch.no_grad() says that it is not needed."""
     _no_gradient("gated_feed_forward_grad", x, w_gate, w_up, grad)
     device, dtype, flat, rows, ff, d, ld, g_ld, u_ld, kind = _check_gated(x, w_gate, w_up, activation)
     g = grad
