@@ -287,3 +287,25 @@ def test_log_probabilities_may_be_masked_in_place(ops, rows):
     r.logprob.mul_(mask * gl)
     got = torch.autograd.grad(r.logprob.sum(), [h, w])
     assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@pytest.mark.parametrize("rows,ff", [(7, 90), (300, 24), (300, 515), (9001, 40)])
+@pytest.mark.parametrize("need", [(True, False), (False, True)])
+def test_some_gradients_of_rows_of_unequal_size_in_fp16(ops, rows, ff, need):
+    """Each gradient by itself, where the others' operands are not made."""
+    x, wg, wu, gy = gated_inputs(rows, ff, 64, F16, seed=11)
+    sizes = 2.0 ** (-5.0 * (torch.arange(rows, device="cuda") % 5))
+    gy = (gy.float().clamp(-4, 4) * sizes[:, None]).half()
+    got = ops.gated_feed_forward_grad(x, wg, wu, gy, need=(need[0], need[1], need[1]))
+    for v, (want, bound), n in zip(got, gated_by_size(x, wg, wu, gy, "silu", sizes, 2 if rows <= 128 or ff <= 32 else 1), (need[0], need[1], need[1])):
+        assert n or v is None
+        if n:
+            near(v, want, bound, "gradient of the gated part")
+    h, w, t, gl, gs = loss_inputs(rows, ff, 64, F16, seed=12)
+    gl, gs = gl * sizes, gs * sizes
+    r = ops.linear_logprobs(h, w, t)
+    got = ops.linear_logprobs_grad(h, w, t, r, gl, gs, need=need)
+    for v, (want, bound), n in zip(got, loss_by_size(h, w, t, 1.0, gl, gs, sizes, 2 if rows <= 128 or ff <= 64 else 1), need):
+        assert n or v is None
+        if n:
+            near(v, want, bound, "gradient of the log probabilities")
